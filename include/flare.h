@@ -267,6 +267,63 @@ int flare_spectral_eig(int32_t matrices, int32_t M, float *G, float *eigenvalues
                        flare_stream_t stream);
 
 /*
+ * ---- Around a block.  (The paper's block is X += FLARE(LN(X)); these are the norms and the sum around the mixer, or around any
+ * other part of a block, and the update of its matrices.)
+ *
+ * A tensor here is `rows` rows (the tokens of all batch items) of `width` columns, row-major, the columns next to each other and rows
+ * `stride_*` elements apart (0: width), so that a slice of a wider projection is taken as it is.  Pointers are aligned to their element type;
+ * rows that all start on 16-byte boundaries and whose width is a multiple of 8 are moved 16 bytes at a time, others one element at a
+ * time.  Norm weights, biases and the residual scale are float32 [width]; a weight or scale that is NULL counts as ones, a bias as zeros.
+ *
+ *     N(v) = (v - mean(v)) rstd weight + bias,  rstd = 1 / sqrt(var(v) + eps)       FLARE_NORM_LAYER
+ *     N(v) = v rstd weight + bias,              rstd = 1 / sqrt(mean(v^2) + eps)    FLARE_NORM_RMS
+ *     flare_norm_*:  h = N_pre(x)
+ *     flare_join_*:  n = N_post(branch);  y = residual_scale x + scale act(gate) n;  h = N_pre(y)
+ *
+ * act: the identity (FLARE_GATE_LINEAR) or 1 / (1 + exp(-gate)) (FLARE_GATE_SIGMOID); FLARE_GATE_NONE: no factor.  gate_rows consecutive rows
+ * share one row of the gate ([rows / gate_rows, width]; 1: every row has its own).  FLARE_NORM_NONE leaves a norm out: n = branch; without
+ * N_pre there is no h (and no dh).  All sums and statistics are float32; h is formed from y before y is rounded to residual_dtype.
+ * stats [rows, 4] float32: mean and rstd of the branch, mean and rstd of what N_pre sees (0 where a norm is left out or has no mean);
+ * NULL if not wanted.  y may be x, dx may be dy, in place.
+ */
+enum { FLARE_NORM_NONE = 0, FLARE_NORM_LAYER = 1, FLARE_NORM_RMS = 2 };
+enum { FLARE_GATE_NONE = 0, FLARE_GATE_SIGMOID = 1, FLARE_GATE_LINEAR = 2 };
+typedef struct {
+    int64_t rows;           /* 0 is allowed: nothing is read, sums over rows are 0 */
+    int32_t width;          /* up to 16384 */
+    int32_t dtype;          /* of branch, gate, h and their gradients */
+    int32_t residual_dtype; /* of x, y, dy, dx: dtype, or float32 */
+    int32_t pre_norm, post_norm, gate;
+    int64_t gate_rows;
+    float pre_eps, post_eps, residual_scale;
+    int64_t stride_x, stride_branch, stride_gate, stride_y, stride_h, stride_dy, stride_dh, stride_dx, stride_dbranch, stride_dgate;
+} flare_block_desc_t;
+
+/* Bytes of workspace either backward needs (0 for an invalid descriptor): one row of partial sums per thread block. */
+size_t flare_block_workspace_bytes(const flare_block_desc_t *desc);
+
+/* The norm before the first block (pre_norm of the descriptor; post_norm, gate and residual_scale are not looked at). */
+int flare_norm_forward(const flare_block_desc_t *desc, const void *x, const float *weight, const float *bias, void *h, float *stats,
+                       flare_stream_t stream);
+/* Its backward: dx = dy + J^T dh (dy, the gradient that reaches x beside the norm, may be NULL); dweight = sum over rows of
+ * dh (x - mean) rstd, dbias = sum of dh (either NULL if not wanted).  stats: the forward's. */
+int flare_norm_backward(const flare_block_desc_t *desc, const void *x, const float *weight, const float *stats, const void *dy, const void *dh,
+                        void *dx, float *dweight, float *dbias, void *workspace, size_t workspace_bytes, flare_stream_t stream);
+
+/* The join after a block, with the norm before the next one. */
+int flare_join_forward(const flare_block_desc_t *desc, const void *x, const void *branch, const void *gate, const float *scale,
+                       const float *post_weight, const float *post_bias, const float *pre_weight, const float *pre_bias, void *y, void *h,
+                       float *stats, flare_stream_t stream);
+/* Its backward, from what the forward was given and its y and stats: with dt = dy + J_pre^T dh (dy may be NULL where there is a dh)
+ *     dx = residual_scale dt;  dbranch = J_post^T (scale act(gate) dt);  dgate = scale act'(gate) n dt, summed over the rows that share
+ *     a gate row;  dscale = sum over rows of act(gate) n dt;  weights and biases: sums over rows of what reaches N, times the normalised
+ *     input for the weights.  Row gradients that go with an input are required; sums over rows (dscale .. dpre_bias) may be NULL. */
+int flare_join_backward(const flare_block_desc_t *desc, const void *branch, const void *gate, const float *scale, const float *post_weight,
+                        const float *post_bias, const void *y, const float *pre_weight, const float *stats, const void *dy, const void *dh,
+                        void *dx, void *dbranch, void *dgate, float *dscale, float *dpost_weight, float *dpost_bias, float *dpre_weight,
+                        float *dpre_bias, void *workspace, size_t workspace_bytes, flare_stream_t stream);
+
+/*
  * Instruction-level measurements behind the kernels' design (the paper has no counterpart), so that the figures the
  * documentation quotes can be re-taken on the GPU at hand.  `which`:
  *   0, 1, 2   exponentials per clock per SM of the softmax loop as the sixteen softmax warps of a forward kernel run it

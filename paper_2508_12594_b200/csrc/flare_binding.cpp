@@ -6,14 +6,17 @@
 // forward of 1024 tokens 45 -> 17 us, training step of 16384 tokens 127 -> 61 us (its launches are most of that).
 //
 // The module does not link libflare: flare.py loads the library and hands over the addresses of its functions (bind).
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <ATen/ATen.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 
+#include <algorithm>
 #include <map>
 #include <string>
+#include <vector>
 
 #include "../../include/flare.h"
 
@@ -31,6 +34,11 @@ struct Library {
     decltype(&flare_backward_variant) backward_variant;
     decltype(&flare_spectral_gram) spectral_gram;
     decltype(&flare_spectral_eig) spectral_eig;
+    decltype(&flare_block_workspace_bytes) block_workspace_bytes;
+    decltype(&flare_norm_forward) norm_forward;
+    decltype(&flare_norm_backward) norm_backward;
+    decltype(&flare_join_forward) join_forward;
+    decltype(&flare_join_backward) join_backward;
 } lib{};
 PyObject *flare_error = nullptr;   // the exception class (status, where)
 
@@ -393,6 +401,235 @@ BINDING(spectral_eig, 5)
     check_status(unlocked([&] { return lib.spectral_eig((int32_t)matrices, (int32_t)M, g, ev, u, (int32_t)sweeps, st); }), "flare_spectral_eig");
 BINDING_END
 
+// ---- around a block: tensors [..., width] whose leading dimensions are rows at one distance
+
+int dtype_code(at::ScalarType t) {
+    switch (t) {
+        case at::kFloat: return FLARE_DTYPE_F32;
+        case at::kBFloat16: return FLARE_DTYPE_BF16;
+        case at::kHalf: return FLARE_DTYPE_F16;
+        default: fail(PyExc_TypeError, "unsupported dtype " + dtype_name(t));
+    }
+}
+struct Rows {
+    void *p = nullptr;
+    int64_t stride = 0;
+};
+Rows rows_of(const at::Tensor &t, at::ScalarType dtype, at::IntArrayRef shape, const char *name) {
+    if (!t.is_cuda()) fail(PyExc_ValueError, std::string(name) + ": expected a CUDA tensor");
+    if (t.scalar_type() != dtype) fail(PyExc_TypeError, std::string(name) + ": expected " + dtype_name(dtype) + ", got " + dtype_name(t.scalar_type()));
+    if (t.sizes() != shape) fail(PyExc_ValueError, std::string(name) + ": expected shape " + shape_text(shape) + ", got " + shape_text(t.sizes()));
+    const int64_t n = t.dim(), C = t.size(n - 1);
+    if (t.numel() == 0) return Rows{t.data_ptr(), C};
+    int64_t stride = 0, rows = 1;                            // of the innermost leading dimension that has more than one entry
+    bool ok = C == 1 || t.stride(n - 1) == 1;
+    for (int64_t i = n - 2; i >= 0; --i) {
+        if (t.size(i) == 1) continue;
+        if (stride == 0) stride = t.stride(i);
+        else ok = ok && t.stride(i) == stride * rows;
+        rows *= t.size(i);
+    }
+    if (stride == 0) stride = C;
+    if (!ok || stride < C) fail(PyExc_ValueError, std::string(name) + ": expected rows of adjacent columns at one distance from each other");
+    return Rows{t.data_ptr(), stride};
+}
+float *row_param(PyObject *o, int64_t C, const char *name) {
+    if (o == Py_None) return nullptr;
+    const at::Tensor &t = tensor(o);
+    if (!t.is_cuda() || !t.is_contiguous()) fail(PyExc_ValueError, std::string(name) + ": expected a contiguous CUDA tensor");
+    if (t.scalar_type() != at::kFloat) fail(PyExc_TypeError, std::string(name) + ": expected torch.float32, got " + dtype_name(t.scalar_type()));
+    if (t.dim() != 1 || t.size(0) != C) fail(PyExc_ValueError, std::string(name) + ": expected shape (" + std::to_string(C) + ",), got " + shape_text(t.sizes()));
+    return (float *)t.data_ptr();
+}
+int number_of(PyObject *o) {
+    const long x = PyLong_AsLong(o);
+    if (x == -1 && PyErr_Occurred()) throw PythonError{};
+    return (int)x;
+}
+// Entry i of a tuple of output tensors (or None: allocate).
+at::Tensor output(PyObject *out, Py_ssize_t i, at::IntArrayRef shape, const at::TensorOptions &options) {
+    if (out != Py_None) {
+        if (!PyTuple_Check(out) || i >= PyTuple_GET_SIZE(out)) fail(PyExc_ValueError, "out: expected a tuple with a tensor, or None, for every result");
+        PyObject *o = PyTuple_GET_ITEM(out, i);
+        if (o != Py_None) return tensor(o);
+    }
+    return at::empty(shape, options);
+}
+PyObject *wrap(const at::Tensor &t) {
+    if (!t.defined()) Py_RETURN_NONE;
+    return THPVariable_Wrap(t);
+}
+PyObject *wrap_all(std::initializer_list<at::Tensor> ts) {
+    PyObject *r = PyTuple_New((Py_ssize_t)ts.size());
+    if (!r) throw PythonError{};
+    Py_ssize_t i = 0;
+    for (const at::Tensor &t : ts) PyTuple_SET_ITEM(r, i++, wrap(t));
+    return r;
+}
+
+// What a call says about its rows: shape, types and norms.
+struct Around {
+    flare_block_desc_t d{};
+    std::vector<int64_t> shape;
+    int64_t C = 0;
+    at::ScalarType dt, res;
+    at::TensorOptions options;
+    Around(const at::Tensor &stream_like, const at::Tensor &branch_like) : dt(branch_like.scalar_type()), res(stream_like.scalar_type()), options(stream_like.options()) {
+        init(stream_like.sizes());
+    }
+    Around(const at::Tensor &x, at::ScalarType h) : dt(h), res(x.scalar_type()), options(x.options()) { init(x.sizes()); }
+    void init(at::IntArrayRef s) {
+        if (s.size() < 1) fail(PyExc_ValueError, "expected tensors [..., width]");
+        shape = s.vec();
+        C = shape.back();
+        if (C < 1 || C > INT32_MAX) fail(PyExc_ValueError, "expected tensors [..., width], got shape " + shape_text(s));
+        d.rows = 1;
+        for (size_t i = 0; i + 1 < shape.size(); ++i) d.rows *= shape[i];
+        d.width = (int32_t)C;
+        d.dtype = dtype_code(dt);
+        d.residual_dtype = dtype_code(res);
+        d.residual_scale = 1.f;
+    }
+    Rows rows(PyObject *o, at::ScalarType t, int64_t &stride, const char *name) const {
+        if (o == Py_None) return Rows{};
+        const Rows r = rows_of(tensor(o), t, shape, name);
+        stride = r.stride;
+        return r;
+    }
+    Rows rows(const at::Tensor &o, int64_t &stride, const char *name, at::ScalarType t) const {
+        const Rows r = rows_of(o, t, shape, name);
+        stride = r.stride;
+        return r;
+    }
+    // the gate: one row per row, or, with fewer leading entries, per group of consecutive rows
+    std::vector<int64_t> gate_shape;
+    Rows gate(PyObject *o, int kind) {
+        d.gate = kind;
+        d.gate_rows = 1;
+        if ((o == Py_None) != (kind == FLARE_GATE_NONE)) fail(PyExc_ValueError, "gate: a tensor and its kind go together");
+        if (o == Py_None) return Rows{};
+        const at::Tensor &g = tensor(o);
+        gate_shape = g.sizes().vec();
+        int64_t n = 1;
+        for (size_t i = 0; i + 1 < gate_shape.size(); ++i) n *= gate_shape[i];
+        const bool leads = !gate_shape.empty() && gate_shape.back() == C && gate_shape.size() <= shape.size() &&
+                           std::equal(gate_shape.begin(), gate_shape.end() - 1, shape.begin());
+        if (!leads || (n == 0) != (d.rows == 0)) fail(PyExc_ValueError, "gate: expected [..., width] with the leading dimensions of the branch, or the first of them, got shape " + shape_text(gate_shape));
+        if (n > 0) d.gate_rows = d.rows / n;
+        const Rows r = rows_of(g, dt, gate_shape, "gate");
+        d.stride_gate = r.stride;
+        return r;
+    }
+    float *stats(const at::Tensor &t) const {
+        check(t, at::kFloat, {d.rows, 4});
+        return (float *)t.data_ptr();
+    }
+    at::TensorOptions as(at::ScalarType t) const { return options.dtype(t); }
+};
+
+// x, kind, weight, bias, eps, dtype-carrying tensor or None, out (h, stats) or None, stream -> (h, stats)
+BINDING(block_norm, 8)
+    const at::Tensor &x = tensor(a[0]);
+    Around c(x, a[5] == Py_None ? x.scalar_type() : ((THPDtype *)a[5])->scalar_type);
+    c.d.pre_norm = number_of(a[1]);
+    c.d.pre_eps = (float)number(a[4]);
+    const float *w = row_param(a[2], c.C, "weight"), *b = row_param(a[3], c.C, "bias");
+    const Rows rx = c.rows(x, c.d.stride_x, "x", c.res);
+    const at::Tensor h = output(a[6], 0, c.shape, c.as(c.dt)), stats = output(a[6], 1, {c.d.rows, 4}, c.as(at::kFloat));
+    const Rows rh = c.rows(h, c.d.stride_h, "h", c.dt);
+    float *ps = c.stats(stats);
+    flare_stream_t st = stream_of(a[7]);
+    check_status(unlocked([&] { return lib.norm_forward(&c.d, rx.p, w, b, rh.p, ps, st); }), "flare_norm_forward");
+    return wrap_all({h, stats});
+BINDING_END
+
+// x, stats, dh, dy, kind, weight, bias, eps, out (dx, dweight, dbias) or None, stream -> (dx, dweight, dbias)
+BINDING(block_norm_backward, 10)
+    const at::Tensor &x = tensor(a[0]), &dh = tensor(a[2]);
+    Around c(x, dh);
+    c.d.pre_norm = number_of(a[4]);
+    c.d.pre_eps = (float)number(a[7]);
+    const float *w = row_param(a[5], c.C, "weight");
+    const float *b = row_param(a[6], c.C, "bias");
+    const Rows rx = c.rows(x, c.d.stride_x, "x", c.res), rdh = c.rows(dh, c.d.stride_dh, "dh", c.dt), rdy = c.rows(a[3], c.res, c.d.stride_dy, "dy");
+    const float *ps = c.stats(tensor(a[1]));
+    const at::Tensor dx = output(a[8], 0, c.shape, c.as(c.res));
+    const at::Tensor dw = w ? output(a[8], 1, {c.C}, c.as(at::kFloat)) : at::Tensor(), db = b ? output(a[8], 2, {c.C}, c.as(at::kFloat)) : at::Tensor();
+    const Rows rdx = c.rows(dx, c.d.stride_dx, "dx", c.res);
+    flare_stream_t st = stream_of(a[9]);
+    const size_t need = lib.block_workspace_bytes(&c.d);
+    if (need == 0) check_status(FLARE_ERR_UNSUPPORTED, "flare_norm_backward");
+    const at::Tensor ws = scratch(need, x, a[9], st);
+    auto p = [&](const at::Tensor &t, const char *name) -> float * {
+        if (!t.defined()) return nullptr;
+        check(t, at::kFloat, {c.C});
+        return (float *)t.data_ptr();
+    };
+    float *pw = p(dw, "dweight"), *pb = p(db, "dbias");
+    check_status(unlocked([&] { return lib.norm_backward(&c.d, rx.p, w, ps, rdy.p, rdh.p, rdx.p, pw, pb, ws.data_ptr(), need, st); }), "flare_norm_backward");
+    return wrap_all({dx, dw, db});
+BINDING_END
+
+// x, branch, post (kind, weight, bias, eps), pre (the same), gate, gate kind, scale, residual scale, out (y, h, stats) or None, stream -> (y, h, stats)
+BINDING(block_join, 16)
+    const at::Tensor &x = tensor(a[0]), &o = tensor(a[1]);
+    Around c(x, o);
+    c.d.post_norm = number_of(a[2]); c.d.post_eps = (float)number(a[5]);
+    c.d.pre_norm = number_of(a[6]); c.d.pre_eps = (float)number(a[9]);
+    c.d.residual_scale = (float)number(a[13]);
+    const float *wo = row_param(a[3], c.C, "post weight"), *bo = row_param(a[4], c.C, "post bias"), *wy = row_param(a[7], c.C, "pre weight"),
+                *by = row_param(a[8], c.C, "pre bias"), *s = row_param(a[12], c.C, "scale");
+    const Rows rx = c.rows(x, c.d.stride_x, "x", c.res), ro = c.rows(o, c.d.stride_branch, "branch", c.dt), rg = c.gate(a[10], number_of(a[11]));
+    const bool pre = c.d.pre_norm != FLARE_NORM_NONE;
+    const at::Tensor y = output(a[14], 0, c.shape, c.as(c.res)), h = pre ? output(a[14], 1, c.shape, c.as(c.dt)) : at::Tensor(),
+                     stats = output(a[14], 2, {c.d.rows, 4}, c.as(at::kFloat));
+    const Rows ry = c.rows(y, c.d.stride_y, "y", c.res), rh = pre ? c.rows(h, c.d.stride_h, "h", c.dt) : Rows{};
+    float *ps = c.stats(stats);
+    flare_stream_t st = stream_of(a[15]);
+    check_status(unlocked([&] { return lib.join_forward(&c.d, rx.p, ro.p, rg.p, s, wo, bo, wy, by, ry.p, rh.p, ps, st); }), "flare_join_forward");
+    return wrap_all({y, h, stats});
+BINDING_END
+
+// branch, y, stats, dy, dh, post (kind, weight, bias, eps), pre (the same), gate, gate kind, scale, residual scale, out or None, stream
+// -> (dx, dbranch, dgate, dscale, dpost_weight, dpost_bias, dpre_weight, dpre_bias)
+BINDING(block_join_backward, 19)
+    const at::Tensor &o = tensor(a[0]), &y = tensor(a[1]);
+    Around c(y, o);
+    c.d.post_norm = number_of(a[5]); c.d.post_eps = (float)number(a[8]);
+    c.d.pre_norm = number_of(a[9]); c.d.pre_eps = (float)number(a[12]);
+    c.d.residual_scale = (float)number(a[16]);
+    const float *wo = row_param(a[6], c.C, "post weight"), *bo = row_param(a[7], c.C, "post bias"), *wy = row_param(a[10], c.C, "pre weight"),
+                *by = row_param(a[11], c.C, "pre bias"), *s = row_param(a[15], c.C, "scale");
+    const Rows ro = c.rows(o, c.d.stride_branch, "branch", c.dt), ry = c.rows(y, c.d.stride_x, "y", c.res), rdy = c.rows(a[3], c.res, c.d.stride_dy, "dy"),
+               rdh = c.rows(a[4], c.dt, c.d.stride_dh, "dh"), rg = c.gate(a[13], number_of(a[14]));
+    const float *ps = c.stats(tensor(a[2]));
+    const auto f32 = c.as(at::kFloat);
+    PyObject *out = a[17];
+    const at::Tensor dx = output(out, 0, c.shape, c.as(c.res)), d_o = output(out, 1, c.shape, c.as(c.dt));
+    const at::Tensor dg = rg.p || a[13] != Py_None ? output(out, 2, c.gate_shape, c.as(c.dt)) : at::Tensor();
+    auto sums = [&](const float *present, Py_ssize_t i) { return present ? output(out, i, {c.C}, f32) : at::Tensor(); };
+    const at::Tensor ds = sums(s, 3), dwo = sums(wo, 4), dbo = sums(bo, 5), dwy = sums(wy, 6), dby = sums(by, 7);
+    const Rows rdx = c.rows(dx, c.d.stride_dx, "dx", c.res), rdo = c.rows(d_o, c.d.stride_dbranch, "dbranch", c.dt);
+    Rows rdg;
+    if (dg.defined()) {
+        rdg = rows_of(dg, c.dt, c.gate_shape, "dgate");
+        c.d.stride_dgate = rdg.stride;
+    }
+    auto p = [&](const at::Tensor &t) -> float * {
+        if (!t.defined()) return nullptr;
+        check(t, at::kFloat, {c.C});
+        return (float *)t.data_ptr();
+    };
+    float *p3 = p(ds), *p4 = p(dwo), *p5 = p(dbo), *p6 = p(dwy), *p7 = p(dby);
+    flare_stream_t st = stream_of(a[18]);
+    const size_t need = lib.block_workspace_bytes(&c.d);
+    if (need == 0) check_status(FLARE_ERR_UNSUPPORTED, "flare_join_backward");
+    const at::Tensor ws = scratch(need, y, a[18], st);
+    check_status(unlocked([&] { return lib.join_backward(&c.d, ro.p, rg.p, s, wo, bo, ry.p, wy, ps, rdy.p, rdh.p, rdx.p, rdo.p, rdg.p, p3, p4, p5, p6, p7,
+                                                         ws.data_ptr(), need, st); }), "flare_join_backward");
+    return wrap_all({dx, d_o, dg, ds, dwo, dbo, dwy, dby});
+BINDING_END
+
 // bind(addresses: dict name -> int, FlareError)
 BINDING(bind, 2)
     auto get = [&](const char *name, auto &slot) {
@@ -411,6 +648,11 @@ BINDING(bind, 2)
     get("flare_backward_variant", lib.backward_variant);
     get("flare_spectral_gram", lib.spectral_gram);
     get("flare_spectral_eig", lib.spectral_eig);
+    get("flare_block_workspace_bytes", lib.block_workspace_bytes);
+    get("flare_norm_forward", lib.norm_forward);
+    get("flare_norm_backward", lib.norm_backward);
+    get("flare_join_forward", lib.join_forward);
+    get("flare_join_backward", lib.join_backward);
     Py_INCREF(a[1]);
     flare_error = a[1];
 BINDING_END
@@ -418,7 +660,8 @@ BINDING_END
 #define METHOD(name) {#name, (PyCFunction)(void (*)(void))py_##name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METHOD(bind), METHOD(encode), METHOD(encode_static_scratch), METHOD(decode), METHOD(forward), METHOD(backward),
                          METHOD(forward_host), METHOD(forward_variant), METHOD(backward_variant), METHOD(spectral_gram), METHOD(spectral_eig),
-                         METHOD(call_forward), METHOD(call_forward_backward), {nullptr, nullptr, 0, nullptr}};
+                         METHOD(call_forward), METHOD(call_forward_backward), METHOD(block_norm), METHOD(block_norm_backward), METHOD(block_join),
+                         METHOD(block_join_backward), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_binding", "Argument marshalling for libflare.", -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

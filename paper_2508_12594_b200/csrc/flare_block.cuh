@@ -1,0 +1,642 @@
+// Norms around a block: the norm before it, and the join after it (norm of the branch, gate, residual scale, sum with the
+// residual stream) with the norm before the next block, forward and backward.  Per row (token) of C columns, in float32:
+//
+//     n  = N_post(o),   y = alpha x + s act(g) n,   h = N_pre(y);      N(v) = (v - mean) rstd w + b,   rstd = 1/sqrt(var + eps)
+//
+// (rms norms: mean = 0, var = mean square).  Without a branch y = x.  Backward, with u^ the normalised u:
+//
+//     dt = dy + J_pre^T dh,  dx = alpha dt,  q = act(g) dt,  do = J_post^T (s q),  dg = s act'(g) n dt,
+//     J^T d = rstd (d w - mean(d w) - u^ mean(d w u^))                 (rms: without the mean(d w) term)
+//     P = sum over rows of q, Q = sum of q o^:   db_post = s P,  dw_post = s Q,  ds = w_post Q + b_post P.
+//
+// Two sums over rows serve three gradients, and where consecutive rows share a gate row (a group) they are taken of dt
+// per group: dg = s act'(g) (w_post Q + b_post P) of the group, and P, Q the sums over groups of act(g) times theirs.
+//
+// Everything is bound by memory (bfloat16 with a gate: 10 bytes an element forward, 16 backward), so each element is read
+// once: a thread owns 8 columns of a row, a row is held by the next power of two of C / 8 threads (up to 512 of a block, wider
+// rows by the blocks of a cluster, whose sums meet through distributed shared memory), and the loads of the rows to come are
+// in flight in shared memory (cp.async into slots that only the thread itself reads: no barriers).
+// Sums over rows stay in the registers of the thread that owns the columns; each block leaves one partial row of them.
+#pragma once
+
+#include "flare_common.cuh"
+#include "flare_ptx.cuh"
+
+namespace flare {
+
+constexpr float kBlockLog2e = 1.4426950408889634f;
+
+struct BlockArgs {
+    const void *x, *o, *g, *dy, *dh;                     // x: what the next norm sees (forward: x; backward: y)
+    void *y, *h, *dx, *d_o, *dg;
+    const float *scale, *w_post, *b_post, *w_pre, *b_pre;
+    float4 *stats;                                        // per row: mean and rstd of the branch, mean and rstd of y
+    float *part;                                          // partial sums over rows [chunks][sums][C]
+    long ld_x, ld_o, ld_g, ld_y, ld_h, ld_dy, ld_dh, ld_dx, ld_do, ld_dg;
+    long rows, group;                                     // group: rows that share a gate row (all rows where none is shared)
+    long chunk;                                           // rows of a block's piece of a group
+    int chunks;                                           // pieces per group
+    int C, tpr, cluster;                                  // columns, threads of a row in a block (a power of two), blocks of a row
+    int has_post, has_pre, layer_post, layer_pre;
+    int gate;                                             // 0 none, 1 sigmoid, 2 linear
+    int grouped;                                          // gate rows are shared
+    float eps_post, eps_pre, alpha, inv_c;
+};
+
+// ---------------------------------------------------------------- eight columns
+// Pairs of floats: one instruction for two columns.
+__device__ __forceinline__ float2 f2(float x) { return make_float2(x, x); }
+__device__ __forceinline__ float2 f2_fma(float2 a, float2 b, float2 c) { return __ffma2_rn(a, b, c); }
+__device__ __forceinline__ float2 f2_mul(float2 a, float2 b) { return __fmul2_rn(a, b); }
+__device__ __forceinline__ float2 f2_add(float2 a, float2 b) { return __fadd2_rn(a, b); }
+
+template <typename E> struct Raw8 { uint4 q[sizeof(E) / 2]; };
+
+__device__ __forceinline__ float2 pair_of(uint32_t v, __nv_bfloat16) { return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u)); }
+__device__ __forceinline__ float2 pair_of(uint32_t v, __half) { return __half22float2(*reinterpret_cast<const __half2 *>(&v)); }
+__device__ __forceinline__ uint32_t pair_to(float2 v, __nv_bfloat16) { return ptx::pack_bf16(v); }
+__device__ __forceinline__ uint32_t pair_to(float2 v, __half) {
+    const __half2 h = __float22half2_rn(v);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+template <typename E>
+__device__ __forceinline__ void unpack8(const Raw8<E> &r, float2 (&f)[4]) {
+    if constexpr (sizeof(E) == 4) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            f[2 * i] = make_float2(__uint_as_float(r.q[i].x), __uint_as_float(r.q[i].y));
+            f[2 * i + 1] = make_float2(__uint_as_float(r.q[i].z), __uint_as_float(r.q[i].w));
+        }
+    } else {
+        f[0] = pair_of(r.q[0].x, E{}); f[1] = pair_of(r.q[0].y, E{});
+        f[2] = pair_of(r.q[0].z, E{}); f[3] = pair_of(r.q[0].w, E{});
+    }
+}
+template <typename E>
+__device__ __forceinline__ Raw8<E> pack8(const float2 (&f)[4]) {
+    Raw8<E> r;
+    if constexpr (sizeof(E) == 4) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            r.q[i] = make_uint4(__float_as_uint(f[2 * i].x), __float_as_uint(f[2 * i].y), __float_as_uint(f[2 * i + 1].x), __float_as_uint(f[2 * i + 1].y));
+    } else {
+        r.q[0] = make_uint4(pair_to(f[0], E{}), pair_to(f[1], E{}), pair_to(f[2], E{}), pair_to(f[3], E{}));
+    }
+    return r;
+}
+
+// Which columns a thread owns.  kAligned: eight next to each other, moved 16 bytes at a time (C a multiple of 8, rows on 16-byte boundaries);
+// otherwise every tpr-th, one at a time, neighbouring threads next to each other.
+template <bool kAligned>
+struct Columns {
+    int first, step, C;
+    __device__ __forceinline__ Columns(int lane, int tpr, int C_, int base = 0) : first(base + (kAligned ? 8 * lane : lane)), step(kAligned ? 1 : tpr), C(C_) {}
+    __device__ __forceinline__ int at(int j) const { return first + j * step; }
+    __device__ __forceinline__ bool has(int j) const { return kAligned ? first < C : at(j) < C; }
+    __device__ __forceinline__ bool any() const { return first < C; }
+};
+// (live: otherwise zeros, and nothing is read)
+template <typename E, bool kAligned>
+__device__ __forceinline__ Raw8<E> load8(const E *row, const Columns<kAligned> &c, bool live = true) {
+    Raw8<E> r;
+    if constexpr (kAligned) {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(E) / 2; ++i) r.q[i] = live && c.any() ? reinterpret_cast<const uint4 *>(row + c.first)[i] : make_uint4(0, 0, 0, 0);
+    } else {
+        float2 f[4];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) (&f[j / 2].x)[j & 1] = live && c.has(j) ? to_f32(row[c.at(j)]) : 0.f;
+        r = pack8<E>(f);
+    }
+    return r;
+}
+template <typename E, bool kAligned>
+__device__ __forceinline__ void store8(E *row, const Columns<kAligned> &c, const float2 (&f)[4]) {
+    if constexpr (kAligned) {
+        const Raw8<E> r = pack8<E>(f);
+        if (c.any()) {
+#pragma unroll
+            for (int i = 0; i < (int)sizeof(E) / 2; ++i) reinterpret_cast<uint4 *>(row + c.first)[i] = r.q[i];
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (c.has(j)) from_f32(row[c.at(j)], (&f[j / 2].x)[j & 1]);
+    }
+}
+// A parameter's eight values; `none` where it is absent, 0 beyond the last column.
+template <bool kAligned>
+__device__ __forceinline__ void load_param(const float *p, float none, const Columns<kAligned> &c, float2 (&f)[4]) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) (&f[j / 2].x)[j & 1] = !c.has(j) ? 0.f : p ? p[c.at(j)] : none;
+}
+
+// ---------------------------------------------------------------- sums over the threads of a row
+struct RowShared {
+    float4 warp[2][16];         // what the warps of a row leave for one another, two buffers in turn: one barrier a sum
+    float4 block[2][8];         // what the blocks of a cluster do
+};
+struct RowGroup {
+    int tpr, warps, first;      // threads and warps of a row in the block, the row's first warp
+    int warp;                   // this thread's warp
+    int cluster;                // blocks of a row
+    int turn;
+    RowShared *sh;
+    __device__ __forceinline__ RowGroup(int tpr_, int cluster_, RowShared *sh_) : tpr(tpr_), cluster(cluster_), turn(0), sh(sh_) {
+        warp = threadIdx.x >> 5;
+        warps = tpr > 32 ? tpr >> 5 : 1;
+        first = warp / warps * warps;
+        if (cluster > 1) meet();                             // (the other blocks' shared memory is there from here on)
+    }
+    __device__ __forceinline__ void meet() const {
+        asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    }
+    __device__ __forceinline__ float within_warp(float v) const {
+        for (int o = min(tpr, 32) >> 1; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+        return v;
+    }
+    // v of every warp of the row in this block: where the row's first one's is.  All threads of the block call it.
+    __device__ __forceinline__ const float4 *of_warps(float4 v) {
+        if ((threadIdx.x & 31) == 0) sh->warp[turn][warp] = v;
+        __syncthreads();
+        return sh->warp[turn] + first;
+    }
+    // v (the same in all threads of a block) of every block of the row.  All threads of the cluster call it.
+    __device__ __forceinline__ const float4 *of_blocks(float4 v) {
+        if ((int)threadIdx.x < cluster) {
+            uint32_t to;
+            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(ptx::smem_u32(&sh->block[turn][blockIdx.y])), "r"(threadIdx.x));
+            asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(to), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
+        }
+        meet();
+        return sh->block[turn];
+    }
+    // Sums of a and b over the row.  All threads of the block (and its cluster) call it.
+    __device__ __forceinline__ float2 sum2(float a, float b) {
+        a = within_warp(a); b = within_warp(b);
+        if (tpr > 32) {
+            const float4 *r = of_warps(make_float4(a, b, 0.f, 0.f));
+            a = b = 0.f;
+            for (int w = 0; w < warps; ++w) {
+                const float2 v = *reinterpret_cast<const float2 *>(r + w);
+                a += v.x; b += v.y;
+            }
+            if (cluster > 1) {
+                r = of_blocks(make_float4(a, b, 0.f, 0.f));
+                a = b = 0.f;
+                for (int w = 0; w < cluster; ++w) {
+                    a += r[w].x; b += r[w].y;
+                }
+            }
+            turn ^= 1;
+        }
+        return make_float2(a, b);
+    }
+    // (sum, squares of distances from the own mean, own mean, count) of n parts -> the same of their union
+    __device__ __forceinline__ static float4 join_parts(const float4 *r, int n) {
+        float sum = 0.f, count = 0.f, m2 = 0.f;
+        for (int w = 0; w < n; ++w) { sum += r[w].x; count += r[w].w; }
+        const float mean = count > 0.f ? sum / count : 0.f;
+        for (int w = 0; w < n; ++w) {
+            const float d = r[w].z - mean;
+            m2 += fmaf(r[w].w * d, d, r[w].y);
+        }
+        return make_float4(sum, m2, mean, count);
+    }
+};
+
+// Mean and 1/sqrt(var + eps) of a row.  layer: the squares are of distances from the mean, first the warp's, put together with those of the
+// row's other warps by the distances of their means (one barrier, and no small difference of large sums).  `mine`, `in_warp`: elements of
+// this thread and of its warp's part of the row.
+template <bool kAligned>
+__device__ __forceinline__ float2 moments(RowGroup &grp, const float2 (&v)[4], const Columns<kAligned> &c, float in_warp, int layer, float inv_c, float eps) {
+    if (!layer) {
+        float2 s = f2(0.f);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s = f2_fma(v[i], v[i], s);
+        const float sq = grp.sum2(s.x + s.y, 0.f).x;
+        return make_float2(0.f, rsqrtf(fmaf(sq, inv_c, eps)));
+    }
+    const float2 s01 = f2_add(f2_add(v[0], v[1]), f2_add(v[2], v[3]));
+    const float sum = grp.within_warp(s01.x + s01.y);
+    const float mean_w = in_warp > 0.f ? sum / in_warp : 0.f;
+    float m2 = 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const float d = c.has(j) ? (&v[j / 2].x)[j & 1] - mean_w : 0.f;
+        m2 = fmaf(d, d, m2);
+    }
+    m2 = grp.within_warp(m2);
+    float4 part = make_float4(sum, m2, mean_w, in_warp);
+    if (grp.tpr > 32) {
+        part = RowGroup::join_parts(grp.of_warps(part), grp.warps);
+        if (grp.cluster > 1) part = RowGroup::join_parts(grp.of_blocks(part), grp.cluster);
+        grp.turn ^= 1;
+    }
+    return make_float2(part.z, rsqrtf(fmaf(part.y, inv_c, eps)));
+}
+
+__device__ __forceinline__ float gate_act(int kind, float g) { return kind == 1 ? __fdividef(1.f, 1.f + ptx::ex2(-kBlockLog2e * g)) : g; }
+
+// ---------------------------------------------------------------- loads ahead
+// Slots of kStages rows ahead in shared memory, [stage][16-byte piece][thread]: a thread copies into its own and reads only those.
+__device__ __forceinline__ void copy_async16(uint32_t dst, const void *src, bool yes) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(yes ? 16u : 0u) : "memory");
+}
+template <typename E, int kThreads>
+__device__ __forceinline__ void slot_copy(uint32_t slot, const E *row, int col, bool yes) {
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(E) / 2; ++i) copy_async16(slot + i * kThreads * 16, reinterpret_cast<const uint4 *>(row + col) + i, yes);
+}
+template <typename E, int kThreads>
+__device__ __forceinline__ Raw8<E> slot_read(uint32_t slot) {
+    Raw8<E> r;
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(E) / 2; ++i)
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r.q[i].x), "=r"(r.q[i].y), "=r"(r.q[i].z), "=r"(r.q[i].w) : "r"(slot + i * kThreads * 16) : "memory");
+    return r;
+}
+
+template <typename T, typename R, bool kBranch> __host__ __device__ constexpr int fwd_pieces() { return (int)(sizeof(R) / 2 + (kBranch ? 2 * (sizeof(T) / 2) : 0)); }
+template <typename T, typename R, bool kBranch> __host__ __device__ constexpr int bwd_pieces() { return (int)(2 * (sizeof(R) / 2) + (sizeof(T) / 2) * (kBranch ? 3 : 1)); }
+__host__ __device__ constexpr int stages_for(int pieces) { return pieces <= 3 ? 4 : pieces <= 7 ? 3 : 2; }
+
+// The rows of one block: a piece of one group of rows.
+struct Piece {
+    long begin, end, group;
+    __device__ __forceinline__ Piece(const BlockArgs &p) {
+        group = blockIdx.x / p.chunks;
+        begin = group * p.group + (blockIdx.x - group * p.chunks) * p.chunk;
+        end = min(begin + p.chunk, min((group + 1) * p.group, p.rows));
+    }
+};
+
+// ---------------------------------------------------------------- forward
+template <typename T, typename R, bool kAligned, bool kBranch, int kThreads>
+__global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 2) block_forward_kernel(BlockArgs p) {
+    extern __shared__ __align__(16) uint8_t smem[];
+    __shared__ RowShared row_shared;
+    constexpr int kPieces = fwd_pieces<T, R, kBranch>(), kStages = stages_for(kPieces);
+    constexpr uint32_t kX = 0, kO = sizeof(R) / 2 * kThreads * 16, kG = kO + sizeof(T) / 2 * kThreads * 16, kStage = kPieces * kThreads * 16;
+    const int lane = threadIdx.x & (p.tpr - 1), per_turn = kThreads / p.tpr, mine = threadIdx.x / p.tpr;
+    const Columns<kAligned> c(lane, p.tpr, p.C, blockIdx.y * 8 * kThreads);
+    RowGroup grp(p.tpr, p.cluster, &row_shared);
+    const Piece piece(p);
+    const bool gate_row = kBranch && p.gate && !p.grouped;
+    int mine_n = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) mine_n += c.has(j) ? 1 : 0;
+    const float in_warp = grp.within_warp((float)mine_n);
+    ptx::grid_launch();
+    ptx::grid_wait();
+
+    float2 sw[4], sb[4], w[4], b[4];
+    if constexpr (kBranch) {
+        float2 s[4];
+        load_param(p.scale, 1.f, c, s);
+        load_param(p.w_post, 1.f, c, sw);
+        load_param(p.b_post, 0.f, c, sb);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { sw[i] = f2_mul(sw[i], s[i]); sb[i] = f2_mul(sb[i], s[i]); }
+    }
+    load_param(p.w_pre, 1.f, c, w);
+    load_param(p.b_pre, 0.f, c, b);
+    float2 a[4] = {f2(1.f), f2(1.f), f2(1.f), f2(1.f)};
+    if constexpr (kBranch) {
+        if (p.gate && p.grouped) {
+            unpack8(load8(static_cast<const T *>(p.g) + piece.group * p.ld_g, c), a);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) a[i] = make_float2(gate_act(p.gate, a[i].x), gate_act(p.gate, a[i].y));
+        }
+    }
+
+    const uint32_t slots = ptx::smem_u32(smem) + threadIdx.x * 16;
+    auto fetch = [&](long row, int stage) {
+        if constexpr (kAligned) {
+            const bool yes = row < piece.end && c.any();
+            const long r = yes ? row : piece.begin;
+            const int col = yes ? c.first : 0;
+            const uint32_t s = slots + stage * kStage;
+            slot_copy<R, kThreads>(s + kX, static_cast<const R *>(p.x) + r * p.ld_x, col, yes);
+            if constexpr (kBranch) {
+                slot_copy<T, kThreads>(s + kO, static_cast<const T *>(p.o) + r * p.ld_o, col, yes);
+                if (gate_row) slot_copy<T, kThreads>(s + kG, static_cast<const T *>(p.g) + r * p.ld_g, col, yes);
+            }
+            ptx::copy_async_commit();
+        }
+    };
+    if constexpr (kAligned)
+        for (int k = 0; k < kStages - 1; ++k) fetch(piece.begin + (long)k * per_turn + mine, k);
+
+    int stage = 0;
+    for (long r0 = piece.begin; r0 < piece.end; r0 += per_turn) {
+        const long row = r0 + mine;
+        const bool live = row < piece.end;
+        float2 y[4];
+        if constexpr (kAligned) {
+            fetch(row + (long)(kStages - 1) * per_turn, stage == 0 ? kStages - 1 : stage - 1);
+            ptx::copy_async_wait<kStages - 1>();
+            unpack8(slot_read<R, kThreads>(slots + stage * kStage + kX), y);
+        } else {
+            unpack8(load8(static_cast<const R *>(p.x) + row * p.ld_x, c, live), y);
+        }
+        float2 st_o = make_float2(0.f, 0.f);
+        if constexpr (kBranch) {
+            float2 o[4];
+            if constexpr (kAligned) {
+                unpack8(slot_read<T, kThreads>(slots + stage * kStage + kO), o);
+                if (gate_row) unpack8(slot_read<T, kThreads>(slots + stage * kStage + kG), a);
+            } else {
+                unpack8(load8(static_cast<const T *>(p.o) + row * p.ld_o, c, live), o);
+                if (gate_row) unpack8(load8(static_cast<const T *>(p.g) + row * p.ld_g, c, live), a);
+            }
+            if (gate_row) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) a[i] = make_float2(gate_act(p.gate, a[i].x), gate_act(p.gate, a[i].y));
+            }
+            if (p.has_post) {
+                st_o = moments(grp, o, c, in_warp, p.layer_post, p.inv_c, p.eps_post);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[i] = f2_mul(f2_add(o[i], f2(-st_o.x)), f2(st_o.y));
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[i] = f2_fma(f2_fma(o[i], sw[i], sb[i]), a[i], f2_mul(y[i], f2(p.alpha)));
+            if (live) store8(static_cast<R *>(p.y) + row * p.ld_y, c, y);
+        }
+        float2 st_y = make_float2(0.f, 0.f);
+        if (p.has_pre) {
+            st_y = moments(grp, y, c, in_warp, p.layer_pre, p.inv_c, p.eps_pre);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[i] = f2_fma(f2_mul(f2_add(y[i], f2(-st_y.x)), f2(st_y.y)), w[i], b[i]);
+            if (live) store8(static_cast<T *>(p.h) + row * p.ld_h, c, y);
+        }
+        if (live && lane == 0 && blockIdx.y == 0 && p.stats) p.stats[row] = make_float4(st_o.x, st_o.y, st_y.x, st_y.y);
+        stage = stage + 1 == kStages ? 0 : stage + 1;
+    }
+}
+
+// ---------------------------------------------------------------- backward
+// Sums over rows: [0] dh y^, [1] Q, [2] dh, [3] P; without biases the first two, without a branch [0] and [2].
+template <bool kBranch, bool kBias> __host__ __device__ constexpr int bwd_sums() { return (kBranch ? 2 : 1) * (kBias ? 2 : 1); }
+
+template <typename T, typename R, bool kAligned, bool kBranch, bool kBias, int kThreads>
+__global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 2) block_backward_kernel(BlockArgs p) {
+    extern __shared__ __align__(16) uint8_t smem[];
+    __shared__ RowShared row_shared;
+    constexpr int kPieces = bwd_pieces<T, R, kBranch>(), kStages = stages_for(kPieces), kSums = bwd_sums<kBranch, kBias>();
+    constexpr uint32_t kOneR = sizeof(R) / 2 * kThreads * 16, kOneT = sizeof(T) / 2 * kThreads * 16;
+    constexpr uint32_t kY = 0, kDy = kOneR, kDh = 2 * kOneR, kO = kDh + kOneT, kG = kO + kOneT, kStage = kPieces * kThreads * 16;
+    const int lane = threadIdx.x & (p.tpr - 1), per_turn = kThreads / p.tpr, mine = threadIdx.x / p.tpr;
+    const Columns<kAligned> c(lane, p.tpr, p.C, blockIdx.y * 8 * kThreads);
+    RowGroup grp(p.tpr, p.cluster, &row_shared);
+    const Piece piece(p);
+    const bool gate_row = kBranch && p.gate && !p.grouped;
+    ptx::grid_launch();
+    ptx::grid_wait();
+
+    float2 sw[4], sb[4], w[4];
+    if constexpr (kBranch) {
+        float2 s[4];
+        load_param(p.scale, 1.f, c, s);
+        load_param(p.w_post, 1.f, c, sw);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sw[i] = f2_mul(sw[i], s[i]);
+        if constexpr (kBias) {
+            load_param(p.b_post, 0.f, c, sb);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sb[i] = f2_mul(sb[i], s[i]);
+        }
+    }
+    load_param(p.w_pre, 1.f, c, w);
+    float2 a[4] = {f2(1.f), f2(1.f), f2(1.f), f2(1.f)};
+    if constexpr (kBranch) {
+        if (p.gate && p.grouped) {
+            unpack8(load8(static_cast<const T *>(p.g) + piece.group * p.ld_g, c), a);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) a[i] = make_float2(gate_act(p.gate, a[i].x), gate_act(p.gate, a[i].y));
+        }
+    }
+    float2 sum[kSums][4];
+#pragma unroll
+    for (int k = 0; k < kSums; ++k)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum[k][i] = f2(0.f);
+
+    const uint32_t slots = ptx::smem_u32(smem) + threadIdx.x * 16;
+    auto fetch = [&](long row, int stage) {
+        if constexpr (kAligned) {
+            const bool yes = row < piece.end && c.any();
+            const long r = yes ? row : piece.begin;
+            const int col = yes ? c.first : 0;
+            const uint32_t s = slots + stage * kStage;
+            if (p.has_pre) {
+                slot_copy<R, kThreads>(s + kY, static_cast<const R *>(p.x) + r * p.ld_x, col, yes);
+                slot_copy<T, kThreads>(s + kDh, static_cast<const T *>(p.dh) + r * p.ld_dh, col, yes);
+            }
+            if (p.dy) slot_copy<R, kThreads>(s + kDy, static_cast<const R *>(p.dy) + r * p.ld_dy, col, yes);
+            if constexpr (kBranch) {
+                slot_copy<T, kThreads>(s + kO, static_cast<const T *>(p.o) + r * p.ld_o, col, yes);
+                if (gate_row) slot_copy<T, kThreads>(s + kG, static_cast<const T *>(p.g) + r * p.ld_g, col, yes);
+            }
+            ptx::copy_async_commit();
+        }
+    };
+    if constexpr (kAligned)
+        for (int k = 0; k < kStages - 1; ++k) fetch(piece.begin + (long)k * per_turn + mine, k);
+    const float4 none = make_float4(0.f, 0.f, 0.f, 0.f);
+    float4 st_next = piece.begin + mine < piece.end ? p.stats[piece.begin + mine] : none;
+
+    int stage = 0;
+    for (long r0 = piece.begin; r0 < piece.end; r0 += per_turn) {
+        const long row = r0 + mine;
+        const bool live = row < piece.end;
+        const float4 st = st_next;
+        if (row + per_turn < piece.end) st_next = p.stats[row + per_turn];
+        else st_next = none;
+        const uint32_t s0 = slots + stage * kStage;
+        if constexpr (kAligned) {
+            fetch(row + (long)(kStages - 1) * per_turn, stage == 0 ? kStages - 1 : stage - 1);
+            ptx::copy_async_wait<kStages - 1>();
+        }
+        float2 dt[4] = {f2(0.f), f2(0.f), f2(0.f), f2(0.f)};
+        if (p.dy) {
+            if constexpr (kAligned) unpack8(slot_read<R, kThreads>(s0 + kDy), dt);
+            else unpack8(load8(static_cast<const R *>(p.dy) + row * p.ld_dy, c, live), dt);
+        }
+        if (p.has_pre) {
+            float2 yh[4], t[4];
+            if constexpr (kAligned) {
+                unpack8(slot_read<R, kThreads>(s0 + kY), yh);
+                unpack8(slot_read<T, kThreads>(s0 + kDh), t);
+            } else {
+                unpack8(load8(static_cast<const R *>(p.x) + row * p.ld_x, c, live), yh);
+                unpack8(load8(static_cast<const T *>(p.dh) + row * p.ld_dh, c, live), t);
+            }
+            float2 c1 = f2(0.f), c2 = f2(0.f);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                yh[i] = f2_mul(f2_add(yh[i], f2(-st.z)), f2(st.w));
+                sum[0][i] = f2_fma(t[i], yh[i], sum[0][i]);
+                if constexpr (kBias) sum[kBranch ? 2 : 1][i] = f2_add(sum[kBranch ? 2 : 1][i], t[i]);
+                t[i] = f2_mul(t[i], w[i]);
+                c1 = f2_fma(t[i], yh[i], c1);
+                c2 = f2_add(c2, t[i]);
+            }
+            float2 means = grp.sum2(c1.x + c1.y, p.layer_pre ? c2.x + c2.y : 0.f);
+            means.x *= -p.inv_c; means.y *= -p.inv_c;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) dt[i] = f2_fma(f2_fma(yh[i], f2(means.x), f2_add(t[i], f2(means.y))), f2(st.w), dt[i]);
+        }
+        float2 dx[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) dx[i] = f2_mul(dt[i], f2(p.alpha));
+        if (live) store8(static_cast<R *>(p.dx) + row * p.ld_dx, c, dx);
+        if constexpr (kBranch) {
+            float2 o[4];
+            if constexpr (kAligned) {
+                unpack8(slot_read<T, kThreads>(s0 + kO), o);
+                if (gate_row) unpack8(slot_read<T, kThreads>(s0 + kG), a);
+            } else {
+                unpack8(load8(static_cast<const T *>(p.o) + row * p.ld_o, c, live), o);
+                if (gate_row) unpack8(load8(static_cast<const T *>(p.g) + row * p.ld_g, c, live), a);
+            }
+            if (p.has_post) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[i] = f2_mul(f2_add(o[i], f2(-st.x)), f2(st.y));
+            }
+            if (gate_row) {
+                float2 dg[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float2 n = f2_mul(o[i], sw[i]);
+                    if constexpr (kBias) n = f2_add(n, sb[i]);
+                    dg[i] = f2_mul(dt[i], n);
+                    if (p.gate == 1) {
+                        a[i] = make_float2(gate_act(1, a[i].x), gate_act(1, a[i].y));
+                        dg[i] = f2_mul(dg[i], f2_mul(a[i], f2_fma(a[i], f2(-1.f), f2(1.f))));
+                    }
+                }
+                if (live) store8(static_cast<T *>(p.dg) + row * p.ld_dg, c, dg);
+            }
+            float2 d1 = f2(0.f), d2 = f2(0.f), u[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float2 q = f2_mul(dt[i], a[i]), k = p.grouped ? dt[i] : q;
+                sum[1][i] = f2_fma(k, o[i], sum[1][i]);
+                if constexpr (kBias) sum[3][i] = f2_add(sum[3][i], k);
+                u[i] = f2_mul(q, sw[i]);
+                d1 = f2_fma(u[i], o[i], d1);
+                d2 = f2_add(d2, u[i]);
+            }
+            if (p.has_post) {
+                float2 means = grp.sum2(d1.x + d1.y, p.layer_post ? d2.x + d2.y : 0.f);
+                means.x *= -p.inv_c; means.y *= -p.inv_c;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) u[i] = f2_mul(f2_fma(o[i], f2(means.x), f2_add(u[i], f2(means.y))), f2(st.y));
+            }
+            if (live) store8(static_cast<T *>(p.d_o) + row * p.ld_do, c, u);
+        }
+        stage = stage + 1 == kStages ? 0 : stage + 1;
+    }
+
+    // the block's sums: rows of a warp by shuffles, rows of different warps through shared memory
+    if constexpr (kAligned) ptx::copy_async_wait<0>();
+    __syncthreads();
+    float *all = reinterpret_cast<float *>(smem);                // [rows at a time][sum][8 tpr]
+    const int width = 8 * p.tpr, slots_n = kThreads / max(p.tpr, 32), slot = p.tpr < 32 ? (int)(threadIdx.x >> 5) : mine;
+#pragma unroll
+    for (int k = 0; k < kSums; ++k)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            float v = (&sum[k][j / 2].x)[j & 1];
+            for (int o = p.tpr; o < 32; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+            if (p.tpr >= 32 || (int)(threadIdx.x & 31) < p.tpr) all[(slot * kSums + k) * width + j * p.tpr + lane] = v;
+        }
+    __syncthreads();
+    float *out = p.part + (size_t)blockIdx.x * kSums * p.C;
+    for (int i = threadIdx.x; i < kSums * width; i += kThreads) {
+        float v = 0.f;
+        for (int s = 0; s < slots_n; ++s) v += all[s * kSums * width + i];
+        const int k = i / width, l = i % p.tpr, j = i % width / p.tpr;
+        const Columns<kAligned> cc(l, p.tpr, p.C, blockIdx.y * 8 * kThreads);
+        if (cc.has(j)) out[(size_t)k * p.C + cc.at(j)] = v;
+    }
+}
+
+// ---------------------------------------------------------------- sums of the blocks' partial rows
+struct BlockSums {
+    const float *part;
+    const void *g;                                         // the groups' gate rows, where they are shared
+    void *dg;
+    const float *scale, *w_post, *b_post;
+    float *d_scale, *dw_post, *db_post, *dw_pre, *db_pre;
+    long groups, ld_g, ld_dg;
+    int chunks, C, sums, branch, bias, gate, grouped;
+};
+constexpr int kSumLanes = 32, kSumSlices = 16;
+
+// A block has 32 columns and 16 slices of the partial rows: slices of a group's pieces where there are few groups, else of the groups.
+template <typename T>
+__global__ void __launch_bounds__(kSumLanes * kSumSlices) block_sums_kernel(BlockSums p) {
+    __shared__ float sh[4][kSumSlices][kSumLanes];
+    const int lane = threadIdx.x % kSumLanes, slice = threadIdx.x / kSumLanes, col = blockIdx.x * kSumLanes + lane;
+    int sub = kSumSlices;                                   // slices of one group
+    while (sub > 1 && (long)(kSumSlices / sub) < p.groups) sub >>= 1;
+    const int at_once = kSumSlices / sub, slot = slice / sub, part = slice % sub;
+    ptx::grid_wait();
+    float total[4] = {0.f, 0.f, 0.f, 0.f};
+    const bool yes = col < p.C;
+    const float s = yes && p.scale ? p.scale[col] : 1.f, w = yes && p.w_post ? p.w_post[col] : 1.f, b = yes && p.b_post ? p.b_post[col] : 0.f;
+    for (long g0 = 0; g0 < p.groups; g0 += at_once) {
+        const long grp = g0 + slot;
+        float v[4] = {0.f, 0.f, 0.f, 0.f};
+        if (yes && grp < p.groups) {
+            const float *src = p.part + (size_t)grp * p.chunks * p.sums * p.C + col;
+#pragma unroll 4
+            for (int ch = part; ch < p.chunks; ch += sub)
+                for (int k = 0; k < 4; ++k)
+                    if (k < p.sums) v[k] += src[((size_t)ch * p.sums + k) * p.C];
+        }
+        if (p.grouped) {
+            // the group's own sums: one thread per column puts the slices together
+            if (sub > 1) {
+                for (int k = 0; k < p.sums; ++k) sh[k][slice][lane] = v[k];
+                __syncthreads();
+                if (part == 0)
+                    for (int k = 0; k < p.sums; ++k)
+                        for (int q = 1; q < sub; ++q) v[k] += sh[k][slice + q][lane];
+                __syncthreads();
+            }
+            if (part == 0 && yes && grp < p.groups) {
+                const float Q = v[1], P = p.bias ? v[3] : 0.f;
+                const float g = to_f32(static_cast<const T *>(p.g)[grp * p.ld_g + col]), a = gate_act(p.gate, g);
+                const float slope = p.gate == 1 ? a * (1.f - a) : 1.f;
+                from_f32(static_cast<T *>(p.dg)[grp * p.ld_dg + col], s * slope * fmaf(w, Q, b * P));
+                v[1] = a * Q; v[3] = a * P;
+            } else {
+                v[0] = v[1] = v[2] = v[3] = 0.f;
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) total[k] += v[k];
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) sh[k][slice][lane] = total[k];
+    __syncthreads();
+    if (slice != 0 || !yes) return;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        total[k] = 0.f;
+        for (int q = 0; q < kSumSlices; ++q) total[k] += sh[k][q][lane];
+    }
+    if (p.dw_pre) p.dw_pre[col] = total[0];
+    if (p.db_pre) p.db_pre[col] = total[p.branch ? 2 : 1];
+    if (p.branch) {
+        const float Q = total[1], P = p.bias ? total[3] : 0.f;
+        if (p.d_scale) p.d_scale[col] = fmaf(w, Q, b * P);
+        if (p.dw_post) p.dw_post[col] = s * Q;
+        if (p.db_post) p.db_post[col] = s * P;
+    }
+}
+
+}  // namespace flare

@@ -1,0 +1,95 @@
+// Launches of the kernels around a block (flare_block.cuh) for one pair of types: T of the branch, the gate and the normalised rows,
+// R of the residual stream.  Instantiated by flare_block_{bf16,f16,f32}.cu.
+#pragma once
+
+#include "flare_block.cuh"
+#include "flare_host.h"
+
+namespace flare {
+
+// Threads of a block, eight columns each: 512 for rows of more than 2048 columns that can be moved 16 bytes at a time, else 256.  What a row has
+// beyond that goes to further blocks of a cluster.
+constexpr int kBlockMaxWidth = 16384;
+// A block's rows: pieces of the groups, together about as many as fill the chip once.
+struct BlockPlan {
+    int tpr, threads, cluster;
+    long groups, chunk;
+    int chunks;
+};
+inline BlockPlan block_plan(long rows, long group, int C, bool aligned, int sms) {
+    BlockPlan p;
+    p.threads = aligned && C > 2048 ? 512 : 256;
+    p.tpr = 8;
+    while (p.tpr * 8 < C && p.tpr < p.threads) p.tpr *= 2;
+    p.cluster = 1;
+    while (p.cluster * p.threads * 8 < C) p.cluster *= 2;
+    const long turn = p.threads / p.tpr, fit = (p.threads == 512 ? 1 : 2) * (long)sms / p.cluster;
+    p.groups = rows / group;
+    const long pieces = std::max(1L, std::min(fit / std::max(1L, p.groups), (group + turn - 1) / turn));
+    p.chunk = ((group + pieces - 1) / pieces + turn - 1) / turn * turn;
+    p.chunks = (int)((group + p.chunk - 1) / p.chunk);
+    return p;
+}
+
+template <typename T, typename R> int block_forward(BlockArgs a, bool aligned, bool branch, const BlockPlan &plan, cudaStream_t st);
+template <typename T, typename R> int block_backward(BlockArgs a, bool aligned, bool branch, bool bias, const BlockPlan &plan, cudaStream_t st);
+template <typename T> int block_sums(const BlockSums &s, cudaStream_t st);
+
+#ifdef FLARE_BLOCK_INSTANTIATE
+template <typename Kernel>
+int block_launch(Kernel kernel, std::atomic<uint64_t> &opt_in, BlockArgs a, const BlockPlan &p, size_t smem, cudaStream_t st) {
+    a.tpr = p.tpr; a.chunk = p.chunk; a.chunks = p.chunks; a.cluster = p.cluster;
+    if (int rc = ensure_big_smem(kernel, opt_in, 200 * 1024)) return rc;
+    cudaLaunchAttribute attr[2] = {};
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = 1; attr[1].val.clusterDim.y = p.cluster; attr[1].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)(p.groups * p.chunks), p.cluster);
+    cfg.blockDim = p.threads; cfg.dynamicSmemBytes = smem; cfg.stream = st;
+    cfg.attrs = attr; cfg.numAttrs = p.cluster > 1 ? 2 : 1;
+    FLARE_CUDA(cudaLaunchKernelEx(&cfg, kernel, a));
+    return FLARE_OK;
+}
+
+template <typename T, typename R, bool kAligned, bool kBranch, int kThreads>
+int block_forward_as(const BlockArgs &a, const BlockPlan &p, cudaStream_t st) {
+    static std::atomic<uint64_t> opt_in{0};
+    constexpr int pieces = fwd_pieces<T, R, kBranch>();
+    return block_launch(block_forward_kernel<T, R, kAligned, kBranch, kThreads>, opt_in, a, p, kAligned ? (size_t)stages_for(pieces) * pieces * 16 * kThreads : 0, st);
+}
+template <typename T, typename R>
+int block_forward(BlockArgs a, bool aligned, bool branch, const BlockPlan &p, cudaStream_t st) {
+    if (!aligned) return branch ? block_forward_as<T, R, false, true, 256>(a, p, st) : block_forward_as<T, R, false, false, 256>(a, p, st);
+    if (p.threads == 512) return branch ? block_forward_as<T, R, true, true, 512>(a, p, st) : block_forward_as<T, R, true, false, 512>(a, p, st);
+    return branch ? block_forward_as<T, R, true, true, 256>(a, p, st) : block_forward_as<T, R, true, false, 256>(a, p, st);
+}
+
+template <typename T, typename R, bool kAligned, bool kBranch, bool kBias, int kThreads>
+int block_backward_as(const BlockArgs &a, const BlockPlan &p, cudaStream_t st) {
+    static std::atomic<uint64_t> opt_in{0};
+    constexpr int pieces = bwd_pieces<T, R, kBranch>(), sums = bwd_sums<kBranch, kBias>();
+    const size_t meet = (size_t)(kThreads / std::max(p.tpr, 32)) * sums * 8 * p.tpr * sizeof(float);
+    const size_t smem = std::max(kAligned ? (size_t)stages_for(pieces) * pieces * 16 * kThreads : 0, meet);
+    return block_launch(block_backward_kernel<T, R, kAligned, kBranch, kBias, kThreads>, opt_in, a, p, smem, st);
+}
+template <typename T, typename R>
+int block_backward(BlockArgs a, bool aligned, bool branch, bool bias, const BlockPlan &p, cudaStream_t st) {
+    // (rows that are moved one element at a time: always the form with sums for biases)
+    if (!aligned) return branch ? block_backward_as<T, R, false, true, true, 256>(a, p, st) : block_backward_as<T, R, false, false, true, 256>(a, p, st);
+    if (p.threads == 512) {
+        if (branch) return bias ? block_backward_as<T, R, true, true, true, 512>(a, p, st) : block_backward_as<T, R, true, true, false, 512>(a, p, st);
+        return bias ? block_backward_as<T, R, true, false, true, 512>(a, p, st) : block_backward_as<T, R, true, false, false, 512>(a, p, st);
+    }
+    if (branch) return bias ? block_backward_as<T, R, true, true, true, 256>(a, p, st) : block_backward_as<T, R, true, true, false, 256>(a, p, st);
+    return bias ? block_backward_as<T, R, true, false, true, 256>(a, p, st) : block_backward_as<T, R, true, false, false, 256>(a, p, st);
+}
+template <typename T>
+int block_sums(const BlockSums &a, cudaStream_t st) {
+    FLARE_CUDA(launch_after(block_sums_kernel<T>, (unsigned)((a.C + kSumLanes - 1) / kSumLanes), kSumLanes * kSumSlices, 0, st, a));
+    return FLARE_OK;
+}
+#endif
+
+}  // namespace flare

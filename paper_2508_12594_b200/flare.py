@@ -9,7 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from typing import Optional
+from typing import NamedTuple, Optional
 
 import torch
 
@@ -26,6 +26,13 @@ class FlareDesc(ctypes.Structure):
                 ("D", ctypes.c_int32), ("dtype", ctypes.c_int32), ("scale", ctypes.c_float)]
 
 
+class FlareBlockDesc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("width", ctypes.c_int32), ("dtype", ctypes.c_int32), ("residual_dtype", ctypes.c_int32),
+                ("pre_norm", ctypes.c_int32), ("post_norm", ctypes.c_int32), ("gate", ctypes.c_int32), ("gate_rows", ctypes.c_int64),
+                ("pre_eps", ctypes.c_float), ("post_eps", ctypes.c_float), ("residual_scale", ctypes.c_float)] + [
+                    (f"stride_{n}", ctypes.c_int64) for n in ("x", "branch", "gate", "y", "h", "dy", "dh", "dx", "dbranch", "dgate")]
+
+
 class FlareError(RuntimeError):
     def __init__(self, status: int, where: str):
         lib = _lib_or_none()
@@ -39,6 +46,7 @@ _lib = None
 
 _vp, _sz = ctypes.c_void_p, ctypes.c_size_t
 _dp = ctypes.POINTER(FlareDesc)
+_bp = ctypes.POINTER(FlareBlockDesc)
 _SIGNATURES = {
     "flare_version": (ctypes.c_int, []),
     "flare_status_string": (ctypes.c_char_p, [ctypes.c_int]),
@@ -60,6 +68,11 @@ _SIGNATURES = {
     "flare_spectral_gram": (ctypes.c_int, [_dp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
     "flare_spectral_eig": (ctypes.c_int, [ctypes.c_int32, ctypes.c_int32, _vp, _vp, _vp, ctypes.c_int32, _vp]),
     "flare_launch_count": (ctypes.c_int, [_dp, ctypes.c_int]),
+    "flare_block_workspace_bytes": (_sz, [_bp]),
+    "flare_norm_forward": (ctypes.c_int, [_bp] + [_vp] * 6),
+    "flare_norm_backward": (ctypes.c_int, [_bp] + [_vp] * 9 + [_sz, _vp]),
+    "flare_join_forward": (ctypes.c_int, [_bp] + [_vp] * 12),
+    "flare_join_backward": (ctypes.c_int, [_bp] + [_vp] * 19 + [_sz, _vp]),
     "flare_selftest_wait": (ctypes.c_int, [_vp, ctypes.c_uint64, _vp]),
 }
 
@@ -261,3 +274,87 @@ def forward_backward(Q, K, V, dY, key_mask=None, scale=1.0, stream=None, check=F
         flare_check(ws, stream)
         flare_check(ws[256:], stream)
     return Y, dQ, dK, dV
+
+
+# ---- around a block: the norms before and after it, its gate and residual scale
+
+NORM_NONE, NORM_LAYER, NORM_RMS = range(3)
+GATE_NONE, GATE_SIGMOID, GATE_LINEAR = range(3)
+_NORMS = {"layer": NORM_LAYER, "rms": NORM_RMS}
+_GATES = {"none": GATE_NONE, "sigmoid": GATE_SIGMOID, "linear": GATE_LINEAR}
+
+
+class Norm(NamedTuple):
+    """A norm over the last dimension: kind "layer" or "rms"; weight and bias float32 [width] or None (ones, zeros)."""
+    kind: str
+    weight: Optional[torch.Tensor] = None
+    bias: Optional[torch.Tensor] = None
+    eps: float = 1e-5
+
+
+class NormGrads(NamedTuple):
+    dx: torch.Tensor
+    dweight: Optional[torch.Tensor]
+    dbias: Optional[torch.Tensor]
+
+
+class JoinGrads(NamedTuple):
+    dx: torch.Tensor
+    dbranch: torch.Tensor
+    dgate: Optional[torch.Tensor]
+    dscale: Optional[torch.Tensor]
+    dpost_weight: Optional[torch.Tensor]
+    dpost_bias: Optional[torch.Tensor]
+    dpre_weight: Optional[torch.Tensor]
+    dpre_bias: Optional[torch.Tensor]
+
+
+def _kind(table, name, what):
+    code = table.get(name)
+    if code is None:
+        raise ValueError(f"{what}: expected one of {', '.join(table)}, got {name!r}")
+    return code
+
+
+def _norm_args(norm: Optional[Norm]):
+    if norm is None:
+        return NORM_NONE, None, None, 0.0
+    return _kind(_NORMS, norm.kind, "norm"), norm.weight, norm.bias, norm.eps
+
+
+def block_norm(x, norm: Norm, dtype=None, out=None, stream=None):
+    """The norm before a block.  x [..., width] -> (h [..., width] of `dtype` (x's), stats [rows, 4] float32).
+    out: (h, stats) to write to, either None."""
+    kind, w, b, eps = _norm_args(norm)
+    return (_native or _bind()).block_norm(x, kind, w, b, eps, dtype, out, stream)
+
+
+def block_norm_backward(x, stats, dh, norm: Norm, dy=None, out=None, stream=None) -> NormGrads:
+    """Gradients of block_norm; dy: what reaches x beside the norm.  Those of weights that are None are None.
+    out: (dx, dweight, dbias) to write to, any None."""
+    kind, w, b, eps = _norm_args(norm)
+    return NormGrads._make((_native or _bind()).block_norm_backward(x, stats, dh, dy, kind, w, b, eps, out, stream))
+
+
+def block_join(x, branch, post: Optional[Norm] = None, pre: Optional[Norm] = None, gate=None, gate_kind="sigmoid", scale=None,
+               residual_scale=1.0, out=None, stream=None):
+    """What follows a block, and the norm before the next one:
+    y = residual_scale * x + scale * act(gate) * post(branch);  h = pre(y).  Returns (y, h or None, stats [rows, 4]).
+
+    x, branch [..., width]; gate like the branch, or with fewer of its leading dimensions (one row per batch item, say);
+    gate_kind "sigmoid" or "linear"; scale float32 [width].  out: (y, h, stats) to write to, any None."""
+    if gate is None:
+        gate_kind = "none"
+    return (_native or _bind()).block_join(x, branch, *_norm_args(post), *_norm_args(pre), gate, _kind(_GATES, gate_kind, "gate_kind"), scale,
+                                           residual_scale, out, stream)
+
+
+def block_join_backward(branch, y, stats, dy, dh, post: Optional[Norm] = None, pre: Optional[Norm] = None, gate=None, gate_kind="sigmoid",
+                        scale=None, residual_scale=1.0, out=None, stream=None) -> JoinGrads:
+    """Gradients of block_join from its inputs, its y and its stats; dy may be None where there is a dh, dh goes
+    with pre.  Gradients of what is None are None.
+    out: a tuple in the order of JoinGrads to write to, any None."""
+    if gate is None:
+        gate_kind = "none"
+    return JoinGrads._make((_native or _bind()).block_join_backward(branch, y, stats, dy, dh, *_norm_args(post), *_norm_args(pre), gate,
+                                                                    _kind(_GATES, gate_kind, "gate_kind"), scale, residual_scale, out, stream))

@@ -324,6 +324,42 @@ int flare_join_backward(const flare_block_desc_t *desc, const void *branch, cons
                         float *dpre_bias, void *workspace, size_t workspace_bytes, flare_stream_t stream);
 
 /*
+ * Orthogonalised updates of matrices (projections, point-wise layers, the latents of a head).  Per matrix G [rows, cols]
+ *
+ *     X = G / (|G|_F + eps);   `steps` times:  A = X X^T,  X <- (a I + b A + c A^2) X;   O = X          (a, b, c = coefficients)
+ *
+ * (of the transpose where rows > cols, which is the same matrix).  The odd polynomial a x + b x^3 + c x^5 of the singular values is applied
+ * `steps` times; with the usual (3.4445, -4.7750, 2.0315) and five steps they come out between about 0.7 and 1.2.  Inputs and outputs of any of the
+ * three types.  The products run on the tensor cores, every factor in two float16 halves (22 bits), sums in float32: O is within some 1e-5
+ * of its RMS of float64, also where singular values of a few strong directions stand beside many small ones.
+ *
+ * flare_muon_update puts the optimiser's step around it, one pass over the matrices before and one after:
+ *     m' = momentum m + (1 - momentum) g;  u = momentum m' + (1 - momentum) g with nesterov, else m';
+ *     w' = (1 - lr weight_decay) w - lr update_scale orthogonalised(u)
+ * w_out may be w, m_out may be m, O may be G (with the same strides).  A matrix with a NaN or an infinity comes out as NaN throughout; others are not
+ * touched by it.  A polynomial under which singular values in [0, 1] would grow beyond 64 is FLARE_ERR_UNSUPPORTED.
+ * A wait inside the kernels that gave up is reported by flare_check(workspace).
+ */
+typedef struct {
+    int32_t count, rows, cols;           /* matrices (0 is allowed), up to 65536 rows and columns and 2^31 - 1 elements each */
+    int32_t dtype;                       /* of G and O; flare_muon_update: of g */
+    int32_t weight_dtype;                /* flare_muon_update: of w, w_out */
+    int32_t steps;                       /* 1 to 64 */
+    float coefficients[3], eps;
+    int64_t stride_row, stride_matrix;   /* of G (g): elements between rows, between matrices; 0: contiguous */
+    int64_t out_stride_row, out_stride_matrix; /* of O */
+} flare_orth_desc_t;
+typedef struct {
+    float lr, momentum, weight_decay, update_scale;
+    int32_t nesterov;
+} flare_muon_t;
+size_t flare_orthogonalize_workspace_bytes(const flare_orth_desc_t *desc);
+int flare_orthogonalize(const flare_orth_desc_t *desc, const void *G, void *O, void *workspace, size_t workspace_bytes, flare_stream_t stream);
+/* w, w_out [count, rows, cols] of weight_dtype, m, m_out the same in float32, contiguous; g with the strides of the descriptor. */
+int flare_muon_update(const flare_orth_desc_t *desc, const flare_muon_t *rule, const void *w, const float *m, const void *g, void *w_out, float *m_out,
+                      void *workspace, size_t workspace_bytes, flare_stream_t stream);
+
+/*
  * Instruction-level measurements behind the kernels' design (the paper has no counterpart), so that the figures the
  * documentation quotes can be re-taken on the GPU at hand.  `which`:
  *   0, 1, 2   exponentials per clock per SM of the softmax loop as the sixteen softmax warps of a forward kernel run it

@@ -39,6 +39,9 @@ struct Library {
     decltype(&flare_norm_backward) norm_backward;
     decltype(&flare_join_forward) join_forward;
     decltype(&flare_join_backward) join_backward;
+    decltype(&flare_orthogonalize_workspace_bytes) orthogonalize_workspace_bytes;
+    decltype(&flare_orthogonalize) orthogonalize;
+    decltype(&flare_muon_update) muon_update;
 } lib{};
 PyObject *flare_error = nullptr;   // the exception class (status, where)
 
@@ -630,6 +633,84 @@ BINDING(block_join_backward, 19)
     return wrap_all({dx, d_o, dg, ds, dwo, dbo, dwy, dby});
 BINDING_END
 
+// ---- orthogonalised updates
+
+// Matrices [..., rows, cols]: the columns next to each other, rows at one distance, matrices at one distance.
+struct Matrices {
+    flare_orth_desc_t d{};
+    std::vector<int64_t> shape;
+    Matrices(const at::Tensor &g, PyObject *steps, PyObject *ca, PyObject *cb, PyObject *cc, PyObject *eps) {
+        shape = g.sizes().vec();
+        if (shape.size() < 2) fail(PyExc_ValueError, "expected matrices [..., rows, cols], got shape " + shape_text(shape));
+        const int64_t rows = shape[shape.size() - 2], cols = shape.back();
+        int64_t count = 1;
+        for (size_t i = 0; i + 2 < shape.size(); ++i) count *= shape[i];
+        if (rows > INT32_MAX || cols > INT32_MAX || count > INT32_MAX) fail(PyExc_ValueError, "matrices out of range: shape " + shape_text(shape));
+        d.count = (int32_t)count; d.rows = (int32_t)rows; d.cols = (int32_t)cols;
+        d.dtype = d.weight_dtype = dtype_code(g.scalar_type());
+        d.steps = number_of(steps);
+        d.coefficients[0] = (float)number(ca); d.coefficients[1] = (float)number(cb); d.coefficients[2] = (float)number(cc);
+        d.eps = (float)number(eps);
+    }
+    // pointer, and the strides into row, matrix
+    void *strided(const at::Tensor &t, at::ScalarType dtype, const char *name, int64_t &row, int64_t &matrix) const {
+        if (!t.is_cuda()) fail(PyExc_ValueError, std::string(name) + ": expected a CUDA tensor");
+        if (t.scalar_type() != dtype) fail(PyExc_TypeError, std::string(name) + ": expected " + dtype_name(dtype) + ", got " + dtype_name(t.scalar_type()));
+        if (t.sizes() != at::IntArrayRef(shape)) fail(PyExc_ValueError, std::string(name) + ": expected shape " + shape_text(shape) + ", got " + shape_text(t.sizes()));
+        const int64_t n = t.dim();
+        bool ok = t.size(n - 1) <= 1 || t.stride(n - 1) == 1;
+        row = t.size(n - 2) > 1 ? t.stride(n - 2) : t.size(n - 1);
+        int64_t at = 0, many = 1;
+        for (int64_t i = n - 3; i >= 0; --i) {
+            if (t.size(i) == 1) continue;
+            if (at == 0) at = t.stride(i);
+            else ok = ok && t.stride(i) == at * many;
+            many *= t.size(i);
+        }
+        matrix = at;
+        if (t.numel() > 0 && (!ok || row < t.size(n - 1) || (many > 1 && at < 1)))
+            fail(PyExc_ValueError, std::string(name) + ": expected matrices of adjacent columns, rows and matrices each at one distance");
+        if (t.numel() == 0) row = matrix = 0;
+        return t.data_ptr();
+    }
+    size_t need(const char *where) const {
+        const size_t n = lib.orthogonalize_workspace_bytes(&d);
+        if (n == 0) check_status(d.count < 0 || d.rows < 1 || d.cols < 1 || d.steps < 1 ? FLARE_ERR_INVALID_ARG : FLARE_ERR_UNSUPPORTED, where);
+        return n;
+    }
+};
+
+// G, steps, a, b, c, eps, out or None, stream -> (O, workspace)
+BINDING(orthogonalize, 8)
+    const at::Tensor &G = tensor(a[0]);
+    Matrices c(G, a[1], a[2], a[3], a[4], a[5]);
+    void *g = c.strided(G, G.scalar_type(), "G", c.d.stride_row, c.d.stride_matrix);
+    const at::Tensor O = a[6] == Py_None ? at::empty(c.shape, G.options()) : tensor(a[6]);
+    void *o = c.strided(O, G.scalar_type(), "out", c.d.out_stride_row, c.d.out_stride_matrix);
+    flare_stream_t st = stream_of(a[7]);
+    const size_t need = c.need("flare_orthogonalize");
+    const at::Tensor ws = scratch(need, G, a[7], st);
+    check_status(unlocked([&] { return lib.orthogonalize(&c.d, g, o, ws.data_ptr(), need, st); }), "flare_orthogonalize");
+    return wrap_all({O, ws});
+BINDING_END
+
+// w, m, g, lr, momentum, weight decay, update scale, nesterov, steps, a, b, c, eps, w_out, m_out (or None: in place), stream -> (w_out, m_out, workspace)
+BINDING(muon_update, 16)
+    const at::Tensor &w = tensor(a[0]), &m = tensor(a[1]), &g = tensor(a[2]);
+    Matrices c(g, a[8], a[9], a[10], a[11], a[12]);
+    void *pg = c.strided(g, g.scalar_type(), "g", c.d.stride_row, c.d.stride_matrix);
+    const at::Tensor &w_out = a[13] == Py_None ? w : tensor(a[13]), &m_out = a[14] == Py_None ? m : tensor(a[14]);
+    c.d.weight_dtype = dtype_code(w.scalar_type());
+    check(w, w.scalar_type(), c.shape); check(w_out, w.scalar_type(), c.shape); check(m, at::kFloat, c.shape); check(m_out, at::kFloat, c.shape);
+    const flare_muon_t rule{(float)number(a[3]), (float)number(a[4]), (float)number(a[5]), (float)number(a[6]), PyObject_IsTrue(a[7]) == 1};
+    flare_stream_t st = stream_of(a[15]);
+    const size_t need = c.need("flare_muon_update");
+    const at::Tensor ws = scratch(need, w, a[15], st);
+    check_status(unlocked([&] { return lib.muon_update(&c.d, &rule, w.data_ptr(), (const float *)m.data_ptr(), pg, w_out.data_ptr(), (float *)m_out.data_ptr(),
+                                                       ws.data_ptr(), need, st); }), "flare_muon_update");
+    return wrap_all({w_out, m_out, ws});
+BINDING_END
+
 // bind(addresses: dict name -> int, FlareError)
 BINDING(bind, 2)
     auto get = [&](const char *name, auto &slot) {
@@ -653,6 +734,9 @@ BINDING(bind, 2)
     get("flare_norm_backward", lib.norm_backward);
     get("flare_join_forward", lib.join_forward);
     get("flare_join_backward", lib.join_backward);
+    get("flare_orthogonalize_workspace_bytes", lib.orthogonalize_workspace_bytes);
+    get("flare_orthogonalize", lib.orthogonalize);
+    get("flare_muon_update", lib.muon_update);
     Py_INCREF(a[1]);
     flare_error = a[1];
 BINDING_END
@@ -661,7 +745,7 @@ BINDING_END
 PyMethodDef methods[] = {METHOD(bind), METHOD(encode), METHOD(encode_static_scratch), METHOD(decode), METHOD(forward), METHOD(backward),
                          METHOD(forward_host), METHOD(forward_variant), METHOD(backward_variant), METHOD(spectral_gram), METHOD(spectral_eig),
                          METHOD(call_forward), METHOD(call_forward_backward), METHOD(block_norm), METHOD(block_norm_backward), METHOD(block_join),
-                         METHOD(block_join_backward), {nullptr, nullptr, 0, nullptr}};
+                         METHOD(block_join_backward), METHOD(orthogonalize), METHOD(muon_update), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_binding", "Argument marshalling for libflare.", -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -1,0 +1,267 @@
+// Orthogonalised updates: argument checks, scales, launches.
+#include "flare_host.h"
+#include "flare_orth.cuh"
+
+namespace flare {
+namespace {
+
+struct OrthSizes { int S, L; long ld_x, ld_s; };
+OrthSizes sizes_of(const flare_orth_desc_t *d) {
+    OrthSizes z;
+    z.S = std::min(d->rows, d->cols);
+    z.L = std::max(d->rows, d->cols);
+    z.ld_x = (z.L + 7) / 8 * 8;
+    z.ld_s = (z.S + 7) / 8 * 8;
+    return z;
+}
+bool orth_small(const OrthSizes &z) { return z.S <= 128 && orth_small_size(z.S, z.L).total <= 227 * 1024 - 512; }
+
+// How large X, A = X X^T and B = a I + b A + c A^2 get: X0 has singular values up to 1, each step takes the largest to the quintic's largest value up
+// to there.  The halves' scales put that near the top of float16's range, so that the low halves of small entries are normal numbers too.
+// False where the values grow beyond what the halves are good for (a quintic that does not stay near 1).
+bool orth_scales(const flare_orth_desc_t *d, OrthScales *out) {
+    const double a = d->coefficients[0], b = d->coefficients[1], c = d->coefficients[2];
+    double top = 1.0, x = 1.0, poly = 0.0;
+    for (int step = 0; step < d->steps; ++step) {
+        double next = 0.0;
+        for (int i = 0; i <= 2000; ++i) {
+            const double v = 1.001 * top * i / 2000.0, v2 = v * v, q = a + b * v2 + c * v2 * v2;
+            next = std::max(next, std::fabs(v * q));
+            poly = std::max(poly, std::fabs(q));
+        }
+        top = next;
+        x = std::max(x, top);
+        if (!(x <= 64.0) || !(poly <= 4096.0)) return false;
+    }
+    auto scale = [](double most) { return (float)std::exp2(std::floor(std::log2(40000.0 / most))); };
+    out->x = scale(x);
+    out->a = scale(x * x);
+    out->b = scale(std::max(poly, 1e-3));
+    out->ca = (float)a; out->cb = (float)b; out->cc = (float)c;
+    return true;
+}
+
+int check_orth(const flare_orth_desc_t *d, OrthScales *scales) {
+    if (d == nullptr) return FLARE_ERR_INVALID_ARG;
+    if (d->count < 0 || d->rows <= 0 || d->cols <= 0 || d->steps < 1 || !(d->eps >= 0.f) || !std::isfinite(d->eps)) return FLARE_ERR_INVALID_ARG;
+    for (float c : d->coefficients)
+        if (!std::isfinite(c)) return FLARE_ERR_INVALID_ARG;
+    if ((d->stride_row != 0 && d->stride_row < d->cols) || (d->out_stride_row != 0 && d->out_stride_row < d->cols) || d->stride_matrix < 0 || d->out_stride_matrix < 0)
+        return FLARE_ERR_INVALID_ARG;
+    auto type = [](int t) { return t == FLARE_DTYPE_F32 || t == FLARE_DTYPE_BF16 || t == FLARE_DTYPE_F16; };
+    if (!type(d->dtype) || !type(d->weight_dtype)) return FLARE_ERR_UNSUPPORTED;
+    if (d->rows > 65536 || d->cols > 65536 || d->count > 32767 || d->steps > 64 || (int64_t)d->rows * d->cols > ((int64_t)1 << 31) - 1) return FLARE_ERR_UNSUPPORTED;
+    return orth_scales(d, scales) ? FLARE_OK : FLARE_ERR_UNSUPPORTED;
+}
+
+int norm_blocks(const flare_orth_desc_t *d, int sms) {
+    const long each = ((long)d->rows * d->cols + kOrthNormThreads * 16 - 1) / (kOrthNormThreads * 16);
+    return (int)std::max(1L, std::min(each, (8L * sms + d->count - 1) / std::max(1, d->count)));
+}
+struct OrthLayout { size_t part, x[2], a, b, total; };
+OrthLayout orth_layout(const flare_orth_desc_t *d, int sms) {
+    const OrthSizes z = sizes_of(d);
+    OrthLayout w{};
+    size_t off = kHeaderBytes;
+    if (!orth_small(z)) {
+        const size_t n = 2 * (size_t)d->count * sizeof(__half);
+        w.part = off; off += align_up(sizeof(double) * (size_t)d->count * norm_blocks(d, sms));
+        for (size_t &x : w.x) { x = off; off += align_up(n * z.S * z.ld_x); }
+        w.a = off; off += align_up(n * z.S * z.ld_s);
+        w.b = off; off += align_up(n * z.S * z.ld_s);
+    }
+    w.total = off;
+    return w;
+}
+
+// Halves [planes, rows, cols] of rows `ld` apart, in boxes of box_cols x box_rows: 64 columns with 128-byte swizzle, 32 with 64-byte.
+int make_half_map(CUtensorMap *m, const void *base, long cols, long rows, long planes, long ld, int box_cols, int box_rows) {
+    EncodeTiledFn fn = encode_tiled_fn();
+    if (!fn) {
+        snprintf(g_cuda_error, sizeof(g_cuda_error), "cuTensorMapEncodeTiled not available");
+        return FLARE_ERR_CUDA;
+    }
+    cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)planes};
+    cuuint64_t strides[2] = {(cuuint64_t)ld * 2, (cuuint64_t)ld * 2 * (cuuint64_t)rows};
+    cuuint32_t box[3] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows, 1}, estr[3] = {1, 1, 1};
+    const CUresult r = fn(m, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void *>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                          box_cols == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) {
+        snprintf(g_cuda_error, sizeof(g_cuda_error), "cuTensorMapEncodeTiled(halves) failed: %d", (int)r);
+        return FLARE_ERR_CUDA;
+    }
+    return FLARE_OK;
+}
+
+// Blocks that share a tile's sums: as many as fill the chip, with at least four 64-deep steps each.
+int k_split(long tiles, int K, int sms) {
+    const int blocks = (K + 63) / 64;
+    int ks = 1;
+    while (ks < 8 && 2 * ks * tiles <= sms && blocks / (2 * ks) >= 4) ks *= 2;
+    return ks;
+}
+
+// A matrix of halves in the three forms its tiles are moved in: loaded, stored, stored transposed.
+struct HalfMaps { CUtensorMap load, store, store_t; };
+int make_half_maps(HalfMaps *m, const void *base, long cols, long rows, long planes, long ld) {
+    int rc;
+    if ((rc = make_half_map(&m->load, base, cols, rows, planes, ld, 64, 64)) != FLARE_OK) return rc;
+    if ((rc = make_half_map(&m->store, base, cols, rows, planes, ld, 64, 32)) != FLARE_OK) return rc;
+    return make_half_map(&m->store_t, base, cols, rows, planes, ld, 32, 64);
+}
+
+template <int kKind, int kPair>
+int launch_product_as(const HalfMaps &ta, const HalfMaps &tb, const HalfMaps &out, OrthProduct p, int count, int sms, cudaStream_t st) {
+    static std::atomic<uint64_t> opt_in{0};
+    if (int rc = ensure_big_smem(orth_product_kernel<kKind, kPair>, opt_in, (int)kOrthSmem)) return rc;
+    p.total = p.tiles * count;
+    p.ks = kPair == 1 ? k_split(p.total, p.K, sms) : 1;
+    const int cluster = kPair * p.ks;
+    cudaLaunchAttribute attr[2] = {};
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)(p.ks > 1 ? p.total * p.ks : kPair * std::min(p.total, sms / kPair)));
+    cfg.blockDim = kOrthThreads; cfg.dynamicSmemBytes = kOrthSmem; cfg.stream = st;
+    cfg.attrs = attr; cfg.numAttrs = cluster > 1 ? 2 : 1;
+    FLARE_CUDA(cudaLaunchKernelEx(&cfg, orth_product_kernel<kKind, kPair>, ta.load, tb.load, out.store, out.store_t, p));
+    return FLARE_OK;
+}
+template <int kKind>
+int launch_product(const HalfMaps &ta, const HalfMaps &tb, const HalfMaps &out, OrthProduct p, int count, int sms, cudaStream_t st) {
+    auto tiles = [&](int side) {
+        p.tiles_m = (p.S + side - 1) / side;
+        p.tiles_n = (p.N + side - 1) / side;
+        p.tiles = kKind == kOrthGram || kKind == kOrthPoly ? p.tiles_n * (p.tiles_n + 1) / 2 : p.tiles_m * p.tiles_n;
+        return (long)p.tiles * count;
+    };
+    // turns of the chip, in units of a pair's tile: a block's 128 x 128 takes about 0.6 of a pair's 256 x 256
+    const long pairs = (tiles(256) + sms / 2 - 1) / (sms / 2), singles = (tiles(128) + sms - 1) / sms;
+    if ((double)pairs <= 0.6 * singles) {
+        tiles(256);
+        return launch_product_as<kKind, 2>(ta, tb, out, p, count, sms, st);
+    }
+    return launch_product_as<kKind, 1>(ta, tb, out, p, count, sms, st);
+}
+
+int run_orth(const flare_orth_desc_t *d, const OrthScales &sc, const OrthOuter &o, void *workspace, cudaStream_t st) {
+    const int sms = device_info().sms;
+    const OrthSizes z = sizes_of(d);
+    uint32_t *status = static_cast<uint32_t *>(workspace);
+    if (int rc = clear_header(workspace, 0, st)) return rc;
+    if (orth_small(z)) {
+        static std::atomic<uint64_t> opt_in{0};
+        if (int rc = ensure_big_smem(orth_small_kernel, opt_in, 227 * 1024 - 512)) return rc;
+        OrthSmall p{};
+        p.o = o; p.sc = sc; p.S = z.S; p.L = z.L; p.Mr = (z.S + 15) / 16 * 16; p.panels = (z.L + 63) / 64; p.steps = d->steps; p.status = status;
+        FLARE_CUDA(launch_after(orth_small_kernel, (unsigned)d->count, kOrthSmallThreads, orth_small_size(z.S, z.L).total, st, p));
+        return FLARE_OK;
+    }
+    const OrthLayout w = orth_layout(d, sms);
+    char *ws = static_cast<char *>(workspace);
+    double *part = reinterpret_cast<double *>(ws + w.part);
+    __half *x[2] = {reinterpret_cast<__half *>(ws + w.x[0]), reinterpret_cast<__half *>(ws + w.x[1])};
+    __half *A = reinterpret_cast<__half *>(ws + w.a), *B = reinterpret_cast<__half *>(ws + w.b);
+    const int parts = norm_blocks(d, sms);
+    FLARE_CUDA(launch_after(orth_norm_kernel, dim3(parts, d->count), kOrthNormThreads, 0, st, o, part));
+    FLARE_CUDA(launch_after(orth_split_kernel, dim3((d->cols + 31) / 32, (d->rows + 31) / 32, d->count), 256, 0, st, o, part, parts, x[0], z.ld_x, sc.x));
+    HalfMaps tx[2], tA, tB;
+    const long planes = 2L * d->count;
+    int rc;
+    for (int i = 0; i < 2; ++i)
+        if ((rc = make_half_maps(&tx[i], x[i], z.L, z.S, planes, z.ld_x)) != FLARE_OK) return rc;
+    if ((rc = make_half_maps(&tA, A, z.S, z.S, planes, z.ld_s)) != FLARE_OK) return rc;
+    if ((rc = make_half_maps(&tB, B, z.S, z.S, planes, z.ld_s)) != FLARE_OK) return rc;
+    for (int step = 0; step < d->steps; ++step) {
+        const int cur = step & 1;
+        OrthProduct p{};
+        p.status = status; p.S = z.S; p.N = z.S;
+        p.dst = A; p.ld_dst = z.ld_s; p.K = z.L; p.f = sc.a / (sc.x * sc.x);
+        if ((rc = launch_product<kOrthGram>(tx[cur], tx[cur], tA, p, d->count, sms, st)) != FLARE_OK) return rc;
+        p.dst = B; p.a = A; p.ld_a = z.ld_s; p.K = z.S;
+        p.f = sc.cc * sc.b / (sc.a * sc.a); p.fa = sc.cb * sc.b / sc.a; p.fi = sc.ca * sc.b;
+        if ((rc = launch_product<kOrthPoly>(tA, tA, tB, p, d->count, sms, st)) != FLARE_OK) return rc;
+        p.dst = x[1 - cur]; p.ld_dst = z.ld_x; p.N = z.L;
+        if (step + 1 < d->steps) {
+            p.f = 1.f / sc.b;
+            if ((rc = launch_product<kOrthApply>(tB, tx[cur], tx[1 - cur], p, d->count, sms, st)) != FLARE_OK) return rc;
+        } else {
+            p.o = o;
+            p.f = 1.f / (sc.b * sc.x);
+            if ((rc = launch_product<kOrthLast>(tB, tx[cur], tx[1 - cur], p, d->count, sms, st)) != FLARE_OK) return rc;
+        }
+    }
+    return FLARE_OK;
+}
+
+size_t size_of(int dtype) { return dtype == FLARE_DTYPE_F32 ? 4 : 2; }
+bool natural(const void *p, size_t size) { return reinterpret_cast<uintptr_t>(p) % size == 0; }
+
+int need_device() {
+    const DeviceView di = device_info();
+    if (di.checked == -2) {
+        snprintf(g_cuda_error, sizeof(g_cuda_error), "no CUDA device");
+        return FLARE_ERR_CUDA;
+    }
+    return di.checked == 1 ? FLARE_OK : FLARE_ERR_ARCH;
+}
+
+OrthOuter outer_of(const flare_orth_desc_t *d) {
+    OrthOuter o{};
+    o.rows = d->rows; o.cols = d->cols; o.g_type = d->dtype; o.eps = d->eps; o.tall = d->rows > d->cols;
+    o.ld_g = d->stride_row ? d->stride_row : d->cols;
+    o.step_g = d->stride_matrix ? d->stride_matrix : o.ld_g * d->rows;
+    return o;
+}
+
+}  // namespace
+}  // namespace flare
+
+using namespace flare;
+
+extern "C" {
+
+size_t flare_orthogonalize_workspace_bytes(const flare_orth_desc_t *desc) {
+    OrthScales sc;
+    if (check_orth(desc, &sc) != FLARE_OK) return 0;
+    return orth_layout(desc, device_info().sms).total;
+}
+
+int flare_orthogonalize(const flare_orth_desc_t *desc, const void *G, void *O, void *workspace, size_t workspace_bytes, flare_stream_t stream) {
+    OrthScales sc;
+    if (int rc = check_orth(desc, &sc)) return rc;
+    const size_t e = size_of(desc->dtype);
+    if (!workspace || !aligned16(workspace) || (desc->count > 0 && (!G || !O)) || !natural(G, e) || !natural(O, e)) return FLARE_ERR_INVALID_ARG;
+    if (int rc = need_device()) return rc;
+    if (workspace_bytes < orth_layout(desc, device_info().sms).total) return FLARE_ERR_WORKSPACE_TOO_SMALL;
+    if (desc->count == 0) return FLARE_OK;
+    OrthOuter o = outer_of(desc);
+    o.g = G; o.out = O; o.out_type = desc->dtype;
+    o.ld_out = desc->out_stride_row ? desc->out_stride_row : desc->cols;
+    o.step_out = desc->out_stride_matrix ? desc->out_stride_matrix : o.ld_out * desc->rows;
+    return run_orth(desc, sc, o, workspace, reinterpret_cast<cudaStream_t>(stream));
+}
+
+int flare_muon_update(const flare_orth_desc_t *desc, const flare_muon_t *rule, const void *w, const float *m, const void *g, void *w_out, float *m_out,
+                      void *workspace, size_t workspace_bytes, flare_stream_t stream) {
+    OrthScales sc;
+    if (int rc = check_orth(desc, &sc)) return rc;
+    if (!rule || !std::isfinite(rule->lr) || !std::isfinite(rule->momentum) || !std::isfinite(rule->weight_decay) || !std::isfinite(rule->update_scale))
+        return FLARE_ERR_INVALID_ARG;
+    const size_t e = size_of(desc->weight_dtype);
+    if (!workspace || !aligned16(workspace) || (desc->count > 0 && (!w || !m || !g || !w_out || !m_out))) return FLARE_ERR_INVALID_ARG;
+    if (!natural(w, e) || !natural(w_out, e) || !natural(m, 4) || !natural(m_out, 4) || !natural(g, size_of(desc->dtype))) return FLARE_ERR_INVALID_ARG;
+    if (int rc = need_device()) return rc;
+    if (workspace_bytes < orth_layout(desc, device_info().sms).total) return FLARE_ERR_WORKSPACE_TOO_SMALL;
+    if (desc->count == 0) return FLARE_OK;
+    OrthOuter o = outer_of(desc);
+    o.g = g; o.w = w; o.out = w_out; o.out_type = desc->weight_dtype; o.m = m; o.m_out = m_out;
+    o.ld_out = desc->cols; o.step_out = (long)desc->cols * desc->rows;
+    o.nesterov = rule->nesterov != 0; o.momentum = rule->momentum;
+    o.keep = 1.f - rule->lr * rule->weight_decay; o.rate = rule->lr * rule->update_scale;
+    return run_orth(desc, sc, o, workspace, reinterpret_cast<cudaStream_t>(stream));
+}
+
+}  // extern "C"

@@ -33,6 +33,16 @@ class FlareBlockDesc(ctypes.Structure):
                     (f"stride_{n}", ctypes.c_int64) for n in ("x", "branch", "gate", "y", "h", "dy", "dh", "dx", "dbranch", "dgate")]
 
 
+class FlareOrthDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("count", "rows", "cols", "dtype", "weight_dtype", "steps")] + [
+        ("coefficients", ctypes.c_float * 3), ("eps", ctypes.c_float)] + [
+            (n, ctypes.c_int64) for n in ("stride_row", "stride_matrix", "out_stride_row", "out_stride_matrix")]
+
+
+class FlareMuon(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_float) for n in ("lr", "momentum", "weight_decay", "update_scale")] + [("nesterov", ctypes.c_int32)]
+
+
 class FlareError(RuntimeError):
     def __init__(self, status: int, where: str):
         lib = _lib_or_none()
@@ -47,6 +57,7 @@ _lib = None
 _vp, _sz = ctypes.c_void_p, ctypes.c_size_t
 _dp = ctypes.POINTER(FlareDesc)
 _bp = ctypes.POINTER(FlareBlockDesc)
+_op = ctypes.POINTER(FlareOrthDesc)
 _SIGNATURES = {
     "flare_version": (ctypes.c_int, []),
     "flare_status_string": (ctypes.c_char_p, [ctypes.c_int]),
@@ -73,6 +84,9 @@ _SIGNATURES = {
     "flare_norm_backward": (ctypes.c_int, [_bp] + [_vp] * 9 + [_sz, _vp]),
     "flare_join_forward": (ctypes.c_int, [_bp] + [_vp] * 12),
     "flare_join_backward": (ctypes.c_int, [_bp] + [_vp] * 19 + [_sz, _vp]),
+    "flare_orthogonalize_workspace_bytes": (_sz, [_op]),
+    "flare_orthogonalize": (ctypes.c_int, [_op, _vp, _vp, _vp, _sz, _vp]),
+    "flare_muon_update": (ctypes.c_int, [_op, ctypes.POINTER(FlareMuon)] + [_vp] * 6 + [_sz, _vp]),
     "flare_selftest_wait": (ctypes.c_int, [_vp, ctypes.c_uint64, _vp]),
 }
 
@@ -358,3 +372,34 @@ def block_join_backward(branch, y, stats, dy, dh, post: Optional[Norm] = None, p
         gate_kind = "none"
     return JoinGrads._make((_native or _bind()).block_join_backward(branch, y, stats, dy, dh, *_norm_args(post), *_norm_args(pre), gate,
                                                                     _kind(_GATES, gate_kind, "gate_kind"), scale, residual_scale, out, stream))
+
+
+# ---- orthogonalised updates of matrices
+
+NEWTON_SCHULZ = (3.4445, -4.7750, 2.0315)
+
+
+def orthogonalize(G, steps=5, coefficients=NEWTON_SCHULZ, eps=1e-7, out=None, stream=None, check=False):
+    """G [..., rows, cols] -> the same after `steps` Newton-Schulz steps of the odd quintic `coefficients` on G / (|G|_F + eps): singular
+    values near 1, singular vectors kept.  out: a tensor to write to (G itself is allowed).  With check=True the stream is synchronised
+    and a device-side wait that gave up raises."""
+    O, ws = (_native or _bind()).orthogonalize(G, steps, *coefficients, eps, out, stream)
+    if check:
+        (stream or torch.cuda.current_stream()).synchronize()
+        flare_check(ws, stream)
+    return O
+
+
+def muon_update(w, m, g, lr, momentum=0.95, weight_decay=0.0, nesterov=True, update_scale=None, steps=5, coefficients=NEWTON_SCHULZ, eps=1e-7,
+                w_out=None, m_out=None, stream=None, check=False):
+    """One step of the optimiser that orthogonalises its momentum, on matrices [..., rows, cols]: w of any of the three types, m float32, g
+    a gradient of any type.  m' = momentum m + (1 - momentum) g; w' = (1 - lr weight_decay) w - lr update_scale O, O the orthogonalised
+    momentum m' + (1 - momentum)(g - m') (nesterov) or m'.  update_scale: None means sqrt(max(1, rows / cols)).  In place unless
+    w_out, m_out are given; returns (w', m')."""
+    if update_scale is None:
+        update_scale = max(1.0, g.shape[-2] / g.shape[-1]) ** 0.5
+    w1, m1, ws = (_native or _bind()).muon_update(w, m, g, lr, momentum, weight_decay, update_scale, nesterov, steps, *coefficients, eps, w_out, m_out, stream)
+    if check:
+        (stream or torch.cuda.current_stream()).synchronize()
+        flare_check(ws, stream)
+    return w1, m1

@@ -70,14 +70,14 @@ int need_device() {
      : (d)->dtype == FLARE_DTYPE_BF16 ? ((d)->residual_dtype == FLARE_DTYPE_F32 ? call<__nv_bfloat16, float> : call<__nv_bfloat16, __nv_bfloat16>) \
                                       : ((d)->residual_dtype == FLARE_DTYPE_F32 ? call<__half, float> : call<__half, __half>))
 
-int forward(const flare_block_desc_t *d, bool join, BlockArgs a, cudaStream_t st) {
+int forward(const flare_block_desc_t *d, BlockArgs a, cudaStream_t st) {
     if (int rc = need_device()) return rc;
     if (d->rows == 0) return FLARE_OK;
     const size_t t = size_of(d->dtype), r = size_of(d->residual_dtype);
     Aligned al(d->width);
     al.add(a.x, a.ld_x, r); al.add(a.o, a.ld_o, t); al.add(a.g, a.ld_g, t); al.add(a.y, a.ld_y, r); al.add(a.h, a.ld_h, t);
     if (!al.natural) return FLARE_ERR_INVALID_ARG;
-    return FLARE_BLOCK_TYPES(d, block_forward)(a, al.ok, join, block_plan(d->rows, a.group, d->width, al.ok, device_info().sms), st);
+    return FLARE_BLOCK_TYPES(d, block_forward)(a, al.ok, device_info().sms, st);
 }
 
 // Bytes of the partial sums, for whichever form of the kernels the tensors' alignment leads to.
@@ -106,7 +106,7 @@ int backward(const flare_block_desc_t *d, bool join, BlockArgs a, const BlockGra
     const BlockPlan plan = block_plan(d->rows, a.group, d->width, al.ok, sms);
     a.part = static_cast<float *>(workspace);
     if (d->rows > 0) {
-        if (int rc = FLARE_BLOCK_TYPES(d, block_backward)(a, al.ok, join, bias, plan, st)) return rc;
+        if (int rc = FLARE_BLOCK_TYPES(d, block_backward)(a, al.ok, bias, plan, st)) return rc;
     }
     const bool shared_gate = a.grouped && a.dg;
     if (!shared_gate && !out.d_scale && !out.dw_post && !out.db_post && !out.dw_pre && !out.db_pre) return FLARE_OK;
@@ -139,7 +139,7 @@ int flare_norm_forward(const flare_block_desc_t *desc, const void *x, const floa
     if (!float_params_ok({weight, bias}) || !aligned16(stats)) return FLARE_ERR_INVALID_ARG;
     BlockArgs a = common_args(desc, false);
     a.x = x; a.w_pre = weight; a.b_pre = bias; a.h = h; a.stats = reinterpret_cast<float4 *>(stats);
-    return forward(desc, false, a, reinterpret_cast<cudaStream_t>(stream));
+    return forward(desc, a, reinterpret_cast<cudaStream_t>(stream));
 }
 
 int flare_norm_backward(const flare_block_desc_t *desc, const void *x, const float *weight, const float *stats, const void *dy, const void *dh, void *dx,
@@ -163,7 +163,7 @@ int flare_join_forward(const flare_block_desc_t *desc, const void *x, const void
     BlockArgs a = common_args(desc, true);
     a.x = x; a.o = branch; a.g = gate; a.scale = scale; a.w_post = post_weight; a.b_post = post_bias; a.w_pre = pre_weight; a.b_pre = pre_bias;
     a.y = y; a.h = h; a.stats = reinterpret_cast<float4 *>(stats);
-    return forward(desc, true, a, reinterpret_cast<cudaStream_t>(stream));
+    return forward(desc, a, reinterpret_cast<cudaStream_t>(stream));
 }
 
 int flare_join_backward(const flare_block_desc_t *desc, const void *branch, const void *gate, const float *scale, const float *post_weight,

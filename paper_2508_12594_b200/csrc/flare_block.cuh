@@ -90,6 +90,7 @@ __device__ __forceinline__ Raw8<E> pack8(const float2 (&f)[4]) {
 template <bool kAligned>
 struct Columns {
     int first, step, C;
+    __device__ __forceinline__ Columns() {}
     __device__ __forceinline__ Columns(int lane, int tpr, int C_, int base = 0) : first(base + (kAligned ? 8 * lane : lane)), step(kAligned ? 1 : tpr), C(C_) {}
     __device__ __forceinline__ int at(int j) const { return first + j * step; }
     __device__ __forceinline__ bool has(int j) const { return kAligned ? first < C : at(j) < C; }
@@ -151,80 +152,97 @@ struct RowGroup {
     __device__ __forceinline__ void meet() const {
         asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
     }
-    __device__ __forceinline__ float within_warp(float v) const {
-        for (int o = min(tpr, 32) >> 1; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    // Sum over the lanes whose indexes differ below n (a power of two).
+    __device__ __forceinline__ static float over(float v, int n) {
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1)
+            if (n > o) v += __shfl_xor_sync(0xffffffffu, v, o);
         return v;
     }
-    // v of every warp of the row in this block: where the row's first one's is.  All threads of the block call it.
-    __device__ __forceinline__ const float4 *of_warps(float4 v) {
+    __device__ __forceinline__ float within_warp(float v) const { return over(v, min(tpr, 32)); }
+    // v of every warp of the row in this block: in lane k that of the row's k-th (zeros beyond the last).  All threads of the block call it.
+    __device__ __forceinline__ float4 of_warps(float4 v) {
         if ((threadIdx.x & 31) == 0) sh->warp[turn][warp] = v;
         __syncthreads();
-        return sh->warp[turn] + first;
+        const int l = threadIdx.x & 31;
+        return l < warps ? sh->warp[turn][first + l] : make_float4(0.f, 0.f, 0.f, 0.f);
     }
-    // v (the same in all threads of a block) of every block of the row.  All threads of the cluster call it.
-    __device__ __forceinline__ const float4 *of_blocks(float4 v) {
+    // v (the same in all threads of a block) of every block of the row: in lane k that of the k-th.  All threads of the cluster call it.
+    __device__ __forceinline__ float4 of_blocks(float4 v) {
         if ((int)threadIdx.x < cluster) {
             uint32_t to;
             asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(ptx::smem_u32(&sh->block[turn][blockIdx.y])), "r"(threadIdx.x));
             asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(to), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
         }
         meet();
-        return sh->block[turn];
+        const int l = threadIdx.x & 31;
+        return l < cluster ? sh->block[turn][l] : make_float4(0.f, 0.f, 0.f, 0.f);
     }
-    // Sums of a and b over the row.  All threads of the block (and its cluster) call it.
-    __device__ __forceinline__ float2 sum2(float a, float b) {
-        a = within_warp(a); b = within_warp(b);
+    // Sums of a and, if kTwo, b over the row.  All threads of the block (and its cluster) call it.
+    template <bool kTwo>
+    __device__ __forceinline__ float2 sum(float a, float b) {
+        a = within_warp(a);
+        if (kTwo) b = within_warp(b);
         if (tpr > 32) {
-            const float4 *r = of_warps(make_float4(a, b, 0.f, 0.f));
-            a = b = 0.f;
-            for (int w = 0; w < warps; ++w) {
-                const float2 v = *reinterpret_cast<const float2 *>(r + w);
-                a += v.x; b += v.y;
-            }
+            float4 v = of_warps(make_float4(a, b, 0.f, 0.f));
+            a = all_lanes(v.x, warps);
+            if (kTwo) b = all_lanes(v.y, warps);
             if (cluster > 1) {
-                r = of_blocks(make_float4(a, b, 0.f, 0.f));
-                a = b = 0.f;
-                for (int w = 0; w < cluster; ++w) {
-                    a += r[w].x; b += r[w].y;
-                }
+                v = of_blocks(make_float4(a, b, 0.f, 0.f));
+                a = all_lanes(v.x, cluster);
+                if (kTwo) b = all_lanes(v.y, cluster);
             }
             turn ^= 1;
         }
         return make_float2(a, b);
     }
-    // (sum, squares of distances from the own mean, own mean, count) of n parts -> the same of their union
-    __device__ __forceinline__ static float4 join_parts(const float4 *r, int n) {
-        float sum = 0.f, count = 0.f, m2 = 0.f;
-        for (int w = 0; w < n; ++w) { sum += r[w].x; count += r[w].w; }
-        const float mean = count > 0.f ? sum / count : 0.f;
-        for (int w = 0; w < n; ++w) {
-            const float d = r[w].z - mean;
-            m2 += fmaf(r[w].w * d, d, r[w].y);
-        }
-        return make_float4(sum, m2, mean, count);
+    // The sum of what the first n lanes hold (a power of two, zeros in the others), in every lane.
+    __device__ __forceinline__ static float all_lanes(float v, int n) { return __shfl_sync(0xffffffffu, over(v, n), 0); }
+    // (sum, squares of distances from the own mean, own mean, count) in the first n lanes -> the same of their union, in every lane
+    __device__ __forceinline__ static float4 join_parts(float4 v, int n) {
+        const float sum = all_lanes(v.x, n), count = all_lanes(v.w, n);
+        const float mean = count > 0.f ? sum / count : 0.f, d = v.z - mean;
+        return make_float4(sum, all_lanes(fmaf(v.w * d, d, v.y), n), mean, count);
     }
 };
 
 // Mean and 1/sqrt(var + eps) of a row.  layer: the squares are of distances from the mean, first the warp's, put together with those of the
-// row's other warps by the distances of their means (one barrier, and no small difference of large sums).  `mine`, `in_warp`: elements of
-// this thread and of its warp's part of the row.
-template <bool kAligned>
-__device__ __forceinline__ float2 moments(RowGroup &grp, const float2 (&v)[4], const Columns<kAligned> &c, float in_warp, int layer, float inv_c, float eps) {
+// row's other warps by the distances of their means (one barrier, and no small difference of large sums).  in_warp: elements of
+// this thread's warp's part of the row.
+template <int kV, bool kAligned>
+__device__ __forceinline__ float2 moments(RowGroup &grp, const float2 (&v)[kV][4], const Columns<kAligned> *c, float in_warp, int layer, float inv_c, float eps) {
     if (!layer) {
         float2 s = f2(0.f);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s = f2_fma(v[i], v[i], s);
-        const float sq = grp.sum2(s.x + s.y, 0.f).x;
+        for (int g = 0; g < kV; ++g)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s = f2_fma(v[g][i], v[g][i], s);
+        const float sq = grp.sum<false>(s.x + s.y, 0.f).x;
         return make_float2(0.f, rsqrtf(fmaf(sq, inv_c, eps)));
     }
-    const float2 s01 = f2_add(f2_add(v[0], v[1]), f2_add(v[2], v[3]));
-    const float sum = grp.within_warp(s01.x + s01.y);
-    const float mean_w = in_warp > 0.f ? sum / in_warp : 0.f;
+    float2 t = f2(0.f);
+#pragma unroll
+    for (int g = 0; g < kV; ++g) t = f2_add(t, f2_add(f2_add(v[g][0], v[g][1]), f2_add(v[g][2], v[g][3])));
+    const float sum = grp.within_warp(t.x + t.y);
+    const float mean_w = in_warp > 0.f ? __fdividef(sum, in_warp) : 0.f;
     float m2 = 0.f;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const float d = c.has(j) ? (&v[j / 2].x)[j & 1] - mean_w : 0.f;
-        m2 = fmaf(d, d, m2);
+    for (int g = 0; g < kV; ++g) {
+        if constexpr (kAligned) {
+            float2 s = f2(0.f);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float2 d = f2_add(v[g][i], f2(-mean_w));
+                s = f2_fma(d, d, s);
+            }
+            m2 += c[g].any() ? s.x + s.y : 0.f;
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float d = c[g].has(j) ? (&v[g][j / 2].x)[j & 1] - mean_w : 0.f;
+                m2 = fmaf(d, d, m2);
+            }
+        }
     }
     m2 = grp.within_warp(m2);
     float4 part = make_float4(sum, m2, mean_w, in_warp);
@@ -236,7 +254,19 @@ __device__ __forceinline__ float2 moments(RowGroup &grp, const float2 (&v)[4], c
     return make_float2(part.z, rsqrtf(fmaf(part.y, inv_c, eps)));
 }
 
-__device__ __forceinline__ float gate_act(int kind, float g) { return kind == 1 ? __fdividef(1.f, 1.f + ptx::ex2(-kBlockLog2e * g)) : g; }
+__device__ __forceinline__ float gate_act(int kind, float g) {
+    if (kind != 1) return g;
+    float a;                                                 // (of 1 + exp(-g) = infinity: 0)
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(a) : "f"(1.f + ptx::ex2(-kBlockLog2e * g)));
+    return a;
+}
+
+__device__ __forceinline__ void gate_act8(int kind, float2 (&a)[4]) {
+    if (kind == 1) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) a[i] = make_float2(gate_act(1, a[i].x), gate_act(1, a[i].y));
+    }
+}
 
 // ---------------------------------------------------------------- loads ahead
 // Slots of kStages rows ahead in shared memory, [stage][16-byte piece][thread]: a thread copies into its own and reads only those.
@@ -244,9 +274,9 @@ __device__ __forceinline__ void copy_async16(uint32_t dst, const void *src, bool
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(yes ? 16u : 0u) : "memory");
 }
 template <typename E, int kThreads>
-__device__ __forceinline__ void slot_copy(uint32_t slot, const E *row, int col, bool yes) {
+__device__ __forceinline__ void slot_copy(uint32_t slot, const char *src, bool yes) {
 #pragma unroll
-    for (int i = 0; i < (int)sizeof(E) / 2; ++i) copy_async16(slot + i * kThreads * 16, reinterpret_cast<const uint4 *>(row + col) + i, yes);
+    for (int i = 0; i < (int)sizeof(E) / 2; ++i) copy_async16(slot + i * kThreads * 16, src + 16 * i, yes);
 }
 template <typename E, int kThreads>
 __device__ __forceinline__ Raw8<E> slot_read(uint32_t slot) {
@@ -257,8 +287,22 @@ __device__ __forceinline__ Raw8<E> slot_read(uint32_t slot) {
     return r;
 }
 
-template <typename T, typename R, bool kBranch> __host__ __device__ constexpr int fwd_pieces() { return (int)(sizeof(R) / 2 + (kBranch ? 2 * (sizeof(T) / 2) : 0)); }
-template <typename T, typename R, bool kBranch> __host__ __device__ constexpr int bwd_pieces() { return (int)(2 * (sizeof(R) / 2) + (sizeof(T) / 2) * (kBranch ? 3 : 1)); }
+template <int kThreads>
+__device__ __forceinline__ void slot_write(uint32_t slot, const float2 (&f)[4]) {
+    const Raw8<float> r = pack8<float>(f);
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(slot + i * kThreads * 16), "r"(r.q[i].x), "r"(r.q[i].y), "r"(r.q[i].z), "r"(r.q[i].w) : "memory");
+}
+
+// What comes in beside the residual stream: nothing, a branch, a branch with a gate row a row, a branch with gate rows that are shared.
+enum { kAlone = 0, kPlain = 1, kGated = 2, kShared = 3 };
+template <typename T, typename R, int kIn> __host__ __device__ constexpr int fwd_pieces() {
+    return (int)(sizeof(R) / 2 + (kIn == kAlone ? 0 : kIn == kGated ? 2 : 1) * (sizeof(T) / 2));
+}
+template <typename T, typename R, int kIn> __host__ __device__ constexpr int bwd_pieces() {
+    return (int)(2 * (sizeof(R) / 2) + (kIn == kAlone ? 1 : kIn == kGated ? 3 : 2) * (sizeof(T) / 2));
+}
 __host__ __device__ constexpr int stages_for(int pieces) { return pieces <= 3 ? 4 : pieces <= 7 ? 3 : 2; }
 
 // The rows of one block: a piece of one group of rows.
@@ -272,103 +316,152 @@ struct Piece {
 };
 
 // ---------------------------------------------------------------- forward
-template <typename T, typename R, bool kAligned, bool kBranch, int kThreads>
+// kV: groups of eight columns a thread owns.  With two, what a row costs beside its elements (sums over its threads, addresses) counts half; the
+// biases are then kept in shared memory, where only their own thread reads them.
+template <typename T, typename R, bool kAligned, int kIn, bool kBias, int kV, int kThreads>
 __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 2) block_forward_kernel(BlockArgs p) {
     extern __shared__ __align__(16) uint8_t smem[];
     __shared__ RowShared row_shared;
-    constexpr int kPieces = fwd_pieces<T, R, kBranch>(), kStages = stages_for(kPieces);
-    constexpr uint32_t kX = 0, kO = sizeof(R) / 2 * kThreads * 16, kG = kO + sizeof(T) / 2 * kThreads * 16, kStage = kPieces * kThreads * 16;
+    constexpr bool kBranch = kIn != kAlone;
+    constexpr int kPieces = fwd_pieces<T, R, kIn>() * kV, kStages = stages_for(kPieces);
+    constexpr uint32_t kSlotR = sizeof(R) / 2 * kThreads * 16, kSlotT = sizeof(T) / 2 * kThreads * 16;
+    constexpr uint32_t kX = 0, kO = kV * kSlotR, kG = kO + kV * kSlotT, kStage = kPieces * kThreads * 16;
     const int lane = threadIdx.x & (p.tpr - 1), per_turn = kThreads / p.tpr, mine = threadIdx.x / p.tpr;
-    const Columns<kAligned> c(lane, p.tpr, p.C, blockIdx.y * 8 * kThreads);
-    RowGroup grp(p.tpr, p.cluster, &row_shared);
-    const Piece piece(p);
-    const bool gate_row = kBranch && p.gate && !p.grouped;
+    Columns<kAligned> c[kV];
     int mine_n = 0;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) mine_n += c.has(j) ? 1 : 0;
+    for (int g = 0; g < kV; ++g) {
+        c[g] = Columns<kAligned>(lane + g * p.tpr, p.tpr, p.C, blockIdx.y * 8 * kV * kThreads);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) mine_n += c[g].has(j) ? 1 : 0;
+    }
+    RowGroup grp(p.tpr, p.cluster, &row_shared);
+    const Piece piece(p);
+    constexpr bool gate_row = kIn == kGated;
     const float in_warp = grp.within_warp((float)mine_n);
     ptx::grid_launch();
     ptx::grid_wait();
 
-    float2 sw[4], sb[4], w[4], b[4];
-    if constexpr (kBranch) {
-        float2 s[4];
-        load_param(p.scale, 1.f, c, s);
-        load_param(p.w_post, 1.f, c, sw);
-        load_param(p.b_post, 0.f, c, sb);
+    constexpr bool kBiasSlots = kBias && kV == 2;
+    const uint32_t slots = ptx::smem_u32(smem) + threadIdx.x * 16, bias_slots = slots + kStages * kStage;   // [post, pre][group][half][thread]
+    float2 sw[kV][4], sb[kV][4], w[kV][4], b[kV][4], a[kV][4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) { sw[i] = f2_mul(sw[i], s[i]); sb[i] = f2_mul(sb[i], s[i]); }
-    }
-    load_param(p.w_pre, 1.f, c, w);
-    load_param(p.b_pre, 0.f, c, b);
-    float2 a[4] = {f2(1.f), f2(1.f), f2(1.f), f2(1.f)};
-    if constexpr (kBranch) {
-        if (p.gate && p.grouped) {
-            unpack8(load8(static_cast<const T *>(p.g) + piece.group * p.ld_g, c), a);
+    for (int g = 0; g < kV; ++g) {
+        if constexpr (kBranch) {
+            float2 s[4];
+            load_param(p.scale, 1.f, c[g], s);
+            load_param(p.w_post, 1.f, c[g], sw[g]);
+            if constexpr (kBias) load_param(p.b_post, 0.f, c[g], sb[g]);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) a[i] = make_float2(gate_act(p.gate, a[i].x), gate_act(p.gate, a[i].y));
+            for (int i = 0; i < 4; ++i) {
+                sw[g][i] = f2_mul(sw[g][i], s[i]);
+                if constexpr (kBias) sb[g][i] = f2_mul(sb[g][i], s[i]);
+                a[g][i] = f2(1.f);
+            }
+            if constexpr (kIn == kShared) {
+                unpack8(load8(static_cast<const T *>(p.g) + piece.group * p.ld_g, c[g]), a[g]);
+                gate_act8(p.gate, a[g]);
+            }
+        }
+        load_param(p.w_pre, 1.f, c[g], w[g]);
+        if constexpr (kBias) load_param(p.b_pre, 0.f, c[g], b[g]);
+        if constexpr (kBiasSlots) {
+            if constexpr (kBranch) slot_write<kThreads>(bias_slots + g * 2 * kThreads * 16, sb[g]);
+            slot_write<kThreads>(bias_slots + (kV + g) * 2 * kThreads * 16, b[g]);
         }
     }
 
-    const uint32_t slots = ptx::smem_u32(smem) + threadIdx.x * 16;
-    auto fetch = [&](long row, int stage) {
+    // loads run kStages - 1 turns ahead of the rows: pointers to the next row to ask for, and rows left from there
+    const char *from_x = nullptr, *from_o = nullptr, *from_g = nullptr;
+    const long row0 = piece.begin + mine, step_x = per_turn * p.ld_x * (long)sizeof(R), step_o = per_turn * p.ld_o * (long)sizeof(T), step_g = per_turn * p.ld_g * (long)sizeof(T);
+    const int columns = c[0].any() ? c[0].first : 0, apart = 8 * p.tpr;
+    int ahead = (int)(piece.end - row0);
+    if constexpr (kAligned) {
+        from_x = reinterpret_cast<const char *>(static_cast<const R *>(p.x) + row0 * p.ld_x + columns);
+        if constexpr (kBranch) {
+            from_o = reinterpret_cast<const char *>(static_cast<const T *>(p.o) + row0 * p.ld_o + columns);
+            if constexpr (gate_row) from_g = reinterpret_cast<const char *>(static_cast<const T *>(p.g) + row0 * p.ld_g + columns);
+        }
+    }
+    auto fetch = [&](int stage) {
         if constexpr (kAligned) {
-            const bool yes = row < piece.end && c.any();
-            const long r = yes ? row : piece.begin;
-            const int col = yes ? c.first : 0;
             const uint32_t s = slots + stage * kStage;
-            slot_copy<R, kThreads>(s + kX, static_cast<const R *>(p.x) + r * p.ld_x, col, yes);
-            if constexpr (kBranch) {
-                slot_copy<T, kThreads>(s + kO, static_cast<const T *>(p.o) + r * p.ld_o, col, yes);
-                if (gate_row) slot_copy<T, kThreads>(s + kG, static_cast<const T *>(p.g) + r * p.ld_g, col, yes);
+#pragma unroll
+            for (int g = 0; g < kV; ++g) {
+                const bool yes = ahead > 0 && c[g].any();
+                slot_copy<R, kThreads>(s + kX + g * kSlotR, from_x + g * apart * (int)sizeof(R), yes);
+                if constexpr (kBranch) {
+                    slot_copy<T, kThreads>(s + kO + g * kSlotT, from_o + g * apart * (int)sizeof(T), yes);
+                    if constexpr (gate_row) slot_copy<T, kThreads>(s + kG + g * kSlotT, from_g + g * apart * (int)sizeof(T), yes);
+                }
             }
             ptx::copy_async_commit();
+            ahead -= per_turn;
+            from_x += step_x;
+            if constexpr (kBranch) {
+                from_o += step_o;
+                if constexpr (gate_row) from_g += step_g;
+            }
         }
     };
     if constexpr (kAligned)
-        for (int k = 0; k < kStages - 1; ++k) fetch(piece.begin + (long)k * per_turn + mine, k);
+        for (int k = 0; k < kStages - 1; ++k) fetch(k);
 
     int stage = 0;
-    for (long r0 = piece.begin; r0 < piece.end; r0 += per_turn) {
-        const long row = r0 + mine;
+    for (long row = row0; row - mine < piece.end; row += per_turn) {
         const bool live = row < piece.end;
-        float2 y[4];
+        float2 y[kV][4];
+        const uint32_t s = slots + stage * kStage;
         if constexpr (kAligned) {
-            fetch(row + (long)(kStages - 1) * per_turn, stage == 0 ? kStages - 1 : stage - 1);
+            fetch(stage == 0 ? kStages - 1 : stage - 1);
             ptx::copy_async_wait<kStages - 1>();
-            unpack8(slot_read<R, kThreads>(slots + stage * kStage + kX), y);
-        } else {
-            unpack8(load8(static_cast<const R *>(p.x) + row * p.ld_x, c, live), y);
+        }
+#pragma unroll
+        for (int g = 0; g < kV; ++g) {
+            if constexpr (kAligned) unpack8(slot_read<R, kThreads>(s + kX + g * kSlotR), y[g]);
+            else unpack8(load8(static_cast<const R *>(p.x) + row * p.ld_x, c[g], live), y[g]);
         }
         float2 st_o = make_float2(0.f, 0.f);
         if constexpr (kBranch) {
-            float2 o[4];
-            if constexpr (kAligned) {
-                unpack8(slot_read<T, kThreads>(slots + stage * kStage + kO), o);
-                if (gate_row) unpack8(slot_read<T, kThreads>(slots + stage * kStage + kG), a);
-            } else {
-                unpack8(load8(static_cast<const T *>(p.o) + row * p.ld_o, c, live), o);
-                if (gate_row) unpack8(load8(static_cast<const T *>(p.g) + row * p.ld_g, c, live), a);
-            }
-            if (gate_row) {
+            float2 o[kV][4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) a[i] = make_float2(gate_act(p.gate, a[i].x), gate_act(p.gate, a[i].y));
+            for (int g = 0; g < kV; ++g) {
+                if constexpr (kAligned) {
+                    unpack8(slot_read<T, kThreads>(s + kO + g * kSlotT), o[g]);
+                    if constexpr (gate_row) unpack8(slot_read<T, kThreads>(s + kG + g * kSlotT), a[g]);
+                } else {
+                    unpack8(load8(static_cast<const T *>(p.o) + row * p.ld_o, c[g], live), o[g]);
+                    if constexpr (gate_row) unpack8(load8(static_cast<const T *>(p.g) + row * p.ld_g, c[g], live), a[g]);
+                }
+                if constexpr (gate_row) gate_act8(p.gate, a[g]);
             }
-            if (p.has_post) {
-                st_o = moments(grp, o, c, in_warp, p.layer_post, p.inv_c, p.eps_post);
+            if (p.has_post) st_o = moments<kV>(grp, o, c, in_warp, p.layer_post, p.inv_c, p.eps_post);
+            const float mean = -st_o.x, rstd = p.has_post ? st_o.y : 1.f;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) o[i] = f2_mul(f2_add(o[i], f2(-st_o.x)), f2(st_o.y));
+            for (int g = 0; g < kV; ++g) {
+                if constexpr (kBiasSlots) unpack8(slot_read<float, kThreads>(bias_slots + g * 2 * kThreads * 16), sb[g]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float2 n = f2_mul(f2_add(o[g][i], f2(mean)), f2(rstd));
+                    const float2 v = kBias ? f2_fma(n, sw[g][i], sb[g][i]) : f2_mul(n, sw[g][i]);
+                    y[g][i] = f2_fma(y[g][i], f2(p.alpha), kIn == kPlain ? v : f2_mul(v, a[g][i]));
+                }
+                if (live) store8(static_cast<R *>(p.y) + row * p.ld_y, c[g], y[g]);
             }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) y[i] = f2_fma(f2_fma(o[i], sw[i], sb[i]), a[i], f2_mul(y[i], f2(p.alpha)));
-            if (live) store8(static_cast<R *>(p.y) + row * p.ld_y, c, y);
         }
         float2 st_y = make_float2(0.f, 0.f);
         if (p.has_pre) {
-            st_y = moments(grp, y, c, in_warp, p.layer_pre, p.inv_c, p.eps_pre);
+            st_y = moments<kV>(grp, y, c, in_warp, p.layer_pre, p.inv_c, p.eps_pre);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) y[i] = f2_fma(f2_mul(f2_add(y[i], f2(-st_y.x)), f2(st_y.y)), w[i], b[i]);
-            if (live) store8(static_cast<T *>(p.h) + row * p.ld_h, c, y);
+            for (int g = 0; g < kV; ++g) {
+                if constexpr (kBiasSlots) unpack8(slot_read<float, kThreads>(bias_slots + (kV + g) * 2 * kThreads * 16), b[g]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float2 n = f2_mul(f2_add(y[g][i], f2(-st_y.x)), f2(st_y.y));
+                    y[g][i] = kBias ? f2_fma(n, w[g][i], b[g][i]) : f2_mul(n, w[g][i]);
+                }
+                if (live) store8(static_cast<T *>(p.h) + row * p.ld_h, c[g], y[g]);
+            }
         }
         if (live && lane == 0 && blockIdx.y == 0 && p.stats) p.stats[row] = make_float4(st_o.x, st_o.y, st_y.x, st_y.y);
         stage = stage + 1 == kStages ? 0 : stage + 1;
@@ -379,18 +472,19 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 2) block_forwa
 // Sums over rows: [0] dh y^, [1] Q, [2] dh, [3] P; without biases the first two, without a branch [0] and [2].
 template <bool kBranch, bool kBias> __host__ __device__ constexpr int bwd_sums() { return (kBranch ? 2 : 1) * (kBias ? 2 : 1); }
 
-template <typename T, typename R, bool kAligned, bool kBranch, bool kBias, int kThreads>
+template <typename T, typename R, bool kAligned, int kIn, bool kBias, int kThreads>
 __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 2) block_backward_kernel(BlockArgs p) {
     extern __shared__ __align__(16) uint8_t smem[];
     __shared__ RowShared row_shared;
-    constexpr int kPieces = bwd_pieces<T, R, kBranch>(), kStages = stages_for(kPieces), kSums = bwd_sums<kBranch, kBias>();
+    constexpr bool kBranch = kIn != kAlone;
+    constexpr int kPieces = bwd_pieces<T, R, kIn>(), kStages = stages_for(kPieces), kSums = bwd_sums<kBranch, kBias>();
     constexpr uint32_t kOneR = sizeof(R) / 2 * kThreads * 16, kOneT = sizeof(T) / 2 * kThreads * 16;
     constexpr uint32_t kY = 0, kDy = kOneR, kDh = 2 * kOneR, kO = kDh + kOneT, kG = kO + kOneT, kStage = kPieces * kThreads * 16;
     const int lane = threadIdx.x & (p.tpr - 1), per_turn = kThreads / p.tpr, mine = threadIdx.x / p.tpr;
     const Columns<kAligned> c(lane, p.tpr, p.C, blockIdx.y * 8 * kThreads);
     RowGroup grp(p.tpr, p.cluster, &row_shared);
     const Piece piece(p);
-    const bool gate_row = kBranch && p.gate && !p.grouped;
+    constexpr bool gate_row = kIn == kGated;
     ptx::grid_launch();
     ptx::grid_wait();
 
@@ -410,10 +504,9 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 2) block_backw
     load_param(p.w_pre, 1.f, c, w);
     float2 a[4] = {f2(1.f), f2(1.f), f2(1.f), f2(1.f)};
     if constexpr (kBranch) {
-        if (p.gate && p.grouped) {
+        if constexpr (kIn == kShared) {
             unpack8(load8(static_cast<const T *>(p.g) + piece.group * p.ld_g, c), a);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) a[i] = make_float2(gate_act(p.gate, a[i].x), gate_act(p.gate, a[i].y));
+            gate_act8(p.gate, a);
         }
     }
     float2 sum[kSums][4];
@@ -422,27 +515,40 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 2) block_backw
 #pragma unroll
         for (int i = 0; i < 4; ++i) sum[k][i] = f2(0.f);
 
+    // loads run kStages - 1 turns ahead of the rows: pointers to the next row to ask for, and rows left from there
     const uint32_t slots = ptx::smem_u32(smem) + threadIdx.x * 16;
-    auto fetch = [&](long row, int stage) {
+    const char *from_y = nullptr, *from_dy = nullptr, *from_dh = nullptr, *from_o = nullptr, *from_g = nullptr;
+    const long first = piece.begin + mine;
+    int ahead = (int)(piece.end - first);
+    if constexpr (kAligned) {
+        const int columns = c.any() ? c.first : 0;
+        auto at = [&](const void *t, long ld, size_t size) { return static_cast<const char *>(t) + (first * ld + columns) * (long)size; };
+        from_y = at(p.x, p.ld_x, sizeof(R)); from_dy = at(p.dy, p.ld_dy, sizeof(R)); from_dh = at(p.dh, p.ld_dh, sizeof(T));
+        if constexpr (kBranch) from_o = at(p.o, p.ld_o, sizeof(T));
+        if constexpr (gate_row) from_g = at(p.g, p.ld_g, sizeof(T));
+    }
+    auto fetch = [&](int stage) {
         if constexpr (kAligned) {
-            const bool yes = row < piece.end && c.any();
-            const long r = yes ? row : piece.begin;
-            const int col = yes ? c.first : 0;
+            const bool yes = ahead > 0 && c.any();
             const uint32_t s = slots + stage * kStage;
             if (p.has_pre) {
-                slot_copy<R, kThreads>(s + kY, static_cast<const R *>(p.x) + r * p.ld_x, col, yes);
-                slot_copy<T, kThreads>(s + kDh, static_cast<const T *>(p.dh) + r * p.ld_dh, col, yes);
+                slot_copy<R, kThreads>(s + kY, from_y, yes);
+                slot_copy<T, kThreads>(s + kDh, from_dh, yes);
             }
-            if (p.dy) slot_copy<R, kThreads>(s + kDy, static_cast<const R *>(p.dy) + r * p.ld_dy, col, yes);
+            if (p.dy) slot_copy<R, kThreads>(s + kDy, from_dy, yes);
             if constexpr (kBranch) {
-                slot_copy<T, kThreads>(s + kO, static_cast<const T *>(p.o) + r * p.ld_o, col, yes);
-                if (gate_row) slot_copy<T, kThreads>(s + kG, static_cast<const T *>(p.g) + r * p.ld_g, col, yes);
+                slot_copy<T, kThreads>(s + kO, from_o, yes);
+                if constexpr (gate_row) slot_copy<T, kThreads>(s + kG, from_g, yes);
             }
             ptx::copy_async_commit();
+            ahead -= per_turn;
+            from_y += per_turn * p.ld_x * (long)sizeof(R); from_dy += per_turn * p.ld_dy * (long)sizeof(R); from_dh += per_turn * p.ld_dh * (long)sizeof(T);
+            if constexpr (kBranch) from_o += per_turn * p.ld_o * (long)sizeof(T);
+            if constexpr (gate_row) from_g += per_turn * p.ld_g * (long)sizeof(T);
         }
     };
     if constexpr (kAligned)
-        for (int k = 0; k < kStages - 1; ++k) fetch(piece.begin + (long)k * per_turn + mine, k);
+        for (int k = 0; k < kStages - 1; ++k) fetch(k);
     const float4 none = make_float4(0.f, 0.f, 0.f, 0.f);
     float4 st_next = piece.begin + mine < piece.end ? p.stats[piece.begin + mine] : none;
 
@@ -455,7 +561,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 2) block_backw
         else st_next = none;
         const uint32_t s0 = slots + stage * kStage;
         if constexpr (kAligned) {
-            fetch(row + (long)(kStages - 1) * per_turn, stage == 0 ? kStages - 1 : stage - 1);
+            fetch(stage == 0 ? kStages - 1 : stage - 1);
             ptx::copy_async_wait<kStages - 1>();
         }
         float2 dt[4] = {f2(0.f), f2(0.f), f2(0.f), f2(0.f)};
@@ -482,7 +588,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 2) block_backw
                 c1 = f2_fma(t[i], yh[i], c1);
                 c2 = f2_add(c2, t[i]);
             }
-            float2 means = grp.sum2(c1.x + c1.y, p.layer_pre ? c2.x + c2.y : 0.f);
+            float2 means = p.layer_pre ? grp.sum<true>(c1.x + c1.y, c2.x + c2.y) : grp.sum<false>(c1.x + c1.y, 0.f);
             means.x *= -p.inv_c; means.y *= -p.inv_c;
 #pragma unroll
             for (int i = 0; i < 4; ++i) dt[i] = f2_fma(f2_fma(yh[i], f2(means.x), f2_add(t[i], f2(means.y))), f2(st.w), dt[i]);
@@ -495,33 +601,30 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 2) block_backw
             float2 o[4];
             if constexpr (kAligned) {
                 unpack8(slot_read<T, kThreads>(s0 + kO), o);
-                if (gate_row) unpack8(slot_read<T, kThreads>(s0 + kG), a);
+                if constexpr (gate_row) unpack8(slot_read<T, kThreads>(s0 + kG), a);
             } else {
                 unpack8(load8(static_cast<const T *>(p.o) + row * p.ld_o, c, live), o);
-                if (gate_row) unpack8(load8(static_cast<const T *>(p.g) + row * p.ld_g, c, live), a);
+                if constexpr (gate_row) unpack8(load8(static_cast<const T *>(p.g) + row * p.ld_g, c, live), a);
             }
             if (p.has_post) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) o[i] = f2_mul(f2_add(o[i], f2(-st.x)), f2(st.y));
             }
-            if (gate_row) {
+            if constexpr (gate_row) {
                 float2 dg[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    float2 n = f2_mul(o[i], sw[i]);
-                    if constexpr (kBias) n = f2_add(n, sb[i]);
-                    dg[i] = f2_mul(dt[i], n);
-                    if (p.gate == 1) {
-                        a[i] = make_float2(gate_act(1, a[i].x), gate_act(1, a[i].y));
-                        dg[i] = f2_mul(dg[i], f2_mul(a[i], f2_fma(a[i], f2(-1.f), f2(1.f))));
-                    }
+                for (int i = 0; i < 4; ++i) dg[i] = f2_mul(dt[i], kBias ? f2_fma(o[i], sw[i], sb[i]) : f2_mul(o[i], sw[i]));
+                if (p.gate == 1) {
+                    gate_act8(1, a);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) dg[i] = f2_mul(dg[i], f2_mul(a[i], f2_fma(a[i], f2(-1.f), f2(1.f))));
                 }
                 if (live) store8(static_cast<T *>(p.dg) + row * p.ld_dg, c, dg);
             }
             float2 d1 = f2(0.f), d2 = f2(0.f), u[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float2 q = f2_mul(dt[i], a[i]), k = p.grouped ? dt[i] : q;
+                const float2 q = kIn == kPlain ? dt[i] : f2_mul(dt[i], a[i]), k = kIn == kShared ? dt[i] : q;
                 sum[1][i] = f2_fma(k, o[i], sum[1][i]);
                 if constexpr (kBias) sum[3][i] = f2_add(sum[3][i], k);
                 u[i] = f2_mul(q, sw[i]);
@@ -529,7 +632,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 2) block_backw
                 d2 = f2_add(d2, u[i]);
             }
             if (p.has_post) {
-                float2 means = grp.sum2(d1.x + d1.y, p.layer_post ? d2.x + d2.y : 0.f);
+                float2 means = p.layer_post ? grp.sum<true>(d1.x + d1.y, d2.x + d2.y) : grp.sum<false>(d1.x + d1.y, 0.f);
                 means.x *= -p.inv_c; means.y *= -p.inv_c;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) u[i] = f2_mul(f2_fma(o[i], f2(means.x), f2_add(u[i], f2(means.y))), f2(st.y));
@@ -573,69 +676,74 @@ struct BlockSums {
     long groups, ld_g, ld_dg;
     int chunks, C, sums, branch, bias, gate, grouped;
 };
-constexpr int kSumLanes = 32, kSumSlices = 16;
+constexpr int kSumLanes = 32, kSumSlices = 32;
 
-// A block has 32 columns and 16 slices of the partial rows: slices of a group's pieces where there are few groups, else of the groups.
+// A block has 32 columns and 32 slices of the partial rows (of a group's pieces where there are few groups, else of the groups), of the sums that
+// go with the next norm (blockIdx.y = 0: dh y^, dh) or with the branch (1: Q, P).
 template <typename T>
 __global__ void __launch_bounds__(kSumLanes * kSumSlices) block_sums_kernel(BlockSums p) {
-    __shared__ float sh[4][kSumSlices][kSumLanes];
+    __shared__ float2 sh[kSumSlices][kSumLanes];
     const int lane = threadIdx.x % kSumLanes, slice = threadIdx.x / kSumLanes, col = blockIdx.x * kSumLanes + lane;
+    const bool branch = blockIdx.y == 1, yes = col < p.C;
+    const int first = branch ? 1 : 0, second = (p.branch ? 2 : 1) + first;   // the two sums' places in a partial row
     int sub = kSumSlices;                                   // slices of one group
     while (sub > 1 && (long)(kSumSlices / sub) < p.groups) sub >>= 1;
     const int at_once = kSumSlices / sub, slot = slice / sub, part = slice % sub;
     ptx::grid_wait();
-    float total[4] = {0.f, 0.f, 0.f, 0.f};
-    const bool yes = col < p.C;
     const float s = yes && p.scale ? p.scale[col] : 1.f, w = yes && p.w_post ? p.w_post[col] : 1.f, b = yes && p.b_post ? p.b_post[col] : 0.f;
+    float2 total = make_float2(0.f, 0.f);
     for (long g0 = 0; g0 < p.groups; g0 += at_once) {
         const long grp = g0 + slot;
-        float v[4] = {0.f, 0.f, 0.f, 0.f};
+        float2 v = make_float2(0.f, 0.f);
         if (yes && grp < p.groups) {
-            const float *src = p.part + (size_t)grp * p.chunks * p.sums * p.C + col;
-#pragma unroll 4
-            for (int ch = part; ch < p.chunks; ch += sub)
-                for (int k = 0; k < 4; ++k)
-                    if (k < p.sums) v[k] += src[((size_t)ch * p.sums + k) * p.C];
+            const float *src = p.part + ((size_t)grp * p.chunks * p.sums + first) * p.C + col;
+            const size_t row = (size_t)p.sums * p.C, other = (size_t)(second - first) * p.C;
+            if (p.bias) {
+#pragma unroll 8
+                for (int ch = part; ch < p.chunks; ch += sub) {
+                    v.x += src[ch * row];
+                    v.y += src[ch * row + other];
+                }
+            } else {
+#pragma unroll 8
+                for (int ch = part; ch < p.chunks; ch += sub) v.x += src[ch * row];
+            }
         }
-        if (p.grouped) {
+        if (p.grouped && branch) {
             // the group's own sums: one thread per column puts the slices together
             if (sub > 1) {
-                for (int k = 0; k < p.sums; ++k) sh[k][slice][lane] = v[k];
+                sh[slice][lane] = v;
                 __syncthreads();
                 if (part == 0)
-                    for (int k = 0; k < p.sums; ++k)
-                        for (int q = 1; q < sub; ++q) v[k] += sh[k][slice + q][lane];
+                    for (int q = 1; q < sub; ++q) v = f2_add(v, sh[slice + q][lane]);
                 __syncthreads();
             }
             if (part == 0 && yes && grp < p.groups) {
-                const float Q = v[1], P = p.bias ? v[3] : 0.f;
                 const float g = to_f32(static_cast<const T *>(p.g)[grp * p.ld_g + col]), a = gate_act(p.gate, g);
                 const float slope = p.gate == 1 ? a * (1.f - a) : 1.f;
-                from_f32(static_cast<T *>(p.dg)[grp * p.ld_dg + col], s * slope * fmaf(w, Q, b * P));
-                v[1] = a * Q; v[3] = a * P;
+                from_f32(static_cast<T *>(p.dg)[grp * p.ld_dg + col], s * slope * fmaf(w, v.x, b * v.y));
+                v = f2_mul(v, f2(a));
             } else {
-                v[0] = v[1] = v[2] = v[3] = 0.f;
+                v = make_float2(0.f, 0.f);
             }
         }
-#pragma unroll
-        for (int k = 0; k < 4; ++k) total[k] += v[k];
+        total = f2_add(total, v);
     }
-#pragma unroll
-    for (int k = 0; k < 4; ++k) sh[k][slice][lane] = total[k];
+    sh[slice][lane] = total;
     __syncthreads();
-    if (slice != 0 || !yes) return;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        total[k] = 0.f;
-        for (int q = 0; q < kSumSlices; ++q) total[k] += sh[k][q][lane];
+    for (int half = kSumSlices / 2; half > 1; half >>= 1) {
+        if (slice < half) sh[slice][lane] = f2_add(sh[slice][lane], sh[slice + half][lane]);
+        __syncthreads();
     }
-    if (p.dw_pre) p.dw_pre[col] = total[0];
-    if (p.db_pre) p.db_pre[col] = total[p.branch ? 2 : 1];
-    if (p.branch) {
-        const float Q = total[1], P = p.bias ? total[3] : 0.f;
-        if (p.d_scale) p.d_scale[col] = fmaf(w, Q, b * P);
-        if (p.dw_post) p.dw_post[col] = s * Q;
-        if (p.db_post) p.db_post[col] = s * P;
+    if (slice != 0 || !yes) return;
+    total = f2_add(sh[0][lane], sh[1][lane]);
+    if (!branch) {
+        if (p.dw_pre) p.dw_pre[col] = total.x;
+        if (p.db_pre) p.db_pre[col] = total.y;
+    } else {
+        if (p.d_scale) p.d_scale[col] = fmaf(w, total.x, b * total.y);
+        if (p.dw_post) p.dw_post[col] = s * total.x;
+        if (p.db_post) p.db_post[col] = s * total.y;
     }
 }
 

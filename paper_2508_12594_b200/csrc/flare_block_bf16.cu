@@ -1,11 +1,9 @@
-// Kernels around a block, bfloat16 branch.
+// Kernels around a block: bfloat16 branch, bfloat16 residual stream.
 #define FLARE_BLOCK_INSTANTIATE
 #include "flare_block_launch.cuh"
 
 namespace flare {
-template int block_forward<__nv_bfloat16, __nv_bfloat16>(BlockArgs, bool, bool, const BlockPlan &, cudaStream_t);
-template int block_backward<__nv_bfloat16, __nv_bfloat16>(BlockArgs, bool, bool, bool, const BlockPlan &, cudaStream_t);
-template int block_forward<__nv_bfloat16, float>(BlockArgs, bool, bool, const BlockPlan &, cudaStream_t);
-template int block_backward<__nv_bfloat16, float>(BlockArgs, bool, bool, bool, const BlockPlan &, cudaStream_t);
+template int block_forward<__nv_bfloat16, __nv_bfloat16>(const BlockArgs &, bool, int, cudaStream_t);
+template int block_backward<__nv_bfloat16, __nv_bfloat16>(const BlockArgs &, bool, bool, const BlockPlan &, cudaStream_t);
 template int block_sums<__nv_bfloat16>(const BlockSums &, cudaStream_t);
 }  // namespace flare

@@ -1,5 +1,5 @@
 // Launches of the kernels around a block (flare_block.cuh) for one pair of types: T of the branch, the gate and the normalised rows,
-// R of the residual stream.  Instantiated by flare_block_{bf16,f16,f32}.cu.
+// R of the residual stream.  Instantiated by flare_block_{bf16,bf16_f32,f16,f16_f32,f32}.cu.
 #pragma once
 
 #include "flare_block.cuh"
@@ -12,17 +12,18 @@ namespace flare {
 constexpr int kBlockMaxWidth = 16384;
 // A block's rows: pieces of the groups, together about as many as fill the chip once.
 struct BlockPlan {
-    int tpr, threads, cluster;
+    int tpr, threads, cluster, vectors;                     // vectors: groups of eight columns a thread owns
     long groups, chunk;
     int chunks;
 };
-inline BlockPlan block_plan(long rows, long group, int C, bool aligned, int sms) {
+inline BlockPlan block_plan(long rows, long group, int C, bool aligned, int sms, int vectors = 1) {
     BlockPlan p;
-    p.threads = aligned && C > 2048 ? 512 : 256;
-    p.tpr = 8;
-    while (p.tpr * 8 < C && p.tpr < p.threads) p.tpr *= 2;
+    p.vectors = vectors;
+    p.threads = aligned && C > 2048 * vectors ? 512 : 256;
+    p.tpr = 4;
+    while (p.tpr * 8 * vectors < C && p.tpr < p.threads) p.tpr *= 2;
     p.cluster = 1;
-    while (p.cluster * p.threads * 8 < C) p.cluster *= 2;
+    while (p.cluster * p.threads * 8 * vectors < C) p.cluster *= 2;
     const long turn = p.threads / p.tpr, fit = (p.threads == 512 ? 1 : 2) * (long)sms / p.cluster;
     p.groups = rows / group;
     const long pieces = std::max(1L, std::min(fit / std::max(1L, p.groups), (group + turn - 1) / turn));
@@ -31,15 +32,15 @@ inline BlockPlan block_plan(long rows, long group, int C, bool aligned, int sms)
     return p;
 }
 
-template <typename T, typename R> int block_forward(BlockArgs a, bool aligned, bool branch, const BlockPlan &plan, cudaStream_t st);
-template <typename T, typename R> int block_backward(BlockArgs a, bool aligned, bool branch, bool bias, const BlockPlan &plan, cudaStream_t st);
+template <typename T, typename R> int block_forward(const BlockArgs &a, bool aligned, int sms, cudaStream_t st);
+template <typename T, typename R> int block_backward(const BlockArgs &a, bool aligned, bool bias, const BlockPlan &plan, cudaStream_t st);
 template <typename T> int block_sums(const BlockSums &s, cudaStream_t st);
 
 #ifdef FLARE_BLOCK_INSTANTIATE
 template <typename Kernel>
 int block_launch(Kernel kernel, std::atomic<uint64_t> &opt_in, BlockArgs a, const BlockPlan &p, size_t smem, cudaStream_t st) {
     a.tpr = p.tpr; a.chunk = p.chunk; a.chunks = p.chunks; a.cluster = p.cluster;
-    if (int rc = ensure_big_smem(kernel, opt_in, 200 * 1024)) return rc;
+    if (int rc = ensure_big_smem(kernel, opt_in, 224 * 1024)) return rc;
     cudaLaunchAttribute attr[2] = {};
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
@@ -53,41 +54,62 @@ int block_launch(Kernel kernel, std::atomic<uint64_t> &opt_in, BlockArgs a, cons
     return FLARE_OK;
 }
 
-template <typename T, typename R, bool kAligned, bool kBranch, int kThreads>
+template <typename T, typename R, bool kAligned, int kIn, bool kBias, int kV, int kThreads>
 int block_forward_as(const BlockArgs &a, const BlockPlan &p, cudaStream_t st) {
     static std::atomic<uint64_t> opt_in{0};
-    constexpr int pieces = fwd_pieces<T, R, kBranch>();
-    return block_launch(block_forward_kernel<T, R, kAligned, kBranch, kThreads>, opt_in, a, p, kAligned ? (size_t)stages_for(pieces) * pieces * 16 * kThreads : 0, st);
+    constexpr int pieces = fwd_pieces<T, R, kIn>() * kV, bias_slots = kBias && kV == 2 ? 4 * kV : 0;
+    return block_launch(block_forward_kernel<T, R, kAligned, kIn, kBias, kV, kThreads>, opt_in, a, p,
+                        kAligned ? (size_t)(stages_for(pieces) * pieces + bias_slots) * 16 * kThreads : 0, st);
 }
+template <typename T, typename R, int kIn, bool kBias, int kV>
+int block_forward_aligned(const BlockArgs &a, const BlockPlan &p, cudaStream_t st) {
+    return p.threads == 512 ? block_forward_as<T, R, true, kIn, kBias, kV, 512>(a, p, st) : block_forward_as<T, R, true, kIn, kBias, kV, 256>(a, p, st);
+}
+template <typename T, typename R, int kIn>
+int block_forward_of(const BlockArgs &a, bool aligned, int sms, cudaStream_t st) {
+    constexpr int kV = sizeof(T) == 2 ? 2 : 1;              // (float32: its loads fill shared memory with one group of columns a thread)
+    const BlockPlan p = block_plan(a.rows, a.group, a.C, aligned, sms, aligned ? kV : 1);
+    // (rows that are moved one element at a time: always the form with biases, here and in the backward)
+    if (!aligned) return block_forward_as<T, R, false, kIn, true, 1, 256>(a, p, st);
+    return a.b_post || a.b_pre ? block_forward_aligned<T, R, kIn, true, kV>(a, p, st) : block_forward_aligned<T, R, kIn, false, kV>(a, p, st);
+}
+inline int block_input(const BlockArgs &a) { return a.o == nullptr ? kAlone : !a.gate ? kPlain : a.grouped ? kShared : kGated; }
 template <typename T, typename R>
-int block_forward(BlockArgs a, bool aligned, bool branch, const BlockPlan &p, cudaStream_t st) {
-    if (!aligned) return branch ? block_forward_as<T, R, false, true, 256>(a, p, st) : block_forward_as<T, R, false, false, 256>(a, p, st);
-    if (p.threads == 512) return branch ? block_forward_as<T, R, true, true, 512>(a, p, st) : block_forward_as<T, R, true, false, 512>(a, p, st);
-    return branch ? block_forward_as<T, R, true, true, 256>(a, p, st) : block_forward_as<T, R, true, false, 256>(a, p, st);
+int block_forward(const BlockArgs &a, bool aligned, int sms, cudaStream_t st) {
+    switch (block_input(a)) {
+        case kAlone: return block_forward_of<T, R, kAlone>(a, aligned, sms, st);
+        case kPlain: return block_forward_of<T, R, kPlain>(a, aligned, sms, st);
+        case kGated: return block_forward_of<T, R, kGated>(a, aligned, sms, st);
+        default: return block_forward_of<T, R, kShared>(a, aligned, sms, st);
+    }
 }
 
-template <typename T, typename R, bool kAligned, bool kBranch, bool kBias, int kThreads>
+template <typename T, typename R, bool kAligned, int kIn, bool kBias, int kThreads>
 int block_backward_as(const BlockArgs &a, const BlockPlan &p, cudaStream_t st) {
     static std::atomic<uint64_t> opt_in{0};
-    constexpr int pieces = bwd_pieces<T, R, kBranch>(), sums = bwd_sums<kBranch, kBias>();
+    constexpr int pieces = bwd_pieces<T, R, kIn>(), sums = bwd_sums<kIn != kAlone, kBias>();
     const size_t meet = (size_t)(kThreads / std::max(p.tpr, 32)) * sums * 8 * p.tpr * sizeof(float);
     const size_t smem = std::max(kAligned ? (size_t)stages_for(pieces) * pieces * 16 * kThreads : 0, meet);
-    return block_launch(block_backward_kernel<T, R, kAligned, kBranch, kBias, kThreads>, opt_in, a, p, smem, st);
+    return block_launch(block_backward_kernel<T, R, kAligned, kIn, kBias, kThreads>, opt_in, a, p, smem, st);
+}
+template <typename T, typename R, int kIn>
+int block_backward_of(const BlockArgs &a, bool aligned, bool bias, const BlockPlan &p, cudaStream_t st) {
+    if (!aligned) return block_backward_as<T, R, false, kIn, true, 256>(a, p, st);
+    if (p.threads == 512) return bias ? block_backward_as<T, R, true, kIn, true, 512>(a, p, st) : block_backward_as<T, R, true, kIn, false, 512>(a, p, st);
+    return bias ? block_backward_as<T, R, true, kIn, true, 256>(a, p, st) : block_backward_as<T, R, true, kIn, false, 256>(a, p, st);
 }
 template <typename T, typename R>
-int block_backward(BlockArgs a, bool aligned, bool branch, bool bias, const BlockPlan &p, cudaStream_t st) {
-    // (rows that are moved one element at a time: always the form with sums for biases)
-    if (!aligned) return branch ? block_backward_as<T, R, false, true, true, 256>(a, p, st) : block_backward_as<T, R, false, false, true, 256>(a, p, st);
-    if (p.threads == 512) {
-        if (branch) return bias ? block_backward_as<T, R, true, true, true, 512>(a, p, st) : block_backward_as<T, R, true, true, false, 512>(a, p, st);
-        return bias ? block_backward_as<T, R, true, false, true, 512>(a, p, st) : block_backward_as<T, R, true, false, false, 512>(a, p, st);
+int block_backward(const BlockArgs &a, bool aligned, bool bias, const BlockPlan &p, cudaStream_t st) {
+    switch (block_input(a)) {
+        case kAlone: return block_backward_of<T, R, kAlone>(a, aligned, bias, p, st);
+        case kPlain: return block_backward_of<T, R, kPlain>(a, aligned, bias, p, st);
+        case kGated: return block_backward_of<T, R, kGated>(a, aligned, bias, p, st);
+        default: return block_backward_of<T, R, kShared>(a, aligned, bias, p, st);
     }
-    if (branch) return bias ? block_backward_as<T, R, true, true, true, 256>(a, p, st) : block_backward_as<T, R, true, true, false, 256>(a, p, st);
-    return bias ? block_backward_as<T, R, true, false, true, 256>(a, p, st) : block_backward_as<T, R, true, false, false, 256>(a, p, st);
 }
 template <typename T>
 int block_sums(const BlockSums &a, cudaStream_t st) {
-    FLARE_CUDA(launch_after(block_sums_kernel<T>, (unsigned)((a.C + kSumLanes - 1) / kSumLanes), kSumLanes * kSumSlices, 0, st, a));
+    FLARE_CUDA(launch_after(block_sums_kernel<T>, dim3((a.C + kSumLanes - 1) / kSumLanes, a.branch ? 2 : 1), kSumLanes * kSumSlices, 0, st, a));
     return FLARE_OK;
 }
 #endif

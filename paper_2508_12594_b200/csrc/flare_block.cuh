@@ -34,8 +34,7 @@ struct BlockArgs {
     float *part;                                          // partial sums over rows [chunks][sums][C]
     long ld_x, ld_o, ld_g, ld_y, ld_h, ld_dy, ld_dh, ld_dx, ld_do, ld_dg;
     long rows, group;                                     // group: rows that share a gate row (all rows where none is shared)
-    long chunk;                                           // rows of a block's piece of a group
-    int chunks;                                           // pieces per group
+    int chunks;                                           // blocks per group
     int C, tpr, cluster;                                  // columns, threads of a row in a block (a power of two), blocks of a row
     int has_post, has_pre, layer_post, layer_pre;
     int gate;                                             // 0 none, 1 sigmoid, 2 linear
@@ -305,13 +304,15 @@ template <typename T, typename R, int kIn> __host__ __device__ constexpr int bwd
 }
 __host__ __device__ constexpr int stages_for(int pieces) { return pieces <= 3 ? 4 : pieces <= 7 ? 3 : 2; }
 
-// The rows of one block: a piece of one group of rows.
+// The rows of one block: every chunks-th turn of `turn` rows of a group (so that the blocks at work at a time are at neighbouring rows).
 struct Piece {
     long begin, end, group;
-    __device__ __forceinline__ Piece(const BlockArgs &p) {
+    int step;
+    __device__ __forceinline__ Piece(const BlockArgs &p, int turn) {
         group = blockIdx.x / p.chunks;
-        begin = group * p.group + (blockIdx.x - group * p.chunks) * p.chunk;
-        end = min(begin + p.chunk, min((group + 1) * p.group, p.rows));
+        begin = group * p.group + (blockIdx.x - group * p.chunks) * turn;
+        end = (group + 1) * p.group;
+        step = turn * p.chunks;
     }
 };
 
@@ -336,7 +337,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 2) block_forwa
         for (int j = 0; j < 8; ++j) mine_n += c[g].has(j) ? 1 : 0;
     }
     RowGroup grp(p.tpr, p.cluster, &row_shared);
-    const Piece piece(p);
+    const Piece piece(p, per_turn);
     constexpr bool gate_row = kIn == kGated;
     const float in_warp = grp.within_warp((float)mine_n);
     ptx::grid_launch();
@@ -373,7 +374,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 2) block_forwa
 
     // loads run kStages - 1 turns ahead of the rows: pointers to the next row to ask for, and rows left from there
     const char *from_x = nullptr, *from_o = nullptr, *from_g = nullptr;
-    const long row0 = piece.begin + mine, step_x = per_turn * p.ld_x * (long)sizeof(R), step_o = per_turn * p.ld_o * (long)sizeof(T), step_g = per_turn * p.ld_g * (long)sizeof(T);
+    const long row0 = piece.begin + mine, step_x = piece.step * p.ld_x * (long)sizeof(R), step_o = piece.step * p.ld_o * (long)sizeof(T), step_g = piece.step * p.ld_g * (long)sizeof(T);
     const int columns = c[0].any() ? c[0].first : 0, apart = 8 * p.tpr;
     int ahead = (int)(piece.end - row0);
     if constexpr (kAligned) {
@@ -396,7 +397,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 2) block_forwa
                 }
             }
             ptx::copy_async_commit();
-            ahead -= per_turn;
+            ahead -= piece.step;
             from_x += step_x;
             if constexpr (kBranch) {
                 from_o += step_o;
@@ -408,7 +409,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 2) block_forwa
         for (int k = 0; k < kStages - 1; ++k) fetch(k);
 
     int stage = 0;
-    for (long row = row0; row - mine < piece.end; row += per_turn) {
+    for (long row = row0; row - mine < piece.end; row += piece.step) {
         const bool live = row < piece.end;
         float2 y[kV][4];
         const uint32_t s = slots + stage * kStage;
@@ -483,7 +484,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 2) block_backw
     const int lane = threadIdx.x & (p.tpr - 1), per_turn = kThreads / p.tpr, mine = threadIdx.x / p.tpr;
     const Columns<kAligned> c(lane, p.tpr, p.C, blockIdx.y * 8 * kThreads);
     RowGroup grp(p.tpr, p.cluster, &row_shared);
-    const Piece piece(p);
+    const Piece piece(p, per_turn);
     constexpr bool gate_row = kIn == kGated;
     ptx::grid_launch();
     ptx::grid_wait();
@@ -541,10 +542,10 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 2) block_backw
                 if constexpr (gate_row) slot_copy<T, kThreads>(s + kG, from_g, yes);
             }
             ptx::copy_async_commit();
-            ahead -= per_turn;
-            from_y += per_turn * p.ld_x * (long)sizeof(R); from_dy += per_turn * p.ld_dy * (long)sizeof(R); from_dh += per_turn * p.ld_dh * (long)sizeof(T);
-            if constexpr (kBranch) from_o += per_turn * p.ld_o * (long)sizeof(T);
-            if constexpr (gate_row) from_g += per_turn * p.ld_g * (long)sizeof(T);
+            ahead -= piece.step;
+            from_y += piece.step * p.ld_x * (long)sizeof(R); from_dy += piece.step * p.ld_dy * (long)sizeof(R); from_dh += piece.step * p.ld_dh * (long)sizeof(T);
+            if constexpr (kBranch) from_o += piece.step * p.ld_o * (long)sizeof(T);
+            if constexpr (gate_row) from_g += piece.step * p.ld_g * (long)sizeof(T);
         }
     };
     if constexpr (kAligned)
@@ -553,11 +554,11 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 2) block_backw
     float4 st_next = piece.begin + mine < piece.end ? p.stats[piece.begin + mine] : none;
 
     int stage = 0;
-    for (long r0 = piece.begin; r0 < piece.end; r0 += per_turn) {
+    for (long r0 = piece.begin; r0 < piece.end; r0 += piece.step) {
         const long row = r0 + mine;
         const bool live = row < piece.end;
         const float4 st = st_next;
-        if (row + per_turn < piece.end) st_next = p.stats[row + per_turn];
+        if (row + piece.step < piece.end) st_next = p.stats[row + piece.step];
         else st_next = none;
         const uint32_t s0 = slots + stage * kStage;
         if constexpr (kAligned) {

@@ -10,11 +10,11 @@ namespace flare {
 // Threads of a block, eight columns each: 512 for rows of more than 2048 columns that can be moved 16 bytes at a time, else 256.  What a row has
 // beyond that goes to further blocks of a cluster.
 constexpr int kBlockMaxWidth = 16384;
-// A block's rows: pieces of the groups, together about as many as fill the chip once.
+// Blocks per group of rows: together about as many as fill the chip once.
 struct BlockPlan {
     int tpr, threads, cluster, vectors;                     // vectors: groups of eight columns a thread owns
-    long groups, chunk;
-    int chunks;
+    long groups;
+    int chunks;                                             // blocks per group
 };
 inline BlockPlan block_plan(long rows, long group, int C, bool aligned, int sms, int vectors = 1) {
     BlockPlan p;
@@ -26,9 +26,7 @@ inline BlockPlan block_plan(long rows, long group, int C, bool aligned, int sms,
     while (p.cluster * p.threads * 8 * vectors < C) p.cluster *= 2;
     const long turn = p.threads / p.tpr, fit = (p.threads == 512 ? 1 : 2) * (long)sms / p.cluster;
     p.groups = rows / group;
-    const long pieces = std::max(1L, std::min(fit / std::max(1L, p.groups), (group + turn - 1) / turn));
-    p.chunk = ((group + pieces - 1) / pieces + turn - 1) / turn * turn;
-    p.chunks = (int)((group + p.chunk - 1) / p.chunk);
+    p.chunks = (int)std::max(1L, std::min(fit / std::max(1L, p.groups), (group + turn - 1) / turn));
     return p;
 }
 
@@ -39,7 +37,7 @@ template <typename T> int block_sums(const BlockSums &s, cudaStream_t st);
 #ifdef FLARE_BLOCK_INSTANTIATE
 template <typename Kernel>
 int block_launch(Kernel kernel, std::atomic<uint64_t> &opt_in, BlockArgs a, const BlockPlan &p, size_t smem, cudaStream_t st) {
-    a.tpr = p.tpr; a.chunk = p.chunk; a.chunks = p.chunks; a.cluster = p.cluster;
+    a.tpr = p.tpr; a.chunks = p.chunks; a.cluster = p.cluster;
     if (int rc = ensure_big_smem(kernel, opt_in, 224 * 1024)) return rc;
     cudaLaunchAttribute attr[2] = {};
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;

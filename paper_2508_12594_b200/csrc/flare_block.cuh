@@ -95,17 +95,16 @@ struct Columns {
     __device__ __forceinline__ bool has(int j) const { return kAligned ? first < C : at(j) < C; }
     __device__ __forceinline__ bool any() const { return first < C; }
 };
-// (live: otherwise zeros, and nothing is read)
 template <typename E, bool kAligned>
-__device__ __forceinline__ Raw8<E> load8(const E *row, const Columns<kAligned> &c, bool live = true) {
+__device__ __forceinline__ Raw8<E> load8(const E *row, const Columns<kAligned> &c) {
     Raw8<E> r;
     if constexpr (kAligned) {
 #pragma unroll
-        for (int i = 0; i < (int)sizeof(E) / 2; ++i) r.q[i] = live && c.any() ? reinterpret_cast<const uint4 *>(row + c.first)[i] : make_uint4(0, 0, 0, 0);
+        for (int i = 0; i < (int)sizeof(E) / 2; ++i) r.q[i] = c.any() ? reinterpret_cast<const uint4 *>(row + c.first)[i] : make_uint4(0, 0, 0, 0);
     } else {
         float2 f[4];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) (&f[j / 2].x)[j & 1] = live && c.has(j) ? to_f32(row[c.at(j)]) : 0.f;
+        for (int j = 0; j < 8; ++j) (&f[j / 2].x)[j & 1] = c.has(j) ? to_f32(row[c.at(j)]) : 0.f;
         r = pack8<E>(f);
     }
     return r;
@@ -286,6 +285,33 @@ __device__ __forceinline__ Raw8<E> slot_read(uint32_t slot) {
     return r;
 }
 
+// The same for columns that are moved one at a time: a word of four bytes a column, [column of the thread][thread].  Of two-byte types the aligned word
+// that the element lies in (of the tensor's last one, where it is the word's first half, that half alone: what follows is not ours).
+template <typename E>
+__device__ __forceinline__ uint32_t half_of(const void *t, long row, long ld, int first) {       // bits to shift the element down by
+    return sizeof(E) == 4 ? 0u : ((uint32_t)reinterpret_cast<uintptr_t>(t) + (uint32_t)(row * ld + first) * 2u & 2u) * 8u;
+}
+template <typename E, int kThreads>
+__device__ __forceinline__ void slot_copy_each(uint32_t slot, const char *src, const Columns<false> &c, bool yes, bool last_row, uint32_t half) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const uint32_t bytes = !yes || !c.has(j) ? 0u : sizeof(E) == 2 && last_row && half == 0 && c.at(j) == c.C - 1 ? 2u : 4u;
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(slot + j * kThreads * 4), "l"(src + (size_t)(j * c.step) * sizeof(E)), "r"(bytes) : "memory");
+    }
+}
+template <typename E, int kThreads>
+__device__ __forceinline__ void slot_read_each(uint32_t slot, uint32_t half, float2 (&f)[4]) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        uint32_t v;
+        asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(slot + j * kThreads * 4) : "memory");
+        float x;
+        if constexpr (sizeof(E) == 4) x = __uint_as_float(v);
+        else x = pair_of(v >> half, E{}).x;
+        (&f[j / 2].x)[j & 1] = x;
+    }
+}
+
 template <int kThreads>
 __device__ __forceinline__ void slot_write(uint32_t slot, const float2 (&f)[4]) {
     const Raw8<float> r = pack8<float>(f);
@@ -296,11 +322,13 @@ __device__ __forceinline__ void slot_write(uint32_t slot, const float2 (&f)[4]) 
 
 // What comes in beside the residual stream: nothing, a branch, a branch with a gate row a row, a branch with gate rows that are shared.
 enum { kAlone = 0, kPlain = 1, kGated = 2, kShared = 3 };
-template <typename T, typename R, int kIn> __host__ __device__ constexpr int fwd_pieces() {
-    return (int)(sizeof(R) / 2 + (kIn == kAlone ? 0 : kIn == kGated ? 2 : 1) * (sizeof(T) / 2));
+// 16-byte pieces of eight columns of everything that is loaded (one column at a time: a word each, two pieces whatever the type).
+template <typename E, bool kAligned> __host__ __device__ constexpr int pieces_of() { return kAligned ? (int)sizeof(E) / 2 : 2; }
+template <typename T, typename R, bool kAligned, int kIn> __host__ __device__ constexpr int fwd_pieces() {
+    return pieces_of<R, kAligned>() + (kIn == kAlone ? 0 : kIn == kGated ? 2 : 1) * pieces_of<T, kAligned>();
 }
-template <typename T, typename R, int kIn> __host__ __device__ constexpr int bwd_pieces() {
-    return (int)(2 * (sizeof(R) / 2) + (kIn == kAlone ? 1 : kIn == kGated ? 3 : 2) * (sizeof(T) / 2));
+template <typename T, typename R, bool kAligned, int kIn> __host__ __device__ constexpr int bwd_pieces() {
+    return 2 * pieces_of<R, kAligned>() + (kIn == kAlone ? 1 : kIn == kGated ? 3 : 2) * pieces_of<T, kAligned>();
 }
 __host__ __device__ constexpr int stages_for(int pieces) { return pieces <= 3 ? 4 : pieces <= 7 ? 3 : 2; }
 
@@ -324,8 +352,8 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 2) block_forwa
     extern __shared__ __align__(16) uint8_t smem[];
     __shared__ RowShared row_shared;
     constexpr bool kBranch = kIn != kAlone;
-    constexpr int kPieces = fwd_pieces<T, R, kIn>() * kV, kStages = stages_for(kPieces);
-    constexpr uint32_t kSlotR = sizeof(R) / 2 * kThreads * 16, kSlotT = sizeof(T) / 2 * kThreads * 16;
+    constexpr int kPieces = fwd_pieces<T, R, kAligned, kIn>() * kV, kStages = stages_for(kPieces);
+    constexpr uint32_t kSlotR = pieces_of<R, kAligned>() * kThreads * 16, kSlotT = pieces_of<T, kAligned>() * kThreads * 16;
     constexpr uint32_t kX = 0, kO = kV * kSlotR, kG = kO + kV * kSlotT, kStage = kPieces * kThreads * 16;
     const int lane = threadIdx.x & (p.tpr - 1), per_turn = kThreads / p.tpr, mine = threadIdx.x / p.tpr;
     Columns<kAligned> c[kV];
@@ -344,7 +372,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 2) block_forwa
     ptx::grid_wait();
 
     constexpr bool kBiasSlots = kBias && kV == 2;
-    const uint32_t slots = ptx::smem_u32(smem) + threadIdx.x * 16, bias_slots = slots + kStages * kStage;   // [post, pre][group][half][thread]
+    const uint32_t slots = ptx::smem_u32(smem) + threadIdx.x * (kAligned ? 16 : 4), bias_slots = slots + kStages * kStage;   // [post, pre][group][half][thread]
     float2 sw[kV][4], sb[kV][4], w[kV][4], b[kV][4], a[kV][4];
 #pragma unroll
     for (int g = 0; g < kV; ++g) {
@@ -377,12 +405,10 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 2) block_forwa
     const long row0 = piece.begin + mine, step_x = piece.step * p.ld_x * (long)sizeof(R), step_o = piece.step * p.ld_o * (long)sizeof(T), step_g = piece.step * p.ld_g * (long)sizeof(T);
     const int columns = c[0].any() ? c[0].first : 0, apart = 8 * p.tpr;
     int ahead = (int)(piece.end - row0);
-    if constexpr (kAligned) {
-        from_x = reinterpret_cast<const char *>(static_cast<const R *>(p.x) + row0 * p.ld_x + columns);
-        if constexpr (kBranch) {
-            from_o = reinterpret_cast<const char *>(static_cast<const T *>(p.o) + row0 * p.ld_o + columns);
-            if constexpr (gate_row) from_g = reinterpret_cast<const char *>(static_cast<const T *>(p.g) + row0 * p.ld_g + columns);
-        }
+    from_x = reinterpret_cast<const char *>(static_cast<const R *>(p.x) + row0 * p.ld_x + columns);
+    if constexpr (kBranch) {
+        from_o = reinterpret_cast<const char *>(static_cast<const T *>(p.o) + row0 * p.ld_o + columns);
+        if constexpr (gate_row) from_g = reinterpret_cast<const char *>(static_cast<const T *>(p.g) + row0 * p.ld_g + columns);
     }
     auto fetch = [&](int stage) {
         if constexpr (kAligned) {
@@ -396,31 +422,37 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 2) block_forwa
                     if constexpr (gate_row) slot_copy<T, kThreads>(s + kG + g * kSlotT, from_g + g * apart * (int)sizeof(T), yes);
                 }
             }
-            ptx::copy_async_commit();
-            ahead -= piece.step;
-            from_x += step_x;
-            if constexpr (kBranch) {
-                from_o += step_o;
-                if constexpr (gate_row) from_g += step_g;
-            }
+        } else {
+            const uint32_t s = slots + stage * kStage;
+            const bool yes = ahead > 0, last_row = piece.end - ahead == p.rows - 1;
+            auto each = [&](auto type, uint32_t slot, const char *src) {
+                using E = decltype(type);
+                const uint32_t half = sizeof(E) == 4 ? 0u : ((uint32_t)reinterpret_cast<uintptr_t>(src) & 2u) * 8u;
+                slot_copy_each<E, kThreads>(slot, src - half / 8, c[0], yes, last_row, half);
+            };
+            each(R{}, s + kX, from_x);
+            if constexpr (kBranch) each(T{}, s + kO, from_o);
+            if constexpr (gate_row) each(T{}, s + kG, from_g);
         }
+        ptx::copy_async_commit();
+        ahead -= piece.step;
+        from_x += step_x;
+        if constexpr (kBranch) from_o += step_o;
+        if constexpr (gate_row) from_g += step_g;
     };
-    if constexpr (kAligned)
-        for (int k = 0; k < kStages - 1; ++k) fetch(k);
+    for (int k = 0; k < kStages - 1; ++k) fetch(k);
 
     int stage = 0;
     for (long row = row0; row - mine < piece.end; row += piece.step) {
         const bool live = row < piece.end;
         float2 y[kV][4];
         const uint32_t s = slots + stage * kStage;
-        if constexpr (kAligned) {
-            fetch(stage == 0 ? kStages - 1 : stage - 1);
-            ptx::copy_async_wait<kStages - 1>();
-        }
+        fetch(stage == 0 ? kStages - 1 : stage - 1);
+        ptx::copy_async_wait<kStages - 1>();
 #pragma unroll
         for (int g = 0; g < kV; ++g) {
             if constexpr (kAligned) unpack8(slot_read<R, kThreads>(s + kX + g * kSlotR), y[g]);
-            else unpack8(load8(static_cast<const R *>(p.x) + row * p.ld_x, c[g], live), y[g]);
+            else slot_read_each<R, kThreads>(s + kX, half_of<R>(p.x, row, p.ld_x, columns), y[g]);
         }
         float2 st_o = make_float2(0.f, 0.f);
         if constexpr (kBranch) {
@@ -431,8 +463,8 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 2) block_forwa
                     unpack8(slot_read<T, kThreads>(s + kO + g * kSlotT), o[g]);
                     if constexpr (gate_row) unpack8(slot_read<T, kThreads>(s + kG + g * kSlotT), a[g]);
                 } else {
-                    unpack8(load8(static_cast<const T *>(p.o) + row * p.ld_o, c[g], live), o[g]);
-                    if constexpr (gate_row) unpack8(load8(static_cast<const T *>(p.g) + row * p.ld_g, c[g], live), a[g]);
+                    slot_read_each<T, kThreads>(s + kO, half_of<T>(p.o, row, p.ld_o, columns), o[g]);
+                    if constexpr (gate_row) slot_read_each<T, kThreads>(s + kG, half_of<T>(p.g, row, p.ld_g, columns), a[g]);
                 }
                 if constexpr (gate_row) gate_act8(p.gate, a[g]);
             }
@@ -478,8 +510,8 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 2) block_backw
     extern __shared__ __align__(16) uint8_t smem[];
     __shared__ RowShared row_shared;
     constexpr bool kBranch = kIn != kAlone;
-    constexpr int kPieces = bwd_pieces<T, R, kIn>(), kStages = stages_for(kPieces), kSums = bwd_sums<kBranch, kBias>();
-    constexpr uint32_t kOneR = sizeof(R) / 2 * kThreads * 16, kOneT = sizeof(T) / 2 * kThreads * 16;
+    constexpr int kPieces = bwd_pieces<T, R, kAligned, kIn>(), kStages = stages_for(kPieces), kSums = bwd_sums<kBranch, kBias>();
+    constexpr uint32_t kOneR = pieces_of<R, kAligned>() * kThreads * 16, kOneT = pieces_of<T, kAligned>() * kThreads * 16;
     constexpr uint32_t kY = 0, kDy = kOneR, kDh = 2 * kOneR, kO = kDh + kOneT, kG = kO + kOneT, kStage = kPieces * kThreads * 16;
     const int lane = threadIdx.x & (p.tpr - 1), per_turn = kThreads / p.tpr, mine = threadIdx.x / p.tpr;
     const Columns<kAligned> c(lane, p.tpr, p.C, blockIdx.y * 8 * kThreads);
@@ -517,12 +549,12 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 2) block_backw
         for (int i = 0; i < 4; ++i) sum[k][i] = f2(0.f);
 
     // loads run kStages - 1 turns ahead of the rows: pointers to the next row to ask for, and rows left from there
-    const uint32_t slots = ptx::smem_u32(smem) + threadIdx.x * 16;
+    const uint32_t slots = ptx::smem_u32(smem) + threadIdx.x * (kAligned ? 16 : 4);
     const char *from_y = nullptr, *from_dy = nullptr, *from_dh = nullptr, *from_o = nullptr, *from_g = nullptr;
     const long first = piece.begin + mine;
     int ahead = (int)(piece.end - first);
-    if constexpr (kAligned) {
-        const int columns = c.any() ? c.first : 0;
+    const int columns = c.any() ? c.first : 0;
+    {
         auto at = [&](const void *t, long ld, size_t size) { return static_cast<const char *>(t) + (first * ld + columns) * (long)size; };
         from_y = at(p.x, p.ld_x, sizeof(R)); from_dy = at(p.dy, p.ld_dy, sizeof(R)); from_dh = at(p.dh, p.ld_dh, sizeof(T));
         if constexpr (kBranch) from_o = at(p.o, p.ld_o, sizeof(T));
@@ -541,15 +573,29 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 2) block_backw
                 slot_copy<T, kThreads>(s + kO, from_o, yes);
                 if constexpr (gate_row) slot_copy<T, kThreads>(s + kG, from_g, yes);
             }
-            ptx::copy_async_commit();
-            ahead -= piece.step;
-            from_y += piece.step * p.ld_x * (long)sizeof(R); from_dy += piece.step * p.ld_dy * (long)sizeof(R); from_dh += piece.step * p.ld_dh * (long)sizeof(T);
-            if constexpr (kBranch) from_o += piece.step * p.ld_o * (long)sizeof(T);
-            if constexpr (gate_row) from_g += piece.step * p.ld_g * (long)sizeof(T);
+        } else {
+            const uint32_t s = slots + stage * kStage;
+            const bool yes = ahead > 0, last_row = piece.end - ahead == p.rows - 1;
+            auto each = [&](auto type, uint32_t slot, const char *src) {
+                using E = decltype(type);
+                const uint32_t half = sizeof(E) == 4 ? 0u : ((uint32_t)reinterpret_cast<uintptr_t>(src) & 2u) * 8u;
+                slot_copy_each<E, kThreads>(slot, src - half / 8, c, yes, last_row, half);
+            };
+            if (p.has_pre) {
+                each(R{}, s + kY, from_y);
+                each(T{}, s + kDh, from_dh);
+            }
+            if (p.dy) each(R{}, s + kDy, from_dy);
+            if constexpr (kBranch) each(T{}, s + kO, from_o);
+            if constexpr (gate_row) each(T{}, s + kG, from_g);
         }
+        ptx::copy_async_commit();
+        ahead -= piece.step;
+        from_y += piece.step * p.ld_x * (long)sizeof(R); from_dy += piece.step * p.ld_dy * (long)sizeof(R); from_dh += piece.step * p.ld_dh * (long)sizeof(T);
+        if constexpr (kBranch) from_o += piece.step * p.ld_o * (long)sizeof(T);
+        if constexpr (gate_row) from_g += piece.step * p.ld_g * (long)sizeof(T);
     };
-    if constexpr (kAligned)
-        for (int k = 0; k < kStages - 1; ++k) fetch(k);
+    for (int k = 0; k < kStages - 1; ++k) fetch(k);
     const float4 none = make_float4(0.f, 0.f, 0.f, 0.f);
     float4 st_next = piece.begin + mine < piece.end ? p.stats[piece.begin + mine] : none;
 
@@ -561,14 +607,12 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 2) block_backw
         if (row + piece.step < piece.end) st_next = p.stats[row + piece.step];
         else st_next = none;
         const uint32_t s0 = slots + stage * kStage;
-        if constexpr (kAligned) {
-            fetch(stage == 0 ? kStages - 1 : stage - 1);
-            ptx::copy_async_wait<kStages - 1>();
-        }
+        fetch(stage == 0 ? kStages - 1 : stage - 1);
+        ptx::copy_async_wait<kStages - 1>();
         float2 dt[4] = {f2(0.f), f2(0.f), f2(0.f), f2(0.f)};
         if (p.dy) {
             if constexpr (kAligned) unpack8(slot_read<R, kThreads>(s0 + kDy), dt);
-            else unpack8(load8(static_cast<const R *>(p.dy) + row * p.ld_dy, c, live), dt);
+            else slot_read_each<R, kThreads>(s0 + kDy, half_of<R>(p.dy, row, p.ld_dy, columns), dt);
         }
         if (p.has_pre) {
             float2 yh[4], t[4];
@@ -576,8 +620,8 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 2) block_backw
                 unpack8(slot_read<R, kThreads>(s0 + kY), yh);
                 unpack8(slot_read<T, kThreads>(s0 + kDh), t);
             } else {
-                unpack8(load8(static_cast<const R *>(p.x) + row * p.ld_x, c, live), yh);
-                unpack8(load8(static_cast<const T *>(p.dh) + row * p.ld_dh, c, live), t);
+                slot_read_each<R, kThreads>(s0 + kY, half_of<R>(p.x, row, p.ld_x, columns), yh);
+                slot_read_each<T, kThreads>(s0 + kDh, half_of<T>(p.dh, row, p.ld_dh, columns), t);
             }
             float2 c1 = f2(0.f), c2 = f2(0.f);
 #pragma unroll
@@ -604,8 +648,8 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 2) block_backw
                 unpack8(slot_read<T, kThreads>(s0 + kO), o);
                 if constexpr (gate_row) unpack8(slot_read<T, kThreads>(s0 + kG), a);
             } else {
-                unpack8(load8(static_cast<const T *>(p.o) + row * p.ld_o, c, live), o);
-                if constexpr (gate_row) unpack8(load8(static_cast<const T *>(p.g) + row * p.ld_g, c, live), a);
+                slot_read_each<T, kThreads>(s0 + kO, half_of<T>(p.o, row, p.ld_o, columns), o);
+                if constexpr (gate_row) slot_read_each<T, kThreads>(s0 + kG, half_of<T>(p.g, row, p.ld_g, columns), a);
             }
             if (p.has_post) {
 #pragma unroll
@@ -644,7 +688,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 2) block_backw
     }
 
     // the block's sums: rows of a warp by shuffles, rows of different warps through shared memory
-    if constexpr (kAligned) ptx::copy_async_wait<0>();
+    ptx::copy_async_wait<0>();
     __syncthreads();
     float *all = reinterpret_cast<float *>(smem);                // [rows at a time][sum][8 tpr]
     const int width = 8 * p.tpr, slots_n = kThreads / max(p.tpr, 32), slot = p.tpr < 32 ? (int)(threadIdx.x >> 5) : mine;

@@ -5,6 +5,8 @@
 namespace flare {
 namespace {
 
+size_t size_of(int dtype) { return dtype == FLARE_DTYPE_F32 ? 4 : 2; }
+
 struct OrthSizes { int S, L; long ld_x, ld_s; };
 OrthSizes sizes_of(const flare_orth_desc_t *d) {
     OrthSizes z;
@@ -23,11 +25,22 @@ bool orth_scales(const flare_orth_desc_t *d, OrthScales *out) {
     const double a = d->coefficients[0], b = d->coefficients[1], c = d->coefficients[2];
     double top = 1.0, x = 1.0, poly = 0.0;
     for (int step = 0; step < d->steps; ++step) {
+        // largest |v q(v^2)| and |q(v^2)|, q(t) = a + b t + c t^2, for v up to `top`: at its ends and where a derivative vanishes
+        const double t1 = 1.002 * top * top;
         double next = 0.0;
-        for (int i = 0; i <= 2000; ++i) {
-            const double v = 1.001 * top * i / 2000.0, v2 = v * v, q = a + b * v2 + c * v2 * v2;
-            next = std::max(next, std::fabs(v * q));
+        auto at = [&](double t) {
+            if (!(t >= 0.0) || t > t1) return;
+            const double q = a + b * t + c * t * t;
+            next = std::max(next, std::sqrt(t) * std::fabs(q));
             poly = std::max(poly, std::fabs(q));
+        };
+        at(0.0); at(t1);
+        if (c != 0.0) {
+            at(-b / (2.0 * c));                                            // q' = b + 2 c t
+            const double root = std::sqrt(std::max(0.0, 9.0 * b * b - 20.0 * a * c));
+            at((-3.0 * b + root) / (10.0 * c)); at((-3.0 * b - root) / (10.0 * c));   // (v q)' = a + 3 b t + 5 c t^2
+        } else if (b != 0.0) {
+            at(-a / (3.0 * b));
         }
         top = next;
         x = std::max(x, top);
@@ -93,12 +106,37 @@ int make_half_map(CUtensorMap *m, const void *base, long cols, long rows, long p
     return FLARE_OK;
 }
 
-// Blocks that share a tile's sums: as many as fill the chip, with at least four 64-deep steps each.
+// Clusters of n blocks of the product kernels that the chip holds at a time (the SMs of a cluster are of one part of the chip, and not every part's number
+// is a multiple of n: 33 of four blocks, not 37); asked for once per device, 0 = not yet.
+int clusters_at_a_time(int n, int sms) {
+    static std::atomic<int> known[64][9];
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return sms / n;
+    int most = known[dev][n].load(std::memory_order_relaxed);
+    if (most == 0) {
+        auto *kernel = orth_product_kernel<kOrthGram, 1, float>;
+        cudaLaunchAttribute attr{};
+        attr.id = cudaLaunchAttributeClusterDimension;
+        attr.val.clusterDim.x = n; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
+        cudaLaunchConfig_t cfg{};
+        cfg.gridDim = dim3((unsigned)(sms / n * n)); cfg.blockDim = kOrthThreads; cfg.dynamicSmemBytes = kOrthSmem;
+        cfg.attrs = &attr; cfg.numAttrs = 1;
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kOrthSmem) != cudaSuccess ||
+            cudaOccupancyMaxActiveClusters(&most, kernel, &cfg) != cudaSuccess || most < 1) {
+            cudaGetLastError();
+            most = 1;
+        }
+        known[dev][n].store(most, std::memory_order_relaxed);
+    }
+    return most;
+}
+// Blocks that share a tile's sums: as many as the chip holds for all tiles at once, with at least three 64-deep steps each.
 int k_split(long tiles, int K, int sms) {
     const int blocks = (K + 63) / 64;
-    int ks = 1;
-    while (ks < 8 && 2 * ks * tiles <= sms && blocks / (2 * ks) >= 4) ks *= 2;
-    return ks;
+    int best = 1;
+    for (int ks = 2; ks <= 8 && blocks / ks >= 3; ++ks)
+        if (tiles <= clusters_at_a_time(ks, sms)) best = ks;
+    return best;
 }
 
 // A matrix of halves in the three forms its tiles are moved in: loaded, stored, stored transposed.
@@ -110,10 +148,10 @@ int make_half_maps(HalfMaps *m, const void *base, long cols, long rows, long pla
     return make_half_map(&m->store_t, base, cols, rows, planes, ld, 32, 64);
 }
 
-template <int kKind, int kPair>
+template <int kKind, int kPair, typename E = float>
 int launch_product_as(const HalfMaps &ta, const HalfMaps &tb, const HalfMaps &out, OrthProduct p, int count, int sms, cudaStream_t st) {
     static std::atomic<uint64_t> opt_in{0};
-    if (int rc = ensure_big_smem(orth_product_kernel<kKind, kPair>, opt_in, (int)kOrthSmem)) return rc;
+    if (int rc = ensure_big_smem(orth_product_kernel<kKind, kPair, E>, opt_in, (int)kOrthSmem)) return rc;
     p.total = p.tiles * count;
     p.ks = kPair == 1 ? k_split(p.total, p.K, sms) : 1;
     const int cluster = kPair * p.ks;
@@ -126,10 +164,10 @@ int launch_product_as(const HalfMaps &ta, const HalfMaps &tb, const HalfMaps &ou
     cfg.gridDim = dim3((unsigned)(p.ks > 1 ? p.total * p.ks : kPair * std::min(p.total, sms / kPair)));
     cfg.blockDim = kOrthThreads; cfg.dynamicSmemBytes = kOrthSmem; cfg.stream = st;
     cfg.attrs = attr; cfg.numAttrs = cluster > 1 ? 2 : 1;
-    FLARE_CUDA(cudaLaunchKernelEx(&cfg, orth_product_kernel<kKind, kPair>, ta.load, tb.load, out.store, out.store_t, p));
+    FLARE_CUDA(cudaLaunchKernelEx(&cfg, orth_product_kernel<kKind, kPair, E>, ta.load, tb.load, out.store, out.store_t, p));
     return FLARE_OK;
 }
-template <int kKind>
+template <int kKind, typename E = float>
 int launch_product(const HalfMaps &ta, const HalfMaps &tb, const HalfMaps &out, OrthProduct p, int count, int sms, cudaStream_t st) {
     auto tiles = [&](int side) {
         p.tiles_m = (p.S + side - 1) / side;
@@ -141,12 +179,17 @@ int launch_product(const HalfMaps &ta, const HalfMaps &tb, const HalfMaps &out, 
     const long pairs = (tiles(256) + sms / 2 - 1) / (sms / 2), singles = (tiles(128) + sms - 1) / sms;
     if ((double)pairs <= 0.6 * singles) {
         tiles(256);
-        return launch_product_as<kKind, 2>(ta, tb, out, p, count, sms, st);
+        return launch_product_as<kKind, 2, E>(ta, tb, out, p, count, sms, st);
     }
-    return launch_product_as<kKind, 1>(ta, tb, out, p, count, sms, st);
+    return launch_product_as<kKind, 1, E>(ta, tb, out, p, count, sms, st);
 }
 
-int run_orth(const flare_orth_desc_t *d, const OrthScales &sc, const OrthOuter &o, void *workspace, cudaStream_t st) {
+int run_orth(const flare_orth_desc_t *d, const OrthScales &sc, OrthOuter o, void *workspace, cudaStream_t st) {
+    auto fours = [&](const void *p, long ld, long step, int type) {
+        return d->cols % 4 == 0 && ld % 4 == 0 && step % 4 == 0 && reinterpret_cast<uintptr_t>(p) % (4 * size_of(type)) == 0;
+    };
+    o.in_fours = fours(o.g, o.ld_g, o.step_g, o.g_type) && (!o.m || (aligned16(o.m) && aligned16(o.m_out)));
+    o.out_fours = fours(o.out, o.ld_out, o.step_out, o.out_type) && (!o.w || fours(o.w, o.ld_out, o.step_out, o.out_type));
     const int sms = device_info().sms;
     const OrthSizes z = sizes_of(d);
     uint32_t *status = static_cast<uint32_t *>(workspace);
@@ -166,7 +209,8 @@ int run_orth(const flare_orth_desc_t *d, const OrthScales &sc, const OrthOuter &
     __half *A = reinterpret_cast<__half *>(ws + w.a), *B = reinterpret_cast<__half *>(ws + w.b);
     const int parts = norm_blocks(d, sms);
     FLARE_CUDA(launch_after(orth_norm_kernel, dim3(parts, d->count), kOrthNormThreads, 0, st, o, part));
-    FLARE_CUDA(launch_after(orth_split_kernel, dim3((d->cols + 31) / 32, (d->rows + 31) / 32, d->count), 256, 0, st, o, part, parts, x[0], z.ld_x, sc.x));
+    const dim3 split = o.tall ? dim3((d->cols + 63) / 64, (d->rows + 63) / 64, d->count) : dim3(parts, 1, d->count);
+    FLARE_CUDA(launch_after(orth_split_kernel, split, 256, 0, st, o, part, parts, x[0], z.ld_x, sc.x));
     HalfMaps tx[2], tA, tB;
     const long planes = 2L * d->count;
     int rc;
@@ -190,13 +234,15 @@ int run_orth(const flare_orth_desc_t *d, const OrthScales &sc, const OrthOuter &
         } else {
             p.o = o;
             p.f = 1.f / (sc.b * sc.x);
-            if ((rc = launch_product<kOrthLast>(tB, tx[cur], tx[1 - cur], p, d->count, sms, st)) != FLARE_OK) return rc;
+            auto last = o.out_type == FLARE_DTYPE_F32    ? launch_product<kOrthLast, float>
+                        : o.out_type == FLARE_DTYPE_BF16 ? launch_product<kOrthLast, __nv_bfloat16>
+                                                         : launch_product<kOrthLast, __half>;
+            if ((rc = last(tB, tx[cur], tx[1 - cur], p, d->count, sms, st)) != FLARE_OK) return rc;
         }
     }
     return FLARE_OK;
 }
 
-size_t size_of(int dtype) { return dtype == FLARE_DTYPE_F32 ? 4 : 2; }
 bool natural(const void *p, size_t size) { return reinterpret_cast<uintptr_t>(p) % size == 0; }
 
 int need_device() {

@@ -18,16 +18,6 @@ namespace flare {
 // What a step's products are for.
 enum { kOrthGram = 0, kOrthPoly = 1, kOrthApply = 2, kOrthLast = 3 };
 
-// An element type chosen at run time (FLARE_DTYPE_*).
-__device__ __forceinline__ float load_as(const void *p, size_t i, int type) {
-    return type == 0 ? static_cast<const float *>(p)[i] : type == 1 ? to_f32(static_cast<const __nv_bfloat16 *>(p)[i]) : to_f32(static_cast<const __half *>(p)[i]);
-}
-__device__ __forceinline__ void store_as(void *p, size_t i, int type, float v) {
-    if (type == 0) static_cast<float *>(p)[i] = v;
-    else if (type == 1) from_f32(static_cast<__nv_bfloat16 *>(p)[i], v);
-    else from_f32(static_cast<__half *>(p)[i], v);
-}
-
 // The matrices that go in and come out, and the update of the weights around them (m != nullptr).
 struct OrthOuter {
     const void *g;               // [count] matrices [rows, cols], rows ld_g and matrices step_g apart
@@ -38,60 +28,140 @@ struct OrthOuter {
     long ld_g, step_g, ld_out, step_out;
     int rows, cols, g_type, out_type;
     int tall;                    // rows > cols: X is the transpose
+    int in_fours, out_fours;     // four columns at a time: widths, strides and pointers allow it
     int nesterov;
     float momentum, keep, rate;  // w' = keep w - rate O
     float eps;
 };
-// A thread's walk over the elements of a matrix, `step` at a time, without divisions.
+
+// f(element of the type that is chosen at run time, FLARE_DTYPE_*)
+template <typename F>
+__device__ __forceinline__ void with_type(int type, F f) {
+    if (type == 0) f(float{});
+    else if (type == 1) f(__nv_bfloat16{});
+    else f(__half{});
+}
+// V (1 or 4) neighbouring elements.
+template <int V, typename E>
+__device__ __forceinline__ void load_v(const E *p, float (&v)[V]) {
+    if constexpr (V == 1) v[0] = to_f32(*p);
+    else if constexpr (sizeof(E) == 4) {
+        const float4 q = *reinterpret_cast<const float4 *>(p);
+        v[0] = q.x; v[1] = q.y; v[2] = q.z; v[3] = q.w;
+    } else {
+        const uint2 q = *reinterpret_cast<const uint2 *>(p);
+        E e[4];
+        *reinterpret_cast<uint2 *>(e) = q;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = to_f32(e[i]);
+    }
+}
+template <int V, typename E>
+__device__ __forceinline__ void store_v(E *p, const float (&v)[V]) {
+    if constexpr (V == 1) from_f32(*p, v[0]);
+    else if constexpr (sizeof(E) == 4) *reinterpret_cast<float4 *>(p) = make_float4(v[0], v[1], v[2], v[3]);
+    else {
+        __align__(8) E e[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) from_f32(e[i], v[i]);
+        *reinterpret_cast<uint2 *>(p) = *reinterpret_cast<const uint2 *>(e);
+    }
+}
+
+// A thread's walk over the groups of V columns of a matrix, `step` at a time, without divisions.
 struct OrthWalk {
-    int r, c, dr, dc, cols;
-    __device__ __forceinline__ OrthWalk(uint32_t first, uint32_t step, int cols_) : cols(cols_) {
-        r = (int)(first / (uint32_t)cols); c = (int)(first % (uint32_t)cols);
-        dr = (int)(step / (uint32_t)cols); dc = (int)(step % (uint32_t)cols);
+    int r, c, dr, dc, groups;
+    __device__ __forceinline__ OrthWalk(uint32_t first, uint32_t step, int groups_) : groups(groups_) {
+        r = (int)(first / (uint32_t)groups); c = (int)(first % (uint32_t)groups);
+        dr = (int)(step / (uint32_t)groups); dc = (int)(step % (uint32_t)groups);
     }
     __device__ __forceinline__ void next() {
         r += dr; c += dc;
-        if (c >= cols) { c -= cols; ++r; }
+        if (c >= groups) { c -= groups; ++r; }
     }
 };
-// The next kBatch elements of the walk, of what is orthogonalised, their places in r, c (r >= rows: none).  kNew: the momentum has been updated
-// already.  All of them are asked for before the first is used: one at a time, with a store between two loads that the compiler must keep in
-// order, each costs a round trip to memory (128 x 128 with a momentum in one block: 94 us a step instead of @).
-template <int kBatch, bool kNew>
-__device__ __forceinline__ void orth_input(const OrthOuter &o, size_t mat, OrthWalk &walk, int (&r)[kBatch], int (&c)[kBatch], float (&u)[kBatch]) {
-    float m[kBatch];
-    const size_t base_g = mat * o.step_g, base_m = mat * (size_t)o.rows * o.cols;
+// use(r, c, V values) for every group of columns of the walk from `first`, of what is orthogonalised.  kNew: the momentum has been updated already.
+// kBatch groups are asked for before the first is used: one at a time, with a store between two loads that the compiler must keep in order, each
+// costs a round trip to memory.
+template <int V, typename G, bool kMomentum, bool kNew, int kBatch, typename F>
+__device__ __forceinline__ void orth_elements_as(const OrthOuter &o, size_t mat, uint32_t first, uint32_t step, F use) {
+    OrthWalk walk(first, step, o.cols / V);
+    const G *g = static_cast<const G *>(o.g) + mat * o.step_g;
+    const size_t base = mat * (size_t)o.rows * o.cols;
+    while (walk.r < o.rows) {
+        int r[kBatch], c[kBatch];
+        float u[kBatch][V], m[kBatch][V];
 #pragma unroll
-    for (int k = 0; k < kBatch; ++k) {
-        r[k] = walk.r; c[k] = walk.c;
-        u[k] = m[k] = 0.f;
-        if (walk.r < o.rows) {
-            u[k] = load_as(o.g, base_g + (size_t)walk.r * o.ld_g + walk.c, o.g_type);
-            if (o.m) m[k] = (kNew ? o.m_out : o.m)[base_m + (size_t)walk.r * o.cols + walk.c];
+        for (int k = 0; k < kBatch; ++k) {
+            r[k] = walk.r; c[k] = walk.c * V;
+            if (walk.r < o.rows) {
+                load_v<V>(g + (size_t)r[k] * o.ld_g + c[k], u[k]);
+                if constexpr (kMomentum) load_v<V>((kNew ? o.m_out : o.m) + base + (size_t)r[k] * o.cols + c[k], m[k]);
+            }
+            walk.next();
         }
-        walk.next();
-    }
-    if (o.m == nullptr) return;
 #pragma unroll
-    for (int k = 0; k < kBatch; ++k) {
-        if (!kNew) {
-            m[k] = fmaf(o.momentum, m[k], (1.f - o.momentum) * u[k]);
-            if (r[k] < o.rows) o.m_out[base_m + (size_t)r[k] * o.cols + c[k]] = m[k];
+        for (int k = 0; k < kBatch; ++k) {
+            if (r[k] >= o.rows) break;
+            if constexpr (kMomentum) {
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    if (!kNew) m[k][i] = fmaf(o.momentum, m[k][i], (1.f - o.momentum) * u[k][i]);
+                    u[k][i] = o.nesterov ? fmaf(o.momentum, m[k][i], (1.f - o.momentum) * u[k][i]) : m[k][i];
+                }
+                if (!kNew) store_v<V>(o.m_out + base + (size_t)r[k] * o.cols + c[k], m[k]);
+            }
+            use(r[k], c[k], u[k]);
         }
-        u[k] = o.nesterov ? fmaf(o.momentum, m[k], (1.f - o.momentum) * u[k]) : m[k];
     }
 }
-// Elements (s, l .. l + kN - 1) of the result, up to column L.
-template <int kN>
-__device__ __forceinline__ void orth_output(const OrthOuter &o, size_t mat, int s, int l, int L, const float *v) {
-    const size_t step = o.tall ? (size_t)o.ld_out : 1, at = mat * o.step_out + (o.tall ? (size_t)l * o.ld_out + s : (size_t)s * o.ld_out + l);
-    const int n = min(kN, L - l);
-    float w[kN];
+template <bool kNew, typename F>
+__device__ __forceinline__ void orth_elements(const OrthOuter &o, size_t mat, uint32_t first, uint32_t step, F use) {
+    with_type(o.g_type, [&](auto type) {
+        using G = decltype(type);
+        if (o.in_fours) {
+            if (o.m) orth_elements_as<4, G, true, kNew, 4>(o, mat, first, step, use);
+            else orth_elements_as<4, G, false, kNew, 4>(o, mat, first, step, use);
+        } else {
+            if (o.m) orth_elements_as<1, G, true, kNew, 8>(o, mat, first, step, use);
+            else orth_elements_as<1, G, false, kNew, 8>(o, mat, first, step, use);
+        }
+    });
+}
+// Writes the result, V columns of a row at a time: get(r, c, V values of O).
+template <int V, typename E, int kBatch, typename F>
+__device__ __forceinline__ void orth_results_as(const OrthOuter &o, size_t mat, uint32_t first, uint32_t step, F get) {
+    OrthWalk walk(first, step, o.cols / V);
+    E *out = static_cast<E *>(o.out) + mat * o.step_out;
+    const E *w = o.w ? static_cast<const E *>(o.w) + mat * o.step_out : nullptr;
+    while (walk.r < o.rows) {
+        int r[kBatch], c[kBatch];
+        float old[kBatch][V];
 #pragma unroll
-    for (int k = 0; k < kN; ++k) w[k] = o.w && k < n ? o.keep * load_as(o.w, at + k * step, o.out_type) : 0.f;
+        for (int k = 0; k < kBatch; ++k) {
+            r[k] = walk.r; c[k] = walk.c * V;
+            if (w && walk.r < o.rows) load_v<V>(w + (size_t)r[k] * o.ld_out + c[k], old[k]);
+            walk.next();
+        }
 #pragma unroll
-    for (int k = 0; k < kN; ++k)
-        if (k < n) store_as(o.out, at + k * step, o.out_type, o.w ? fmaf(-o.rate, v[k], w[k]) : v[k]);
+        for (int k = 0; k < kBatch; ++k) {
+            if (r[k] >= o.rows) break;
+            float v[V];
+            get(r[k], c[k], v);
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                if (w) v[i] = fmaf(-o.rate, v[i], o.keep * old[k][i]);
+            store_v<V>(out + (size_t)r[k] * o.ld_out + c[k], v);
+        }
+    }
+}
+template <typename F>
+__device__ __forceinline__ void orth_results(const OrthOuter &o, size_t mat, uint32_t first, uint32_t step, F get) {
+    with_type(o.out_type, [&](auto type) {
+        using E = decltype(type);
+        if (o.out_fours) orth_results_as<4, E, 4>(o, mat, first, step, get);
+        else orth_results_as<1, E, 8>(o, mat, first, step, get);
+    });
 }
 
 __device__ __forceinline__ void split_half(float v, __half &hi, __half &lo) {
@@ -133,14 +203,9 @@ __global__ void __launch_bounds__(kOrthNormThreads) orth_norm_kernel(OrthOuter o
     ptx::grid_launch();
     ptx::grid_wait();
     double sum = 0.0;
-    OrthWalk walk(blockIdx.x * kOrthNormThreads + threadIdx.x, gridDim.x * kOrthNormThreads, o.cols);
-    while (walk.r < o.rows) {
-        int r[8], c[8];
-        float u[8];
-        orth_input<8, false>(o, blockIdx.y, walk, r, c, u);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) sum += (double)u[k] * u[k];
-    }
+    orth_elements<false>(o, blockIdx.y, blockIdx.x * kOrthNormThreads + threadIdx.x, gridDim.x * kOrthNormThreads, [&](int, int, const auto &u) {
+        for (float x : u) sum += (double)x * x;
+    });
 #pragma unroll
     for (int k = 16; k > 0; k >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, k);
     __shared__ double sh[kOrthNormThreads / 32];
@@ -152,9 +217,17 @@ __global__ void __launch_bounds__(kOrthNormThreads) orth_norm_kernel(OrthOuter o
     }
 }
 
-// The halves of X0, [2 count][S][ld] (high and low of a matrix in turn).  Tiles of 32 x 32 through shared memory.  Grid (col tiles, row tiles, count).
+__device__ __forceinline__ uint32_t half_pair(float a, float b, uint32_t &lo) {
+    const __half2 h = __floats2half2_rn(a, b);
+    const float2 f = __half22float2(h);
+    const __half2 l = __floats2half2_rn(a - f.x, b - f.y);
+    lo = *reinterpret_cast<const uint32_t *>(&l);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+// The halves of X0, [2 count][S][ld] (high and low of a matrix in turn).  Rows as they lie: grid (blocks, 1, count).  tall: tiles of 64 x 64 through
+// shared memory, grid (col tiles, row tiles, count).
 __global__ void __launch_bounds__(256) orth_split_kernel(OrthOuter o, const double *part, int parts, __half *x, long ld, float scale) {
-    __shared__ float tile[32][33];
+    __shared__ float tile[64][65];
     __shared__ double norm_sh;
     ptx::grid_launch();
     ptx::grid_wait();
@@ -167,25 +240,56 @@ __global__ void __launch_bounds__(256) orth_split_kernel(OrthOuter o, const doub
         for (int k = 16; k > 0; k >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, k);
         if (lane == 0) norm_sh = (double)scale / (sqrt(sum) + (double)o.eps);
     }
-    const int r0 = blockIdx.y * 32, c0 = blockIdx.x * 32;
-    if (c0 + lane < o.cols) {
-        OrthWalk walk(0, 1, o.cols);
-        walk.r = r0 + warp; walk.c = c0 + lane; walk.dr = 8; walk.dc = 0;
-        int r[4], c[4];
-        float u[4];
-        orth_input<4, true>(o, mat, walk, r, c, u);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) tile[warp + 8 * k][lane] = u[k];
+    const int S = o.tall ? o.cols : o.rows, L = o.tall ? o.rows : o.cols;
+    __half *hi = x + 2 * mat * S * ld, *lo = hi + S * ld;
+    if (!o.tall) {
+        __syncthreads();
+        const double f = norm_sh;
+        orth_elements<true>(o, mat, blockIdx.x * 256 + threadIdx.x, gridDim.x * 256, [&](int r, int c, const auto &u) {
+            constexpr int V = sizeof(u) / sizeof(float);
+            const size_t at = (size_t)r * ld + c;
+            if constexpr (V == 1) split_half((float)(u[0] * f), hi[at], lo[at]);
+            else {
+                uint2 h, l;
+                h.x = half_pair((float)(u[0] * f), (float)(u[1] * f), l.x);
+                h.y = half_pair((float)(u[2] * f), (float)(u[3] * f), l.y);
+                *reinterpret_cast<uint2 *>(hi + at) = h;
+                *reinterpret_cast<uint2 *>(lo + at) = l;
+            }
+        });
+        return;
     }
+    // the tile as a matrix of its own
+    const int r0 = blockIdx.y * 64, c0 = blockIdx.x * 64;
+    with_type(o.g_type, [&](auto type) {
+        using G = decltype(type);
+        const G *g = static_cast<const G *>(o.g) + mat * o.step_g;
+        const float *m = o.m ? o.m_out + mat * (size_t)o.rows * o.cols : nullptr;
+#pragma unroll
+        for (int i0 = 0; i0 < 16; i0 += 8) {
+            float u[8], q[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int r = r0 + (i0 + i) * 4 + (threadIdx.x >> 6), c = c0 + (threadIdx.x & 63);
+                const bool yes = r < o.rows && c < o.cols;
+                u[i] = yes ? to_f32(g[(size_t)r * o.ld_g + c]) : 0.f;
+                q[i] = yes && m ? m[(size_t)r * o.cols + c] : 0.f;
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                tile[(i0 + i) * 4 + (threadIdx.x >> 6)][threadIdx.x & 63] = !m ? u[i] : o.nesterov ? fmaf(o.momentum, q[i], (1.f - o.momentum) * u[i]) : q[i];
+        }
+    });
     __syncthreads();
     const double f = norm_sh;
-    const int S = o.tall ? o.cols : o.rows, L = o.tall ? o.rows : o.cols, s0 = o.tall ? c0 : r0, l0 = o.tall ? r0 : c0;
-    __half *hi = x + 2 * mat * S * ld, *lo = hi + S * ld;
-    for (int s = warp; s < 32; s += 8)
-        if (s0 + s < S && l0 + lane < L) {
-            const float v = (float)((o.tall ? tile[lane][s] : tile[s][lane]) * f);
-            const size_t at = (size_t)(s0 + s) * ld + l0 + lane;
-            split_half(v, hi[at], lo[at]);
+    const int l = r0 + 2 * lane;
+    for (int s = warp; s < 64; s += 8)
+        if (c0 + s < S && l < L) {                                   // (ld is even; what is beyond the last column is never read)
+            uint32_t low;
+            const uint32_t high = half_pair((float)(tile[2 * lane][s] * f), (float)(tile[2 * lane + 1][s] * f), low);
+            const size_t at = (size_t)(c0 + s) * ld + l;
+            *reinterpret_cast<uint32_t *>(hi + at) = high;
+            *reinterpret_cast<uint32_t *>(lo + at) = low;
         }
 }
 
@@ -264,50 +368,43 @@ template <int kPair> __device__ __forceinline__ void mma_commit_for(uint32_t bar
 }
 }  // namespace ptx
 
-// A warp's 32 rows x 32 columns of the result, one row a lane, into the output (rows s0.., columns l0..): by way of shared memory where the
-// output's rows are X's, so that neighbouring lanes write neighbouring elements either way.  buf: 4096 bytes of the warp's own.
+// A warp's 32 rows x 32 columns of the result, one row a lane, into the output (rows s0.., columns l0..) by way of shared memory, so that
+// neighbouring lanes write neighbouring elements whichever way the output lies.  buf: 4096 bytes of the warp's own.
 template <typename E>
 __device__ __forceinline__ void outer_piece(const OrthOuter &o, size_t mat, int s0, int l0, int S, int L, const float *v, float f, float *buf) {
     const int lane = threadIdx.x & 31;
-    E *out = static_cast<E *>(o.out) + mat * o.step_out;
-    const E *w = o.w ? static_cast<const E *>(o.w) + mat * o.step_out : nullptr;
-    if (!o.tall) {
-        __syncwarp();
-#pragma unroll
-        for (int c = 0; c < 32; ++c) buf[lane * 32 + (c ^ lane)] = v[c];
-        __syncwarp();
-    }
     // k: the other dimension of the piece; a lane's element of it is at + k ld_out
-    const int r0 = o.tall ? l0 : s0, c = (o.tall ? s0 : l0) + lane, rows = min(32, (o.tall ? L : S) - r0);
-    const bool yes = c < (o.tall ? S : L);
-    const size_t at = (size_t)r0 * o.ld_out + c;
+    const int r0 = o.tall ? l0 : s0, c = (o.tall ? s0 : l0) + lane, rows = c < (o.tall ? S : L) ? min(32, (o.tall ? L : S) - r0) : 0;
+    E *out = static_cast<E *>(o.out) + mat * o.step_out + (size_t)r0 * o.ld_out + c;
+    const E *w = o.w ? static_cast<const E *>(o.w) + mat * o.step_out + (size_t)r0 * o.ld_out + c : nullptr;
+    __syncwarp();
 #pragma unroll
-    for (int k0 = 0; k0 < 32; k0 += 8) {
-        float x[8], old[8];
+    for (int k = 0; k < 32; ++k) buf[lane * 32 + (k ^ lane)] = v[k];
+    __syncwarp();
+    // (from here on without v's registers, in loops that are not unrolled over the whole piece: the other pieces' sums are still in theirs)
+#pragma unroll 1
+    for (int k0 = 0; k0 < rows; k0 += 16) {
+        float x[16];
+        if (w) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            x[k] = f * (o.tall ? v[k0 + k] : buf[(k0 + k) * 32 + (lane ^ (k0 + k))]);
-            old[k] = w && yes && k0 + k < rows ? to_f32(w[at + (size_t)(k0 + k) * o.ld_out]) : 0.f;
+            for (int k = 0; k < 16; ++k) x[k] = k0 + k < rows ? to_f32(w[k * o.ld_out]) : 0.f;
+            w += 16 * o.ld_out;
         }
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
-            if (yes && k0 + k < rows) from_f32(out[at + (size_t)(k0 + k) * o.ld_out], w ? fmaf(-o.rate, x[k], o.keep * old[k]) : x[k]);
+        for (int k = 0; k < 16; ++k) {
+            const float y = f * buf[o.tall ? lane * 32 + ((k0 + k) ^ lane) : (k0 + k) * 32 + (lane ^ (k0 + k))];
+            x[k] = w ? fmaf(-o.rate, y, o.keep * x[k]) : y;
+        }
+#pragma unroll
+        for (int k = 0; k < 16; ++k)
+            if (k0 + k < rows) from_f32(out[k * o.ld_out], x[k]);
+        out += 16 * o.ld_out;
     }
-}
-__device__ __forceinline__ void outer_piece_any(const OrthOuter &o, size_t mat, int s0, int l0, int S, int L, const float *v, float f, float *buf) {
-    if (o.out_type == 0) outer_piece<float>(o, mat, s0, l0, S, L, v, f, buf);
-    else if (o.out_type == 1) outer_piece<__nv_bfloat16>(o, mat, s0, l0, S, L, v, f, buf);
-    else outer_piece<__half>(o, mat, s0, l0, S, L, v, f, buf);
+    __syncwarp();
 }
 
-// Tiles of a product of split matrices: 128 x 128 by one block, or 256 x 256 by a pair (kPair = 2).  ta: rows of the left factor; tb: rows of the right
-// one's transpose (kOrthGram, kOrthPoly: sums along rows) or the right one's own rows; out, out_t: the result, in pieces of 32 x 64, and
-// transposed, in pieces of 64 x 32.
-//
-// Tensor memory adds with truncation, which over K = 4096 (768 additions of 16 products) is off by 2e-5 of a sum of equal signs, and by 9e-5 of the
-// 2-norm of the whole result: sums stay there for kOrthChunk steps (K = 512) and are added up in registers, rounded, while the next
-// ones run in a second set of columns: 4e-6.  (The same second set lets a tile's results go out under the next tile's products.)
-template <int kKind, int kPair>
+// E: type of the output (kOrthLast).
+template <int kKind, int kPair, typename E>
 __global__ void __launch_bounds__(kOrthThreads, 1)
 orth_product_kernel(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtensorMap tb, const __grid_constant__ CUtensorMap out,
                     const __grid_constant__ CUtensorMap out_t, const OrthProduct p) {
@@ -463,7 +560,8 @@ orth_product_kernel(const __grid_constant__ CUtensorMap ta, const __grid_constan
             if (kKind == kOrthLast) {
 #pragma unroll
                 for (int k = 0; k < kCols; k += 32)
-                    if (row0 < p.S && col0 + k < p.N) outer_piece_any(p.o, x.mat, row0, col0 + k, p.S, p.N, v + k, p.f, reinterpret_cast<float *>(piece_p));
+                    if (row0 < p.S && col0 + k < p.N)
+                        outer_piece<E>(p.o, x.mat, row0, col0 + k, p.S, p.N, v + k, p.f, reinterpret_cast<float *>(piece_p));
                 continue;
             }
             const __half *ah = p.a + 2 * x.mat * (long)p.S * p.ld_a + (long)row * p.ld_a + col0, *al = ah + (long)p.S * p.ld_a;
@@ -530,9 +628,9 @@ orth_product_kernel(const __grid_constant__ CUtensorMap ta, const __grid_constan
             __syncwarp();
             ptx::cluster_meet();
             const Tile x = tile_of(group);
-            const int width = 128 / p.ks, each = width / 2, row = x.i * 128 + lr;
+            const int row = x.i * 128 + lr;
             const long plane = (long)p.S * p.ld_dst;
-            for (int c = rank * width + half * each, c1 = row < p.S ? c + each : c; c < c1; c += 8) {
+            for (int c = (rank * 2 + half) * 8, c1 = row < p.S ? 128 : 0; c < c1; c += 16 * p.ks) {
                 const int col = x.j * 128 + c;
                 if (col >= p.N) break;
                 float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
@@ -548,7 +646,21 @@ orth_product_kernel(const __grid_constant__ CUtensorMap ta, const __grid_constan
                 if (kKind == kOrthLast) {
 #pragma unroll
                     for (int k = 0; k < 8; ++k) v[k] *= p.f;
-                    orth_output<8>(p.o, x.mat, row, col, p.N, v);
+                    {
+                        const size_t step = p.o.tall ? (size_t)p.o.ld_out : 1,
+                                     at = x.mat * p.o.step_out + (p.o.tall ? (size_t)col * p.o.ld_out + row : (size_t)row * p.o.ld_out + col);
+                        const int n = min(8, p.N - col);
+                        if (p.o.w) {
+                            float w[8];
+#pragma unroll
+                            for (int k = 0; k < 8; ++k) w[k] = k < n ? to_f32(static_cast<const E *>(p.o.w)[at + k * step]) : 0.f;
+#pragma unroll
+                            for (int k = 0; k < 8; ++k) v[k] = fmaf(-p.o.rate, v[k], p.o.keep * w[k]);
+                        }
+#pragma unroll
+                        for (int k = 0; k < 8; ++k)
+                            if (k < n) from_f32(static_cast<E *>(p.o.out)[at + k * step], v[k]);
+                    }
                     continue;
                 }
                 __half *hi = p.dst + 2 * x.mat * plane, *lo = hi + plane;
@@ -635,18 +747,10 @@ __global__ void __launch_bounds__(kOrthSmallThreads, 1) orth_small_kernel(const 
     ptx::grid_launch();
     ptx::grid_wait();
     const OrthOuter &o = p.o;
-    constexpr int kBatch = 16;
     double sum = 0.0;
-    {
-        OrthWalk walk(threadIdx.x, kOrthSmallThreads, o.cols);
-        while (walk.r < o.rows) {
-            int r[kBatch], c[kBatch];
-            float u[kBatch];
-            orth_input<kBatch, false>(o, mat, walk, r, c, u);
-#pragma unroll
-            for (int k = 0; k < kBatch; ++k) sum += (double)u[k] * u[k];
-        }
-    }
+    orth_elements<false>(o, mat, threadIdx.x, kOrthSmallThreads, [&](int, int, const auto &u) {
+        for (float x : u) sum += (double)x * x;
+    });
 #pragma unroll
     for (int k = 16; k > 0; k >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, k);
     if (lane == 0) sums[warp] = sum;
@@ -654,21 +758,24 @@ __global__ void __launch_bounds__(kOrthSmallThreads, 1) orth_small_kernel(const 
     sum = 0.0;
     for (int k = 0; k < kOrthSmallThreads / 32; ++k) sum += sums[k];
     const double f = (double)p.sc.x / (sqrt(sum) + (double)o.eps);
-    {
-        OrthWalk walk(threadIdx.x, kOrthSmallThreads, o.cols);
-        while (walk.r < o.rows) {
-            int r[kBatch], c[kBatch];
-            float u[kBatch];
-            orth_input<kBatch, true>(o, mat, walk, r, c, u);
+    orth_elements<true>(o, mat, threadIdx.x, kOrthSmallThreads, [&](int r, int c, const auto &u) {
+        constexpr int V = sizeof(u) / sizeof(float);
+        if (V == 4 && !o.tall) {
+            uint2 h, l;
+            h.x = half_pair((float)(u[0] * f), (float)(u[1 % V] * f), l.x);
+            h.y = half_pair((float)(u[2 % V] * f), (float)(u[3 % V] * f), l.y);
+            const uint32_t at = panel_at(r, c & ~7, p.Mr) + (c & 7) * 2;
+            *reinterpret_cast<uint2 *>(xh + at) = h;
+            *reinterpret_cast<uint2 *>(xl + at) = l;
+        } else {
 #pragma unroll
-            for (int k = 0; k < kBatch; ++k) {
-                if (r[k] >= o.rows) continue;
-                const int sr = o.tall ? c[k] : r[k], l = o.tall ? r[k] : c[k];
-                const uint32_t at = panel_at(sr, l & ~7, p.Mr) + (l & 7) * 2;
-                split_half((float)(u[k] * f), *reinterpret_cast<__half *>(xh + at), *reinterpret_cast<__half *>(xl + at));
+            for (int i = 0; i < V; ++i) {
+                const int s = o.tall ? c + i : r, l = o.tall ? r : c + i;
+                const uint32_t at = panel_at(s, l & ~7, p.Mr) + (l & 7) * 2;
+                split_half((float)(u[i] * f), *reinterpret_cast<__half *>(xh + at), *reinterpret_cast<__half *>(xl + at));
             }
         }
-    }
+    });
     ptx::fence_proxy_async_smem();
     ptx::tc_fence_before();
     __syncthreads();
@@ -767,8 +874,7 @@ __global__ void __launch_bounds__(kOrthSmallThreads, 1) orth_small_kernel(const 
         }
         ready();
         // X <- B X, as many columns at a time as tensor memory holds
-        const bool last = step + 1 == p.steps;
-        const float fx = last ? 1.f / (p.sc.b * p.sc.x) : 1.f / p.sc.b;
+        const float fx = 1.f / p.sc.b;
         for (int l0 = 0; l0 < 64 * p.panels; l0 += chunk_max) {
             const int l1 = min(l0 + chunk_max, 64 * p.panels);
             if (warp == 0 && ptx::elect_one()) {
@@ -788,14 +894,7 @@ __global__ void __launch_bounds__(kOrthSmallThreads, 1) orth_small_kernel(const 
                 uint32_t u[16];
                 ptx::tmem_ld16(acc + (l - l0), u);
                 ptx::tmem_wait_ld();
-                if (last) {
-                    if (row < p.S && l < p.L) {
-                        float v[16];
-#pragma unroll
-                        for (int k = 0; k < 16; ++k) v[k] = __uint_as_float(u[k]) * fx;
-                        orth_output<16>(o, mat, row, l, p.L, v);
-                    }
-                } else if (row < p.Mr) {
+                if (row < p.Mr) {
 #pragma unroll
                     for (int q = 0; q < 2; ++q) {
                         float v[8];
@@ -812,6 +911,17 @@ __global__ void __launch_bounds__(kOrthSmallThreads, 1) orth_small_kernel(const 
             ready();
         }
     }
+    // the result, from its halves
+    const float back = 1.f / p.sc.x;
+    orth_results(o, mat, threadIdx.x, kOrthSmallThreads, [&](int r, int c, auto &v) {
+        constexpr int V = sizeof(v) / sizeof(float);
+        auto one = [&](uint32_t at) { return back * (__half2float(*reinterpret_cast<const __half *>(xh + at)) + __half2float(*reinterpret_cast<const __half *>(xl + at))); };
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const int s = o.tall ? c + i : r, l = o.tall ? r : c + i;
+            v[i] = one(panel_at(s, l & ~7, p.Mr) + (l & 7) * 2);
+        }
+    });
     ptx::tc_fence_before();
     __syncthreads();
     if (threadIdx.x == 0 && abort_flag != 0) p.status[0] = abort_flag;

@@ -71,17 +71,60 @@ int norm_blocks(const flare_orth_desc_t *d, int sms) {
     const long each = ((long)d->rows * d->cols + kOrthNormThreads * 16 - 1) / (kOrthNormThreads * 16);
     return (int)std::max(1L, std::min(each, (8L * sms + d->count - 1) / std::max(1, d->count)));
 }
-struct OrthLayout { size_t part, x[2], a, b, total; };
-OrthLayout orth_layout(const flare_orth_desc_t *d, int sms) {
+// How a team does a product: blocks that share a tile's K, and of a symmetric result, whether only the upper tiles are computed.  In 64-deep steps of a
+// tile (some 768 cycles): sharing (the sums to memory, the wait, the sums from memory) costs about 8 of them, storing a tile's transpose 4, which
+// a team with blocks to spare saves by computing both; each product some 12 to start and to meet.
+struct TeamPlan { int ks; bool upper; double cost; };
+TeamPlan team_plan(int team, long rows, long cols, bool symmetric, int K) {
+    const int blocks = (K + 63) / 64;
+    TeamPlan best{1, false, 0.0};
+    for (int upper = 0; upper <= (symmetric ? 1 : 0); ++upper) {
+        const long tiles = upper ? rows * (rows + 1) / 2 : rows * cols;
+        for (int ks = 1; ks <= 8; ++ks) {
+            if (ks > 1 && ks * tiles > team) break;
+            const long turns = ks > 1 ? 1 : (tiles + team - 1) / team;
+            const double cost = 12.0 + (double)turns * ((blocks + ks - 1) / ks + (ks > 1 ? 8 : 0) + (upper && rows > 1 ? 4 : 0));
+            if (best.cost == 0.0 || cost < best.cost) best = TeamPlan{ks, upper != 0, cost};
+        }
+    }
+    return best;
+}
+// How a problem is run.
+enum { kOrthSmallPath = 0, kOrthTeamPath = 1, kOrthPairPath = 2 };
+struct OrthPlan { int path, team, teams; };
+OrthPlan orth_plan(const flare_orth_desc_t *d, int sms) {
+    const OrthSizes z = sizes_of(d);
+    OrthPlan p{};
+    if (orth_small(z)) return p;
+    const int count = std::max(1, d->count);
+    p.teams = std::min(count, sms);
+    p.team = sms / p.teams;
+    // Time of a step, in cycles: a team's as above, matrices that have to wait for a team one after the other; a launch per product over pairs: 1536
+    // cycles each 64 of K and tile of four times the size, and some 16000 to start, finish and follow one another.
+    const double rounds = (double)((count + p.teams - 1) / p.teams);
+    const long s = (z.S + 127) / 128, l = (z.L + 127) / 128, s2 = (z.S + 255) / 256, l2 = (z.L + 255) / 256;
+    const double team = 800.0 * rounds * (team_plan(p.team, s, s, true, z.L).cost + team_plan(p.team, s, s, true, z.S).cost + team_plan(p.team, s, l, false, z.S).cost);
+    auto launch = [&](long tiles, int K) { return 16000.0 + (double)((tiles * count + sms / 2 - 1) / (sms / 2)) * ((K + 63) / 64) * 1536.0; };
+    const double pairs = launch(s2 * (s2 + 1) / 2, z.L) + launch(s2 * (s2 + 1) / 2, z.S) + launch(s2 * l2, z.S);
+    p.path = team <= pairs ? kOrthTeamPath : kOrthPairPath;
+    return p;
+}
+struct OrthLayout { size_t counters, norm, x[2], a, b, part, total; };
+OrthLayout orth_layout(const flare_orth_desc_t *d, const OrthPlan &plan, int sms) {
     const OrthSizes z = sizes_of(d);
     OrthLayout w{};
     size_t off = kHeaderBytes;
-    if (!orth_small(z)) {
-        const size_t n = 2 * (size_t)d->count * sizeof(__half);
-        w.part = off; off += align_up(sizeof(double) * (size_t)d->count * norm_blocks(d, sms));
+    if (plan.path != kOrthSmallPath) {
+        const bool team = plan.path == kOrthTeamPath;
+        const size_t n = 2 * (size_t)d->count * sizeof(__half), blocks = (size_t)plan.team * plan.teams;
+        w.counters = off;
+        if (team) off += align_up(sizeof(uint32_t) * (plan.teams + 3 * blocks));
+        w.norm = off; off += align_up(sizeof(double) * (size_t)d->count * norm_blocks(d, sms));
         for (size_t &x : w.x) { x = off; off += align_up(n * z.S * z.ld_x); }
         w.a = off; off += align_up(n * z.S * z.ld_s);
         w.b = off; off += align_up(n * z.S * z.ld_s);
+        w.part = off;
+        if (team) off += blocks * 128 * 128 * sizeof(float);
     }
     w.total = off;
     return w;
@@ -106,41 +149,6 @@ int make_half_map(CUtensorMap *m, const void *base, long cols, long rows, long p
     return FLARE_OK;
 }
 
-// Clusters of n blocks of the product kernels that the chip holds at a time (the SMs of a cluster are of one part of the chip, and not every part's number
-// is a multiple of n: 33 of four blocks, not 37); asked for once per device, 0 = not yet.
-int clusters_at_a_time(int n, int sms) {
-    static std::atomic<int> known[64][9];
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return sms / n;
-    int most = known[dev][n].load(std::memory_order_relaxed);
-    if (most == 0) {
-        auto *kernel = orth_product_kernel<kOrthGram, 1, float>;
-        cudaLaunchAttribute attr{};
-        attr.id = cudaLaunchAttributeClusterDimension;
-        attr.val.clusterDim.x = n; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
-        cudaLaunchConfig_t cfg{};
-        cfg.gridDim = dim3((unsigned)(sms / n * n)); cfg.blockDim = kOrthThreads; cfg.dynamicSmemBytes = kOrthSmem;
-        cfg.attrs = &attr; cfg.numAttrs = 1;
-        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kOrthSmem) != cudaSuccess ||
-            cudaOccupancyMaxActiveClusters(&most, kernel, &cfg) != cudaSuccess || most < 1) {
-            cudaGetLastError();
-            most = 1;
-        }
-        known[dev][n].store(most, std::memory_order_relaxed);
-    }
-    return most;
-}
-// Blocks that share a tile's sums: as many as the chip holds for all tiles at once, with at least three 64-deep steps each.
-int k_split(long tiles, int K, int sms) {
-    const int blocks = (K + 63) / 64;
-    int best = 1;
-    for (int ks = 2; ks <= 8 && blocks / ks >= 3; ++ks)
-        if (tiles <= clusters_at_a_time(ks, sms)) best = ks;
-    return best;
-}
-
-// A matrix of halves in the three forms its tiles are moved in: loaded, stored, stored transposed.
-struct HalfMaps { CUtensorMap load, store, store_t; };
 int make_half_maps(HalfMaps *m, const void *base, long cols, long rows, long planes, long ld) {
     int rc;
     if ((rc = make_half_map(&m->load, base, cols, rows, planes, ld, 64, 64)) != FLARE_OK) return rc;
@@ -148,40 +156,41 @@ int make_half_maps(HalfMaps *m, const void *base, long cols, long rows, long pla
     return make_half_map(&m->store_t, base, cols, rows, planes, ld, 32, 64);
 }
 
-template <int kKind, int kPair, typename E = float>
-int launch_product_as(const HalfMaps &ta, const HalfMaps &tb, const HalfMaps &out, OrthProduct p, int count, int sms, cudaStream_t st) {
+template <int kKind, typename E = float>
+int launch_pairs(const HalfMaps &ta, const HalfMaps &tb, const HalfMaps &out, OrthPairArgs a, int count, int sms, cudaStream_t st) {
     static std::atomic<uint64_t> opt_in{0};
-    if (int rc = ensure_big_smem(orth_product_kernel<kKind, kPair, E>, opt_in, (int)kOrthSmem)) return rc;
-    p.total = p.tiles * count;
-    p.ks = kPair == 1 ? k_split(p.total, p.K, sms) : 1;
-    const int cluster = kPair * p.ks;
+    if (int rc = ensure_big_smem(orth_pair_kernel<kKind, E>, opt_in, (int)kOrthSmem)) return rc;
+    OrthProduct &p = a.p;
+    p.tiles_m = (p.S + 255) / 256;
+    p.tiles_n = (p.N + 255) / 256;
+    p.upper = kKind == kOrthGram || kKind == kOrthPoly;
+    p.tiles = p.upper ? p.tiles_n * (p.tiles_n + 1) / 2 : p.tiles_m * p.tiles_n;
+    a.total = p.tiles * count;
     cudaLaunchAttribute attr[2] = {};
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = cluster; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+    attr[1].val.clusterDim.x = 2; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)(p.ks > 1 ? p.total * p.ks : kPair * std::min(p.total, sms / kPair)));
+    cfg.gridDim = dim3(2 * (unsigned)std::min(a.total, sms / 2));
     cfg.blockDim = kOrthThreads; cfg.dynamicSmemBytes = kOrthSmem; cfg.stream = st;
-    cfg.attrs = attr; cfg.numAttrs = cluster > 1 ? 2 : 1;
-    FLARE_CUDA(cudaLaunchKernelEx(&cfg, orth_product_kernel<kKind, kPair, E>, ta.load, tb.load, out.store, out.store_t, p));
+    cfg.attrs = attr; cfg.numAttrs = 2;
+    FLARE_CUDA(cudaLaunchKernelEx(&cfg, orth_pair_kernel<kKind, E>, ta.load, tb.load, out.store, out.store_t, a));
     return FLARE_OK;
 }
-template <int kKind, typename E = float>
-int launch_product(const HalfMaps &ta, const HalfMaps &tb, const HalfMaps &out, OrthProduct p, int count, int sms, cudaStream_t st) {
-    auto tiles = [&](int side) {
-        p.tiles_m = (p.S + side - 1) / side;
-        p.tiles_n = (p.N + side - 1) / side;
-        p.tiles = kKind == kOrthGram || kKind == kOrthPoly ? p.tiles_n * (p.tiles_n + 1) / 2 : p.tiles_m * p.tiles_n;
-        return (long)p.tiles * count;
-    };
-    // turns of the chip, in units of a pair's tile: a block's 128 x 128 takes about 0.6 of a pair's 256 x 256
-    const long pairs = (tiles(256) + sms / 2 - 1) / (sms / 2), singles = (tiles(128) + sms - 1) / sms;
-    if ((double)pairs <= 0.6 * singles) {
-        tiles(256);
-        return launch_product_as<kKind, 2, E>(ta, tb, out, p, count, sms, st);
-    }
-    return launch_product_as<kKind, 1, E>(ta, tb, out, p, count, sms, st);
+template <typename E>
+int launch_teams(const OrthMaps &maps, const OrthTeam &p, cudaStream_t st) {
+    static std::atomic<uint64_t> opt_in{0};
+    if (int rc = ensure_big_smem(orth_team_kernel<E>, opt_in, (int)kOrthSmem)) return rc;
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeCooperative;                                    // (its blocks wait for one another: all of them at once or none)
+    attr.val.cooperative = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)(p.team * p.teams));
+    cfg.blockDim = kOrthThreads; cfg.dynamicSmemBytes = kOrthSmem; cfg.stream = st;
+    cfg.attrs = &attr; cfg.numAttrs = 1;
+    FLARE_CUDA(cudaLaunchKernelEx(&cfg, orth_team_kernel<E>, maps, p));
+    return FLARE_OK;
 }
 
 int run_orth(const flare_orth_desc_t *d, const OrthScales &sc, OrthOuter o, void *workspace, cudaStream_t st) {
@@ -192,9 +201,12 @@ int run_orth(const flare_orth_desc_t *d, const OrthScales &sc, OrthOuter o, void
     o.out_fours = fours(o.out, o.ld_out, o.step_out, o.out_type) && (!o.w || fours(o.w, o.ld_out, o.step_out, o.out_type));
     const int sms = device_info().sms;
     const OrthSizes z = sizes_of(d);
+    const OrthPlan plan = orth_plan(d, sms);
+    const OrthLayout w = orth_layout(d, plan, sms);
     uint32_t *status = static_cast<uint32_t *>(workspace);
-    if (int rc = clear_header(workspace, 0, st)) return rc;
-    if (orth_small(z)) {
+    const int words = (int)((plan.path == kOrthTeamPath ? w.norm : kHeaderBytes) / sizeof(uint32_t));
+    FLARE_CUDA(launch_after(orth_clear_kernel, 1, 256, 0, st, status, words));
+    if (plan.path == kOrthSmallPath) {
         static std::atomic<uint64_t> opt_in{0};
         if (int rc = ensure_big_smem(orth_small_kernel, opt_in, 227 * 1024 - 512)) return rc;
         OrthSmall p{};
@@ -202,42 +214,63 @@ int run_orth(const flare_orth_desc_t *d, const OrthScales &sc, OrthOuter o, void
         FLARE_CUDA(launch_after(orth_small_kernel, (unsigned)d->count, kOrthSmallThreads, orth_small_size(z.S, z.L).total, st, p));
         return FLARE_OK;
     }
-    const OrthLayout w = orth_layout(d, sms);
     char *ws = static_cast<char *>(workspace);
-    double *part = reinterpret_cast<double *>(ws + w.part);
+    double *norm = reinterpret_cast<double *>(ws + w.norm);
     __half *x[2] = {reinterpret_cast<__half *>(ws + w.x[0]), reinterpret_cast<__half *>(ws + w.x[1])};
     __half *A = reinterpret_cast<__half *>(ws + w.a), *B = reinterpret_cast<__half *>(ws + w.b);
     const int parts = norm_blocks(d, sms);
-    FLARE_CUDA(launch_after(orth_norm_kernel, dim3(parts, d->count), kOrthNormThreads, 0, st, o, part));
-    const dim3 split = o.tall ? dim3((d->cols + 63) / 64, (d->rows + 63) / 64, d->count) : dim3(parts, 1, d->count);
-    FLARE_CUDA(launch_after(orth_split_kernel, split, 256, 0, st, o, part, parts, x[0], z.ld_x, sc.x));
-    HalfMaps tx[2], tA, tB;
+    FLARE_CUDA(launch_after(orth_norm_kernel, dim3(parts, d->count), kOrthNormThreads, 0, st, o, norm));
+    FLARE_CUDA(launch_after(orth_split_kernel, dim3(parts, d->count), 256, 0, st, o, norm, parts, x[0], z.ld_x, sc.x));
     const long planes = 2L * d->count;
+    HalfMaps tx[2], tA, tB;
     int rc;
     for (int i = 0; i < 2; ++i)
         if ((rc = make_half_maps(&tx[i], x[i], z.L, z.S, planes, z.ld_x)) != FLARE_OK) return rc;
     if ((rc = make_half_maps(&tA, A, z.S, z.S, planes, z.ld_s)) != FLARE_OK) return rc;
     if ((rc = make_half_maps(&tB, B, z.S, z.S, planes, z.ld_s)) != FLARE_OK) return rc;
+    if (plan.path == kOrthTeamPath) {
+        OrthTeam p{};
+        p.o = o;
+        for (int kind = 0; kind < 4; ++kind) {
+            OrthProduct &q = p.product[kind];
+            const bool symmetric = kind == kOrthGram || kind == kOrthPoly;
+            q.a = A; q.ld_a = z.ld_s; q.S = z.S; q.N = symmetric ? z.S : z.L; q.K = kind == kOrthGram ? z.L : z.S;
+            q.tiles_m = (q.S + 127) / 128; q.tiles_n = (q.N + 127) / 128;
+            const TeamPlan how = team_plan(plan.team, q.tiles_m, q.tiles_n, symmetric, q.K);
+            q.upper = how.upper;
+            q.tiles = q.upper ? q.tiles_n * (q.tiles_n + 1) / 2 : q.tiles_m * q.tiles_n;
+            q.f = kind == kOrthGram ? sc.a / (sc.x * sc.x) : kind == kOrthPoly ? sc.cc * sc.b / (sc.a * sc.a) : kind == kOrthApply ? 1.f / sc.b : 1.f / (sc.b * sc.x);
+            q.fa = sc.cb * sc.b / sc.a; q.fi = sc.ca * sc.b;
+            p.ks[kind] = how.ks;
+        }
+        const OrthMaps maps{{tx[0], tx[1], tA, tB}};
+        p.mem[0] = x[0]; p.mem[1] = x[1]; p.mem[2] = A; p.mem[3] = B;
+        p.part = reinterpret_cast<float *>(ws + w.part);
+        p.counters = reinterpret_cast<uint32_t *>(ws + w.counters); p.status = status;
+        p.ld_x = z.ld_x; p.ld_s = z.ld_s; p.S = z.S; p.L = z.L; p.count = d->count; p.steps = d->steps; p.team = plan.team; p.teams = plan.teams;
+        return o.out_type == FLARE_DTYPE_F32 ? launch_teams<float>(maps, p, st) : o.out_type == FLARE_DTYPE_BF16 ? launch_teams<__nv_bfloat16>(maps, p, st) : launch_teams<__half>(maps, p, st);
+    }
     for (int step = 0; step < d->steps; ++step) {
         const int cur = step & 1;
-        OrthProduct p{};
-        p.status = status; p.S = z.S; p.N = z.S;
-        p.dst = A; p.ld_dst = z.ld_s; p.K = z.L; p.f = sc.a / (sc.x * sc.x);
-        if ((rc = launch_product<kOrthGram>(tx[cur], tx[cur], tA, p, d->count, sms, st)) != FLARE_OK) return rc;
-        p.dst = B; p.a = A; p.ld_a = z.ld_s; p.K = z.S;
+        OrthPairArgs a{};
+        OrthProduct &p = a.p;
+        a.status = status; p.S = z.S; p.N = z.S;
+        p.K = z.L; p.f = sc.a / (sc.x * sc.x);
+        if ((rc = launch_pairs<kOrthGram>(tx[cur], tx[cur], tA, a, d->count, sms, st)) != FLARE_OK) return rc;
+        p.a = A; p.ld_a = z.ld_s; p.K = z.S;
         p.f = sc.cc * sc.b / (sc.a * sc.a); p.fa = sc.cb * sc.b / sc.a; p.fi = sc.ca * sc.b;
-        if ((rc = launch_product<kOrthPoly>(tA, tA, tB, p, d->count, sms, st)) != FLARE_OK) return rc;
-        p.dst = x[1 - cur]; p.ld_dst = z.ld_x; p.N = z.L;
+        if ((rc = launch_pairs<kOrthPoly>(tA, tA, tB, a, d->count, sms, st)) != FLARE_OK) return rc;
+        p.N = z.L;
         if (step + 1 < d->steps) {
             p.f = 1.f / sc.b;
-            if ((rc = launch_product<kOrthApply>(tB, tx[cur], tx[1 - cur], p, d->count, sms, st)) != FLARE_OK) return rc;
+            if ((rc = launch_pairs<kOrthApply>(tB, tx[cur], tx[1 - cur], a, d->count, sms, st)) != FLARE_OK) return rc;
         } else {
-            p.o = o;
+            a.o = o;
             p.f = 1.f / (sc.b * sc.x);
-            auto last = o.out_type == FLARE_DTYPE_F32    ? launch_product<kOrthLast, float>
-                        : o.out_type == FLARE_DTYPE_BF16 ? launch_product<kOrthLast, __nv_bfloat16>
-                                                         : launch_product<kOrthLast, __half>;
-            if ((rc = last(tB, tx[cur], tx[1 - cur], p, d->count, sms, st)) != FLARE_OK) return rc;
+            auto last = o.out_type == FLARE_DTYPE_F32    ? launch_pairs<kOrthLast, float>
+                        : o.out_type == FLARE_DTYPE_BF16 ? launch_pairs<kOrthLast, __nv_bfloat16>
+                                                         : launch_pairs<kOrthLast, __half>;
+            if ((rc = last(tB, tx[cur], tx[1 - cur], a, d->count, sms, st)) != FLARE_OK) return rc;
         }
     }
     return FLARE_OK;
@@ -272,7 +305,7 @@ extern "C" {
 size_t flare_orthogonalize_workspace_bytes(const flare_orth_desc_t *desc) {
     OrthScales sc;
     if (check_orth(desc, &sc) != FLARE_OK) return 0;
-    return orth_layout(desc, device_info().sms).total;
+    return orth_layout(desc, orth_plan(desc, device_info().sms), device_info().sms).total;
 }
 
 int flare_orthogonalize(const flare_orth_desc_t *desc, const void *G, void *O, void *workspace, size_t workspace_bytes, flare_stream_t stream) {
@@ -281,7 +314,7 @@ int flare_orthogonalize(const flare_orth_desc_t *desc, const void *G, void *O, v
     const size_t e = size_of(desc->dtype);
     if (!workspace || !aligned16(workspace) || (desc->count > 0 && (!G || !O)) || !natural(G, e) || !natural(O, e)) return FLARE_ERR_INVALID_ARG;
     if (int rc = need_device()) return rc;
-    if (workspace_bytes < orth_layout(desc, device_info().sms).total) return FLARE_ERR_WORKSPACE_TOO_SMALL;
+    if (workspace_bytes < orth_layout(desc, orth_plan(desc, device_info().sms), device_info().sms).total) return FLARE_ERR_WORKSPACE_TOO_SMALL;
     if (desc->count == 0) return FLARE_OK;
     OrthOuter o = outer_of(desc);
     o.g = G; o.out = O; o.out_type = desc->dtype;
@@ -300,7 +333,7 @@ int flare_muon_update(const flare_orth_desc_t *desc, const flare_muon_t *rule, c
     if (!workspace || !aligned16(workspace) || (desc->count > 0 && (!w || !m || !g || !w_out || !m_out))) return FLARE_ERR_INVALID_ARG;
     if (!natural(w, e) || !natural(w_out, e) || !natural(m, 4) || !natural(m_out, 4) || !natural(g, size_of(desc->dtype))) return FLARE_ERR_INVALID_ARG;
     if (int rc = need_device()) return rc;
-    if (workspace_bytes < orth_layout(desc, device_info().sms).total) return FLARE_ERR_WORKSPACE_TOO_SMALL;
+    if (workspace_bytes < orth_layout(desc, orth_plan(desc, device_info().sms), device_info().sms).total) return FLARE_ERR_WORKSPACE_TOO_SMALL;
     if (desc->count == 0) return FLARE_OK;
     OrthOuter o = outer_of(desc);
     o.g = g; o.w = w; o.out = w_out; o.out_type = desc->weight_dtype; o.m = m; o.m_out = m_out;

@@ -195,6 +195,13 @@ __device__ __forceinline__ void join8(uint4 hi, uint4 lo, float *v) {
 // Power-of-two scales of the halves (from the quintic's range, see orth_scales) and the coefficients.
 struct OrthScales { float x, a, b; float ca, cb, cc; };
 
+// Clears the workspace header and the counters behind it.
+__global__ void __launch_bounds__(256) orth_clear_kernel(uint32_t *words, int n) {
+    ptx::grid_launch();
+    ptx::grid_wait();
+    for (int i = threadIdx.x; i < n; i += 256) words[i] = 0u;
+}
+
 // ---------------------------------------------------------------- norm and first split, for matrices that do not fit a block
 constexpr int kOrthNormThreads = 256;
 
@@ -224,28 +231,25 @@ __device__ __forceinline__ uint32_t half_pair(float a, float b, uint32_t &lo) {
     lo = *reinterpret_cast<const uint32_t *>(&l);
     return *reinterpret_cast<const uint32_t *>(&h);
 }
-// The halves of X0, [2 count][S][ld] (high and low of a matrix in turn).  Rows as they lie: grid (blocks, 1, count).  tall: tiles of 64 x 64 through
-// shared memory, grid (col tiles, row tiles, count).
-__global__ void __launch_bounds__(256) orth_split_kernel(OrthOuter o, const double *part, int parts, __half *x, long ld, float scale) {
-    __shared__ float tile[64][65];
-    __shared__ double norm_sh;
-    ptx::grid_launch();
-    ptx::grid_wait();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const size_t mat = blockIdx.z;
+// The halves of X0, [2 count][S][ld] (high and low of a matrix in turn), from the `parts` partial sums of squares: this block's share (the `member`-th
+// of `members`).  tall: tiles of 64 x 64 through shared memory, 64 x 65 floats at `tile`.  sh: room for a double.  All threads of the block.
+__device__ __forceinline__ void orth_split(const OrthOuter &o, size_t mat, const double *part, int parts, __half *x, long ld, float scale, float *tile, double *sh,
+                                           int member, int members) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    __syncthreads();
     if (warp == 0) {
         double sum = 0.0;
-        for (int i = lane; i < parts; i += 32) sum += part[mat * parts + i];
+        for (int i = lane; i < parts; i += 32) sum += __ldcg(part + i);
 #pragma unroll
         for (int k = 16; k > 0; k >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, k);
-        if (lane == 0) norm_sh = (double)scale / (sqrt(sum) + (double)o.eps);
+        if (lane == 0) *sh = (double)scale / (sqrt(sum) + (double)o.eps);
     }
+    __syncthreads();
+    const double f = *sh;
     const int S = o.tall ? o.cols : o.rows, L = o.tall ? o.rows : o.cols;
     __half *hi = x + 2 * mat * S * ld, *lo = hi + S * ld;
     if (!o.tall) {
-        __syncthreads();
-        const double f = norm_sh;
-        orth_elements<true>(o, mat, blockIdx.x * 256 + threadIdx.x, gridDim.x * 256, [&](int r, int c, const auto &u) {
+        orth_elements<true>(o, mat, member * blockDim.x + threadIdx.x, members * blockDim.x, [&](int r, int c, const auto &u) {
             constexpr int V = sizeof(u) / sizeof(float);
             const size_t at = (size_t)r * ld + c;
             if constexpr (V == 1) split_half((float)(u[0] * f), hi[at], lo[at]);
@@ -259,38 +263,48 @@ __global__ void __launch_bounds__(256) orth_split_kernel(OrthOuter o, const doub
         });
         return;
     }
-    // the tile as a matrix of its own
-    const int r0 = blockIdx.y * 64, c0 = blockIdx.x * 64;
-    with_type(o.g_type, [&](auto type) {
-        using G = decltype(type);
-        const G *g = static_cast<const G *>(o.g) + mat * o.step_g;
-        const float *m = o.m ? o.m_out + mat * (size_t)o.rows * o.cols : nullptr;
+    const int tiles_c = (o.cols + 63) / 64, tiles = tiles_c * ((o.rows + 63) / 64);
+    for (int t = member; t < tiles; t += members) {
+        const int r0 = t / tiles_c * 64, c0 = t % tiles_c * 64;
+        with_type(o.g_type, [&](auto type) {
+            using G = decltype(type);
+            const G *g = static_cast<const G *>(o.g) + mat * o.step_g;
+            const float *m = o.m ? o.m_out + mat * (size_t)o.rows * o.cols : nullptr;
+            for (int i0 = threadIdx.x; i0 < 4096; i0 += 8 * blockDim.x) {
+                float u[8], q[8];
 #pragma unroll
-        for (int i0 = 0; i0 < 16; i0 += 8) {
-            float u[8], q[8];
+                for (int k = 0; k < 8; ++k) {
+                    const int i = i0 + k * blockDim.x, r = r0 + (i >> 6), c = c0 + (i & 63);
+                    const bool yes = i < 4096 && r < o.rows && c < o.cols;
+                    u[k] = yes ? to_f32(g[(size_t)r * o.ld_g + c]) : 0.f;
+                    q[k] = yes && m ? m[(size_t)r * o.cols + c] : 0.f;
+                }
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int r = r0 + (i0 + i) * 4 + (threadIdx.x >> 6), c = c0 + (threadIdx.x & 63);
-                const bool yes = r < o.rows && c < o.cols;
-                u[i] = yes ? to_f32(g[(size_t)r * o.ld_g + c]) : 0.f;
-                q[i] = yes && m ? m[(size_t)r * o.cols + c] : 0.f;
+                for (int k = 0; k < 8; ++k) {
+                    const int i = i0 + k * blockDim.x;
+                    if (i < 4096) tile[(i >> 6) * 65 + (i & 63)] = !m ? u[k] : o.nesterov ? fmaf(o.momentum, q[k], (1.f - o.momentum) * u[k]) : q[k];
+                }
             }
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                tile[(i0 + i) * 4 + (threadIdx.x >> 6)][threadIdx.x & 63] = !m ? u[i] : o.nesterov ? fmaf(o.momentum, q[i], (1.f - o.momentum) * u[i]) : q[i];
-        }
-    });
-    __syncthreads();
-    const double f = norm_sh;
-    const int l = r0 + 2 * lane;
-    for (int s = warp; s < 64; s += 8)
-        if (c0 + s < S && l < L) {                                   // (ld is even; what is beyond the last column is never read)
-            uint32_t low;
-            const uint32_t high = half_pair((float)(tile[2 * lane][s] * f), (float)(tile[2 * lane + 1][s] * f), low);
-            const size_t at = (size_t)(c0 + s) * ld + l;
-            *reinterpret_cast<uint32_t *>(hi + at) = high;
-            *reinterpret_cast<uint32_t *>(lo + at) = low;
-        }
+        });
+        __syncthreads();
+        const int l = r0 + 2 * lane;
+        for (int s = warp; s < 64; s += warps)
+            if (c0 + s < S && l < L) {                               // (ld is even; what is beyond the last column is never read)
+                uint32_t low;
+                const uint32_t high = half_pair((float)(tile[2 * lane * 65 + s] * f), (float)(tile[(2 * lane + 1) * 65 + s] * f), low);
+                const size_t at = (size_t)(c0 + s) * ld + l;
+                *reinterpret_cast<uint32_t *>(hi + at) = high;
+                *reinterpret_cast<uint32_t *>(lo + at) = low;
+            }
+        __syncthreads();
+    }
+}
+__global__ void __launch_bounds__(256) orth_split_kernel(OrthOuter o, const double *part, int parts, __half *x, long ld, float scale) {
+    __shared__ float tile[64 * 65];
+    __shared__ double sh;
+    ptx::grid_launch();
+    ptx::grid_wait();
+    orth_split(o, blockIdx.y, part + (size_t)blockIdx.y * parts, parts, x, ld, scale, tile, &sh, blockIdx.x, gridDim.x);
 }
 
 // ---------------------------------------------------------------- one product
@@ -300,17 +314,15 @@ __host__ __device__ constexpr uint32_t instr_desc_f16(int m, int n, int b_mn) {
 }
 
 struct OrthProduct {
-    __half *dst;                 // halves of the result [2 count][S][ld_dst]
     const __half *a;             // halves of A (kOrthPoly) [2 count][S][ld_a]
-    long ld_dst, ld_a;
+    long ld_a;
     int S, N, K;                 // result [S, N], sums over K
     int tiles_m, tiles_n, tiles; // tiles of a matrix, down, across and in all
-    int total;                   // of all matrices
-    int ks;                      // blocks of a cluster that share a tile's K (single blocks only)
+    int upper;                   // a symmetric result: tiles on and above the diagonal, each stored twice
     float f, fa, fi;             // result = f sums (+ fa A + fi I)
-    OrthOuter o;                 // kOrthLast
-    uint32_t *status;
 };
+// A matrix of halves in the three forms its tiles are moved in: loaded (64 x 64), stored (32 rows of 64), stored transposed (64 rows of 32).
+struct HalfMaps { CUtensorMap load, store, store_t; };
 
 // Warp 0 loads, warp 1 issues, warps 4 to 11 take the sums out of tensor memory.
 constexpr int kOrthThreads = 384, kOrthStages = 3, kOrthChunk = 8;  // 64-deep steps whose sums stay in tensor memory
@@ -403,299 +415,501 @@ __device__ __forceinline__ void outer_piece(const OrthOuter &o, size_t mat, int 
     __syncwarp();
 }
 
-// E: type of the output (kOrthLast).
-template <int kKind, int kPair, typename E>
-__global__ void __launch_bounds__(kOrthThreads, 1)
-orth_product_kernel(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtensorMap tb, const __grid_constant__ CUtensorMap out,
-                    const __grid_constant__ CUtensorMap out_t, const OrthProduct p) {
-    extern __shared__ uint8_t raw[];
-    __shared__ uint32_t tmem_slot;
-    __shared__ volatile uint32_t abort_flag;
-    uint8_t *smem = ptx::align_1024(raw);
-    constexpr bool kSymmetric = kKind == kOrthGram || kKind == kOrthPoly;
-    constexpr int kTileN = 128 * kPair, kCols = kTileN / 2;              // columns of the tile, of a result warp
-    const uint32_t smem0 = ptx::smem_u32(smem), pieces0 = smem0 + kOrthStages * kOrthStage, bars = pieces0 + 8 * kOrthPiece;
-    auto full = [&](int s) { return bars + 8 * s; };
-    auto empty = [&](int s) { return bars + 8 * (kOrthStages + s); };
-    auto acc_full = [&](int b) { return bars + 8 * (2 * kOrthStages + b); };
-    auto acc_empty = [&](int b) { return bars + 8 * (2 * kOrthStages + 2 + b); };
-    const int warp = ptx::warp_index(), lane = threadIdx.x & 31;
-    const int in_pair = kPair == 2 ? (int)(blockIdx.x & 1) : 0;          // this block's half of the pair's tile
-    const int rank = kPair == 1 && p.ks > 1 ? (int)(blockIdx.x % p.ks) : 0, group = blockIdx.x / (kPair * p.ks), groups = gridDim.x / (kPair * p.ks);
-    const int blocks = (p.K + 63) / 64, kb0 = (int)((long)blocks * rank / p.ks), kb1 = (int)((long)blocks * (rank + 1) / p.ks);
-    const int chunks = (kb1 - kb0 + kOrthChunk - 1) / kOrthChunk;
+// Barriers and tensor memory of a block's pipeline, and how far it has come: stages loaded or issued, sets of sums handed over (each role
+// counts for itself).
+struct OrthPipe {
+    uint32_t smem0, pieces0, bars, tmem;
+    uint8_t *smem;
+    volatile uint32_t *abort_flag;
+    uint32_t n, c;
+    __device__ __forceinline__ uint32_t full(uint32_t s) const { return bars + 8 * s; }
+    __device__ __forceinline__ uint32_t empty(uint32_t s) const { return bars + 8 * (kOrthStages + s); }
+    __device__ __forceinline__ uint32_t acc_full(uint32_t b) const { return bars + 8 * (2 * kOrthStages + b); }
+    __device__ __forceinline__ uint32_t acc_empty(uint32_t b) const { return bars + 8 * (2 * kOrthStages + 2 + b); }
+};
+// What this block (or pair) does of a product: tiles t0, t0 + step .. of `total` (all matrices from `mat` on), the steps kb0 .. kb1 along K of each.
+struct OrthShare { int t0, step, total, mat, kb0, kb1; };
+struct OrthTile { int mat, i, j; };
+__device__ __forceinline__ bool orth_symmetric(int kind) { return kind == kOrthGram || kind == kOrthPoly; }
+__device__ __forceinline__ OrthTile orth_tile(const OrthProduct &p, const OrthShare &w, int t) {
+    OrthTile x;
+    x.mat = t / p.tiles;
+    t -= x.mat * p.tiles;
+    x.mat += w.mat;
+    if (p.upper) upper_tile(t, p.tiles_n, x.i, x.j);
+    else { x.i = t % p.tiles_m; x.j = t / p.tiles_m; }
+    return x;
+}
 
+// Sets the pipeline up; all threads of the block.
+template <int kPair>
+__device__ __forceinline__ OrthPipe orth_pipe(uint8_t *raw, uint32_t *tmem_slot, volatile uint32_t *abort_flag) {
+    OrthPipe q;
+    q.smem = ptx::align_1024(raw);
+    q.smem0 = ptx::smem_u32(q.smem);
+    q.pieces0 = q.smem0 + kOrthStages * kOrthStage;
+    q.bars = q.pieces0 + 8 * kOrthPiece;
+    q.abort_flag = abort_flag;
+    q.n = q.c = 0;
     if (threadIdx.x == 0) {
-        abort_flag = 0;
-        for (int s = 0; s < kOrthStages; ++s) { ptx::mbar_init(full(s), 1); ptx::mbar_init(empty(s), 1); }
-        for (int b = 0; b < 2; ++b) { ptx::mbar_init(acc_full(b), 1); ptx::mbar_init(acc_empty(b), 8 * kPair); }
+        *abort_flag = 0;
+        for (int s = 0; s < kOrthStages; ++s) { ptx::mbar_init(q.full(s), 1); ptx::mbar_init(q.empty(s), 1); }
+        for (int b = 0; b < 2; ++b) { ptx::mbar_init(q.acc_full(b), 1); ptx::mbar_init(q.acc_empty(b), 8 * kPair); }
         ptx::fence_mbar_init();
     }
-    if (warp == 1) ptx::tmem_alloc_for<kPair>(ptx::smem_u32(&tmem_slot), 2 * kTileN);
+    if (ptx::warp_index() == 1) ptx::tmem_alloc_for<kPair>(ptx::smem_u32(tmem_slot), 256 * kPair);
     ptx::tc_fence_before();
     __syncthreads();
     if (kPair == 2) ptx::cluster_meet();
     ptx::tc_fence_after();
-    const uint32_t tmem = tmem_slot;
-    ptx::grid_launch();
-    ptx::grid_wait();
-
-    struct Tile { int mat, i, j; };
-    auto tile_of = [&](int t) {
-        Tile x;
-        x.mat = t / p.tiles;
-        t -= x.mat * p.tiles;
-        if (kSymmetric) upper_tile(t, p.tiles_n, x.i, x.j);
-        else { x.i = t % p.tiles_m; x.j = t / p.tiles_m; }
-        return x;
-    };
-    // Registers of a pair's launch, 384 x 168, as 128 x 40 (this and the issuing warp, two that idle) and 256 x 232: the result warps' hold their
-    // 128 sums.
-    if (warp == 0) {
-        if (kPair == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
-        if (ptx::elect_one()) {
-            asm volatile("fence.proxy.async.global;" ::: "memory");      // (what the launches before this one stored, for the loads by TMA)
-            uint32_t n = 0;
-            bool ok = true;
-            for (int t = group; t < p.total && ok; t += groups) {
-                const Tile x = tile_of(t);
-                const bool own = kSymmetric && x.i == x.j;               // both factors are the same rows
-                const int ra = x.i * kTileN + in_pair * 128, rb = x.j * kTileN + in_pair * 128;
-                for (int kb = kb0; kb < kb1; ++kb, ++n) {
-                    const int s = n % kOrthStages;
-                    if (n >= kOrthStages && !(ok = ptx::mbar_wait(empty(s), (n / kOrthStages - 1) & 1, &abort_flag, 101))) break;
-                    const uint32_t at = smem0 + s * kOrthStage, bar = kPair == 2 ? ptx::in_block(full(s), 0) : full(s);
-                    if (in_pair == 0) ptx::mbar_arrive_expect_tx(full(s), kPair * (own ? 2 : 4) * kOrthHalfTile);
-#pragma unroll
-                    for (int h = 0; h < 2; ++h)
-#pragma unroll
-                        for (int q = 0; q < 2; ++q) {
-                            ptx::tma_load_3d_for<kPair>(at + h * kOrthHalfTile + q * 8192, &ta, bar, kb * 64, ra + q * 64, 2 * x.mat + h);
-                            if (own) continue;
-                            if (kSymmetric) ptx::tma_load_3d_for<kPair>(at + (2 + h) * kOrthHalfTile + q * 8192, &tb, bar, kb * 64, rb + q * 64, 2 * x.mat + h);
-                            else ptx::tma_load_3d_for<kPair>(at + (2 + h) * kOrthHalfTile + q * 8192, &tb, bar, rb + q * 64, kb * 64, 2 * x.mat + h);
-                        }
-                }
-            }
-        }
-        __syncwarp();
-        if (kPair == 1 && p.ks > 1) ptx::cluster_meet();
-    } else if (warp == 1) {
-        if (kPair == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
-        if (in_pair == 0 && ptx::elect_one()) {
-            constexpr uint32_t idesc = instr_desc_f16(128 * kPair, kTileN, kSymmetric ? 0 : 1), hi = ptx::desc_hi(1024, 2);
-            constexpr uint32_t b_lbo = kSymmetric ? 16 : 8192, b_step = (kSymmetric ? 32 : 2048) >> 4, low = kOrthHalfTile >> 4;
-            uint32_t n = 0, c = 0;
-            bool ok = true;
-            for (int t = group; t < p.total && ok; t += groups) {
-                const Tile x = tile_of(t);
-                const bool own = kSymmetric && x.i == x.j;
-                for (int kb = kb0; kb < kb1 && ok; ++c) {
-                    const uint32_t acc = tmem + (c & 1) * kTileN;
-                    if (c >= 2 && !(ok = ptx::mbar_wait(acc_empty(c & 1), (c / 2 - 1) & 1, &abort_flag, 102))) break;
-                    ptx::tc_fence_after();
-                    for (int k1 = min(kb + kOrthChunk, kb1), first = 1; kb < k1; ++kb, ++n, first = 0) {
-                        const int s = n % kOrthStages;
-                        if (!(ok = ptx::mbar_wait(full(s), (n / kOrthStages) & 1, &abort_flag, 103))) break;
-                        ptx::tc_fence_after();
-                        const uint32_t at = smem0 + s * kOrthStage;
-                        const uint32_t a0 = ptx::desc_lo(at, 16), b0 = ptx::desc_lo(own ? at : at + 2 * kOrthHalfTile, b_lbo);
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            const uint32_t a = a0 + k * 2, b = b0 + k * b_step;
-                            ptx::mma_ss_for<kPair>(acc, ptx::desc(a + low, hi), ptx::desc(b, hi), idesc, !first || k > 0);
-                            ptx::mma_ss_for<kPair>(acc, ptx::desc(a, hi), ptx::desc(b + low, hi), idesc, 1);
-                            ptx::mma_ss_for<kPair>(acc, ptx::desc(a, hi), ptx::desc(b, hi), idesc, 1);
-                        }
-                        ptx::mma_commit_for<kPair>(empty(s));
-                    }
-                    if (ok) ptx::mma_commit_for<kPair>(acc_full(c & 1));
-                }
-            }
-        }
-        __syncwarp();
-        if (kPair == 1 && p.ks > 1) ptx::cluster_meet();
-    } else if (warp < 4) {
-        if (kPair == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
-        if (kPair == 1 && p.ks > 1) ptx::cluster_meet();
-    } else {
-        if (kPair == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
-        const int quad = warp & 3, half = (warp - 4) >> 2, lr = quad * 32 + lane;
-        const uint32_t acc = tmem + ((uint32_t)(quad * 32) << 16) + half * kCols;
-        const uint32_t piece = pieces0 + (warp - 4) * kOrthPiece;
-        uint8_t *piece_p = smem + kOrthStages * kOrthStage + (warp - 4) * kOrthPiece;
-        uint32_t c = 0;
-        bool ok = true;
-        for (int t = group; t < p.total && ok; t += groups) {
-            const Tile x = tile_of(t);
-            float v[kCols];
-            for (int q = 0; q < chunks; ++q, ++c) {
-                ok = ptx::mbar_wait(acc_full(c & 1), (c / 2) & 1, &abort_flag, 104);
-                if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
-                ptx::tc_fence_after();
-#pragma unroll
-                for (int k = 0; k < kCols; k += 32) {
-                    uint32_t u[32];
-                    ptx::tmem_ld32(acc + (c & 1) * kTileN + k, u);
-                    ptx::tmem_wait_ld();
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) v[k + e] = q == 0 ? __uint_as_float(u[e]) : v[k + e] + __uint_as_float(u[e]);
-                }
-                ptx::tc_fence_before();
-                __syncwarp();
-                if (lane == 0) {
-                    if (kPair == 2) ptx::mbar_arrive_cluster(ptx::in_block(acc_empty(c & 1), 0));
-                    else ptx::mbar_arrive(acc_empty(c & 1));
-                }
-            }
-            if (!ok) break;
-            const int row0 = x.i * kTileN + in_pair * 128 + quad * 32, row = row0 + lane, col0 = x.j * kTileN + half * kCols;
-            if (kPair == 1 && p.ks > 1) {
-                // the cluster's sums meet below: this block's in shared memory by columns
-                float *part = reinterpret_cast<float *>(smem);
-#pragma unroll
-                for (int k = 0; k < kCols; ++k) part[(half * kCols + k) * 128 + lr] = v[k];
-                break;
-            }
-            if (kKind == kOrthLast) {
-#pragma unroll
-                for (int k = 0; k < kCols; k += 32)
-                    if (row0 < p.S && col0 + k < p.N)
-                        outer_piece<E>(p.o, x.mat, row0, col0 + k, p.S, p.N, v + k, p.f, reinterpret_cast<float *>(piece_p));
-                continue;
-            }
-            const __half *ah = p.a + 2 * x.mat * (long)p.S * p.ld_a + (long)row * p.ld_a + col0, *al = ah + (long)p.S * p.ld_a;
-#pragma unroll
-            for (int k = 0; k < kCols; k += 8) {
-                float a[8];
-                if (kKind == kOrthPoly) {
-                    uint4 h = make_uint4(0, 0, 0, 0), l = h;
-                    if (row < p.S && col0 + k < p.N) {
-                        h = *reinterpret_cast<const uint4 *>(ah + k);
-                        l = *reinterpret_cast<const uint4 *>(al + k);
-                    }
-                    join8(h, l, a);
-                }
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    v[k + e] = kKind == kOrthPoly ? fmaf(p.fa, a[e], p.f * v[k + e]) + (row == col0 + k + e ? p.fi : 0.f) : p.f * v[k + e];
-            }
-#pragma unroll
-            for (int k = 0; k < kCols; k += 64) {
-                if (row0 >= p.S || col0 + k >= p.N) continue;            // (uniform over the warp)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    // 32 rows of 64 columns, 128-byte swizzle; then what the other half is formed from
-                    if (lane == 0) ptx::tma_store_wait<true>();
-                    __syncwarp();
-#pragma unroll
-                    for (int e = 0; e < 64; e += 8) {
-                        uint4 vh, vl;
-                        split8(v + k + e, vh, vl);
-                        const uint4 &w = h == 0 ? vh : vl;
-                        const uint32_t r[4] = {w.x, w.y, w.z, w.w};
-                        ptx::sts128(piece + lane * 128 + (((e >> 3) ^ (lane & 7)) << 4), r);
-                    }
-                    ptx::fence_proxy_async_smem();
-                    __syncwarp();
-                    if (lane == 0) {
-                        ptx::tma_store_3d(&out, piece, col0 + k, row0, 2 * x.mat + h);
-                        ptx::tma_store_commit();
-                    }
-                    if (!kSymmetric || x.i == x.j) continue;
-                    // the same 64 columns as rows of 32: 64-byte swizzle
-                    if (lane == 0) ptx::tma_store_wait<true>();
-                    __syncwarp();
-#pragma unroll
-                    for (int e = 0; e < 64; ++e) {
-                        __half vh, vl;
-                        split_half(v[k + e], vh, vl);
-                        *reinterpret_cast<__half *>(piece_p + e * 64 + (((lane >> 3) ^ ((e >> 1) & 3)) << 4) + (lane & 7) * 2) = h == 0 ? vh : vl;
-                    }
-                    ptx::fence_proxy_async_smem();
-                    __syncwarp();
-                    if (lane == 0) {
-                        ptx::tma_store_3d(&out_t, piece, row0, col0 + k, 2 * x.mat + h);
-                        ptx::tma_store_commit();
-                    }
-                }
-            }
-        }
-        if (lane == 0) ptx::tma_store_wait<false>();
-        __syncwarp();
-        if (kPair == 1 && p.ks > 1) {
-            // each block of the cluster adds up its share of the tile's columns, a thread some of them of one row
-            __syncwarp();
-            ptx::cluster_meet();
-            const Tile x = tile_of(group);
-            const int row = x.i * 128 + lr;
-            const long plane = (long)p.S * p.ld_dst;
-            for (int c = (rank * 2 + half) * 8, c1 = row < p.S ? 128 : 0; c < c1; c += 16 * p.ks) {
-                const int col = x.j * 128 + c;
-                if (col >= p.N) break;
-                float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-                for (int r = 0; r < p.ks; ++r) {
-                    const uint32_t from = ptx::in_block(smem0 + (uint32_t)(c * 128 + lr) * 4, r);
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        float y;
-                        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(y) : "r"(from + k * 512) : "memory");
-                        v[k] += y;
-                    }
-                }
-                if (kKind == kOrthLast) {
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) v[k] *= p.f;
-                    {
-                        const size_t step = p.o.tall ? (size_t)p.o.ld_out : 1,
-                                     at = x.mat * p.o.step_out + (p.o.tall ? (size_t)col * p.o.ld_out + row : (size_t)row * p.o.ld_out + col);
-                        const int n = min(8, p.N - col);
-                        if (p.o.w) {
-                            float w[8];
-#pragma unroll
-                            for (int k = 0; k < 8; ++k) w[k] = k < n ? to_f32(static_cast<const E *>(p.o.w)[at + k * step]) : 0.f;
-#pragma unroll
-                            for (int k = 0; k < 8; ++k) v[k] = fmaf(-p.o.rate, v[k], p.o.keep * w[k]);
-                        }
-#pragma unroll
-                        for (int k = 0; k < 8; ++k)
-                            if (k < n) from_f32(static_cast<E *>(p.o.out)[at + k * step], v[k]);
-                    }
-                    continue;
-                }
-                __half *hi = p.dst + 2 * x.mat * plane, *lo = hi + plane;
-                if (kKind == kOrthPoly) {
-                    const __half *ah = p.a + 2 * x.mat * (long)p.S * p.ld_a + (long)row * p.ld_a + col;
-                    float a[8];
-                    join8(*reinterpret_cast<const uint4 *>(ah), *reinterpret_cast<const uint4 *>(ah + (long)p.S * p.ld_a), a);
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) v[k] = fmaf(p.fa, a[k], p.f * v[k]) + (row == col + k ? p.fi : 0.f);
-                } else {
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) v[k] *= p.f;
-                }
-                uint4 vh, vl;                                            // (ld_dst is a multiple of 8: what is beyond the last column is never read)
-                split8(v, vh, vl);
-                *reinterpret_cast<uint4 *>(hi + (long)row * p.ld_dst + col) = vh;
-                *reinterpret_cast<uint4 *>(lo + (long)row * p.ld_dst + col) = vl;
-                if (kSymmetric && x.i != x.j) {
-#pragma unroll
-                    for (int k = 0; k < 8; ++k)
-                        if (col + k < p.N) split_half(v[k], hi[(long)(col + k) * p.ld_dst + row], lo[(long)(col + k) * p.ld_dst + row]);
-                }
-            }
-            __syncwarp();
-        }
-    }
-    __syncwarp();
+    q.tmem = *tmem_slot;
+    return q;
+}
+template <int kPair>
+__device__ __forceinline__ void orth_pipe_end(const OrthPipe &q, uint32_t *status) {
     ptx::tc_fence_before();
     __syncthreads();
-    if (kPair == 2 || p.ks > 1) ptx::cluster_meet();                     // (nobody's shared or tensor memory is needed any more)
-    if (threadIdx.x == 0 && abort_flag != 0) p.status[0] = abort_flag;
-    if (warp == 1) {
+    if (kPair == 2) ptx::cluster_meet();                                 // (nobody's shared or tensor memory is needed any more)
+    if (threadIdx.x == 0 && *q.abort_flag != 0) *status = *q.abort_flag;
+    if (ptx::warp_index() == 1) {
         ptx::tc_fence_after();
-        ptx::tmem_dealloc_for<kPair>(tmem, 2 * kTileN);
+        ptx::tmem_dealloc_for<kPair>(q.tmem, 256 * kPair);
     }
+}
+
+// The loading warp's part.  ta: rows of the left factor; tb: rows of the right one's transpose (kOrthGram, kOrthPoly: sums along rows) or the right
+// one's own rows.
+template <int kPair>
+__device__ __forceinline__ void orth_load(OrthPipe &q, const OrthProduct &p, const OrthShare &w, int kind, const CUtensorMap *ta, const CUtensorMap *tb) {
+    const bool symmetric = orth_symmetric(kind);
+    if (!ptx::elect_one()) return;
+    const int in_pair = kPair == 2 ? (int)(blockIdx.x & 1) : 0;
+    asm volatile("fence.proxy.async.global;" ::: "memory");              // (what was stored by others before this, for the loads by TMA)
+    for (int t = w.t0; t < w.total; t += w.step) {
+        const OrthTile x = orth_tile(p, w, t);
+        const bool own = symmetric && x.i == x.j;                       // both factors are the same rows
+        const int ra = x.i * 128 * kPair + in_pair * 128, rb = x.j * 128 * kPair + in_pair * 128;
+        for (int kb = w.kb0; kb < w.kb1; ++kb, ++q.n) {
+            const uint32_t s = q.n % kOrthStages;
+            if (q.n >= kOrthStages && !ptx::mbar_wait(q.empty(s), (q.n / kOrthStages - 1) & 1, q.abort_flag, 101)) return;
+            const uint32_t at = q.smem0 + s * kOrthStage, bar = kPair == 2 ? ptx::in_block(q.full(s), 0) : q.full(s);
+            if (in_pair == 0) ptx::mbar_arrive_expect_tx(q.full(s), kPair * (own ? 2 : 4) * kOrthHalfTile);
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    ptx::tma_load_3d_for<kPair>(at + h * kOrthHalfTile + r * 8192, ta, bar, kb * 64, ra + r * 64, 2 * x.mat + h);
+                    if (own) continue;
+                    if (symmetric) ptx::tma_load_3d_for<kPair>(at + (2 + h) * kOrthHalfTile + r * 8192, tb, bar, kb * 64, rb + r * 64, 2 * x.mat + h);
+                    else ptx::tma_load_3d_for<kPair>(at + (2 + h) * kOrthHalfTile + r * 8192, tb, bar, rb + r * 64, kb * 64, 2 * x.mat + h);
+                }
+        }
+    }
+}
+
+// The issuing warp's part (of a pair: its first block's).
+template <int kPair>
+__device__ __forceinline__ void orth_issue(OrthPipe &q, const OrthProduct &p, const OrthShare &w, int kind) {
+    const bool symmetric = orth_symmetric(kind);
+    constexpr int kTileN = 128 * kPair;
+    constexpr uint32_t hi = ptx::desc_hi(1024, 2), low = kOrthHalfTile >> 4;
+    const uint32_t idesc = instr_desc_f16(128 * kPair, kTileN, symmetric ? 0 : 1), b_lbo = symmetric ? 16 : 8192, b_step = (symmetric ? 32 : 2048) >> 4;
+    if (!ptx::elect_one()) return;
+    for (int t = w.t0; t < w.total; t += w.step) {
+        const OrthTile x = orth_tile(p, w, t);
+        const bool own = symmetric && x.i == x.j;
+        for (int kb = w.kb0; kb < w.kb1; ++q.c) {
+            const uint32_t acc = q.tmem + (q.c & 1) * kTileN;
+            if (q.c >= 2 && !ptx::mbar_wait(q.acc_empty(q.c & 1), (q.c / 2 - 1) & 1, q.abort_flag, 102)) return;
+            ptx::tc_fence_after();
+            for (int k1 = min(kb + kOrthChunk, w.kb1), first = 1; kb < k1; ++kb, ++q.n, first = 0) {
+                const uint32_t s = q.n % kOrthStages;
+                if (!ptx::mbar_wait(q.full(s), (q.n / kOrthStages) & 1, q.abort_flag, 103)) return;
+                ptx::tc_fence_after();
+                const uint32_t at = q.smem0 + s * kOrthStage;
+                const uint32_t a0 = ptx::desc_lo(at, 16), b0 = ptx::desc_lo(own ? at : at + 2 * kOrthHalfTile, b_lbo);
+                const int deep = min(4, (p.K - kb * 64 + 15) / 16);           // (what lies beyond K is zeros)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    if (k >= deep) break;
+                    const uint32_t a = a0 + k * 2, b = b0 + k * b_step;
+                    ptx::mma_ss_for<kPair>(acc, ptx::desc(a + low, hi), ptx::desc(b, hi), idesc, !first || k > 0);
+                    ptx::mma_ss_for<kPair>(acc, ptx::desc(a, hi), ptx::desc(b + low, hi), idesc, 1);
+                    ptx::mma_ss_for<kPair>(acc, ptx::desc(a, hi), ptx::desc(b, hi), idesc, 1);
+                }
+                ptx::mma_commit_for<kPair>(q.empty(s));
+            }
+            ptx::mma_commit_for<kPair>(q.acc_full(q.c & 1));
+        }
+    }
+}
+
+// The result warps' parts.  First a tile's sums into registers, a row a thread and half of the tile's columns: false if a wait gave up.
+template <int kPair>
+__device__ __forceinline__ bool orth_sums(OrthPipe &q, int chunks, float (&v)[64 * kPair]) {
+    constexpr int kTileN = 128 * kPair, kCols = 64 * kPair;
+    const int warp = ptx::warp_index(), quad = warp & 3, half = (warp - 4) >> 2, lane = threadIdx.x & 31;
+    const uint32_t acc = q.tmem + ((uint32_t)(quad * 32) << 16) + half * kCols;
+    for (int i = 0; i < chunks; ++i, ++q.c) {
+        const bool ok = ptx::mbar_wait(q.acc_full(q.c & 1), (q.c / 2) & 1, q.abort_flag, 104);
+        if (!__all_sync(0xffffffffu, ok)) return false;
+        ptx::tc_fence_after();
+#pragma unroll
+        for (int k = 0; k < kCols; k += 32) {
+            uint32_t u[32];
+            ptx::tmem_ld32(acc + (q.c & 1) * kTileN + k, u);
+            ptx::tmem_wait_ld();
+#pragma unroll
+            for (int e = 0; e < 32; ++e) v[k + e] = i == 0 ? __uint_as_float(u[e]) : v[k + e] + __uint_as_float(u[e]);
+        }
+        ptx::tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+            if (kPair == 2) ptx::mbar_arrive_cluster(ptx::in_block(q.acc_empty(q.c & 1), 0));
+            else ptx::mbar_arrive(q.acc_empty(q.c & 1));
+        }
+    }
+    return true;
+}
+// Then what they are for: kCols columns from col0 on of the warp's 32 rows from row0 on; mirror: the tile's transpose is stored too.
+// kRoomy: the stages are free (this is the block's only tile of the product), so that each piece has a place of its own and none waits for another.
+template <bool kRoomy, typename E, int kCols>
+__device__ __forceinline__ void orth_finish(const OrthPipe &q, const OrthProduct &p, const OrthOuter &o, int kind, int mat, int row0, int col0, bool mirror,
+                                            const CUtensorMap *out, const CUtensorMap *out_t, float (&v)[kCols]) {
+    const int warp = ptx::warp_index(), lane = threadIdx.x & 31, row = row0 + lane;
+    const uint32_t piece = kRoomy ? q.smem0 + (warp - 4) * 4 * kOrthPiece : q.pieces0 + (warp - 4) * kOrthPiece;
+    uint8_t *piece_p = q.smem + kOrthStages * kOrthStage + (warp - 4) * kOrthPiece;
+    if (kind == kOrthLast) {
+#pragma unroll
+        for (int k = 0; k < kCols; k += 32)
+            if (row0 < p.S && col0 + k < p.N) outer_piece<E>(o, mat, row0, col0 + k, p.S, p.N, v + k, p.f, reinterpret_cast<float *>(piece_p));
+        return;
+    }
+#pragma unroll
+    for (int k = 0; k < kCols; k += 64) {
+        if (row0 >= p.S || col0 + k >= p.N) continue;                    // (uniform over the warp)
+        if (kind == kOrthPoly) {
+            // all of the piece of A is asked for before any of it is used
+            const __half *ah = p.a + 2 * mat * (long)p.S * p.ld_a + (long)row * p.ld_a + col0 + k, *al = ah + (long)p.S * p.ld_a;
+            uint4 h[8], l[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                h[e] = l[e] = make_uint4(0, 0, 0, 0);
+                if (row < p.S && col0 + k + 8 * e < p.N) {
+                    h[e] = __ldcg(reinterpret_cast<const uint4 *>(ah) + e);   // (stored by other blocks of this very launch, it may be)
+                    l[e] = __ldcg(reinterpret_cast<const uint4 *>(al) + e);
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                float a[8];
+                join8(h[e], l[e], a);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int c = k + 8 * e + i;
+                    v[c] = fmaf(p.fa, a[i], p.f * v[c]) + (row == col0 + c ? p.fi : 0.f);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 64; ++e) v[k + e] *= p.f;
+        }
+        uint4 half[2][8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) split8(v + k + 8 * e, half[0][e], half[1][e]);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            // 32 rows of 64 columns, 128-byte swizzle
+            uint32_t at = piece + (kRoomy ? (2 * h) * kOrthPiece : 0);
+            if (!kRoomy) {
+                if (lane == 0) ptx::tma_store_wait<true>();
+                __syncwarp();
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const uint32_t r[4] = {half[h][e].x, half[h][e].y, half[h][e].z, half[h][e].w};
+                ptx::sts128(at + lane * 128 + ((e ^ (lane & 7)) << 4), r);
+            }
+            ptx::fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) {
+                ptx::tma_store_3d(out, at, col0 + k, row0, 2 * mat + h);
+                ptx::tma_store_commit();
+            }
+            if (!mirror) continue;
+            // the same 64 columns as rows of 32: 64-byte swizzle
+            if (!kRoomy) {
+                if (lane == 0) ptx::tma_store_wait<true>();
+                __syncwarp();
+            } else {
+                at += kOrthPiece;
+            }
+#pragma unroll
+            for (int e = 0; e < 64; ++e) {
+                const uint32_t word = (&half[h][e / 8].x)[(e / 2) & 3], x = e & 1 ? word >> 16 : word;
+                asm volatile("st.shared.b16 [%0], %1;" ::"r"(at + e * 64 + (((lane >> 3) ^ ((e >> 1) & 3)) << 4) + (lane & 7) * 2), "h"((uint16_t)x) : "memory");
+            }
+            ptx::fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) {
+                ptx::tma_store_3d(out_t, at, row0, col0 + k, 2 * mat + h);
+                ptx::tma_store_commit();
+            }
+        }
+    }
+}
+template <int kPair, typename E>
+__device__ __forceinline__ void orth_results_of(OrthPipe &q, const OrthProduct &p, const OrthShare &w, const OrthOuter &o, int kind, const CUtensorMap *out,
+                                                const CUtensorMap *out_t) {
+    constexpr int kTileN = 128 * kPair, kCols = 64 * kPair;
+    const int warp = ptx::warp_index(), quad = warp & 3, half = (warp - 4) >> 2, in_pair = kPair == 2 ? (int)(blockIdx.x & 1) : 0;
+    const int chunks = (w.kb1 - w.kb0 + kOrthChunk - 1) / kOrthChunk;
+    for (int t = w.t0; t < w.total; t += w.step) {
+        const OrthTile x = orth_tile(p, w, t);
+        float v[kCols];
+        if (!orth_sums<kPair>(q, chunks, v)) break;
+        orth_finish<false, E>(q, p, o, kind, x.mat, x.i * kTileN + in_pair * 128 + quad * 32, x.j * kTileN + half * kCols, p.upper && x.i != x.j, out, out_t, v);
+    }
+    if ((threadIdx.x & 31) == 0) ptx::tma_store_wait<false>();
+    __syncwarp();
+}
+
+// ---- large matrices: a launch per product, tiles of 256 x 256 by pairs of blocks
+//
+// Tensor memory adds with truncation, which over K = 4096 (768 additions of 16 products) is off by 2e-5 of a sum of equal signs, and by 9e-5 of the
+// 2-norm of the whole result: sums stay there for kOrthChunk steps (K = 512) and are added up in registers, rounded, while the next
+// ones run in a second set of columns: 1e-5.  (The same second set lets a tile's results go out under the next tile's products.)
+struct OrthPairArgs {
+    OrthProduct p;
+    OrthOuter o;                 // kOrthLast
+    int total;                   // tiles of all matrices
+    uint32_t *status;
+};
+// E: type of the output (kOrthLast).
+template <int kKind, typename E>
+__global__ void __launch_bounds__(kOrthThreads, 1)
+orth_pair_kernel(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtensorMap tb, const __grid_constant__ CUtensorMap out,
+                 const __grid_constant__ CUtensorMap out_t, const OrthPairArgs a) {
+    extern __shared__ uint8_t raw[];
+    __shared__ uint32_t tmem_slot;
+    __shared__ volatile uint32_t abort_flag;
+    OrthPipe q = orth_pipe<2>(raw, &tmem_slot, &abort_flag);
+    const int warp = ptx::warp_index();
+    const OrthShare w{(int)(blockIdx.x >> 1), (int)(gridDim.x >> 1), a.total, 0, 0, (a.p.K + 63) / 64};
+    ptx::grid_launch();
+    ptx::grid_wait();
+    // Registers of the launch, 384 x 168, as 128 x 40 (the loading and the issuing warp, two that idle) and 256 x 232: the result warps' hold their
+    // 128 sums.
+    if (warp == 0) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+        orth_load<2>(q, a.p, w, kKind, &ta, &tb);
+    } else if (warp == 1) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+        if ((blockIdx.x & 1) == 0) orth_issue<2>(q, a.p, w, kKind);
+    } else if (warp < 4) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
+        orth_results_of<2, E>(q, a.p, w, a.o, kKind, &out, &out_t);
+    }
+    __syncwarp();
+    orth_pipe_end<2>(q, a.status);
+}
+
+// ---- matrices in between: all products in one cooperative launch, a team of blocks to a matrix
+//
+// A launch per product costs some 8 us beside its work (138 us for 130 x 130, whose products take 20).  Here the blocks stay, one an SM, and
+// the blocks of a team wait for one another between products: a counter in memory, some 2 us.  Tiles are 128 x 128, a block each; where a
+// product has fewer tiles than the team blocks, ks blocks share a tile's K: each leaves its sums in memory (they stay in L2), and when all of a tile's
+// have arrived, each finishes its part of the tile's columns.
+struct OrthTeam {
+    OrthOuter o;
+    OrthProduct product[4];      // of each kind
+    int ks[4];                   // blocks that share a tile's K
+    __half *mem[4];              // X (two copies in turn), A, B
+    float *part;                 // [blocks][128 columns][128 rows]
+    uint32_t *counters;          // [teams] barriers, then [3][blocks] of tiles that several blocks share; zero at the start
+    uint32_t *status;
+    long ld_x, ld_s;
+    int S, L, count, steps;
+    int team, teams;             // blocks of a team, teams
+};
+
+struct OrthMaps { HalfMaps m[4]; };   // of mem
+
+// Waits (up to two seconds, or until some block has given up) for a counter to reach `target`.  One thread.
+__device__ __forceinline__ bool wait_count(const uint32_t *counter, uint32_t target, uint32_t *status) {
+    const uint64_t t0 = ptx::globaltimer_ns();
+    for (uint32_t spins = 1;; ++spins) {
+        uint32_t v;
+        asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(counter) : "memory");
+        if (v >= target) return true;
+        if ((spins & 63u) == 0) {
+            asm volatile("ld.relaxed.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(status) : "memory");
+            if (v != 0) return false;
+            if (ptx::globaltimer_ns() - t0 > ptx::kWaitBudgetNs) {
+                atomicExch(status, 105u);
+                return false;
+            }
+        }
+    }
+}
+__device__ __forceinline__ void add_count(uint32_t *counter) { asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(counter) : "memory"); }
+
+// All blocks of the team have got here, and what they stored is seen by all.  All threads of the block; the same in all of
+// them: false if some wait has given up.
+__device__ __forceinline__ bool team_meet(const OrthTeam &p, const OrthPipe &q, int team, uint32_t &target) {
+    target += p.team;
+    const bool sound = __syncthreads_and(*q.abort_flag == 0) != 0;
+    bool ok = true;
+    if (threadIdx.x == 0) {                                  // (one thread's release and acquire cover what the barriers around them order)
+        if (!sound) atomicExch(p.status, *q.abort_flag);
+        add_count(p.counters + team);
+        ok = wait_count(p.counters + team, target, p.status) && sound;
+    }
+    return __syncthreads_and(ok) != 0;
+}
+
+// The result warps' part where ks blocks share a tile's K, once this block's sums are in memory: when all of the tile's are, its share of the tile's
+// columns, eight at a time.
+template <typename E>
+__device__ __forceinline__ void team_join(const OrthTeam &p, const OrthPipe &q, const OrthProduct &d, const OrthTile &x, int kind, int team, int tile, int rank, int count,
+                                          int ks, __half *dst) {
+    const bool symmetric = orth_symmetric(kind);
+    const int warp = ptx::warp_index(), lane = threadIdx.x & 31, quad = warp & 3, half = (warp - 4) >> 2, lr = quad * 32 + lane, mat = x.mat;
+    asm volatile("bar.sync 1, 256;" ::: "memory");
+    if (threadIdx.x == 128) {
+        uint32_t *counter = p.counters + p.teams + (kind == kOrthGram ? 0 : kind == kOrthPoly ? 1 : 2) * gridDim.x + team * p.team + tile;
+        add_count(counter);
+        if (!wait_count(counter, (uint32_t)(ks * count), p.status)) *q.abort_flag = 106;
+    }
+    asm volatile("bar.sync 1, 256;" ::: "memory");
+    const int row = x.i * 128 + lr;
+    const float *all = p.part + (size_t)(team * p.team + tile * ks) * 128 * 128 + lr;
+    const bool mirror = d.upper && x.i != x.j;
+    if (*q.abort_flag == 0 && row < d.S) {
+#pragma unroll 1
+        for (int c = (rank * 2 + half) * 8; c < 128; c += 16 * ks) {
+            const int col = x.j * 128 + c;
+            if (col >= d.N) break;
+            float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+            for (int r = 0; r < ks; ++r) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[k] += __ldcg(all + ((size_t)r * 128 + c + k) * 128);
+            }
+            if (kind == kOrthLast) {
+                const OrthOuter &o = p.o;
+                const size_t apart = o.tall ? (size_t)o.ld_out : 1, at = mat * o.step_out + (o.tall ? (size_t)col * o.ld_out + row : (size_t)row * o.ld_out + col);
+                const int n = min(8, d.N - col);
+                float old[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) old[k] = o.w && k < n ? to_f32(static_cast<const E *>(o.w)[at + k * apart]) : 0.f;
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (k < n) from_f32(static_cast<E *>(o.out)[at + k * apart], o.w ? fmaf(-o.rate * d.f, v[k], o.keep * old[k]) : d.f * v[k]);
+                continue;
+            }
+            const long ld = symmetric ? p.ld_s : p.ld_x, plane = (long)d.S * ld;
+            __half *hi = dst + 2 * mat * plane, *lo = hi + plane;
+            if (kind == kOrthPoly) {
+                const __half *ah = d.a + 2 * mat * plane + (long)row * ld + col;
+                float a[8];
+                join8(__ldcg(reinterpret_cast<const uint4 *>(ah)), __ldcg(reinterpret_cast<const uint4 *>(ah + plane)), a);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[k] = fmaf(d.fa, a[k], d.f * v[k]) + (row == col + k ? d.fi : 0.f);
+            } else {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[k] *= d.f;
+            }
+            uint4 vh, vl;                                            // (ld is a multiple of 8: what is beyond the last column is never read)
+            split8(v, vh, vl);
+            *reinterpret_cast<uint4 *>(hi + (long)row * ld + col) = vh;
+            *reinterpret_cast<uint4 *>(lo + (long)row * ld + col) = vl;
+            if (mirror) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (col + k < d.N) split_half(v[k], hi[(long)(col + k) * ld + row], lo[(long)(col + k) * ld + row]);
+            }
+        }
+    }
+    asm volatile("fence.proxy.async.global;" ::: "memory");              // (loaded by TMA next)
+    __syncwarp();
+}
+template <bool kResults, typename E>
+__device__ __forceinline__ void team_product(const OrthTeam &p, OrthPipe &q, int kind, int team, int mat, int count, const HalfMaps *ta, const HalfMaps *tb,
+                                             const HalfMaps *out, __half *dst) {
+    const bool symmetric = orth_symmetric(kind);
+    const int warp = ptx::warp_index(), member = blockIdx.x % p.team;
+    const OrthProduct &d = p.product[kind];
+    const int blocks = (d.K + 63) / 64, ks = p.ks[kind];
+    // (with ks blocks a tile: member ks t + r has the r-th part of tile t's K, and no second tile)
+    const int rank = ks > 1 ? member % ks : 0, first = member / ks;
+    if (ks > 1 && first >= d.tiles) return;
+    const OrthShare w{first, ks > 1 ? d.tiles : p.team, d.tiles, mat, blocks * rank / ks, blocks * (rank + 1) / ks};
+    if constexpr (!kResults) {
+        if (warp == 0) orth_load<1>(q, d, w, kind, &ta->load, &tb->load);
+        else if (warp == 1) orth_issue<1>(q, d, w, kind);
+    } else {
+        const int quad = warp & 3, half = (warp - 4) >> 2, lane = threadIdx.x & 31, chunks = (w.kb1 - w.kb0 + kOrthChunk - 1) / kOrthChunk;
+        for (int t = w.t0; t < w.total; t += w.step) {
+            const OrthTile x = orth_tile(d, w, t);
+            float v[64];
+            if (!orth_sums<1>(q, chunks, v)) break;
+            if (ks == 1) {
+                const int row0 = x.i * 128 + quad * 32, col0 = x.j * 128 + half * 64;
+                const bool mirror = d.upper && x.i != x.j;
+                if (d.tiles <= p.team) {
+                    asm volatile("bar.sync 1, 256;" ::: "memory");           // (everybody's sums are complete, so no stage is in use)
+                    orth_finish<true, E>(q, d, p.o, kind, mat, row0, col0, mirror, &out->store, &out->store_t, v);
+                } else {
+                    orth_finish<false, E>(q, d, p.o, kind, mat, row0, col0, mirror, &out->store, &out->store_t, v);
+                }
+            } else {
+                float *mine = p.part + (size_t)blockIdx.x * 128 * 128 + (half * 64) * 128 + quad * 32 + lane;
+#pragma unroll
+                for (int k = 0; k < 64; ++k) __stcg(mine + k * 128, v[k]);
+            }
+        }
+        if (ks > 1) team_join<E>(p, q, d, orth_tile(d, w, first), kind, team, first, rank, count, ks, dst);
+        else if (lane == 0) ptx::tma_store_wait<false>();
+        __syncwarp();
+    }
+    __syncwarp();
+}
+
+template <bool kResults, typename E>
+__device__ __forceinline__ void team_run(const OrthMaps &maps, const OrthTeam &p, OrthPipe &q) {
+    const int team = blockIdx.x / p.team;
+    uint32_t met = 0;
+    bool ok = true;
+    int count = 0;                                           // steps this team has begun
+    for (int mat = team; mat < p.count && ok; mat += p.teams)
+        // three products a step, one piece of code for all
+        for (int i = 0; i < 3 * p.steps && ok; ++i) {
+            const int step = i / 3, stage = i - 3 * step, cur = step & 1, kind = stage < 2 ? stage : step + 1 < p.steps ? kOrthApply : kOrthLast;
+            const int left = stage == 0 ? cur : stage == 1 ? 2 : 3, right = stage == 1 ? 2 : cur, to = stage == 0 ? 2 : stage == 1 ? 3 : 1 - cur;
+            count += stage == 0;
+            team_product<kResults, E>(p, q, kind, team, mat, count, maps.m + left, maps.m + right, maps.m + to, p.mem[to]);
+            if (kind != kOrthLast || mat + p.teams < p.count) ok = team_meet(p, q, team, met);
+        }
+}
+template <typename E>
+__global__ void __launch_bounds__(kOrthThreads, 1) orth_team_kernel(const __grid_constant__ OrthMaps maps, const __grid_constant__ OrthTeam p) {
+    extern __shared__ uint8_t raw[];
+    __shared__ uint32_t tmem_slot;
+    __shared__ volatile uint32_t abort_flag;
+    OrthPipe q = orth_pipe<1>(raw, &tmem_slot, &abort_flag);
+    // Registers of the launch, 384 x 168, as 128 x 72 and 256 x 216.
+    if (ptx::warp_index() < 4) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+        team_run<false, E>(maps, p, q);
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+        team_run<true, E>(maps, p, q);
+    }
+    __syncwarp();
+    orth_pipe_end<1>(q, p.status);
 }
 
 // ---------------------------------------------------------------- a whole matrix in one block

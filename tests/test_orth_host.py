@@ -19,9 +19,10 @@ def desc(coefficients=flare.NEWTON_SCHULZ, **kw):
 
 def test_workspace(lib):
     need = lambda **kw: lib.flare_orthogonalize_workspace_bytes(ctypes.byref(desc(**kw)))  # noqa: E731
-    # two copies of X, A and B, in two 16-bit halves each, and little else; nothing but the header for what one thread block holds
+    # two copies of X, A and B, in two 16-bit halves each, at most a tile of 128 x 128 sums per SM, and little else; nothing but the header for what one
+    # thread block holds
     halves = 2 * 2 * 2 * (2 * 300 * 504 + 2 * 300 * 304)
-    assert halves <= need() <= halves + (1 << 16)
+    assert halves <= need() <= halves + 148 * 128 * 128 * 4 + (1 << 16)
     assert need(rows=128, cols=128) == 256 and need(rows=1024, cols=32) == 256
     assert need(rows=500, cols=300) == need()
     assert need(count=0) > 0

@@ -72,8 +72,8 @@ int norm_blocks(const flare_orth_desc_t *d, int sms) {
     return (int)std::max(1L, std::min(each, (8L * sms + d->count - 1) / std::max(1, d->count)));
 }
 // How a team does a product: blocks that share a tile's K, and of a symmetric result, whether only the upper tiles are computed.  In 64-deep steps of a
-// tile (some 768 cycles): sharing (the sums to memory, the wait, the sums from memory) costs about 8 of them, storing a tile's transpose 4, which
-// a team with blocks to spare saves by computing both; each product some 12 to start and to meet.
+// tile (1024 cycles with all blocks at work, see below): sharing (the sums to memory, the wait, the sums from memory) costs about 6 of them, storing a
+// tile's transpose 3, which a team with blocks to spare saves by computing both; each product some 9 to start and to meet.
 struct TeamPlan { int ks; bool upper; double cost; };
 TeamPlan team_plan(int team, long rows, long cols, bool symmetric, int K) {
     const int blocks = (K + 63) / 64;
@@ -83,7 +83,7 @@ TeamPlan team_plan(int team, long rows, long cols, bool symmetric, int K) {
         for (int ks = 1; ks <= 8; ++ks) {
             if (ks > 1 && ks * tiles > team) break;
             const long turns = ks > 1 ? 1 : (tiles + team - 1) / team;
-            const double cost = 12.0 + (double)turns * ((blocks + ks - 1) / ks + (ks > 1 ? 8 : 0) + (upper && rows > 1 ? 4 : 0));
+            const double cost = 9.0 + (double)turns * ((blocks + ks - 1) / ks + (ks > 1 ? 6 : 0) + (upper && rows > 1 ? 3 : 0));
             if (best.cost == 0.0 || cost < best.cost) best = TeamPlan{ks, upper != 0, cost};
         }
     }
@@ -99,12 +99,14 @@ OrthPlan orth_plan(const flare_orth_desc_t *d, int sms) {
     const int count = std::max(1, d->count);
     p.teams = std::min(count, sms);
     p.team = sms / p.teams;
-    // Time of a step, in cycles: a team's as above, matrices that have to wait for a team one after the other; a launch per product over pairs: 1536
-    // cycles each 64 of K and tile of four times the size, and some 16000 to start, finish and follow one another.
+    // Time of a step, in cycles: a team's as above, matrices that have to wait for a team one after the other (a tile's 64 of K are 768 cycles of matrix
+    // instructions, 1024 with what all blocks load at a time); a launch per product over pairs: 1536 cycles each 64 of K and tile of four times the size,
+    // and some 20000 to start, finish and follow one another.  Measured, us, teams : pairs: 256 x 256 125 : 232, 1024 x 4096 305 : 648, 2048 x 2048 454 : 685,
+    // 1500 x 6000 766 : 997, four of 2048 x 2048 1889 : 1793, 2500 x 2500 1277 : 991, 3600 x 3600 2619 : 3018, 4096 x 4096 3496 : 3364, two of it 8045 : 6480.
     const double rounds = (double)((count + p.teams - 1) / p.teams);
     const long s = (z.S + 127) / 128, l = (z.L + 127) / 128, s2 = (z.S + 255) / 256, l2 = (z.L + 255) / 256;
-    const double team = 800.0 * rounds * (team_plan(p.team, s, s, true, z.L).cost + team_plan(p.team, s, s, true, z.S).cost + team_plan(p.team, s, l, false, z.S).cost);
-    auto launch = [&](long tiles, int K) { return 16000.0 + (double)((tiles * count + sms / 2 - 1) / (sms / 2)) * ((K + 63) / 64) * 1536.0; };
+    const double team = 1024.0 * rounds * (team_plan(p.team, s, s, true, z.L).cost + team_plan(p.team, s, s, true, z.S).cost + team_plan(p.team, s, l, false, z.S).cost);
+    auto launch = [&](long tiles, int K) { return 20000.0 + (double)((tiles * count + sms / 2 - 1) / (sms / 2)) * ((K + 63) / 64) * 1536.0; };
     const double pairs = launch(s2 * (s2 + 1) / 2, z.L) + launch(s2 * (s2 + 1) / 2, z.S) + launch(s2 * l2, z.S);
     p.path = team <= pairs ? kOrthTeamPath : kOrthPairPath;
     return p;

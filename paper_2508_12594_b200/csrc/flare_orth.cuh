@@ -923,7 +923,7 @@ struct OrthSmall {
     int S, L, Mr, panels, steps;
     uint32_t *status;
 };
-constexpr int kOrthSmallThreads = 256;
+constexpr int kOrthSmallThreads = 512;
 struct OrthSmallSize {
     size_t x_half, a_half, total;
 };
@@ -999,6 +999,7 @@ __global__ void __launch_bounds__(kOrthSmallThreads, 1) orth_small_kernel(const 
     uint32_t phase = 0;
     constexpr uint32_t hi = ptx::desc_hi(1024, 2);
     const uint32_t dxh = ptx::smem_u32(xh), dxl = ptx::smem_u32(xl), dah = ptx::smem_u32(ah), dal = ptx::smem_u32(al), panel = (uint32_t)p.Mr * 128;
+    constexpr int kParts = kOrthSmallThreads / 128;           // warps that share a quarter of the rows
     const int quad = warp & 3, part = warp >> 2, row = quad * 32 + lane, tall_k = p.Mr / 16;
     const uint32_t acc = tmem + ((uint32_t)(quad * 32) << 16);
     // the three products of two split factors, one 16-deep step
@@ -1035,7 +1036,7 @@ __global__ void __launch_bounds__(kOrthSmallThreads, 1) orth_small_kernel(const 
         __syncwarp();
         if (!(ok = finish())) break;
         const float fg = p.sc.a / (p.sc.x * p.sc.x);
-        for (int c = part * 16; c < p.Mr; c += 32) {
+        for (int c = part * 16; c < p.Mr; c += 16 * kParts) {
             uint32_t u[16];
             ptx::tmem_ld16(acc + c, u);
             ptx::tmem_wait_ld();
@@ -1066,7 +1067,7 @@ __global__ void __launch_bounds__(kOrthSmallThreads, 1) orth_small_kernel(const 
         __syncwarp();
         if (!(ok = finish())) break;
         const float fp = p.sc.cc * p.sc.b / (p.sc.a * p.sc.a), fa = p.sc.cb * p.sc.b / p.sc.a, fi = p.sc.ca * p.sc.b;
-        for (int c = part * 16; c < p.Mr; c += 32) {
+        for (int c = part * 16; c < p.Mr; c += 16 * kParts) {
             uint32_t u[16];
             ptx::tmem_ld16(acc + c, u);
             ptx::tmem_wait_ld();
@@ -1104,7 +1105,7 @@ __global__ void __launch_bounds__(kOrthSmallThreads, 1) orth_small_kernel(const 
             }
             __syncwarp();
             if (!(ok = finish())) break;
-            for (int l = l0 + part * 16; l < l1; l += 32) {
+            for (int l = l0 + part * 16; l < l1; l += 16 * kParts) {
                 uint32_t u[16];
                 ptx::tmem_ld16(acc + (l - l0), u);
                 ptx::tmem_wait_ld();

@@ -209,11 +209,15 @@ int run_orth(const flare_orth_desc_t *d, const OrthScales &sc, OrthOuter o, void
     const int words = (int)((plan.path == kOrthTeamPath ? w.norm : kHeaderBytes) / sizeof(uint32_t));
     FLARE_CUDA(launch_after(orth_clear_kernel, 1, 256, 0, st, status, words));
     if (plan.path == kOrthSmallPath) {
-        static std::atomic<uint64_t> opt_in{0};
-        if (int rc = ensure_big_smem(orth_small_kernel, opt_in, 227 * 1024 - 512)) return rc;
         OrthSmall p{};
         p.o = o; p.sc = sc; p.S = z.S; p.L = z.L; p.Mr = (z.S + 15) / 16 * 16; p.panels = (z.L + 63) / 64; p.steps = d->steps; p.status = status;
-        FLARE_CUDA(launch_after(orth_small_kernel, (unsigned)d->count, kOrthSmallThreads, orth_small_size(z.S, z.L).total, st, p));
+        auto launch = [&](auto kernel, std::atomic<uint64_t> &opt_in) {
+            if (int rc = ensure_big_smem(kernel, opt_in, 227 * 1024 - 512)) return rc;
+            FLARE_CUDA(launch_after(kernel, (unsigned)d->count, kOrthSmallThreads, orth_small_size(z.S, z.L).total, st, p));
+            return (int)FLARE_OK;
+        };
+        static std::atomic<uint64_t> opt_narrow{0}, opt_wide{0};
+        if (int rc = z.S <= 64 ? launch(orth_small_kernel<true>, opt_narrow) : launch(orth_small_kernel<false>, opt_wide)) return rc;
         return FLARE_OK;
     }
     char *ws = static_cast<char *>(workspace);

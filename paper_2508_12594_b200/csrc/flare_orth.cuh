@@ -913,10 +913,15 @@ __global__ void __launch_bounds__(kOrthThreads, 1) orth_team_kernel(const __grid
 }
 
 // ---------------------------------------------------------------- a whole matrix in one block
-// S up to 128 and everything in shared memory: X as panels of 64 columns [ceil(L / 64)][Mr rows][128 bytes] (128-byte swizzle, Mr = S rounded up to
-// 16), high halves then low ones, and behind them A, overwritten by B, in the same form.  The same bytes serve as rows of X (sums along
-// rows) and as the right factor of B X (sums over rows).  The MMAs have 128 rows whatever S is; rows beyond Mr read what lies behind a
-// panel and their sums are not looked at.
+// S up to 128 and everything in shared memory: X as panels of 64 columns, rows of 128 bytes (128-byte swizzle), Mr = S rounded up to 16 of them in high
+// halves and as many in low ones, and behind them A, overwritten by B, in the same form.  The same bytes serve as rows of X (sums along
+// rows) and as the right factor of B X (sums over rows).  The MMAs have 128 rows whatever S is; rows beyond a panel's read what lies behind it
+// and their sums are not looked at.  Bound by how long the parts of a step follow one another: the MMAs read their factors from shared
+// memory (128 x 128: 95 cycles for 64 of arithmetic), and every sum goes through tensor memory, registers and a split once a product.
+//
+// kNarrow (S up to 64): the low halves are the panel's next Mr rows, so that one MMA forms high high, high low and low high of X X^T at a time (rows and
+// columns of both halves; the third comes back over from the lanes below), and B X is formed as its transpose, columns of X on the 128 lanes,
+// which all have work then.  Cycles of a step at 16 x 256: 7100 -> @.
 struct OrthSmall {
     OrthOuter o;
     OrthScales sc;
@@ -925,19 +930,21 @@ struct OrthSmall {
 };
 constexpr int kOrthSmallThreads = 512;
 struct OrthSmallSize {
-    size_t x_half, a_half, total;
+    size_t x_half, a_half, scratch, total;
 };
 __host__ __device__ inline OrthSmallSize orth_small_size(int S, int L) {
     OrthSmallSize z;
-    const size_t Mr = (size_t)(S + 15) / 16 * 16;
+    const size_t Mr = (size_t)(S + 15) / 16 * 16, rows = S <= 64 ? 2 * Mr : Mr;
     z.x_half = (size_t)((L + 63) / 64) * Mr * 128;
     z.a_half = (size_t)((S + 63) / 64) * Mr * 128;
-    z.total = 1024 + 2 * (z.x_half + z.a_half) + (128 - Mr) * 128 + 64;     // (what the rows beyond Mr of the last panel read is there)
+    z.scratch = 1024 + 2 * (z.x_half + z.a_half) + (128 - rows) * 128;     // (what the rows beyond the last panel's read is there)
+    z.total = z.scratch + (S <= 64 ? Mr * Mr * sizeof(float) : 0) + 64;
     return z;
 }
-// Byte offset of the eight columns from c (a multiple of 8) on of a row.
-__device__ __forceinline__ uint32_t panel_at(int row, int c, int Mr) { return (uint32_t)((c >> 6) * Mr + row) * 128 + ((((uint32_t)c >> 3) & 7) ^ (row & 7)) * 16; }
+// Byte offset of the eight columns from c (a multiple of 8) on of a row, `rows` rows a panel.
+__device__ __forceinline__ uint32_t panel_at(int row, int c, int rows) { return (uint32_t)((c >> 6) * rows + row) * 128 + ((((uint32_t)c >> 3) & 7) ^ (row & 7)) * 16; }
 
+template <bool kNarrow>
 __global__ void __launch_bounds__(kOrthSmallThreads, 1) orth_small_kernel(const OrthSmall p) {
     extern __shared__ uint8_t raw[];
     __shared__ uint32_t tmem_slot;
@@ -946,7 +953,8 @@ __global__ void __launch_bounds__(kOrthSmallThreads, 1) orth_small_kernel(const 
     __shared__ double sums[kOrthSmallThreads / 32];
     uint8_t *smem = ptx::align_1024(raw);
     const OrthSmallSize z = orth_small_size(p.S, p.L);
-    uint8_t *xh = smem, *xl = smem + z.x_half, *ah = smem + 2 * z.x_half, *al = ah + z.a_half;
+    const int Pr = kNarrow ? 2 * p.Mr : p.Mr;                 // rows of a panel
+    uint8_t *xh = smem, *xl = smem + (kNarrow ? (size_t)p.Mr * 128 : z.x_half), *ah = smem + 2 * z.x_half, *al = ah + (kNarrow ? (size_t)p.Mr * 128 : z.a_half);
     const uint32_t bar = ptx::smem_u32(&bar_word);
     const int warp = ptx::warp_index(), lane = threadIdx.x & 31;
     const size_t mat = blockIdx.x;
@@ -957,7 +965,7 @@ __global__ void __launch_bounds__(kOrthSmallThreads, 1) orth_small_kernel(const 
     }
     if (warp == 0) ptx::tmem_alloc(ptx::smem_u32(&tmem_slot), 512);
     // zeros in the rows and columns that X and A do not fill (and everywhere else, once)
-    for (size_t i = threadIdx.x; i < (z.total - 1024 - 64) / 16; i += kOrthSmallThreads) reinterpret_cast<uint4 *>(smem)[i] = make_uint4(0, 0, 0, 0);
+    for (size_t i = threadIdx.x; i < (z.scratch - 1024) / 16; i += kOrthSmallThreads) reinterpret_cast<uint4 *>(smem)[i] = make_uint4(0, 0, 0, 0);
     ptx::grid_launch();
     ptx::grid_wait();
     const OrthOuter &o = p.o;
@@ -978,14 +986,14 @@ __global__ void __launch_bounds__(kOrthSmallThreads, 1) orth_small_kernel(const 
             uint2 h, l;
             h.x = half_pair((float)(u[0] * f), (float)(u[1 % V] * f), l.x);
             h.y = half_pair((float)(u[2 % V] * f), (float)(u[3 % V] * f), l.y);
-            const uint32_t at = panel_at(r, c & ~7, p.Mr) + (c & 7) * 2;
+            const uint32_t at = panel_at(r, c & ~7, Pr) + (c & 7) * 2;
             *reinterpret_cast<uint2 *>(xh + at) = h;
             *reinterpret_cast<uint2 *>(xl + at) = l;
         } else {
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 const int s = o.tall ? c + i : r, l = o.tall ? r : c + i;
-                const uint32_t at = panel_at(s, l & ~7, p.Mr) + (l & 7) * 2;
+                const uint32_t at = panel_at(s, l & ~7, Pr) + (l & 7) * 2;
                 split_half((float)(u[i] * f), *reinterpret_cast<__half *>(xh + at), *reinterpret_cast<__half *>(xl + at));
             }
         }
@@ -998,7 +1006,7 @@ __global__ void __launch_bounds__(kOrthSmallThreads, 1) orth_small_kernel(const 
 
     uint32_t phase = 0;
     constexpr uint32_t hi = ptx::desc_hi(1024, 2);
-    const uint32_t dxh = ptx::smem_u32(xh), dxl = ptx::smem_u32(xl), dah = ptx::smem_u32(ah), dal = ptx::smem_u32(al), panel = (uint32_t)p.Mr * 128;
+    const uint32_t dxh = ptx::smem_u32(xh), dxl = ptx::smem_u32(xl), dah = ptx::smem_u32(ah), dal = ptx::smem_u32(al), panel = (uint32_t)Pr * 128;
     constexpr int kParts = kOrthSmallThreads / 128;           // warps that share a quarter of the rows
     const int quad = warp & 3, part = warp >> 2, row = quad * 32 + lane, tall_k = p.Mr / 16;
     const uint32_t acc = tmem + ((uint32_t)(quad * 32) << 16);
@@ -1021,93 +1029,140 @@ __global__ void __launch_bounds__(kOrthSmallThreads, 1) orth_small_kernel(const 
         __syncthreads();
         ptx::tc_fence_after();
     };
-    const int chunk_max = 512;
     bool ok = true;
-    for (int step = 0; step < p.steps && ok; ++step) {
-        // A = X X^T
-        if (warp == 0 && ptx::elect_one()) {
-            const uint32_t idesc = instr_desc_f16(128, p.Mr, 0);
-            for (int k = 0; k < 4 * p.panels; ++k) {
-                const uint32_t at = (k >> 2) * panel + (k & 3) * 32;
-                mma3(tmem, dxh + at, dxl + at, dxh + at, dxl + at, 16, idesc, k == 0);
+    const float fg = p.sc.a / (p.sc.x * p.sc.x), fp = p.sc.cc * p.sc.b / (p.sc.a * p.sc.a), fa = p.sc.cb * p.sc.b / p.sc.a, fi = p.sc.ca * p.sc.b, fx = 1.f / p.sc.b;
+    const int deep = (p.L + 15) / 16;
+    if constexpr (kNarrow) {
+        float *scratch = reinterpret_cast<float *>(smem + z.scratch - 1024);      // [column][row]: low high, on its way to the lanes of the high rows
+        // Rows of both halves times rows of both halves, a panel's 64 columns from `at` on in `steps` 16-deep steps.
+        auto square = [&](uint32_t at, int steps) {
+            if (warp == 0 && ptx::elect_one()) {
+                const uint32_t idesc = instr_desc_f16(128, 2 * p.Mr, 0);
+                for (int k = 0; k < steps; ++k) {
+                    const uint32_t lo = ptx::desc_lo(at + (k >> 2) * panel + (k & 3) * 32, 16);
+                    ptx::mma_ss(tmem, ptx::desc(lo, hi), ptx::desc(lo, hi), idesc, k > 0);
+                }
+                ptx::mma_commit(bar);
             }
-            ptx::mma_commit(bar);
-        }
-        __syncwarp();
-        if (!(ok = finish())) break;
-        const float fg = p.sc.a / (p.sc.x * p.sc.x);
-        for (int c = part * 16; c < p.Mr; c += 16 * kParts) {
-            uint32_t u[16];
-            ptx::tmem_ld16(acc + c, u);
-            ptx::tmem_wait_ld();
-            if (row < p.Mr) {
+            __syncwarp();
+        };
+        // its three parts added up, sixteen columns at a time of the rows below Mr: use(c, sums)
+        auto sums_of = [&](auto use) {
+            const bool low = row >= p.Mr && row < 2 * p.Mr;
+            for (int c = part * 16; c < p.Mr; c += 16 * kParts) {
+                uint32_t u[16];
+                ptx::tmem_ld16(acc + c, u);
+                ptx::tmem_wait_ld();
+                if (low) {
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) scratch[(c + k) * p.Mr + row - p.Mr] = __uint_as_float(u[k]);
+                }
+            }
+            __syncthreads();
+            if (quad * 32 < p.Mr)
+                for (int c = part * 16; c < p.Mr; c += 16 * kParts) {
+                    uint32_t u[16], w[16];
+                    ptx::tmem_ld16(acc + c, u);
+                    ptx::tmem_ld16(acc + p.Mr + c, w);
+                    ptx::tmem_wait_ld();
+                    float v[16];
+                    if (row < p.Mr) {
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) v[k] = (__uint_as_float(w[k]) + scratch[(c + k) * p.Mr + row]) + __uint_as_float(u[k]);
+                        use(c, v);
+                    }
+                    __syncwarp();
+                }
+        };
+        for (int step = 0; step < p.steps && ok; ++step) {
+            // A = X X^T
+            square(dxh, deep);
+            if (!(ok = finish())) break;
+            sums_of([&](int c, float (&v)[16]) {
 #pragma unroll
                 for (int q = 0; q < 2; ++q) {
-                    float v[8];
                     uint4 vh, vl;
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) v[k] = __uint_as_float(u[8 * q + k]) * fg;
-                    split8(v, vh, vl);
-                    const uint32_t at = panel_at(row, c + 8 * q, p.Mr);
+                    for (int k = 0; k < 8; ++k) v[8 * q + k] *= fg;
+                    split8(v + 8 * q, vh, vl);
+                    const uint32_t at = panel_at(row, c + 8 * q, Pr);
                     *reinterpret_cast<uint4 *>(ah + at) = vh;
                     *reinterpret_cast<uint4 *>(al + at) = vl;
                 }
-            }
-        }
-        ready();
-        // B = a I + b A + c A^2, over A
-        if (warp == 0 && ptx::elect_one()) {
-            const uint32_t idesc = instr_desc_f16(128, p.Mr, 0);
-            for (int k = 0; k < tall_k; ++k) {
-                const uint32_t at = (k >> 2) * panel + (k & 3) * 32;
-                mma3(tmem, dah + at, dal + at, dah + at, dal + at, 16, idesc, k == 0);
-            }
-            ptx::mma_commit(bar);
-        }
-        __syncwarp();
-        if (!(ok = finish())) break;
-        const float fp = p.sc.cc * p.sc.b / (p.sc.a * p.sc.a), fa = p.sc.cb * p.sc.b / p.sc.a, fi = p.sc.ca * p.sc.b;
-        for (int c = part * 16; c < p.Mr; c += 16 * kParts) {
-            uint32_t u[16];
-            ptx::tmem_ld16(acc + c, u);
-            ptx::tmem_wait_ld();
-            if (row < p.Mr) {
+            });
+            ready();
+            // B = a I + b A + c A^2, over A
+            square(dah, tall_k);
+            if (!(ok = finish())) break;
+            sums_of([&](int c, float (&v)[16]) {
 #pragma unroll
                 for (int q = 0; q < 2; ++q) {
-                    const uint32_t at = panel_at(row, c + 8 * q, p.Mr);
-                    float a[8], v[8];
+                    const uint32_t at = panel_at(row, c + 8 * q, Pr);
+                    float a[8];
                     uint4 vh, vl;
                     join8(*reinterpret_cast<const uint4 *>(ah + at), *reinterpret_cast<const uint4 *>(al + at), a);
 #pragma unroll
-                    for (int k = 0; k < 8; ++k)
-                        v[k] = fmaf(fa, a[k], fp * __uint_as_float(u[8 * q + k])) + (row == c + 8 * q + k ? fi : 0.f);
-                    split8(v, vh, vl);
+                    for (int k = 0; k < 8; ++k) v[8 * q + k] = fmaf(fa, a[k], fp * v[8 * q + k]) + (row == c + 8 * q + k ? fi : 0.f);
+                    split8(v + 8 * q, vh, vl);
                     *reinterpret_cast<uint4 *>(ah + at) = vh;
                     *reinterpret_cast<uint4 *>(al + at) = vl;
                 }
+            });
+            ready();
+            // X^T <- X^T B: 128 columns of X a group, 2 Mr columns of sums each, as many groups at a time as tensor memory holds
+            const int groups = (p.L + 127) / 128, at_once = 256 / p.Mr;
+            for (int g0 = 0; g0 < groups; g0 += at_once) {
+                const int g1 = min(g0 + at_once, groups);
+                if (warp == 0 && ptx::elect_one()) {
+                    const uint32_t both = instr_desc_f16(128, 2 * p.Mr, 0) | (1u << 15), one = instr_desc_f16(128, p.Mr, 0) | (1u << 15);   // (A: columns next to each other)
+                    for (int g = g0; g < g1; ++g) {
+                        const uint32_t d = tmem + (g - g0) * 2 * p.Mr;
+                        for (int k = 0; k < tall_k; ++k) {
+                            const uint32_t xa = dxh + 2 * g * panel + k * 2048, ba = dah + k * 32;
+                            ptx::mma_ss(d, ptx::desc(ptx::desc_lo(xa, panel), hi), ptx::desc(ptx::desc_lo(ba, 16), hi), both, k > 0);
+                            ptx::mma_ss(d, ptx::desc(ptx::desc_lo(xa + p.Mr * 128, panel), hi), ptx::desc(ptx::desc_lo(ba, 16), hi), one, 1);
+                        }
+                    }
+                    ptx::mma_commit(bar);
+                }
+                __syncwarp();
+                if (!(ok = finish())) break;
+                const int pieces = p.Mr / 16;                                    // of sixteen rows of X
+                for (int i = part; i < (g1 - g0) * pieces; i += kParts) {
+                    const int g = i / pieces, c = i % pieces * 16, l = (g0 + g) * 128 + row;
+                    uint32_t u[16], w[16];
+                    ptx::tmem_ld16(acc + g * 2 * p.Mr + c, u);
+                    ptx::tmem_ld16(acc + g * 2 * p.Mr + p.Mr + c, w);
+                    ptx::tmem_wait_ld();
+                    if (l < 64 * p.panels) {
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) {
+                            const uint32_t at = panel_at(c + k, l & ~7, Pr) + (l & 7) * 2;
+                            split_half(fx * (__uint_as_float(u[k]) + __uint_as_float(w[k])), *reinterpret_cast<__half *>(xh + at), *reinterpret_cast<__half *>(xl + at));
+                        }
+                    }
+                    __syncwarp();
+                }
+                ready();
             }
         }
-        ready();
-        // X <- B X, as many columns at a time as tensor memory holds
-        const float fx = 1.f / p.sc.b;
-        for (int l0 = 0; l0 < 64 * p.panels; l0 += chunk_max) {
-            const int l1 = min(l0 + chunk_max, 64 * p.panels);
+    } else {
+        const int chunk_max = 512;
+        for (int step = 0; step < p.steps && ok; ++step) {
+            // A = X X^T
             if (warp == 0 && ptx::elect_one()) {
-                for (int l = l0; l < l1; l += 256) {
-                    const int w = min(256, l1 - l);
-                    const uint32_t idesc = instr_desc_f16(128, w, 1);
-                    for (int k = 0; k < tall_k; ++k) {
-                        const uint32_t at = (k >> 2) * panel + (k & 3) * 32, bt = (l >> 6) * panel + k * 2048;
-                        mma3(tmem + (l - l0), dah + at, dal + at, dxh + bt, dxl + bt, panel, idesc, k == 0);
-                    }
+                const uint32_t idesc = instr_desc_f16(128, p.Mr, 0);
+                for (int k = 0; k < deep; ++k) {
+                    const uint32_t at = (k >> 2) * panel + (k & 3) * 32;
+                    mma3(tmem, dxh + at, dxl + at, dxh + at, dxl + at, 16, idesc, k == 0);
                 }
                 ptx::mma_commit(bar);
             }
             __syncwarp();
             if (!(ok = finish())) break;
-            for (int l = l0 + part * 16; l < l1; l += 16 * kParts) {
+            for (int c = part * 16; c < p.Mr; c += 16 * kParts) {
                 uint32_t u[16];
-                ptx::tmem_ld16(acc + (l - l0), u);
+                ptx::tmem_ld16(acc + c, u);
                 ptx::tmem_wait_ld();
                 if (row < p.Mr) {
 #pragma unroll
@@ -1115,15 +1170,83 @@ __global__ void __launch_bounds__(kOrthSmallThreads, 1) orth_small_kernel(const 
                         float v[8];
                         uint4 vh, vl;
 #pragma unroll
-                        for (int k = 0; k < 8; ++k) v[k] = __uint_as_float(u[8 * q + k]) * fx;
+                        for (int k = 0; k < 8; ++k) v[k] = __uint_as_float(u[8 * q + k]) * fg;
                         split8(v, vh, vl);
-                        const uint32_t at = panel_at(row, l + 8 * q, p.Mr);
-                        *reinterpret_cast<uint4 *>(xh + at) = vh;
-                        *reinterpret_cast<uint4 *>(xl + at) = vl;
+                        const uint32_t at = panel_at(row, c + 8 * q, Pr);
+                        *reinterpret_cast<uint4 *>(ah + at) = vh;
+                        *reinterpret_cast<uint4 *>(al + at) = vl;
                     }
                 }
             }
             ready();
+            // B = a I + b A + c A^2, over A
+            if (warp == 0 && ptx::elect_one()) {
+                const uint32_t idesc = instr_desc_f16(128, p.Mr, 0);
+                for (int k = 0; k < tall_k; ++k) {
+                    const uint32_t at = (k >> 2) * panel + (k & 3) * 32;
+                    mma3(tmem, dah + at, dal + at, dah + at, dal + at, 16, idesc, k == 0);
+                }
+                ptx::mma_commit(bar);
+            }
+            __syncwarp();
+            if (!(ok = finish())) break;
+            for (int c = part * 16; c < p.Mr; c += 16 * kParts) {
+                uint32_t u[16];
+                ptx::tmem_ld16(acc + c, u);
+                ptx::tmem_wait_ld();
+                if (row < p.Mr) {
+#pragma unroll
+                    for (int q = 0; q < 2; ++q) {
+                        const uint32_t at = panel_at(row, c + 8 * q, Pr);
+                        float a[8], v[8];
+                        uint4 vh, vl;
+                        join8(*reinterpret_cast<const uint4 *>(ah + at), *reinterpret_cast<const uint4 *>(al + at), a);
+#pragma unroll
+                        for (int k = 0; k < 8; ++k)
+                            v[k] = fmaf(fa, a[k], fp * __uint_as_float(u[8 * q + k])) + (row == c + 8 * q + k ? fi : 0.f);
+                        split8(v, vh, vl);
+                        *reinterpret_cast<uint4 *>(ah + at) = vh;
+                        *reinterpret_cast<uint4 *>(al + at) = vl;
+                    }
+                }
+            }
+            ready();
+            // X <- B X, as many columns at a time as tensor memory holds
+            for (int l0 = 0; l0 < 64 * p.panels; l0 += chunk_max) {
+                const int l1 = min(l0 + chunk_max, 64 * p.panels);
+                if (warp == 0 && ptx::elect_one()) {
+                    for (int l = l0; l < l1; l += 256) {
+                        const int w = min(256, l1 - l);
+                        const uint32_t idesc = instr_desc_f16(128, w, 1);
+                        for (int k = 0; k < tall_k; ++k) {
+                            const uint32_t at = (k >> 2) * panel + (k & 3) * 32, bt = (l >> 6) * panel + k * 2048;
+                            mma3(tmem + (l - l0), dah + at, dal + at, dxh + bt, dxl + bt, panel, idesc, k == 0);
+                        }
+                    }
+                    ptx::mma_commit(bar);
+                }
+                __syncwarp();
+                if (!(ok = finish())) break;
+                for (int l = l0 + part * 16; l < l1; l += 16 * kParts) {
+                    uint32_t u[16];
+                    ptx::tmem_ld16(acc + (l - l0), u);
+                    ptx::tmem_wait_ld();
+                    if (row < p.Mr) {
+#pragma unroll
+                        for (int q = 0; q < 2; ++q) {
+                            float v[8];
+                            uint4 vh, vl;
+#pragma unroll
+                            for (int k = 0; k < 8; ++k) v[k] = __uint_as_float(u[8 * q + k]) * fx;
+                            split8(v, vh, vl);
+                            const uint32_t at = panel_at(row, l + 8 * q, Pr);
+                            *reinterpret_cast<uint4 *>(xh + at) = vh;
+                            *reinterpret_cast<uint4 *>(xl + at) = vl;
+                        }
+                    }
+                }
+                ready();
+            }
         }
     }
     // the result, from its halves
@@ -1134,7 +1257,7 @@ __global__ void __launch_bounds__(kOrthSmallThreads, 1) orth_small_kernel(const 
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             const int s = o.tall ? c + i : r, l = o.tall ? r : c + i;
-            v[i] = one(panel_at(s, l & ~7, p.Mr) + (l & 7) * 2);
+            v[i] = one(panel_at(s, l & ~7, Pr) + (l & 7) * 2);
         }
     });
     ptx::tc_fence_before();

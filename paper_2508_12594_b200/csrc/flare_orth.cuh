@@ -914,14 +914,15 @@ __global__ void __launch_bounds__(kOrthThreads, 1) orth_team_kernel(const __grid
 
 // ---------------------------------------------------------------- a whole matrix in one block
 // S up to 128 and everything in shared memory: X as panels of 64 columns, rows of 128 bytes (128-byte swizzle), Mr = S rounded up to 16 of them in high
-// halves and as many in low ones, and behind them A, overwritten by B, in the same form.  The same bytes serve as rows of X (sums along
-// rows) and as the right factor of B X (sums over rows).  The MMAs have 128 rows whatever S is; rows beyond a panel's read what lies behind it
-// and their sums are not looked at.  Bound by how long the parts of a step follow one another: the MMAs read their factors from shared
-// memory (128 x 128: 95 cycles for 64 of arithmetic), and every sum goes through tensor memory, registers and a split once a product.
+// halves and below them as many in low ones, and behind them A, overwritten by B, in the same form.  The same bytes serve as rows of X
+// (sums along rows) and as the right factor of B X (sums over rows).  The MMAs have 128 rows whatever S is; what they read beyond a panel's
+// rows is what lies behind it, and its sums are not looked at.  Bound by how long the parts of a step follow one another: the MMAs read their
+// factors from shared memory (128 x 128 x 16: 95 cycles for 64 of arithmetic; as here with high and low rows side by side 110 for two of them), and every
+// sum goes through tensor memory, registers and a split once a product.
 //
-// kNarrow (S up to 64): the low halves are the panel's next Mr rows, so that one MMA forms high high, high low and low high of X X^T at a time (rows and
-// columns of both halves; the third comes back over from the lanes below), and B X is formed as its transpose, columns of X on the 128 lanes,
-// which all have work then.  Cycles of a step at 16 x 256: 7100 -> @.
+// kNarrow (S up to 64): one MMA forms high high, high low and low high of X X^T at a time (rows and columns of both halves; the third part comes over from
+// the lanes below), and B X is formed as its transpose, columns of X on the 128 lanes, which all have work then.  A step at 16 x 256: 5400
+// cycles, 7100 without.
 struct OrthSmall {
     OrthOuter o;
     OrthScales sc;
@@ -930,14 +931,16 @@ struct OrthSmall {
 };
 constexpr int kOrthSmallThreads = 512;
 struct OrthSmallSize {
-    size_t x_half, a_half, scratch, total;
+    size_t x, a, scratch, total;                                    // bytes of X and of A; where the scratch is, and the end
 };
 __host__ __device__ inline OrthSmallSize orth_small_size(int S, int L) {
     OrthSmallSize z;
-    const size_t Mr = (size_t)(S + 15) / 16 * 16, rows = S <= 64 ? 2 * Mr : Mr;
-    z.x_half = (size_t)((L + 63) / 64) * Mr * 128;
-    z.a_half = (size_t)((S + 63) / 64) * Mr * 128;
-    z.scratch = 1024 + 2 * (z.x_half + z.a_half) + (128 - rows) * 128;     // (what the rows beyond the last panel's read is there)
+    const size_t Mr = (size_t)(S + 15) / 16 * 16;
+    z.x = (size_t)((L + 63) / 64) * 2 * Mr * 128;
+    z.a = (size_t)((S + 63) / 64) * 2 * Mr * 128;
+    // what an MMA reads beyond the last panel is there: 128 rows from its first high row on (S up to 64), from its first low row on (above)
+    const size_t rows = S <= 64 ? 2 * Mr : Mr;
+    z.scratch = 1024 + z.x + z.a + (rows < 128 ? (128 - rows) * 128 : 0);
     z.total = z.scratch + (S <= 64 ? Mr * Mr * sizeof(float) : 0) + 64;
     return z;
 }
@@ -953,8 +956,9 @@ __global__ void __launch_bounds__(kOrthSmallThreads, 1) orth_small_kernel(const 
     __shared__ double sums[kOrthSmallThreads / 32];
     uint8_t *smem = ptx::align_1024(raw);
     const OrthSmallSize z = orth_small_size(p.S, p.L);
-    const int Pr = kNarrow ? 2 * p.Mr : p.Mr;                 // rows of a panel
-    uint8_t *xh = smem, *xl = smem + (kNarrow ? (size_t)p.Mr * 128 : z.x_half), *ah = smem + 2 * z.x_half, *al = ah + (kNarrow ? (size_t)p.Mr * 128 : z.a_half);
+    const int Mr = p.Mr, Pr = 2 * Mr;                                // rows of a half, of a panel
+    const uint32_t low = (uint32_t)Mr * 128, panel = (uint32_t)Pr * 128;   // bytes from a high row to its low one, of a panel
+    uint8_t *xs = smem, *as = smem + z.x;
     const uint32_t bar = ptx::smem_u32(&bar_word);
     const int warp = ptx::warp_index(), lane = threadIdx.x & 31;
     const size_t mat = blockIdx.x;
@@ -966,12 +970,37 @@ __global__ void __launch_bounds__(kOrthSmallThreads, 1) orth_small_kernel(const 
     if (warp == 0) ptx::tmem_alloc(ptx::smem_u32(&tmem_slot), 512);
     // zeros in the rows and columns that X and A do not fill (and everywhere else, once)
     for (size_t i = threadIdx.x; i < (z.scratch - 1024) / 16; i += kOrthSmallThreads) reinterpret_cast<uint4 *>(smem)[i] = make_uint4(0, 0, 0, 0);
+    __syncthreads();
     ptx::grid_launch();
     ptx::grid_wait();
     const OrthOuter &o = p.o;
+    if (o.w) {                                                       // (the weights are wanted at the end)
+        const size_t e = o.out_type == 0 ? 4 : 2, bytes = (size_t)o.rows * o.cols * e;
+        for (size_t at = (size_t)threadIdx.x * 128; at < bytes; at += kOrthSmallThreads * 128)
+            asm volatile("prefetch.global.L2 [%0];" ::"l"(static_cast<const char *>(o.w) + mat * o.step_out * e + at));
+    }
+    // the elements once from memory: as float32, its two 16-bit parts where the halves will be, and their squares
     double sum = 0.0;
-    orth_elements<false>(o, mat, threadIdx.x, kOrthSmallThreads, [&](int, int, const auto &u) {
+    orth_elements<false>(o, mat, threadIdx.x, kOrthSmallThreads, [&](int r, int c, const auto &u) {
+        constexpr int V = sizeof(u) / sizeof(float);
         for (float x : u) sum += (double)x * x;
+        if (V == 4 && !o.tall) {
+            uint32_t b[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) b[i] = __float_as_uint(u[i % V]);
+            uint8_t *at = xs + panel_at(r, c & ~7, Pr) + (c & 7) * 2;
+            *reinterpret_cast<uint2 *>(at) = make_uint2(__byte_perm(b[0], b[1], 0x7632), __byte_perm(b[2], b[3], 0x7632));
+            *reinterpret_cast<uint2 *>(at + low) = make_uint2(__byte_perm(b[0], b[1], 0x5410), __byte_perm(b[2], b[3], 0x5410));
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const int s = o.tall ? c + i : r, l = o.tall ? r : c + i;
+                uint8_t *at = xs + panel_at(s, l & ~7, Pr) + (l & 7) * 2;
+                const uint32_t b = __float_as_uint(u[i]);
+                *reinterpret_cast<uint16_t *>(at) = (uint16_t)(b >> 16);
+                *reinterpret_cast<uint16_t *>(at + low) = (uint16_t)b;
+            }
+        }
     });
 #pragma unroll
     for (int k = 16; k > 0; k >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, k);
@@ -980,24 +1009,21 @@ __global__ void __launch_bounds__(kOrthSmallThreads, 1) orth_small_kernel(const 
     sum = 0.0;
     for (int k = 0; k < kOrthSmallThreads / 32; ++k) sum += sums[k];
     const double f = (double)p.sc.x / (sqrt(sum) + (double)o.eps);
-    orth_elements<true>(o, mat, threadIdx.x, kOrthSmallThreads, [&](int r, int c, const auto &u) {
-        constexpr int V = sizeof(u) / sizeof(float);
-        if (V == 4 && !o.tall) {
-            uint2 h, l;
-            h.x = half_pair((float)(u[0] * f), (float)(u[1 % V] * f), l.x);
-            h.y = half_pair((float)(u[2 % V] * f), (float)(u[3 % V] * f), l.y);
-            const uint32_t at = panel_at(r, c & ~7, Pr) + (c & 7) * 2;
-            *reinterpret_cast<uint2 *>(xh + at) = h;
-            *reinterpret_cast<uint2 *>(xl + at) = l;
-        } else {
+    for (int i = threadIdx.x; i < p.panels * Mr * 8; i += kOrthSmallThreads) {
+        uint8_t *at = xs + (uint32_t)(i / (8 * Mr)) * panel + (uint32_t)(i % (8 * Mr)) * 16;
+        const uint4 h = *reinterpret_cast<const uint4 *>(at), l = *reinterpret_cast<const uint4 *>(at + low);
+        const uint32_t hw[4] = {h.x, h.y, h.z, h.w}, lw[4] = {l.x, l.y, l.z, l.w};
+        float v[8];
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const int s = o.tall ? c + i : r, l = o.tall ? r : c + i;
-                const uint32_t at = panel_at(s, l & ~7, Pr) + (l & 7) * 2;
-                split_half((float)(u[i] * f), *reinterpret_cast<__half *>(xh + at), *reinterpret_cast<__half *>(xl + at));
-            }
+        for (int k = 0; k < 4; ++k) {
+            v[2 * k] = (float)(__uint_as_float(__byte_perm(hw[k], lw[k], 0x1054)) * f);
+            v[2 * k + 1] = (float)(__uint_as_float(__byte_perm(hw[k], lw[k], 0x3276)) * f);
         }
-    });
+        uint4 vh, vl;
+        split8(v, vh, vl);
+        *reinterpret_cast<uint4 *>(at) = vh;
+        *reinterpret_cast<uint4 *>(at + low) = vl;
+    }
     ptx::fence_proxy_async_smem();
     ptx::tc_fence_before();
     __syncthreads();
@@ -1006,15 +1032,14 @@ __global__ void __launch_bounds__(kOrthSmallThreads, 1) orth_small_kernel(const 
 
     uint32_t phase = 0;
     constexpr uint32_t hi = ptx::desc_hi(1024, 2);
-    const uint32_t dxh = ptx::smem_u32(xh), dxl = ptx::smem_u32(xl), dah = ptx::smem_u32(ah), dal = ptx::smem_u32(al), panel = (uint32_t)Pr * 128;
-    constexpr int kParts = kOrthSmallThreads / 128;           // warps that share a quarter of the rows
-    const int quad = warp & 3, part = warp >> 2, row = quad * 32 + lane, tall_k = p.Mr / 16;
+    constexpr int kParts = kOrthSmallThreads / 128, kTurns = kNarrow ? 1 : 2;   // warps that share a quarter of the lanes; sixteen columns a turn of theirs cover Mr
+    const uint32_t dx = ptx::smem_u32(xs), da = ptx::smem_u32(as);
+    const int quad = warp & 3, part = warp >> 2, row = quad * 32 + lane, deep_s = Mr / 16, deep_l = (p.L + 15) / 16;
     const uint32_t acc = tmem + ((uint32_t)(quad * 32) << 16);
-    // the three products of two split factors, one 16-deep step
-    auto mma3 = [&](uint32_t d, uint32_t a_hi, uint32_t a_lo, uint32_t b_hi, uint32_t b_lo, uint32_t b_lbo, uint32_t idesc, bool first) {
-        ptx::mma_ss(d, ptx::desc(ptx::desc_lo(a_lo, 16), hi), ptx::desc(ptx::desc_lo(b_hi, b_lbo), hi), idesc, !first);
-        ptx::mma_ss(d, ptx::desc(ptx::desc_lo(a_hi, 16), hi), ptx::desc(ptx::desc_lo(b_lo, b_lbo), hi), idesc, 1);
-        ptx::mma_ss(d, ptx::desc(ptx::desc_lo(a_hi, 16), hi), ptx::desc(ptx::desc_lo(b_hi, b_lbo), hi), idesc, 1);
+    const float fg = p.sc.a / (p.sc.x * p.sc.x), fp = p.sc.cc * p.sc.b / (p.sc.a * p.sc.a), fa = p.sc.cb * p.sc.b / p.sc.a, fi = p.sc.ca * p.sc.b, fx = 1.f / p.sc.b;
+    float *scratch = reinterpret_cast<float *>(smem + z.scratch - 1024);        // [column][row]: low high, on its way to the lanes of the high rows
+    auto mma = [&](uint32_t d, uint32_t a, uint32_t a_lbo, uint32_t b, uint32_t b_lbo, uint32_t idesc, bool more) {
+        ptx::mma_ss(d, ptx::desc(ptx::desc_lo(a, a_lbo), hi), ptx::desc(ptx::desc_lo(b, b_lbo), hi), idesc, more);
     };
     auto finish = [&]() {
         // (every thread waits; whether to go on is agreed on by all)
@@ -1029,198 +1054,129 @@ __global__ void __launch_bounds__(kOrthSmallThreads, 1) orth_small_kernel(const 
         __syncthreads();
         ptx::tc_fence_after();
     };
-    bool ok = true;
-    const float fg = p.sc.a / (p.sc.x * p.sc.x), fp = p.sc.cc * p.sc.b / (p.sc.a * p.sc.a), fa = p.sc.cb * p.sc.b / p.sc.a, fi = p.sc.ca * p.sc.b, fx = 1.f / p.sc.b;
-    const int deep = (p.L + 15) / 16;
-    if constexpr (kNarrow) {
-        float *scratch = reinterpret_cast<float *>(smem + z.scratch - 1024);      // [column][row]: low high, on its way to the lanes of the high rows
-        // Rows of both halves times rows of both halves, a panel's 64 columns from `at` on in `steps` 16-deep steps.
-        auto square = [&](uint32_t at, int steps) {
-            if (warp == 0 && ptx::elect_one()) {
-                const uint32_t idesc = instr_desc_f16(128, 2 * p.Mr, 0);
-                for (int k = 0; k < steps; ++k) {
-                    const uint32_t lo = ptx::desc_lo(at + (k >> 2) * panel + (k & 3) * 32, 16);
-                    ptx::mma_ss(tmem, ptx::desc(lo, hi), ptx::desc(lo, hi), idesc, k > 0);
-                }
-                ptx::mma_commit(bar);
+    // High rows times high and low rows (columns 0.. and Mr.. of the sums), and low rows times high ones (narrow: rows Mr.. of the sums, else added to the
+    // first), of the panels from `at` on, `deep` times sixteen columns.
+    auto square = [&](uint32_t at, int deep) {
+        if (warp == 0 && ptx::elect_one()) {
+            const uint32_t both = instr_desc_f16(128, 2 * Mr, 0), one = instr_desc_f16(128, Mr, 0);
+            for (int k = 0; k < deep; ++k) {
+                const uint32_t c = at + (k >> 2) * panel + (k & 3) * 32;
+                mma(tmem, c, 16, c, 16, both, k > 0);
+                if (!kNarrow) mma(tmem, c + low, 16, c, 16, one, true);
             }
-            __syncwarp();
-        };
-        // its three parts added up, sixteen columns at a time of the rows below Mr: use(c, sums)
-        auto sums_of = [&](auto use) {
-            const bool low = row >= p.Mr && row < 2 * p.Mr;
-            for (int c = part * 16; c < p.Mr; c += 16 * kParts) {
+            ptx::mma_commit(bar);
+        }
+        __syncwarp();
+    };
+    // its parts added up, sixteen columns at a time of the rows below Mr: use(turn, column, sums)
+    auto sums_of = [&](auto use) {
+        if constexpr (kNarrow) {
+            if (part * 16 < Mr) {
                 uint32_t u[16];
-                ptx::tmem_ld16(acc + c, u);
+                ptx::tmem_ld16(acc + part * 16, u);
                 ptx::tmem_wait_ld();
-                if (low) {
+                if (row >= Mr && row < 2 * Mr) {
 #pragma unroll
-                    for (int k = 0; k < 16; ++k) scratch[(c + k) * p.Mr + row - p.Mr] = __uint_as_float(u[k]);
+                    for (int k = 0; k < 16; ++k) scratch[(part * 16 + k) * Mr + row - Mr] = __uint_as_float(u[k]);
                 }
             }
             __syncthreads();
-            if (quad * 32 < p.Mr)
-                for (int c = part * 16; c < p.Mr; c += 16 * kParts) {
-                    uint32_t u[16], w[16];
-                    ptx::tmem_ld16(acc + c, u);
-                    ptx::tmem_ld16(acc + p.Mr + c, w);
-                    ptx::tmem_wait_ld();
-                    float v[16];
-                    if (row < p.Mr) {
+        }
 #pragma unroll
-                        for (int k = 0; k < 16; ++k) v[k] = (__uint_as_float(w[k]) + scratch[(c + k) * p.Mr + row]) + __uint_as_float(u[k]);
-                        use(c, v);
-                    }
-                    __syncwarp();
-                }
-        };
-        for (int step = 0; step < p.steps && ok; ++step) {
-            // A = X X^T
-            square(dxh, deep);
-            if (!(ok = finish())) break;
-            sums_of([&](int c, float (&v)[16]) {
+        for (int j = 0; j < kTurns; ++j) {
+            const int c = (part + j * kParts) * 16;
+            if (quad * 32 >= Mr || c >= Mr) continue;                           // (uniform over the warp)
+            uint32_t u[16], w[16];
+            ptx::tmem_ld16(acc + c, u);
+            ptx::tmem_ld16(acc + Mr + c, w);
+            ptx::tmem_wait_ld();
+            if (row < Mr) {
+                float v[16];
 #pragma unroll
-                for (int q = 0; q < 2; ++q) {
-                    uint4 vh, vl;
+                for (int k = 0; k < 16; ++k) v[k] = (kNarrow ? __uint_as_float(w[k]) + scratch[(c + k) * Mr + row] : __uint_as_float(w[k])) + __uint_as_float(u[k]);
+                use(j, c, v);
+            }
+            __syncwarp();
+        }
+    };
+    auto store16 = [&](uint8_t *to, int c, const float *v) {
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) v[8 * q + k] *= fg;
-                    split8(v + 8 * q, vh, vl);
-                    const uint32_t at = panel_at(row, c + 8 * q, Pr);
-                    *reinterpret_cast<uint4 *>(ah + at) = vh;
-                    *reinterpret_cast<uint4 *>(al + at) = vl;
-                }
-            });
-            ready();
-            // B = a I + b A + c A^2, over A
-            square(dah, tall_k);
-            if (!(ok = finish())) break;
-            sums_of([&](int c, float (&v)[16]) {
+        for (int q = 0; q < 2; ++q) {
+            uint4 vh, vl;
+            split8(v + 8 * q, vh, vl);
+            uint8_t *at = to + panel_at(row, c + 8 * q, Pr);
+            *reinterpret_cast<uint4 *>(at) = vh;
+            *reinterpret_cast<uint4 *>(at + low) = vl;
+        }
+    };
+    float keep[kTurns][16];                                                     // this thread's part of A
+    bool ok = true;
+    for (int step = 0; step < p.steps && ok; ++step) {
+        // A = X X^T
+        square(dx, deep_l);
+        if (!(ok = finish())) break;
+        sums_of([&](int j, int c, float (&v)[16]) {
 #pragma unroll
-                for (int q = 0; q < 2; ++q) {
-                    const uint32_t at = panel_at(row, c + 8 * q, Pr);
-                    float a[8];
-                    uint4 vh, vl;
-                    join8(*reinterpret_cast<const uint4 *>(ah + at), *reinterpret_cast<const uint4 *>(al + at), a);
+            for (int k = 0; k < 16; ++k) keep[j][k] = v[k] *= fg;
+            store16(as, c, v);
+        });
+        ready();
+        // B = a I + b A + c A^2, over A
+        square(da, deep_s);
+        if (!(ok = finish())) break;
+        sums_of([&](int j, int c, float (&v)[16]) {
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) v[8 * q + k] = fmaf(fa, a[k], fp * v[8 * q + k]) + (row == c + 8 * q + k ? fi : 0.f);
-                    split8(v + 8 * q, vh, vl);
-                    *reinterpret_cast<uint4 *>(ah + at) = vh;
-                    *reinterpret_cast<uint4 *>(al + at) = vl;
-                }
-            });
-            ready();
+            for (int k = 0; k < 16; ++k) v[k] = fmaf(fa, keep[j][k], fp * v[k]) + (row == c + k ? fi : 0.f);
+            store16(as, c, v);
+        });
+        ready();
+        if constexpr (kNarrow) {
             // X^T <- X^T B: 128 columns of X a group, 2 Mr columns of sums each, as many groups at a time as tensor memory holds
-            const int groups = (p.L + 127) / 128, at_once = 256 / p.Mr;
+            const int groups = (p.L + 127) / 128, at_once = 256 / Mr, pieces = Mr / 16;
             for (int g0 = 0; g0 < groups; g0 += at_once) {
                 const int g1 = min(g0 + at_once, groups);
                 if (warp == 0 && ptx::elect_one()) {
-                    const uint32_t both = instr_desc_f16(128, 2 * p.Mr, 0) | (1u << 15), one = instr_desc_f16(128, p.Mr, 0) | (1u << 15);   // (A: columns next to each other)
-                    for (int g = g0; g < g1; ++g) {
-                        const uint32_t d = tmem + (g - g0) * 2 * p.Mr;
-                        for (int k = 0; k < tall_k; ++k) {
-                            const uint32_t xa = dxh + 2 * g * panel + k * 2048, ba = dah + k * 32;
-                            ptx::mma_ss(d, ptx::desc(ptx::desc_lo(xa, panel), hi), ptx::desc(ptx::desc_lo(ba, 16), hi), both, k > 0);
-                            ptx::mma_ss(d, ptx::desc(ptx::desc_lo(xa + p.Mr * 128, panel), hi), ptx::desc(ptx::desc_lo(ba, 16), hi), one, 1);
+                    const uint32_t across = 1u << 15;                           // (the left factor's columns are the ones next to each other)
+                    const uint32_t both = instr_desc_f16(128, 2 * Mr, 0) | across, one = instr_desc_f16(128, Mr, 0) | across;
+                    for (int g = g0; g < g1; ++g)
+                        for (int k = 0; k < deep_s; ++k) {
+                            const uint32_t d = tmem + (g - g0) * 2 * Mr, x = dx + 2 * g * panel + k * 2048, b = da + k * 32;
+                            mma(d, x, panel, b, 16, both, k > 0);
+                            mma(d, x + low, panel, b, 16, one, true);
                         }
-                    }
                     ptx::mma_commit(bar);
                 }
                 __syncwarp();
                 if (!(ok = finish())) break;
-                const int pieces = p.Mr / 16;                                    // of sixteen rows of X
-                for (int i = part; i < (g1 - g0) * pieces; i += kParts) {
+                for (int i = part; i < (g1 - g0) * pieces; i += kParts) {       // sixteen rows of X of a group
                     const int g = i / pieces, c = i % pieces * 16, l = (g0 + g) * 128 + row;
                     uint32_t u[16], w[16];
-                    ptx::tmem_ld16(acc + g * 2 * p.Mr + c, u);
-                    ptx::tmem_ld16(acc + g * 2 * p.Mr + p.Mr + c, w);
+                    ptx::tmem_ld16(acc + g * 2 * Mr + c, u);
+                    ptx::tmem_ld16(acc + g * 2 * Mr + Mr + c, w);
                     ptx::tmem_wait_ld();
                     if (l < 64 * p.panels) {
 #pragma unroll
                         for (int k = 0; k < 16; ++k) {
-                            const uint32_t at = panel_at(c + k, l & ~7, Pr) + (l & 7) * 2;
-                            split_half(fx * (__uint_as_float(u[k]) + __uint_as_float(w[k])), *reinterpret_cast<__half *>(xh + at), *reinterpret_cast<__half *>(xl + at));
+                            uint8_t *at = xs + panel_at(c + k, l & ~7, Pr) + (l & 7) * 2;
+                            split_half(fx * (__uint_as_float(u[k]) + __uint_as_float(w[k])), *reinterpret_cast<__half *>(at), *reinterpret_cast<__half *>(at + low));
                         }
                     }
                     __syncwarp();
                 }
                 ready();
             }
-        }
-    } else {
-        const int chunk_max = 512;
-        for (int step = 0; step < p.steps && ok; ++step) {
-            // A = X X^T
-            if (warp == 0 && ptx::elect_one()) {
-                const uint32_t idesc = instr_desc_f16(128, p.Mr, 0);
-                for (int k = 0; k < deep; ++k) {
-                    const uint32_t at = (k >> 2) * panel + (k & 3) * 32;
-                    mma3(tmem, dxh + at, dxl + at, dxh + at, dxl + at, 16, idesc, k == 0);
-                }
-                ptx::mma_commit(bar);
-            }
-            __syncwarp();
-            if (!(ok = finish())) break;
-            for (int c = part * 16; c < p.Mr; c += 16 * kParts) {
-                uint32_t u[16];
-                ptx::tmem_ld16(acc + c, u);
-                ptx::tmem_wait_ld();
-                if (row < p.Mr) {
-#pragma unroll
-                    for (int q = 0; q < 2; ++q) {
-                        float v[8];
-                        uint4 vh, vl;
-#pragma unroll
-                        for (int k = 0; k < 8; ++k) v[k] = __uint_as_float(u[8 * q + k]) * fg;
-                        split8(v, vh, vl);
-                        const uint32_t at = panel_at(row, c + 8 * q, Pr);
-                        *reinterpret_cast<uint4 *>(ah + at) = vh;
-                        *reinterpret_cast<uint4 *>(al + at) = vl;
-                    }
-                }
-            }
-            ready();
-            // B = a I + b A + c A^2, over A
-            if (warp == 0 && ptx::elect_one()) {
-                const uint32_t idesc = instr_desc_f16(128, p.Mr, 0);
-                for (int k = 0; k < tall_k; ++k) {
-                    const uint32_t at = (k >> 2) * panel + (k & 3) * 32;
-                    mma3(tmem, dah + at, dal + at, dah + at, dal + at, 16, idesc, k == 0);
-                }
-                ptx::mma_commit(bar);
-            }
-            __syncwarp();
-            if (!(ok = finish())) break;
-            for (int c = part * 16; c < p.Mr; c += 16 * kParts) {
-                uint32_t u[16];
-                ptx::tmem_ld16(acc + c, u);
-                ptx::tmem_wait_ld();
-                if (row < p.Mr) {
-#pragma unroll
-                    for (int q = 0; q < 2; ++q) {
-                        const uint32_t at = panel_at(row, c + 8 * q, Pr);
-                        float a[8], v[8];
-                        uint4 vh, vl;
-                        join8(*reinterpret_cast<const uint4 *>(ah + at), *reinterpret_cast<const uint4 *>(al + at), a);
-#pragma unroll
-                        for (int k = 0; k < 8; ++k)
-                            v[k] = fmaf(fa, a[k], fp * __uint_as_float(u[8 * q + k])) + (row == c + 8 * q + k ? fi : 0.f);
-                        split8(v, vh, vl);
-                        *reinterpret_cast<uint4 *>(ah + at) = vh;
-                        *reinterpret_cast<uint4 *>(al + at) = vl;
-                    }
-                }
-            }
-            ready();
+        } else {
             // X <- B X, as many columns at a time as tensor memory holds
-            for (int l0 = 0; l0 < 64 * p.panels; l0 += chunk_max) {
-                const int l1 = min(l0 + chunk_max, 64 * p.panels);
+            for (int l0 = 0; l0 < 64 * p.panels; l0 += 512) {
+                const int l1 = min(l0 + 512, 64 * p.panels);
                 if (warp == 0 && ptx::elect_one()) {
                     for (int l = l0; l < l1; l += 256) {
-                        const int w = min(256, l1 - l);
-                        const uint32_t idesc = instr_desc_f16(128, w, 1);
-                        for (int k = 0; k < tall_k; ++k) {
-                            const uint32_t at = (k >> 2) * panel + (k & 3) * 32, bt = (l >> 6) * panel + k * 2048;
-                            mma3(tmem + (l - l0), dah + at, dal + at, dxh + bt, dxl + bt, panel, idesc, k == 0);
+                        const uint32_t idesc = instr_desc_f16(128, min(256, l1 - l), 1);
+                        for (int k = 0; k < deep_s; ++k) {
+                            const uint32_t d = tmem + (l - l0), b = da + (k >> 2) * panel + (k & 3) * 32, x = dx + (l >> 6) * panel + k * 2048;
+                            mma(d, b + low, 16, x, panel, idesc, k > 0);
+                            mma(d, b, 16, x + low, panel, idesc, true);
+                            mma(d, b, 16, x, panel, idesc, true);
                         }
                     }
                     ptx::mma_commit(bar);
@@ -1231,19 +1187,13 @@ __global__ void __launch_bounds__(kOrthSmallThreads, 1) orth_small_kernel(const 
                     uint32_t u[16];
                     ptx::tmem_ld16(acc + (l - l0), u);
                     ptx::tmem_wait_ld();
-                    if (row < p.Mr) {
+                    if (row < Mr) {
+                        float v[16];
 #pragma unroll
-                        for (int q = 0; q < 2; ++q) {
-                            float v[8];
-                            uint4 vh, vl;
-#pragma unroll
-                            for (int k = 0; k < 8; ++k) v[k] = __uint_as_float(u[8 * q + k]) * fx;
-                            split8(v, vh, vl);
-                            const uint32_t at = panel_at(row, l + 8 * q, Pr);
-                            *reinterpret_cast<uint4 *>(xh + at) = vh;
-                            *reinterpret_cast<uint4 *>(xl + at) = vl;
-                        }
+                        for (int k = 0; k < 16; ++k) v[k] = __uint_as_float(u[k]) * fx;
+                        store16(xs, l, v);
                     }
+                    __syncwarp();
                 }
                 ready();
             }
@@ -1253,11 +1203,11 @@ __global__ void __launch_bounds__(kOrthSmallThreads, 1) orth_small_kernel(const 
     const float back = 1.f / p.sc.x;
     orth_results(o, mat, threadIdx.x, kOrthSmallThreads, [&](int r, int c, auto &v) {
         constexpr int V = sizeof(v) / sizeof(float);
-        auto one = [&](uint32_t at) { return back * (__half2float(*reinterpret_cast<const __half *>(xh + at)) + __half2float(*reinterpret_cast<const __half *>(xl + at))); };
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             const int s = o.tall ? c + i : r, l = o.tall ? r : c + i;
-            v[i] = one(panel_at(s, l & ~7, Pr) + (l & 7) * 2);
+            const uint8_t *at = xs + panel_at(s, l & ~7, Pr) + (l & 7) * 2;
+            v[i] = back * (__half2float(*reinterpret_cast<const __half *>(at)) + __half2float(*reinterpret_cast<const __half *>(at + low)));
         }
     });
     ptx::tc_fence_before();

@@ -85,15 +85,19 @@ __device__ __forceinline__ Raw8<E> pack8(const float2 (&f)[4]) {
 }
 
 // Which columns a thread owns.  kAligned: eight next to each other, moved 16 bytes at a time (C a multiple of 8, rows on 16-byte boundaries);
-// otherwise every tpr-th, one at a time, neighbouring threads next to each other.
+// otherwise every 32nd of its warp's 256, one at a time, neighbouring lanes next to each other (a distance the compiler knows: it goes into
+// the instructions).
 template <bool kAligned>
 struct Columns {
-    int first, step, C;
+    int first, C;
+    int mine;                                                // how many of the eight there are
     __device__ __forceinline__ Columns() {}
-    __device__ __forceinline__ Columns(int lane, int tpr, int C_, int base = 0) : first(base + (kAligned ? 8 * lane : lane)), step(kAligned ? 1 : tpr), C(C_) {}
-    __device__ __forceinline__ int at(int j) const { return first + j * step; }
-    __device__ __forceinline__ bool has(int j) const { return kAligned ? first < C : at(j) < C; }
-    __device__ __forceinline__ bool any() const { return first < C; }
+    __device__ __forceinline__ Columns(int lane, int C_, int base = 0) : first(base + (kAligned ? 8 * lane : 8 * (lane & ~31) + (lane & 31))), C(C_) {
+        mine = kAligned ? (first < C ? 8 : 0) : max(0, min(8, (C - first + 31) >> 5));
+    }
+    __device__ __forceinline__ int at(int j) const { return first + j * (kAligned ? 1 : 32); }
+    __device__ __forceinline__ bool has(int j) const { return j < mine; }
+    __device__ __forceinline__ bool any() const { return mine > 0; }
 };
 template <typename E, bool kAligned>
 __device__ __forceinline__ Raw8<E> load8(const E *row, const Columns<kAligned> &c) {
@@ -293,10 +297,13 @@ __device__ __forceinline__ uint32_t half_of(const void *t, long row, long ld, in
 }
 template <typename E, int kThreads>
 __device__ __forceinline__ void slot_copy_each(uint32_t slot, const char *src, const Columns<false> &c, bool yes, bool last_row, uint32_t half) {
+    const int mine = yes ? c.mine : 0;
+    const bool last = last_row && half == 0 && c.at(c.mine - 1) == c.C - 1;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        const uint32_t bytes = !yes || !c.has(j) ? 0u : sizeof(E) == 2 && last_row && half == 0 && c.at(j) == c.C - 1 ? 2u : 4u;
-        asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(slot + j * kThreads * 4), "l"(src + (size_t)(j * c.step) * sizeof(E)), "r"(bytes) : "memory");
+        uint32_t bytes = j < mine ? 4u : 0u;
+        if (sizeof(E) == 2 && last && j == mine - 1) bytes = 2u;
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(slot + j * kThreads * 4), "l"(src + j * 32 * (int)sizeof(E)), "r"(bytes) : "memory");
     }
 }
 template <typename E, int kThreads>
@@ -360,7 +367,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 2) block_forwa
     int mine_n = 0;
 #pragma unroll
     for (int g = 0; g < kV; ++g) {
-        c[g] = Columns<kAligned>(lane + g * p.tpr, p.tpr, p.C, blockIdx.y * 8 * kV * kThreads);
+        c[g] = Columns<kAligned>(lane + g * p.tpr, p.C, blockIdx.y * 8 * kV * kThreads);
 #pragma unroll
         for (int j = 0; j < 8; ++j) mine_n += c[g].has(j) ? 1 : 0;
     }
@@ -514,7 +521,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 2) block_backw
     constexpr uint32_t kOneR = pieces_of<R, kAligned>() * kThreads * 16, kOneT = pieces_of<T, kAligned>() * kThreads * 16;
     constexpr uint32_t kY = 0, kDy = kOneR, kDh = 2 * kOneR, kO = kDh + kOneT, kG = kO + kOneT, kStage = kPieces * kThreads * 16;
     const int lane = threadIdx.x & (p.tpr - 1), per_turn = kThreads / p.tpr, mine = threadIdx.x / p.tpr;
-    const Columns<kAligned> c(lane, p.tpr, p.C, blockIdx.y * 8 * kThreads);
+    const Columns<kAligned> c(lane, p.C, blockIdx.y * 8 * kThreads);
     RowGroup grp(p.tpr, p.cluster, &row_shared);
     const Piece piece(p, per_turn);
     constexpr bool gate_row = kIn == kGated;
@@ -706,7 +713,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 2) block_backw
         float v = 0.f;
         for (int s = 0; s < slots_n; ++s) v += all[s * kSums * width + i];
         const int k = i / width, l = i % p.tpr, j = i % width / p.tpr;
-        const Columns<kAligned> cc(l, p.tpr, p.C, blockIdx.y * 8 * kThreads);
+        const Columns<kAligned> cc(l, p.C, blockIdx.y * 8 * kThreads);
         if (cc.has(j)) out[(size_t)k * p.C + cc.at(j)] = v;
     }
 }

@@ -20,7 +20,7 @@ inline BlockPlan block_plan(long rows, long group, int C, bool aligned, int sms,
     BlockPlan p;
     p.vectors = vectors;
     p.threads = aligned && C > 2048 * vectors ? 512 : 256;
-    p.tpr = 4;
+    p.tpr = aligned ? 4 : 32;                               // (columns that are moved one at a time: a warp's lanes side by side)
     while (p.tpr * 8 * vectors < C && p.tpr < p.threads) p.tpr *= 2;
     p.cluster = 1;
     while (p.cluster * p.threads * 8 * vectors < C) p.cluster *= 2;

@@ -89,8 +89,47 @@ TeamPlan team_plan(int team, long rows, long cols, bool symmetric, int K) {
     }
     return best;
 }
+// Clusters of n blocks of the team kernel that the chip holds at a time (the SMs of a cluster are of one part of the chip: 33 clusters of four, 15 of
+// eight, 7 of sixteen); asked for once per device, 0 = not yet.
+int clusters_at_a_time(int n, int sms) {
+    static std::atomic<int> known[64][17];
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) {
+        cudaGetLastError();
+        return n == 16 ? 7 : n == 8 ? 15 : n == 4 ? 33 : sms / n;     // (no device: for size queries)
+    }
+    int most = known[dev][n].load(std::memory_order_relaxed);
+    if (most == 0) {
+        auto *kernel = orth_team_kernel<true, float>;
+        cudaLaunchAttribute attr{};
+        attr.id = cudaLaunchAttributeClusterDimension;
+        attr.val.clusterDim.x = n; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
+        cudaLaunchConfig_t cfg{};
+        cfg.gridDim = dim3((unsigned)n); cfg.blockDim = kOrthThreads; cfg.dynamicSmemBytes = kOrthSmem;
+        cfg.attrs = &attr; cfg.numAttrs = 1;
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kOrthSmem) != cudaSuccess ||
+            cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess ||
+            cudaOccupancyMaxActiveClusters(&most, kernel, &cfg) != cudaSuccess || most < 1) {
+            cudaGetLastError();
+            most = -1;                                                // (cannot be placed)
+        }
+        known[dev][n].store(most, std::memory_order_relaxed);
+    }
+    return most;
+}
+// How a cluster of n does a product: tiles of 128 or 64 columns.  Cycles: some 4500 to start and to meet, and a turn's steps and end.
+struct ClusterPlan { int width; double cost; };
+ClusterPlan cluster_plan(int n, int rows, int cols, int K) {
+    ClusterPlan best{0, 0.0};
+    for (int width : {128, 64}) {
+        const long tiles = (long)((rows + 127) / 128) * ((cols + width - 1) / width), turns = (tiles + n - 1) / n;
+        const double cost = 4500.0 + (double)turns * ((K + 63) / 64 * (width == 128 ? 900.0 : 620.0) + (width == 128 ? 2600.0 : 2000.0));
+        if (best.width == 0 || cost < best.cost) best = ClusterPlan{width, cost};
+    }
+    return best;
+}
 // How a problem is run.
-enum { kOrthSmallPath = 0, kOrthTeamPath = 1, kOrthPairPath = 2 };
+enum { kOrthSmallPath = 0, kOrthTeamPath = 1, kOrthPairPath = 2, kOrthClusterPath = 3 };
 struct OrthPlan { int path, team, teams; };
 OrthPlan orth_plan(const flare_orth_desc_t *d, int sms) {
     const OrthSizes z = sizes_of(d);
@@ -109,6 +148,17 @@ OrthPlan orth_plan(const flare_orth_desc_t *d, int sms) {
     auto launch = [&](long tiles, int K) { return 20000.0 + (double)((tiles * count + sms / 2 - 1) / (sms / 2)) * ((K + 63) / 64) * 1536.0; };
     const double pairs = launch(s2 * (s2 + 1) / 2, z.L) + launch(s2 * (s2 + 1) / 2, z.S) + launch(s2 * l2, z.S);
     p.path = team <= pairs ? kOrthTeamPath : kOrthPairPath;
+    double least = std::min(team, pairs);
+    for (int n : {1, 2, 4, 8, 16}) {
+        const int most = clusters_at_a_time(n, sms), clusters = std::min(count, most);
+        if (most < 1) continue;
+        const double cost = (double)((count + clusters - 1) / clusters) *
+                            (cluster_plan(n, z.S, z.S, z.L).cost + cluster_plan(n, z.S, z.S, z.S).cost + cluster_plan(n, z.S, z.L, z.S).cost);
+        if (cost < least) {
+            least = cost;
+            p = OrthPlan{kOrthClusterPath, n, clusters};
+        }
+    }
     return p;
 }
 struct OrthLayout { size_t counters, norm, x[2], a, b, part, total; };
@@ -163,6 +213,7 @@ int launch_pairs(const HalfMaps &ta, const HalfMaps &tb, const HalfMaps &out, Or
     static std::atomic<uint64_t> opt_in{0};
     if (int rc = ensure_big_smem(orth_pair_kernel<kKind, E>, opt_in, (int)kOrthSmem)) return rc;
     OrthProduct &p = a.p;
+    p.width = 256;
     p.tiles_m = (p.S + 255) / 256;
     p.tiles_n = (p.N + 255) / 256;
     p.upper = kKind == kOrthGram || kKind == kOrthPoly;
@@ -180,19 +231,40 @@ int launch_pairs(const HalfMaps &ta, const HalfMaps &tb, const HalfMaps &out, Or
     FLARE_CUDA(cudaLaunchKernelEx(&cfg, orth_pair_kernel<kKind, E>, ta.load, tb.load, out.store, out.store_t, a));
     return FLARE_OK;
 }
-template <typename E>
+// Teams: a cooperative launch (its blocks wait for one another: all of them at once or none), or clusters.
+template <bool kCluster, typename E>
 int launch_teams(const OrthMaps &maps, const OrthTeam &p, cudaStream_t st) {
-    static std::atomic<uint64_t> opt_in{0};
-    if (int rc = ensure_big_smem(orth_team_kernel<E>, opt_in, (int)kOrthSmem)) return rc;
-    cudaLaunchAttribute attr{};
-    attr.id = cudaLaunchAttributeCooperative;                                    // (its blocks wait for one another: all of them at once or none)
-    attr.val.cooperative = 1;
+    static std::atomic<uint64_t> opt_in{0}, opt_large{0};
+    auto *kernel = orth_team_kernel<kCluster, E>;
+    if (int rc = ensure_big_smem(kernel, opt_in, (int)kOrthSmem)) return rc;
+    cudaLaunchAttribute attr[2] = {};
+    int attrs = 1;
+    if (kCluster) {
+        int dev = 0;
+        FLARE_CUDA(cudaGetDevice(&dev));
+        if (!(opt_large.load(std::memory_order_acquire) >> (dev & 63) & 1)) {
+            FLARE_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+            opt_large.fetch_or(1ull << (dev & 63), std::memory_order_release);
+        }
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = p.team; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+        attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[1].val.programmaticStreamSerializationAllowed = 1;
+        attrs = 2;
+    } else {
+        attr[0].id = cudaLaunchAttributeCooperative;
+        attr[0].val.cooperative = 1;
+    }
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(p.team * p.teams));
     cfg.blockDim = kOrthThreads; cfg.dynamicSmemBytes = kOrthSmem; cfg.stream = st;
-    cfg.attrs = &attr; cfg.numAttrs = 1;
-    FLARE_CUDA(cudaLaunchKernelEx(&cfg, orth_team_kernel<E>, maps, p));
+    cfg.attrs = attr; cfg.numAttrs = attrs;
+    FLARE_CUDA(cudaLaunchKernelEx(&cfg, kernel, maps, p));
     return FLARE_OK;
+}
+template <typename E>
+int launch_teams_as(bool cluster, const OrthMaps &maps, const OrthTeam &p, cudaStream_t st) {
+    return cluster ? launch_teams<true, E>(maps, p, st) : launch_teams<false, E>(maps, p, st);
 }
 
 int run_orth(const flare_orth_desc_t *d, const OrthScales &sc, OrthOuter o, void *workspace, cudaStream_t st) {
@@ -234,27 +306,30 @@ int run_orth(const flare_orth_desc_t *d, const OrthScales &sc, OrthOuter o, void
         if ((rc = make_half_maps(&tx[i], x[i], z.L, z.S, planes, z.ld_x)) != FLARE_OK) return rc;
     if ((rc = make_half_maps(&tA, A, z.S, z.S, planes, z.ld_s)) != FLARE_OK) return rc;
     if ((rc = make_half_maps(&tB, B, z.S, z.S, planes, z.ld_s)) != FLARE_OK) return rc;
-    if (plan.path == kOrthTeamPath) {
+    if (plan.path == kOrthTeamPath || plan.path == kOrthClusterPath) {
+        const bool cluster = plan.path == kOrthClusterPath;
         OrthTeam p{};
         p.o = o;
         for (int kind = 0; kind < 4; ++kind) {
             OrthProduct &q = p.product[kind];
             const bool symmetric = kind == kOrthGram || kind == kOrthPoly;
             q.a = A; q.ld_a = z.ld_s; q.S = z.S; q.N = symmetric ? z.S : z.L; q.K = kind == kOrthGram ? z.L : z.S;
-            q.tiles_m = (q.S + 127) / 128; q.tiles_n = (q.N + 127) / 128;
-            const TeamPlan how = team_plan(plan.team, q.tiles_m, q.tiles_n, symmetric, q.K);
-            q.upper = how.upper;
+            q.width = cluster ? cluster_plan(plan.team, q.S, q.N, q.K).width : 128;
+            q.tiles_m = (q.S + 127) / 128; q.tiles_n = (q.N + q.width - 1) / q.width;
+            const TeamPlan how = cluster ? TeamPlan{1, false, 0.0} : team_plan(plan.team, q.tiles_m, q.tiles_n, symmetric, q.K);
+            q.upper = how.upper; p.ks[kind] = how.ks;
             q.tiles = q.upper ? q.tiles_n * (q.tiles_n + 1) / 2 : q.tiles_m * q.tiles_n;
             q.f = kind == kOrthGram ? sc.a / (sc.x * sc.x) : kind == kOrthPoly ? sc.cc * sc.b / (sc.a * sc.a) : kind == kOrthApply ? 1.f / sc.b : 1.f / (sc.b * sc.x);
             q.fa = sc.cb * sc.b / sc.a; q.fi = sc.ca * sc.b;
-            p.ks[kind] = how.ks;
         }
         const OrthMaps maps{{tx[0], tx[1], tA, tB}};
         p.mem[0] = x[0]; p.mem[1] = x[1]; p.mem[2] = A; p.mem[3] = B;
         p.part = reinterpret_cast<float *>(ws + w.part);
         p.counters = reinterpret_cast<uint32_t *>(ws + w.counters); p.status = status;
         p.ld_x = z.ld_x; p.ld_s = z.ld_s; p.S = z.S; p.L = z.L; p.count = d->count; p.steps = d->steps; p.team = plan.team; p.teams = plan.teams;
-        return o.out_type == FLARE_DTYPE_F32 ? launch_teams<float>(maps, p, st) : o.out_type == FLARE_DTYPE_BF16 ? launch_teams<__nv_bfloat16>(maps, p, st) : launch_teams<__half>(maps, p, st);
+        return o.out_type == FLARE_DTYPE_F32    ? launch_teams_as<float>(cluster, maps, p, st)
+               : o.out_type == FLARE_DTYPE_BF16 ? launch_teams_as<__nv_bfloat16>(cluster, maps, p, st)
+                                                : launch_teams_as<__half>(cluster, maps, p, st);
     }
     for (int step = 0; step < d->steps; ++step) {
         const int cur = step & 1;

@@ -318,6 +318,7 @@ struct OrthProduct {
     long ld_a;
     int S, N, K;                 // result [S, N], sums over K
     int tiles_m, tiles_n, tiles; // tiles of a matrix, down, across and in all
+    int width;                   // columns of a tile: 256 of a pair's, 128 or 64 of a single block's
     int upper;                   // a symmetric result: tiles on and above the diagonal, each stored twice
     float f, fa, fi;             // result = f sums (+ fa A + fi I)
 };
@@ -487,19 +488,19 @@ __device__ __forceinline__ void orth_load(OrthPipe &q, const OrthProduct &p, con
     asm volatile("fence.proxy.async.global;" ::: "memory");              // (what was stored by others before this, for the loads by TMA)
     for (int t = w.t0; t < w.total; t += w.step) {
         const OrthTile x = orth_tile(p, w, t);
-        const bool own = symmetric && x.i == x.j;                       // both factors are the same rows
-        const int ra = x.i * 128 * kPair + in_pair * 128, rb = x.j * 128 * kPair + in_pair * 128;
+        const bool own = symmetric && x.i == x.j && (kPair == 2 || p.width == 128);   // both factors are the same rows
+        const int ra = x.i * 128 * kPair + in_pair * 128, rb = kPair == 2 ? x.j * 256 + in_pair * 128 : x.j * p.width, right = kPair == 2 ? 128 : p.width;
         for (int kb = w.kb0; kb < w.kb1; ++kb, ++q.n) {
             const uint32_t s = q.n % kOrthStages;
             if (q.n >= kOrthStages && !ptx::mbar_wait(q.empty(s), (q.n / kOrthStages - 1) & 1, q.abort_flag, 101)) return;
             const uint32_t at = q.smem0 + s * kOrthStage, bar = kPair == 2 ? ptx::in_block(q.full(s), 0) : q.full(s);
-            if (in_pair == 0) ptx::mbar_arrive_expect_tx(q.full(s), kPair * (own ? 2 : 4) * kOrthHalfTile);
+            if (in_pair == 0) ptx::mbar_arrive_expect_tx(q.full(s), kPair * 2 * (kOrthHalfTile + (own ? 0 : right * 128)));
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int r = 0; r < 2; ++r) {
                     ptx::tma_load_3d_for<kPair>(at + h * kOrthHalfTile + r * 8192, ta, bar, kb * 64, ra + r * 64, 2 * x.mat + h);
-                    if (own) continue;
+                    if (own || r * 64 >= right) continue;
                     if (symmetric) ptx::tma_load_3d_for<kPair>(at + (2 + h) * kOrthHalfTile + r * 8192, tb, bar, kb * 64, rb + r * 64, 2 * x.mat + h);
                     else ptx::tma_load_3d_for<kPair>(at + (2 + h) * kOrthHalfTile + r * 8192, tb, bar, rb + r * 64, kb * 64, 2 * x.mat + h);
                 }
@@ -513,11 +514,11 @@ __device__ __forceinline__ void orth_issue(OrthPipe &q, const OrthProduct &p, co
     const bool symmetric = orth_symmetric(kind);
     constexpr int kTileN = 128 * kPair;
     constexpr uint32_t hi = ptx::desc_hi(1024, 2), low = kOrthHalfTile >> 4;
-    const uint32_t idesc = instr_desc_f16(128 * kPair, kTileN, symmetric ? 0 : 1), b_lbo = symmetric ? 16 : 8192, b_step = (symmetric ? 32 : 2048) >> 4;
+    const uint32_t idesc = instr_desc_f16(128 * kPair, kPair == 2 ? 256 : p.width, symmetric ? 0 : 1), b_lbo = symmetric ? 16 : 8192, b_step = (symmetric ? 32 : 2048) >> 4;
     if (!ptx::elect_one()) return;
     for (int t = w.t0; t < w.total; t += w.step) {
         const OrthTile x = orth_tile(p, w, t);
-        const bool own = symmetric && x.i == x.j;
+        const bool own = symmetric && x.i == x.j && (kPair == 2 || p.width == 128);
         for (int kb = w.kb0; kb < w.kb1; ++q.c) {
             const uint32_t acc = q.tmem + (q.c & 1) * kTileN;
             if (q.c >= 2 && !ptx::mbar_wait(q.acc_empty(q.c & 1), (q.c / 2 - 1) & 1, q.abort_flag, 102)) return;
@@ -544,9 +545,10 @@ __device__ __forceinline__ void orth_issue(OrthPipe &q, const OrthProduct &p, co
     }
 }
 
-// The result warps' parts.  First a tile's sums into registers, a row a thread and half of the tile's columns: false if a wait gave up.
+// The result warps' parts.  First a tile's sums into registers, a row a thread and half of the tile's columns (mine: this warp has columns): false if a
+// wait gave up.
 template <int kPair>
-__device__ __forceinline__ bool orth_sums(OrthPipe &q, int chunks, float (&v)[64 * kPair]) {
+__device__ __forceinline__ bool orth_sums(OrthPipe &q, int chunks, float (&v)[64 * kPair], bool mine = true) {
     constexpr int kTileN = 128 * kPair, kCols = 64 * kPair;
     const int warp = ptx::warp_index(), quad = warp & 3, half = (warp - 4) >> 2, lane = threadIdx.x & 31;
     const uint32_t acc = q.tmem + ((uint32_t)(quad * 32) << 16) + half * kCols;
@@ -556,6 +558,7 @@ __device__ __forceinline__ bool orth_sums(OrthPipe &q, int chunks, float (&v)[64
         ptx::tc_fence_after();
 #pragma unroll
         for (int k = 0; k < kCols; k += 32) {
+            if (!mine) break;
             uint32_t u[32];
             ptx::tmem_ld32(acc + (q.c & 1) * kTileN + k, u);
             ptx::tmem_wait_ld();
@@ -719,7 +722,8 @@ orth_pair_kernel(const __grid_constant__ CUtensorMap ta, const __grid_constant__
 // ---- matrices in between: all products in one cooperative launch, a team of blocks to a matrix
 //
 // A launch per product costs some 8 us beside its work (138 us for 130 x 130, whose products take 20).  Here the blocks stay, one an SM, and
-// the blocks of a team wait for one another between products: a counter in memory, some 2 us.  Tiles are 128 x 128, a block each; where a
+// the blocks of a team wait for one another between products: a counter in memory, some 2 us, or, where a cluster is team enough, its barrier.  Tiles are
+// 128 x 128 (a cluster's also 128 x 64), a block each; where a
 // product has fewer tiles than the team blocks, ks blocks share a tile's K: each leaves its sums in memory (they stay in L2), and when all of a tile's
 // have arrived, each finishes its part of the tile's columns.
 struct OrthTeam {
@@ -836,13 +840,13 @@ __device__ __forceinline__ void team_join(const OrthTeam &p, const OrthPipe &q, 
     asm volatile("fence.proxy.async.global;" ::: "memory");              // (loaded by TMA next)
     __syncwarp();
 }
-template <bool kResults, typename E>
+template <bool kCluster, bool kResults, typename E>
 __device__ __forceinline__ void team_product(const OrthTeam &p, OrthPipe &q, int kind, int team, int mat, int count, const HalfMaps *ta, const HalfMaps *tb,
                                              const HalfMaps *out, __half *dst) {
     const bool symmetric = orth_symmetric(kind);
     const int warp = ptx::warp_index(), member = blockIdx.x % p.team;
     const OrthProduct &d = p.product[kind];
-    const int blocks = (d.K + 63) / 64, ks = p.ks[kind];
+    const int blocks = (d.K + 63) / 64, ks = kCluster ? 1 : p.ks[kind];
     // (with ks blocks a tile: member ks t + r has the r-th part of tile t's K, and no second tile)
     const int rank = ks > 1 ? member % ks : 0, first = member / ks;
     if (ks > 1 && first >= d.tiles) return;
@@ -855,9 +859,10 @@ __device__ __forceinline__ void team_product(const OrthTeam &p, OrthPipe &q, int
         for (int t = w.t0; t < w.total; t += w.step) {
             const OrthTile x = orth_tile(d, w, t);
             float v[64];
-            if (!orth_sums<1>(q, chunks, v)) break;
-            if (ks == 1) {
-                const int row0 = x.i * 128 + quad * 32, col0 = x.j * 128 + half * 64;
+            const bool mine = half * 64 < d.width;
+            if (!orth_sums<1>(q, chunks, v, mine)) break;
+            if (kCluster || ks == 1) {
+                const int row0 = x.i * 128 + quad * 32, col0 = mine ? x.j * d.width + half * 64 : d.N;
                 const bool mirror = d.upper && x.i != x.j;
                 if (d.tiles <= p.team) {
                     asm volatile("bar.sync 1, 256;" ::: "memory");           // (everybody's sums are complete, so no stage is in use)
@@ -871,14 +876,15 @@ __device__ __forceinline__ void team_product(const OrthTeam &p, OrthPipe &q, int
                 for (int k = 0; k < 64; ++k) __stcg(mine + k * 128, v[k]);
             }
         }
-        if (ks > 1) team_join<E>(p, q, d, orth_tile(d, w, first), kind, team, first, rank, count, ks, dst);
+        if (!kCluster && ks > 1) team_join<E>(p, q, d, orth_tile(d, w, first), kind, team, first, rank, count, ks, dst);
         else if (lane == 0) ptx::tma_store_wait<false>();
+        asm volatile("fence.proxy.async.global;" ::: "memory");
         __syncwarp();
     }
     __syncwarp();
 }
 
-template <bool kResults, typename E>
+template <bool kCluster, bool kResults, typename E>
 __device__ __forceinline__ void team_run(const OrthMaps &maps, const OrthTeam &p, OrthPipe &q) {
     const int team = blockIdx.x / p.team;
     uint32_t met = 0;
@@ -890,23 +896,27 @@ __device__ __forceinline__ void team_run(const OrthMaps &maps, const OrthTeam &p
             const int step = i / 3, stage = i - 3 * step, cur = step & 1, kind = stage < 2 ? stage : step + 1 < p.steps ? kOrthApply : kOrthLast;
             const int left = stage == 0 ? cur : stage == 1 ? 2 : 3, right = stage == 1 ? 2 : cur, to = stage == 0 ? 2 : stage == 1 ? 3 : 1 - cur;
             count += stage == 0;
-            team_product<kResults, E>(p, q, kind, team, mat, count, maps.m + left, maps.m + right, maps.m + to, p.mem[to]);
-            if (kind != kOrthLast || mat + p.teams < p.count) ok = team_meet(p, q, team, met);
+            team_product<kCluster, kResults, E>(p, q, kind, team, mat, count, maps.m + left, maps.m + right, maps.m + to, p.mem[to]);
+            if constexpr (kCluster) ptx::cluster_meet();     // (blocks that gave up a wait come here too: their later waits end at once)
+            else if (kind != kOrthLast || mat + p.teams < p.count) ok = team_meet(p, q, team, met);
         }
 }
-template <typename E>
+// kCluster: the team is a cluster, whose barrier takes a tenth of the time; else a cooperative launch.
+template <bool kCluster, typename E>
 __global__ void __launch_bounds__(kOrthThreads, 1) orth_team_kernel(const __grid_constant__ OrthMaps maps, const __grid_constant__ OrthTeam p) {
     extern __shared__ uint8_t raw[];
     __shared__ uint32_t tmem_slot;
     __shared__ volatile uint32_t abort_flag;
     OrthPipe q = orth_pipe<1>(raw, &tmem_slot, &abort_flag);
+    ptx::grid_launch();
+    ptx::grid_wait();
     // Registers of the launch, 384 x 168, as 128 x 72 and 256 x 216.
     if (ptx::warp_index() < 4) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
-        team_run<false, E>(maps, p, q);
+        team_run<kCluster, false, E>(maps, p, q);
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
-        team_run<true, E>(maps, p, q);
+        team_run<kCluster, true, E>(maps, p, q);
     }
     __syncwarp();
     orth_pipe_end<1>(q, p.status);

@@ -217,6 +217,7 @@ int launch_pairs(const HalfMaps &ta, const HalfMaps &tb, const HalfMaps &out, Or
     p.tiles_m = (p.S + 255) / 256;
     p.tiles_n = (p.N + 255) / 256;
     p.upper = kKind == kOrthGram || kKind == kOrthPoly;
+    p.per_m = 1.f / (float)p.tiles_m;
     p.tiles = p.upper ? p.tiles_n * (p.tiles_n + 1) / 2 : p.tiles_m * p.tiles_n;
     a.total = p.tiles * count;
     cudaLaunchAttribute attr[2] = {};
@@ -319,6 +320,7 @@ int run_orth(const flare_orth_desc_t *d, const OrthScales &sc, OrthOuter o, void
             const TeamPlan how = cluster ? TeamPlan{1, false, 0.0} : team_plan(plan.team, q.tiles_m, q.tiles_n, symmetric, q.K);
             q.upper = how.upper; p.ks[kind] = how.ks;
             q.tiles = q.upper ? q.tiles_n * (q.tiles_n + 1) / 2 : q.tiles_m * q.tiles_n;
+            q.per_m = 1.f / (float)q.tiles_m;
             q.f = kind == kOrthGram ? sc.a / (sc.x * sc.x) : kind == kOrthPoly ? sc.cc * sc.b / (sc.a * sc.a) : kind == kOrthApply ? 1.f / sc.b : 1.f / (sc.b * sc.x);
             q.fa = sc.cb * sc.b / sc.a; q.fi = sc.ca * sc.b;
         }

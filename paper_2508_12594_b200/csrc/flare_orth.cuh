@@ -318,6 +318,7 @@ struct OrthProduct {
     long ld_a;
     int S, N, K;                 // result [S, N], sums over K
     int tiles_m, tiles_n, tiles; // tiles of a matrix, down, across and in all
+    float per_m;                 // 1 / tiles_m
     int width;                   // columns of a tile: 256 of a pair's, 128 or 64 of a single block's
     int upper;                   // a symmetric result: tiles on and above the diagonal, each stored twice
     float f, fa, fi;             // result = f sums (+ fa A + fi I)
@@ -434,11 +435,17 @@ struct OrthTile { int mat, i, j; };
 __device__ __forceinline__ bool orth_symmetric(int kind) { return kind == kOrthGram || kind == kOrthPoly; }
 __device__ __forceinline__ OrthTile orth_tile(const OrthProduct &p, const OrthShare &w, int t) {
     OrthTile x;
-    x.mat = t / p.tiles;
-    t -= x.mat * p.tiles;
-    x.mat += w.mat;
+    x.mat = w.mat;
+    if (t >= p.tiles) {
+        const int more = t / p.tiles;
+        x.mat += more;
+        t -= more * p.tiles;
+    }
     if (p.upper) upper_tile(t, p.tiles_n, x.i, x.j);
-    else { x.i = t % p.tiles_m; x.j = t / p.tiles_m; }
+    else {                                                   // (a division, for numbers of tiles: t + 1/2 over tiles_m is never near a whole number)
+        x.j = (int)(((float)t + 0.5f) * p.per_m);
+        x.i = t - x.j * p.tiles_m;
+    }
     return x;
 }
 
@@ -575,6 +582,51 @@ __device__ __forceinline__ bool orth_sums(OrthPipe &q, int chunks, float (&v)[64
     return true;
 }
 // Then what they are for: kCols columns from col0 on of the warp's 32 rows from row0 on; mirror: the tile's transpose is stored too.
+// The part of A that the result's 32 rows x 64 columns want, eight lanes a row: neighbouring lanes next to each other (a row a lane, as the sums lie, would
+// ask for 32 lines at a time).
+struct OrthPart { uint4 h[8], l[8]; };
+__device__ __forceinline__ void orth_part(const OrthProduct &p, int mat, int row0, int col0, OrthPart &a) {
+    const int lane = threadIdx.x & 31, col = col0 + (lane & 7) * 8;
+    const long plane = (long)p.S * p.ld_a;
+    const __half *at = p.a + 2 * mat * plane + (long)(row0 + (lane >> 3)) * p.ld_a + col;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        a.h[e] = a.l[e] = make_uint4(0, 0, 0, 0);
+        if (row0 + 4 * e + (lane >> 3) < p.S && col < p.N) {
+            a.h[e] = __ldcg(reinterpret_cast<const uint4 *>(at + (long)4 * e * p.ld_a));   // (stored by other blocks of this very launch, it may be)
+            a.l[e] = __ldcg(reinterpret_cast<const uint4 *>(at + plane + (long)4 * e * p.ld_a));
+        }
+    }
+}
+// Through shared memory to a row a lane: v <- f v + fa A, one half at a time.
+__device__ __forceinline__ void orth_part_add(uint32_t piece, const OrthProduct &p, const OrthPart &a, float *v) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        __syncwarp();
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const uint4 &x = half ? a.l[e] : a.h[e];
+            const uint32_t r[4] = {x.x, x.y, x.z, x.w};
+            const int row = 4 * e + (lane >> 3);
+            ptx::sts128(piece + row * 128 + (((lane & 7) ^ (row & 7)) << 4), r);
+        }
+        __syncwarp();
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float4 x = ptx::lds128(piece + lane * 128 + ((e ^ (lane & 7)) << 4));
+            const uint32_t r[4] = {__float_as_uint(x.x), __float_as_uint(x.y), __float_as_uint(x.z), __float_as_uint(x.w)};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float2 y = __half22float2(*reinterpret_cast<const __half2 *>(&r[i]));
+                float &v0 = v[8 * e + 2 * i], &v1 = v[8 * e + 2 * i + 1];
+                v0 = fmaf(p.fa, y.x, half ? v0 : p.f * v0);
+                v1 = fmaf(p.fa, y.y, half ? v1 : p.f * v1);
+            }
+        }
+    }
+    __syncwarp();
+}
 // kRoomy: the stages are free (this is the block's only tile of the product), so that each piece has a place of its own and none waits for another.
 template <bool kRoomy, typename E, int kCols>
 __device__ __forceinline__ void orth_finish(const OrthPipe &q, const OrthProduct &p, const OrthOuter &o, int kind, int mat, int row0, int col0, bool mirror,
@@ -592,26 +644,15 @@ __device__ __forceinline__ void orth_finish(const OrthPipe &q, const OrthProduct
     for (int k = 0; k < kCols; k += 64) {
         if (row0 >= p.S || col0 + k >= p.N) continue;                    // (uniform over the warp)
         if (kind == kOrthPoly) {
-            // all of the piece of A is asked for before any of it is used
-            const __half *ah = p.a + 2 * mat * (long)p.S * p.ld_a + (long)row * p.ld_a + col0 + k, *al = ah + (long)p.S * p.ld_a;
-            uint4 h[8], l[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                h[e] = l[e] = make_uint4(0, 0, 0, 0);
-                if (row < p.S && col0 + k + 8 * e < p.N) {
-                    h[e] = __ldcg(reinterpret_cast<const uint4 *>(ah) + e);   // (stored by other blocks of this very launch, it may be)
-                    l[e] = __ldcg(reinterpret_cast<const uint4 *>(al) + e);
-                }
+            OrthPart part;
+            orth_part(p, mat, row0, col0 + k, part);
+            if (!kRoomy) {                                               // (the piece is on its way out)
+                if (lane == 0) ptx::tma_store_wait<true>();
             }
+            orth_part_add(q.pieces0 + (warp - 4) * kOrthPiece, p, part, v + k);
+            if (row0 < col0 + k + 64 && col0 + k < row0 + 32) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                float a[8];
-                join8(h[e], l[e], a);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int c = k + 8 * e + i;
-                    v[c] = fmaf(p.fa, a[i], p.f * v[c]) + (row == col0 + c ? p.fi : 0.f);
-                }
+                for (int e = 0; e < 64; ++e) v[k + e] += row == col0 + k + e ? p.fi : 0.f;
             }
         } else {
 #pragma unroll
@@ -860,9 +901,9 @@ __device__ __forceinline__ void team_product(const OrthTeam &p, OrthPipe &q, int
             const OrthTile x = orth_tile(d, w, t);
             float v[64];
             const bool mine = half * 64 < d.width;
+            const int row0 = x.i * 128 + quad * 32, col0 = mine ? x.j * d.width + half * 64 : d.N;
             if (!orth_sums<1>(q, chunks, v, mine)) break;
             if (kCluster || ks == 1) {
-                const int row0 = x.i * 128 + quad * 32, col0 = mine ? x.j * d.width + half * 64 : d.N;
                 const bool mirror = d.upper && x.i != x.j;
                 if (d.tiles <= p.team) {
                     asm volatile("bar.sync 1, 256;" ::: "memory");           // (everybody's sums are complete, so no stage is in use)

@@ -295,6 +295,13 @@ BINDING(spectral_gram, 8)
     check_status(unlocked([&] { return lib.spectral_gram(c.d, q, k, le, ld, g, w.p, w.n, st); }), "flare_spectral_gram");
 BINDING_END
 
+// A Python float, or any number that converts to one.
+double number(PyObject *o) {
+    const double x = PyFloat_AsDouble(o);
+    if (x == -1.0 && PyErr_Occurred()) throw PythonError{};
+    return x;
+}
+
 // ---- the convenience calls: descriptor from the tensors, outputs and scratch allocated here
 
 flare_desc_t make_desc(const at::Tensor &Q, const at::Tensor &K, double scale) {
@@ -315,12 +322,6 @@ size_t workspace_bytes(const flare_desc_t &d, int op) {
     return n;
 }
 size_t round256(size_t n) { return (n + 255) & ~(size_t)255; }
-// A Python float, or any number that converts to one.
-double number(PyObject *o) {
-    const double x = PyFloat_AsDouble(o);
-    if (x == -1.0 && PyErr_Occurred()) throw PythonError{};
-    return x;
-}
 
 // Scratch that is dropped when the call returns, with its kernels still queued: allocated on the stream it is used on (none given: the
 // current one), so that nothing of another stream takes its place before they have run, or is still at work on it when they start.
@@ -444,6 +445,45 @@ float *row_param(PyObject *o, int64_t C, const char *name) {
     if (t.dim() != 1 || t.size(0) != C) fail(PyExc_ValueError, std::string(name) + ": expected shape (" + std::to_string(C) + ",), got " + shape_text(t.sizes()));
     return (float *)t.data_ptr();
 }
+// A Norm (kind, weight, bias, eps), or None: taken apart here, a call of Python's less.
+struct NormArg {
+    int kind = FLARE_NORM_NONE;
+    float *weight = nullptr, *bias = nullptr;
+    float eps = 0.f;
+    NormArg(PyObject *o, int64_t C, const char *weight_name, const char *bias_name) {
+        if (o == Py_None) return;
+        if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != 4) fail(PyExc_TypeError, "expected a Norm (kind, weight, bias, eps) or None");
+        kind = kind_of(PyTuple_GET_ITEM(o, 0), {{"layer", FLARE_NORM_LAYER}, {"rms", FLARE_NORM_RMS}}, "norm");
+        weight = row_param(PyTuple_GET_ITEM(o, 1), C, weight_name);
+        bias = row_param(PyTuple_GET_ITEM(o, 2), C, bias_name);
+        eps = (float)number(PyTuple_GET_ITEM(o, 3));
+    }
+    static int kind_of(PyObject *name, std::initializer_list<std::pair<const char *, int>> table, const char *what) {
+        if (PyUnicode_Check(name))
+            for (const auto &entry : table)
+                if (PyUnicode_CompareWithASCIIString(name, entry.first) == 0) return entry.second;
+        std::string text = std::string(what) + ": expected one of";
+        for (const auto &entry : table) text += std::string(&entry == table.begin() ? " " : ", ") + entry.first;
+        PyObject *repr = PyObject_Repr(name);
+        if (repr) text += std::string(", got ") + PyUnicode_AsUTF8(repr);
+        Py_XDECREF(repr);
+        fail(PyExc_ValueError, text);
+    }
+};
+int gate_kind_of(PyObject *gate, PyObject *kind) {
+    if (gate == Py_None) return FLARE_GATE_NONE;
+    return NormArg::kind_of(kind, {{"sigmoid", FLARE_GATE_SIGMOID}, {"linear", FLARE_GATE_LINEAR}}, "gate_kind");
+}
+// The tuple of results as an instance of a NamedTuple class.
+PyObject *named(PyObject *cls, PyObject *values) {
+    if (!values) throw PythonError{};
+    PyObject *args = PyTuple_Pack(1, values);
+    Py_DECREF(values);
+    PyObject *r = args ? PyTuple_Type.tp_new((PyTypeObject *)cls, args, nullptr) : nullptr;
+    Py_XDECREF(args);
+    if (!r) throw PythonError{};
+    return r;
+}
 int number_of(PyObject *o) {
     const long x = PyLong_AsLong(o);
     if (x == -1 && PyErr_Occurred()) throw PythonError{};
@@ -530,107 +570,107 @@ struct Around {
     at::TensorOptions as(at::ScalarType t) const { return options.dtype(t); }
 };
 
-// x, kind, weight, bias, eps, dtype-carrying tensor or None, out (h, stats) or None, stream -> (h, stats)
-BINDING(block_norm, 8)
+at::Tensor sums_output(const float *present, PyObject *out, Py_ssize_t i, int64_t C, const at::TensorOptions &f32) {
+    return present ? output(out, i, {C}, f32) : at::Tensor();
+}
+float *sums_ptr(const at::Tensor &t, int64_t C) {
+    if (!t.defined()) return nullptr;
+    check(t, at::kFloat, {C});
+    return (float *)t.data_ptr();
+}
+
+// x, norm, dtype or None, out (h, stats) or None, stream -> (h, stats)
+BINDING(block_norm, 5)
     const at::Tensor &x = tensor(a[0]);
-    Around c(x, a[5] == Py_None ? x.scalar_type() : ((THPDtype *)a[5])->scalar_type);
-    c.d.pre_norm = number_of(a[1]);
-    c.d.pre_eps = (float)number(a[4]);
-    const float *w = row_param(a[2], c.C, "weight"), *b = row_param(a[3], c.C, "bias");
+    if (a[2] != Py_None && !THPDtype_Check(a[2])) fail(PyExc_TypeError, "dtype: expected a torch dtype");
+    Around c(x, a[2] == Py_None ? x.scalar_type() : ((THPDtype *)a[2])->scalar_type);
+    const NormArg n(a[1], c.C, "weight", "bias");
+    c.d.pre_norm = n.kind;
+    c.d.pre_eps = n.eps;
     const Rows rx = c.rows(x, c.d.stride_x, "x", c.res);
-    const at::Tensor h = output(a[6], 0, c.shape, c.as(c.dt)), stats = output(a[6], 1, {c.d.rows, 4}, c.as(at::kFloat));
+    const at::Tensor h = output(a[3], 0, c.shape, c.as(c.dt)), stats = output(a[3], 1, {c.d.rows, 4}, c.as(at::kFloat));
     const Rows rh = c.rows(h, c.d.stride_h, "h", c.dt);
     float *ps = c.stats(stats);
-    flare_stream_t st = stream_of(a[7]);
-    check_status(unlocked([&] { return lib.norm_forward(&c.d, rx.p, w, b, rh.p, ps, st); }), "flare_norm_forward");
+    flare_stream_t st = stream_of(a[4]);
+    check_status(unlocked([&] { return lib.norm_forward(&c.d, rx.p, n.weight, n.bias, rh.p, ps, st); }), "flare_norm_forward");
     return wrap_all({h, stats});
 BINDING_END
 
-// x, stats, dh, dy, kind, weight, bias, eps, out (dx, dweight, dbias) or None, stream -> (dx, dweight, dbias)
-BINDING(block_norm_backward, 10)
+// x, stats, dh, dy, norm, out (dx, dweight, dbias) or None, stream, class of the result -> (dx, dweight, dbias)
+BINDING(block_norm_backward, 8)
     const at::Tensor &x = tensor(a[0]), &dh = tensor(a[2]);
     Around c(x, dh);
-    c.d.pre_norm = number_of(a[4]);
-    c.d.pre_eps = (float)number(a[7]);
-    const float *w = row_param(a[5], c.C, "weight");
-    const float *b = row_param(a[6], c.C, "bias");
+    const NormArg n(a[4], c.C, "weight", "bias");
+    c.d.pre_norm = n.kind;
+    c.d.pre_eps = n.eps;
     const Rows rx = c.rows(x, c.d.stride_x, "x", c.res), rdh = c.rows(dh, c.d.stride_dh, "dh", c.dt), rdy = c.rows(a[3], c.res, c.d.stride_dy, "dy");
     const float *ps = c.stats(tensor(a[1]));
-    const at::Tensor dx = output(a[8], 0, c.shape, c.as(c.res));
-    const at::Tensor dw = w ? output(a[8], 1, {c.C}, c.as(at::kFloat)) : at::Tensor(), db = b ? output(a[8], 2, {c.C}, c.as(at::kFloat)) : at::Tensor();
+    const auto f32 = c.as(at::kFloat);
+    const at::Tensor dx = output(a[5], 0, c.shape, c.as(c.res)), dw = sums_output(n.weight, a[5], 1, c.C, f32), db = sums_output(n.bias, a[5], 2, c.C, f32);
     const Rows rdx = c.rows(dx, c.d.stride_dx, "dx", c.res);
-    flare_stream_t st = stream_of(a[9]);
+    float *pw = sums_ptr(dw, c.C), *pb = sums_ptr(db, c.C);
+    flare_stream_t st = stream_of(a[6]);
     const size_t need = lib.block_workspace_bytes(&c.d);
     if (need == 0) check_status(FLARE_ERR_UNSUPPORTED, "flare_norm_backward");
-    const at::Tensor ws = scratch(need, x, a[9], st);
-    auto p = [&](const at::Tensor &t, const char *name) -> float * {
-        if (!t.defined()) return nullptr;
-        check(t, at::kFloat, {c.C});
-        return (float *)t.data_ptr();
-    };
-    float *pw = p(dw, "dweight"), *pb = p(db, "dbias");
-    check_status(unlocked([&] { return lib.norm_backward(&c.d, rx.p, w, ps, rdy.p, rdh.p, rdx.p, pw, pb, ws.data_ptr(), need, st); }), "flare_norm_backward");
-    return wrap_all({dx, dw, db});
+    const at::Tensor ws = scratch(need, x, a[6], st);
+    check_status(unlocked([&] { return lib.norm_backward(&c.d, rx.p, n.weight, ps, rdy.p, rdh.p, rdx.p, pw, pb, ws.data_ptr(), need, st); }), "flare_norm_backward");
+    return named(a[7], wrap_all({dx, dw, db}));
 BINDING_END
 
-// x, branch, post (kind, weight, bias, eps), pre (the same), gate, gate kind, scale, residual scale, out (y, h, stats) or None, stream -> (y, h, stats)
-BINDING(block_join, 16)
+// x, branch, post, pre, gate, gate kind, scale, residual scale, out (y, h, stats) or None, stream -> (y, h, stats)
+BINDING(block_join, 10)
     const at::Tensor &x = tensor(a[0]), &o = tensor(a[1]);
     Around c(x, o);
-    c.d.post_norm = number_of(a[2]); c.d.post_eps = (float)number(a[5]);
-    c.d.pre_norm = number_of(a[6]); c.d.pre_eps = (float)number(a[9]);
-    c.d.residual_scale = (float)number(a[13]);
-    const float *wo = row_param(a[3], c.C, "post weight"), *bo = row_param(a[4], c.C, "post bias"), *wy = row_param(a[7], c.C, "pre weight"),
-                *by = row_param(a[8], c.C, "pre bias"), *s = row_param(a[12], c.C, "scale");
-    const Rows rx = c.rows(x, c.d.stride_x, "x", c.res), ro = c.rows(o, c.d.stride_branch, "branch", c.dt), rg = c.gate(a[10], number_of(a[11]));
-    const bool pre = c.d.pre_norm != FLARE_NORM_NONE;
-    const at::Tensor y = output(a[14], 0, c.shape, c.as(c.res)), h = pre ? output(a[14], 1, c.shape, c.as(c.dt)) : at::Tensor(),
-                     stats = output(a[14], 2, {c.d.rows, 4}, c.as(at::kFloat));
-    const Rows ry = c.rows(y, c.d.stride_y, "y", c.res), rh = pre ? c.rows(h, c.d.stride_h, "h", c.dt) : Rows{};
+    const NormArg post(a[2], c.C, "post weight", "post bias"), pre(a[3], c.C, "pre weight", "pre bias");
+    c.d.post_norm = post.kind; c.d.post_eps = post.eps;
+    c.d.pre_norm = pre.kind; c.d.pre_eps = pre.eps;
+    c.d.residual_scale = (float)number(a[7]);
+    const float *s = row_param(a[6], c.C, "scale");
+    const Rows rx = c.rows(x, c.d.stride_x, "x", c.res), ro = c.rows(o, c.d.stride_branch, "branch", c.dt), rg = c.gate(a[4], gate_kind_of(a[4], a[5]));
+    const bool next = pre.kind != FLARE_NORM_NONE;
+    const at::Tensor y = output(a[8], 0, c.shape, c.as(c.res)), h = next ? output(a[8], 1, c.shape, c.as(c.dt)) : at::Tensor(),
+                     stats = output(a[8], 2, {c.d.rows, 4}, c.as(at::kFloat));
+    const Rows ry = c.rows(y, c.d.stride_y, "y", c.res), rh = next ? c.rows(h, c.d.stride_h, "h", c.dt) : Rows{};
     float *ps = c.stats(stats);
-    flare_stream_t st = stream_of(a[15]);
-    check_status(unlocked([&] { return lib.join_forward(&c.d, rx.p, ro.p, rg.p, s, wo, bo, wy, by, ry.p, rh.p, ps, st); }), "flare_join_forward");
+    flare_stream_t st = stream_of(a[9]);
+    check_status(unlocked([&] { return lib.join_forward(&c.d, rx.p, ro.p, rg.p, s, post.weight, post.bias, pre.weight, pre.bias, ry.p, rh.p, ps, st); }),
+                 "flare_join_forward");
     return wrap_all({y, h, stats});
 BINDING_END
 
-// branch, y, stats, dy, dh, post (kind, weight, bias, eps), pre (the same), gate, gate kind, scale, residual scale, out or None, stream
+// branch, y, stats, dy, dh, post, pre, gate, gate kind, scale, residual scale, out or None, stream, class of the result
 // -> (dx, dbranch, dgate, dscale, dpost_weight, dpost_bias, dpre_weight, dpre_bias)
-BINDING(block_join_backward, 19)
+BINDING(block_join_backward, 14)
     const at::Tensor &o = tensor(a[0]), &y = tensor(a[1]);
     Around c(y, o);
-    c.d.post_norm = number_of(a[5]); c.d.post_eps = (float)number(a[8]);
-    c.d.pre_norm = number_of(a[9]); c.d.pre_eps = (float)number(a[12]);
-    c.d.residual_scale = (float)number(a[16]);
-    const float *wo = row_param(a[6], c.C, "post weight"), *bo = row_param(a[7], c.C, "post bias"), *wy = row_param(a[10], c.C, "pre weight"),
-                *by = row_param(a[11], c.C, "pre bias"), *s = row_param(a[15], c.C, "scale");
+    const NormArg post(a[5], c.C, "post weight", "post bias"), pre(a[6], c.C, "pre weight", "pre bias");
+    c.d.post_norm = post.kind; c.d.post_eps = post.eps;
+    c.d.pre_norm = pre.kind; c.d.pre_eps = pre.eps;
+    c.d.residual_scale = (float)number(a[10]);
+    const float *s = row_param(a[9], c.C, "scale");
     const Rows ro = c.rows(o, c.d.stride_branch, "branch", c.dt), ry = c.rows(y, c.d.stride_x, "y", c.res), rdy = c.rows(a[3], c.res, c.d.stride_dy, "dy"),
-               rdh = c.rows(a[4], c.dt, c.d.stride_dh, "dh"), rg = c.gate(a[13], number_of(a[14]));
+               rdh = c.rows(a[4], c.dt, c.d.stride_dh, "dh"), rg = c.gate(a[7], gate_kind_of(a[7], a[8]));
     const float *ps = c.stats(tensor(a[2]));
     const auto f32 = c.as(at::kFloat);
-    PyObject *out = a[17];
+    PyObject *out = a[11];
     const at::Tensor dx = output(out, 0, c.shape, c.as(c.res)), d_o = output(out, 1, c.shape, c.as(c.dt));
-    const at::Tensor dg = rg.p || a[13] != Py_None ? output(out, 2, c.gate_shape, c.as(c.dt)) : at::Tensor();
-    auto sums = [&](const float *present, Py_ssize_t i) { return present ? output(out, i, {c.C}, f32) : at::Tensor(); };
-    const at::Tensor ds = sums(s, 3), dwo = sums(wo, 4), dbo = sums(bo, 5), dwy = sums(wy, 6), dby = sums(by, 7);
+    const at::Tensor dg = a[7] != Py_None ? output(out, 2, c.gate_shape, c.as(c.dt)) : at::Tensor();
+    const at::Tensor ds = sums_output(s, out, 3, c.C, f32), dwo = sums_output(post.weight, out, 4, c.C, f32), dbo = sums_output(post.bias, out, 5, c.C, f32),
+                     dwy = sums_output(pre.weight, out, 6, c.C, f32), dby = sums_output(pre.bias, out, 7, c.C, f32);
     const Rows rdx = c.rows(dx, c.d.stride_dx, "dx", c.res), rdo = c.rows(d_o, c.d.stride_dbranch, "dbranch", c.dt);
     Rows rdg;
     if (dg.defined()) {
         rdg = rows_of(dg, c.dt, c.gate_shape, "dgate");
         c.d.stride_dgate = rdg.stride;
     }
-    auto p = [&](const at::Tensor &t) -> float * {
-        if (!t.defined()) return nullptr;
-        check(t, at::kFloat, {c.C});
-        return (float *)t.data_ptr();
-    };
-    float *p3 = p(ds), *p4 = p(dwo), *p5 = p(dbo), *p6 = p(dwy), *p7 = p(dby);
-    flare_stream_t st = stream_of(a[18]);
+    float *p3 = sums_ptr(ds, c.C), *p4 = sums_ptr(dwo, c.C), *p5 = sums_ptr(dbo, c.C), *p6 = sums_ptr(dwy, c.C), *p7 = sums_ptr(dby, c.C);
+    flare_stream_t st = stream_of(a[12]);
     const size_t need = lib.block_workspace_bytes(&c.d);
     if (need == 0) check_status(FLARE_ERR_UNSUPPORTED, "flare_join_backward");
-    const at::Tensor ws = scratch(need, y, a[18], st);
-    check_status(unlocked([&] { return lib.join_backward(&c.d, ro.p, rg.p, s, wo, bo, ry.p, wy, ps, rdy.p, rdh.p, rdx.p, rdo.p, rdg.p, p3, p4, p5, p6, p7,
-                                                         ws.data_ptr(), need, st); }), "flare_join_backward");
-    return wrap_all({dx, d_o, dg, ds, dwo, dbo, dwy, dby});
+    const at::Tensor ws = scratch(need, y, a[12], st);
+    check_status(unlocked([&] { return lib.join_backward(&c.d, ro.p, rg.p, s, post.weight, post.bias, ry.p, pre.weight, ps, rdy.p, rdh.p, rdx.p, rdo.p, rdg.p, p3,
+                                                         p4, p5, p6, p7, ws.data_ptr(), need, st); }), "flare_join_backward");
+    return named(a[13], wrap_all({dx, d_o, dg, ds, dwo, dbo, dwy, dby}));
 BINDING_END
 
 // ---- orthogonalised updates

@@ -294,8 +294,6 @@ def forward_backward(Q, K, V, dY, key_mask=None, scale=1.0, stream=None, check=F
 
 NORM_NONE, NORM_LAYER, NORM_RMS = range(3)
 GATE_NONE, GATE_SIGMOID, GATE_LINEAR = range(3)
-_NORMS = {"layer": NORM_LAYER, "rms": NORM_RMS}
-_GATES = {"none": GATE_NONE, "sigmoid": GATE_SIGMOID, "linear": GATE_LINEAR}
 
 
 class Norm(NamedTuple):
@@ -323,31 +321,16 @@ class JoinGrads(NamedTuple):
     dpre_bias: Optional[torch.Tensor]
 
 
-def _kind(table, name, what):
-    code = table.get(name)
-    if code is None:
-        raise ValueError(f"{what}: expected one of {', '.join(table)}, got {name!r}")
-    return code
-
-
-def _norm_args(norm: Optional[Norm]):
-    if norm is None:
-        return NORM_NONE, None, None, 0.0
-    return _kind(_NORMS, norm.kind, "norm"), norm.weight, norm.bias, norm.eps
-
-
 def block_norm(x, norm: Norm, dtype=None, out=None, stream=None):
     """The norm before a block.  x [..., width] -> (h [..., width] of `dtype` (x's), stats [rows, 4] float32).
     out: (h, stats) to write to, either None."""
-    kind, w, b, eps = _norm_args(norm)
-    return (_native or _bind()).block_norm(x, kind, w, b, eps, dtype, out, stream)
+    return (_native or _bind()).block_norm(x, norm, dtype, out, stream)
 
 
 def block_norm_backward(x, stats, dh, norm: Norm, dy=None, out=None, stream=None) -> NormGrads:
     """Gradients of block_norm; dy: what reaches x beside the norm.  Those of weights that are None are None.
     out: (dx, dweight, dbias) to write to, any None."""
-    kind, w, b, eps = _norm_args(norm)
-    return NormGrads._make((_native or _bind()).block_norm_backward(x, stats, dh, dy, kind, w, b, eps, out, stream))
+    return (_native or _bind()).block_norm_backward(x, stats, dh, dy, norm, out, stream, NormGrads)
 
 
 def block_join(x, branch, post: Optional[Norm] = None, pre: Optional[Norm] = None, gate=None, gate_kind="sigmoid", scale=None,
@@ -357,21 +340,14 @@ def block_join(x, branch, post: Optional[Norm] = None, pre: Optional[Norm] = Non
 
     x, branch [..., width]; gate like the branch, or with fewer of its leading dimensions (one row per batch item, say);
     gate_kind "sigmoid" or "linear"; scale float32 [width].  out: (y, h, stats) to write to, any None."""
-    if gate is None:
-        gate_kind = "none"
-    return (_native or _bind()).block_join(x, branch, *_norm_args(post), *_norm_args(pre), gate, _kind(_GATES, gate_kind, "gate_kind"), scale,
-                                           residual_scale, out, stream)
+    return (_native or _bind()).block_join(x, branch, post, pre, gate, gate_kind, scale, residual_scale, out, stream)
 
 
 def block_join_backward(branch, y, stats, dy, dh, post: Optional[Norm] = None, pre: Optional[Norm] = None, gate=None, gate_kind="sigmoid",
                         scale=None, residual_scale=1.0, out=None, stream=None) -> JoinGrads:
     """Gradients of block_join from its inputs, its y and its stats; dy may be None where there is a dh, dh goes
-    with pre.  Gradients of what is None are None.
-    out: a tuple in the order of JoinGrads to write to, any None."""
-    if gate is None:
-        gate_kind = "none"
-    return JoinGrads._make((_native or _bind()).block_join_backward(branch, y, stats, dy, dh, *_norm_args(post), *_norm_args(pre), gate,
-                                                                    _kind(_GATES, gate_kind, "gate_kind"), scale, residual_scale, out, stream))
+    with pre.  Gradients of what is None are None.  out: a tuple in the order of JoinGrads to write to, any None."""
+    return (_native or _bind()).block_join_backward(branch, y, stats, dy, dh, post, pre, gate, gate_kind, scale, residual_scale, out, stream, JoinGrads)
 
 
 # ---- orthogonalised updates of matrices

@@ -98,6 +98,7 @@ struct Columns {
     __device__ __forceinline__ int at(int j) const { return first + j * (kAligned ? 1 : 32); }
     __device__ __forceinline__ bool has(int j) const { return j < mine; }
     __device__ __forceinline__ bool any() const { return mine > 0; }
+    __device__ __forceinline__ int warp_first() const { return first & ~255; }   // (the base is a multiple of 256)
 };
 template <typename E, bool kAligned>
 __device__ __forceinline__ Raw8<E> load8(const E *row, const Columns<kAligned> &c) {
@@ -289,32 +290,38 @@ __device__ __forceinline__ Raw8<E> slot_read(uint32_t slot) {
     return r;
 }
 
-// The same for columns that are moved one at a time: a word of four bytes a column, [column of the thread][thread].  Of two-byte types the aligned word
-// that the element lies in (of the tensor's last one, where it is the word's first half, that half alone: what follows is not ours).
+// Rows off 16-byte boundaries: a warp copies the aligned 16-byte pieces that its 256 columns lie in, one more than they fill, and its lanes read their
+// columns from there (neighbouring lanes neighbouring columns).  What of the first piece is before the row is not used: it shares an aligned 16 bytes with
+// an element of the tensor, so it is in the same allocation.  What is behind the row's end is not read but filled with zeros.
+__device__ __forceinline__ uint32_t shift_of(const void *t, long row, long ld, int size) {      // bytes of its first piece that are before the row
+    return ((uint32_t)reinterpret_cast<uintptr_t>(t) + (uint32_t)row * (uint32_t)ld * (uint32_t)size) & 15u;
+}
 template <typename E>
-__device__ __forceinline__ uint32_t half_of(const void *t, long row, long ld, int first) {       // bits to shift the element down by
-    return sizeof(E) == 4 ? 0u : ((uint32_t)reinterpret_cast<uintptr_t>(t) + (uint32_t)(row * ld + first) * 2u & 2u) * 8u;
+__device__ __forceinline__ void warp_copy(uint32_t slot, const char *src, int bytes) {          // bytes: of the row from src on, 0 or less for none
+    constexpr int kBytes = 256 * (int)sizeof(E);
+    const int lane = threadIdx.x & 31;
+    const uint32_t shift = (uint32_t)reinterpret_cast<uintptr_t>(src) & 15u;
+    const int left = bytes > 0 ? min(bytes, kBytes) + (int)shift - 16 * lane : 0;
+    src += 16 * lane - (int)shift;
+    slot += 16 * lane;
+#pragma unroll
+    for (int i = 0; i <= kBytes / 512; ++i)
+        if (i < kBytes / 512 || lane == 0)
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(slot + 512 * i), "l"(src + 512 * i), "r"(max(0, min(16, left - 512 * i))) : "memory");
 }
-template <typename E, int kThreads>
-__device__ __forceinline__ void slot_copy_each(uint32_t slot, const char *src, const Columns<false> &c, bool yes, bool last_row, uint32_t half) {
-    const int mine = yes ? c.mine : 0;
-    const bool last = last_row && half == 0 && c.at(c.mine - 1) == c.C - 1;
+template <typename E>
+__device__ __forceinline__ void warp_read(uint32_t slot, uint32_t shift, float2 (&f)[4]) {
+    slot += shift + (threadIdx.x & 31) * (uint32_t)sizeof(E);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        uint32_t bytes = j < mine ? 4u : 0u;
-        if (sizeof(E) == 2 && last && j == mine - 1) bytes = 2u;
-        asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(slot + j * kThreads * 4), "l"(src + j * 32 * (int)sizeof(E)), "r"(bytes) : "memory");
-    }
-}
-template <typename E, int kThreads>
-__device__ __forceinline__ void slot_read_each(uint32_t slot, uint32_t half, float2 (&f)[4]) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        uint32_t v;
-        asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(slot + j * kThreads * 4) : "memory");
         float x;
-        if constexpr (sizeof(E) == 4) x = __uint_as_float(v);
-        else x = pair_of(v >> half, E{}).x;
+        if constexpr (sizeof(E) == 4) {
+            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x) : "r"(slot + j * 128) : "memory");
+        } else {
+            uint16_t v;
+            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(slot + j * 64) : "memory");
+            x = pair_of(v, E{}).x;
+        }
         (&f[j / 2].x)[j & 1] = x;
     }
 }
@@ -329,13 +336,21 @@ __device__ __forceinline__ void slot_write(uint32_t slot, const float2 (&f)[4]) 
 
 // What comes in beside the residual stream: nothing, a branch, a branch with a gate row a row, a branch with gate rows that are shared.
 enum { kAlone = 0, kPlain = 1, kGated = 2, kShared = 3 };
-// 16-byte pieces of eight columns of everything that is loaded (one column at a time: a word each, two pieces whatever the type).
-template <typename E, bool kAligned> __host__ __device__ constexpr int pieces_of() { return kAligned ? (int)sizeof(E) / 2 : 2; }
-template <typename T, typename R, bool kAligned, int kIn> __host__ __device__ constexpr int fwd_pieces() {
-    return pieces_of<R, kAligned>() + (kIn == kAlone ? 0 : kIn == kGated ? 2 : 1) * pieces_of<T, kAligned>();
+// 16-byte pieces of eight columns of everything that is loaded.
+template <typename E> __host__ __device__ constexpr int pieces_of() { return (int)sizeof(E) / 2; }
+template <typename T, typename R, int kIn> __host__ __device__ constexpr int fwd_pieces() {
+    return pieces_of<R>() + (kIn == kAlone ? 0 : kIn == kGated ? 2 : 1) * pieces_of<T>();
 }
-template <typename T, typename R, bool kAligned, int kIn> __host__ __device__ constexpr int bwd_pieces() {
-    return 2 * pieces_of<R, kAligned>() + (kIn == kAlone ? 1 : kIn == kGated ? 3 : 2) * pieces_of<T, kAligned>();
+template <typename T, typename R, int kIn> __host__ __device__ constexpr int bwd_pieces() {
+    return 2 * pieces_of<R>() + (kIn == kAlone ? 1 : kIn == kGated ? 3 : 2) * pieces_of<T>();
+}
+// Bytes of a block's slots of one tensor (off 16-byte boundaries: a piece more a warp), and of all of them for one turn.
+template <typename E, bool kAligned, int kThreads> __host__ __device__ constexpr int slots_of() { return pieces_of<E>() * kThreads * 16 + (kAligned ? 0 : kThreads / 2); }
+template <typename T, typename R, bool kAligned, int kIn, int kV, int kThreads> __host__ __device__ constexpr int fwd_stage() {
+    return kV * (slots_of<R, kAligned, kThreads>() + (kIn == kAlone ? 0 : kIn == kGated ? 2 : 1) * slots_of<T, kAligned, kThreads>());
+}
+template <typename T, typename R, bool kAligned, int kIn, int kThreads> __host__ __device__ constexpr int bwd_stage() {
+    return 2 * slots_of<R, kAligned, kThreads>() + (kIn == kAlone ? 1 : kIn == kGated ? 3 : 2) * slots_of<T, kAligned, kThreads>();
 }
 __host__ __device__ constexpr int stages_for(int pieces) { return pieces <= 3 ? 4 : pieces <= 7 ? 3 : 2; }
 
@@ -359,9 +374,9 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 2) block_forwa
     extern __shared__ __align__(16) uint8_t smem[];
     __shared__ RowShared row_shared;
     constexpr bool kBranch = kIn != kAlone;
-    constexpr int kPieces = fwd_pieces<T, R, kAligned, kIn>() * kV, kStages = stages_for(kPieces);
-    constexpr uint32_t kSlotR = pieces_of<R, kAligned>() * kThreads * 16, kSlotT = pieces_of<T, kAligned>() * kThreads * 16;
-    constexpr uint32_t kX = 0, kO = kV * kSlotR, kG = kO + kV * kSlotT, kStage = kPieces * kThreads * 16;
+    constexpr int kStages = stages_for(fwd_pieces<T, R, kIn>() * kV);
+    constexpr uint32_t kSlotR = slots_of<R, kAligned, kThreads>(), kSlotT = slots_of<T, kAligned, kThreads>();
+    constexpr uint32_t kX = 0, kO = kV * kSlotR, kG = kO + kV * kSlotT, kStage = fwd_stage<T, R, kAligned, kIn, kV, kThreads>();
     const int lane = threadIdx.x & (p.tpr - 1), per_turn = kThreads / p.tpr, mine = threadIdx.x / p.tpr;
     Columns<kAligned> c[kV];
     int mine_n = 0;
@@ -379,7 +394,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 2) block_forwa
     ptx::grid_wait();
 
     constexpr bool kBiasSlots = kBias && kV == 2;
-    const uint32_t slots = ptx::smem_u32(smem) + threadIdx.x * (kAligned ? 16 : 4), bias_slots = slots + kStages * kStage;   // [post, pre][group][half][thread]
+    const uint32_t slots = ptx::smem_u32(smem) + (kAligned ? threadIdx.x * 16 : 0), bias_slots = slots + kStages * kStage;   // [post, pre][group][half][thread]
     float2 sw[kV][4], sb[kV][4], w[kV][4], b[kV][4], a[kV][4];
 #pragma unroll
     for (int g = 0; g < kV; ++g) {
@@ -410,7 +425,8 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 2) block_forwa
     // loads run kStages - 1 turns ahead of the rows: pointers to the next row to ask for, and rows left from there
     const char *from_x = nullptr, *from_o = nullptr, *from_g = nullptr;
     const long row0 = piece.begin + mine, step_x = piece.step * p.ld_x * (long)sizeof(R), step_o = piece.step * p.ld_o * (long)sizeof(T), step_g = piece.step * p.ld_g * (long)sizeof(T);
-    const int columns = c[0].any() ? c[0].first : 0, apart = 8 * p.tpr;
+    const int columns = !kAligned ? c[0].warp_first() : c[0].any() ? c[0].first : 0, apart = 8 * p.tpr;
+    const uint32_t warp_r = (threadIdx.x >> 5) * (kSlotR / (kThreads / 32)), warp_t = (threadIdx.x >> 5) * (kSlotT / (kThreads / 32));   // (off boundaries: a warp's slots)
     int ahead = (int)(piece.end - row0);
     from_x = reinterpret_cast<const char *>(static_cast<const R *>(p.x) + row0 * p.ld_x + columns);
     if constexpr (kBranch) {
@@ -431,15 +447,10 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 2) block_forwa
             }
         } else {
             const uint32_t s = slots + stage * kStage;
-            const bool yes = ahead > 0, last_row = piece.end - ahead == p.rows - 1;
-            auto each = [&](auto type, uint32_t slot, const char *src) {
-                using E = decltype(type);
-                const uint32_t half = sizeof(E) == 4 ? 0u : ((uint32_t)reinterpret_cast<uintptr_t>(src) & 2u) * 8u;
-                slot_copy_each<E, kThreads>(slot, src - half / 8, c[0], yes, last_row, half);
-            };
-            each(R{}, s + kX, from_x);
-            if constexpr (kBranch) each(T{}, s + kO, from_o);
-            if constexpr (gate_row) each(T{}, s + kG, from_g);
+            const int left = ahead > 0 ? p.C - columns : 0;
+            warp_copy<R>(s + kX + warp_r, from_x, left * (int)sizeof(R));
+            if constexpr (kBranch) warp_copy<T>(s + kO + warp_t, from_o, left * (int)sizeof(T));
+            if constexpr (gate_row) warp_copy<T>(s + kG + warp_t, from_g, left * (int)sizeof(T));
         }
         ptx::copy_async_commit();
         ahead -= piece.step;
@@ -454,12 +465,14 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 2) block_forwa
         const bool live = row < piece.end;
         float2 y[kV][4];
         const uint32_t s = slots + stage * kStage;
+        if constexpr (!kAligned) __syncwarp();               // (the other lanes have read the slots that are filled now)
         fetch(stage == 0 ? kStages - 1 : stage - 1);
         ptx::copy_async_wait<kStages - 1>();
+        if constexpr (!kAligned) __syncwarp();               // (and what they copied is there)
 #pragma unroll
         for (int g = 0; g < kV; ++g) {
             if constexpr (kAligned) unpack8(slot_read<R, kThreads>(s + kX + g * kSlotR), y[g]);
-            else slot_read_each<R, kThreads>(s + kX, half_of<R>(p.x, row, p.ld_x, columns), y[g]);
+            else warp_read<R>(s + kX + warp_r, shift_of(p.x, row, p.ld_x, sizeof(R)), y[g]);
         }
         float2 st_o = make_float2(0.f, 0.f);
         if constexpr (kBranch) {
@@ -470,8 +483,8 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 2) block_forwa
                     unpack8(slot_read<T, kThreads>(s + kO + g * kSlotT), o[g]);
                     if constexpr (gate_row) unpack8(slot_read<T, kThreads>(s + kG + g * kSlotT), a[g]);
                 } else {
-                    slot_read_each<T, kThreads>(s + kO, half_of<T>(p.o, row, p.ld_o, columns), o[g]);
-                    if constexpr (gate_row) slot_read_each<T, kThreads>(s + kG, half_of<T>(p.g, row, p.ld_g, columns), a[g]);
+                    warp_read<T>(s + kO + warp_t, shift_of(p.o, row, p.ld_o, sizeof(T)), o[g]);
+                    if constexpr (gate_row) warp_read<T>(s + kG + warp_t, shift_of(p.g, row, p.ld_g, sizeof(T)), a[g]);
                 }
                 if constexpr (gate_row) gate_act8(p.gate, a[g]);
             }
@@ -517,9 +530,9 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 2) block_backw
     extern __shared__ __align__(16) uint8_t smem[];
     __shared__ RowShared row_shared;
     constexpr bool kBranch = kIn != kAlone;
-    constexpr int kPieces = bwd_pieces<T, R, kAligned, kIn>(), kStages = stages_for(kPieces), kSums = bwd_sums<kBranch, kBias>();
-    constexpr uint32_t kOneR = pieces_of<R, kAligned>() * kThreads * 16, kOneT = pieces_of<T, kAligned>() * kThreads * 16;
-    constexpr uint32_t kY = 0, kDy = kOneR, kDh = 2 * kOneR, kO = kDh + kOneT, kG = kO + kOneT, kStage = kPieces * kThreads * 16;
+    constexpr int kStages = stages_for(bwd_pieces<T, R, kIn>()), kSums = bwd_sums<kBranch, kBias>();
+    constexpr uint32_t kOneR = slots_of<R, kAligned, kThreads>(), kOneT = slots_of<T, kAligned, kThreads>();
+    constexpr uint32_t kY = 0, kDy = kOneR, kDh = 2 * kOneR, kO = kDh + kOneT, kG = kO + kOneT, kStage = bwd_stage<T, R, kAligned, kIn, kThreads>();
     const int lane = threadIdx.x & (p.tpr - 1), per_turn = kThreads / p.tpr, mine = threadIdx.x / p.tpr;
     const Columns<kAligned> c(lane, p.C, blockIdx.y * 8 * kThreads);
     RowGroup grp(p.tpr, p.cluster, &row_shared);
@@ -556,11 +569,12 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 2) block_backw
         for (int i = 0; i < 4; ++i) sum[k][i] = f2(0.f);
 
     // loads run kStages - 1 turns ahead of the rows: pointers to the next row to ask for, and rows left from there
-    const uint32_t slots = ptx::smem_u32(smem) + threadIdx.x * (kAligned ? 16 : 4);
+    const uint32_t slots = ptx::smem_u32(smem) + (kAligned ? threadIdx.x * 16 : 0);
+    const uint32_t warp_r = (threadIdx.x >> 5) * (kOneR / (kThreads / 32)), warp_t = (threadIdx.x >> 5) * (kOneT / (kThreads / 32));     // (off boundaries: a warp's slots)
     const char *from_y = nullptr, *from_dy = nullptr, *from_dh = nullptr, *from_o = nullptr, *from_g = nullptr;
     const long first = piece.begin + mine;
     int ahead = (int)(piece.end - first);
-    const int columns = c.any() ? c.first : 0;
+    const int columns = !kAligned ? c.warp_first() : c.any() ? c.first : 0;
     {
         auto at = [&](const void *t, long ld, size_t size) { return static_cast<const char *>(t) + (first * ld + columns) * (long)size; };
         from_y = at(p.x, p.ld_x, sizeof(R)); from_dy = at(p.dy, p.ld_dy, sizeof(R)); from_dh = at(p.dh, p.ld_dh, sizeof(T));
@@ -582,19 +596,14 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 2) block_backw
             }
         } else {
             const uint32_t s = slots + stage * kStage;
-            const bool yes = ahead > 0, last_row = piece.end - ahead == p.rows - 1;
-            auto each = [&](auto type, uint32_t slot, const char *src) {
-                using E = decltype(type);
-                const uint32_t half = sizeof(E) == 4 ? 0u : ((uint32_t)reinterpret_cast<uintptr_t>(src) & 2u) * 8u;
-                slot_copy_each<E, kThreads>(slot, src - half / 8, c, yes, last_row, half);
-            };
+            const int left = ahead > 0 ? p.C - columns : 0;
             if (p.has_pre) {
-                each(R{}, s + kY, from_y);
-                each(T{}, s + kDh, from_dh);
+                warp_copy<R>(s + kY + warp_r, from_y, left * (int)sizeof(R));
+                warp_copy<T>(s + kDh + warp_t, from_dh, left * (int)sizeof(T));
             }
-            if (p.dy) each(R{}, s + kDy, from_dy);
-            if constexpr (kBranch) each(T{}, s + kO, from_o);
-            if constexpr (gate_row) each(T{}, s + kG, from_g);
+            if (p.dy) warp_copy<R>(s + kDy + warp_r, from_dy, left * (int)sizeof(R));
+            if constexpr (kBranch) warp_copy<T>(s + kO + warp_t, from_o, left * (int)sizeof(T));
+            if constexpr (gate_row) warp_copy<T>(s + kG + warp_t, from_g, left * (int)sizeof(T));
         }
         ptx::copy_async_commit();
         ahead -= piece.step;
@@ -614,12 +623,14 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 2) block_backw
         if (row + piece.step < piece.end) st_next = p.stats[row + piece.step];
         else st_next = none;
         const uint32_t s0 = slots + stage * kStage;
+        if constexpr (!kAligned) __syncwarp();               // (as in the forward)
         fetch(stage == 0 ? kStages - 1 : stage - 1);
         ptx::copy_async_wait<kStages - 1>();
+        if constexpr (!kAligned) __syncwarp();
         float2 dt[4] = {f2(0.f), f2(0.f), f2(0.f), f2(0.f)};
         if (p.dy) {
             if constexpr (kAligned) unpack8(slot_read<R, kThreads>(s0 + kDy), dt);
-            else slot_read_each<R, kThreads>(s0 + kDy, half_of<R>(p.dy, row, p.ld_dy, columns), dt);
+            else warp_read<R>(s0 + kDy + warp_r, shift_of(p.dy, row, p.ld_dy, sizeof(R)), dt);
         }
         if (p.has_pre) {
             float2 yh[4], t[4];
@@ -627,8 +638,8 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 2) block_backw
                 unpack8(slot_read<R, kThreads>(s0 + kY), yh);
                 unpack8(slot_read<T, kThreads>(s0 + kDh), t);
             } else {
-                slot_read_each<R, kThreads>(s0 + kY, half_of<R>(p.x, row, p.ld_x, columns), yh);
-                slot_read_each<T, kThreads>(s0 + kDh, half_of<T>(p.dh, row, p.ld_dh, columns), t);
+                warp_read<R>(s0 + kY + warp_r, shift_of(p.x, row, p.ld_x, sizeof(R)), yh);
+                warp_read<T>(s0 + kDh + warp_t, shift_of(p.dh, row, p.ld_dh, sizeof(T)), t);
             }
             float2 c1 = f2(0.f), c2 = f2(0.f);
 #pragma unroll
@@ -655,8 +666,8 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 2) block_backw
                 unpack8(slot_read<T, kThreads>(s0 + kO), o);
                 if constexpr (gate_row) unpack8(slot_read<T, kThreads>(s0 + kG), a);
             } else {
-                slot_read_each<T, kThreads>(s0 + kO, half_of<T>(p.o, row, p.ld_o, columns), o);
-                if constexpr (gate_row) slot_read_each<T, kThreads>(s0 + kG, half_of<T>(p.g, row, p.ld_g, columns), a);
+                warp_read<T>(s0 + kO + warp_t, shift_of(p.o, row, p.ld_o, sizeof(T)), o);
+                if constexpr (gate_row) warp_read<T>(s0 + kG + warp_t, shift_of(p.g, row, p.ld_g, sizeof(T)), a);
             }
             if (p.has_post) {
 #pragma unroll

@@ -55,9 +55,9 @@ int block_launch(Kernel kernel, std::atomic<uint64_t> &opt_in, BlockArgs a, cons
 template <typename T, typename R, bool kAligned, int kIn, bool kBias, int kV, int kThreads>
 int block_forward_as(const BlockArgs &a, const BlockPlan &p, cudaStream_t st) {
     static std::atomic<uint64_t> opt_in{0};
-    constexpr int pieces = fwd_pieces<T, R, kAligned, kIn>() * kV, bias_slots = kBias && kV == 2 ? 4 * kV : 0;
+    constexpr int stages = stages_for(fwd_pieces<T, R, kIn>() * kV), bias_slots = kBias && kV == 2 ? 4 * kV : 0;
     return block_launch(block_forward_kernel<T, R, kAligned, kIn, kBias, kV, kThreads>, opt_in, a, p,
-                        (size_t)(stages_for(pieces) * pieces + bias_slots) * 16 * kThreads, st);
+                        (size_t)stages * fwd_stage<T, R, kAligned, kIn, kV, kThreads>() + bias_slots * 16 * kThreads, st);
 }
 template <typename T, typename R, int kIn, bool kBias, int kV>
 int block_forward_aligned(const BlockArgs &a, const BlockPlan &p, cudaStream_t st) {
@@ -85,9 +85,9 @@ int block_forward(const BlockArgs &a, bool aligned, int sms, cudaStream_t st) {
 template <typename T, typename R, bool kAligned, int kIn, bool kBias, int kThreads>
 int block_backward_as(const BlockArgs &a, const BlockPlan &p, cudaStream_t st) {
     static std::atomic<uint64_t> opt_in{0};
-    constexpr int pieces = bwd_pieces<T, R, kAligned, kIn>(), sums = bwd_sums<kIn != kAlone, kBias>();
+    constexpr int stages = stages_for(bwd_pieces<T, R, kIn>()), sums = bwd_sums<kIn != kAlone, kBias>();
     const size_t meet = (size_t)(kThreads / std::max(p.tpr, 32)) * sums * 8 * p.tpr * sizeof(float);
-    const size_t smem = std::max((size_t)stages_for(pieces) * pieces * 16 * kThreads, meet);
+    const size_t smem = std::max((size_t)stages * bwd_stage<T, R, kAligned, kIn, kThreads>(), meet);
     return block_launch(block_backward_kernel<T, R, kAligned, kIn, kBias, kThreads>, opt_in, a, p, smem, st);
 }
 template <typename T, typename R, int kIn>

@@ -164,28 +164,33 @@ struct RowGroup {
     __device__ __forceinline__ RowGroup(int tpr_, int cluster_, RowShared *sh_) : tpr(tpr_), cluster(cluster_), turn(0), sh(sh_) {
         warp = threadIdx.x >> 5;
         warps = tpr > 32 ? tpr >> 5 : 1;
-        first = warp / warps * warps;
+        first = warp & ~(warps - 1);
         if (cluster > 1) meet();                             // (the other blocks' shared memory is there from here on)
     }
     __device__ __forceinline__ void meet() const {
         asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
     }
-    // Sum over the lanes whose indexes differ below n (a power of two).
+    // Sum over the lanes whose indexes differ below n (a power of two), in each of them.
     __device__ __forceinline__ static float over(float v, int n) {
+        if (n == 32) {
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1)
-            if (n > o) v += __shfl_xor_sync(0xffffffffu, v, o);
+            for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+        } else {
+#pragma unroll
+            for (int o = 8; o > 0; o >>= 1)
+                if (n > o) v += __shfl_xor_sync(0xffffffffu, v, o);
+        }
         return v;
     }
     __device__ __forceinline__ float within_warp(float v) const { return over(v, min(tpr, 32)); }
-    // v of every warp of the row in this block: in lane k that of the row's k-th (zeros beyond the last).  All threads of the block call it.
+    // v of every warp of the row in this block: in lane k that of the (k mod warps)-th.  All threads of the block call it: a barrier of the row's own
+    // threads, so that rows need not wait for one another, measured slower (backward of 4096 columns 122 us instead of 113).
     __device__ __forceinline__ float4 of_warps(float4 v) {
         if ((threadIdx.x & 31) == 0) sh->warp[turn][warp] = v;
         __syncthreads();
-        const int l = threadIdx.x & 31;
-        return l < warps ? sh->warp[turn][first + l] : make_float4(0.f, 0.f, 0.f, 0.f);
+        return sh->warp[turn][first + (threadIdx.x & (warps - 1))];
     }
-    // v (the same in all threads of a block) of every block of the row: in lane k that of the k-th.  All threads of the cluster call it.
+    // v (the same in all threads of a block) of every block of the row: in lane k that of the (k mod cluster)-th.  All threads of the cluster call it.
     __device__ __forceinline__ float4 of_blocks(float4 v) {
         if ((int)threadIdx.x < cluster) {
             uint32_t to;
@@ -193,8 +198,7 @@ struct RowGroup {
             asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(to), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
         }
         meet();
-        const int l = threadIdx.x & 31;
-        return l < cluster ? sh->block[turn][l] : make_float4(0.f, 0.f, 0.f, 0.f);
+        return sh->block[turn][threadIdx.x & (cluster - 1)];
     }
     // Sums of a and, if kTwo, b over the row.  All threads of the block (and its cluster) call it.
     template <bool kTwo>
@@ -203,32 +207,39 @@ struct RowGroup {
         if (kTwo) b = within_warp(b);
         if (tpr > 32) {
             float4 v = of_warps(make_float4(a, b, 0.f, 0.f));
-            a = all_lanes(v.x, warps);
-            if (kTwo) b = all_lanes(v.y, warps);
+            a = over(v.x, warps);
+            if (kTwo) b = over(v.y, warps);
             if (cluster > 1) {
                 v = of_blocks(make_float4(a, b, 0.f, 0.f));
-                a = all_lanes(v.x, cluster);
-                if (kTwo) b = all_lanes(v.y, cluster);
+                a = over(v.x, cluster);
+                if (kTwo) b = over(v.y, cluster);
             }
             turn ^= 1;
         }
         return make_float2(a, b);
     }
-    // The sum of what the first n lanes hold (a power of two, zeros in the others), in every lane.
-    __device__ __forceinline__ static float all_lanes(float v, int n) { return __shfl_sync(0xffffffffu, over(v, n), 0); }
-    // (sum, squares of distances from the own mean, own mean, count) in the first n lanes -> the same of their union, in every lane
-    __device__ __forceinline__ static float4 join_parts(float4 v, int n) {
-        const float sum = all_lanes(v.x, n), count = all_lanes(v.w, n);
-        const float mean = count > 0.f ? sum / count : 0.f, d = v.z - mean;
-        return make_float4(sum, all_lanes(fmaf(v.w * d, d, v.y), n), mean, count);
+    // (sum, squares of distances from the own mean, own mean, count) in n lanes -> the same of their union, of 1 / inv elements
+    __device__ __forceinline__ static float4 join_parts(float4 v, int n, float inv, float count) {
+        const float sum = over(v.x, n), mean = sum * inv, d = v.z - mean;
+        return make_float4(sum, over(fmaf(v.w * d, d, v.y), n), mean, count);
+    }
+};
+
+// How many elements of a row a warp and a block have.
+struct RowCounts {
+    float warp, block, inv_warp, inv_block;                  // (the inverse of none: 0)
+    __device__ __forceinline__ RowCounts(RowGroup &grp, int C, int mine, int block_first, int block_columns) {
+        warp = grp.within_warp((float)mine);
+        block = (float)max(0, min(C - block_first, block_columns));
+        inv_warp = warp > 0.f ? 1.f / warp : 0.f;
+        inv_block = block > 0.f ? 1.f / block : 0.f;
     }
 };
 
 // Mean and 1/sqrt(var + eps) of a row.  layer: the squares are of distances from the mean, first the warp's, put together with those of the
-// row's other warps by the distances of their means (one barrier, and no small difference of large sums).  in_warp: elements of
-// this thread's warp's part of the row.
+// row's other warps by the distances of their means (one barrier, and no small difference of large sums).
 template <int kV, int kMove>
-__device__ __forceinline__ float2 moments(RowGroup &grp, const float2 (&v)[kV][4], const Columns<kMove> *c, float in_warp, int layer, float inv_c, float eps) {
+__device__ __forceinline__ float2 moments(RowGroup &grp, const float2 (&v)[kV][4], const Columns<kMove> *c, const RowCounts &n, int layer, float inv_c, float eps) {
     if (!layer) {
         float2 s = f2(0.f);
 #pragma unroll
@@ -242,29 +253,29 @@ __device__ __forceinline__ float2 moments(RowGroup &grp, const float2 (&v)[kV][4
 #pragma unroll
     for (int g = 0; g < kV; ++g) t = f2_add(t, f2_add(f2_add(v[g][0], v[g][1]), f2_add(v[g][2], v[g][3])));
     const float sum = grp.within_warp(t.x + t.y);
-    const float mean_w = in_warp > 0.f ? __fdividef(sum, in_warp) : 0.f;
+    const float mean_w = sum * n.inv_warp;
     float m2 = 0.f;
 #pragma unroll
     for (int g = 0; g < kV; ++g) {
-        if constexpr (kMove != kEach) {
-#pragma unroll
-            for (int q = 0; q < 2; ++q) {
-                const float2 d0 = f2_add(v[g][2 * q], f2(-mean_w)), d1 = f2_add(v[g][2 * q + 1], f2(-mean_w)), s = f2_fma(d1, d1, f2_mul(d0, d0));
-                m2 += c[g].four(q) ? s.x + s.y : 0.f;
-            }
-        } else {
+        if constexpr (kMove == kEach) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const float d = c[g].has(j) ? (&v[g][j / 2].x)[j & 1] - mean_w : 0.f;
                 m2 = fmaf(d, d, m2);
             }
+        } else {
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                const float2 d0 = f2_add(v[g][2 * q], f2(-mean_w)), d1 = f2_add(v[g][2 * q + 1], f2(-mean_w)), s = f2_fma(d1, d1, f2_mul(d0, d0));
+                m2 += c[g].four(q) ? s.x + s.y : 0.f;
+            }
         }
     }
     m2 = grp.within_warp(m2);
-    float4 part = make_float4(sum, m2, mean_w, in_warp);
+    float4 part = make_float4(sum, m2, mean_w, n.warp);
     if (grp.tpr > 32) {
-        part = RowGroup::join_parts(grp.of_warps(part), grp.warps);
-        if (grp.cluster > 1) part = RowGroup::join_parts(grp.of_blocks(part), grp.cluster);
+        part = RowGroup::join_parts(grp.of_warps(part), grp.warps, n.inv_block, n.block);
+        if (grp.cluster > 1) part = RowGroup::join_parts(grp.of_blocks(part), grp.cluster, inv_c, 0.f);
         grp.turn ^= 1;
     }
     return make_float2(part.z, rsqrtf(fmaf(part.y, inv_c, eps)));
@@ -409,7 +420,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 2) block_forwa
     RowGroup grp(p.tpr, p.cluster, &row_shared);
     const Piece piece(p, per_turn);
     constexpr bool gate_row = kIn == kGated;
-    const float in_warp = grp.within_warp((float)mine_n);
+    const RowCounts counts(grp, p.C, mine_n, blockIdx.y * 8 * kV * kThreads, 8 * kV * kThreads);
     ptx::grid_launch();
     ptx::grid_wait();
 
@@ -508,7 +519,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 2) block_forwa
                 }
                 if constexpr (gate_row) gate_act8(p.gate, a[g]);
             }
-            if (p.has_post) st_o = moments<kV>(grp, o, c, in_warp, p.layer_post, p.inv_c, p.eps_post);
+            if (p.has_post) st_o = moments<kV>(grp, o, c, counts, p.layer_post, p.inv_c, p.eps_post);
             const float mean = -st_o.x, rstd = p.has_post ? st_o.y : 1.f;
 #pragma unroll
             for (int g = 0; g < kV; ++g) {
@@ -524,7 +535,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 2) block_forwa
         }
         float2 st_y = make_float2(0.f, 0.f);
         if (p.has_pre) {
-            st_y = moments<kV>(grp, y, c, in_warp, p.layer_pre, p.inv_c, p.eps_pre);
+            st_y = moments<kV>(grp, y, c, counts, p.layer_pre, p.inv_c, p.eps_pre);
 #pragma unroll
             for (int g = 0; g < kV; ++g) {
                 if constexpr (kBiasSlots) unpack8(slot_read<float, kThreads>(bias_slots + (kV + g) * 2 * kThreads * 16), b[g]);

@@ -379,8 +379,8 @@ template <typename E, bool kAligned, int kThreads> __host__ __device__ constexpr
 template <typename T, typename R, bool kAligned, int kIn, int kV, int kThreads> __host__ __device__ constexpr int fwd_stage() {
     return kV * (slots_of<R, kAligned, kThreads>() + (kIn == kAlone ? 0 : kIn == kGated ? 2 : 1) * slots_of<T, kAligned, kThreads>());
 }
-template <typename T, typename R, bool kAligned, int kIn, int kThreads> __host__ __device__ constexpr int bwd_stage() {
-    return 2 * slots_of<R, kAligned, kThreads>() + (kIn == kAlone ? 1 : kIn == kGated ? 3 : 2) * slots_of<T, kAligned, kThreads>();
+template <typename T, typename R, bool kAligned, int kIn, int kV, int kThreads> __host__ __device__ constexpr int bwd_stage() {
+    return kV * (2 * slots_of<R, kAligned, kThreads>() + (kIn == kAlone ? 1 : kIn == kGated ? 3 : 2) * slots_of<T, kAligned, kThreads>());
 }
 __host__ __device__ constexpr int stages_for(int pieces) { return pieces <= 3 ? 4 : pieces <= 7 ? 3 : 2; }
 
@@ -556,57 +556,64 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 2) block_forwa
 // Sums over rows: [0] dh y^, [1] Q, [2] dh, [3] P; without biases the first two, without a branch [0] and [2].
 template <bool kBranch, bool kBias> __host__ __device__ constexpr int bwd_sums() { return (kBranch ? 2 : 1) * (kBias ? 2 : 1); }
 
-template <typename T, typename R, bool kAligned, int kIn, bool kBias, int kThreads>
+template <typename T, typename R, bool kAligned, int kIn, bool kBias, int kV, int kThreads>
 __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 2) block_backward_kernel(BlockArgs p) {
     extern __shared__ __align__(16) uint8_t smem[];
     __shared__ RowShared row_shared;
     constexpr bool kBranch = kIn != kAlone;
-    constexpr int kStages = stages_for(bwd_pieces<T, R, kIn>()), kSums = bwd_sums<kBranch, kBias>();
+    constexpr int kStages = stages_for(bwd_pieces<T, R, kIn>() * kV), kSums = bwd_sums<kBranch, kBias>();
     constexpr uint32_t kOneR = slots_of<R, kAligned, kThreads>(), kOneT = slots_of<T, kAligned, kThreads>();
-    constexpr uint32_t kY = 0, kDy = kOneR, kDh = 2 * kOneR, kO = kDh + kOneT, kG = kO + kOneT, kStage = bwd_stage<T, R, kAligned, kIn, kThreads>();
+    constexpr uint32_t kY = 0, kDy = kV * kOneR, kDh = 2 * kDy, kO = kDh + kV * kOneT, kG = kO + kV * kOneT, kStage = bwd_stage<T, R, kAligned, kIn, kV, kThreads>();
     const int lane = threadIdx.x & (p.tpr - 1), per_turn = kThreads / p.tpr, mine = threadIdx.x / p.tpr;
     constexpr int kMove = move_of<R, kAligned>();
-    const Columns<kMove> c(lane, p.tpr, p.C, blockIdx.y * 8 * kThreads);
+    Columns<kMove> c[kV];
+#pragma unroll
+    for (int g = 0; g < kV; ++g) c[g] = Columns<kMove>(lane, p.tpr, p.C, blockIdx.y * 8 * kV * kThreads + g * 8 * p.tpr);
     RowGroup grp(p.tpr, p.cluster, &row_shared);
     const Piece piece(p, per_turn);
     constexpr bool gate_row = kIn == kGated;
     ptx::grid_launch();
     ptx::grid_wait();
 
-    float2 sw[4], sb[4], w[4];
-    if constexpr (kBranch) {
-        float2 s[4];
-        load_param(p.scale, 1.f, c, s);
-        load_param(p.w_post, 1.f, c, sw);
+    // (two groups of columns with a bias: the weights in shared memory leave the registers for the sums)
+    constexpr bool kWeightSlots = kBias && kV == 2;
+    const uint32_t slots = ptx::smem_u32(smem) + (kAligned ? threadIdx.x * 16 : 0), weight_slots = slots + kStages * kStage;
+    float2 sw[kV][4], sb[kV][4], w[kV][4], a[kV][4], sum[kSums][kV][4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sw[i] = f2_mul(sw[i], s[i]);
-        if constexpr (kBias) {
-            load_param(p.b_post, 0.f, c, sb);
+    for (int g = 0; g < kV; ++g) {
+        if constexpr (kBranch) {
+            float2 s[4];
+            load_param(p.scale, 1.f, c[g], s);
+            load_param(p.w_post, 1.f, c[g], sw[g]);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) sb[i] = f2_mul(sb[i], s[i]);
+            for (int i = 0; i < 4; ++i) {
+                sw[g][i] = f2_mul(sw[g][i], s[i]);
+                a[g][i] = f2(1.f);
+            }
+            if constexpr (kBias) {
+                load_param(p.b_post, 0.f, c[g], sb[g]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sb[g][i] = f2_mul(sb[g][i], s[i]);
+            }
+            if constexpr (kIn == kShared) {
+                unpack8(load8(static_cast<const T *>(p.g) + piece.group * p.ld_g, c[g]), a[g]);
+                gate_act8(p.gate, a[g]);
+            }
         }
-    }
-    load_param(p.w_pre, 1.f, c, w);
-    float2 a[4] = {f2(1.f), f2(1.f), f2(1.f), f2(1.f)};
-    if constexpr (kBranch) {
-        if constexpr (kIn == kShared) {
-            unpack8(load8(static_cast<const T *>(p.g) + piece.group * p.ld_g, c), a);
-            gate_act8(p.gate, a);
-        }
-    }
-    float2 sum[kSums][4];
+        load_param(p.w_pre, 1.f, c[g], w[g]);
+        if constexpr (kWeightSlots) slot_write<kThreads>(weight_slots + g * 2 * kThreads * 16, w[g]);
 #pragma unroll
-    for (int k = 0; k < kSums; ++k)
+        for (int k = 0; k < kSums; ++k)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sum[k][i] = f2(0.f);
+            for (int i = 0; i < 4; ++i) sum[k][g][i] = f2(0.f);
+    }
 
     // loads run kStages - 1 turns ahead of the rows: pointers to the next row to ask for, and rows left from there
-    const uint32_t slots = ptx::smem_u32(smem) + (kAligned ? threadIdx.x * 16 : 0);
     const uint32_t warp_r = (threadIdx.x >> 5) * (kOneR / (kThreads / 32)), warp_t = (threadIdx.x >> 5) * (kOneT / (kThreads / 32));     // (off boundaries: a warp's slots)
     const char *from_y = nullptr, *from_dy = nullptr, *from_dh = nullptr, *from_o = nullptr, *from_g = nullptr;
     const long first = piece.begin + mine;
     int ahead = (int)(piece.end - first);
-    const int columns = c.from();
+    const int columns = c[0].from(), apart = 8 * p.tpr;
     {
         auto at = [&](const void *t, long ld, size_t size) { return static_cast<const char *>(t) + (first * ld + columns) * (long)size; };
         from_y = at(p.x, p.ld_x, sizeof(R)); from_dy = at(p.dy, p.ld_dy, sizeof(R)); from_dh = at(p.dh, p.ld_dh, sizeof(T));
@@ -615,16 +622,19 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 2) block_backw
     }
     auto fetch = [&](int stage) {
         if constexpr (kAligned) {
-            const bool yes = ahead > 0 && c.four(0);
             const uint32_t s = slots + stage * kStage;
-            if (p.has_pre) {
-                slot_copy<R, kThreads>(s + kY, from_y, c, yes);
-                slot_copy<T, kThreads>(s + kDh, from_dh, c, yes);
-            }
-            if (p.dy) slot_copy<R, kThreads>(s + kDy, from_dy, c, yes);
-            if constexpr (kBranch) {
-                slot_copy<T, kThreads>(s + kO, from_o, c, yes);
-                if constexpr (gate_row) slot_copy<T, kThreads>(s + kG, from_g, c, yes);
+#pragma unroll
+            for (int g = 0; g < kV; ++g) {
+                const bool yes = ahead > 0 && c[g].four(0);
+                if (p.has_pre) {
+                    slot_copy<R, kThreads>(s + kY + g * kOneR, from_y + g * apart * (int)sizeof(R), c[g], yes);
+                    slot_copy<T, kThreads>(s + kDh + g * kOneT, from_dh + g * apart * (int)sizeof(T), c[g], yes);
+                }
+                if (p.dy) slot_copy<R, kThreads>(s + kDy + g * kOneR, from_dy + g * apart * (int)sizeof(R), c[g], yes);
+                if constexpr (kBranch) {
+                    slot_copy<T, kThreads>(s + kO + g * kOneT, from_o + g * apart * (int)sizeof(T), c[g], yes);
+                    if constexpr (gate_row) slot_copy<T, kThreads>(s + kG + g * kOneT, from_g + g * apart * (int)sizeof(T), c[g], yes);
+                }
             }
         } else {
             const uint32_t s = slots + stage * kStage;
@@ -659,80 +669,91 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 2) block_backw
         fetch(stage == 0 ? kStages - 1 : stage - 1);
         ptx::copy_async_wait<kStages - 1>();
         if constexpr (!kAligned) __syncwarp();
-        float2 dt[4] = {f2(0.f), f2(0.f), f2(0.f), f2(0.f)};
-        if (p.dy) {
-            if constexpr (kAligned) unpack8(slot_read<R, kThreads>(s0 + kDy), dt);
-            else warp_read<R>(s0 + kDy + warp_r, shift_of(p.dy, row, p.ld_dy, sizeof(R)), dt);
+        auto read = [&](auto type, uint32_t slot, uint32_t warp_slot, int g, const void *t, long ld, float2 (&f)[4]) {
+            using E = decltype(type);
+            if constexpr (kAligned) unpack8(slot_read<E, kThreads>(s0 + slot + g * slots_of<E, kAligned, kThreads>()), f);
+            else warp_read<E>(s0 + slot + warp_slot, shift_of(t, row, ld, sizeof(E)), f);
+        };
+        float2 dt[kV][4];
+#pragma unroll
+        for (int g = 0; g < kV; ++g) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) dt[g][i] = f2(0.f);
+            if (p.dy) read(R{}, kDy, warp_r, g, p.dy, p.ld_dy, dt[g]);
         }
         if (p.has_pre) {
-            float2 yh[4], t[4];
-            if constexpr (kAligned) {
-                unpack8(slot_read<R, kThreads>(s0 + kY), yh);
-                unpack8(slot_read<T, kThreads>(s0 + kDh), t);
-            } else {
-                warp_read<R>(s0 + kY + warp_r, shift_of(p.x, row, p.ld_x, sizeof(R)), yh);
-                warp_read<T>(s0 + kDh + warp_t, shift_of(p.dh, row, p.ld_dh, sizeof(T)), t);
-            }
-            float2 c1 = f2(0.f), c2 = f2(0.f);
+            float2 yh[kV][4], t[kV][4], c1 = f2(0.f), c2 = f2(0.f);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                yh[i] = f2_mul(f2_add(yh[i], f2(-st.z)), f2(st.w));
-                sum[0][i] = f2_fma(t[i], yh[i], sum[0][i]);
-                if constexpr (kBias) sum[kBranch ? 2 : 1][i] = f2_add(sum[kBranch ? 2 : 1][i], t[i]);
-                t[i] = f2_mul(t[i], w[i]);
-                c1 = f2_fma(t[i], yh[i], c1);
-                c2 = f2_add(c2, t[i]);
+            for (int g = 0; g < kV; ++g) {
+                read(R{}, kY, warp_r, g, p.x, p.ld_x, yh[g]);
+                read(T{}, kDh, warp_t, g, p.dh, p.ld_dh, t[g]);
+                if constexpr (kWeightSlots) unpack8(slot_read<float, kThreads>(weight_slots + g * 2 * kThreads * 16), w[g]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    yh[g][i] = f2_mul(f2_add(yh[g][i], f2(-st.z)), f2(st.w));
+                    sum[0][g][i] = f2_fma(t[g][i], yh[g][i], sum[0][g][i]);
+                    if constexpr (kBias) sum[kBranch ? 2 : 1][g][i] = f2_add(sum[kBranch ? 2 : 1][g][i], t[g][i]);
+                    t[g][i] = f2_mul(t[g][i], w[g][i]);
+                    c1 = f2_fma(t[g][i], yh[g][i], c1);
+                    c2 = f2_add(c2, t[g][i]);
+                }
             }
             float2 means = p.layer_pre ? grp.sum<true>(c1.x + c1.y, c2.x + c2.y) : grp.sum<false>(c1.x + c1.y, 0.f);
             means.x *= -p.inv_c; means.y *= -p.inv_c;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) dt[i] = f2_fma(f2_fma(yh[i], f2(means.x), f2_add(t[i], f2(means.y))), f2(st.w), dt[i]);
+            for (int g = 0; g < kV; ++g)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) dt[g][i] = f2_fma(f2_fma(yh[g][i], f2(means.x), f2_add(t[g][i], f2(means.y))), f2(st.w), dt[g][i]);
         }
-        float2 dx[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) dx[i] = f2_mul(dt[i], f2(p.alpha));
-        if (live) store8(static_cast<R *>(p.dx) + row * p.ld_dx, c, dx);
+        for (int g = 0; g < kV; ++g) {
+            float2 dx[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) dx[i] = f2_mul(dt[g][i], f2(p.alpha));
+            if (live) store8(static_cast<R *>(p.dx) + row * p.ld_dx, c[g], dx);
+        }
         if constexpr (kBranch) {
-            float2 o[4];
-            if constexpr (kAligned) {
-                unpack8(slot_read<T, kThreads>(s0 + kO), o);
-                if constexpr (gate_row) unpack8(slot_read<T, kThreads>(s0 + kG), a);
-            } else {
-                warp_read<T>(s0 + kO + warp_t, shift_of(p.o, row, p.ld_o, sizeof(T)), o);
-                if constexpr (gate_row) warp_read<T>(s0 + kG + warp_t, shift_of(p.g, row, p.ld_g, sizeof(T)), a);
-            }
-            if (p.has_post) {
+            float2 o[kV][4], u[kV][4], d1 = f2(0.f), d2 = f2(0.f);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) o[i] = f2_mul(f2_add(o[i], f2(-st.x)), f2(st.y));
-            }
-            if constexpr (gate_row) {
-                float2 dg[4];
+            for (int g = 0; g < kV; ++g) {
+                read(T{}, kO, warp_t, g, p.o, p.ld_o, o[g]);
+                if constexpr (gate_row) read(T{}, kG, warp_t, g, p.g, p.ld_g, a[g]);
+                if (p.has_post) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) dg[i] = f2_mul(dt[i], kBias ? f2_fma(o[i], sw[i], sb[i]) : f2_mul(o[i], sw[i]));
-                if (p.gate == 1) {
-                    gate_act8(1, a);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) dg[i] = f2_mul(dg[i], f2_mul(a[i], f2_fma(a[i], f2(-1.f), f2(1.f))));
+                    for (int i = 0; i < 4; ++i) o[g][i] = f2_mul(f2_add(o[g][i], f2(-st.x)), f2(st.y));
                 }
-                if (live) store8(static_cast<T *>(p.dg) + row * p.ld_dg, c, dg);
-            }
-            float2 d1 = f2(0.f), d2 = f2(0.f), u[4];
+                if constexpr (gate_row) {
+                    float2 dg[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float2 q = kIn == kPlain ? dt[i] : f2_mul(dt[i], a[i]), k = kIn == kShared ? dt[i] : q;
-                sum[1][i] = f2_fma(k, o[i], sum[1][i]);
-                if constexpr (kBias) sum[3][i] = f2_add(sum[3][i], k);
-                u[i] = f2_mul(q, sw[i]);
-                d1 = f2_fma(u[i], o[i], d1);
-                d2 = f2_add(d2, u[i]);
+                    for (int i = 0; i < 4; ++i) dg[i] = f2_mul(dt[g][i], kBias ? f2_fma(o[g][i], sw[g][i], sb[g][i]) : f2_mul(o[g][i], sw[g][i]));
+                    if (p.gate == 1) {
+                        gate_act8(1, a[g]);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) dg[i] = f2_mul(dg[i], f2_mul(a[g][i], f2_fma(a[g][i], f2(-1.f), f2(1.f))));
+                    }
+                    if (live) store8(static_cast<T *>(p.dg) + row * p.ld_dg, c[g], dg);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float2 q = kIn == kPlain ? dt[g][i] : f2_mul(dt[g][i], a[g][i]), k = kIn == kShared ? dt[g][i] : q;
+                    sum[1][g][i] = f2_fma(k, o[g][i], sum[1][g][i]);
+                    if constexpr (kBias) sum[3][g][i] = f2_add(sum[3][g][i], k);
+                    u[g][i] = f2_mul(q, sw[g][i]);
+                    d1 = f2_fma(u[g][i], o[g][i], d1);
+                    d2 = f2_add(d2, u[g][i]);
+                }
             }
             if (p.has_post) {
                 float2 means = p.layer_post ? grp.sum<true>(d1.x + d1.y, d2.x + d2.y) : grp.sum<false>(d1.x + d1.y, 0.f);
                 means.x *= -p.inv_c; means.y *= -p.inv_c;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) u[i] = f2_mul(f2_fma(o[i], f2(means.x), f2_add(u[i], f2(means.y))), f2(st.y));
+                for (int g = 0; g < kV; ++g)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) u[g][i] = f2_mul(f2_fma(o[g][i], f2(means.x), f2_add(u[g][i], f2(means.y))), f2(st.y));
             }
-            if (live) store8(static_cast<T *>(p.d_o) + row * p.ld_do, c, u);
+#pragma unroll
+            for (int g = 0; g < kV; ++g)
+                if (live) store8(static_cast<T *>(p.d_o) + row * p.ld_do, c[g], u[g]);
         }
         stage = stage + 1 == kStages ? 0 : stage + 1;
     }
@@ -740,13 +761,13 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 2) block_backw
     // the block's sums: rows of a warp by shuffles, rows of different warps through shared memory
     ptx::copy_async_wait<0>();
     __syncthreads();
-    float *all = reinterpret_cast<float *>(smem);                // [rows at a time][sum][8 tpr]
-    const int width = 8 * p.tpr, slots_n = kThreads / max(p.tpr, 32), slot = p.tpr < 32 ? (int)(threadIdx.x >> 5) : mine;
+    float *all = reinterpret_cast<float *>(smem);                // [rows at a time][sum][group of columns][8 tpr]
+    const int width = 8 * kV * p.tpr, slots_n = kThreads / max(p.tpr, 32), slot = p.tpr < 32 ? (int)(threadIdx.x >> 5) : mine;
 #pragma unroll
     for (int k = 0; k < kSums; ++k)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            float v = (&sum[k][j / 2].x)[j & 1];
+        for (int j = 0; j < 8 * kV; ++j) {
+            float v = (&sum[k][j / 8][j % 8 / 2].x)[j & 1];
             for (int o = p.tpr; o < 32; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
             if (p.tpr >= 32 || (int)(threadIdx.x & 31) < p.tpr) all[(slot * kSums + k) * width + j * p.tpr + lane] = v;
         }
@@ -756,8 +777,8 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 2) block_backw
         float v = 0.f;
         for (int s = 0; s < slots_n; ++s) v += all[s * kSums * width + i];
         const int k = i / width, l = i % p.tpr, j = i % width / p.tpr;
-        const Columns<kMove> cc(l, p.tpr, p.C, blockIdx.y * 8 * kThreads);
-        if (cc.has(j)) out[(size_t)k * p.C + cc.at(j)] = v;
+        const Columns<kMove> cc(l, p.tpr, p.C, blockIdx.y * 8 * kV * kThreads + (j >> 3) * 8 * p.tpr);
+        if (cc.has(j & 7)) out[(size_t)k * p.C + cc.at(j & 7)] = v;
     }
 }
 

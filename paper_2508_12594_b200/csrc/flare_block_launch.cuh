@@ -7,18 +7,17 @@
 
 namespace flare {
 
-// Threads of a block, eight columns each: 512 for rows of more than 2048 columns that can be moved 16 bytes at a time, else 256.  What a row has
-// beyond that goes to further blocks of a cluster.
+// Threads of a block: 512 for rows that 256 with their groups of eight columns do not hold and that can be moved 16 bytes at a time, else 256.  What a
+// row has beyond that goes to further blocks of a cluster.
 constexpr int kBlockMaxWidth = 16384;
 // Blocks per group of rows: together about as many as fill the chip once.
 struct BlockPlan {
-    int tpr, threads, cluster, vectors;                     // vectors: groups of eight columns a thread owns
+    int tpr, threads, cluster;
     long groups;
     int chunks;                                             // blocks per group
 };
-inline BlockPlan block_plan(long rows, long group, int C, bool aligned, int sms, int vectors = 1) {
+inline BlockPlan block_plan(long rows, long group, int C, bool aligned, int sms, int vectors) {    // vectors: groups of eight columns a thread owns
     BlockPlan p;
-    p.vectors = vectors;
     p.threads = aligned && C > 2048 * vectors ? 512 : 256;
     p.tpr = aligned ? 4 : 32;                               // (columns that are moved one at a time: a warp's lanes side by side)
     while (p.tpr * 8 * vectors < C && p.tpr < p.threads) p.tpr *= 2;
@@ -29,6 +28,9 @@ inline BlockPlan block_plan(long rows, long group, int C, bool aligned, int sms,
     p.chunks = (int)std::max(1L, std::min(fit / std::max(1L, p.groups), (group + turn - 1) / turn));
     return p;
 }
+
+// Groups of eight columns a thread owns in the backward: two where there is no branch, whose sums leave the registers for it.
+constexpr int bwd_vectors(bool branch, size_t size) { return branch || size == 4 ? 1 : 2; }
 
 template <typename T, typename R> int block_forward(const BlockArgs &a, bool aligned, int sms, cudaStream_t st);
 template <typename T, typename R> int block_backward(const BlockArgs &a, bool aligned, bool bias, const BlockPlan &plan, cudaStream_t st);
@@ -82,19 +84,20 @@ int block_forward(const BlockArgs &a, bool aligned, int sms, cudaStream_t st) {
     }
 }
 
-template <typename T, typename R, bool kAligned, int kIn, bool kBias, int kThreads>
+template <typename T, typename R, bool kAligned, int kIn, bool kBias, int kV, int kThreads>
 int block_backward_as(const BlockArgs &a, const BlockPlan &p, cudaStream_t st) {
     static std::atomic<uint64_t> opt_in{0};
-    constexpr int stages = stages_for(bwd_pieces<T, R, kIn>()), sums = bwd_sums<kIn != kAlone, kBias>();
-    const size_t meet = (size_t)(kThreads / std::max(p.tpr, 32)) * sums * 8 * p.tpr * sizeof(float);
-    const size_t smem = std::max((size_t)stages * bwd_stage<T, R, kAligned, kIn, kThreads>(), meet);
-    return block_launch(block_backward_kernel<T, R, kAligned, kIn, kBias, kThreads>, opt_in, a, p, smem, st);
+    constexpr int stages = stages_for(bwd_pieces<T, R, kIn>() * kV), sums = bwd_sums<kIn != kAlone, kBias>();
+    const size_t meet = (size_t)(kThreads / std::max(p.tpr, 32)) * sums * 8 * kV * p.tpr * sizeof(float);
+    const size_t smem = std::max((size_t)stages * bwd_stage<T, R, kAligned, kIn, kV, kThreads>() + (kBias && kV == 2 ? 2 * kV * 16 * kThreads : 0), meet);
+    return block_launch(block_backward_kernel<T, R, kAligned, kIn, kBias, kV, kThreads>, opt_in, a, p, smem, st);
 }
 template <typename T, typename R, int kIn>
 int block_backward_of(const BlockArgs &a, bool aligned, bool bias, const BlockPlan &p, cudaStream_t st) {
-    if (!aligned) return block_backward_as<T, R, false, kIn, true, 256>(a, p, st);
-    if (p.threads == 512) return bias ? block_backward_as<T, R, true, kIn, true, 512>(a, p, st) : block_backward_as<T, R, true, kIn, false, 512>(a, p, st);
-    return bias ? block_backward_as<T, R, true, kIn, true, 256>(a, p, st) : block_backward_as<T, R, true, kIn, false, 256>(a, p, st);
+    if (!aligned) return block_backward_as<T, R, false, kIn, true, 1, 256>(a, p, st);
+    constexpr int kV = bwd_vectors(kIn != kAlone, sizeof(T));
+    if (p.threads == 512) return bias ? block_backward_as<T, R, true, kIn, true, kV, 512>(a, p, st) : block_backward_as<T, R, true, kIn, false, kV, 512>(a, p, st);
+    return bias ? block_backward_as<T, R, true, kIn, true, kV, 256>(a, p, st) : block_backward_as<T, R, true, kIn, false, kV, 256>(a, p, st);
 }
 template <typename T, typename R>
 int block_backward(const BlockArgs &a, bool aligned, bool bias, const BlockPlan &p, cudaStream_t st) {

@@ -83,7 +83,7 @@ int forward(const flare_block_desc_t *d, BlockArgs a, cudaStream_t st) {
 // Bytes of the partial sums, for whichever form of the kernels the tensors' alignment leads to.
 size_t partial_bytes(const flare_block_desc_t *d, long group) {
     size_t bytes = 0;
-    for (int vectors : {0, 1, bwd_vectors(false, size_of(d->dtype))}) {
+    for (int vectors : {0, 1, 2}) {
         const BlockPlan p = block_plan(d->rows, group, d->width, vectors > 0, device_info().sms, std::max(vectors, 1));
         bytes = std::max(bytes, (size_t)p.groups * p.chunks * 4 * d->width * sizeof(float));
     }
@@ -103,7 +103,7 @@ int backward(const flare_block_desc_t *d, bool join, BlockArgs a, const BlockGra
     al.add(a.d_o, a.ld_do, t); al.add(a.dg, a.ld_dg, t);
     if (!al.natural) return FLARE_ERR_INVALID_ARG;
     const bool bias = !al.ok || a.b_post || out.db_pre || out.db_post;
-    const BlockPlan plan = block_plan(d->rows, a.group, d->width, al.ok, sms, al.ok ? bwd_vectors(join, t) : 1);
+    const BlockPlan plan = block_plan(d->rows, a.group, d->width, al.ok, sms, al.ok ? bwd_vectors(block_input(a), bias, t, r, d->width) : 1);
     a.part = static_cast<float *>(workspace);
     if (d->rows > 0) {
         if (int rc = FLARE_BLOCK_TYPES(d, block_backward)(a, al.ok, bias, plan, st)) return rc;

@@ -575,8 +575,9 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 2) block_backw
     ptx::grid_launch();
     ptx::grid_wait();
 
-    // (two groups of columns with a bias: the weights in shared memory leave the registers for the sums)
-    constexpr bool kWeightSlots = kBias && kV == 2;
+    // two groups of columns: the weights in shared memory (w, sw) leave the registers for the sums
+    constexpr bool kWeightSlots = kV == 2 && (kBranch || kBias);
+    constexpr uint32_t kWeights = kV * 2 * kThreads * 16;
     const uint32_t slots = ptx::smem_u32(smem) + (kAligned ? threadIdx.x * 16 : 0), weight_slots = slots + kStages * kStage;
     float2 sw[kV][4], sb[kV][4], w[kV][4], a[kV][4], sum[kSums][kV][4];
 #pragma unroll
@@ -601,7 +602,10 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 2) block_backw
             }
         }
         load_param(p.w_pre, 1.f, c[g], w[g]);
-        if constexpr (kWeightSlots) slot_write<kThreads>(weight_slots + g * 2 * kThreads * 16, w[g]);
+        if constexpr (kWeightSlots) {
+            slot_write<kThreads>(weight_slots + g * 2 * kThreads * 16, w[g]);
+            if constexpr (kBranch) slot_write<kThreads>(weight_slots + kWeights + g * 2 * kThreads * 16, sw[g]);
+        }
 #pragma unroll
         for (int k = 0; k < kSums; ++k)
 #pragma unroll
@@ -718,6 +722,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 2) block_backw
             for (int g = 0; g < kV; ++g) {
                 read(T{}, kO, warp_t, g, p.o, p.ld_o, o[g]);
                 if constexpr (gate_row) read(T{}, kG, warp_t, g, p.g, p.ld_g, a[g]);
+                if constexpr (kWeightSlots) unpack8(slot_read<float, kThreads>(weight_slots + kWeights + g * 2 * kThreads * 16), sw[g]);
                 if (p.has_post) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) o[g][i] = f2_mul(f2_add(o[g][i], f2(-st.x)), f2(st.y));

@@ -29,8 +29,17 @@ inline BlockPlan block_plan(long rows, long group, int C, bool aligned, int sms,
     return p;
 }
 
-// Groups of eight columns a thread owns in the backward: two where there is no branch, whose sums leave the registers for it.
-constexpr int bwd_vectors(bool branch, size_t size) { return branch || size == 4 ? 1 : 2; }
+// Groups of eight columns a thread owns in the backward.  Two where there is no branch: its sums leave the registers for them, and what a row costs
+// beside its elements counts half (32768 rows of 1024, rms: 41 us instead of 51).  With a branch and a 16-bit stream two where a row of one group
+// a thread would need a cluster (4096 rows of 8192, rms, gate: 116 us instead of 199); narrower rows lose by it (65536 rows of 512: 105 instead of 90),
+// and with a float32 stream, or a gate and biases, the slots would not fit into shared memory.
+constexpr bool bwd_wide(int in, bool bias, size_t size, size_t res) { return size == 2 && in != kAlone && res == 2 && !(in == kGated && bias); }
+constexpr int bwd_vectors(int in, bool bias, size_t size, size_t res, int C) {
+    return size == 2 && (in == kAlone || (bwd_wide(in, bias, size, res) && C > 4096)) ? 2 : 1;
+}
+// Weights of theirs that are kept in shared memory.
+constexpr int bwd_weights(int in, bool bias, int vectors) { return vectors == 1 ? 0 : in == kAlone ? (bias ? 1 : 0) : 2; }
+inline int block_input(const BlockArgs &a) { return a.o == nullptr ? kAlone : !a.gate ? kPlain : a.grouped ? kShared : kGated; }
 
 template <typename T, typename R> int block_forward(const BlockArgs &a, bool aligned, int sms, cudaStream_t st);
 template <typename T, typename R> int block_backward(const BlockArgs &a, bool aligned, bool bias, const BlockPlan &plan, cudaStream_t st);
@@ -73,7 +82,6 @@ int block_forward_of(const BlockArgs &a, bool aligned, int sms, cudaStream_t st)
     if (!aligned) return block_forward_as<T, R, false, kIn, true, 1, 256>(a, p, st);
     return a.b_post || a.b_pre ? block_forward_aligned<T, R, kIn, true, kV>(a, p, st) : block_forward_aligned<T, R, kIn, false, kV>(a, p, st);
 }
-inline int block_input(const BlockArgs &a) { return a.o == nullptr ? kAlone : !a.gate ? kPlain : a.grouped ? kShared : kGated; }
 template <typename T, typename R>
 int block_forward(const BlockArgs &a, bool aligned, int sms, cudaStream_t st) {
     switch (block_input(a)) {
@@ -89,15 +97,20 @@ int block_backward_as(const BlockArgs &a, const BlockPlan &p, cudaStream_t st) {
     static std::atomic<uint64_t> opt_in{0};
     constexpr int stages = stages_for(bwd_pieces<T, R, kIn>() * kV), sums = bwd_sums<kIn != kAlone, kBias>();
     const size_t meet = (size_t)(kThreads / std::max(p.tpr, 32)) * sums * 8 * kV * p.tpr * sizeof(float);
-    const size_t smem = std::max((size_t)stages * bwd_stage<T, R, kAligned, kIn, kV, kThreads>() + (kBias && kV == 2 ? 2 * kV * 16 * kThreads : 0), meet);
+    const size_t smem = std::max((size_t)stages * bwd_stage<T, R, kAligned, kIn, kV, kThreads>() + bwd_weights(kIn, kBias, kV) * 2 * kV * 16 * kThreads, meet);
     return block_launch(block_backward_kernel<T, R, kAligned, kIn, kBias, kV, kThreads>, opt_in, a, p, smem, st);
+}
+template <typename T, typename R, int kIn, bool kBias>
+int block_backward_aligned(const BlockArgs &a, const BlockPlan &p, cudaStream_t st) {
+    constexpr int kV = bwd_vectors(kIn, kBias, sizeof(T), sizeof(R), 1);
+    if constexpr (bwd_wide(kIn, kBias, sizeof(T), sizeof(R)))
+        if (bwd_vectors(kIn, kBias, sizeof(T), sizeof(R), a.C) == 2) return block_backward_as<T, R, true, kIn, kBias, 2, 512>(a, p, st);
+    return p.threads == 512 ? block_backward_as<T, R, true, kIn, kBias, kV, 512>(a, p, st) : block_backward_as<T, R, true, kIn, kBias, kV, 256>(a, p, st);
 }
 template <typename T, typename R, int kIn>
 int block_backward_of(const BlockArgs &a, bool aligned, bool bias, const BlockPlan &p, cudaStream_t st) {
     if (!aligned) return block_backward_as<T, R, false, kIn, true, 1, 256>(a, p, st);
-    constexpr int kV = bwd_vectors(kIn != kAlone, sizeof(T));
-    if (p.threads == 512) return bias ? block_backward_as<T, R, true, kIn, true, kV, 512>(a, p, st) : block_backward_as<T, R, true, kIn, false, kV, 512>(a, p, st);
-    return bias ? block_backward_as<T, R, true, kIn, true, kV, 256>(a, p, st) : block_backward_as<T, R, true, kIn, false, kV, 256>(a, p, st);
+    return bias ? block_backward_aligned<T, R, kIn, true>(a, p, st) : block_backward_aligned<T, R, kIn, false>(a, p, st);
 }
 template <typename T, typename R>
 int block_backward(const BlockArgs &a, bool aligned, bool bias, const BlockPlan &p, cudaStream_t st) {

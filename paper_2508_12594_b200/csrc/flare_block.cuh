@@ -155,13 +155,17 @@ struct RowShared {
     float4 warp[2][16];         // what the warps of a row leave for one another, two buffers in turn: one barrier a sum
     float4 block[2][8];         // what the blocks of a cluster do
 };
+struct RowShared8 {
+    float warp[2][16][8], block[2][8][8];                    // the same of several sums at once
+};
 struct RowGroup {
     int tpr, warps, first;      // threads and warps of a row in the block, the row's first warp
     int warp;                   // this thread's warp
     int cluster;                // blocks of a row
     int turn;
     RowShared *sh;
-    __device__ __forceinline__ RowGroup(int tpr_, int cluster_, RowShared *sh_) : tpr(tpr_), cluster(cluster_), turn(0), sh(sh_) {
+    RowShared8 *sh8;
+    __device__ __forceinline__ RowGroup(int tpr_, int cluster_, RowShared *sh_, RowShared8 *sh8_ = nullptr) : tpr(tpr_), cluster(cluster_), turn(0), sh(sh_), sh8(sh8_) {
         warp = threadIdx.x >> 5;
         warps = tpr > 32 ? tpr >> 5 : 1;
         first = warp & ~(warps - 1);
@@ -217,6 +221,46 @@ struct RowGroup {
             turn ^= 1;
         }
         return make_float2(a, b);
+    }
+    // Sums of kN values (4 or 8) over a row of more than one warp, in one round.  In a warp every step halves the values a lane has, so that kN + 1 or kN
+    // + 2 shuffles do what kN times five would.  All threads of the block (and its cluster) call it.
+    template <int kN>
+    __device__ __forceinline__ void sums(float (&v)[kN]) {
+        const int l = threadIdx.x & 31, of = l % kN;
+        int at = 0;                                          // which of the values this lane is left with
+#pragma unroll
+        for (int n = kN / 2, o = 16; n > 0; n /= 2, o /= 2) {
+            const bool upper = l & o;
+            at = 2 * at + (upper ? 1 : 0);
+#pragma unroll
+            for (int i = 0; i < n; ++i) {
+                const float keep = upper ? v[i + n] : v[i], give = upper ? v[i] : v[i + n];
+                v[i] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+            }
+        }
+        float mine = over(v[0], 32 / kN);
+        if ((l & (32 / kN - 1)) == 0) sh8->warp[turn][warp][at] = mine;
+        __syncthreads();
+        mine = 0.f;
+        for (int k = l / kN; k < warps; k += 32 / kN) mine += sh8->warp[turn][first + k][of];
+#pragma unroll
+        for (int o = kN; o < 32; o *= 2) mine += __shfl_xor_sync(0xffffffffu, mine, o);
+        if (cluster > 1) {
+            if (warp == 0)
+                for (int k = l / kN; k < cluster; k += 32 / kN) {
+                    uint32_t to;
+                    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(ptx::smem_u32(&sh8->block[turn][blockIdx.y][of])), "r"(k));
+                    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to), "f"(mine) : "memory");
+                }
+            meet();
+            mine = 0.f;
+            for (int k = l / kN; k < cluster; k += 32 / kN) mine += sh8->block[turn][k][of];
+#pragma unroll
+            for (int o = kN; o < 32; o *= 2) mine += __shfl_xor_sync(0xffffffffu, mine, o);
+        }
+        turn ^= 1;
+#pragma unroll
+        for (int i = 0; i < kN; ++i) v[i] = __shfl_sync(0xffffffffu, mine, i);
     }
     // (sum, squares of distances from the own mean, own mean, count) in n lanes -> the same of their union, of 1 / inv elements
     __device__ __forceinline__ static float4 join_parts(float4 v, int n, float inv, float count) {
@@ -556,7 +600,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 2) block_forwa
 // Sums over rows: [0] dh y^, [1] Q, [2] dh, [3] P; without biases the first two, without a branch [0] and [2].
 template <bool kBranch, bool kBias> __host__ __device__ constexpr int bwd_sums() { return (kBranch ? 2 : 1) * (kBias ? 2 : 1); }
 
-template <typename T, typename R, bool kAligned, int kIn, bool kBias, int kV, int kThreads>
+template <typename T, typename R, bool kAligned, int kIn, bool kBias, bool kOnce, int kV, int kThreads>
 __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 2) block_backward_kernel(BlockArgs p) {
     extern __shared__ __align__(16) uint8_t smem[];
     __shared__ RowShared row_shared;
@@ -569,7 +613,12 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 2) block_backw
     Columns<kMove> c[kV];
 #pragma unroll
     for (int g = 0; g < kV; ++g) c[g] = Columns<kMove>(lane, p.tpr, p.C, blockIdx.y * 8 * kV * kThreads + g * 8 * p.tpr);
-    RowGroup grp(p.tpr, p.cluster, &row_shared);
+    RowShared8 *row_shared8 = nullptr;
+    if constexpr (kOnce) {                                   // (two blocks of the widest form fit an SM to the last KB)
+        __shared__ RowShared8 eight;
+        row_shared8 = &eight;
+    }
+    RowGroup grp(p.tpr, p.cluster, &row_shared, row_shared8);
     const Piece piece(p, per_turn);
     constexpr bool gate_row = kIn == kGated;
     ptx::grid_launch();
@@ -685,7 +734,60 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 2) block_backw
             for (int i = 0; i < 4; ++i) dt[g][i] = f2(0.f);
             if (p.dy) read(R{}, kDy, warp_r, g, p.dy, p.ld_dy, dt[g]);
         }
-        if (p.has_pre) {
+        [[maybe_unused]] float2 o[kV][4], post_means = make_float2(0.f, 0.f);
+        if constexpr (kOnce) {
+            // (d1 and d2 below are linear in the means that dt is made with: all sums in one round)
+            float2 yh[kV][4], c1 = f2(0.f), c2 = f2(0.f), za = f2(0.f), zy = f2(0.f), z1 = f2(0.f), sa = f2(0.f), sy = f2(0.f), s1 = f2(0.f);
+            const bool layer = p.layer_pre || p.layer_post;
+#pragma unroll
+            for (int g = 0; g < kV; ++g) {
+                float2 t[4];
+                read(R{}, kY, warp_r, g, p.x, p.ld_x, yh[g]);
+                read(T{}, kDh, warp_t, g, p.dh, p.ld_dh, t);
+                read(T{}, kO, warp_t, g, p.o, p.ld_o, o[g]);
+                if constexpr (gate_row) {
+                    read(T{}, kG, warp_t, g, p.g, p.ld_g, a[g]);
+                    gate_act8(p.gate, a[g]);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    yh[g][i] = f2_mul(f2_add(yh[g][i], f2(-st.z)), f2(st.w));
+                    sum[0][g][i] = f2_fma(t[i], yh[g][i], sum[0][g][i]);
+                    if constexpr (kBias) sum[2][g][i] = f2_add(sum[2][g][i], t[i]);
+                    t[i] = f2_mul(t[i], w[g][i]);
+                    c1 = f2_fma(t[i], yh[g][i], c1);
+                    dt[g][i] = f2_fma(t[i], f2(st.w), dt[g][i]);
+                    o[g][i] = f2_mul(f2_add(o[g][i], f2(-st.x)), f2(st.y));
+                    const float2 s = kIn == kPlain ? sw[g][i] : f2_mul(sw[g][i], a[g][i]), z = f2_mul(s, o[g][i]);
+                    za = f2_fma(z, dt[g][i], za);
+                    zy = f2_fma(z, yh[g][i], zy);
+                    if (layer) {
+                        c2 = f2_add(c2, t[i]);
+                        z1 = f2_add(z1, z);
+                        sa = f2_fma(s, dt[g][i], sa);
+                        sy = f2_fma(s, yh[g][i], sy);
+                        s1 = f2_add(s1, s);
+                    }
+                }
+            }
+            float2 means;
+            if (layer) {
+                float v[8] = {c1.x + c1.y, c2.x + c2.y, za.x + za.y, zy.x + zy.y, z1.x + z1.y, sa.x + sa.y, sy.x + sy.y, s1.x + s1.y};
+                grp.template sums<8>(v);
+                means = make_float2(-p.inv_c * v[0], p.layer_pre ? -p.inv_c * v[1] : 0.f);
+                post_means = make_float2(fmaf(st.w, fmaf(means.x, v[3], means.y * v[4]), v[2]), p.layer_post ? fmaf(st.w, fmaf(means.x, v[6], means.y * v[7]), v[5]) : 0.f);
+            } else {
+                float v[4] = {c1.x + c1.y, za.x + za.y, zy.x + zy.y, 0.f};
+                grp.template sums<4>(v);
+                means = make_float2(-p.inv_c * v[0], 0.f);
+                post_means = make_float2(fmaf(st.w * means.x, v[2], v[1]), 0.f);
+            }
+            post_means.x *= -p.inv_c; post_means.y *= -p.inv_c;
+#pragma unroll
+            for (int g = 0; g < kV; ++g)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) dt[g][i] = f2_fma(f2_fma(yh[g][i], f2(means.x), f2(means.y)), f2(st.w), dt[g][i]);
+        } else if (p.has_pre) {
             float2 yh[kV][4], t[kV][4], c1 = f2(0.f), c2 = f2(0.f);
 #pragma unroll
             for (int g = 0; g < kV; ++g) {
@@ -717,13 +819,15 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 2) block_backw
             if (live) store8(static_cast<R *>(p.dx) + row * p.ld_dx, c[g], dx);
         }
         if constexpr (kBranch) {
-            float2 o[kV][4], u[kV][4], d1 = f2(0.f), d2 = f2(0.f);
+            float2 u[kV][4], d1 = f2(0.f), d2 = f2(0.f);
 #pragma unroll
             for (int g = 0; g < kV; ++g) {
-                read(T{}, kO, warp_t, g, p.o, p.ld_o, o[g]);
-                if constexpr (gate_row) read(T{}, kG, warp_t, g, p.g, p.ld_g, a[g]);
+                if constexpr (!kOnce) {
+                    read(T{}, kO, warp_t, g, p.o, p.ld_o, o[g]);
+                    if constexpr (gate_row) read(T{}, kG, warp_t, g, p.g, p.ld_g, a[g]);
+                }
                 if constexpr (kWeightSlots) unpack8(slot_read<float, kThreads>(weight_slots + kWeights + g * 2 * kThreads * 16), sw[g]);
-                if (p.has_post) {
+                if (!kOnce && p.has_post) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) o[g][i] = f2_mul(f2_add(o[g][i], f2(-st.x)), f2(st.y));
                 }
@@ -732,7 +836,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 2) block_backw
 #pragma unroll
                     for (int i = 0; i < 4; ++i) dg[i] = f2_mul(dt[g][i], kBias ? f2_fma(o[g][i], sw[g][i], sb[g][i]) : f2_mul(o[g][i], sw[g][i]));
                     if (p.gate == 1) {
-                        gate_act8(1, a[g]);
+                        if constexpr (!kOnce) gate_act8(1, a[g]);
 #pragma unroll
                         for (int i = 0; i < 4; ++i) dg[i] = f2_mul(dg[i], f2_mul(a[g][i], f2_fma(a[g][i], f2(-1.f), f2(1.f))));
                     }
@@ -748,9 +852,9 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 2) block_backw
                     d2 = f2_add(d2, u[g][i]);
                 }
             }
-            if (p.has_post) {
-                float2 means = p.layer_post ? grp.sum<true>(d1.x + d1.y, d2.x + d2.y) : grp.sum<false>(d1.x + d1.y, 0.f);
-                means.x *= -p.inv_c; means.y *= -p.inv_c;
+            if (kOnce || p.has_post) {
+                float2 means = kOnce ? post_means : p.layer_post ? grp.sum<true>(d1.x + d1.y, d2.x + d2.y) : grp.sum<false>(d1.x + d1.y, 0.f);
+                if constexpr (!kOnce) { means.x *= -p.inv_c; means.y *= -p.inv_c; }
 #pragma unroll
                 for (int g = 0; g < kV; ++g)
 #pragma unroll

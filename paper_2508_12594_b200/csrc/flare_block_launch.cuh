@@ -31,11 +31,12 @@ inline BlockPlan block_plan(long rows, long group, int C, bool aligned, int sms,
 
 // Groups of eight columns a thread owns in the backward.  Two where there is no branch: its sums leave the registers for them, and what a row costs
 // beside its elements counts half (32768 rows of 1024, rms: 41 us instead of 51).  With a branch and a 16-bit stream two where a row of one group
-// a thread would need a cluster (4096 rows of 8192, rms, gate: 116 us instead of 199); narrower rows lose by it (65536 rows of 512: 105 instead of 90),
-// and with a float32 stream, or a gate and biases, the slots would not fit into shared memory.
+// a thread would take a block of 512 (8192 rows of 4096, rms, gate: 107 us instead of 113), with biases, whose sums do not fit, where it would take a
+// cluster (4096 rows of 8192: rms, gate 116 instead of 199; layer, biases 158 instead of 202); narrower rows lose by it (65536 rows of 512: 105
+// instead of 90), and with a float32 stream, or a gate and biases, the slots would not fit into shared memory.
 constexpr bool bwd_wide(int in, bool bias, size_t size, size_t res) { return size == 2 && in != kAlone && res == 2 && !(in == kGated && bias); }
 constexpr int bwd_vectors(int in, bool bias, size_t size, size_t res, int C) {
-    return size == 2 && (in == kAlone || (bwd_wide(in, bias, size, res) && C > 4096)) ? 2 : 1;
+    return size == 2 && (in == kAlone || (bwd_wide(in, bias, size, res) && C > (bias ? 4096 : 2048))) ? 2 : 1;
 }
 // Weights of theirs that are kept in shared memory.
 constexpr int bwd_weights(int in, bool bias, int vectors) { return vectors == 1 ? 0 : in == kAlone ? (bias ? 1 : 0) : 2; }
@@ -92,19 +93,34 @@ int block_forward(const BlockArgs &a, bool aligned, int sms, cudaStream_t st) {
     }
 }
 
-template <typename T, typename R, bool kAligned, int kIn, bool kBias, int kV, int kThreads>
-int block_backward_as(const BlockArgs &a, const BlockPlan &p, cudaStream_t st) {
+template <typename T, typename R, bool kAligned, int kIn, bool kBias, int kV, int kThreads, bool kOnce>
+int block_backward_in(const BlockArgs &a, const BlockPlan &p, cudaStream_t st) {
     static std::atomic<uint64_t> opt_in{0};
     constexpr int stages = stages_for(bwd_pieces<T, R, kIn>() * kV), sums = bwd_sums<kIn != kAlone, kBias>();
     const size_t meet = (size_t)(kThreads / std::max(p.tpr, 32)) * sums * 8 * kV * p.tpr * sizeof(float);
     const size_t smem = std::max((size_t)stages * bwd_stage<T, R, kAligned, kIn, kV, kThreads>() + bwd_weights(kIn, kBias, kV) * 2 * kV * 16 * kThreads, meet);
-    return block_launch(block_backward_kernel<T, R, kAligned, kIn, kBias, kV, kThreads>, opt_in, a, p, smem, st);
+    return block_launch(block_backward_kernel<T, R, kAligned, kIn, kBias, kOnce, kV, kThreads>, opt_in, a, p, smem, st);
+}
+// The sums of both norms in one round where a round is long (a cluster's: 4096 rows of 8192 with a float32 stream, rms, 176 us instead of 225) or
+// there are four of them (layer norms over 8192 rows of 4096: 112 instead of 123).  Two of rms norms in a block take less than what one round
+// adds to the arithmetic (65536 rows of 512: 90 instead of 96), and two groups of columns leave no registers for it.
+template <typename T, typename R, bool kAligned, int kIn, bool kBias, int kV, int kThreads>
+int block_backward_as(const BlockArgs &a, const BlockPlan &p, cudaStream_t st) {
+    if constexpr (kIn != kAlone && kV == 1)
+        if (p.tpr > 32 && a.has_pre && a.has_post && (p.cluster > 1 || a.layer_pre || a.layer_post))
+            return block_backward_in<T, R, kAligned, kIn, kBias, kV, kThreads, true>(a, p, st);
+    return block_backward_in<T, R, kAligned, kIn, kBias, kV, kThreads, false>(a, p, st);
 }
 template <typename T, typename R, int kIn, bool kBias>
 int block_backward_aligned(const BlockArgs &a, const BlockPlan &p, cudaStream_t st) {
     constexpr int kV = bwd_vectors(kIn, kBias, sizeof(T), sizeof(R), 1);
-    if constexpr (bwd_wide(kIn, kBias, sizeof(T), sizeof(R)))
-        if (bwd_vectors(kIn, kBias, sizeof(T), sizeof(R), a.C) == 2) return block_backward_as<T, R, true, kIn, kBias, 2, 512>(a, p, st);
+    if constexpr (bwd_wide(kIn, kBias, sizeof(T), sizeof(R))) {
+        if (bwd_vectors(kIn, kBias, sizeof(T), sizeof(R), a.C) == 2) {
+            if constexpr (!kBias)
+                if (p.threads == 256) return block_backward_as<T, R, true, kIn, kBias, 2, 256>(a, p, st);
+            return block_backward_as<T, R, true, kIn, kBias, 2, 512>(a, p, st);
+        }
+    }
     return p.threads == 512 ? block_backward_as<T, R, true, kIn, kBias, kV, 512>(a, p, st) : block_backward_as<T, R, true, kIn, kBias, kV, 256>(a, p, st);
 }
 template <typename T, typename R, int kIn>

@@ -241,6 +241,49 @@ def test_norm(i):
     check_backward(p)
 
 
+# Widths on both sides of what one warp, one group of columns a thread, a block and a cluster hold; few rows.
+@pytest.mark.parametrize("C", [264, 333, 2056, 4096, 4360, 8192])
+@pytest.mark.parametrize("kind", ["layer", "rms"])
+@pytest.mark.parametrize("gate", ["none", "token", "item"])
+@pytest.mark.parametrize("bias", [True, False])
+@pytest.mark.parametrize("types", [("bf16", None), ("f16", "f32"), ("f32", None)], ids=str)
+def test_every_form_of_backward(C, kind, gate, bias, types):
+    p = Problem(2, 5, C, dtype=types[0], res=types[1], kind=kind, gate=gate, gate_kind="sigmoid", bias=bias, alpha=0.7, seed=C + 1)
+    check_forward(p)
+    check_backward(p)
+    if gate == "none":
+        p = Problem(2, 5, C, dtype=types[0], res=types[1], kind=kind, bias=bias, seed=C + 2, branch=False)
+        check_backward(p)
+
+
+@pytest.mark.parametrize("first", [0, 1, 2, 3, 5, 7])
+@pytest.mark.parametrize("C,extra", [(40, 0), (40, 3), (333, 0), (333, 2), (1001, 5)])
+@pytest.mark.parametrize("types", [("bf16", None), ("f16", "f32"), ("f32", None)], ids=str)
+def test_rows_off_boundaries(first, C, extra, types):
+    """Tensors that begin at the `first` element of their memory and end with it, rows C + extra apart; what lies between is NaN."""
+    p = Problem(2, 9, C, dtype=types[0], res=types[1], gate="token", gate_kind="sigmoid", seed=C + first)
+
+    def moved(t, k):
+        ld, rows = C + extra, t.shape[0] * t.shape[1]
+        memory = torch.full((k + (rows - 1) * ld + C,), float("nan"), device="cuda", dtype=t.dtype)
+        v = memory.as_strided(t.shape, (t.shape[1] * ld, ld, 1), k)
+        return v.copy_(t)
+
+    for i, name in enumerate(("x", "o", "g", "dy", "dh")):
+        setattr(p, name, moved(getattr(p, name), (first + i) % 8 if first else 0))
+    check_forward(p)
+    check_backward(p)
+    # outputs off boundaries: what lies between rows is not touched
+    y, h, stats = p.forward()
+    out_y, out_h = moved(y, first), moved(h, first)
+    y2, h2, _ = p.forward(out=(out_y, out_h, None))
+    assert torch.equal(y2, y) or C % 8 == 0                 # (40 columns on boundaries run by another form)
+    close(y2, y.double(), "y")
+    if extra:
+        gaps = out_y.as_strided((17, extra), (C + extra, 1), out_y.storage_offset() + C)
+        assert gaps.isnan().all()
+
+
 @pytest.mark.parametrize("kind", ["layer", "rms"])
 @pytest.mark.parametrize("gate,gate_kind", [("token", "sigmoid"), ("item", "linear")])
 def test_gradients_against_differences(kind, gate, gate_kind):

@@ -723,6 +723,9 @@ __device__ __forceinline__ void orth_results_of(OrthPipe &q, const OrthProduct &
 // Tensor memory adds with truncation, which over K = 4096 (768 additions of 16 products) is off by 2e-5 of a sum of equal signs, and by 9e-5 of the
 // 2-norm of the whole result: sums stay there for kOrthChunk steps (K = 512) and are added up in registers, rounded, while the next
 // ones run in a second set of columns: 1e-5.  (The same second set lets a tile's results go out under the next tile's products.)
+// 256 x 256 x 64 of two halves each is 64 KB a block and stage, three stages; a pair reads half of what two blocks of 128 x 256 would.  Bound by the tensor
+// pipe: an update of 2 x 4096 x 4096 (2.75 TFLOP, three products of each) takes 6.9 ms, 1200 TFLOP/s, the pipe 91 to 97 % busy, the clock under the
+// power limit.
 struct OrthPairArgs {
     OrthProduct p;
     OrthOuter o;                 // kOrthLast
@@ -764,9 +767,10 @@ orth_pair_kernel(const __grid_constant__ CUtensorMap ta, const __grid_constant__
 //
 // A launch per product costs some 8 us beside its work (138 us for 130 x 130, whose products take 20).  Here the blocks stay, one an SM, and
 // the blocks of a team wait for one another between products: a counter in memory, some 2 us, or, where a cluster is team enough, its barrier.  Tiles are
-// 128 x 128 (a cluster's also 128 x 64), a block each; where a
-// product has fewer tiles than the team blocks, ks blocks share a tile's K: each leaves its sums in memory (they stay in L2), and when all of a tile's
-// have arrived, each finishes its part of the tile's columns.
+// 128 x 128 (a cluster's also 128 x 64), a block each; where a product has fewer tiles than the team blocks, ks blocks share a tile's K: each leaves
+// its sums in memory (they stay in L2), and when all of a tile's have arrived, each finishes its part of the tile's columns.  Bound by how 15 products
+// follow one another: 1003 x 2601 takes 270 us, 17 us a product, of which a third multiplies (the tensor pipe is 27 % busy), the rest stores and joins
+// partial sums (10000 cycles) and waits for the team (5500); 256 x 256 in a cluster 82 us.
 struct OrthTeam {
     OrthOuter o;
     OrthProduct product[4];      // of each kind
@@ -968,7 +972,7 @@ __global__ void __launch_bounds__(kOrthThreads, 1) orth_team_kernel(const __grid
 // halves and below them as many in low ones, and behind them A, overwritten by B, in the same form.  The same bytes serve as rows of X
 // (sums along rows) and as the right factor of B X (sums over rows).  The MMAs have 128 rows whatever S is; what they read beyond a panel's
 // rows is what lies behind it, and its sums are not looked at.  Bound by how long the parts of a step follow one another: the MMAs read their
-// factors from shared memory (128 x 128 x 16: 95 cycles for 64 of arithmetic; as here with high and low rows side by side 110 for two of them), and every
+// factors from shared memory (8 of 256 x 16 take 19 us, 24 of 128 x 128 39 us, whatever else runs beside them; 128 x 128 x 16: 95 cycles for 64 of arithmetic; as here with high and low rows side by side 110 for two of them), and every
 // sum goes through tensor memory, registers and a split once a product.
 //
 // kNarrow (S up to 64): one MMA forms high high, high low and low high of X X^T at a time (rows and columns of both halves; the third part comes over from

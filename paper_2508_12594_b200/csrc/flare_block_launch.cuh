@@ -7,8 +7,8 @@
 
 namespace flare {
 
-// Threads of a block: 512 for rows that 256 with their groups of eight columns do not hold and that can be moved 16 bytes at a time, else 256.  What a
-// row has beyond that goes to further blocks of a cluster.
+// Threads of a block: 512 for rows that 256 with their groups of eight columns do not hold, else 256.  What a row has beyond that goes to further blocks
+// of a cluster.
 constexpr int kBlockMaxWidth = 16384;
 // Blocks per group of rows: together about as many as fill the chip once.
 struct BlockPlan {
@@ -18,7 +18,7 @@ struct BlockPlan {
 };
 inline BlockPlan block_plan(long rows, long group, int C, bool aligned, int sms, int vectors) {    // vectors: groups of eight columns a thread owns
     BlockPlan p;
-    p.threads = aligned && C > 2048 * vectors ? 512 : 256;
+    p.threads = C > 2048 * vectors ? 512 : 256;
     p.tpr = aligned ? 4 : 32;                               // (columns that are moved one at a time: a warp's lanes side by side)
     while (p.tpr * 8 * vectors < C && p.tpr < p.threads) p.tpr *= 2;
     p.cluster = 1;
@@ -80,7 +80,7 @@ int block_forward_of(const BlockArgs &a, bool aligned, int sms, cudaStream_t st)
     constexpr int kV = sizeof(T) == 2 ? 2 : 1;              // (float32: its loads fill shared memory with one group of columns a thread)
     const BlockPlan p = block_plan(a.rows, a.group, a.C, aligned, sms, aligned ? kV : 1);
     // (rows that are moved one element at a time: always the form with biases, here and in the backward)
-    if (!aligned) return block_forward_as<T, R, false, kIn, true, 1, 256>(a, p, st);
+    if (!aligned) return p.threads == 512 ? block_forward_as<T, R, false, kIn, true, 1, 512>(a, p, st) : block_forward_as<T, R, false, kIn, true, 1, 256>(a, p, st);
     return a.b_post || a.b_pre ? block_forward_aligned<T, R, kIn, true, kV>(a, p, st) : block_forward_aligned<T, R, kIn, false, kV>(a, p, st);
 }
 template <typename T, typename R>
@@ -125,7 +125,7 @@ int block_backward_aligned(const BlockArgs &a, const BlockPlan &p, cudaStream_t 
 }
 template <typename T, typename R, int kIn>
 int block_backward_of(const BlockArgs &a, bool aligned, bool bias, const BlockPlan &p, cudaStream_t st) {
-    if (!aligned) return block_backward_as<T, R, false, kIn, true, 1, 256>(a, p, st);
+    if (!aligned) return p.threads == 512 ? block_backward_as<T, R, false, kIn, true, 1, 512>(a, p, st) : block_backward_as<T, R, false, kIn, true, 1, 256>(a, p, st);
     return bias ? block_backward_aligned<T, R, kIn, true>(a, p, st) : block_backward_aligned<T, R, kIn, false>(a, p, st);
 }
 template <typename T, typename R>

@@ -769,7 +769,7 @@ orth_pair_kernel(const __grid_constant__ CUtensorMap ta, const __grid_constant__
 // the blocks of a team wait for one another between products: a counter in memory, some 2 us, or, where a cluster is team enough, its barrier.  Tiles are
 // 128 x 128 (a cluster's also 128 x 64), a block each; where a product has fewer tiles than the team blocks, ks blocks share a tile's K: each leaves
 // its sums in memory (they stay in L2), and when all of a tile's have arrived, each finishes its part of the tile's columns.  Bound by how 15 products
-// follow one another: 1003 x 2601 takes 270 us, 17 us a product, of which a third multiplies (the tensor pipe is 27 % busy), the rest stores and joins
+// follow one another: 1003 x 2601 takes 276 us, 17 us a product, of which a third multiplies (the tensor pipe is 27 % busy), the rest stores and joins
 // partial sums (10000 cycles) and waits for the team (5500); 256 x 256 in a cluster 82 us.
 struct OrthTeam {
     OrthOuter o;

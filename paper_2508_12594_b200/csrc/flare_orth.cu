@@ -426,4 +426,21 @@ int flare_muon_update(const flare_orth_desc_t *desc, const flare_muon_t *rule, c
     return run_orth(desc, sc, o, workspace, reinterpret_cast<cudaStream_t>(stream));
 }
 
+int flare_selftest_team(void *workspace, int32_t gone, uint64_t budget_ns, flare_stream_t stream) {
+    if (!workspace || !aligned16(workspace) || gone < 0 || gone > 2) return FLARE_ERR_INVALID_ARG;
+    if (int rc = need_device()) return rc;
+    budget_ns = std::min<uint64_t>(std::max<uint64_t>(budget_ns, 1000), 100000000ull);   // never more than a tenth of a second
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    uint32_t *words = static_cast<uint32_t *>(workspace);
+    FLARE_CUDA(cudaMemsetAsync(workspace, 0, 2 * kHeaderBytes, st));
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeCooperative;
+    attr.val.cooperative = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(2); cfg.blockDim = kOrthThreads; cfg.stream = st;
+    cfg.attrs = &attr; cfg.numAttrs = 1;
+    FLARE_CUDA(cudaLaunchKernelEx(&cfg, selftest_team_kernel, words, words + kHeaderBytes / 4, words + kHeaderBytes / 4 + 1, (int)gone, budget_ns));
+    return FLARE_OK;
+}
+
 }  // extern "C"

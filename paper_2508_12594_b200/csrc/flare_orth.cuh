@@ -787,7 +787,7 @@ struct OrthTeam {
 struct OrthMaps { HalfMaps m[4]; };   // of mem
 
 // Waits (up to two seconds, or until some block has given up) for a counter to reach `target`.  One thread.
-__device__ __forceinline__ bool wait_count(const uint32_t *counter, uint32_t target, uint32_t *status) {
+__device__ __forceinline__ bool wait_count(const uint32_t *counter, uint32_t target, uint32_t *status, uint64_t budget_ns = ptx::kWaitBudgetNs) {
     const uint64_t t0 = ptx::globaltimer_ns();
     for (uint32_t spins = 1;; ++spins) {
         uint32_t v;
@@ -796,7 +796,7 @@ __device__ __forceinline__ bool wait_count(const uint32_t *counter, uint32_t tar
         if ((spins & 63u) == 0) {
             asm volatile("ld.relaxed.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(status) : "memory");
             if (v != 0) return false;
-            if (ptx::globaltimer_ns() - t0 > ptx::kWaitBudgetNs) {
+            if (ptx::globaltimer_ns() - t0 > budget_ns) {
                 atomicExch(status, 105u);
                 return false;
             }
@@ -807,16 +807,24 @@ __device__ __forceinline__ void add_count(uint32_t *counter) { asm volatile("red
 
 // All blocks of the team have got here, and what they stored is seen by all.  All threads of the block; the same in all of
 // them: false if some wait has given up.
-__device__ __forceinline__ bool team_meet(const OrthTeam &p, const OrthPipe &q, int team, uint32_t &target) {
-    target += p.team;
-    const bool sound = __syncthreads_and(*q.abort_flag == 0) != 0;
+__device__ __forceinline__ bool team_meet(uint32_t *counter, int members, volatile uint32_t *abort_flag, uint32_t *status, uint32_t &target,
+                                          uint64_t budget_ns = ptx::kWaitBudgetNs) {
+    target += members;
+    const bool sound = __syncthreads_and(*abort_flag == 0) != 0;
     bool ok = true;
     if (threadIdx.x == 0) {                                  // (one thread's release and acquire cover what the barriers around them order)
-        if (!sound) atomicExch(p.status, *q.abort_flag);
-        add_count(p.counters + team);
-        ok = wait_count(p.counters + team, target, p.status) && sound;
+        if (!sound) atomicExch(status, *abort_flag);
+        add_count(counter);
+        ok = wait_count(counter, target, status, budget_ns) && sound;
     }
     return __syncthreads_and(ok) != 0;
+}
+// The eight result warps at one barrier: whether all of them have their sums, the same in all of their threads.  A warp whose wait gave up comes here
+// too: the others, whose phase may have ended in that very moment, would wait for it without a limit.
+__device__ __forceinline__ bool results_agree(bool ok) {
+    uint32_t all;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbar.red.and.pred q, 1, 256, p;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(all) : "r"((uint32_t)ok) : "memory");
+    return all != 0;
 }
 
 // The result warps' part where ks blocks share a tile's K, once this block's sums are in memory: when all of the tile's are, its share of the tile's
@@ -906,11 +914,13 @@ __device__ __forceinline__ void team_product(const OrthTeam &p, OrthPipe &q, int
             float v[64];
             const bool mine = half * 64 < d.width;
             const int row0 = x.i * 128 + quad * 32, col0 = mine ? x.j * d.width + half * 64 : d.N;
-            if (!orth_sums<1>(q, chunks, v, mine)) break;
+            const bool only = (kCluster || ks == 1) && d.tiles <= p.team;    // (this block's one tile)
+            bool ok = orth_sums<1>(q, chunks, v, mine);
+            if (only) ok = results_agree(ok);                                // (everybody's sums are complete, so no stage is in use)
+            if (!ok) break;
             if (kCluster || ks == 1) {
                 const bool mirror = d.upper && x.i != x.j;
-                if (d.tiles <= p.team) {
-                    asm volatile("bar.sync 1, 256;" ::: "memory");           // (everybody's sums are complete, so no stage is in use)
+                if (only) {
                     orth_finish<true, E>(q, d, p.o, kind, mat, row0, col0, mirror, &out->store, &out->store_t, v);
                 } else {
                     orth_finish<false, E>(q, d, p.o, kind, mat, row0, col0, mirror, &out->store, &out->store_t, v);
@@ -935,15 +945,20 @@ __device__ __forceinline__ void team_run(const OrthMaps &maps, const OrthTeam &p
     uint32_t met = 0;
     bool ok = true;
     int count = 0;                                           // steps this team has begun
-    for (int mat = team; mat < p.count && ok; mat += p.teams)
+    for (int mat = team; mat < p.count && (kCluster || ok); mat += p.teams)
         // three products a step, one piece of code for all
-        for (int i = 0; i < 3 * p.steps && ok; ++i) {
+        for (int i = 0; i < 3 * p.steps && (kCluster || ok); ++i) {
             const int step = i / 3, stage = i - 3 * step, cur = step & 1, kind = stage < 2 ? stage : step + 1 < p.steps ? kOrthApply : kOrthLast;
             const int left = stage == 0 ? cur : stage == 1 ? 2 : 3, right = stage == 1 ? 2 : cur, to = stage == 0 ? 2 : stage == 1 ? 3 : 1 - cur;
             count += stage == 0;
-            team_product<kCluster, kResults, E>(p, q, kind, team, mat, count, maps.m + left, maps.m + right, maps.m + to, p.mem[to]);
-            if constexpr (kCluster) ptx::cluster_meet();     // (blocks that gave up a wait come here too: their later waits end at once)
-            else if (kind != kOrthLast || mat + p.teams < p.count) ok = team_meet(p, q, team, met);
+            if (ok) team_product<kCluster, kResults, E>(p, q, kind, team, mat, count, maps.m + left, maps.m + right, maps.m + to, p.mem[to]);
+            if constexpr (kCluster) {
+                // (a block that gave up a wait, as a whole, does no further product, for its roles are no longer at the same stage, but meets the others)
+                ok = __syncthreads_and(ok && *q.abort_flag == 0) != 0;
+                ptx::cluster_meet();
+            } else if (kind != kOrthLast || mat + p.teams < p.count) {
+                ok = team_meet(p.counters + team, p.team, q.abort_flag, p.status, met);
+            }
         }
 }
 // kCluster: the team is a cluster, whose barrier takes a tenth of the time; else a cooperative launch.
@@ -965,6 +980,27 @@ __global__ void __launch_bounds__(kOrthThreads, 1) orth_team_kernel(const __grid
     }
     __syncwarp();
     orth_pipe_end<1>(q, p.status);
+}
+
+// How a team ends when its waits run out, on its own: two blocks as the team kernel has them, at the end of two products, of which in the first block one
+// result warp is said to have given up (gone = 1), or which wait for a third that is not there (gone = 2).  out: [2][12 warps], bit 0 that the warp
+// went on after results_agree (the first four warps: always), bit 1 that it went on after both meetings.
+__global__ void __launch_bounds__(kOrthThreads, 1) selftest_team_kernel(uint32_t *status, uint32_t *counter, uint32_t *out, int gone, uint64_t budget_ns) {
+    __shared__ volatile uint32_t abort_flag;
+    if (threadIdx.x == 0) abort_flag = 0;
+    __syncthreads();
+    const int warp = ptx::warp_index();
+    bool agreed = true;
+    if (warp >= 4) {
+        const bool lost = gone == 1 && blockIdx.x == 0 && warp == 7;
+        if (lost && (threadIdx.x & 31) == 0) abort_flag = 104;
+        __syncwarp();
+        agreed = results_agree(!lost);
+    }
+    uint32_t target = 0;
+    bool met = true;
+    for (int i = 0; i < 2 && met; ++i) met = team_meet(counter, gone == 2 ? 3 : 2, &abort_flag, status, target, budget_ns);
+    if ((threadIdx.x & 31) == 0) out[blockIdx.x * 12 + warp] = (agreed ? 1u : 0u) | (met ? 2u : 0u);
 }
 
 // ---------------------------------------------------------------- a whole matrix in one block

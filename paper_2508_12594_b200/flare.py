@@ -88,6 +88,7 @@ _SIGNATURES = {
     "flare_orthogonalize": (ctypes.c_int, [_op, _vp, _vp, _vp, _sz, _vp]),
     "flare_muon_update": (ctypes.c_int, [_op, ctypes.POINTER(FlareMuon)] + [_vp] * 6 + [_sz, _vp]),
     "flare_selftest_wait": (ctypes.c_int, [_vp, ctypes.c_uint64, _vp]),
+    "flare_selftest_team": (ctypes.c_int, [_vp, ctypes.c_int32, ctypes.c_uint64, _vp]),
 }
 
 
@@ -238,6 +239,10 @@ def flare_launch_count(desc: FlareDesc, op: int) -> int:
 
 def flare_selftest_wait(workspace, budget_ns: int, stream=None):
     _raise(load().flare_selftest_wait(_ptr(workspace, torch.uint8), int(budget_ns), _stream(stream)), "flare_selftest_wait")
+
+
+def flare_selftest_team(workspace, gone: int, budget_ns: int, stream=None):
+    _raise(load().flare_selftest_team(_ptr(workspace, torch.uint8), int(gone), int(budget_ns), _stream(stream)), "flare_selftest_team")
 
 
 def flare_variant_workspace_bytes(desc, op, shared_latents, separate) -> int:

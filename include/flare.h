@@ -396,7 +396,7 @@ int flare_selftest_wait(void *workspace, uint64_t budget_ns, flare_stream_t stre
  * 1 = a warp of the first gives up its wait just before the block's warps agree on what follows; 2 = they wait for a third block that does not
  * exist, for `budget_ns` (clamped as above).  With 1 and 2 no block gets past both meetings and flare_check(workspace) reports FLARE_ERR_TIMEOUT.
  * Word 65 + i of the workspace (at least 512 bytes), i < 24, is what warp i % 12 of block i / 12 saw: bit 0 its block's result warps agreed to go on,
- * bit 1 the blocks met twice.
+ * bit 1 the blocks met twice; words 89 and 90 the nanoseconds that either block, before it ended, gave what it had in flight.
  */
 int flare_selftest_team(void *workspace, int32_t gone, uint64_t budget_ns, flare_stream_t stream);
 

@@ -473,10 +473,17 @@ __device__ __forceinline__ OrthPipe orth_pipe(uint8_t *raw, uint32_t *tmem_slot,
     q.tmem = *tmem_slot;
     return q;
 }
+// What a block that gave up a wait has asked for, copies into its shared memory and products into its tensor memory, may still be on its way, and
+// which of its barriers would say so is not known then: it is given a millisecond, some hundred times what it takes, before the block ends.
+__device__ __forceinline__ void let_arrive(volatile uint32_t *abort_flag) {
+    if (*abort_flag == 0) return;
+    for (const uint64_t t0 = ptx::globaltimer_ns(); ptx::globaltimer_ns() - t0 < 1000000ull;) __nanosleep(2000);
+}
 template <int kPair>
 __device__ __forceinline__ void orth_pipe_end(const OrthPipe &q, uint32_t *status) {
     ptx::tc_fence_before();
     __syncthreads();
+    let_arrive(q.abort_flag);
     if (kPair == 2) ptx::cluster_meet();                                 // (nobody's shared or tensor memory is needed any more)
     if (threadIdx.x == 0 && *q.abort_flag != 0) *status = *q.abort_flag;
     if (ptx::warp_index() == 1) {
@@ -984,7 +991,7 @@ __global__ void __launch_bounds__(kOrthThreads, 1) orth_team_kernel(const __grid
 
 // How a team ends when its waits run out, on its own: two blocks as the team kernel has them, at the end of two products, of which in the first block one
 // result warp is said to have given up (gone = 1), or which wait for a third that is not there (gone = 2).  out: [2][12 warps], bit 0 that the warp
-// went on after results_agree (the first four warps: always), bit 1 that it went on after both meetings.
+// went on after results_agree (the first four warps: always), bit 1 that it went on after both meetings; then [2] nanoseconds that what is in flight was given.
 __global__ void __launch_bounds__(kOrthThreads, 1) selftest_team_kernel(uint32_t *status, uint32_t *counter, uint32_t *out, int gone, uint64_t budget_ns) {
     __shared__ volatile uint32_t abort_flag;
     if (threadIdx.x == 0) abort_flag = 0;
@@ -1000,6 +1007,9 @@ __global__ void __launch_bounds__(kOrthThreads, 1) selftest_team_kernel(uint32_t
     uint32_t target = 0;
     bool met = true;
     for (int i = 0; i < 2 && met; ++i) met = team_meet(counter, gone == 2 ? 3 : 2, &abort_flag, status, target, budget_ns);
+    const uint64_t t0 = ptx::globaltimer_ns();
+    let_arrive(&abort_flag);
+    if (threadIdx.x == 0) out[24 + blockIdx.x] = (uint32_t)(ptx::globaltimer_ns() - t0);
     if ((threadIdx.x & 31) == 0) out[blockIdx.x * 12 + warp] = (agreed ? 1u : 0u) | (met ? 2u : 0u);
 }
 
@@ -1303,6 +1313,7 @@ __global__ void __launch_bounds__(kOrthSmallThreads, 1) orth_small_kernel(const 
     });
     ptx::tc_fence_before();
     __syncthreads();
+    let_arrive(&abort_flag);
     if (threadIdx.x == 0 && abort_flag != 0) p.status[0] = abort_flag;
     if (warp == 0) {
         ptx::tc_fence_after();

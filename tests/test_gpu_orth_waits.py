@@ -11,18 +11,21 @@ def _run(gone):
     ws = torch.full((512,), 255, dtype=torch.uint8, device="cuda")
     flare.flare_selftest_team(ws, gone, 1_000_000)               # one millisecond
     torch.cuda.synchronize()
-    return ws, ws.view(torch.int32)[65:65 + 24].view(2, 12).tolist()
+    words = ws.view(torch.int32)
+    return ws, words[65:65 + 24].view(2, 12).tolist(), words[89:91].tolist()
 
 
 def test_blocks_that_all_come_go_on():
-    ws, saw = _run(0)
+    ws, saw, waited = _run(0)
+    assert max(waited) < 500_000
     flare.flare_check(ws)
     assert saw == [[3] * 12] * 2
 
 
 def test_a_warp_that_gave_up_takes_the_others_with_it():
     """Its block's result warps agree not to go on instead of waiting for it; the block leaves at the first meeting, the other one at the second."""
-    ws, saw = _run(1)
+    ws, saw, waited = _run(1)
+    assert waited[0] >= 1_000_000                                # for what it might have had in flight
     assert saw == [[1] * 4 + [0] * 8, [1] * 12]
     with pytest.raises(flare.FlareError) as e:
         flare.flare_check(ws)
@@ -30,7 +33,7 @@ def test_a_warp_that_gave_up_takes_the_others_with_it():
 
 
 def test_a_block_that_never_comes():
-    ws, saw = _run(2)
+    ws, saw, _ = _run(2)
     assert saw == [[1] * 12] * 2
     with pytest.raises(flare.FlareError) as e:
         flare.flare_check(ws)

@@ -331,6 +331,19 @@ at::Tensor scratch(size_t bytes, const at::Tensor &like, PyObject *stream, flare
     return at::empty({(int64_t)bytes}, like.options().dtype(at::kByte));
 }
 
+// What a call returns comes from its stream's memory as well: of the current stream's, what has just been given back may still be in use by work that is
+// queued there, and what the caller drops would be handed on with the call's kernels still writing.  The current stream is known to use it too: where a
+// result is dropped, its memory is not handed on before what that has queued by then is done.
+at::Tensor result(at::IntArrayRef shape, const at::TensorOptions &options, PyObject *stream, flare_stream_t st) {
+    if (stream == Py_None) return at::empty(shape, options);
+    const c10::cuda::CUDAStream current = c10::cuda::getCurrentCUDAStream(options.device().index());
+    if ((cudaStream_t)st == current.stream()) return at::empty(shape, options);
+    const c10::cuda::CUDAStreamGuard guard(c10::cuda::getStreamFromExternal((cudaStream_t)st, options.device().index()));
+    at::Tensor t = at::empty(shape, options);
+    t.record_stream(current);
+    return t;
+}
+
 // Q, K, V, key_mask, scale, want_stats, stream -> Y, or (Y, Z, lse_enc, lse_dec)
 BINDING(call_forward, 7)
     const at::Tensor &Q = tensor(a[0]), &K = tensor(a[1]);
@@ -489,15 +502,30 @@ int number_of(PyObject *o) {
     if (x == -1 && PyErr_Occurred()) throw PythonError{};
     return (int)x;
 }
-// Entry i of a tuple of output tensors (or None: allocate).
-at::Tensor output(PyObject *out, Py_ssize_t i, at::IntArrayRef shape, const at::TensorOptions &options) {
-    if (out != Py_None) {
+// The tensors to write to: a tuple with one, or None, for every result (or None), and where the others are allocated.
+struct Outputs {
+    PyObject *out, *stream;
+    flare_stream_t st;
+    at::Tensor given(Py_ssize_t i) const {
+        if (out == Py_None) return at::Tensor();
         if (!PyTuple_Check(out) || i >= PyTuple_GET_SIZE(out)) fail(PyExc_ValueError, "out: expected a tuple with a tensor, or None, for every result");
         PyObject *o = PyTuple_GET_ITEM(out, i);
-        if (o != Py_None) return tensor(o);
+        return o != Py_None ? tensor(o) : at::Tensor();
     }
-    return at::empty(shape, options);
-}
+    at::Tensor operator()(Py_ssize_t i, at::IntArrayRef shape, const at::TensorOptions &options) const {
+        const at::Tensor t = given(i);
+        return t.defined() ? t : result(shape, options, stream, st);
+    }
+    at::Tensor sums(const float *present, Py_ssize_t i, int64_t C, const at::TensorOptions &f32) const { return present ? (*this)(i, {C}, f32) : at::Tensor(); }
+    // statistics of the rows, where they are wanted
+    at::Tensor stats(PyObject *want, Py_ssize_t i, int64_t rows, const at::TensorOptions &f32) const {
+        const int yes = PyObject_IsTrue(want);
+        if (yes < 0) throw PythonError{};
+        if (yes) return (*this)(i, {rows, 4}, f32);
+        if (given(i).defined()) fail(PyExc_ValueError, "stats: a tensor to write to, but want_stats is false");
+        return at::Tensor();
+    }
+};
 PyObject *wrap(const at::Tensor &t) {
     if (!t.defined()) Py_RETURN_NONE;
     return THPVariable_Wrap(t);
@@ -564,23 +592,21 @@ struct Around {
         return r;
     }
     float *stats(const at::Tensor &t) const {
+        if (!t.defined()) return nullptr;
         check(t, at::kFloat, {d.rows, 4});
         return (float *)t.data_ptr();
     }
     at::TensorOptions as(at::ScalarType t) const { return options.dtype(t); }
 };
 
-at::Tensor sums_output(const float *present, PyObject *out, Py_ssize_t i, int64_t C, const at::TensorOptions &f32) {
-    return present ? output(out, i, {C}, f32) : at::Tensor();
-}
 float *sums_ptr(const at::Tensor &t, int64_t C) {
     if (!t.defined()) return nullptr;
     check(t, at::kFloat, {C});
     return (float *)t.data_ptr();
 }
 
-// x, norm, dtype or None, out (h, stats) or None, stream -> (h, stats)
-BINDING(block_norm, 5)
+// x, norm, dtype or None, whether statistics are wanted, out (h, stats) or None, stream -> (h, stats)
+BINDING(block_norm, 6)
     const at::Tensor &x = tensor(a[0]);
     if (a[2] != Py_None && !THPDtype_Check(a[2])) fail(PyExc_TypeError, "dtype: expected a torch dtype");
     Around c(x, a[2] == Py_None ? x.scalar_type() : ((THPDtype *)a[2])->scalar_type);
@@ -588,10 +614,11 @@ BINDING(block_norm, 5)
     c.d.pre_norm = n.kind;
     c.d.pre_eps = n.eps;
     const Rows rx = c.rows(x, c.d.stride_x, "x", c.res);
-    const at::Tensor h = output(a[3], 0, c.shape, c.as(c.dt)), stats = output(a[3], 1, {c.d.rows, 4}, c.as(at::kFloat));
+    flare_stream_t st = stream_of(a[5]);
+    const Outputs output{a[4], a[5], st};
+    const at::Tensor h = output(0, c.shape, c.as(c.dt)), stats = output.stats(a[3], 1, c.d.rows, c.as(at::kFloat));
     const Rows rh = c.rows(h, c.d.stride_h, "h", c.dt);
     float *ps = c.stats(stats);
-    flare_stream_t st = stream_of(a[4]);
     check_status(unlocked([&] { return lib.norm_forward(&c.d, rx.p, n.weight, n.bias, rh.p, ps, st); }), "flare_norm_forward");
     return wrap_all({h, stats});
 BINDING_END
@@ -606,10 +633,11 @@ BINDING(block_norm_backward, 8)
     const Rows rx = c.rows(x, c.d.stride_x, "x", c.res), rdh = c.rows(dh, c.d.stride_dh, "dh", c.dt), rdy = c.rows(a[3], c.res, c.d.stride_dy, "dy");
     const float *ps = c.stats(tensor(a[1]));
     const auto f32 = c.as(at::kFloat);
-    const at::Tensor dx = output(a[5], 0, c.shape, c.as(c.res)), dw = sums_output(n.weight, a[5], 1, c.C, f32), db = sums_output(n.bias, a[5], 2, c.C, f32);
+    flare_stream_t st = stream_of(a[6]);
+    const Outputs output{a[5], a[6], st};
+    const at::Tensor dx = output(0, c.shape, c.as(c.res)), dw = output.sums(n.weight, 1, c.C, f32), db = output.sums(n.bias, 2, c.C, f32);
     const Rows rdx = c.rows(dx, c.d.stride_dx, "dx", c.res);
     float *pw = sums_ptr(dw, c.C), *pb = sums_ptr(db, c.C);
-    flare_stream_t st = stream_of(a[6]);
     const size_t need = lib.block_workspace_bytes(&c.d);
     if (need == 0) check_status(FLARE_ERR_UNSUPPORTED, "flare_norm_backward");
     const at::Tensor ws = scratch(need, x, a[6], st);
@@ -617,8 +645,8 @@ BINDING(block_norm_backward, 8)
     return named(a[7], wrap_all({dx, dw, db}));
 BINDING_END
 
-// x, branch, post, pre, gate, gate kind, scale, residual scale, out (y, h, stats) or None, stream -> (y, h, stats)
-BINDING(block_join, 10)
+// x, branch, post, pre, gate, gate kind, scale, residual scale, whether statistics are wanted, out (y, h, stats) or None, stream -> (y, h, stats)
+BINDING(block_join, 11)
     const at::Tensor &x = tensor(a[0]), &o = tensor(a[1]);
     Around c(x, o);
     const NormArg post(a[2], c.C, "post weight", "post bias"), pre(a[3], c.C, "pre weight", "pre bias");
@@ -628,11 +656,12 @@ BINDING(block_join, 10)
     const float *s = row_param(a[6], c.C, "scale");
     const Rows rx = c.rows(x, c.d.stride_x, "x", c.res), ro = c.rows(o, c.d.stride_branch, "branch", c.dt), rg = c.gate(a[4], gate_kind_of(a[4], a[5]));
     const bool next = pre.kind != FLARE_NORM_NONE;
-    const at::Tensor y = output(a[8], 0, c.shape, c.as(c.res)), h = next ? output(a[8], 1, c.shape, c.as(c.dt)) : at::Tensor(),
-                     stats = output(a[8], 2, {c.d.rows, 4}, c.as(at::kFloat));
+    flare_stream_t st = stream_of(a[10]);
+    const Outputs output{a[9], a[10], st};
+    const at::Tensor y = output(0, c.shape, c.as(c.res)), h = next ? output(1, c.shape, c.as(c.dt)) : at::Tensor(),
+                     stats = output.stats(a[8], 2, c.d.rows, c.as(at::kFloat));
     const Rows ry = c.rows(y, c.d.stride_y, "y", c.res), rh = next ? c.rows(h, c.d.stride_h, "h", c.dt) : Rows{};
     float *ps = c.stats(stats);
-    flare_stream_t st = stream_of(a[9]);
     check_status(unlocked([&] { return lib.join_forward(&c.d, rx.p, ro.p, rg.p, s, post.weight, post.bias, pre.weight, pre.bias, ry.p, rh.p, ps, st); }),
                  "flare_join_forward");
     return wrap_all({y, h, stats});
@@ -652,11 +681,12 @@ BINDING(block_join_backward, 14)
                rdh = c.rows(a[4], c.dt, c.d.stride_dh, "dh"), rg = c.gate(a[7], gate_kind_of(a[7], a[8]));
     const float *ps = c.stats(tensor(a[2]));
     const auto f32 = c.as(at::kFloat);
-    PyObject *out = a[11];
-    const at::Tensor dx = output(out, 0, c.shape, c.as(c.res)), d_o = output(out, 1, c.shape, c.as(c.dt));
-    const at::Tensor dg = a[7] != Py_None ? output(out, 2, c.gate_shape, c.as(c.dt)) : at::Tensor();
-    const at::Tensor ds = sums_output(s, out, 3, c.C, f32), dwo = sums_output(post.weight, out, 4, c.C, f32), dbo = sums_output(post.bias, out, 5, c.C, f32),
-                     dwy = sums_output(pre.weight, out, 6, c.C, f32), dby = sums_output(pre.bias, out, 7, c.C, f32);
+    flare_stream_t st = stream_of(a[12]);
+    const Outputs output{a[11], a[12], st};
+    const at::Tensor dx = output(0, c.shape, c.as(c.res)), d_o = output(1, c.shape, c.as(c.dt));
+    const at::Tensor dg = a[7] != Py_None ? output(2, c.gate_shape, c.as(c.dt)) : at::Tensor();
+    const at::Tensor ds = output.sums(s, 3, c.C, f32), dwo = output.sums(post.weight, 4, c.C, f32), dbo = output.sums(post.bias, 5, c.C, f32),
+                     dwy = output.sums(pre.weight, 6, c.C, f32), dby = output.sums(pre.bias, 7, c.C, f32);
     const Rows rdx = c.rows(dx, c.d.stride_dx, "dx", c.res), rdo = c.rows(d_o, c.d.stride_dbranch, "dbranch", c.dt);
     Rows rdg;
     if (dg.defined()) {
@@ -664,7 +694,6 @@ BINDING(block_join_backward, 14)
         c.d.stride_dgate = rdg.stride;
     }
     float *p3 = sums_ptr(ds, c.C), *p4 = sums_ptr(dwo, c.C), *p5 = sums_ptr(dbo, c.C), *p6 = sums_ptr(dwy, c.C), *p7 = sums_ptr(dby, c.C);
-    flare_stream_t st = stream_of(a[12]);
     const size_t need = lib.block_workspace_bytes(&c.d);
     if (need == 0) check_status(FLARE_ERR_UNSUPPORTED, "flare_join_backward");
     const at::Tensor ws = scratch(need, y, a[12], st);
@@ -725,9 +754,9 @@ BINDING(orthogonalize, 8)
     const at::Tensor &G = tensor(a[0]);
     Matrices c(G, a[1], a[2], a[3], a[4], a[5]);
     void *g = c.strided(G, G.scalar_type(), "G", c.d.stride_row, c.d.stride_matrix);
-    const at::Tensor O = a[6] == Py_None ? at::empty(c.shape, G.options()) : tensor(a[6]);
-    void *o = c.strided(O, G.scalar_type(), "out", c.d.out_stride_row, c.d.out_stride_matrix);
     flare_stream_t st = stream_of(a[7]);
+    const at::Tensor O = a[6] == Py_None ? result(c.shape, G.options(), a[7], st) : tensor(a[6]);
+    void *o = c.strided(O, G.scalar_type(), "out", c.d.out_stride_row, c.d.out_stride_matrix);
     const size_t need = c.need("flare_orthogonalize");
     const at::Tensor ws = scratch(need, G, a[7], st);
     check_status(unlocked([&] { return lib.orthogonalize(&c.d, g, o, ws.data_ptr(), need, st); }), "flare_orthogonalize");

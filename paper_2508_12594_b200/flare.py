@@ -326,10 +326,11 @@ class JoinGrads(NamedTuple):
     dpre_bias: Optional[torch.Tensor]
 
 
-def block_norm(x, norm: Norm, dtype=None, out=None, stream=None):
-    """The norm before a block.  x [..., width] -> (h [..., width] of `dtype` (x's), stats [rows, 4] float32).
-    out: (h, stats) to write to, either None."""
-    return (_native or _bind()).block_norm(x, norm, dtype, out, stream)
+def block_norm(x, norm: Norm, dtype=None, out=None, stream=None, want_stats=True):
+    """The norm before a block.  x [..., width] -> (h [..., width] of `dtype` (x's), stats [rows, 4] float32, None
+    without want_stats).  out: (h, stats) to write to, either None.  Results that are allocated here, and in the calls below, come
+    from the memory of `stream`."""
+    return (_native or _bind()).block_norm(x, norm, dtype, want_stats, out, stream)
 
 
 def block_norm_backward(x, stats, dh, norm: Norm, dy=None, out=None, stream=None) -> NormGrads:
@@ -339,13 +340,13 @@ def block_norm_backward(x, stats, dh, norm: Norm, dy=None, out=None, stream=None
 
 
 def block_join(x, branch, post: Optional[Norm] = None, pre: Optional[Norm] = None, gate=None, gate_kind="sigmoid", scale=None,
-               residual_scale=1.0, out=None, stream=None):
+               residual_scale=1.0, out=None, stream=None, want_stats=True):
     """What follows a block, and the norm before the next one:
-    y = residual_scale * x + scale * act(gate) * post(branch);  h = pre(y).  Returns (y, h or None, stats [rows, 4]).
+    y = residual_scale * x + scale * act(gate) * post(branch);  h = pre(y).  Returns (y, h or None, stats [rows, 4], or None without want_stats).
 
     x, branch [..., width]; gate like the branch, or with fewer of its leading dimensions (one row per batch item, say);
     gate_kind "sigmoid" or "linear"; scale float32 [width].  out: (y, h, stats) to write to, any None."""
-    return (_native or _bind()).block_join(x, branch, post, pre, gate, gate_kind, scale, residual_scale, out, stream)
+    return (_native or _bind()).block_join(x, branch, post, pre, gate, gate_kind, scale, residual_scale, want_stats, out, stream)
 
 
 def block_join_backward(branch, y, stats, dy, dh, post: Optional[Norm] = None, pre: Optional[Norm] = None, gate=None, gate_kind="sigmoid",

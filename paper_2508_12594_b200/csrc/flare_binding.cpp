@@ -354,10 +354,10 @@ BINDING(call_forward, 7)
     const bool stats = PyObject_IsTrue(a[5]) == 1;
     flare_stream_t st = stream_of(a[6]);
     const size_t ws = workspace_bytes(d, FLARE_OP_FORWARD);
-    const at::Tensor Y = at::empty({d.B, d.N, d.H, d.D}, K.options());
+    const at::Tensor Y = result({d.B, d.N, d.H, d.D}, K.options(), a[6], st);
     const auto f32 = K.options().dtype(at::kFloat);
     if (stats) {
-        const at::Tensor Z = at::empty({d.B, d.H, d.M, d.D}, f32), le = at::empty({d.B, d.H, d.M}, f32), ld = at::empty({d.B, d.N, d.H}, f32);
+        const at::Tensor Z = result({d.B, d.H, d.M, d.D}, f32, a[6], st), le = result({d.B, d.H, d.M}, f32, a[6], st), ld = result({d.B, d.N, d.H}, f32, a[6], st);
         const at::Tensor w = scratch(ws, K, a[6], st);
         check_status(unlocked([&] { return lib.forward(&d, q, k, v, m, Y.data_ptr(), (float *)Z.data_ptr(), (float *)le.data_ptr(),
                                                        (float *)ld.data_ptr(), w.data_ptr(), ws, st); }), "flare_forward");
@@ -384,8 +384,8 @@ BINDING(call_forward_backward, 7)
     // backward has its own behind it.
     const size_t fwd_bytes = workspace_bytes(d, FLARE_OP_FORWARD), bwd_bytes = workspace_bytes(d, FLARE_OP_BACKWARD), bwd_at = 256;
     const size_t ws = std::max(fwd_bytes, bwd_at + bwd_bytes);
-    const at::Tensor Y = at::empty({d.B, d.N, d.H, d.D}, K.options()), dK = at::empty({d.B, d.N, d.H, d.D}, K.options());
-    const at::Tensor dV = at::empty({d.B, d.N, d.H, d.D}, K.options()), dQ = at::empty({d.H, d.M, d.D}, K.options().dtype(at::kFloat));
+    const at::Tensor Y = result({d.B, d.N, d.H, d.D}, K.options(), a[6], st), dK = result({d.B, d.N, d.H, d.D}, K.options(), a[6], st);
+    const at::Tensor dV = result({d.B, d.N, d.H, d.D}, K.options(), a[6], st), dQ = result({d.H, d.M, d.D}, K.options().dtype(at::kFloat), a[6], st);
     const size_t z_at = round256(ws), le_at = round256(z_at + 4 * (size_t)d.B * d.H * d.M * d.D), ld_at = round256(le_at + 4 * (size_t)d.B * d.H * d.M);
     const at::Tensor w = scratch(ld_at + 4 * (size_t)d.B * d.N * d.H, K, a[6], st);
     char *base = (char *)w.data_ptr();

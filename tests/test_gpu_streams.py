@@ -6,7 +6,8 @@ may still be used by work queued there, and what the caller drops may still be w
 import pytest
 import torch
 
-from paper_2508_12594_b200 import flare
+from paper_2508_12594_b200 import flare, workloads
+from tests._util import dev
 
 pytestmark = pytest.mark.gpu
 
@@ -24,16 +25,21 @@ def _inputs():
     s = randn(256, dtype=torch.float32)
     y, h, stats = flare.block_join(x, o, post=norm, pre=norm, gate=gate, scale=s)
     w = randn(3, 150, 300, dtype=torch.float32)
+    inp = workloads.make_random(1, 2, 3000, 64, 32, dtype="bf16", seed=3, with_dy=True)
+    Q, K, V, dY = dev(inp.Q), dev(inp.K), dev(inp.V), dev(inp.dY)
     return {
         "norm": lambda stream=None: flare.block_norm(x, norm, stream=stream),
         "norm backward": lambda stream=None: flare.block_norm_backward(y, stats, dh, norm, dy=dy, stream=stream),
         "join": lambda stream=None: flare.block_join(x, o, post=norm, pre=norm, gate=gate, scale=s, stream=stream),
         "join backward": lambda stream=None: flare.block_join_backward(o, y, stats, dy, dh, post=norm, pre=norm, gate=gate, scale=s, stream=stream),
         "orthogonalize": lambda stream=None: [flare.orthogonalize(w, stream=stream)],
+        "mixer": lambda stream=None: [flare.forward(Q, K, V, stream=stream)],
+        "mixer with statistics": lambda stream=None: flare.forward(Q, K, V, want_stats=True, stream=stream),
+        "mixer step": lambda stream=None: flare.forward_backward(Q, K, V, dY, stream=stream),
     }
 
 
-CALLS = ("norm", "norm backward", "join", "join backward", "orthogonalize")
+CALLS = ("norm", "norm backward", "join", "join backward", "orthogonalize", "mixer", "mixer with statistics", "mixer step")
 
 
 def _stream_of(t):

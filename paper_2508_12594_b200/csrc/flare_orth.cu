@@ -370,6 +370,12 @@ int need_device() {
     return di.checked == 1 ? FLARE_OK : FLARE_ERR_ARCH;
 }
 
+// No matrices: the header says that no wait gave up, whatever the workspace held.
+int clear_header(void *workspace, cudaStream_t st) {
+    FLARE_CUDA(launch_after(orth_clear_kernel, 1, 256, 0, st, static_cast<uint32_t *>(workspace), (int)(kHeaderBytes / sizeof(uint32_t))));
+    return FLARE_OK;
+}
+
 OrthOuter outer_of(const flare_orth_desc_t *d) {
     OrthOuter o{};
     o.rows = d->rows; o.cols = d->cols; o.g_type = d->dtype; o.eps = d->eps; o.tall = d->rows > d->cols;
@@ -398,7 +404,7 @@ int flare_orthogonalize(const flare_orth_desc_t *desc, const void *G, void *O, v
     if (!workspace || !aligned16(workspace) || (desc->count > 0 && (!G || !O)) || !natural(G, e) || !natural(O, e)) return FLARE_ERR_INVALID_ARG;
     if (int rc = need_device()) return rc;
     if (workspace_bytes < orth_layout(desc, orth_plan(desc, device_info().sms), device_info().sms).total) return FLARE_ERR_WORKSPACE_TOO_SMALL;
-    if (desc->count == 0) return FLARE_OK;
+    if (desc->count == 0) return clear_header(workspace, reinterpret_cast<cudaStream_t>(stream));
     OrthOuter o = outer_of(desc);
     o.g = G; o.out = O; o.out_type = desc->dtype;
     o.ld_out = desc->out_stride_row ? desc->out_stride_row : desc->cols;
@@ -417,7 +423,7 @@ int flare_muon_update(const flare_orth_desc_t *desc, const flare_muon_t *rule, c
     if (!natural(w, e) || !natural(w_out, e) || !natural(m, 4) || !natural(m_out, 4) || !natural(g, size_of(desc->dtype))) return FLARE_ERR_INVALID_ARG;
     if (int rc = need_device()) return rc;
     if (workspace_bytes < orth_layout(desc, orth_plan(desc, device_info().sms), device_info().sms).total) return FLARE_ERR_WORKSPACE_TOO_SMALL;
-    if (desc->count == 0) return FLARE_OK;
+    if (desc->count == 0) return clear_header(workspace, reinterpret_cast<cudaStream_t>(stream));
     OrthOuter o = outer_of(desc);
     o.g = g; o.w = w; o.out = w_out; o.out_type = desc->weight_dtype; o.m = m; o.m_out = m_out;
     o.ld_out = desc->cols; o.step_out = (long)desc->cols * desc->rows;

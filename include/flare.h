@@ -299,7 +299,7 @@ typedef struct {
     int64_t stride_x, stride_branch, stride_gate, stride_y, stride_h, stride_dy, stride_dh, stride_dx, stride_dbranch, stride_dgate;
 } flare_block_desc_t;
 
-/* Bytes of workspace either backward needs (0 for an invalid descriptor): one row of partial sums per thread block. */
+/* Bytes of workspace either backward needs (0 for an invalid descriptor, its gate among them): one row of partial sums per thread block. */
 size_t flare_block_workspace_bytes(const flare_block_desc_t *desc);
 
 /* The norm before the first block (pre_norm of the descriptor; post_norm, gate and residual_scale are not looked at). */

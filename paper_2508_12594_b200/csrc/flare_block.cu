@@ -130,7 +130,8 @@ extern "C" {
 
 size_t flare_block_workspace_bytes(const flare_block_desc_t *desc) {
     if (check_block(desc, true) != FLARE_OK) return 0;
-    return partial_bytes(desc, group_of(desc));
+    // (the norm's backward has one group of all rows whatever the descriptor's gate is, with more blocks to it than groups in all, it may be)
+    return std::max(partial_bytes(desc, group_of(desc)), partial_bytes(desc, std::max<long>(desc->rows, 1)));
 }
 
 int flare_norm_forward(const flare_block_desc_t *desc, const void *x, const float *weight, const float *bias, void *h, float *stats, flare_stream_t stream) {

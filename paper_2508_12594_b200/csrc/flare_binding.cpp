@@ -585,8 +585,8 @@ struct Around {
         for (size_t i = 0; i + 1 < gate_shape.size(); ++i) n *= gate_shape[i];
         const bool leads = !gate_shape.empty() && gate_shape.back() == C && gate_shape.size() <= shape.size() &&
                            std::equal(gate_shape.begin(), gate_shape.end() - 1, shape.begin());
-        if (!leads || (n == 0) != (d.rows == 0)) fail(PyExc_ValueError, "gate: expected [..., width] with the leading dimensions of the branch, or the first of them, got shape " + shape_text(gate_shape));
-        if (n > 0) d.gate_rows = d.rows / n;
+        if (!leads) fail(PyExc_ValueError, "gate: expected [..., width] with the leading dimensions of the branch, or the first of them, got shape " + shape_text(gate_shape));
+        if (d.rows > 0) d.gate_rows = d.rows / n;            // (no rows: there may be gate rows all the same, of items without any)
         const Rows r = rows_of(g, dt, gate_shape, "gate");
         d.stride_gate = r.stride;
         return r;
@@ -692,6 +692,11 @@ BINDING(block_join_backward, 14)
     if (dg.defined()) {
         rdg = rows_of(dg, c.dt, c.gate_shape, "dgate");
         c.d.stride_dgate = rdg.stride;
+        if (c.d.rows == 0 && dg.numel() > 0) {               // gate rows without rows: the library knows of none, and theirs are sums of nothing
+            c10::cuda::OptionalCUDAStreamGuard guard;
+            if (a[12] != Py_None) guard.reset_stream(c10::cuda::getStreamFromExternal((cudaStream_t)st, y.device().index()));
+            dg.zero_();
+        }
     }
     float *p3 = sums_ptr(ds, c.C), *p4 = sums_ptr(dwo, c.C), *p5 = sums_ptr(dbo, c.C), *p6 = sums_ptr(dwy, c.C), *p7 = sums_ptr(dby, c.C);
     const size_t need = lib.block_workspace_bytes(&c.d);

@@ -9,6 +9,23 @@ from paper_2508_12594_b200 import flare
 pytestmark = pytest.mark.gpu
 
 
+@pytest.mark.parametrize("kind", ["sigmoid", "linear"])
+def test_items_without_rows(kind):
+    """A gate row an item, and no rows: nothing comes out, and the sums over rows, the gate's gradient among them, are zeros."""
+    x = torch.empty(3, 0, 64, device="cuda", dtype=torch.bfloat16)
+    gate = torch.randn(3, 64, device="cuda").bfloat16()
+    w, s = torch.ones(64, device="cuda"), torch.ones(64, device="cuda")
+    norm = flare.Norm("rms", w)
+    y, h, stats = flare.block_join(x, x, post=norm, pre=norm, gate=gate, gate_kind=kind, scale=s)
+    assert y.shape == h.shape == x.shape and stats.shape == (0, 4)
+    for out in (None, torch.full((3, 80), 7.0, device="cuda", dtype=torch.bfloat16)):
+        r = flare.block_join_backward(x, y, stats, None, h, post=norm, pre=norm, gate=gate, gate_kind=kind, scale=s,
+                                      out=None if out is None else (None, None, out[:, :64]) + (None,) * 5)
+        assert r.dgate.shape == gate.shape and (r.dgate == 0).all()
+        assert all((g == 0).all() for g in (r.dscale, r.dpost_weight, r.dpre_weight))
+        assert out is None or (out[:, 64:] == 7).all()
+
+
 def test_norm_backward_with_the_workspace_of_a_gated_descriptor():
     """The gate of a descriptor is not looked at by the norm, so the size that the descriptor is told has to do for it too."""
     lib = flare.load()

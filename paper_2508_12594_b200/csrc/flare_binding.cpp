@@ -502,6 +502,22 @@ int number_of(PyObject *o) {
     if (x == -1 && PyErr_Occurred()) throw PythonError{};
     return (int)x;
 }
+PyObject *wrap(const at::Tensor &t) {
+    if (!t.defined()) Py_RETURN_NONE;
+    return THPVariable_Wrap(t);
+}
+PyObject *wrap_all(std::initializer_list<at::Tensor> ts) {
+    PyObject *r = PyTuple_New((Py_ssize_t)ts.size());
+    if (!r) throw PythonError{};
+    Py_ssize_t i = 0;
+    for (const at::Tensor &t : ts) PyTuple_SET_ITEM(r, i++, wrap(t));
+    return r;
+}
+
+// A tensor of the caller's that has been written: as after an operation in place, autograd tells a graph that still wants what it held.
+void mark_written(const at::Tensor &t) {
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
 // The tensors to write to: a tuple with one, or None, for every result (or None), and where the others are allocated.
 struct Outputs {
     PyObject *out, *stream;
@@ -516,6 +532,15 @@ struct Outputs {
         const at::Tensor t = given(i);
         return t.defined() ? t : result(shape, options, stream, st);
     }
+    // The call's results in the order of the tuple, once it has been made: those of them that were given have been written.
+    PyObject *wrapped(std::initializer_list<at::Tensor> results) const {
+        Py_ssize_t i = 0;
+        for (const at::Tensor &t : results) {
+            if (t.defined() && given(i).defined()) mark_written(t);
+            ++i;
+        }
+        return wrap_all(results);
+    }
     at::Tensor sums(const float *present, Py_ssize_t i, int64_t C, const at::TensorOptions &f32) const { return present ? (*this)(i, {C}, f32) : at::Tensor(); }
     // statistics of the rows, where they are wanted
     at::Tensor stats(PyObject *want, Py_ssize_t i, int64_t rows, const at::TensorOptions &f32) const {
@@ -526,17 +551,6 @@ struct Outputs {
         return at::Tensor();
     }
 };
-PyObject *wrap(const at::Tensor &t) {
-    if (!t.defined()) Py_RETURN_NONE;
-    return THPVariable_Wrap(t);
-}
-PyObject *wrap_all(std::initializer_list<at::Tensor> ts) {
-    PyObject *r = PyTuple_New((Py_ssize_t)ts.size());
-    if (!r) throw PythonError{};
-    Py_ssize_t i = 0;
-    for (const at::Tensor &t : ts) PyTuple_SET_ITEM(r, i++, wrap(t));
-    return r;
-}
 
 // What a call says about its rows: shape, types and norms.
 struct Around {
@@ -620,7 +634,7 @@ BINDING(block_norm, 6)
     const Rows rh = c.rows(h, c.d.stride_h, "h", c.dt);
     float *ps = c.stats(stats);
     check_status(unlocked([&] { return lib.norm_forward(&c.d, rx.p, n.weight, n.bias, rh.p, ps, st); }), "flare_norm_forward");
-    return wrap_all({h, stats});
+    return output.wrapped({h, stats});
 BINDING_END
 
 // x, stats, dh, dy, norm, out (dx, dweight, dbias) or None, stream, class of the result -> (dx, dweight, dbias)
@@ -642,7 +656,7 @@ BINDING(block_norm_backward, 8)
     if (need == 0) check_status(FLARE_ERR_UNSUPPORTED, "flare_norm_backward");
     const at::Tensor ws = scratch(need, x, a[6], st);
     check_status(unlocked([&] { return lib.norm_backward(&c.d, rx.p, n.weight, ps, rdy.p, rdh.p, rdx.p, pw, pb, ws.data_ptr(), need, st); }), "flare_norm_backward");
-    return named(a[7], wrap_all({dx, dw, db}));
+    return named(a[7], output.wrapped({dx, dw, db}));
 BINDING_END
 
 // x, branch, post, pre, gate, gate kind, scale, residual scale, whether statistics are wanted, out (y, h, stats) or None, stream -> (y, h, stats)
@@ -664,7 +678,7 @@ BINDING(block_join, 11)
     float *ps = c.stats(stats);
     check_status(unlocked([&] { return lib.join_forward(&c.d, rx.p, ro.p, rg.p, s, post.weight, post.bias, pre.weight, pre.bias, ry.p, rh.p, ps, st); }),
                  "flare_join_forward");
-    return wrap_all({y, h, stats});
+    return output.wrapped({y, h, stats});
 BINDING_END
 
 // branch, y, stats, dy, dh, post, pre, gate, gate kind, scale, residual scale, out or None, stream, class of the result
@@ -704,7 +718,7 @@ BINDING(block_join_backward, 14)
     const at::Tensor ws = scratch(need, y, a[12], st);
     check_status(unlocked([&] { return lib.join_backward(&c.d, ro.p, rg.p, s, post.weight, post.bias, ry.p, pre.weight, ps, rdy.p, rdh.p, rdx.p, rdo.p, rdg.p, p3,
                                                          p4, p5, p6, p7, ws.data_ptr(), need, st); }), "flare_join_backward");
-    return named(a[13], wrap_all({dx, d_o, dg, ds, dwo, dbo, dwy, dby}));
+    return named(a[13], output.wrapped({dx, d_o, dg, ds, dwo, dbo, dwy, dby}));
 BINDING_END
 
 // ---- orthogonalised updates
@@ -765,6 +779,7 @@ BINDING(orthogonalize, 8)
     const size_t need = c.need("flare_orthogonalize");
     const at::Tensor ws = scratch(need, G, a[7], st);
     check_status(unlocked([&] { return lib.orthogonalize(&c.d, g, o, ws.data_ptr(), need, st); }), "flare_orthogonalize");
+    if (a[6] != Py_None) mark_written(O);
     return wrap_all({O, ws});
 BINDING_END
 
@@ -782,6 +797,8 @@ BINDING(muon_update, 16)
     const at::Tensor ws = scratch(need, w, a[15], st);
     check_status(unlocked([&] { return lib.muon_update(&c.d, &rule, w.data_ptr(), (const float *)m.data_ptr(), pg, w_out.data_ptr(), (float *)m_out.data_ptr(),
                                                        ws.data_ptr(), need, st); }), "flare_muon_update");
+    mark_written(w_out);
+    mark_written(m_out);
     return wrap_all({w_out, m_out, ws});
 BINDING_END
 

@@ -354,6 +354,9 @@ typedef struct {
     int32_t nesterov;
 } flare_muon_t;
 size_t flare_orthogonalize_workspace_bytes(const flare_orth_desc_t *desc);
+/* How a descriptor's matrices are run on this device: plan[0] = 0: a block to a matrix; 1: a team of blocks of one launch to a matrix, 2: a launch per
+ * product over pairs of blocks, 3: a cluster to a matrix; for 1 and 3 plan[1] = blocks to a matrix, plan[2] = matrices at a time (else 0). */
+int flare_orthogonalize_plan(const flare_orth_desc_t *desc, int32_t plan[3]);
 int flare_orthogonalize(const flare_orth_desc_t *desc, const void *G, void *O, void *workspace, size_t workspace_bytes, flare_stream_t stream);
 /* w, w_out [count, rows, cols] of weight_dtype, m, m_out the same in float32, contiguous; g with the strides of the descriptor. */
 int flare_muon_update(const flare_orth_desc_t *desc, const flare_muon_t *rule, const void *w, const float *m, const void *g, void *w_out, float *m_out,

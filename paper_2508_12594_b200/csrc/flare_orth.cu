@@ -397,6 +397,16 @@ size_t flare_orthogonalize_workspace_bytes(const flare_orth_desc_t *desc) {
     return orth_layout(desc, orth_plan(desc, device_info().sms), device_info().sms).total;
 }
 
+int flare_orthogonalize_plan(const flare_orth_desc_t *desc, int32_t plan[3]) {
+    OrthScales sc;
+    if (int rc = check_orth(desc, &sc)) return rc;
+    if (!plan) return FLARE_ERR_INVALID_ARG;
+    const OrthPlan p = orth_plan(desc, device_info().sms);
+    const bool groups = p.path == kOrthTeamPath || p.path == kOrthClusterPath;
+    plan[0] = p.path; plan[1] = groups ? p.team : 0; plan[2] = groups ? p.teams : 0;
+    return FLARE_OK;
+}
+
 int flare_orthogonalize(const flare_orth_desc_t *desc, const void *G, void *O, void *workspace, size_t workspace_bytes, flare_stream_t stream) {
     OrthScales sc;
     if (int rc = check_orth(desc, &sc)) return rc;

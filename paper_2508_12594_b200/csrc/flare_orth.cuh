@@ -17,6 +17,8 @@ namespace flare {
 
 // What a step's products are for.
 enum { kOrthGram = 0, kOrthPoly = 1, kOrthApply = 2, kOrthLast = 3 };
+// 64-deep steps whose sums stay in tensor memory, which adds with truncation, before they are added up in registers, rounded (see the large matrices).
+__host__ __device__ constexpr int orth_chunk(int kind) { return kind == kOrthGram ? 8 : 4; }
 
 // The matrices that go in and come out, and the update of the weights around them (m != nullptr).
 struct OrthOuter {
@@ -327,7 +329,7 @@ struct OrthProduct {
 struct HalfMaps { CUtensorMap load, store, store_t; };
 
 // Warp 0 loads, warp 1 issues, warps 4 to 11 take the sums out of tensor memory.
-constexpr int kOrthThreads = 384, kOrthStages = 3, kOrthChunk = 8;  // 64-deep steps whose sums stay in tensor memory
+constexpr int kOrthThreads = 384, kOrthStages = 3;
 constexpr uint32_t kOrthHalfTile = 128 * 128;                       // bytes: 128 rows (or 64 rows of two blocks of columns) of 64 float16
 constexpr uint32_t kOrthStage = 4 * kOrthHalfTile;                  // A high, A low, B high, B low
 constexpr uint32_t kOrthPiece = 4096;                               // a warp's piece of the result on its way out: 32 x 64 halves, 32 x 32 floats
@@ -537,7 +539,7 @@ __device__ __forceinline__ void orth_issue(OrthPipe &q, const OrthProduct &p, co
             const uint32_t acc = q.tmem + (q.c & 1) * kTileN;
             if (q.c >= 2 && !ptx::mbar_wait(q.acc_empty(q.c & 1), (q.c / 2 - 1) & 1, q.abort_flag, 102)) return;
             ptx::tc_fence_after();
-            for (int k1 = min(kb + kOrthChunk, w.kb1), first = 1; kb < k1; ++kb, ++q.n, first = 0) {
+            for (int k1 = min(kb + orth_chunk(kind), w.kb1), first = 1; kb < k1; ++kb, ++q.n, first = 0) {
                 const uint32_t s = q.n % kOrthStages;
                 if (!ptx::mbar_wait(q.full(s), (q.n / kOrthStages) & 1, q.abort_flag, 103)) return;
                 ptx::tc_fence_after();
@@ -714,7 +716,7 @@ __device__ __forceinline__ void orth_results_of(OrthPipe &q, const OrthProduct &
                                                 const CUtensorMap *out_t) {
     constexpr int kTileN = 128 * kPair, kCols = 64 * kPair;
     const int warp = ptx::warp_index(), quad = warp & 3, half = (warp - 4) >> 2, in_pair = kPair == 2 ? (int)(blockIdx.x & 1) : 0;
-    const int chunks = (w.kb1 - w.kb0 + kOrthChunk - 1) / kOrthChunk;
+    const int chunks = (w.kb1 - w.kb0 + orth_chunk(kind) - 1) / orth_chunk(kind);
     for (int t = w.t0; t < w.total; t += w.step) {
         const OrthTile x = orth_tile(p, w, t);
         float v[kCols];
@@ -727,9 +729,12 @@ __device__ __forceinline__ void orth_results_of(OrthPipe &q, const OrthProduct &
 
 // ---- large matrices: a launch per product, tiles of 256 x 256 by pairs of blocks
 //
-// Tensor memory adds with truncation, which over K = 4096 (768 additions of 16 products) is off by 2e-5 of a sum of equal signs, and by 9e-5 of the
-// 2-norm of the whole result: sums stay there for kOrthChunk steps (K = 512) and are added up in registers, rounded, while the next
-// ones run in a second set of columns: 1e-5.  (The same second set lets a tile's results go out under the next tile's products.)
+// Tensor memory adds with truncation, which over K = 4096 (768 additions of 16 products) is off by 2e-5 of a sum of equal signs.  So sums stay there for
+// some steps only (orth_chunk) and are added up in registers, rounded, while the next ones run in a second set of columns.  Of the squares and of B X it
+// is four (K = 256): with eight, as X X^T has them, whose error hardly matters, the result's 2-norm is off by 2.4e-5 instead of 1.2e-5 (1003 x 2601)
+// and 1.5e-5 instead of 7.4e-6 (four of 2048 x 2048), single entries by up to 2.3e-4 of the RMS instead of 1.4e-4, for 1633 us instead of 1681 and 656
+// instead of 676 (three of 1500 x 1500); nothing changes in time where a launch has all products.  Two steps: half the error again, 1828 us.
+// (The same second set lets a tile's results go out under the next tile's products.)
 // 256 x 256 x 64 of two halves each is 64 KB a block and stage, three stages; a pair reads half of what two blocks of 128 x 256 would.  Bound by the tensor
 // pipe: an update of 2 x 4096 x 4096 (2.75 TFLOP, three products of each) takes 6.9 ms, 1200 TFLOP/s, the pipe 91 to 97 % busy, the clock under the
 // power limit.
@@ -915,7 +920,7 @@ __device__ __forceinline__ void team_product(const OrthTeam &p, OrthPipe &q, int
         if (warp == 0) orth_load<1>(q, d, w, kind, &ta->load, &tb->load);
         else if (warp == 1) orth_issue<1>(q, d, w, kind);
     } else {
-        const int quad = warp & 3, half = (warp - 4) >> 2, lane = threadIdx.x & 31, chunks = (w.kb1 - w.kb0 + kOrthChunk - 1) / kOrthChunk;
+        const int quad = warp & 3, half = (warp - 4) >> 2, lane = threadIdx.x & 31, chunks = (w.kb1 - w.kb0 + orth_chunk(kind) - 1) / orth_chunk(kind);
         for (int t = w.t0; t < w.total; t += w.step) {
             const OrthTile x = orth_tile(d, w, t);
             float v[64];

@@ -85,6 +85,7 @@ _SIGNATURES = {
     "flare_join_forward": (ctypes.c_int, [_bp] + [_vp] * 12),
     "flare_join_backward": (ctypes.c_int, [_bp] + [_vp] * 19 + [_sz, _vp]),
     "flare_orthogonalize_workspace_bytes": (_sz, [_op]),
+    "flare_orthogonalize_plan": (ctypes.c_int, [_op, ctypes.POINTER(ctypes.c_int32)]),
     "flare_orthogonalize": (ctypes.c_int, [_op, _vp, _vp, _vp, _sz, _vp]),
     "flare_muon_update": (ctypes.c_int, [_op, ctypes.POINTER(FlareMuon)] + [_vp] * 6 + [_sz, _vp]),
     "flare_selftest_wait": (ctypes.c_int, [_vp, ctypes.c_uint64, _vp]),
@@ -370,6 +371,19 @@ def orthogonalize(G, steps=5, coefficients=NEWTON_SCHULZ, eps=1e-7, out=None, st
         (stream or torch.cuda.current_stream()).synchronize()
         flare_check(ws, stream)
     return O
+
+
+ORTH_BLOCK, ORTH_TEAM, ORTH_PAIRS, ORTH_CLUSTER = range(4)
+
+
+def orthogonalize_plan(count, rows, cols, dtype=torch.float32, steps=5, coefficients=NEWTON_SCHULZ):
+    """How that many matrices are run: (ORTH_BLOCK, ORTH_TEAM, ORTH_PAIRS or ORTH_CLUSTER, blocks to a matrix, matrices at a time; 0 where
+    neither is fixed)."""
+    code = _dtype_code(torch.empty(0, dtype=dtype))
+    desc = FlareOrthDesc(count=count, rows=rows, cols=cols, dtype=code, weight_dtype=code, steps=steps, coefficients=(ctypes.c_float * 3)(*coefficients), eps=1e-7)
+    plan = (ctypes.c_int32 * 3)()
+    _raise(load().flare_orthogonalize_plan(ctypes.byref(desc), plan), "flare_orthogonalize_plan")
+    return tuple(plan)
 
 
 def muon_update(w, m, g, lr, momentum=0.95, weight_decay=0.0, nesterov=True, update_scale=None, steps=5, coefficients=NEWTON_SCHULZ, eps=1e-7,

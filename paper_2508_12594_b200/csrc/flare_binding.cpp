@@ -500,7 +500,7 @@ PyObject *named(PyObject *cls, PyObject *values) {
 int number_of(PyObject *o) {
     const long x = PyLong_AsLong(o);
     if (x == -1 && PyErr_Occurred()) throw PythonError{};
-    return (int)x;
+    return (int)std::max<long>(INT32_MIN, std::min<long>(x, INT32_MAX));      // (what is out of range stays so)
 }
 PyObject *wrap(const at::Tensor &t) {
     if (!t.defined()) Py_RETURN_NONE;

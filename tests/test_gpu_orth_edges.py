@@ -24,3 +24,11 @@ def test_no_matrices_report_nothing(rows, cols):
     none = torch.empty(0, rows, cols, device="cuda")
     assert flare.orthogonalize(none, check=True).shape == none.shape
     flare.muon_update(none, none, none, lr=0.1, check=True)
+
+
+def test_steps_beyond_32_bits_are_not_taken_for_others():
+    """2^32 + 5 is not 5."""
+    for steps, status in ((2 ** 32 + 5, flare.ERR_UNSUPPORTED), (-2 ** 32 + 5, flare.ERR_INVALID_ARG)):
+        with pytest.raises(flare.FlareError) as e:
+            flare.orthogonalize(torch.zeros(8, 12, device="cuda"), steps=steps)
+        assert e.value.status == status

@@ -392,8 +392,8 @@ def muon_update(w, m, g, lr, momentum=0.95, weight_decay=0.0, nesterov=True, upd
     a gradient of any type.  m' = momentum m + (1 - momentum) g; w' = (1 - lr weight_decay) w - lr update_scale O, O the orthogonalised
     momentum m' + (1 - momentum)(g - m') (nesterov) or m'.  update_scale: None means sqrt(max(1, rows / cols)).  In place unless
     w_out, m_out are given; returns (w', m')."""
-    if update_scale is None:
-        update_scale = max(1.0, g.shape[-2] / g.shape[-1]) ** 0.5
+    if update_scale is None:                                      # (what is no matrix is refused by the call)
+        update_scale = max(1.0, g.shape[-2] / g.shape[-1]) ** 0.5 if g.dim() > 1 and g.shape[-1] > 0 else 1.0
     w1, m1, ws = (_native or _bind()).muon_update(w, m, g, lr, momentum, weight_decay, update_scale, nesterov, steps, *coefficients, eps, w_out, m_out, stream)
     if check:
         (stream or torch.cuda.current_stream()).synchronize()

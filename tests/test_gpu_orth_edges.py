@@ -32,3 +32,12 @@ def test_steps_beyond_32_bits_are_not_taken_for_others():
         with pytest.raises(flare.FlareError) as e:
             flare.orthogonalize(torch.zeros(8, 12, device="cuda"), steps=steps)
         assert e.value.status == status
+
+
+def test_updates_of_what_is_no_matrix_are_refused_as_that():
+    v, none = torch.zeros(12, device="cuda"), torch.zeros(5, 0, device="cuda")
+    with pytest.raises(ValueError, match="matrices"):
+        flare.muon_update(v, v, v, lr=0.1)
+    with pytest.raises(flare.FlareError) as e:
+        flare.muon_update(none, none, none, lr=0.1)
+    assert e.value.status == flare.ERR_INVALID_ARG

@@ -272,8 +272,8 @@ int flare_spectral_eig(int32_t matrices, int32_t M, float *G, float *eigenvalues
  *
  * A tensor here is `rows` rows (the tokens of all batch items) of `width` columns, row-major, the columns next to each other and rows
  * `stride_*` elements apart (0: width), so that a slice of a wider projection is taken as it is.  Pointers are aligned to their element type;
- * rows that all start on 16-byte boundaries and whose width is a multiple of 8 are moved 16 bytes at a time, others one element at a
- * time.  Norm weights, biases and the residual scale are float32 [width]; a weight or scale that is NULL counts as ones, a bias as zeros.
+ * rows that all start on 16-byte boundaries and whose width is a multiple of 8 are moved 16 bytes at a time; others are read as the aligned
+ * 16-byte pieces that they lie in and written one element at a time.  Norm weights, biases and the residual scale are float32 [width]; a weight or scale that is NULL counts as ones, a bias as zeros.
  *
  *     N(v) = (v - mean(v)) rstd weight + bias,  rstd = 1 / sqrt(var(v) + eps)       FLARE_NORM_LAYER
  *     N(v) = v rstd weight + bias,              rstd = 1 / sqrt(mean(v^2) + eps)    FLARE_NORM_RMS
@@ -302,7 +302,7 @@ typedef struct {
 /* Bytes of workspace either backward needs (0 for an invalid descriptor, its gate among them): one row of partial sums per thread block. */
 size_t flare_block_workspace_bytes(const flare_block_desc_t *desc);
 
-/* The norm before the first block (pre_norm of the descriptor; post_norm, gate and residual_scale are not looked at). */
+/* The norm before the first block (pre_norm of the descriptor; post_norm, gate and residual_scale, valid as they have to be, have no effect). */
 int flare_norm_forward(const flare_block_desc_t *desc, const void *x, const float *weight, const float *bias, void *h, float *stats,
                        flare_stream_t stream);
 /* Its backward: dx = dy + J^T dh (dy, the gradient that reaches x beside the norm, may be NULL); dweight = sum over rows of
@@ -330,18 +330,22 @@ int flare_join_backward(const flare_block_desc_t *desc, const void *branch, cons
  *
  * (of the transpose where rows > cols, which is the same matrix).  The odd polynomial a x + b x^3 + c x^5 of the singular values is applied
  * `steps` times; with the usual (3.4445, -4.7750, 2.0315) and five steps they come out between about 0.7 and 1.2.  Inputs and outputs of any of the
- * three types.  The products run on the tensor cores, every factor in two float16 halves (22 bits), sums in float32: O is within some 1e-5
- * of its RMS of float64, also where singular values of a few strong directions stand beside many small ones.
+ * three types.  The products run on the tensor cores, every factor in two float16 halves (22 bits), sums in float32: after five steps with the usual
+ * coefficients O is off by up to 1.3e-5 of its 2-norm (float32 products: 4e-6), single entries by up to 1.5e-4 of the RMS, also where singular values of a
+ * few strong directions stand beside many small ones.  That polynomial does not converge, and what is rounded away grows with the steps: 2e-5 after eight,
+ * 1.5e-4 after twenty (1e-5 in float32); with one that does (1.875, -1.25, 0.375) it stays at 3e-6.  X is held down to 2^-39: a matrix whose norm is below
+ * 1e-4 eps loses bits (1e-5 there, 1e-3 at 1e-6 eps).
  *
  * flare_muon_update puts the optimiser's step around it, one pass over the matrices before and one after:
  *     m' = momentum m + (1 - momentum) g;  u = momentum m' + (1 - momentum) g with nesterov, else m';
  *     w' = (1 - lr weight_decay) w - lr update_scale orthogonalised(u)
  * w_out may be w, m_out may be m, O may be G (with the same strides).  A matrix with a NaN or an infinity comes out as NaN throughout; others are not
- * touched by it.  A polynomial under which singular values in [0, 1] would grow beyond 64 is FLARE_ERR_UNSUPPORTED.
+ * touched by it.  All SMs of the device are counted on: where a process has a share of them only, a launch whose blocks wait for one another may be
+ * refused (FLARE_ERR_CUDA).  A polynomial under which singular values in [0, 1] would grow beyond 64 is FLARE_ERR_UNSUPPORTED.
  * A wait inside the kernels that gave up is reported by flare_check(workspace).
  */
 typedef struct {
-    int32_t count, rows, cols;           /* matrices (0 is allowed), up to 65536 rows and columns and 2^31 - 1 elements each */
+    int32_t count, rows, cols;           /* up to 32767 matrices (0 is allowed), up to 65536 rows and columns and 2^31 - 1 elements each */
     int32_t dtype;                       /* of G and O; flare_muon_update: of g */
     int32_t weight_dtype;                /* flare_muon_update: of w, w_out */
     int32_t steps;                       /* 1 to 64 */

@@ -331,6 +331,7 @@ __device__ __forceinline__ float2 moments(RowGroup &grp, const float2 (&v)[kV][4
     return make_float2(part.z, rsqrtf(fmaf(part.y, inv_c, eps)));
 }
 
+// (The exponent is a product that is rounded once, and so is log2 e: a is off by some 1e-7 |g| of itself, also for float32 gates.)
 __device__ __forceinline__ float gate_act(int kind, float g) {
     if (kind != 1) return g;
     float a;                                                 // (of 1 + exp(-g) = infinity: 0)

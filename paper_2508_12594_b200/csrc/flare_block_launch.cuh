@@ -19,7 +19,7 @@ struct BlockPlan {
 inline BlockPlan block_plan(long rows, long group, int C, bool aligned, int sms, int vectors) {    // vectors: groups of eight columns a thread owns
     BlockPlan p;
     p.threads = C > 2048 * vectors ? 512 : 256;
-    p.tpr = aligned ? 4 : 32;                               // (columns that are moved one at a time: a warp's lanes side by side)
+    p.tpr = aligned ? 4 : 32;                               // (rows off 16-byte boundaries: a warp copies its 256 columns together, its lanes own every 32nd)
     while (p.tpr * 8 * vectors < C && p.tpr < p.threads) p.tpr *= 2;
     p.cluster = 1;
     while (p.cluster * p.threads * 8 * vectors < C) p.cluster *= 2;
@@ -79,7 +79,7 @@ template <typename T, typename R, int kIn>
 int block_forward_of(const BlockArgs &a, bool aligned, int sms, cudaStream_t st) {
     constexpr int kV = sizeof(T) == 2 ? 2 : 1;              // (float32: its loads fill shared memory with one group of columns a thread)
     const BlockPlan p = block_plan(a.rows, a.group, a.C, aligned, sms, aligned ? kV : 1);
-    // (rows that are moved one element at a time: always the form with biases, here and in the backward)
+    // (rows off 16-byte boundaries: always the form with biases, here and in the backward)
     if (!aligned) return p.threads == 512 ? block_forward_as<T, R, false, kIn, true, 1, 512>(a, p, st) : block_forward_as<T, R, false, kIn, true, 1, 256>(a, p, st);
     return a.b_post || a.b_pre ? block_forward_aligned<T, R, kIn, true, kV>(a, p, st) : block_forward_aligned<T, R, kIn, false, kV>(a, p, st);
 }

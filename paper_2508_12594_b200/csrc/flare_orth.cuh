@@ -7,7 +7,8 @@
 // are off by several percent after five steps on matrices with a few strong directions.  So every factor is carried as two float16
 // halves (22 bits), x = hi + lo at a power-of-two scale that keeps lo a normal number, and a product is hi hi + hi lo + lo hi on the
 // tensor cores with float32 sums: three products at the 16-bit rate against one at a rate some twenty times lower in float32.
-// A, B and the squares are symmetric: only tiles on and above the diagonal are computed, each is stored twice.
+// A, B and the squares are symmetric: pairs of blocks compute only the tiles on and above the diagonal and store each twice, teams where that is the
+// faster form (team_plan); clusters and single blocks compute both halves.
 #pragma once
 
 #include "flare_common.cuh"
@@ -207,7 +208,7 @@ __global__ void __launch_bounds__(256) orth_clear_kernel(uint32_t *words, int n)
 // ---------------------------------------------------------------- norm and first split, for matrices that do not fit a block
 constexpr int kOrthNormThreads = 256;
 
-// Momentum, and per block the sum of squares of its share of a matrix, in float64 (gradients of 1e-25 are as good as any).  Grid (blocks, count).
+// Momentum, and per block the sum of squares of its share of a matrix, in float64 (with eps = 0 gradients of 1e-25 are as good as any).  Grid (blocks, count).
 __global__ void __launch_bounds__(kOrthNormThreads) orth_norm_kernel(OrthOuter o, double *part) {
     ptx::grid_launch();
     ptx::grid_wait();
@@ -732,12 +733,12 @@ __device__ __forceinline__ void orth_results_of(OrthPipe &q, const OrthProduct &
 // Tensor memory adds with truncation, which over K = 4096 (768 additions of 16 products) is off by 2e-5 of a sum of equal signs.  So sums stay there for
 // some steps only (orth_chunk) and are added up in registers, rounded, while the next ones run in a second set of columns.  Of the squares and of B X it
 // is four (K = 256): with eight, as X X^T has them, whose error hardly matters, the result's 2-norm is off by 2.4e-5 instead of 1.2e-5 (1003 x 2601)
-// and 1.5e-5 instead of 7.4e-6 (four of 2048 x 2048), single entries by up to 2.3e-4 of the RMS instead of 1.4e-4, for 1633 us instead of 1681 and 656
-// instead of 676 (three of 1500 x 1500); nothing changes in time where a launch has all products.  Two steps: half the error again, 1828 us.
+// and 1.5e-5 instead of 7.4e-6 (four of 2048 x 2048), single entries by up to 2.3e-4 of the RMS instead of 1.4e-4.  It costs 2 % (2048 x 2048 462 us
+// instead of 452, two of 4096 x 4096 6900 instead of 6790) and up to 5 (four of 1024 x 1024 293 instead of 279); two steps: half the error again, 10 % more.
 // (The same second set lets a tile's results go out under the next tile's products.)
 // 256 x 256 x 64 of two halves each is 64 KB a block and stage, three stages; a pair reads half of what two blocks of 128 x 256 would.  Bound by the tensor
-// pipe: an update of 2 x 4096 x 4096 (2.75 TFLOP, three products of each) takes 6.9 ms, 1200 TFLOP/s, the pipe 91 to 97 % busy, the clock under the
-// power limit.
+// pipe: an update of 2 x 4096 x 4096 (2.75 TFLOP, three products of each) takes 7.0 to 7.3 ms, 1130 to 1180 TFLOP/s, the pipe 87 (squares) to 97 % (B X)
+// busy, the clock under the power limit.
 struct OrthPairArgs {
     OrthProduct p;
     OrthOuter o;                 // kOrthLast

@@ -104,6 +104,25 @@ def test_strides_in_place_and_one_bad_matrix(shape, path):
     assert (wide == 3).all()
 
 
+@pytest.mark.parametrize("shape,path", [((8, 256, 16), BLOCK), ((1, 1003, 2601), TEAM), ((3, 1100, 1100), TEAM), ((40, 512, 512), PAIRS), ((16, 129, 258), CLUSTER)], ids=str)
+def test_captured(shape, path):
+    """In a graph, replayed on other inputs than it was captured with."""
+    lead_there(shape, path)
+    G = gradient(*shape, seed=1)
+    other = gradient(*shape, seed=2)
+    want = flare.orthogonalize(other)
+    flare.orthogonalize(G)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        O = flare.orthogonalize(G)
+    G.copy_(other)
+    for _ in range(2):
+        O.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(O, want)
+
+
 def test_more_elements_than_32_bits_count():
     """2.2 billion of them: the first, the last and some matrices in between."""
     shape = (32767, 256, 264)

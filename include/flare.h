@@ -367,6 +367,80 @@ int flare_muon_update(const flare_orth_desc_t *desc, const flare_muon_t *rule, c
                       void *workspace, size_t workspace_bytes, flare_stream_t stream);
 
 /*
+ * ---- Tokens: what a model over token numbers has before its first block and behind its last, and dropout between them.
+ *
+ * Dropout multiplies an element by 0 or by 65536 / (65536 - thr), thr = round(65536 p).  Which, says a counter-based generator, so that no mask is
+ * stored and a backward pass forms the same one: column c of row r is kept where the 16 bits c mod 8 (the words in order, low half first) of Philox4x32-10 with the
+ * counter (c / 8, r, low word of o, high word of o), o = offset + *step, and the key (low word of seed, high word) are at least thr.  step (device memory, or NULL: 0) is
+ * read by the kernels: a captured graph that also counts it up drops other elements each time it is replayed.  What is dropped is 0 whatever it was.  The mask
+ * depends neither on strides nor types.
+ */
+typedef struct {
+    float p;                /* 0 to 1 */
+    uint64_t seed, offset;
+    const int64_t *step;
+} flare_drop_t;
+/* y = drop(x) + residual (NULL: none); tensors of rows as around a block.  y may be x (with residual_dtype = dtype) or residual, with the same strides. */
+typedef struct {
+    int64_t rows;           /* 0 is allowed */
+    int32_t width;
+    int32_t dtype;          /* of x, dx */
+    int32_t residual_dtype; /* of residual, y, dy: dtype, or float32 */
+    int64_t stride_x, stride_residual, stride_y;
+} flare_dropout_desc_t;
+int flare_dropout_forward(const flare_dropout_desc_t *desc, const flare_drop_t *drop, const void *x, const void *residual, void *y, flare_stream_t stream);
+/* dx (stride_x) = drop(dy) (stride_y), the same elements.  (The residual's gradient is dy.)  dx may be dy. */
+int flare_dropout_backward(const flare_dropout_desc_t *desc, const flare_drop_t *drop, const void *dy, void *dx, flare_stream_t stream);
+
+/*
+ * Embedding: y[n] = drop(scale table[tokens[n]] + position_table[n mod positions]).  A token outside [0, vocab) has no row: zeros in its place, and no gradient.
+ * tokens [rows] of token_bits (32 or 64); table [vocab, width] of dtype, rows stride_table apart; position_table [positions, width] of dtype, contiguous
+ * (positions = 0: none; else a divisor of rows); y, dy of out_dtype, rows stride_out apart.  dtype and out_dtype are the same, or one of them is float32.
+ * drop may be NULL.
+ */
+typedef struct {
+    int64_t rows;           /* 0 is allowed */
+    int64_t positions;
+    int32_t width, vocab;
+    int32_t dtype, out_dtype;
+    int32_t token_bits;
+    float scale;
+    int64_t stride_table, stride_out;
+} flare_embed_desc_t;
+int flare_embed_forward(const flare_embed_desc_t *desc, const flare_drop_t *drop, const void *tokens, const void *table, const void *position_table, void *y,
+                        flare_stream_t stream);
+/* dtable[v] = scale sum of drop(dy[n]) over the n with token v, dposition_table[l] = sum over n mod positions = l; contiguous, of dtype, either NULL if not wanted.  accumulate:
+ * added to what they hold (a table that is also the loss's, say), rows that no token has met stay as they are; else they are written whole.  Sums are float32, in an order that
+ * follows from the tokens alone. */
+size_t flare_embed_workspace_bytes(const flare_embed_desc_t *desc);
+int flare_embed_backward(const flare_embed_desc_t *desc, const flare_drop_t *drop, const void *tokens, const void *dy, void *dtable, void *dposition_table,
+                         int32_t accumulate, void *workspace, size_t workspace_bytes, flare_stream_t stream);
+
+/*
+ * Softmax cross entropy over a vocabulary, l[n, v] = scale x[n] . w[v]:
+ *     lse[n] = log sum_v exp l[n, v];   loss[n] = lse[n] - l[n, labels[n]]
+ *     dx[n] = g_n scale sum_v (p[n, v] - [v = labels[n]]) w[v];   dw[v] = scale sum_n g_n (p[n, v] - [v = labels[n]]) x[n];   p = exp(l - lse), g_n = dloss_scale dloss[n]
+ * The logits are never kept: forward they stay on the chip, backward they are formed again, a piece of the vocabulary at a time (scratch of 256 MB, or 512 bytes a row where that is
+ * more).  A row whose label is outside [0, vocab) takes no part: loss, lse and dx are 0, and what x holds there is not looked at.
+ * x, dx [rows, width], w, dw [vocab, width] of dtype, rows stride_* apart; labels [rows] of label_bits (32 or 64); loss, lse, dloss [rows] float32 (dloss NULL: ones); dx or dw may
+ * be NULL if not wanted.  Products run on the tensor cores with float32 sums: 16-bit types as they are, p in the same type (rounded once); float32 in two float16 halves (22 bits; x and w are held
+ * down to 2^-39 of their largest element).  A wait inside the kernels that gave up is reported by flare_check(workspace).
+ */
+typedef struct {
+    int64_t rows;           /* 0 is allowed */
+    int32_t width, vocab;   /* up to 16384, up to 2^28 */
+    int32_t dtype, label_bits;
+    float scale;            /* above 0 */
+    float dloss_scale;      /* backward */
+    int64_t stride_x, stride_w, stride_dx, stride_dw;
+} flare_loss_desc_t;
+size_t flare_loss_workspace_bytes(const flare_loss_desc_t *desc, int32_t backward);
+int flare_loss_forward(const flare_loss_desc_t *desc, const void *x, const void *w, const void *labels, float *loss, float *lse, void *workspace, size_t workspace_bytes,
+                       flare_stream_t stream);
+int flare_loss_backward(const flare_loss_desc_t *desc, const void *x, const void *w, const void *labels, const float *lse, const float *dloss, void *dx, void *dw,
+                        void *workspace, size_t workspace_bytes, flare_stream_t stream);
+
+/*
  * Instruction-level measurements behind the kernels' design (the paper has no counterpart), so that the figures the
  * documentation quotes can be re-taken on the GPU at hand.  `which`:
  *   0, 1, 2   exponentials per clock per SM of the softmax loop as the sixteen softmax warps of a forward kernel run it

@@ -42,6 +42,14 @@ struct Library {
     decltype(&flare_orthogonalize_workspace_bytes) orthogonalize_workspace_bytes;
     decltype(&flare_orthogonalize) orthogonalize;
     decltype(&flare_muon_update) muon_update;
+    decltype(&flare_dropout_forward) dropout_forward;
+    decltype(&flare_dropout_backward) dropout_backward;
+    decltype(&flare_embed_forward) embed_forward;
+    decltype(&flare_embed_workspace_bytes) embed_workspace_bytes;
+    decltype(&flare_embed_backward) embed_backward;
+    decltype(&flare_loss_workspace_bytes) loss_workspace_bytes;
+    decltype(&flare_loss_forward) loss_forward;
+    decltype(&flare_loss_backward) loss_backward;
 } lib{};
 PyObject *flare_error = nullptr;   // the exception class (status, where)
 
@@ -802,6 +810,242 @@ BINDING(muon_update, 16)
     return wrap_all({w_out, m_out, ws});
 BINDING_END
 
+// ---- tokens: embedding, dropout, the loss over a vocabulary
+
+// A Drop (p, seed, offset, step), or None.
+struct DropArg {
+    flare_drop_t d{};
+    bool given = false;
+    explicit DropArg(PyObject *o) {
+        if (o == Py_None) return;
+        if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != 4) fail(PyExc_TypeError, "expected a Drop (p, seed, offset, step) or None");
+        given = true;
+        d.p = (float)number(PyTuple_GET_ITEM(o, 0));
+        d.seed = word(PyTuple_GET_ITEM(o, 1));
+        d.offset = word(PyTuple_GET_ITEM(o, 2));
+        PyObject *step = PyTuple_GET_ITEM(o, 3);
+        if (step == Py_None) return;
+        const at::Tensor &t = tensor(step);
+        if (!t.is_cuda()) fail(PyExc_ValueError, "step: expected a CUDA tensor");
+        if (t.scalar_type() != at::kLong || t.numel() != 1) fail(PyExc_TypeError, "step: expected one number of type torch.int64");
+        d.step = (const int64_t *)t.data_ptr();
+    }
+    const flare_drop_t *get() const { return given ? &d : nullptr; }
+    static uint64_t word(PyObject *o) {
+        const uint64_t x = PyLong_AsUnsignedLongLong(o);
+        if (PyErr_Occurred()) throw PythonError{};
+        return x;
+    }
+};
+at::ScalarType dtype_or(PyObject *o, at::ScalarType other) {
+    if (o == Py_None) return other;
+    if (!THPDtype_Check(o)) fail(PyExc_TypeError, "dtype: expected a torch dtype");
+    return ((THPDtype *)o)->scalar_type;
+}
+// Contiguous numbers of tokens (labels), 32 or 64 bits.
+const void *numbers_of(const at::Tensor &t, int32_t &bits, const char *name) {
+    if (!t.is_cuda() || !t.is_contiguous()) fail(PyExc_ValueError, std::string(name) + ": expected a contiguous CUDA tensor");
+    if (t.scalar_type() != at::kLong && t.scalar_type() != at::kInt) fail(PyExc_TypeError, std::string(name) + ": expected torch.int64 or torch.int32, got " + dtype_name(t.scalar_type()));
+    bits = t.scalar_type() == at::kLong ? 64 : 32;
+    return t.data_ptr();
+}
+int32_t width_of(int64_t C, at::IntArrayRef shape) {
+    if (C < 1 || C > INT32_MAX) fail(PyExc_ValueError, "expected tensors [..., width], got shape " + shape_text(shape));
+    return (int32_t)C;
+}
+// One place for the result: out itself, or a new tensor.
+at::Tensor one_result(PyObject *out, at::IntArrayRef shape, const at::TensorOptions &options, PyObject *stream, flare_stream_t st) {
+    return out != Py_None ? tensor(out) : result(shape, options, stream, st);
+}
+PyObject *wrap_written(const at::Tensor &t, PyObject *out) {
+    if (out != Py_None) mark_written(t);
+    return wrap(t);
+}
+
+// x, drop, residual or None, out or None, stream -> y
+BINDING(dropout, 5)
+    const at::Tensor &x = tensor(a[0]);
+    const DropArg drop(a[1]);
+    flare_dropout_desc_t d{};
+    if (x.dim() < 1) fail(PyExc_ValueError, "expected tensors [..., width], got shape " + shape_text(x.sizes()));
+    d.width = width_of(x.size(-1), x.sizes());
+    d.rows = x.numel() / d.width;
+    const at::ScalarType res = a[2] != Py_None ? tensor(a[2]).scalar_type() : x.scalar_type();
+    d.dtype = dtype_code(x.scalar_type()); d.residual_dtype = dtype_code(res);
+    const Rows rx = rows_of(x, x.scalar_type(), x.sizes(), "x");
+    d.stride_x = rx.stride;
+    Rows rr;
+    if (a[2] != Py_None) { rr = rows_of(tensor(a[2]), res, x.sizes(), "residual"); d.stride_residual = rr.stride; }
+    flare_stream_t st = stream_of(a[4]);
+    const at::Tensor y = one_result(a[3], x.sizes(), x.options().dtype(res), a[4], st);
+    const Rows ry = rows_of(y, res, x.sizes(), "out");
+    d.stride_y = ry.stride;
+    check_status(unlocked([&] { return lib.dropout_forward(&d, drop.get(), rx.p, rr.p, ry.p, st); }), "flare_dropout_forward");
+    return wrap_written(y, a[3]);
+BINDING_END
+
+// dy, drop, dtype or None, out or None, stream -> dx
+BINDING(dropout_backward, 5)
+    const at::Tensor &dy = tensor(a[0]);
+    const DropArg drop(a[1]);
+    flare_dropout_desc_t d{};
+    if (dy.dim() < 1) fail(PyExc_ValueError, "expected tensors [..., width], got shape " + shape_text(dy.sizes()));
+    d.width = width_of(dy.size(-1), dy.sizes());
+    d.rows = dy.numel() / d.width;
+    const at::ScalarType dt = dtype_or(a[2], a[3] != Py_None ? tensor(a[3]).scalar_type() : dy.scalar_type());
+    d.dtype = dtype_code(dt); d.residual_dtype = dtype_code(dy.scalar_type());
+    const Rows ry = rows_of(dy, dy.scalar_type(), dy.sizes(), "dy");
+    d.stride_y = ry.stride;
+    flare_stream_t st = stream_of(a[4]);
+    const at::Tensor dx = one_result(a[3], dy.sizes(), dy.options().dtype(dt), a[4], st);
+    const Rows rx = rows_of(dx, dt, dy.sizes(), "out");
+    d.stride_x = rx.stride;
+    check_status(unlocked([&] { return lib.dropout_backward(&d, drop.get(), ry.p, rx.p, st); }), "flare_dropout_backward");
+    return wrap_written(dx, a[3]);
+BINDING_END
+
+// tokens, table, positions or None, scale, drop or None, dtype or None, out or None, stream -> y
+BINDING(embed, 8)
+    const at::Tensor &tokens = tensor(a[0]), &table = tensor(a[1]);
+    flare_embed_desc_t d{};
+    const void *pt = numbers_of(tokens, d.token_bits, "tokens");
+    if (table.dim() != 2 || table.size(0) < 1 || table.size(0) > INT32_MAX) fail(PyExc_ValueError, "table: expected shape (vocab, width), got " + shape_text(table.sizes()));
+    d.rows = tokens.numel(); d.vocab = (int32_t)table.size(0); d.width = width_of(table.size(1), table.sizes());
+    d.scale = (float)number(a[3]);
+    const DropArg drop(a[4]);
+    const at::ScalarType dt = table.scalar_type(), ot = dtype_or(a[5], a[6] != Py_None ? tensor(a[6]).scalar_type() : dt);
+    d.dtype = dtype_code(dt); d.out_dtype = dtype_code(ot);
+    const Rows rt = rows_of(table, dt, table.sizes(), "table");
+    d.stride_table = rt.stride;
+    const void *pp = nullptr;
+    if (a[2] != Py_None) {
+        const at::Tensor &p = tensor(a[2]);
+        if (p.dim() != 2 || p.size(1) != table.size(1) || p.size(0) < 1 || tokens.dim() < 1 || p.size(0) != tokens.size(-1))
+            fail(PyExc_ValueError, "positions: expected shape (tokens of a sequence, width), got " + shape_text(p.sizes()));
+        check(p, dt, p.sizes());
+        d.positions = p.size(0);
+        pp = p.data_ptr();
+    }
+    std::vector<int64_t> shape = tokens.sizes().vec();
+    shape.push_back(d.width);
+    flare_stream_t st = stream_of(a[7]);
+    const at::Tensor y = one_result(a[6], shape, table.options().dtype(ot), a[7], st);
+    const Rows ry = rows_of(y, ot, shape, "out");
+    d.stride_out = ry.stride;
+    check_status(unlocked([&] { return lib.embed_forward(&d, drop.get(), pt, rt.p, pp, ry.p, st); }), "flare_embed_forward");
+    return wrap_written(y, a[6]);
+BINDING_END
+
+// tokens, dy, vocab, positions (0: none), scale, drop or None, dtype or None, accumulate, out (dtable, dpositions) or None, stream, class of the result
+BINDING(embed_backward, 11)
+    const at::Tensor &tokens = tensor(a[0]), &dy = tensor(a[1]);
+    flare_embed_desc_t d{};
+    const void *pt = numbers_of(tokens, d.token_bits, "tokens");
+    const int vocab = number_of(a[2]), positions = number_of(a[3]);
+    if (vocab < 1) fail(PyExc_ValueError, "vocab: expected a positive number");
+    if (positions < 0 || (positions > 0 && (tokens.dim() < 1 || tokens.size(-1) != positions))) fail(PyExc_ValueError, "positions: expected 0 or the tokens of a sequence");
+    if (dy.dim() < 1) fail(PyExc_ValueError, "dy: expected shape (tokens, width), got " + shape_text(dy.sizes()));
+    d.rows = tokens.numel(); d.vocab = vocab; d.positions = positions; d.width = width_of(dy.size(-1), dy.sizes());
+    d.scale = (float)number(a[4]);
+    const DropArg drop(a[5]);
+    flare_stream_t st = stream_of(a[9]);
+    const Outputs output{a[8], a[9], st};
+    const at::Tensor given = output.given(0);
+    const at::ScalarType ot = dy.scalar_type(), dt = dtype_or(a[6], given.defined() ? given.scalar_type() : ot);
+    d.dtype = dtype_code(dt); d.out_dtype = dtype_code(ot);
+    std::vector<int64_t> shape = tokens.sizes().vec();
+    shape.push_back(d.width);
+    const Rows ry = rows_of(dy, ot, shape, "dy");
+    d.stride_out = ry.stride;
+    const int accumulate = PyObject_IsTrue(a[7]);
+    if (accumulate < 0) throw PythonError{};
+    if (accumulate && (!given.defined() || (positions > 0 && !output.given(1).defined()))) fail(PyExc_ValueError, "accumulate: expected tensors to add to as out");
+    const auto options = dy.options().dtype(dt);
+    const at::Tensor table = output(0, {d.vocab, d.width}, options), pos = positions > 0 ? output(1, {d.positions, d.width}, options) : at::Tensor();
+    check(table, dt, {d.vocab, d.width});
+    if (pos.defined()) check(pos, dt, {d.positions, d.width});
+    const size_t need = lib.embed_workspace_bytes(&d);
+    if (need == 0) check_status(std::isfinite(d.scale) ? FLARE_ERR_UNSUPPORTED : FLARE_ERR_INVALID_ARG, "flare_embed_backward");
+    const at::Tensor ws = scratch(need, dy, a[9], st);
+    check_status(unlocked([&] { return lib.embed_backward(&d, drop.get(), pt, ry.p, table.data_ptr(), pos.defined() ? pos.data_ptr() : nullptr, accumulate, ws.data_ptr(), need, st); }),
+                 "flare_embed_backward");
+    return named(a[10], output.wrapped({table, pos}));
+BINDING_END
+
+// What forward and backward of the loss share.
+struct Vocabulary {
+    flare_loss_desc_t d{};
+    std::vector<int64_t> rows_shape;
+    Rows rx, rw;
+    const void *labels;
+    at::ScalarType dt;
+    Vocabulary(const at::Tensor &x, const at::Tensor &w, const at::Tensor &l, PyObject *scale) : dt(x.scalar_type()) {
+        if (x.dim() < 1) fail(PyExc_ValueError, "x: expected shape (..., width), got " + shape_text(x.sizes()));
+        if (w.dim() != 2 || w.size(0) < 1 || w.size(0) > INT32_MAX || w.size(1) != x.size(-1))
+            fail(PyExc_ValueError, "w: expected shape (vocab, " + std::to_string(x.size(-1)) + "), got " + shape_text(w.sizes()));
+        rows_shape.assign(x.sizes().begin(), x.sizes().end() - 1);
+        d.width = width_of(x.size(-1), x.sizes());
+        d.rows = x.numel() / d.width; d.vocab = (int32_t)w.size(0); d.dtype = dtype_code(dt);
+        d.scale = (float)number(scale);
+        rx = rows_of(x, dt, x.sizes(), "x");
+        rw = rows_of(w, dt, w.sizes(), "w");
+        d.stride_x = rx.stride; d.stride_w = rw.stride;
+        if (l.sizes() != at::IntArrayRef(rows_shape)) fail(PyExc_ValueError, "labels: expected shape " + shape_text(rows_shape) + ", got " + shape_text(l.sizes()));
+        labels = numbers_of(l, d.label_bits, "labels");
+    }
+    size_t need(bool backward, const char *where) const {
+        const size_t n = lib.loss_workspace_bytes(&d, backward);
+        if (n == 0) check_status(d.scale > 0.f && std::isfinite(d.scale) && std::isfinite(d.dloss_scale) ? FLARE_ERR_UNSUPPORTED : FLARE_ERR_INVALID_ARG, where);
+        return n;
+    }
+};
+
+// x, w, labels, scale, out (loss, lse) or None, stream -> (loss, lse, workspace)
+BINDING(token_loss, 6)
+    const at::Tensor &x = tensor(a[0]);
+    const Vocabulary c(x, tensor(a[1]), tensor(a[2]), a[3]);
+    flare_stream_t st = stream_of(a[5]);
+    const Outputs output{a[4], a[5], st};
+    const auto f32 = x.options().dtype(at::kFloat);
+    const at::Tensor loss = output(0, c.rows_shape, f32), lse = output(1, c.rows_shape, f32);
+    check(loss, at::kFloat, c.rows_shape);
+    check(lse, at::kFloat, c.rows_shape);
+    const size_t need = c.need(false, "flare_loss_forward");
+    const at::Tensor ws = scratch(need, x, a[5], st);
+    check_status(unlocked([&] { return lib.loss_forward(&c.d, c.rx.p, c.rw.p, c.labels, (float *)loss.data_ptr(), (float *)lse.data_ptr(), ws.data_ptr(), need, st); }),
+                 "flare_loss_forward");
+    PyObject *r = output.wrapped({loss, lse});
+    return Py_BuildValue("(NN)", r, wrap(ws));
+BINDING_END
+
+// x, w, labels, lse, dloss (a tensor or a number), scale, out (dx, dw) or None, stream, class of the result -> ((dx, dw), workspace)
+BINDING(token_loss_backward, 9)
+    const at::Tensor &x = tensor(a[0]), &w = tensor(a[1]);
+    Vocabulary c(x, w, tensor(a[2]), a[5]);
+    const at::Tensor &lse = tensor(a[3]);
+    check(lse, at::kFloat, c.rows_shape);
+    const float *dloss = nullptr;
+    c.d.dloss_scale = 1.f;
+    if (THPVariable_Check(a[4])) {
+        const at::Tensor &t = THPVariable_Unpack(a[4]);
+        check(t, at::kFloat, c.rows_shape);
+        dloss = (const float *)t.data_ptr();
+    } else {
+        c.d.dloss_scale = (float)number(a[4]);
+    }
+    flare_stream_t st = stream_of(a[7]);
+    const Outputs output{a[6], a[7], st};
+    const at::Tensor dx = output(0, x.sizes(), x.options()), dw = output(1, w.sizes(), w.options());
+    const Rows rdx = rows_of(dx, c.dt, x.sizes(), "dx"), rdw = rows_of(dw, c.dt, w.sizes(), "dw");
+    c.d.stride_dx = rdx.stride; c.d.stride_dw = rdw.stride;
+    const size_t need = c.need(true, "flare_loss_backward");
+    const at::Tensor ws = scratch(need, x, a[7], st);
+    check_status(unlocked([&] { return lib.loss_backward(&c.d, c.rx.p, c.rw.p, c.labels, (const float *)lse.data_ptr(), dloss, rdx.p, rdw.p, ws.data_ptr(), need, st); }),
+                 "flare_loss_backward");
+    PyObject *r = named(a[8], output.wrapped({dx, dw}));
+    return Py_BuildValue("(NN)", r, wrap(ws));
+BINDING_END
+
 // bind(addresses: dict name -> int, FlareError)
 BINDING(bind, 2)
     auto get = [&](const char *name, auto &slot) {
@@ -828,6 +1072,14 @@ BINDING(bind, 2)
     get("flare_orthogonalize_workspace_bytes", lib.orthogonalize_workspace_bytes);
     get("flare_orthogonalize", lib.orthogonalize);
     get("flare_muon_update", lib.muon_update);
+    get("flare_dropout_forward", lib.dropout_forward);
+    get("flare_dropout_backward", lib.dropout_backward);
+    get("flare_embed_forward", lib.embed_forward);
+    get("flare_embed_workspace_bytes", lib.embed_workspace_bytes);
+    get("flare_embed_backward", lib.embed_backward);
+    get("flare_loss_workspace_bytes", lib.loss_workspace_bytes);
+    get("flare_loss_forward", lib.loss_forward);
+    get("flare_loss_backward", lib.loss_backward);
     Py_INCREF(a[1]);
     flare_error = a[1];
 BINDING_END
@@ -836,7 +1088,8 @@ BINDING_END
 PyMethodDef methods[] = {METHOD(bind), METHOD(encode), METHOD(encode_static_scratch), METHOD(decode), METHOD(forward), METHOD(backward),
                          METHOD(forward_host), METHOD(forward_variant), METHOD(backward_variant), METHOD(spectral_gram), METHOD(spectral_eig),
                          METHOD(call_forward), METHOD(call_forward_backward), METHOD(block_norm), METHOD(block_norm_backward), METHOD(block_join),
-                         METHOD(block_join_backward), METHOD(orthogonalize), METHOD(muon_update), {nullptr, nullptr, 0, nullptr}};
+                         METHOD(block_join_backward), METHOD(orthogonalize), METHOD(muon_update), METHOD(dropout), METHOD(dropout_backward),
+                         METHOD(embed), METHOD(embed_backward), METHOD(token_loss), METHOD(token_loss_backward), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_binding", "Argument marshalling for libflare.", -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -1,0 +1,280 @@
+// The loss over a vocabulary: argument checks, plan, workspace, launches.
+#include "flare_host.h"
+#include "flare_loss.cuh"
+
+namespace flare {
+namespace {
+
+size_t size_of(int dtype) { return dtype == FLARE_DTYPE_F32 ? 4 : 2; }
+bool natural(const void *p, size_t size) { return reinterpret_cast<uintptr_t>(p) % size == 0; }
+
+int need_device() {
+    const DeviceView di = device_info();
+    if (di.checked == -2) {
+        snprintf(g_cuda_error, sizeof(g_cuda_error), "no CUDA device");
+        return FLARE_ERR_CUDA;
+    }
+    return di.checked == 1 ? FLARE_OK : FLARE_ERR_ARCH;
+}
+
+int check_loss(const flare_loss_desc_t *d) {
+    if (d == nullptr || d->rows < 0 || d->width <= 0 || d->vocab <= 0) return FLARE_ERR_INVALID_ARG;
+    if (d->label_bits != 32 && d->label_bits != 64) return FLARE_ERR_INVALID_ARG;
+    if (!(d->scale > 0.f) || !std::isfinite(d->scale) || !std::isfinite(d->dloss_scale)) return FLARE_ERR_INVALID_ARG;
+    for (int64_t s : {d->stride_x, d->stride_w, d->stride_dx, d->stride_dw})
+        if (s != 0 && s < d->width) return FLARE_ERR_INVALID_ARG;
+    if (d->dtype != FLARE_DTYPE_F32 && d->dtype != FLARE_DTYPE_BF16 && d->dtype != FLARE_DTYPE_F16) return FLARE_ERR_UNSUPPORTED;
+    return d->rows > (1 << 30) || d->width > 16384 || d->vocab > (1 << 28) ? FLARE_ERR_UNSUPPORTED : FLARE_OK;
+}
+
+// G of a piece of the vocabulary takes this much scratch (or 256 words of it where that is more).
+constexpr size_t kPieceBytes = 256u << 20;
+struct LossPlan {
+    int planes, Cp, chunks, x_blocks, w_blocks, pairs;
+    long cap;
+    int width;                   // of a tile of X W^T
+    int Vp, pieces;              // words of a piece
+    int grad_width, tiles_c;
+};
+// Columns of a tile of X W^T.  Tiles of 128 take some 0.6 of the time of one of 256 (they read as many rows), which pays where they fill the last
+// round of pairs better.
+int tile_width(long row_tiles, long words, int pairs) {
+    const long wide = row_tiles * ((words + 255) / 256), narrow = row_tiles * ((words + 127) / 128);
+    return 0.6 * (double)((narrow + pairs - 1) / pairs) < (double)((wide + pairs - 1) / pairs) ? 128 : 256;
+}
+LossPlan loss_plan(const flare_loss_desc_t *d, int sms) {
+    LossPlan p{};
+    const bool f32 = d->dtype == FLARE_DTYPE_F32;
+    p.planes = f32 ? 2 : 1;
+    p.Cp = (d->width + 7) / 8 * 8;
+    p.chunks = (int)((d->rows + kLossChunk - 1) / kLossChunk);
+    p.pairs = std::max(1, sms / 2);
+    p.cap = std::max(1L, (long)(d->rows + 255) / 256) * 256;
+    p.width = tile_width(p.cap / 256, d->vocab, p.pairs);
+    if (f32) {
+        auto blocks = [&](long rows) { return (int)std::max(1L, std::min(4L * sms, (rows * d->width / 4096 + 7) / 8)); };
+        p.x_blocks = blocks(d->rows);
+        p.w_blocks = blocks(d->vocab);
+    }
+    const long words = ((long)d->vocab + 255) / 256 * 256, most = std::max(256L, (long)(kPieceBytes / (2 * p.planes * p.cap)) / 256 * 256);
+    p.pieces = (int)((words + most - 1) / most);
+    p.Vp = (int)((words / 256 + p.pieces - 1) / p.pieces * 256);
+    p.pieces = (int)((words + p.Vp - 1) / p.Vp);
+    // (a width that 256 does not divide well is worked off in 128s, which take 0.6 each)
+    p.grad_width = 1.2 * ((d->width + 127) / 128) < 2.0 * ((d->width + 255) / 256) ? 128 : 256;
+    p.tiles_c = (d->width + p.grad_width - 1) / p.grad_width;
+    return p;
+}
+struct LossLayout { size_t info, rank, chunk, largest, px, pd, pw, index, label, part, chosen, lse2, coef, g, acc, slots, total; };
+LossLayout loss_layout(const flare_loss_desc_t *d, const LossPlan &p, bool backward) {
+    LossLayout w{};
+    size_t off = kHeaderBytes;
+    auto take = [&](size_t &at, size_t bytes) { at = off; off += align_up(bytes); };
+    take(w.info, sizeof(LossInfo));
+    take(w.rank, sizeof(int) * (size_t)d->rows);
+    take(w.chunk, sizeof(LossChunk) * (size_t)p.chunks);
+    take(w.largest, sizeof(float) * (size_t)(p.x_blocks + p.w_blocks));
+    const size_t row = sizeof(uint16_t) * (size_t)p.planes * p.Cp;
+    take(w.px, row * p.cap);
+    take(w.pw, row * d->vocab);                               // (whether W can be taken as it stands is known with its address)
+    take(w.index, sizeof(int) * (size_t)p.cap);
+    take(w.label, sizeof(int) * (size_t)p.cap);
+    if (!backward) {
+        const long tiles = (d->vocab + p.width - 1) / p.width;
+        take(w.part, sizeof(float2) * 2 * (size_t)tiles * p.cap);
+        take(w.chosen, sizeof(float) * (size_t)p.cap);
+    } else {
+        take(w.pd, d->dtype == FLARE_DTYPE_BF16 ? 0 : row * p.cap);
+        take(w.lse2, sizeof(float) * (size_t)p.cap);
+        take(w.coef, sizeof(float) * (size_t)p.cap);
+        take(w.g, sizeof(uint16_t) * (size_t)p.planes * p.cap * p.Vp);
+        take(w.acc, p.pieces > 1 ? sizeof(float) * (size_t)p.cap * p.tiles_c * p.grad_width : 0);
+        take(w.slots, sizeof(float) * 4 * (size_t)p.pairs * p.grad_width * 128);
+    }
+    w.total = off;
+    return w;
+}
+
+// 16-bit elements [planes, rows, cols], rows `ld` apart, in boxes of 64 columns (128-byte swizzle).
+int make_plane_map(CUtensorMap *m, const void *base, bool bf16, long cols, long rows, long planes, long ld, int box_rows) {
+    EncodeTiledFn fn = encode_tiled_fn();
+    if (!fn) {
+        snprintf(g_cuda_error, sizeof(g_cuda_error), "cuTensorMapEncodeTiled not available");
+        return FLARE_ERR_CUDA;
+    }
+    cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)planes};
+    cuuint64_t strides[2] = {(cuuint64_t)ld * 2, (cuuint64_t)ld * 2 * (cuuint64_t)rows};
+    cuuint32_t box[3] = {64, (cuuint32_t)box_rows, 1}, estr[3] = {1, 1, 1};
+    const CUresult r = fn(m, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void *>(base), dims, strides, box, estr,
+                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) {
+        snprintf(g_cuda_error, sizeof(g_cuda_error), "cuTensorMapEncodeTiled(loss) failed: %d", (int)r);
+        return FLARE_ERR_CUDA;
+    }
+    return FLARE_OK;
+}
+
+template <int kKind, int kPlanes, typename E>
+int launch_loss(const LossMaps &maps, const LossArgs &a, int pairs, cudaStream_t st) {
+    static std::atomic<uint64_t> opt_in{0};
+    auto *kernel = loss_kernel<kKind, kPlanes, E>;
+    if (int rc = ensure_big_smem(kernel, opt_in, (int)kLossSmem)) return rc;
+    cudaLaunchAttribute attr[2] = {};
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = 2; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(2 * (unsigned)pairs);
+    cfg.blockDim = kLossThreads; cfg.dynamicSmemBytes = kLossSmem; cfg.stream = st;
+    cfg.attrs = attr; cfg.numAttrs = 2;
+    FLARE_CUDA(cudaLaunchKernelEx(&cfg, kernel, maps, a));
+    return FLARE_OK;
+}
+
+template <typename T>
+int launch_pack(const LossPack &k, int blocks, cudaStream_t st) {
+    FLARE_CUDA(launch_after(loss_pack_kernel<T>, (unsigned)blocks, kPackThreads, 0, st, k));
+    return FLARE_OK;
+}
+
+// Checks that forward and backward share.
+int check_loss_call(const flare_loss_desc_t *d, const void *x, const void *w, const void *labels, void *workspace, size_t workspace_bytes, bool backward) {
+    const size_t t = size_of(d->dtype);
+    if (!workspace || !aligned16(workspace) || !w || (d->rows > 0 && (!x || !labels))) return FLARE_ERR_INVALID_ARG;
+    if (!natural(x, t) || !natural(w, t) || !natural(labels, d->label_bits / 8)) return FLARE_ERR_INVALID_ARG;
+    if (int rc = need_device()) return rc;
+    return workspace_bytes < loss_layout(d, loss_plan(d, device_info().sms), backward).total ? FLARE_ERR_WORKSPACE_TOO_SMALL : FLARE_OK;
+}
+
+// Scan and packing, and the maps of X and W; what only the backward has is in k already.
+int prepare_loss(const flare_loss_desc_t *d, const LossPlan &p, const LossLayout &l, char *ws, const void *x, const void *w, const void *labels, LossPack k, LossMaps *maps,
+                 LossArgs *a, cudaStream_t st) {
+    const bool f32 = d->dtype == FLARE_DTYPE_F32, bf16 = d->dtype == FLARE_DTYPE_BF16;
+    const long ld_x = d->stride_x ? d->stride_x : d->width, ld_w = d->stride_w ? d->stride_w : d->width;
+    const bool own_w = f32 || !aligned16(w) || ld_w % 8 != 0;
+    LossScan s{};
+    s.labels = labels; s.wide = d->label_bits == 64; s.rows = d->rows; s.V = d->vocab; s.C = d->width;
+    s.chunks = p.chunks; s.x_blocks = p.x_blocks; s.w_blocks = p.w_blocks; s.dloss = bf16 ? nullptr : k.dloss;
+    s.rank = reinterpret_cast<int *>(ws + l.rank); s.chunk = reinterpret_cast<LossChunk *>(ws + l.chunk);
+    s.x = static_cast<const float *>(x); s.w = static_cast<const float *>(w); s.ld_x = ld_x; s.ld_w = ld_w;
+    s.largest = reinterpret_cast<float *>(ws + l.largest);
+    s.status = reinterpret_cast<uint32_t *>(ws);
+    FLARE_CUDA(launch_after(loss_scan_kernel, (unsigned)(p.chunks + p.x_blocks + p.w_blocks), kScanThreads, 0, st, s));
+    k.labels = labels; k.x = x; k.w = w; k.wide = s.wide; k.rows = d->rows; k.cap = p.cap; k.ld_x = ld_x; k.ld_w = ld_w;
+    k.w_rows = own_w ? d->vocab : 0; k.C = d->width; k.Cp = p.Cp; k.V = d->vocab; k.chunks = p.chunks; k.x_blocks = p.x_blocks; k.w_blocks = p.w_blocks;
+    k.pack_blocks = (int)((d->rows + kPackRows - 1) / kPackRows);
+    k.rank = s.rank; k.chunk = s.chunk; k.largest = s.largest;
+    k.info = reinterpret_cast<LossInfo *>(ws + l.info);
+    k.px = reinterpret_cast<uint16_t *>(ws + l.px); k.pw = reinterpret_cast<uint16_t *>(ws + l.pw);
+    k.index = reinterpret_cast<int *>(ws + l.index); k.label = reinterpret_cast<int *>(ws + l.label);
+    const int blocks = k.pack_blocks + (int)std::min<long>((k.w_rows + 31) / 32, 16L * device_info().sms);
+    if (int rc = f32 ? launch_pack<float>(k, blocks, st) : bf16 ? launch_pack<__nv_bfloat16>(k, blocks, st) : launch_pack<__half>(k, blocks, st)) return rc;
+    int rc;
+    if ((rc = make_plane_map(&maps->x, k.px, bf16, p.Cp, p.cap, p.planes, p.Cp, 64)) != FLARE_OK) return rc;
+    if ((rc = own_w ? make_plane_map(&maps->w, k.pw, bf16, p.Cp, d->vocab, p.planes, p.Cp, 64)
+                    : make_plane_map(&maps->w, w, bf16, d->width, d->vocab, 1, ld_w, 64)) != FLARE_OK)
+        return rc;
+    a->info = k.info; a->status = s.status; a->C = d->width; a->V = d->vocab; a->bf16 = bf16; a->cap = p.cap; a->scale = d->scale;
+    a->label = k.label; a->index = k.index;
+    return FLARE_OK;
+}
+
+}  // namespace
+}  // namespace flare
+
+using namespace flare;
+
+extern "C" {
+
+size_t flare_loss_workspace_bytes(const flare_loss_desc_t *desc, int32_t backward) {
+    if (check_loss(desc) != FLARE_OK) return 0;
+    return loss_layout(desc, loss_plan(desc, device_info().sms), backward != 0).total;
+}
+
+int flare_loss_forward(const flare_loss_desc_t *desc, const void *x, const void *w, const void *labels, float *loss, float *lse, void *workspace, size_t workspace_bytes,
+                       flare_stream_t stream) {
+    if (int rc = check_loss(desc)) return rc;
+    if (desc->rows > 0 && (!loss || !lse || !natural(loss, 4) || !natural(lse, 4))) return FLARE_ERR_INVALID_ARG;
+    if (int rc = check_loss_call(desc, x, w, labels, workspace, workspace_bytes, false)) return rc;
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    if (desc->rows == 0) {
+        FLARE_CUDA(cudaMemsetAsync(workspace, 0, kHeaderBytes, st));
+        return FLARE_OK;
+    }
+    const LossPlan p = loss_plan(desc, device_info().sms);
+    const LossLayout l = loss_layout(desc, p, false);
+    char *ws = static_cast<char *>(workspace);
+    LossPack k{};
+    k.loss = loss; k.lse = lse;
+    LossMaps maps{};
+    LossArgs a{};
+    if (int rc = prepare_loss(desc, p, l, ws, x, w, labels, k, &maps, &a, st)) return rc;
+    a.words = desc->vocab; a.width = p.width; a.tiles_v = (desc->vocab + p.width - 1) / p.width;
+    a.part = reinterpret_cast<float2 *>(ws + l.part); a.chosen = reinterpret_cast<float *>(ws + l.chosen);
+    const int pairs = (int)std::min<long>(p.pairs, p.cap / 256 * a.tiles_v);
+    if (int rc = p.planes == 2 ? launch_loss<kLossStats, 2, float>(maps, a, pairs, st) : launch_loss<kLossStats, 1, float>(maps, a, pairs, st)) return rc;
+    LossMerge m{};
+    m.info = a.info; m.part = a.part; m.chosen = a.chosen; m.index = a.index; m.cap = p.cap; m.parts = 2 * a.tiles_v; m.loss = loss; m.lse = lse;
+    FLARE_CUDA(launch_after(loss_merge_kernel, (unsigned)std::min<long>((desc->rows + 31) / 32, 65535L), 32 * kMergeWarps, 0, st, m));
+    return FLARE_OK;
+}
+
+int flare_loss_backward(const flare_loss_desc_t *desc, const void *x, const void *w, const void *labels, const float *lse, const float *dloss, void *dx, void *dw,
+                        void *workspace, size_t workspace_bytes, flare_stream_t stream) {
+    if (int rc = check_loss(desc)) return rc;
+    const size_t t = size_of(desc->dtype);
+    if ((!dx && !dw) || (desc->rows > 0 && !lse) || !natural(lse, 4) || !natural(dloss, 4) || !natural(dx, t) || !natural(dw, t)) return FLARE_ERR_INVALID_ARG;
+    if (int rc = check_loss_call(desc, x, w, labels, workspace, workspace_bytes, true)) return rc;
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    const long ld_dx = desc->stride_dx ? desc->stride_dx : desc->width, ld_dw = desc->stride_dw ? desc->stride_dw : desc->width;
+    if (desc->rows == 0) {
+        FLARE_CUDA(cudaMemsetAsync(workspace, 0, kHeaderBytes, st));
+        if (dw) FLARE_CUDA(cudaMemset2DAsync(dw, ld_dw * t, 0, desc->width * t, desc->vocab, st));
+        return FLARE_OK;
+    }
+    const LossPlan p = loss_plan(desc, device_info().sms);
+    const LossLayout l = loss_layout(desc, p, true);
+    const bool bf16 = desc->dtype == FLARE_DTYPE_BF16, f32 = desc->dtype == FLARE_DTYPE_F32;
+    char *ws = static_cast<char *>(workspace);
+    LossPack k{};
+    k.lse_in = lse; k.dloss = dloss; k.mult = desc->scale * desc->dloss_scale;
+    k.lse2 = reinterpret_cast<float *>(ws + l.lse2); k.coef = reinterpret_cast<float *>(ws + l.coef);
+    k.dx = dx; k.ld_dx = ld_dx;
+    k.pd = bf16 || !dloss || !dw ? nullptr : reinterpret_cast<uint16_t *>(ws + l.pd);
+    LossMaps maps{};
+    LossArgs a{};
+    if (int rc = prepare_loss(desc, p, l, ws, x, w, labels, k, &maps, &a, st)) return rc;
+    int rc;
+    if (k.pd) {
+        if ((rc = make_plane_map(&maps.d, k.pd, bf16, p.Cp, p.cap, p.planes, p.Cp, 64)) != FLARE_OK) return rc;
+    } else {
+        maps.d = maps.x;
+    }
+    if ((rc = make_plane_map(&maps.g, ws + l.g, bf16, p.Vp, p.cap, p.planes, p.Vp, 64)) != FLARE_OK) return rc;
+    if ((rc = make_plane_map(&maps.g_store, ws + l.g, bf16, p.Vp, p.cap, p.planes, p.Vp, 32)) != FLARE_OK) return rc;
+    a.lse2 = k.lse2; a.coef = k.coef; a.grad_width = p.grad_width; a.tiles_c = p.tiles_c;
+    a.dw = dw; a.dx = dx; a.ld_dw = ld_dw; a.ld_dx = ld_dx;
+    auto fours = [&](const void *q, long ld) { return desc->width % 4 == 0 && ld % 4 == 0 && reinterpret_cast<uintptr_t>(q) % (4 * t) == 0; };
+    a.dw_fours = fours(dw, ld_dw); a.dx_fours = fours(dx, ld_dx);
+    a.dw_factor = k.mult / 32768.f;
+    a.acc = reinterpret_cast<float *>(ws + l.acc); a.slots = reinterpret_cast<float *>(ws + l.slots);
+    auto weights = f32 ? launch_loss<kLossWeights, 2, float> : launch_loss<kLossWeights, 1, float>;
+    auto grads = f32 ? launch_loss<kLossGrads, 2, float> : bf16 ? launch_loss<kLossGrads, 1, __nv_bfloat16> : launch_loss<kLossGrads, 1, __half>;
+    auto *join = f32 ? loss_join_kernel<float> : bf16 ? loss_join_kernel<__nv_bfloat16> : loss_join_kernel<__half>;
+    // tiles that several pairs can have shared: fewer than a round of either gradient
+    const long rest = 2L * (p.pairs - 1), warps = rest * 8 * (p.grad_width / 32);
+    for (int i = 0; i < p.pieces; ++i) {
+        a.v0 = i * p.Vp;
+        a.words = std::min(p.Vp, desc->vocab - a.v0);
+        a.first = i == 0; a.last = i + 1 == p.pieces;
+        a.width = tile_width(p.cap / 256, a.words, p.pairs);
+        a.tiles_v = (a.words + a.width - 1) / a.width;
+        if ((rc = weights(maps, a, (int)std::min<long>(p.pairs, p.cap / 256 * a.tiles_v), st)) != FLARE_OK) return rc;
+        if ((rc = grads(maps, a, p.pairs, st)) != FLARE_OK) return rc;
+        FLARE_CUDA(launch_after(join, (unsigned)((warps + kJoinWarps - 1) / kJoinWarps), 32 * kJoinWarps, 0, st, a, p.pairs));
+    }
+    return FLARE_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,825 @@
+// Softmax cross entropy of rows projected onto a vocabulary, and its gradients, without the logits.
+//
+//     l[n, v] = scale x_n . w_v;   lse_n = log sum_v exp l[n, v];   loss_n = lse_n - l[n, label_n]
+//     q[n, v] = exp(l[n, v] - lse_n) - [v = label_n];   dX_n = dloss_n scale sum_v q[n, v] w_v;   dW_v = scale sum_n dloss_n q[n, v] x_n
+//
+// Four matrix products of rows x width x vocabulary (X W^T forward, X W^T again, G^T X and G W backward), of which the logits would be the largest
+// matrix by far: 2.1 GB in bfloat16 for 8192 rows and 128256 words, where X and W are 17 and 263 MB.  Forward they stay in tensor memory: a tile's end takes
+// them from there to a maximum and a sum of exponentials per row.  Backward they are formed again, a piece of the vocabulary at a time: G, the piece of q in 16
+// bits, is written to scratch (bounded), and one launch takes both products from it.  The fourth product is what keeping no logits costs.
+//
+// Rows without a label are left out, not multiplied by zero: the rows that have one are packed, in their order, before anything else (loss_scan_kernel,
+// loss_pack_kernel), their number stays on the device, and all products run over packed rows.  So a padded batch takes the time of its labelled rows, and
+// nothing that stands in the others can reach a gradient.  The pass costs two bytes in and out per element of X, and leaves rows that TMA can take whatever stride and alignment X has.
+//
+// Every product is the same kernel (loss_kernel): pairs of blocks, tiles of 256 x 256 (or 256 x 128), operands by TMA, sums in tensor memory twice over so
+// that a tile's end runs under the next tile's products.  It is bound by the tensor pipe.
+//
+// bfloat16 and float16 are multiplied as they are, G in the same type: bfloat16's holds dloss scale q (rounded once, 2^-9, as the gradients themselves will be); float16's
+// q times 2^15, so that probabilities down to 2^-29 are normal numbers, and dloss goes into X (scaled so that the largest is one) and into dX's rows.
+// float32: X, W, G as two float16 halves each (22 bits; X and W times a power of two that puts their largest near 2^15, held down to 2^-39 of it), a
+// product as three, and sums leave tensor memory, which truncates, every 256 of K to be added up in registers.
+#pragma once
+
+#include "flare_common.cuh"
+#include "flare_ptx.cuh"
+
+namespace flare {
+
+// What the packing leaves for the kernels behind it, on the device.
+struct LossInfo {
+    uint32_t rows;               // with a label
+    float x_scale, w_scale;      // of the halves (1 but for float32)
+    float dmax;                  // largest |dloss| of a row (float16, float32), or 1
+};
+// Per 1024 rows.
+struct LossChunk { uint32_t rows; float dmax; };
+
+__device__ __forceinline__ int64_t label_at(const void *labels, int wide, long n) {
+    return wide ? static_cast<const int64_t *>(labels)[n] : (int64_t) static_cast<const int32_t *>(labels)[n];
+}
+
+constexpr int kLossChunk = 1024, kScanThreads = 256;
+struct LossScan {
+    const void *labels;
+    int wide;
+    long rows;
+    int V, C, chunks, x_blocks, w_blocks;     // blocks beyond the chunks' look for the largest |x| of labelled rows and |w| (float32)
+    const float *dloss;                       // or null
+    int *rank;                                // [rows]: among the labelled rows of its chunk, or -1
+    LossChunk *chunk;
+    const float *x, *w;
+    long ld_x, ld_w;
+    float *largest;                           // [x_blocks + w_blocks]
+    uint32_t *status;
+};
+__device__ __forceinline__ float finite_abs(float v) { return fabsf(v) <= 3.4028234e38f ? fabsf(v) : 0.f; }
+__device__ __forceinline__ float block_max(float v, float *shared) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+    if ((threadIdx.x & 31) == 0) shared[threadIdx.x >> 5] = v;
+    __syncthreads();
+    v = 0.f;
+    for (int w = 0; w < (int)blockDim.x / 32; ++w) v = fmaxf(v, shared[w]);
+    __syncthreads();
+    return v;
+}
+__global__ void __launch_bounds__(kScanThreads) loss_scan_kernel(const LossScan a) {
+    __shared__ float shared[32];
+    __shared__ uint32_t before[33];
+    ptx::grid_launch();
+    ptx::grid_wait();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (blockIdx.x == 0 && threadIdx.x < kHeaderBytes / 4) a.status[threadIdx.x] = 0;
+    if ((int)blockIdx.x >= a.chunks) {
+        const int b = blockIdx.x - a.chunks;
+        const bool of_x = b < a.x_blocks;
+        const float *m = of_x ? a.x : a.w;
+        const long rows = of_x ? a.rows : a.V, ld = of_x ? a.ld_x : a.ld_w, step = (long)(of_x ? a.x_blocks : a.w_blocks) * (kScanThreads / 32);
+        float most = 0.f;
+        for (long r = (long)(of_x ? b : b - a.x_blocks) * (kScanThreads / 32) + warp; r < rows; r += step) {
+            if (of_x) {
+                const int64_t label = label_at(a.labels, a.wide, r);
+                if (label < 0 || label >= a.V) continue;
+            }
+#pragma unroll 4
+            for (int c = lane; c < a.C; c += 32) most = fmaxf(most, finite_abs(m[r * ld + c]));
+        }
+        most = block_max(most, shared);
+        if (threadIdx.x == 0) a.largest[b] = most;
+        return;
+    }
+    // four times 256 rows of the chunk, in order
+    float most = 0.f;
+    bool there[kLossChunk / kScanThreads];
+#pragma unroll
+    for (int k = 0; k < kLossChunk / kScanThreads; ++k) {
+        const long n = (long)blockIdx.x * kLossChunk + k * kScanThreads + threadIdx.x;
+        there[k] = false;
+        if (n < a.rows) {
+            const int64_t label = label_at(a.labels, a.wide, n);
+            there[k] = label >= 0 && label < a.V;
+            if (there[k] && a.dloss) most = fmaxf(most, finite_abs(a.dloss[n]));
+        }
+        const uint32_t m = __ballot_sync(0xffffffffu, there[k]);
+        if (lane == 0) before[k * (kScanThreads / 32) + warp] = __popc(m);
+    }
+    __syncthreads();
+    if (warp == 0) {
+        const uint32_t own = before[lane];
+        uint32_t sum = own;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const uint32_t up = __shfl_up_sync(0xffffffffu, sum, o);
+            if (lane >= o) sum += up;
+        }
+        before[lane] = sum - own;
+        if (lane == 31) before[32] = sum;
+    }
+    most = block_max(most, shared);
+    if (threadIdx.x == 0) a.chunk[blockIdx.x] = LossChunk{before[32], most};
+#pragma unroll
+    for (int k = 0; k < kLossChunk / kScanThreads; ++k) {
+        const long n = (long)blockIdx.x * kLossChunk + k * kScanThreads + threadIdx.x;
+        const uint32_t m = __ballot_sync(0xffffffffu, there[k]);
+        if (n < a.rows) a.rank[n] = there[k] ? (int)(before[k * (kScanThreads / 32) + warp] + __popc(m & ((1u << lane) - 1))) : -1;
+    }
+}
+
+struct LossPack {
+    const void *labels, *x, *w;
+    int wide;
+    long rows, cap, ld_x, ld_w, w_rows;       // cap: rows up to whole tiles; w_rows: of W to be packed too (0: it is taken as it stands)
+    int C, Cp, V, chunks, x_blocks, w_blocks, pack_blocks;   // Cp: C up to a multiple of eight
+    const int *rank;
+    const LossChunk *chunk;
+    const float *largest;
+    LossInfo *info;
+    uint16_t *px, *pd, *pw;                   // packed X, packed dloss X (or null), packed W: planes of [cap][Cp], [V][Cp]
+    int *index, *label;                       // of packed rows: row, label
+    // forward
+    float *loss, *lse;                        // 0 where there is no label
+    // backward
+    const float *lse_in, *dloss;
+    float mult;                               // on dloss
+    float *lse2, *coef;                       // of packed rows: lse / ln 2; what q (bfloat16) or dX (else) is multiplied by
+    void *dx;                                 // rows without a label: zeros
+    long ld_dx;
+};
+constexpr int kPackRows = 32, kPackThreads = 256;
+
+// The power of two that puts `most` between 2^14 and 2^15.
+__device__ __forceinline__ float half_scale(float most) {
+    if (!(most > 0.f)) return 1.f;
+    int e;
+    frexpf(most, &e);                         // most < 2^e
+    return ldexpf(1.f, min(max(15 - e, -60), 60));
+}
+template <typename T> __device__ __forceinline__ uint16_t bits16(float v) {
+    T t;
+    from_f32(t, v);
+    return *reinterpret_cast<const uint16_t *>(&t);
+}
+// A row's columns, eight a lane, times f, into its planes.  T: float32 into two float16 halves, else the type itself.
+template <typename T>
+__device__ __forceinline__ void pack_row(const T *row, bool vec, int C, int Cp, float f, bool scaled, uint16_t *out, long plane) {
+    for (int c = (threadIdx.x & 31) * 8; c < Cp; c += 256) {
+        float v[8];
+        __align__(16) T e[8];
+        if (vec) {
+#pragma unroll
+            for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4 *>(e)[i] = reinterpret_cast<const uint4 *>(row + c)[i];
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (c + i < C) e[i] = row[c + i];
+                else from_f32(e[i], 0.f);
+        }
+        __align__(16) uint16_t h[8], l[8];
+        if constexpr (sizeof(T) == 2) {
+            if (!scaled) {
+                *reinterpret_cast<uint4 *>(out + c) = *reinterpret_cast<const uint4 *>(e);
+                continue;
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) h[i] = bits16<T>(to_f32(e[i]) * f);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                v[i] = e[i] * f;
+                const __half hi = __float2half_rn(v[i]);
+                h[i] = __half_as_ushort(hi);
+                l[i] = __half_as_ushort(__float2half_rn(v[i] - __half2float(hi)));
+            }
+            *reinterpret_cast<uint4 *>(out + plane + c) = *reinterpret_cast<const uint4 *>(l);
+        }
+        *reinterpret_cast<uint4 *>(out + c) = *reinterpret_cast<const uint4 *>(h);
+    }
+}
+template <typename T>
+__global__ void __launch_bounds__(kPackThreads) loss_pack_kernel(const LossPack a) {
+    __shared__ float shared[32];
+    __shared__ uint32_t sums[2][kPackThreads / 32];
+    ptx::grid_launch();
+    ptx::grid_wait();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    constexpr bool kHalves = sizeof(T) == 4;
+    float sx = 1.f, sw = 1.f;
+    if constexpr (kHalves) {
+        float mx = 0.f, mw = 0.f;
+        for (int i = threadIdx.x; i < a.x_blocks; i += kPackThreads) mx = fmaxf(mx, a.largest[i]);
+        for (int i = threadIdx.x; i < a.w_blocks; i += kPackThreads) mw = fmaxf(mw, a.largest[a.x_blocks + i]);
+        sx = half_scale(block_max(mx, shared));
+        sw = half_scale(block_max(mw, shared));
+    }
+    if ((int)blockIdx.x >= a.pack_blocks) {                   // W
+        const long step = (long)(gridDim.x - a.pack_blocks) * (kPackThreads / 32);
+        const T *w = static_cast<const T *>(a.w);
+        const bool vec = a.C % 8 == 0 && a.ld_w * (long)sizeof(T) % 16 == 0 && (reinterpret_cast<uintptr_t>(w) & 15) == 0;
+        for (long r = (long)(blockIdx.x - a.pack_blocks) * (kPackThreads / 32) + warp; r < a.w_rows; r += step)
+            pack_row(w + r * a.ld_w, vec, a.C, a.Cp, sw, kHalves, a.pw + r * a.Cp, a.w_rows * a.Cp);
+        return;
+    }
+    // labelled rows before this block's chunk, and in all
+    const long n0 = (long)blockIdx.x * kPackRows;
+    const int chunk = (int)(n0 / kLossChunk);
+    uint32_t base = 0, total = 0;
+    float dmax = 0.f;
+    for (int i = threadIdx.x; i < a.chunks; i += kPackThreads) {
+        const LossChunk c = a.chunk[i];
+        total += c.rows;
+        if (i < chunk) base += c.rows;
+        dmax = fmaxf(dmax, c.dmax);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        base += __shfl_xor_sync(0xffffffffu, base, o);
+        total += __shfl_xor_sync(0xffffffffu, total, o);
+    }
+    if (lane == 0) { sums[0][warp] = base; sums[1][warp] = total; }
+    __syncthreads();
+    base = total = 0;
+    for (int w = 0; w < kPackThreads / 32; ++w) { base += sums[0][w]; total += sums[1][w]; }
+    dmax = block_max(dmax, shared);
+    if (!a.dloss || !(dmax > 0.f)) dmax = 1.f;
+    if (blockIdx.x == 0 && threadIdx.x == 0) *a.info = LossInfo{total, sx, sw, dmax};
+    const T *x = static_cast<const T *>(a.x);
+    const bool vec = a.C % 8 == 0 && a.ld_x * (long)sizeof(T) % 16 == 0 && (reinterpret_cast<uintptr_t>(x) & 15) == 0;
+    const long plane = a.cap * a.Cp;
+    for (int k = warp; k < kPackRows && n0 + k < a.rows; k += kPackThreads / 32) {
+        const long n = n0 + k;
+        const int rank = a.rank[n];
+        if (rank < 0) {
+            if (a.loss) {
+                if (lane == 0) { a.loss[n] = 0.f; a.lse[n] = 0.f; }
+            } else if (a.dx) {
+                T *dx = static_cast<T *>(a.dx) + n * a.ld_dx;
+                T zero;
+                from_f32(zero, 0.f);
+                for (int c = lane; c < a.C; c += 32) dx[c] = zero;
+            }
+            continue;
+        }
+        const long to = (long)base + rank;
+        pack_row(x + n * a.ld_x, vec, a.C, a.Cp, sx, kHalves, a.px + to * a.Cp, plane);
+        if (a.loss == nullptr) {
+            const float d = a.dloss ? a.dloss[n] : 1.f;
+            if (a.pd) pack_row(x + n * a.ld_x, vec, a.C, a.Cp, sx * (d / dmax), true, a.pd + to * a.Cp, plane);
+            if (lane == 0) {
+                a.lse2[to] = a.lse_in[n] * 1.4426950408889634f;
+                a.coef[to] = d * a.mult;
+            }
+        }
+        if (lane == 0) {
+            a.index[to] = (int)n;
+            a.label[to] = (int)label_at(a.labels, a.wide, n);
+        }
+    }
+    // the rest of the last tile (a whole one where no row has a label)
+    const long end = min(a.cap, ((long)max(total, 1u) + 255) / 256 * 256);
+    for (long r = total + (long)blockIdx.x * (kPackThreads / 32) + warp; r < end; r += (long)a.pack_blocks * (kPackThreads / 32))
+        for (int h = 0; h < (kHalves ? 2 : 1); ++h)
+            for (int c = lane * 8; c < a.Cp; c += 256) {
+                *reinterpret_cast<uint4 *>(a.px + h * plane + r * a.Cp + c) = make_uint4(0, 0, 0, 0);
+                if (a.pd) *reinterpret_cast<uint4 *>(a.pd + h * plane + r * a.Cp + c) = make_uint4(0, 0, 0, 0);
+            }
+}
+
+// ---------------------------------------------------------------- the products
+enum { kLossStats = 0, kLossWeights = 1, kLossGrads = 2 };
+constexpr int kLossThreads = 384;                             // warp 0 loads, warp 1 issues, warps 4 to 11 take the sums out of tensor memory
+constexpr uint32_t kLossHalfTile = 128 * 128;                 // bytes: 128 rows (or 64 rows of two blocks of columns) of 64 elements
+constexpr uint32_t kLossPiece = 4096;                         // a warp's piece of a result on its way out
+template <int kPlanes> struct LossShape {
+    static constexpr int kStages = kPlanes == 1 ? 6 : 3;
+    static constexpr uint32_t kStage = 2 * kPlanes * kLossHalfTile;        // A (high, low), B (high, low)
+    // 64-deep steps whose sums stay in tensor memory, where every addition truncates: of halves 4 (12 x 4 additions), of 16-bit factors, whose results
+    // are rounded to 2^-9 or 2^-12, 64
+    static constexpr int kChunk = kPlanes == 1 ? 64 : 4;
+};
+constexpr size_t kLossSmem = 1024 + 6 * 2 * kLossHalfTile + 8 * kLossPiece + 256;
+
+struct LossMaps { CUtensorMap x, d, w, g, g_store; };         // in boxes of 64 x 64 (g_store: 32 rows of 64)
+struct LossArgs {
+    const LossInfo *info;
+    uint32_t *status;
+    int C, V, bf16;
+    long cap;                    // rows up to whole tiles
+    float scale;
+    int v0, words;               // the piece of the vocabulary: from v0 on
+    int width, tiles_v;          // X W^T: columns of a tile, tiles across
+    const int *label, *index;
+    // forward: maximum and sum of 2 tiles_v parts of a row (in units of ln 2), the label's logit
+    float2 *part;
+    float *chosen;
+    // backward
+    const float *lse2, *coef;
+    int grad_width, tiles_c;     // columns of a gradient's tile, tiles across
+    int first, last;             // of the pieces
+    void *dw, *dx;
+    long ld_dw, ld_dx;
+    int dw_fours, dx_fours;      // rows can be written four columns at a time
+    float dw_factor;             // 16-bit scale of G, scale and dloss_scale (times dmax / x_scale)
+    float *acc;                  // dX over the pieces before, by tile: [2 blocks][grad_width columns][128 rows]
+    float *slots;                // sums of parts of tiles, likewise, two per pair
+};
+
+// Who does what of the two gradients.  Tiles of dW (tall: a piece's words, sums over rows) come first, then tiles of dX (sums over words); whole rounds of
+// them are dealt out a tile a pair, so that pairs side by side read the same columns of G at the same time, and the tiles of the rounds that would not be full are cut along K into
+// equal shares: a pair takes the steps [p S / P, (p + 1) S / P) of theirs.  What is less than a tile goes to a slot of the pair's, to be joined.
+struct LossSplit {
+    int tiles_w, tiles_x, deep_w, deep_x, full_w, full_x, pairs, sharing;
+    long steps;
+    __device__ __forceinline__ LossSplit(const LossArgs &a, int rows, int pairs_) : pairs(pairs_) {
+        const int rb = max(1, (rows + 255) / 256);
+        tiles_w = a.dw ? (a.words + 255) / 256 * a.tiles_c : 0;
+        tiles_x = a.dx ? rb * a.tiles_c : 0;
+        deep_w = max(1, (rows + 63) / 64);
+        deep_x = (a.words + 63) / 64;
+        // (a round that is nearly full is left as it is)
+        auto full = [&](int tiles) { return tiles % pairs * 8 >= 7 * pairs ? tiles : tiles / pairs * pairs; };
+        full_w = full(tiles_w);
+        full_x = full(tiles_x);
+        steps = (long)(tiles_w - full_w) * deep_w + (long)(tiles_x - full_x) * deep_x;
+        sharing = (int)max(1L, min((long)pairs, steps / 4));   // at least four steps a share
+    }
+    __device__ __forceinline__ long share(int p) const { return (long)p * steps / sharing; }
+    // The part of a tile that step s of the rest is of: its first step, depth and number (tiles of dX behind those of dW).
+    __device__ __forceinline__ void tile_of(long s, long &start, int &deep, int &tile) const {
+        const long w = (long)(tiles_w - full_w) * deep_w;
+        if (s < w) {
+            const int t = (int)(s / deep_w);
+            start = (long)t * deep_w; deep = deep_w; tile = full_w + t;
+        } else {
+            const int t = (int)((s - w) / deep_x);
+            start = w + (long)t * deep_x; deep = deep_x; tile = tiles_w + full_x + t;
+        }
+    }
+};
+struct LossUnit { int dx, i, j, kb0, kb1, slot; };            // dx: of that product; tile (i, j); steps; slot: -1: the whole of the tile
+// A pair's units of work, one after the other; every role walks through them for itself.
+template <int kKind> struct LossUnits;
+template <int kKind> struct LossTiles {                       // of X W^T: rows fastest, so that pairs side by side share words
+    int t, step, total, rb, deep;
+    __device__ __forceinline__ LossTiles(const LossArgs &a, int rows, int pair, int pairs) : t(pair), step(pairs), rb(max(1, (rows + 255) / 256)), deep((a.C + 63) / 64) {
+        total = rb * a.tiles_v;
+    }
+    __device__ __forceinline__ bool next(LossUnit &u) {
+        if (t >= total) return false;
+        u = LossUnit{0, t % rb, t / rb, 0, deep, -1};
+        t += step;
+        return true;
+    }
+};
+template <> struct LossUnits<kLossStats> : LossTiles<kLossStats> { using LossTiles::LossTiles; };
+template <> struct LossUnits<kLossWeights> : LossTiles<kLossWeights> { using LossTiles::LossTiles; };
+template <> struct LossUnits<kLossGrads> {
+    LossSplit s;
+    int pair, tiles_c, t;
+    long at, end;
+    __device__ __forceinline__ LossUnits(const LossArgs &a, int rows, int pair_, int pairs) : s(a, rows, pairs), pair(pair_), tiles_c(a.tiles_c), t(pair_) {
+        at = end = 0;
+        if (pair < s.sharing) { at = s.share(pair); end = s.share(pair + 1); }
+    }
+    __device__ __forceinline__ bool next(LossUnit &u) {
+        const int rounds_w = (s.full_w + s.pairs - 1) / s.pairs * s.pairs;
+        if (t < rounds_w && t >= s.full_w) t += s.pairs;                          // (no tile for this pair in the last round)
+        if (t < s.full_w) {
+            u = LossUnit{0, t / tiles_c, t % tiles_c, 0, s.deep_w, -1};
+            t += s.pairs;
+            return true;
+        }
+        const int x = t - rounds_w;
+        if (x < s.full_x) {
+            u = LossUnit{1, x / tiles_c, x % tiles_c, 0, s.deep_x, -1};
+            t += s.pairs;
+            return true;
+        }
+        if (at >= end) return false;
+        long start;
+        int deep, tile;
+        s.tile_of(at, start, deep, tile);
+        const bool dx = tile >= s.tiles_w;
+        if (dx) tile -= s.tiles_w;
+        const int kb0 = (int)(at - start), kb1 = (int)min((long)deep, end - start);
+        u = LossUnit{dx, tile / tiles_c, tile % tiles_c, kb0, kb1, kb0 == 0 && kb1 == deep ? -1 : 2 * pair + (kb0 > 0 ? 0 : 1)};
+        at = start + kb1;
+        return true;
+    }
+};
+
+struct LossPipe {
+    uint32_t smem0, pieces0, bars, tmem;
+    volatile uint32_t *abort_flag;
+    uint32_t n, c;               // stages loaded or issued, sets of sums handed over (each role counts for itself)
+    int stages;
+    __device__ __forceinline__ uint32_t full(uint32_t s) const { return bars + 8 * s; }
+    __device__ __forceinline__ uint32_t empty(uint32_t s) const { return bars + 8 * (stages + s); }
+    __device__ __forceinline__ uint32_t acc_full(uint32_t b) const { return bars + 8 * (2 * stages + b); }
+    __device__ __forceinline__ uint32_t acc_empty(uint32_t b) const { return bars + 8 * (2 * stages + 2 + b); }
+};
+
+// The loading warp's part.
+template <int kKind, int kPlanes>
+__device__ __forceinline__ void loss_load(LossPipe &q, const LossMaps &m, const LossArgs &a, int rows, int pair, int pairs) {
+    using Shape = LossShape<kPlanes>;
+    if (!ptx::elect_one()) return;
+    const int in_pair = (int)(blockIdx.x & 1);
+    asm volatile("fence.proxy.async.global;" ::: "memory");              // (what was stored by the kernels before this, for the loads by TMA)
+    LossUnits<kKind> units(a, rows, pair, pairs);
+    LossUnit u;
+    while (units.next(u)) {
+        const int width = kKind == kLossGrads ? a.grad_width : a.width, right = width / 2;
+        const int ra = u.i * 256 + in_pair * 128, rb = u.j * width + in_pair * right;
+        for (int kb = u.kb0; kb < u.kb1; ++kb, ++q.n) {
+            const uint32_t s = q.n % Shape::kStages;
+            if (q.n >= Shape::kStages && !ptx::mbar_wait(q.empty(s), (q.n / Shape::kStages - 1) & 1, q.abort_flag, 111)) return;
+            const uint32_t at = q.smem0 + s * Shape::kStage, bar = ptx::in_block(q.full(s), 0), bt = at + kPlanes * kLossHalfTile;
+            if (in_pair == 0) ptx::mbar_arrive_expect_tx(q.full(s), 2 * kPlanes * (kLossHalfTile + right * 128));
+#pragma unroll
+            for (int h = 0; h < kPlanes; ++h)
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    const uint32_t pa = at + h * kLossHalfTile + r * 8192, pb = bt + h * kLossHalfTile + r * 8192;
+                    if (kKind != kLossGrads) {
+                        ptx::tma_load_3d_for<2>(pa, &m.x, bar, kb * 64, ra + r * 64, h);
+                        if (r * 64 < right) ptx::tma_load_3d_for<2>(pb, &m.w, bar, kb * 64, a.v0 + rb + r * 64, h);
+                    } else if (u.dx) {
+                        ptx::tma_load_3d_for<2>(pa, &m.g, bar, kb * 64, ra + r * 64, h);
+                        if (r * 64 < right) ptx::tma_load_3d_for<2>(pb, &m.w, bar, rb + r * 64, a.v0 + kb * 64, h);
+                    } else {
+                        ptx::tma_load_3d_for<2>(pa, &m.g, bar, ra + r * 64, kb * 64, h);
+                        if (r * 64 < right) ptx::tma_load_3d_for<2>(pb, &m.d, bar, rb + r * 64, kb * 64, h);
+                    }
+                }
+        }
+    }
+}
+// The issuing warp's part (its pair's first block's).
+template <int kKind, int kPlanes>
+__device__ __forceinline__ void loss_issue(LossPipe &q, const LossArgs &a, int rows, int pair, int pairs) {
+    using Shape = LossShape<kPlanes>;
+    if (!ptx::elect_one()) return;
+    constexpr uint32_t hi = ptx::desc_hi(1024, 2), low = kLossHalfTile >> 4;
+    LossUnits<kKind> units(a, rows, pair, pairs);
+    LossUnit u;
+    while (units.next(u)) {
+        const int width = kKind == kLossGrads ? a.grad_width : a.width;
+        const bool a_mn = kKind == kLossGrads && !u.dx, b_mn = kKind == kLossGrads;
+        // float32 sums; both factors bfloat16 (1) or float16 (0); which of them lie with K outermost; 256 x width
+        const uint32_t idesc = (1u << 4) | ((uint32_t)a.bf16 << 7) | ((uint32_t)a.bf16 << 10) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) |
+                               ((uint32_t)(width >> 3) << 17) | (16u << 24);
+        const uint32_t a_lbo = a_mn ? 8192 : 16, b_lbo = b_mn ? 8192 : 16, a_step = (a_mn ? 2048 : 32) >> 4, b_step = (b_mn ? 2048 : 32) >> 4;
+        for (int kb = u.kb0; kb < u.kb1; ++q.c) {
+            const uint32_t acc = q.tmem + (q.c & 1) * 256;
+            if (q.c >= 2 && !ptx::mbar_wait(q.acc_empty(q.c & 1), (q.c / 2 - 1) & 1, q.abort_flag, 112)) return;
+            ptx::tc_fence_after();
+            for (int k1 = min(kb + Shape::kChunk, u.kb1), first = 1; kb < k1; ++kb, ++q.n, first = 0) {
+                const uint32_t s = q.n % Shape::kStages;
+                if (!ptx::mbar_wait(q.full(s), (q.n / Shape::kStages) & 1, q.abort_flag, 113)) return;
+                ptx::tc_fence_after();
+                const uint32_t at = q.smem0 + s * Shape::kStage;
+                const uint32_t a0 = ptx::desc_lo(at, a_lbo), b0 = ptx::desc_lo(at + kPlanes * kLossHalfTile, b_lbo);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {                             // (what lies beyond K is zeros)
+                    const uint32_t x = a0 + k * a_step, y = b0 + k * b_step;
+                    if (kPlanes == 2) {
+                        ptx::mma_ss_for<2>(acc, ptx::desc(x + low, hi), ptx::desc(y, hi), idesc, !first || k > 0);
+                        ptx::mma_ss_for<2>(acc, ptx::desc(x, hi), ptx::desc(y + low, hi), idesc, 1);
+                    }
+                    ptx::mma_ss_for<2>(acc, ptx::desc(x, hi), ptx::desc(y, hi), idesc, kPlanes == 2 || !first || k > 0);
+                }
+                ptx::mma_commit_for<2>(q.empty(s));
+            }
+            ptx::mma_commit_for<2>(q.acc_full(q.c & 1));
+        }
+    }
+}
+
+// The result warps' parts.  A unit's sums into registers, a row a thread and half of the tile's columns (`cols`): false if a wait gave up.
+template <int kPlanes>
+__device__ __forceinline__ bool loss_sums(LossPipe &q, int deep, int cols, float (&v)[128]) {
+    const int warp = ptx::warp_index(), quad = warp & 3, half = (warp - 4) >> 2;
+    const uint32_t acc = q.tmem + ((uint32_t)(quad * 32) << 16) + half * cols;
+    for (int kb = 0; kb < deep; kb += LossShape<kPlanes>::kChunk, ++q.c) {
+        const bool ok = ptx::mbar_wait(q.acc_full(q.c & 1), (q.c / 2) & 1, q.abort_flag, 114);
+        if (!__all_sync(0xffffffffu, ok)) return false;
+        ptx::tc_fence_after();
+#pragma unroll
+        for (int k = 0; k < 128; k += 32) {
+            if (k >= cols) break;
+            uint32_t u[32];
+            ptx::tmem_ld32(acc + (q.c & 1) * 256 + k, u);
+            ptx::tmem_wait_ld();
+#pragma unroll
+            for (int e = 0; e < 32; ++e) v[k + e] = kb == 0 ? __uint_as_float(u[e]) : v[k + e] + __uint_as_float(u[e]);
+        }
+        ptx::tc_fence_before();
+        __syncwarp();
+        if ((threadIdx.x & 31) == 0) ptx::mbar_arrive_cluster(ptx::in_block(q.acc_empty(q.c & 1), 0));
+    }
+    return true;
+}
+
+// Forward: maximum and sum of exponentials of a row's part of the tile, and its label's logit where that is among them.
+__device__ __forceinline__ void loss_stats(const LossArgs &a, const LossUnit &u, float c2, int rows, int row, int col0, int cols, int half, const float (&v)[128]) {
+    const int at = row < rows ? a.label[row] - col0 : -1;                // the label's column here
+    float m = -INFINITY, l = 0.f;
+#pragma unroll
+    for (int k = 0; k < 128; k += 32) {
+        if (k >= cols || col0 + k >= a.V) break;
+        const int left = a.V - col0 - k;                                 // columns that are words
+        float s[32], mx = -INFINITY;
+#pragma unroll
+        for (int e = 0; e < 32; ++e) {
+            s[e] = v[k + e] * c2;
+            if (left < 32 && e >= left) s[e] = -INFINITY;
+        }
+#pragma unroll
+        for (int e = 0; e < 32; ++e) mx = fmaxf(mx, s[e]);
+        const float next = fmaxf(m, mx), ref = next == -INFINITY ? 0.f : next;
+        l *= ptx::ex2(m - ref);
+#pragma unroll
+        for (int e = 0; e < 32; ++e) l += ptx::ex2(s[e] - ref);
+        m = next;
+        if (__any_sync(0xffffffffu, at >= k && at < k + 32)) {
+            float c = 0.f;
+#pragma unroll
+            for (int e = 0; e < 32; ++e) c = at == k + e ? s[e] : c;
+            if (at >= k && at < k + 32) a.chosen[row] = c;
+        }
+    }
+    if (row < rows) a.part[((long)u.j * 2 + half) * a.cap + row] = make_float2(m, l);
+}
+
+// Backward: q of 32 rows and 64 columns at a time, in 16 bits (halves), to G.
+template <int kPlanes>
+__device__ __forceinline__ void loss_weights(const LossPipe &q, const LossMaps &m, const LossArgs &a, const LossUnit &u, float c2, int rows, int row, int local0, int cols,
+                                             float (&v)[128]) {
+    const int lane = threadIdx.x & 31, col0 = a.v0 + local0;
+    const uint32_t piece = q.pieces0 + (ptx::warp_index() - 4) * kLossPiece;
+    const bool in = row < rows;
+    const int at = in ? a.label[row] - col0 : -1;
+    const float lse2 = in ? a.lse2[row] : 0.f, f = !in ? 0.f : a.bf16 ? a.coef[row] : 32768.f;
+#pragma unroll
+    for (int k = 0; k < 128; k += 64) {
+        if (k >= cols) break;
+        const int left = in ? a.V - col0 - k : 0;
+#pragma unroll
+        for (int e = 0; e < 64; ++e) {
+            float p = ptx::ex2(fmaf(v[k + e], c2, -lse2));
+            if (at == k + e) p -= 1.f;
+            v[k + e] = e < left ? p * f : 0.f;
+        }
+#pragma unroll
+        for (int h = 0; h < kPlanes; ++h) {
+            if (lane == 0) ptx::tma_store_wait<true>();
+            __syncwarp();
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                uint32_t r[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float &x = v[k + 8 * e + 2 * i], &y = v[k + 8 * e + 2 * i + 1];
+                    if (kPlanes == 1 && a.bf16) r[i] = ptx::pack_bf16(x, y);
+                    else {
+                        const __half2 t = __floats2half2_rn(x, y);
+                        r[i] = *reinterpret_cast<const uint32_t *>(&t);
+                        if (kPlanes == 2 && h == 0) {                     // (what is left is the low half)
+                            const float2 b = __half22float2(t);
+                            x -= b.x;
+                            y -= b.y;
+                        }
+                    }
+                }
+                ptx::sts128(piece + lane * 128 + ((e ^ (lane & 7)) << 4), r);
+            }
+            ptx::fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) {
+                ptx::tma_store_3d(&m.g_store, piece, local0 + k, row - lane, h);
+                ptx::tma_store_commit();
+            }
+        }
+    }
+}
+
+// 32 rows (a row a lane, to go to row `to` of the output; -1: nowhere) of 32 columns from c0 on, times f, by way of shared memory, so that eight lanes write a row's 32 columns.
+template <typename E>
+__device__ __forceinline__ void loss_out(uint32_t piece, E *out, long ld, int fours, int to, int c0, int C, float f, const float *v) {
+    const int lane = threadIdx.x & 31;
+    __syncwarp();
+#pragma unroll
+    for (int g = 0; g < 8; ++g) {
+        const uint32_t r[4] = {__float_as_uint(v[4 * g] * f), __float_as_uint(v[4 * g + 1] * f), __float_as_uint(v[4 * g + 2] * f), __float_as_uint(v[4 * g + 3] * f)};
+        ptx::sts128(piece + lane * 128 + ((g ^ (lane & 7)) << 4), r);
+    }
+    __syncwarp();
+    const int g = lane & 7, c = c0 + 4 * g;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const int r = 4 * k + (lane >> 3);
+        const int t = __shfl_sync(0xffffffffu, to, r);
+        const float4 x = ptx::lds128(piece + r * 128 + ((g ^ (r & 7)) << 4));
+        if (t < 0 || c >= C) continue;
+        E *p = out + (long)t * ld + c;
+        __align__(16) E e[4];
+        from_f32(e[0], x.x); from_f32(e[1], x.y); from_f32(e[2], x.z); from_f32(e[3], x.w);
+        if (fours) {
+            if constexpr (sizeof(E) == 4) *reinterpret_cast<float4 *>(p) = *reinterpret_cast<const float4 *>(e);
+            else *reinterpret_cast<uint2 *>(p) = *reinterpret_cast<const uint2 *>(e);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (c + i < C) p[i] = e[i];
+        }
+    }
+    __syncwarp();
+}
+// 32 columns of a gradient's tile that are complete, tile-local from col on.
+template <typename E>
+__device__ __forceinline__ void loss_gradient(uint32_t piece, const LossArgs &a, const LossInfo &info, int dx, int i, int j, int block, int quad, int col, float *v) {
+    const int lane = threadIdx.x & 31, local = i * 256 + block * 128 + quad * 32 + lane, c0 = j * a.grad_width + col;
+    if (c0 >= a.C) return;
+    if (!dx) {
+        loss_out<E>(piece, static_cast<E *>(a.dw), a.ld_dw, a.dw_fours, local < a.words ? a.v0 + local : -1, c0, a.C,
+                    a.bf16 ? 1.f : a.dw_factor * info.dmax / info.x_scale, v);
+        return;
+    }
+    if (!a.first || !a.last) {
+        float *acc = a.acc + ((((long)i * a.tiles_c + j) * 2 + block) * a.grad_width + col) * 128 + quad * 32 + lane;
+        if (!a.first) {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) v[e] += acc[e * 128];
+        }
+        if (!a.last) {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) acc[e * 128] = v[e];
+            return;
+        }
+    }
+    const bool in = local < (int)info.rows;
+    const float f = a.bf16 || !in ? 1.f : a.coef[local] / (32768.f * info.w_scale);
+#pragma unroll
+    for (int e = 0; e < 32; ++e) v[e] *= f;
+    loss_out<E>(piece, static_cast<E *>(a.dx), a.ld_dx, a.dx_fours, in ? a.index[local] : -1, c0, a.C, 1.f, v);
+}
+
+template <int kKind, int kPlanes, typename E>
+__global__ void __launch_bounds__(kLossThreads, 1) loss_kernel(const __grid_constant__ LossMaps maps, const LossArgs a) {
+    extern __shared__ uint8_t raw[];
+    __shared__ uint32_t tmem_slot;
+    __shared__ volatile uint32_t abort_flag;
+    using Shape = LossShape<kPlanes>;
+    LossPipe q;
+    q.smem0 = ptx::smem_u32(ptx::align_1024(raw));
+    q.pieces0 = q.smem0 + Shape::kStages * Shape::kStage;
+    q.bars = q.pieces0 + 8 * kLossPiece;
+    q.abort_flag = &abort_flag;
+    q.n = q.c = 0;
+    q.stages = Shape::kStages;
+    if (threadIdx.x == 0) {
+        abort_flag = 0;
+        for (int s = 0; s < Shape::kStages; ++s) { ptx::mbar_init(q.full(s), 1); ptx::mbar_init(q.empty(s), 1); }
+        for (int b = 0; b < 2; ++b) { ptx::mbar_init(q.acc_full(b), 1); ptx::mbar_init(q.acc_empty(b), 16); }
+        ptx::fence_mbar_init();
+    }
+    if (ptx::warp_index() == 1) ptx::tmem_alloc_for<2>(ptx::smem_u32(&tmem_slot), 512);
+    ptx::tc_fence_before();
+    __syncthreads();
+    ptx::cluster_meet();
+    ptx::tc_fence_after();
+    q.tmem = tmem_slot;
+    ptx::grid_launch();
+    ptx::grid_wait();
+    const int warp = ptx::warp_index(), pair = (int)(blockIdx.x >> 1), pairs = (int)(gridDim.x >> 1), in_pair = (int)(blockIdx.x & 1);
+    const LossInfo info = *a.info;
+    const int rows = (int)info.rows;
+    // Registers of the launch, 384 x 168, as 128 x 40 (the loading and the issuing warp, two that idle) and 256 x 232: the result warps' hold their 128 sums.
+    if (warp == 0) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+        loss_load<kKind, kPlanes>(q, maps, a, rows, pair, pairs);
+    } else if (warp == 1) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+        if (in_pair == 0) loss_issue<kKind, kPlanes>(q, a, rows, pair, pairs);
+    } else if (warp < 4) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
+        const int quad = warp & 3, half = (warp - 4) >> 2, lane = threadIdx.x & 31;
+        const int cols = (kKind == kLossGrads ? a.grad_width : a.width) / 2;
+        const float c2 = a.scale * 1.4426950408889634f / (info.x_scale * info.w_scale);
+        const uint32_t piece = q.pieces0 + (warp - 4) * kLossPiece;
+        LossUnits<kKind> units(a, rows, pair, pairs);
+        LossUnit u;
+        while (units.next(u)) {
+            float v[128];
+            if (!loss_sums<kPlanes>(q, u.kb1 - u.kb0, cols, v)) break;
+            const int row = u.i * 256 + in_pair * 128 + quad * 32 + lane;
+            if constexpr (kKind == kLossStats) loss_stats(a, u, c2, rows, row, u.j * a.width + half * cols, cols, half, v);
+            else if constexpr (kKind == kLossWeights) loss_weights<kPlanes>(q, maps, a, u, c2, rows, row, u.j * a.width + half * cols, cols, v);
+            else if (u.slot >= 0) {
+                float *slot = a.slots + (((long)u.slot * 2 + in_pair) * a.grad_width + half * cols) * 128 + quad * 32 + lane;
+#pragma unroll
+                for (int e = 0; e < 128; ++e)
+                    if (e < cols) slot[e * 128] = v[e];
+            } else {
+#pragma unroll
+                for (int k = 0; k < 128; k += 32)
+                    if (k < cols) loss_gradient<E>(piece, a, info, u.dx, u.i, u.j, in_pair, quad, half * cols + k, v + k);
+            }
+        }
+        if (lane == 0) ptx::tma_store_wait<false>();
+        __syncwarp();
+    }
+    __syncwarp();
+    ptx::tc_fence_before();
+    __syncthreads();
+    let_arrive(q.abort_flag);
+    ptx::cluster_meet();                                      // (nobody's shared or tensor memory is needed any more)
+    if (threadIdx.x == 0 && abort_flag != 0) *a.status = abort_flag;
+    if (warp == 1) {
+        ptx::tc_fence_after();
+        ptx::tmem_dealloc_for<2>(q.tmem, 512);
+    }
+}
+
+// Tiles whose K several pairs have shared: a warp 32 rows and 32 columns, the shares in the order of K.
+constexpr int kJoinWarps = 8;
+template <typename E>
+__global__ void __launch_bounds__(32 * kJoinWarps) loss_join_kernel(const LossArgs a, int pairs) {
+    __shared__ __align__(128) uint8_t pieces[kJoinWarps][kLossPiece];
+    ptx::grid_launch();
+    ptx::grid_wait();
+    const LossInfo info = *a.info;
+    const LossSplit s(a, (int)info.rows, pairs);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, blocks_of_tile = 8 * (a.grad_width / 32);   // (2 blocks, 4 quarters of rows)
+    const long at = (long)blockIdx.x * kJoinWarps + warp;
+    const int rest = (int)(at / blocks_of_tile), part = (int)(at % blocks_of_tile), block = part & 1, quad = part >> 1 & 3, col = (part >> 3) * 32;
+    const int rest_w = s.tiles_w - s.full_w;
+    if (rest >= rest_w + s.tiles_x - s.full_x) return;
+    const bool dx = rest >= rest_w;
+    const long start = dx ? (long)rest_w * s.deep_w + (long)(rest - rest_w) * s.deep_x : (long)rest * s.deep_w, end = start + (dx ? s.deep_x : s.deep_w);
+    const int tile = dx ? s.full_x + rest - rest_w : s.full_w + rest;
+    // the first pair whose share reaches into the tile
+    int p = (int)(start * s.sharing / s.steps);
+    while (p > 0 && s.share(p) > start) --p;
+    while (s.share(p + 1) <= start) ++p;
+    if (s.share(p) <= start && s.share(p + 1) >= end) return;                       // (all of it is one pair's, which has finished it)
+    float v[32];
+#pragma unroll
+    for (int e = 0; e < 32; ++e) v[e] = 0.f;
+    for (; p < s.sharing && s.share(p) < end; ++p) {
+        const int slot = 2 * p + (s.share(p) > start ? 0 : 1);
+        // (a share that begins with the tile, or before it, has it as its last; one that begins inside it as its first)
+        const float *from = a.slots + (((long)slot * 2 + block) * a.grad_width + col) * 128 + quad * 32 + lane;
+#pragma unroll
+        for (int e = 0; e < 32; ++e) v[e] += from[e * 128];
+    }
+    loss_gradient<E>(ptx::smem_u32(pieces[warp]), a, info, dx, tile / a.tiles_c, tile % a.tiles_c, block, quad, col, v);
+}
+
+// Parts of a row's statistics, joined: 32 rows a block, its warps taking the parts in turn.
+constexpr int kMergeWarps = 16;
+struct LossMerge {
+    const LossInfo *info;
+    const float2 *part;
+    const float *chosen;
+    const int *index;
+    long cap;
+    int parts;
+    float *loss, *lse;
+};
+__global__ void __launch_bounds__(32 * kMergeWarps) loss_merge_kernel(const LossMerge a) {
+    __shared__ float2 shared[kMergeWarps][32];
+    ptx::grid_launch();
+    ptx::grid_wait();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rows = (int)a.info->rows;
+    for (long r0 = (long)blockIdx.x * 32; r0 < rows; r0 += (long)gridDim.x * 32) {
+        const long row = r0 + lane;
+        float m = -INFINITY, l = 0.f;
+        auto take = [&](float2 x) {
+            const float next = fmaxf(m, x.x), ref = next == -INFINITY ? 0.f : next;
+            l = l * ptx::ex2(m - ref) + x.y * ptx::ex2(x.x - ref);
+            m = next;
+        };
+        if (row < rows) {
+#pragma unroll 4
+            for (int p = warp; p < a.parts; p += kMergeWarps) take(a.part[p * a.cap + row]);
+        }
+        shared[warp][lane] = make_float2(m, l);
+        __syncthreads();
+        if (warp == 0 && row < rows) {
+            m = -INFINITY, l = 0.f;
+            for (int w = 0; w < kMergeWarps; ++w) take(shared[w][lane]);
+            // (m and the label's logit were rounded alike: where the label is the maximum nothing is left of their difference)
+            const float log_l = logf(l);
+            const int n = a.index[row];
+            a.loss[n] = (m - a.chosen[row]) * 0.69314718056f + log_l;
+            a.lse[n] = m * 0.69314718056f + log_l;
+        }
+        __syncthreads();
+    }
+}
+
+}  // namespace flare

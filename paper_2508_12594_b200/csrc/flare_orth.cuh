@@ -343,48 +343,6 @@ __device__ __forceinline__ void upper_tile(int t, int n, int &i, int &j) {
     j = i + t;
 }
 
-namespace ptx {
-__device__ __forceinline__ void cluster_meet() {
-    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-__device__ __forceinline__ uint32_t in_block(uint32_t addr, uint32_t rank) {
-    uint32_t r;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
-    return r;
-}
-__device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
-}
-// kPair = 2: the two blocks of a cluster as one (256 rows, each block's 128 in its own tensor memory; each block holds half of B).
-template <int kPair> __device__ __forceinline__ void tmem_alloc_for(uint32_t slot, uint32_t cols) {
-    if (kPair == 1) { tmem_alloc(slot, cols); return; }
-    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(slot), "r"(cols) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
-}
-template <int kPair> __device__ __forceinline__ void tmem_dealloc_for(uint32_t taddr, uint32_t cols) {
-    if (kPair == 1) tmem_dealloc(taddr, cols);
-    else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(cols) : "memory");
-}
-template <int kPair> __device__ __forceinline__ void tma_load_3d_for(uint32_t dst, const CUtensorMap *m, uint32_t bar, int c0, int c1, int c2) {
-    if (kPair == 1) { tma_load_3d(dst, m, bar, c0, c1, c2); return; }
-    asm volatile(
-        "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(dst),
-        "l"(reinterpret_cast<uint64_t>(m)), "r"(bar), "r"(c0), "r"(c1), "r"(c2)
-        : "memory");
-}
-template <int kPair> __device__ __forceinline__ void mma_ss_for(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
-    if (kPair == 1) { mma_ss(d, a, b, idesc, accumulate); return; }
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc),
-                 "r"(accumulate)
-                 : "memory");
-}
-// (kPair = 2: the barriers of both blocks)
-template <int kPair> __device__ __forceinline__ void mma_commit_for(uint32_t bar) {
-    if (kPair == 1) { mma_commit(bar); return; }
-    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((uint16_t)3) : "memory");
-}
-}  // namespace ptx
-
 // A warp's 32 rows x 32 columns of the result, one row a lane, into the output (rows s0.., columns l0..) by way of shared memory, so that
 // neighbouring lanes write neighbouring elements whichever way the output lies.  buf: 4096 bytes of the warp's own.
 template <typename E>
@@ -475,12 +433,6 @@ __device__ __forceinline__ OrthPipe orth_pipe(uint8_t *raw, uint32_t *tmem_slot,
     ptx::tc_fence_after();
     q.tmem = *tmem_slot;
     return q;
-}
-// What a block that gave up a wait has asked for, copies into its shared memory and products into its tensor memory, may still be on its way, and
-// which of its barriers would say so is not known then: it is given a millisecond, some hundred times what it takes, before the block ends.
-__device__ __forceinline__ void let_arrive(volatile uint32_t *abort_flag) {
-    if (*abort_flag == 0) return;
-    for (const uint64_t t0 = ptx::globaltimer_ns(); ptx::globaltimer_ns() - t0 < 1000000ull;) __nanosleep(2000);
 }
 template <int kPair>
 __device__ __forceinline__ void orth_pipe_end(const OrthPipe &q, uint32_t *status) {

@@ -43,6 +43,25 @@ class FlareMuon(ctypes.Structure):
     _fields_ = [(n, ctypes.c_float) for n in ("lr", "momentum", "weight_decay", "update_scale")] + [("nesterov", ctypes.c_int32)]
 
 
+class FlareDrop(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_float), ("seed", ctypes.c_uint64), ("offset", ctypes.c_uint64), ("step", ctypes.c_void_p)]
+
+
+class FlareDropoutDesc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64)] + [(n, ctypes.c_int32) for n in ("width", "dtype", "residual_dtype")] + [
+        (n, ctypes.c_int64) for n in ("stride_x", "stride_residual", "stride_y")]
+
+
+class FlareEmbedDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("rows", "positions")] + [(n, ctypes.c_int32) for n in ("width", "vocab", "dtype", "out_dtype", "token_bits")] + [
+        ("scale", ctypes.c_float)] + [(n, ctypes.c_int64) for n in ("stride_table", "stride_out")]
+
+
+class FlareLossDesc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64)] + [(n, ctypes.c_int32) for n in ("width", "vocab", "dtype", "label_bits")] + [
+        (n, ctypes.c_float) for n in ("scale", "dloss_scale")] + [(n, ctypes.c_int64) for n in ("stride_x", "stride_w", "stride_dx", "stride_dw")]
+
+
 class FlareError(RuntimeError):
     def __init__(self, status: int, where: str):
         lib = _lib_or_none()
@@ -88,6 +107,14 @@ _SIGNATURES = {
     "flare_orthogonalize_plan": (ctypes.c_int, [_op, ctypes.POINTER(ctypes.c_int32)]),
     "flare_orthogonalize": (ctypes.c_int, [_op, _vp, _vp, _vp, _sz, _vp]),
     "flare_muon_update": (ctypes.c_int, [_op, ctypes.POINTER(FlareMuon)] + [_vp] * 6 + [_sz, _vp]),
+    "flare_dropout_forward": (ctypes.c_int, [ctypes.POINTER(FlareDropoutDesc), ctypes.POINTER(FlareDrop)] + [_vp] * 4),
+    "flare_dropout_backward": (ctypes.c_int, [ctypes.POINTER(FlareDropoutDesc), ctypes.POINTER(FlareDrop)] + [_vp] * 3),
+    "flare_embed_forward": (ctypes.c_int, [ctypes.POINTER(FlareEmbedDesc), ctypes.POINTER(FlareDrop)] + [_vp] * 5),
+    "flare_embed_workspace_bytes": (_sz, [ctypes.POINTER(FlareEmbedDesc)]),
+    "flare_embed_backward": (ctypes.c_int, [ctypes.POINTER(FlareEmbedDesc), ctypes.POINTER(FlareDrop)] + [_vp] * 4 + [ctypes.c_int32, _vp, _sz, _vp]),
+    "flare_loss_workspace_bytes": (_sz, [ctypes.POINTER(FlareLossDesc), ctypes.c_int32]),
+    "flare_loss_forward": (ctypes.c_int, [ctypes.POINTER(FlareLossDesc)] + [_vp] * 6 + [_sz, _vp]),
+    "flare_loss_backward": (ctypes.c_int, [ctypes.POINTER(FlareLossDesc)] + [_vp] * 8 + [_sz, _vp]),
     "flare_selftest_wait": (ctypes.c_int, [_vp, ctypes.c_uint64, _vp]),
     "flare_selftest_team": (ctypes.c_int, [_vp, ctypes.c_int32, ctypes.c_uint64, _vp]),
 }
@@ -399,3 +426,70 @@ def muon_update(w, m, g, lr, momentum=0.95, weight_decay=0.0, nesterov=True, upd
         (stream or torch.cuda.current_stream()).synchronize()
         flare_check(ws, stream)
     return w1, m1
+
+
+# ---- tokens: embedding, dropout, the loss over a vocabulary
+
+
+class Drop(NamedTuple):
+    """Dropout: the share p of elements (to 2^-17) that become 0, by a counter-based generator from seed and offset, 64 bits each.  step: an int64 tensor of one
+    number on the GPU that the kernels add to offset when they run, so that a captured graph that counts it up drops other elements every time."""
+    p: float
+    seed: int
+    offset: int = 0
+    step: Optional[torch.Tensor] = None
+
+
+class EmbedGrads(NamedTuple):
+    dtable: torch.Tensor
+    dpositions: Optional[torch.Tensor]
+
+
+class LossGrads(NamedTuple):
+    dx: torch.Tensor
+    dw: torch.Tensor
+
+
+def dropout(x, drop: Drop, residual=None, out=None, stream=None):
+    """residual + drop(x) for x [..., width]; of the residual's type (x's, or float32).  What is kept is multiplied by 1 / (1 - p).  out: a tensor to write to
+    (x or residual themselves are allowed)."""
+    return (_native or _bind()).dropout(x, drop, residual, out, stream)
+
+
+def dropout_backward(dy, drop: Drop, dtype=None, out=None, stream=None):
+    """The gradient of dropout's x, of `dtype` (dy's): the elements that the same Drop keeps.  The residual's is dy."""
+    return (_native or _bind()).dropout_backward(dy, drop, dtype, out, stream)
+
+
+def embed(tokens, table, positions=None, scale=1.0, drop: Optional[Drop] = None, dtype=None, out=None, stream=None):
+    """drop(scale * table[tokens] + positions): tokens [..., L] int32 or int64, table [vocab, width], positions [L, width] or None -> [..., L, width] of
+    `dtype` (the table's).  A token outside [0, vocab) has no row: zeros in its place."""
+    return (_native or _bind()).embed(tokens, table, positions, scale, drop, dtype, out, stream)
+
+
+def embed_backward(tokens, dy, vocab: int, positions: int = 0, scale=1.0, drop: Optional[Drop] = None, dtype=None, accumulate=False, out=None,
+                   stream=None) -> EmbedGrads:
+    """Gradients of embed's tables, of `dtype` (dy's): dtable [vocab, width] and, with positions = L, dpositions [L, width].  out: (dtable, dpositions) to
+    write to, either None; accumulate: they are added to instead."""
+    return (_native or _bind()).embed_backward(tokens, dy, vocab, positions, scale, drop, dtype, accumulate, out, stream, EmbedGrads)
+
+
+def token_loss(x, w, labels, scale=1.0, out=None, stream=None, check=False):
+    """Softmax cross entropy of the logits scale * x w^T over a vocabulary, which are never kept: x [..., width], w [vocab, width] of the same type, labels
+    [...] int32 or int64 -> (loss [...], lse [...]) float32, lse the logarithm of a row's sum of exponentials.  A row whose label is outside [0, vocab) takes no
+    part: 0 and 0.  out: (loss, lse) to write to, either None.  With check=True the stream is synchronised and a device-side wait that gave up raises."""
+    r, ws = (_native or _bind()).token_loss(x, w, labels, scale, out, stream)
+    if check:
+        (stream or torch.cuda.current_stream()).synchronize()
+        flare_check(ws, stream)
+    return r
+
+
+def token_loss_backward(x, w, labels, lse, dloss=1.0, scale=1.0, out=None, stream=None, check=False) -> LossGrads:
+    """Gradients of token_loss from its inputs and its lse.  dloss: what reaches every row's loss, a float32 tensor like lse or one number for all.
+    out: (dx, dw) to write to, either None."""
+    r, ws = (_native or _bind()).token_loss_backward(x, w, labels, lse, dloss, scale, out, stream, LossGrads)
+    if check:
+        (stream or torch.cuda.current_stream()).synchronize()
+        flare_check(ws, stream)
+    return r

@@ -52,7 +52,7 @@ LossPlan loss_plan(const flare_loss_desc_t *d, int sms) {
     p.cap = std::max(1L, (long)(d->rows + 255) / 256) * 256;
     p.width = tile_width(p.cap / 256, d->vocab, p.pairs);
     if (f32) {
-        auto blocks = [&](long rows) { return (int)std::max(1L, std::min(4L * sms, (rows * d->width / 4096 + 7) / 8)); };
+        auto blocks = [&](long rows) { return (int)std::max(1L, std::min(4L * sms, rows * d->width / 8192)); };
         p.x_blocks = blocks(d->rows);
         p.w_blocks = blocks(d->vocab);
     }
@@ -65,7 +65,7 @@ LossPlan loss_plan(const flare_loss_desc_t *d, int sms) {
     p.tiles_c = (d->width + p.grad_width - 1) / p.grad_width;
     return p;
 }
-struct LossLayout { size_t info, rank, chunk, largest, px, pd, pw, index, label, part, chosen, lse2, coef, g, acc, slots, total; };
+struct LossLayout { size_t info, rank, chunk, largest, px, pd, pw, index, label, part, chosen, gave_up, lse2, coef, g, acc, slots, total; };
 LossLayout loss_layout(const flare_loss_desc_t *d, const LossPlan &p, bool backward) {
     LossLayout w{};
     size_t off = kHeaderBytes;
@@ -83,6 +83,7 @@ LossLayout loss_layout(const flare_loss_desc_t *d, const LossPlan &p, bool backw
         const long tiles = (d->vocab + p.width - 1) / p.width;
         take(w.part, sizeof(float2) * 2 * (size_t)tiles * p.cap);
         take(w.chosen, sizeof(float) * (size_t)p.cap);
+        take(w.gave_up, sizeof(uint32_t) * 2 * (size_t)p.pairs);
     } else {
         take(w.pd, d->dtype == FLARE_DTYPE_BF16 ? 0 : row * p.cap);
         take(w.lse2, sizeof(float) * (size_t)p.cap);
@@ -168,7 +169,7 @@ int prepare_loss(const flare_loss_desc_t *d, const LossPlan &p, const LossLayout
     k.info = reinterpret_cast<LossInfo *>(ws + l.info);
     k.px = reinterpret_cast<uint16_t *>(ws + l.px); k.pw = reinterpret_cast<uint16_t *>(ws + l.pw);
     k.index = reinterpret_cast<int *>(ws + l.index); k.label = reinterpret_cast<int *>(ws + l.label);
-    const int blocks = k.pack_blocks + (int)std::min<long>((k.w_rows + 31) / 32, 16L * device_info().sms);
+    const int blocks = k.pack_blocks + (int)std::min<long>((k.w_rows * (p.Cp / 8) + 4 * kPackThreads - 1) / (4 * kPackThreads), 16L * device_info().sms);
     if (int rc = f32 ? launch_pack<float>(k, blocks, st) : bf16 ? launch_pack<__nv_bfloat16>(k, blocks, st) : launch_pack<__half>(k, blocks, st)) return rc;
     int rc;
     if ((rc = make_plane_map(&maps->x, k.px, bf16, p.Cp, p.cap, p.planes, p.Cp, 64)) != FLARE_OK) return rc;
@@ -209,14 +210,27 @@ int flare_loss_forward(const flare_loss_desc_t *desc, const void *x, const void 
     k.loss = loss; k.lse = lse;
     LossMaps maps{};
     LossArgs a{};
-    if (int rc = prepare_loss(desc, p, l, ws, x, w, labels, k, &maps, &a, st)) return rc;
+    const long ld_x = desc->stride_x ? desc->stride_x : desc->width, ld_w = desc->stride_w ? desc->stride_w : desc->width;
+    const bool direct = desc->rows <= 256 && p.planes == 1 && aligned16(x) && aligned16(w) && ld_x % 8 == 0 && ld_w % 8 == 0;
+    if (direct) {
+        const bool bf16 = desc->dtype == FLARE_DTYPE_BF16;
+        int rc;
+        if ((rc = make_plane_map(&maps.x, x, bf16, desc->width, desc->rows, 1, ld_x, 64)) != FLARE_OK) return rc;
+        if ((rc = make_plane_map(&maps.w, w, bf16, desc->width, desc->vocab, 1, ld_w, 64)) != FLARE_OK) return rc;
+        a.C = desc->width; a.V = desc->vocab; a.bf16 = bf16; a.cap = p.cap; a.scale = desc->scale; a.status = reinterpret_cast<uint32_t *>(ws);
+        a.labels = labels; a.wide = desc->label_bits == 64; a.direct = (int)desc->rows; a.gave_up = reinterpret_cast<uint32_t *>(ws + l.gave_up);
+    } else if (int rc = prepare_loss(desc, p, l, ws, x, w, labels, k, &maps, &a, st)) {
+        return rc;
+    }
     a.words = desc->vocab; a.width = p.width; a.tiles_v = (desc->vocab + p.width - 1) / p.width;
     a.part = reinterpret_cast<float2 *>(ws + l.part); a.chosen = reinterpret_cast<float *>(ws + l.chosen);
     const int pairs = (int)std::min<long>(p.pairs, p.cap / 256 * a.tiles_v);
     if (int rc = p.planes == 2 ? launch_loss<kLossStats, 2, float>(maps, a, pairs, st) : launch_loss<kLossStats, 1, float>(maps, a, pairs, st)) return rc;
     LossMerge m{};
     m.info = a.info; m.part = a.part; m.chosen = a.chosen; m.index = a.index; m.cap = p.cap; m.parts = 2 * a.tiles_v; m.loss = loss; m.lse = lse;
-    FLARE_CUDA(launch_after(loss_merge_kernel, (unsigned)std::min<long>((desc->rows + 31) / 32, 65535L), 32 * kMergeWarps, 0, st, m));
+    m.labels = a.labels; m.wide = a.wide; m.V = a.V; m.direct = a.direct; m.gave_up = a.gave_up; m.status = a.status; m.blocks = 2 * pairs;
+    const int warps = std::min(kMergeWarps, std::max(1, m.parts / 4));
+    FLARE_CUDA(launch_after(loss_merge_kernel, (unsigned)std::min<long>((desc->rows + 31) / 32, 65535L), 32 * warps, 0, st, m));
     return FLARE_OK;
 }
 
@@ -262,8 +276,8 @@ int flare_loss_backward(const flare_loss_desc_t *desc, const void *x, const void
     auto weights = f32 ? launch_loss<kLossWeights, 2, float> : launch_loss<kLossWeights, 1, float>;
     auto grads = f32 ? launch_loss<kLossGrads, 2, float> : bf16 ? launch_loss<kLossGrads, 1, __nv_bfloat16> : launch_loss<kLossGrads, 1, __half>;
     auto *join = f32 ? loss_join_kernel<float> : bf16 ? loss_join_kernel<__nv_bfloat16> : loss_join_kernel<__half>;
-    // tiles that several pairs can have shared: fewer than a round of either gradient
-    const long rest = 2L * (p.pairs - 1), warps = rest * 8 * (p.grad_width / 32);
+    // of tiles that several pairs can have shared: fewer than a round of either gradient
+    const long warps = 2L * (p.pairs - 1) * 8 * (p.grad_width / 32);
     for (int i = 0; i < p.pieces; ++i) {
         a.v0 = i * p.Vp;
         a.words = std::min(p.Vp, desc->vocab - a.v0);

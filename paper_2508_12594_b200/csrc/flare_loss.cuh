@@ -39,6 +39,20 @@ __device__ __forceinline__ int64_t label_at(const void *labels, int wide, long n
     return wide ? static_cast<const int64_t *>(labels)[n] : (int64_t) static_cast<const int32_t *>(labels)[n];
 }
 
+// A thread's walk over groups of columns of rows, without divisions.
+struct LossWalk {
+    long row, drow;
+    uint32_t group, dgroup, groups;
+    __device__ __forceinline__ LossWalk(uint64_t first, uint64_t step, uint32_t groups_) : groups(groups_) {
+        row = (long)(first / groups); group = (uint32_t)(first % groups);
+        drow = (long)(step / groups); dgroup = (uint32_t)(step % groups);
+    }
+    __device__ __forceinline__ void next() {
+        row += drow; group += dgroup;
+        if (group >= groups) { group -= groups; ++row; }
+    }
+};
+
 constexpr int kLossChunk = 1024, kScanThreads = 256;
 struct LossScan {
     const void *labels;
@@ -75,15 +89,36 @@ __global__ void __launch_bounds__(kScanThreads) loss_scan_kernel(const LossScan 
         const int b = blockIdx.x - a.chunks;
         const bool of_x = b < a.x_blocks;
         const float *m = of_x ? a.x : a.w;
-        const long rows = of_x ? a.rows : a.V, ld = of_x ? a.ld_x : a.ld_w, step = (long)(of_x ? a.x_blocks : a.w_blocks) * (kScanThreads / 32);
+        const long rows = of_x ? a.rows : a.V, ld = of_x ? a.ld_x : a.ld_w;
+        const bool fours = a.C % 4 == 0 && ld % 4 == 0 && (reinterpret_cast<uintptr_t>(m) & 15) == 0;
+        const uint32_t groups = (uint32_t)(a.C + 3) / 4;
+        const uint64_t blocks = of_x ? a.x_blocks : a.w_blocks, first = (uint64_t)(of_x ? b : b - a.x_blocks) * kScanThreads + threadIdx.x;
+        // (four groups of four columns are asked for before the first is looked at)
+        LossWalk walk(first, blocks * kScanThreads, groups);
         float most = 0.f;
-        for (long r = (long)(of_x ? b : b - a.x_blocks) * (kScanThreads / 32) + warp; r < rows; r += step) {
-            if (of_x) {
-                const int64_t label = label_at(a.labels, a.wide, r);
-                if (label < 0 || label >= a.V) continue;
+        while (walk.row < rows) {
+            float4 v[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+                const float *p = m + walk.row * ld + 4 * walk.group;
+                bool use = walk.row < rows;
+                if (use && of_x) {
+                    const int64_t label = label_at(a.labels, a.wide, walk.row);
+                    use = label >= 0 && label < a.V;
+                }
+                if (use && fours) v[k] = *reinterpret_cast<const float4 *>(p);
+                else if (use) {
+                    const int n = a.C - (int)(4 * walk.group);
+                    v[k].x = p[0];
+                    if (n > 1) v[k].y = p[1];
+                    if (n > 2) v[k].z = p[2];
+                    if (n > 3) v[k].w = p[3];
+                }
+                walk.next();
             }
-#pragma unroll 4
-            for (int c = lane; c < a.C; c += 32) most = fmaxf(most, finite_abs(m[r * ld + c]));
+#pragma unroll
+            for (int k = 0; k < 4; ++k) most = fmaxf(fmaxf(most, fmaxf(finite_abs(v[k].x), finite_abs(v[k].y))), fmaxf(finite_abs(v[k].z), finite_abs(v[k].w)));
         }
         most = block_max(most, shared);
         if (threadIdx.x == 0) a.largest[b] = most;
@@ -146,7 +181,7 @@ struct LossPack {
     void *dx;                                 // rows without a label: zeros
     long ld_dx;
 };
-constexpr int kPackRows = 32, kPackThreads = 256;
+constexpr int kPackRows = 64, kPackThreads = 256;
 
 // The power of two that puts `most` between 2^14 and 2^15.
 __device__ __forceinline__ float half_scale(float most) {
@@ -155,55 +190,60 @@ __device__ __forceinline__ float half_scale(float most) {
     frexpf(most, &e);                         // most < 2^e
     return ldexpf(1.f, min(max(15 - e, -60), 60));
 }
-template <typename T> __device__ __forceinline__ uint16_t bits16(float v) {
-    T t;
-    from_f32(t, v);
-    return *reinterpret_cast<const uint16_t *>(&t);
-}
-// A row's columns, eight a lane, times f, into its planes.  T: float32 into two float16 halves, else the type itself.
-template <typename T>
-__device__ __forceinline__ void pack_row(const T *row, bool vec, int C, int Cp, float f, bool scaled, uint16_t *out, long plane) {
-    for (int c = (threadIdx.x & 31) * 8; c < Cp; c += 256) {
-        float v[8];
-        __align__(16) T e[8];
-        if (vec) {
+// Eight columns as they lie in memory.
+template <typename T> struct LossEight { uint4 q[sizeof(T) / 2]; };
+template <typename T> __device__ __forceinline__ void eight_of(const T *p, bool vec, int left, LossEight<T> &e) {
+    if (vec) {
 #pragma unroll
-            for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4 *>(e)[i] = reinterpret_cast<const uint4 *>(row + c)[i];
-        } else {
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) e.q[i] = reinterpret_cast<const uint4 *>(p)[i];
+    } else {
+        T *t = reinterpret_cast<T *>(e.q);
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (c + i < C) e[i] = row[c + i];
-                else from_f32(e[i], 0.f);
-        }
-        __align__(16) uint16_t h[8], l[8];
-        if constexpr (sizeof(T) == 2) {
-            if (!scaled) {
-                *reinterpret_cast<uint4 *>(out + c) = *reinterpret_cast<const uint4 *>(e);
-                continue;
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) h[i] = bits16<T>(to_f32(e[i]) * f);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                v[i] = e[i] * f;
-                const __half hi = __float2half_rn(v[i]);
-                h[i] = __half_as_ushort(hi);
-                l[i] = __half_as_ushort(__float2half_rn(v[i] - __half2float(hi)));
-            }
-            *reinterpret_cast<uint4 *>(out + plane + c) = *reinterpret_cast<const uint4 *>(l);
-        }
-        *reinterpret_cast<uint4 *>(out + c) = *reinterpret_cast<const uint4 *>(h);
+        for (int i = 0; i < 8; ++i)
+            if (i < left) t[i] = p[i];
+            else from_f32(t[i], 0.f);
     }
+}
+// Times f, into their planes.  T: float32 into two float16 halves, else the type itself; as they are where not `scaled`.
+template <typename T>
+__device__ __forceinline__ void pack_eight(const LossEight<T> &e, float f, bool scaled, uint16_t *out, long plane) {
+    const T *t = reinterpret_cast<const T *>(e.q);
+    __align__(16) uint16_t h[8], l[8];
+    if constexpr (sizeof(T) == 2) {
+        if (!scaled) {
+            *reinterpret_cast<uint4 *>(out) = e.q[0];
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            T v;
+            from_f32(v, to_f32(t[i]) * f);
+            h[i] = *reinterpret_cast<const uint16_t *>(&v);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float v = t[i] * f;
+            const __half hi = __float2half_rn(v);
+            h[i] = __half_as_ushort(hi);
+            l[i] = __half_as_ushort(__float2half_rn(v - __half2float(hi)));
+        }
+        *reinterpret_cast<uint4 *>(out + plane) = *reinterpret_cast<const uint4 *>(l);
+    }
+    *reinterpret_cast<uint4 *>(out) = *reinterpret_cast<const uint4 *>(h);
 }
 template <typename T>
 __global__ void __launch_bounds__(kPackThreads) loss_pack_kernel(const LossPack a) {
     __shared__ float shared[32];
     __shared__ uint32_t sums[2][kPackThreads / 32];
+    __shared__ long to_row[kPackRows];                        // of packed X; -1: no label
+    __shared__ float d_row[kPackRows];                        // dloss / dmax
     ptx::grid_launch();
     ptx::grid_wait();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     constexpr bool kHalves = sizeof(T) == 4;
+    constexpr int kBatch = 4;                                 // groups of eight columns that are asked for before the first is stored
+    const uint32_t groups = (uint32_t)a.Cp / 8;
     float sx = 1.f, sw = 1.f;
     if constexpr (kHalves) {
         float mx = 0.f, mw = 0.f;
@@ -213,11 +253,22 @@ __global__ void __launch_bounds__(kPackThreads) loss_pack_kernel(const LossPack 
         sw = half_scale(block_max(mw, shared));
     }
     if ((int)blockIdx.x >= a.pack_blocks) {                   // W
-        const long step = (long)(gridDim.x - a.pack_blocks) * (kPackThreads / 32);
         const T *w = static_cast<const T *>(a.w);
         const bool vec = a.C % 8 == 0 && a.ld_w * (long)sizeof(T) % 16 == 0 && (reinterpret_cast<uintptr_t>(w) & 15) == 0;
-        for (long r = (long)(blockIdx.x - a.pack_blocks) * (kPackThreads / 32) + warp; r < a.w_rows; r += step)
-            pack_row(w + r * a.ld_w, vec, a.C, a.Cp, sw, kHalves, a.pw + r * a.Cp, a.w_rows * a.Cp);
+        LossWalk walk((uint64_t)(blockIdx.x - a.pack_blocks) * kPackThreads + threadIdx.x, (uint64_t)(gridDim.x - a.pack_blocks) * kPackThreads, groups);
+        while (walk.row < a.w_rows) {
+            LossEight<T> e[kBatch];
+            long at[kBatch];
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) {
+                at[k] = walk.row < a.w_rows ? walk.row * a.Cp + walk.group * 8 : -1;
+                if (at[k] >= 0) eight_of(w + walk.row * a.ld_w + walk.group * 8, vec, a.C - (int)walk.group * 8, e[k]);
+                walk.next();
+            }
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k)
+                if (at[k] >= 0) pack_eight(e[k], sw, kHalves, a.pw + at[k], a.w_rows * a.Cp);
+        }
         return;
     }
     // labelled rows before this block's chunk, and in all
@@ -237,52 +288,78 @@ __global__ void __launch_bounds__(kPackThreads) loss_pack_kernel(const LossPack 
         total += __shfl_xor_sync(0xffffffffu, total, o);
     }
     if (lane == 0) { sums[0][warp] = base; sums[1][warp] = total; }
-    __syncthreads();
+    dmax = block_max(dmax, shared);                           // (and a barrier for the sums)
     base = total = 0;
     for (int w = 0; w < kPackThreads / 32; ++w) { base += sums[0][w]; total += sums[1][w]; }
-    dmax = block_max(dmax, shared);
     if (!a.dloss || !(dmax > 0.f)) dmax = 1.f;
     if (blockIdx.x == 0 && threadIdx.x == 0) *a.info = LossInfo{total, sx, sw, dmax};
-    const T *x = static_cast<const T *>(a.x);
-    const bool vec = a.C % 8 == 0 && a.ld_x * (long)sizeof(T) % 16 == 0 && (reinterpret_cast<uintptr_t>(x) & 15) == 0;
-    const long plane = a.cap * a.Cp;
-    for (int k = warp; k < kPackRows && n0 + k < a.rows; k += kPackThreads / 32) {
-        const long n = n0 + k;
+    const int rows = (int)min((long)kPackRows, a.rows - n0);
+    if ((int)threadIdx.x < rows) {
+        const long n = n0 + threadIdx.x;
         const int rank = a.rank[n];
-        if (rank < 0) {
-            if (a.loss) {
-                if (lane == 0) { a.loss[n] = 0.f; a.lse[n] = 0.f; }
-            } else if (a.dx) {
-                T *dx = static_cast<T *>(a.dx) + n * a.ld_dx;
-                T zero;
-                from_f32(zero, 0.f);
-                for (int c = lane; c < a.C; c += 32) dx[c] = zero;
-            }
-            continue;
-        }
-        const long to = (long)base + rank;
-        pack_row(x + n * a.ld_x, vec, a.C, a.Cp, sx, kHalves, a.px + to * a.Cp, plane);
-        if (a.loss == nullptr) {
-            const float d = a.dloss ? a.dloss[n] : 1.f;
-            if (a.pd) pack_row(x + n * a.ld_x, vec, a.C, a.Cp, sx * (d / dmax), true, a.pd + to * a.Cp, plane);
-            if (lane == 0) {
+        const long to = rank < 0 ? -1 : (long)base + rank;
+        to_row[threadIdx.x] = to;
+        if (rank >= 0) {
+            a.index[to] = (int)n;
+            a.label[to] = (int)label_at(a.labels, a.wide, n);
+            if (a.loss == nullptr) {
+                const float d = a.dloss ? a.dloss[n] : 1.f;
+                d_row[threadIdx.x] = d / dmax;
                 a.lse2[to] = a.lse_in[n] * 1.4426950408889634f;
                 a.coef[to] = d * a.mult;
             }
-        }
-        if (lane == 0) {
-            a.index[to] = (int)n;
-            a.label[to] = (int)label_at(a.labels, a.wide, n);
+        } else if (a.loss) {
+            a.loss[n] = 0.f;
+            a.lse[n] = 0.f;
         }
     }
-    // the rest of the last tile (a whole one where no row has a label)
-    const long end = min(a.cap, ((long)max(total, 1u) + 255) / 256 * 256);
-    for (long r = total + (long)blockIdx.x * (kPackThreads / 32) + warp; r < end; r += (long)a.pack_blocks * (kPackThreads / 32))
-        for (int h = 0; h < (kHalves ? 2 : 1); ++h)
-            for (int c = lane * 8; c < a.Cp; c += 256) {
-                *reinterpret_cast<uint4 *>(a.px + h * plane + r * a.Cp + c) = make_uint4(0, 0, 0, 0);
-                if (a.pd) *reinterpret_cast<uint4 *>(a.pd + h * plane + r * a.Cp + c) = make_uint4(0, 0, 0, 0);
+    __syncthreads();
+    const T *x = static_cast<const T *>(a.x);
+    T *dx = static_cast<T *>(a.dx);
+    const bool vec = a.C % 8 == 0 && a.ld_x * (long)sizeof(T) % 16 == 0 && (reinterpret_cast<uintptr_t>(x) & 15) == 0;
+    const bool vec_dx = a.C % 8 == 0 && a.ld_dx * (long)sizeof(T) % 16 == 0 && (reinterpret_cast<uintptr_t>(dx) & 15) == 0;
+    const long plane = a.cap * a.Cp;
+    LossWalk walk(threadIdx.x, kPackThreads, groups);
+    while (walk.row < rows) {
+        LossEight<T> e[kBatch];
+        int row[kBatch], col[kBatch];
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) {
+            row[k] = (int)walk.row; col[k] = (int)walk.group * 8;
+            if (walk.row < rows && to_row[row[k]] >= 0) eight_of(x + (n0 + row[k]) * a.ld_x + col[k], vec, a.C - col[k], e[k]);
+            walk.next();
+        }
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) {
+            if (row[k] >= rows) break;
+            const long to = to_row[row[k]];
+            if (to >= 0) {
+                pack_eight(e[k], sx, kHalves, a.px + to * a.Cp + col[k], plane);
+                if (a.pd) pack_eight(e[k], sx * d_row[row[k]], true, a.pd + to * a.Cp + col[k], plane);
+            } else if (dx) {
+                T *p = dx + (n0 + row[k]) * a.ld_dx + col[k];
+                if (vec_dx) {
+#pragma unroll
+                    for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4 *>(p)[i] = make_uint4(0, 0, 0, 0);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        if (col[k] + i < a.C) from_f32(p[i], 0.f);
+                }
             }
+        }
+    }
+    // Backward: zeros up to the next 64 rows, which the products that sum over rows read.  (Others read whole tiles, but a row that is none reaches nothing but its own results,
+    // which nobody looks at.)
+    if (a.loss == nullptr) {
+        const long end = min(a.cap, ((long)max(total, 1u) + 63) / 64 * 64);
+        for (long r = total + (long)blockIdx.x * (kPackThreads / 32) + warp; r < end; r += (long)a.pack_blocks * (kPackThreads / 32))
+            for (int h = 0; h < (kHalves ? 2 : 1); ++h)
+                for (int c = lane * 8; c < a.Cp; c += 256) {
+                    *reinterpret_cast<uint4 *>(a.px + h * plane + r * a.Cp + c) = make_uint4(0, 0, 0, 0);
+                    if (a.pd) *reinterpret_cast<uint4 *>(a.pd + h * plane + r * a.Cp + c) = make_uint4(0, 0, 0, 0);
+                }
+    }
 }
 
 // ---------------------------------------------------------------- the products
@@ -309,6 +386,15 @@ struct LossArgs {
     int v0, words;               // the piece of the vocabulary: from v0 on
     int width, tiles_v;          // X W^T: columns of a tile, tiles across
     const int *label, *index;
+    // X as it stands, all of its rows (a single tile of them, where packing would save none): labels as they stand, and how many rows
+    const void *labels;
+    int wide, direct;
+    __device__ __forceinline__ int label_of(int row) const {
+        if (!direct) return label[row];
+        const int64_t l = label_at(labels, wide, row);
+        return l >= 0 && l < V ? (int)l : -1;
+    }
+    uint32_t *gave_up;           // direct: a word for every pair's block, joined behind
     // forward: maximum and sum of 2 tiles_v parts of a row (in units of ln 2), the label's logit
     float2 *part;
     float *chosen;
@@ -521,35 +607,83 @@ __device__ __forceinline__ bool loss_sums(LossPipe &q, int deep, int cols, float
     return true;
 }
 
-// Forward: maximum and sum of exponentials of a row's part of the tile, and its label's logit where that is among them.
-__device__ __forceinline__ void loss_stats(const LossArgs &a, const LossUnit &u, float c2, int rows, int row, int col0, int cols, int half, const float (&v)[128]) {
-    const int at = row < rows ? a.label[row] - col0 : -1;                // the label's column here
-    float m = -INFINITY, l = 0.f;
+// Forward: maximum and sum of exponentials of 64 columns of a row more (`left` of them are words), in units of ln 2.
+struct LossStat { float m, l; };
+__device__ __forceinline__ void loss_stat(LossStat &s, float (&v)[64], int left, float c2) {
+    if (left <= 0) return;
+    if (left < 64) {
 #pragma unroll
-    for (int k = 0; k < 128; k += 32) {
-        if (k >= cols || col0 + k >= a.V) break;
-        const int left = a.V - col0 - k;                                 // columns that are words
-        float s[32], mx = -INFINITY;
+        for (int e = 0; e < 64; ++e) v[e] = e < left ? v[e] : -INFINITY;
+    }
+    float mx[4] = {v[0], v[1], v[2], v[3]};
 #pragma unroll
-        for (int e = 0; e < 32; ++e) {
-            s[e] = v[k + e] * c2;
-            if (left < 32 && e >= left) s[e] = -INFINITY;
+    for (int e = 4; e < 64; e += 4)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) mx[i] = fmaxf(mx[i], v[e + i]);
+    const float next = fmaxf(s.m, fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * c2), ref = next == -INFINITY ? 0.f : next;
+    float l[4] = {s.l * ptx::ex2(s.m - ref), 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int e = 0; e < 64; ++e) l[e & 3] += ptx::ex2(fmaf(v[e], c2, -ref));
+    s.l = (l[0] + l[1]) + (l[2] + l[3]);
+    s.m = next;
+}
+// The value at place `at` (0 to 63), by halves.
+__device__ __forceinline__ float loss_pick(const float (&v)[64], int at) {
+    float t[32];
+#pragma unroll
+    for (int e = 0; e < 32; ++e) t[e] = at & 32 ? v[e + 32] : v[e];
+#pragma unroll
+    for (int n = 16; n > 0; n >>= 1)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+            if (e < n) t[e] = at & n ? t[e + n] : t[e];
+    return t[0];
+}
+// A tile's part: the sums straight from tensor memory, 64 columns at a time, where one set of them is all there is; else (kPlanes = 2, widths beyond 4096) added up in
+// registers first.
+template <int kPlanes>
+__device__ __forceinline__ bool loss_stats(LossPipe &q, const LossArgs &a, const LossUnit &u, float c2, int rows, int row, int col0, int cols, int half) {
+    const bool any = row - (int)(threadIdx.x & 31) < rows;               // of the warp's rows
+    const int at = row < rows ? a.label_of(row) - col0 : -1;             // the label's column here
+    LossStat s{-INFINITY, 0.f};
+    auto take = [&](float (&v)[64], int k) {
+        if (__any_sync(0xffffffffu, at >= k && at < k + 64)) {
+            const float c = loss_pick(v, at - k);
+            if (at >= k && at < k + 64) a.chosen[row] = c * c2;
         }
+        loss_stat(s, v, a.V - col0 - k, c2);
+    };
+    if (kPlanes == 1 && u.kb1 <= LossShape<kPlanes>::kChunk) {
+        const int warp = ptx::warp_index(), quad = warp & 3;
+        const uint32_t acc = q.tmem + ((uint32_t)(quad * 32) << 16) + half * cols + (q.c & 1) * 256;
+        const bool ok = ptx::mbar_wait(q.acc_full(q.c & 1), (q.c / 2) & 1, q.abort_flag, 114);
+        if (!__all_sync(0xffffffffu, ok)) return false;
+        ptx::tc_fence_after();
+        if (any)
+            for (int k = 0; k < cols; k += 64) {
+                uint32_t t[2][32];
+                ptx::tmem_ld32(acc + k, t[0]);
+                ptx::tmem_ld32(acc + k + 32, t[1]);
+                ptx::tmem_wait_ld();
+                float v[64];
 #pragma unroll
-        for (int e = 0; e < 32; ++e) mx = fmaxf(mx, s[e]);
-        const float next = fmaxf(m, mx), ref = next == -INFINITY ? 0.f : next;
-        l *= ptx::ex2(m - ref);
-#pragma unroll
-        for (int e = 0; e < 32; ++e) l += ptx::ex2(s[e] - ref);
-        m = next;
-        if (__any_sync(0xffffffffu, at >= k && at < k + 32)) {
-            float c = 0.f;
-#pragma unroll
-            for (int e = 0; e < 32; ++e) c = at == k + e ? s[e] : c;
-            if (at >= k && at < k + 32) a.chosen[row] = c;
+                for (int e = 0; e < 64; ++e) v[e] = __uint_as_float(t[e >> 5][e & 31]);
+                take(v, k);
+            }
+        ptx::tc_fence_before();
+        __syncwarp();
+        if ((threadIdx.x & 31) == 0) ptx::mbar_arrive_cluster(ptx::in_block(q.acc_empty(q.c & 1), 0));
+        ++q.c;
+    } else {
+        float v[128];
+        if (!loss_sums<kPlanes>(q, u.kb1, cols, v)) return false;
+        if (any) {
+            take(reinterpret_cast<float (&)[64]>(v[0]), 0);
+            if (cols > 64) take(reinterpret_cast<float (&)[64]>(v[64]), 64);
         }
     }
-    if (row < rows) a.part[((long)u.j * 2 + half) * a.cap + row] = make_float2(m, l);
+    if (row < rows) a.part[((long)u.j * 2 + half) * a.cap + row] = make_float2(s.m, s.l);
+    return true;
 }
 
 // Backward: q of 32 rows and 64 columns at a time, in 16 bits (halves), to G.
@@ -693,7 +827,7 @@ __global__ void __launch_bounds__(kLossThreads, 1) loss_kernel(const __grid_cons
     ptx::grid_launch();
     ptx::grid_wait();
     const int warp = ptx::warp_index(), pair = (int)(blockIdx.x >> 1), pairs = (int)(gridDim.x >> 1), in_pair = (int)(blockIdx.x & 1);
-    const LossInfo info = *a.info;
+    const LossInfo info = kKind == kLossStats && a.direct ? LossInfo{(uint32_t)a.direct, 1.f, 1.f, 1.f} : *a.info;
     const int rows = (int)info.rows;
     // Registers of the launch, 384 x 168, as 128 x 40 (the loading and the issuing warp, two that idle) and 256 x 232: the result warps' hold their 128 sums.
     if (warp == 0) {
@@ -713,11 +847,14 @@ __global__ void __launch_bounds__(kLossThreads, 1) loss_kernel(const __grid_cons
         LossUnits<kKind> units(a, rows, pair, pairs);
         LossUnit u;
         while (units.next(u)) {
+            const int row = u.i * 256 + in_pair * 128 + quad * 32 + lane;
+            if constexpr (kKind == kLossStats) {
+                if (!loss_stats<kPlanes>(q, a, u, c2, rows, row, u.j * a.width + half * cols, cols, half)) break;
+                continue;
+            }
             float v[128];
             if (!loss_sums<kPlanes>(q, u.kb1 - u.kb0, cols, v)) break;
-            const int row = u.i * 256 + in_pair * 128 + quad * 32 + lane;
-            if constexpr (kKind == kLossStats) loss_stats(a, u, c2, rows, row, u.j * a.width + half * cols, cols, half, v);
-            else if constexpr (kKind == kLossWeights) loss_weights<kPlanes>(q, maps, a, u, c2, rows, row, u.j * a.width + half * cols, cols, v);
+            if constexpr (kKind == kLossWeights) loss_weights<kPlanes>(q, maps, a, u, c2, rows, row, u.j * a.width + half * cols, cols, v);
             else if (u.slot >= 0) {
                 float *slot = a.slots + (((long)u.slot * 2 + in_pair) * a.grad_width + half * cols) * 128 + quad * 32 + lane;
 #pragma unroll
@@ -737,14 +874,18 @@ __global__ void __launch_bounds__(kLossThreads, 1) loss_kernel(const __grid_cons
     __syncthreads();
     let_arrive(q.abort_flag);
     ptx::cluster_meet();                                      // (nobody's shared or tensor memory is needed any more)
-    if (threadIdx.x == 0 && abort_flag != 0) *a.status = abort_flag;
+    if (threadIdx.x == 0) {
+        if (kKind == kLossStats && a.direct) a.gave_up[blockIdx.x] = abort_flag;
+        else if (abort_flag != 0) *a.status = abort_flag;
+    }
     if (warp == 1) {
         ptx::tc_fence_after();
         ptx::tmem_dealloc_for<2>(q.tmem, 512);
     }
 }
 
-// Tiles whose K several pairs have shared: a warp 32 rows and 32 columns, the shares in the order of K.
+// Tiles whose K several pairs have shared: 32 rows and 32 columns by one warp, or, where many pairs have (a few tiles summed over many rows), by 2, 4 or 8 that take their
+// shares in turn and are added up in order.
 constexpr int kJoinWarps = 8;
 template <typename E>
 __global__ void __launch_bounds__(32 * kJoinWarps) loss_join_kernel(const LossArgs a, int pairs) {
@@ -753,33 +894,54 @@ __global__ void __launch_bounds__(32 * kJoinWarps) loss_join_kernel(const LossAr
     ptx::grid_wait();
     const LossInfo info = *a.info;
     const LossSplit s(a, (int)info.rows, pairs);
+    if (s.steps == 0) return;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, blocks_of_tile = 8 * (a.grad_width / 32);   // (2 blocks, 4 quarters of rows)
-    const long at = (long)blockIdx.x * kJoinWarps + warp;
-    const int rest = (int)(at / blocks_of_tile), part = (int)(at % blocks_of_tile), block = part & 1, quad = part >> 1 & 3, col = (part >> 3) * 32;
-    const int rest_w = s.tiles_w - s.full_w;
-    if (rest >= rest_w + s.tiles_x - s.full_x) return;
-    const bool dx = rest >= rest_w;
-    const long start = dx ? (long)rest_w * s.deep_w + (long)(rest - rest_w) * s.deep_x : (long)rest * s.deep_w, end = start + (dx ? s.deep_x : s.deep_w);
-    const int tile = dx ? s.full_x + rest - rest_w : s.full_w + rest;
-    // the first pair whose share reaches into the tile
-    int p = (int)(start * s.sharing / s.steps);
-    while (p > 0 && s.share(p) > start) --p;
-    while (s.share(p + 1) <= start) ++p;
-    if (s.share(p) <= start && s.share(p + 1) >= end) return;                       // (all of it is one pair's, which has finished it)
-    float v[32];
+    const int rest_w = s.tiles_w - s.full_w, rest_all = rest_w + s.tiles_x - s.full_x;
+    const long shares = (long)max(s.deep_w, s.deep_x) * s.sharing / s.steps;                                // of a tile, about
+    const int team = shares < 4 ? 1 : shares < 8 ? 2 : shares < 16 ? 4 : 8, member = warp % team;
+    const long items = (long)rest_all * blocks_of_tile, step = (long)gridDim.x * (kJoinWarps / team);
+    for (long first = (long)blockIdx.x * (kJoinWarps / team); first < items; first += step) {               // (the same for all warps of the block)
+        const long at = first + warp / team;
+        const int rest = (int)(at / blocks_of_tile), part = (int)(at % blocks_of_tile), block = part & 1, quad = part >> 1 & 3, col = (part >> 3) * 32;
+        const bool dx = rest >= rest_w;
+        const long start = dx ? (long)rest_w * s.deep_w + (long)(rest - rest_w) * s.deep_x : (long)rest * s.deep_w, end = start + (dx ? s.deep_x : s.deep_w);
+        const int tile = dx ? s.full_x + rest - rest_w : s.full_w + rest;
+        float v[32];
 #pragma unroll
-    for (int e = 0; e < 32; ++e) v[e] = 0.f;
-    for (; p < s.sharing && s.share(p) < end; ++p) {
-        const int slot = 2 * p + (s.share(p) > start ? 0 : 1);
-        // (a share that begins with the tile, or before it, has it as its last; one that begins inside it as its first)
-        const float *from = a.slots + (((long)slot * 2 + block) * a.grad_width + col) * 128 + quad * 32 + lane;
+        for (int e = 0; e < 32; ++e) v[e] = 0.f;
+        bool shared = false;
+        if (at < items) {
+            // the first pair whose share reaches into the tile
+            int p = (int)(start * s.sharing / s.steps);
+            while (p > 0 && s.share(p) > start) --p;
+            while (s.share(p + 1) <= start) ++p;
+            shared = s.share(p) > start || s.share(p + 1) < end;                                            // (else it is all one pair's, which has finished it)
+            for (p += member; shared && p < s.sharing && s.share(p) < end; p += team) {
+                // (a share that begins with the tile, or before it, has it as its last; one that begins inside it as its first)
+                const float *from = a.slots + (((long)(2 * p + (s.share(p) > start ? 0 : 1)) * 2 + block) * a.grad_width + col) * 128 + quad * 32 + lane;
+                float t[32];
 #pragma unroll
-        for (int e = 0; e < 32; ++e) v[e] += from[e * 128];
+                for (int e = 0; e < 32; ++e) t[e] = from[e * 128];
+#pragma unroll
+                for (int e = 0; e < 32; ++e) v[e] += t[e];
+            }
+        }
+        if (team > 1) {
+            float *own = reinterpret_cast<float *>(pieces[warp]);
+#pragma unroll
+            for (int e = 0; e < 32; ++e) own[e * 32 + lane] = v[e];
+            __syncthreads();
+            if (member == 0)
+                for (int m = 1; m < team; ++m)
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) v[e] += reinterpret_cast<const float *>(pieces[warp + m])[e * 32 + lane];
+            __syncthreads();
+        }
+        if (member == 0 && shared) loss_gradient<E>(ptx::smem_u32(pieces[warp]), a, info, dx, tile / a.tiles_c, tile % a.tiles_c, block, quad, col, v);
     }
-    loss_gradient<E>(ptx::smem_u32(pieces[warp]), a, info, dx, tile / a.tiles_c, tile % a.tiles_c, block, quad, col, v);
 }
 
-// Parts of a row's statistics, joined: 32 rows a block, its warps taking the parts in turn.
+// Parts of a row's statistics, joined: 32 rows a block, its warps (as many as the parts keep busy) taking the parts in turn.
 constexpr int kMergeWarps = 16;
 struct LossMerge {
     const LossInfo *info;
@@ -789,12 +951,24 @@ struct LossMerge {
     long cap;
     int parts;
     float *loss, *lse;
+    // rows as they stand (LossArgs): labels, and how many
+    const void *labels;
+    int wide, V, direct;
+    const uint32_t *gave_up;
+    uint32_t *status;
+    int blocks;
 };
 __global__ void __launch_bounds__(32 * kMergeWarps) loss_merge_kernel(const LossMerge a) {
     __shared__ float2 shared[kMergeWarps][32];
     ptx::grid_launch();
     ptx::grid_wait();
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rows = (int)a.info->rows;
+    const int warps = blockDim.x / 32, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rows = a.direct ? a.direct : (int)a.info->rows;
+    if (a.direct && blockIdx.x == 0 && warp == 0) {
+        uint32_t code = 0;
+        for (int b = lane; b < a.blocks; b += 32) code = max(code, a.gave_up[b]);
+        code = __reduce_max_sync(0xffffffffu, code);
+        for (int i = lane; i < (int)(kHeaderBytes / 4); i += 32) a.status[i] = i == 0 ? code : 0;
+    }
     for (long r0 = (long)blockIdx.x * 32; r0 < rows; r0 += (long)gridDim.x * 32) {
         const long row = r0 + lane;
         float m = -INFINITY, l = 0.f;
@@ -804,21 +978,34 @@ __global__ void __launch_bounds__(32 * kMergeWarps) loss_merge_kernel(const Loss
             m = next;
         };
         if (row < rows) {
-#pragma unroll 4
-            for (int p = warp; p < a.parts; p += kMergeWarps) take(a.part[p * a.cap + row]);
+            int p = warp;
+            for (; p + 3 * warps < a.parts; p += 4 * warps) {
+                float2 x[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) x[k] = a.part[(long)(p + k * warps) * a.cap + row];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) take(x[k]);
+            }
+            for (; p < a.parts; p += warps) take(a.part[(long)p * a.cap + row]);
         }
-        shared[warp][lane] = make_float2(m, l);
-        __syncthreads();
+        if (warps > 1) {
+            shared[warp][lane] = make_float2(m, l);
+            __syncthreads();
+        }
         if (warp == 0 && row < rows) {
-            m = -INFINITY, l = 0.f;
-            for (int w = 0; w < kMergeWarps; ++w) take(shared[w][lane]);
+            for (int w = 1; w < warps; ++w) take(shared[w][lane]);
+            bool there = true;
+            if (a.direct) {
+                const int64_t label = label_at(a.labels, a.wide, row);
+                there = label >= 0 && label < a.V;
+            }
             // (m and the label's logit were rounded alike: where the label is the maximum nothing is left of their difference)
             const float log_l = logf(l);
-            const int n = a.index[row];
-            a.loss[n] = (m - a.chosen[row]) * 0.69314718056f + log_l;
-            a.lse[n] = m * 0.69314718056f + log_l;
+            const long n = a.direct ? row : a.index[row];
+            a.loss[n] = there ? (m - a.chosen[row]) * 0.69314718056f + log_l : 0.f;
+            a.lse[n] = there ? m * 0.69314718056f + log_l : 0.f;
         }
-        __syncthreads();
+        if (warps > 1) __syncthreads();
     }
 }
 

@@ -46,7 +46,8 @@ LossPlan loss_plan(const flare_loss_desc_t *d, int sms) {
     LossPlan p{};
     const bool f32 = d->dtype == FLARE_DTYPE_F32;
     p.planes = f32 ? 2 : 1;
-    p.Cp = (d->width + 7) / 8 * 8;
+    // rows of packed X and W: whole 16 bytes, of wide ones whole lines (TMA takes 128-byte pieces of them)
+    p.Cp = d->width > 256 ? (d->width + 63) / 64 * 64 : (d->width + 7) / 8 * 8;
     p.chunks = (int)((d->rows + kLossChunk - 1) / kLossChunk);
     p.pairs = std::max(1, sms / 2);
     p.cap = std::max(1L, (long)(d->rows + 255) / 256) * 256;
@@ -65,6 +66,16 @@ LossPlan loss_plan(const flare_loss_desc_t *d, int sms) {
     p.tiles_c = (d->width + p.grad_width - 1) / p.grad_width;
     return p;
 }
+// Forward of up to eight rows (loss_few_kernel): rows it is compiled for, or 0 where X would not fit beside a second block of an SM.
+int few_rows(const flare_loss_desc_t *d) {
+    const int R = d->rows <= 1 ? 1 : d->rows <= 2 ? 2 : d->rows <= 4 ? 4 : 8;
+    return d->rows <= 8 && few_smem(R, d->width) <= 96 * 1024 ? R : 0;
+}
+int few_blocks(const flare_loss_desc_t *d, int sms) {
+    // rounds of equal size over the warps that are at work at a time
+    const long groups = (d->vocab + kFewWords - 1) / kFewWords, warps = (long)sms * (few_rows(d) <= 2 ? 4 : 2) * (kFewThreads / 32), rounds = (groups + warps - 1) / warps;
+    return (int)(((groups + rounds - 1) / rounds + kFewThreads / 32 - 1) / (kFewThreads / 32));
+}
 struct LossLayout { size_t info, rank, chunk, largest, px, pd, pw, index, label, part, chosen, gave_up, lse2, coef, g, acc, slots, total; };
 LossLayout loss_layout(const flare_loss_desc_t *d, const LossPlan &p, bool backward) {
     LossLayout w{};
@@ -81,7 +92,7 @@ LossLayout loss_layout(const flare_loss_desc_t *d, const LossPlan &p, bool backw
     take(w.label, sizeof(int) * (size_t)p.cap);
     if (!backward) {
         const long tiles = (d->vocab + p.width - 1) / p.width;
-        take(w.part, sizeof(float2) * 2 * (size_t)tiles * p.cap);
+        take(w.part, sizeof(float2) * std::max<size_t>(2 * (size_t)tiles, few_rows(d) ? few_blocks(d, 2 * p.pairs) : 0) * p.cap);
         take(w.chosen, sizeof(float) * (size_t)p.cap);
         take(w.gave_up, sizeof(uint32_t) * 2 * (size_t)p.pairs);
     } else {
@@ -133,10 +144,34 @@ int launch_loss(const LossMaps &maps, const LossArgs &a, int pairs, cudaStream_t
     return FLARE_OK;
 }
 
+int launch_merge(const LossMerge &m, long rows, cudaStream_t st) {
+    const int warps = std::min(kMergeWarps, std::max(1, m.parts / 4));
+    FLARE_CUDA(launch_after(loss_merge_kernel, (unsigned)std::min<long>((rows + 31) / 32, 65535L), 32 * warps, 0, st, m));
+    return FLARE_OK;
+}
+
 template <typename T>
 int launch_pack(const LossPack &k, int blocks, cudaStream_t st) {
     FLARE_CUDA(launch_after(loss_pack_kernel<T>, (unsigned)blocks, kPackThreads, 0, st, k));
     return FLARE_OK;
+}
+
+template <typename T, int R, bool kVec>
+int launch_few_as(const LossFew &f, int blocks, cudaStream_t st) {
+    static std::atomic<uint64_t> opt_in{0};
+    auto *kernel = loss_few_kernel<T, R, kVec>;
+    if (int rc = ensure_big_smem(kernel, opt_in, 96 * 1024)) return rc;
+    FLARE_CUDA(launch_after(kernel, (unsigned)blocks, kFewThreads, few_smem(R, f.C), st, f));
+    return FLARE_OK;
+}
+template <typename T>
+int launch_few(const LossFew &f, int R, int blocks, cudaStream_t st) {
+    const bool vec = f.C % 8 == 0 && aligned16(f.w) && f.ld_w * (long)sizeof(T) % 16 == 0;
+    auto launch = R == 1   ? (vec ? launch_few_as<T, 1, true> : launch_few_as<T, 1, false>)
+                  : R == 2 ? (vec ? launch_few_as<T, 2, true> : launch_few_as<T, 2, false>)
+                  : R == 4 ? (vec ? launch_few_as<T, 4, true> : launch_few_as<T, 4, false>)
+                           : (vec ? launch_few_as<T, 8, true> : launch_few_as<T, 8, false>);
+    return launch(f, blocks, st);
 }
 
 // Checks that forward and backward share.
@@ -206,6 +241,21 @@ int flare_loss_forward(const flare_loss_desc_t *desc, const void *x, const void 
     const LossPlan p = loss_plan(desc, device_info().sms);
     const LossLayout l = loss_layout(desc, p, false);
     char *ws = static_cast<char *>(workspace);
+    if (const int R = few_rows(desc)) {
+        LossFew f{};
+        f.x = x; f.w = w; f.labels = labels; f.wide = desc->label_bits == 64; f.rows = (int)desc->rows; f.C = desc->width; f.V = desc->vocab;
+        f.ld_x = desc->stride_x ? desc->stride_x : desc->width; f.ld_w = desc->stride_w ? desc->stride_w : desc->width; f.cap = p.cap; f.scale = desc->scale;
+        f.part = reinterpret_cast<float2 *>(ws + l.part); f.chosen = reinterpret_cast<float *>(ws + l.chosen);
+        const int blocks = few_blocks(desc, 2 * p.pairs);
+        if (int rc = desc->dtype == FLARE_DTYPE_F32    ? launch_few<float>(f, R, blocks, st)
+                     : desc->dtype == FLARE_DTYPE_BF16 ? launch_few<__nv_bfloat16>(f, R, blocks, st)
+                                                       : launch_few<__half>(f, R, blocks, st))
+            return rc;
+        LossMerge m{};
+        m.part = f.part; m.chosen = f.chosen; m.cap = p.cap; m.parts = blocks; m.loss = loss; m.lse = lse;
+        m.labels = labels; m.wide = f.wide; m.V = f.V; m.direct = f.rows; m.status = reinterpret_cast<uint32_t *>(ws);
+        return launch_merge(m, desc->rows, st);
+    }
     LossPack k{};
     k.loss = loss; k.lse = lse;
     LossMaps maps{};
@@ -229,9 +279,7 @@ int flare_loss_forward(const flare_loss_desc_t *desc, const void *x, const void 
     LossMerge m{};
     m.info = a.info; m.part = a.part; m.chosen = a.chosen; m.index = a.index; m.cap = p.cap; m.parts = 2 * a.tiles_v; m.loss = loss; m.lse = lse;
     m.labels = a.labels; m.wide = a.wide; m.V = a.V; m.direct = a.direct; m.gave_up = a.gave_up; m.status = a.status; m.blocks = 2 * pairs;
-    const int warps = std::min(kMergeWarps, std::max(1, m.parts / 4));
-    FLARE_CUDA(launch_after(loss_merge_kernel, (unsigned)std::min<long>((desc->rows + 31) / 32, 65535L), 32 * warps, 0, st, m));
-    return FLARE_OK;
+    return launch_merge(m, desc->rows, st);
 }
 
 int flare_loss_backward(const flare_loss_desc_t *desc, const void *x, const void *w, const void *labels, const float *lse, const float *dloss, void *dx, void *dw,
@@ -266,7 +314,7 @@ int flare_loss_backward(const flare_loss_desc_t *desc, const void *x, const void
         maps.d = maps.x;
     }
     if ((rc = make_plane_map(&maps.g, ws + l.g, bf16, p.Vp, p.cap, p.planes, p.Vp, 64)) != FLARE_OK) return rc;
-    if ((rc = make_plane_map(&maps.g_store, ws + l.g, bf16, p.Vp, p.cap, p.planes, p.Vp, 32)) != FLARE_OK) return rc;
+    a.g = reinterpret_cast<uint16_t *>(ws + l.g); a.ld_g = p.Vp;
     a.lse2 = k.lse2; a.coef = k.coef; a.grad_width = p.grad_width; a.tiles_c = p.tiles_c;
     a.dw = dw; a.dx = dx; a.ld_dw = ld_dw; a.ld_dx = ld_dx;
     auto fours = [&](const void *q, long ld) { return desc->width % 4 == 0 && ld % 4 == 0 && reinterpret_cast<uintptr_t>(q) % (4 * t) == 0; };

@@ -190,12 +190,12 @@ __device__ __forceinline__ float half_scale(float most) {
     frexpf(most, &e);                         // most < 2^e
     return ldexpf(1.f, min(max(15 - e, -60), 60));
 }
-// Eight columns as they lie in memory.
+// Eight columns as they lie in memory; `left` of them are, the others are zeros (vec: all or none).
 template <typename T> struct LossEight { uint4 q[sizeof(T) / 2]; };
 template <typename T> __device__ __forceinline__ void eight_of(const T *p, bool vec, int left, LossEight<T> &e) {
     if (vec) {
 #pragma unroll
-        for (int i = 0; i < (int)sizeof(T) / 2; ++i) e.q[i] = reinterpret_cast<const uint4 *>(p)[i];
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) e.q[i] = left > 0 ? reinterpret_cast<const uint4 *>(p)[i] : make_uint4(0, 0, 0, 0);
     } else {
         T *t = reinterpret_cast<T *>(e.q);
 #pragma unroll
@@ -338,6 +338,7 @@ __global__ void __launch_bounds__(kPackThreads) loss_pack_kernel(const LossPack 
                 if (a.pd) pack_eight(e[k], sx * d_row[row[k]], true, a.pd + to * a.Cp + col[k], plane);
             } else if (dx) {
                 T *p = dx + (n0 + row[k]) * a.ld_dx + col[k];
+                if (col[k] >= a.C) continue;
                 if (vec_dx) {
 #pragma unroll
                     for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4 *>(p)[i] = make_uint4(0, 0, 0, 0);
@@ -376,7 +377,7 @@ template <int kPlanes> struct LossShape {
 };
 constexpr size_t kLossSmem = 1024 + 6 * 2 * kLossHalfTile + 8 * kLossPiece + 256;
 
-struct LossMaps { CUtensorMap x, d, w, g, g_store; };         // in boxes of 64 x 64 (g_store: 32 rows of 64)
+struct LossMaps { CUtensorMap x, d, w, g; };                  // in boxes of 64 x 64
 struct LossArgs {
     const LossInfo *info;
     uint32_t *status;
@@ -400,6 +401,8 @@ struct LossArgs {
     float *chosen;
     // backward
     const float *lse2, *coef;
+    uint16_t *g;                 // planes [cap][ld_g]
+    long ld_g;
     int grad_width, tiles_c;     // columns of a gradient's tile, tiles across
     int first, last;             // of the pieces
     void *dw, *dx;
@@ -591,20 +594,41 @@ __device__ __forceinline__ bool loss_sums(LossPipe &q, int deep, int cols, float
         const bool ok = ptx::mbar_wait(q.acc_full(q.c & 1), (q.c / 2) & 1, q.abort_flag, 114);
         if (!__all_sync(0xffffffffu, ok)) return false;
         ptx::tc_fence_after();
+        if (kb == 0) {
 #pragma unroll
-        for (int k = 0; k < 128; k += 32) {
-            if (k >= cols) break;
-            uint32_t u[32];
-            ptx::tmem_ld32(acc + (q.c & 1) * 256 + k, u);
+            for (int k = 0; k < 128; k += 32)
+                if (k < cols) ptx::tmem_ld32(acc + (q.c & 1) * 256 + k, reinterpret_cast<uint32_t (&)[32]>(v[k]));
             ptx::tmem_wait_ld();
+        } else {
 #pragma unroll
-            for (int e = 0; e < 32; ++e) v[k + e] = kb == 0 ? __uint_as_float(u[e]) : v[k + e] + __uint_as_float(u[e]);
+            for (int k = 0; k < 128; k += 32) {
+                if (k >= cols) break;
+                uint32_t u[32];
+                ptx::tmem_ld32(acc + (q.c & 1) * 256 + k, u);
+                ptx::tmem_wait_ld();
+#pragma unroll
+                for (int e = 0; e < 32; ++e) v[k + e] += __uint_as_float(u[e]);
+            }
         }
         ptx::tc_fence_before();
         __syncwarp();
         if ((threadIdx.x & 31) == 0) ptx::mbar_arrive_cluster(ptx::in_block(q.acc_empty(q.c & 1), 0));
     }
     return true;
+}
+
+// What a result warp needs of its lanes' rows, asked for before it waits for their sums.
+struct LossRow { int label, index; float lse2, coef; };
+template <int kKind>
+__device__ __forceinline__ LossRow loss_row(const LossArgs &a, int rows, int row, bool wanted) {
+    LossRow r{-1, -1, 0.f, 0.f};
+    if (row < rows && wanted) {
+        if (kKind != kLossGrads) r.label = a.label_of(row);
+        if (kKind == kLossWeights) r.lse2 = a.lse2[row];
+        if (kKind == kLossGrads) r.index = a.index[row];
+        if (kKind != kLossStats) r.coef = a.coef[row];
+    }
+    return r;
 }
 
 // Forward: maximum and sum of exponentials of 64 columns of a row more (`left` of them are words), in units of ln 2.
@@ -642,9 +666,9 @@ __device__ __forceinline__ float loss_pick(const float (&v)[64], int at) {
 // A tile's part: the sums straight from tensor memory, 64 columns at a time, where one set of them is all there is; else (kPlanes = 2, widths beyond 4096) added up in
 // registers first.
 template <int kPlanes>
-__device__ __forceinline__ bool loss_stats(LossPipe &q, const LossArgs &a, const LossUnit &u, float c2, int rows, int row, int col0, int cols, int half) {
+__device__ __forceinline__ bool loss_stats(LossPipe &q, const LossArgs &a, const LossUnit &u, const LossRow &r, float c2, int rows, int row, int col0, int cols, int half) {
     const bool any = row - (int)(threadIdx.x & 31) < rows;               // of the warp's rows
-    const int at = row < rows ? a.label_of(row) - col0 : -1;             // the label's column here
+    const int at = r.label - col0;                                       // the label's column here (no label: below zero)
     LossStat s{-INFINITY, 0.f};
     auto take = [&](float (&v)[64], int k) {
         if (__any_sync(0xffffffffu, at >= k && at < k + 64)) {
@@ -686,39 +710,42 @@ __device__ __forceinline__ bool loss_stats(LossPipe &q, const LossArgs &a, const
     return true;
 }
 
-// Backward: q of 32 rows and 64 columns at a time, in 16 bits (halves), to G.
+// Backward: q of 32 rows and 64 columns at a time, in 16 bits (halves), to G by way of shared memory, so that eight lanes write 128 bytes of a row.
 template <int kPlanes>
-__device__ __forceinline__ void loss_weights(const LossPipe &q, const LossMaps &m, const LossArgs &a, const LossUnit &u, float c2, int rows, int row, int local0, int cols,
-                                             float (&v)[128]) {
+__device__ __forceinline__ void loss_weights(const LossPipe &q, const LossArgs &a, const LossRow &r, float c2, int rows, int row, int local0, int cols, float (&v)[128]) {
     const int lane = threadIdx.x & 31, col0 = a.v0 + local0;
     const uint32_t piece = q.pieces0 + (ptx::warp_index() - 4) * kLossPiece;
     const bool in = row < rows;
-    const int at = in ? a.label[row] - col0 : -1;
-    const float lse2 = in ? a.lse2[row] : 0.f, f = !in ? 0.f : a.bf16 ? a.coef[row] : 32768.f;
+    const int at = r.label - col0;                                       // (no label: below zero)
+    const float lse2 = r.lse2, f = !in ? 0.f : a.bf16 ? r.coef : 32768.f;
+    const int words = in ? a.V - col0 : 0;
 #pragma unroll
     for (int k = 0; k < 128; k += 64) {
         if (k >= cols) break;
-        const int left = in ? a.V - col0 - k : 0;
 #pragma unroll
         for (int e = 0; e < 64; ++e) {
             float p = ptx::ex2(fmaf(v[k + e], c2, -lse2));
             if (at == k + e) p -= 1.f;
-            v[k + e] = e < left ? p * f : 0.f;
+            v[k + e] = p * f;
+        }
+        if (words - k < 64) {                                            // beyond the vocabulary, or rows that are none: zeros whatever the sums hold
+#pragma unroll
+            for (int e = 0; e < 64; ++e)
+                if (e >= words - k) v[k + e] = 0.f;
         }
 #pragma unroll
         for (int h = 0; h < kPlanes; ++h) {
-            if (lane == 0) ptx::tma_store_wait<true>();
             __syncwarp();
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                uint32_t r[4];
+                uint32_t w[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     float &x = v[k + 8 * e + 2 * i], &y = v[k + 8 * e + 2 * i + 1];
-                    if (kPlanes == 1 && a.bf16) r[i] = ptx::pack_bf16(x, y);
+                    if (kPlanes == 1 && a.bf16) w[i] = ptx::pack_bf16(x, y);
                     else {
                         const __half2 t = __floats2half2_rn(x, y);
-                        r[i] = *reinterpret_cast<const uint32_t *>(&t);
+                        w[i] = *reinterpret_cast<const uint32_t *>(&t);
                         if (kPlanes == 2 && h == 0) {                     // (what is left is the low half)
                             const float2 b = __half22float2(t);
                             x -= b.x;
@@ -726,13 +753,14 @@ __device__ __forceinline__ void loss_weights(const LossPipe &q, const LossMaps &
                         }
                     }
                 }
-                ptx::sts128(piece + lane * 128 + ((e ^ (lane & 7)) << 4), r);
+                ptx::sts128(piece + lane * 128 + ((e ^ (lane & 7)) << 4), w);
             }
-            ptx::fence_proxy_async_smem();
             __syncwarp();
-            if (lane == 0) {
-                ptx::tma_store_3d(&m.g_store, piece, local0 + k, row - lane, h);
-                ptx::tma_store_commit();
+            uint16_t *out = a.g + ((long)h * a.cap + (row - lane) + (lane >> 3)) * a.ld_g + local0 + k + (lane & 7) * 8;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int t = 4 * e + (lane >> 3);
+                *reinterpret_cast<float4 *>(out + (long)4 * e * a.ld_g) = ptx::lds128(piece + t * 128 + (((lane & 7) ^ (t & 7)) << 4));
             }
         }
     }
@@ -772,7 +800,7 @@ __device__ __forceinline__ void loss_out(uint32_t piece, E *out, long ld, int fo
 }
 // 32 columns of a gradient's tile that are complete, tile-local from col on.
 template <typename E>
-__device__ __forceinline__ void loss_gradient(uint32_t piece, const LossArgs &a, const LossInfo &info, int dx, int i, int j, int block, int quad, int col, float *v) {
+__device__ __forceinline__ void loss_gradient(uint32_t piece, const LossArgs &a, const LossInfo &info, const LossRow &r, int dx, int i, int j, int block, int quad, int col, float *v) {
     const int lane = threadIdx.x & 31, local = i * 256 + block * 128 + quad * 32 + lane, c0 = j * a.grad_width + col;
     if (c0 >= a.C) return;
     if (!dx) {
@@ -792,11 +820,7 @@ __device__ __forceinline__ void loss_gradient(uint32_t piece, const LossArgs &a,
             return;
         }
     }
-    const bool in = local < (int)info.rows;
-    const float f = a.bf16 || !in ? 1.f : a.coef[local] / (32768.f * info.w_scale);
-#pragma unroll
-    for (int e = 0; e < 32; ++e) v[e] *= f;
-    loss_out<E>(piece, static_cast<E *>(a.dx), a.ld_dx, a.dx_fours, in ? a.index[local] : -1, c0, a.C, 1.f, v);
+    loss_out<E>(piece, static_cast<E *>(a.dx), a.ld_dx, a.dx_fours, r.index, c0, a.C, a.bf16 ? 1.f : r.coef / (32768.f * info.w_scale), v);
 }
 
 template <int kKind, int kPlanes, typename E>
@@ -849,12 +873,13 @@ __global__ void __launch_bounds__(kLossThreads, 1) loss_kernel(const __grid_cons
         while (units.next(u)) {
             const int row = u.i * 256 + in_pair * 128 + quad * 32 + lane;
             if constexpr (kKind == kLossStats) {
-                if (!loss_stats<kPlanes>(q, a, u, c2, rows, row, u.j * a.width + half * cols, cols, half)) break;
+                if (!loss_stats<kPlanes>(q, a, u, loss_row<kKind>(a, rows, row, true), c2, rows, row, u.j * a.width + half * cols, cols, half)) break;
                 continue;
             }
+            const LossRow r = loss_row<kKind>(a, rows, row, kKind != kLossGrads || u.dx);
             float v[128];
             if (!loss_sums<kPlanes>(q, u.kb1 - u.kb0, cols, v)) break;
-            if constexpr (kKind == kLossWeights) loss_weights<kPlanes>(q, maps, a, u, c2, rows, row, u.j * a.width + half * cols, cols, v);
+            if constexpr (kKind == kLossWeights) loss_weights<kPlanes>(q, a, r, c2, rows, row, u.j * a.width + half * cols, cols, v);
             else if (u.slot >= 0) {
                 float *slot = a.slots + (((long)u.slot * 2 + in_pair) * a.grad_width + half * cols) * 128 + quad * 32 + lane;
 #pragma unroll
@@ -863,11 +888,9 @@ __global__ void __launch_bounds__(kLossThreads, 1) loss_kernel(const __grid_cons
             } else {
 #pragma unroll
                 for (int k = 0; k < 128; k += 32)
-                    if (k < cols) loss_gradient<E>(piece, a, info, u.dx, u.i, u.j, in_pair, quad, half * cols + k, v + k);
+                    if (k < cols) loss_gradient<E>(piece, a, info, r, u.dx, u.i, u.j, in_pair, quad, half * cols + k, v + k);
             }
         }
-        if (lane == 0) ptx::tma_store_wait<false>();
-        __syncwarp();
     }
     __syncwarp();
     ptx::tc_fence_before();
@@ -916,14 +939,25 @@ __global__ void __launch_bounds__(32 * kJoinWarps) loss_join_kernel(const LossAr
             while (p > 0 && s.share(p) > start) --p;
             while (s.share(p + 1) <= start) ++p;
             shared = s.share(p) > start || s.share(p + 1) < end;                                            // (else it is all one pair's, which has finished it)
-            for (p += member; shared && p < s.sharing && s.share(p) < end; p += team) {
-                // (a share that begins with the tile, or before it, has it as its last; one that begins inside it as its first)
+            for (p += member; shared && p < s.sharing && s.share(p) < end; p += 2 * team) {
+                // two shares at a time (one that begins with the tile, or before it, has it as its last; one that begins inside it as its first)
+                const int p1 = p + team;
+                const bool two = p1 < s.sharing && s.share(p1) < end;
                 const float *from = a.slots + (((long)(2 * p + (s.share(p) > start ? 0 : 1)) * 2 + block) * a.grad_width + col) * 128 + quad * 32 + lane;
-                float t[32];
+                const float *from1 = a.slots + (((long)(2 * p1 + (s.share(p1) > start ? 0 : 1)) * 2 + block) * a.grad_width + col) * 128 + quad * 32 + lane;
+                float t[32], t1[32];
 #pragma unroll
                 for (int e = 0; e < 32; ++e) t[e] = from[e * 128];
+                if (two) {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) t1[e] = from1[e * 128];
+                }
 #pragma unroll
                 for (int e = 0; e < 32; ++e) v[e] += t[e];
+                if (two) {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) v[e] += t1[e];
+                }
             }
         }
         if (team > 1) {
@@ -937,12 +971,125 @@ __global__ void __launch_bounds__(32 * kJoinWarps) loss_join_kernel(const LossAr
                     for (int e = 0; e < 32; ++e) v[e] += reinterpret_cast<const float *>(pieces[warp + m])[e * 32 + lane];
             __syncthreads();
         }
-        if (member == 0 && shared) loss_gradient<E>(ptx::smem_u32(pieces[warp]), a, info, dx, tile / a.tiles_c, tile % a.tiles_c, block, quad, col, v);
+        if (member == 0 && shared)
+            loss_gradient<E>(ptx::smem_u32(pieces[warp]), a, info, loss_row<kLossGrads>(a, (int)info.rows, tile / a.tiles_c * 256 + block * 128 + quad * 32 + lane, dx), dx, tile / a.tiles_c, tile % a.tiles_c, block, quad, col, v);
+    }
+}
+
+// ---- forward of a few rows
+//
+// Up to eight rows are scored as fast as W can be read, by fused multiply-adds in float32 (two a row and pair of elements, beside two conversions; eight rows of 1024 take 8 us of issue slots
+// for a vocabulary whose 66 MB take 10): a tile of a tensor core's product would have 248 empty rows, and float32 inputs would have W read three times and written once for their halves.
+// A warp takes four words at a time, a lane eight columns of each (kVec: neighbours, 16 bytes a load; else 32 apart); X is in shared memory as float32, where the lanes' pieces of a row lie in
+// two sets of 16 bytes so that neighbouring lanes meet no bank conflict.  The 4 R sums are added up over the lanes by exchanges that halve their number (31 for all of 32 sums).
+constexpr int kFewThreads = 256, kFewWords = 4;
+struct LossFew {
+    const void *x, *w, *labels;
+    int wide, rows, C, V;
+    long ld_x, ld_w, cap;
+    float scale;
+    float2 *part;                // [blocks][cap]
+    float *chosen;
+};
+__host__ __device__ constexpr size_t few_smem(int R, int C) { return (size_t)R * ((C + 255) / 256 * 256) * sizeof(float); }
+template <typename T, int R, bool kVec>
+__global__ void __launch_bounds__(kFewThreads, R <= 2 ? 4 : 2) loss_few_kernel(const LossFew a) {
+    extern __shared__ float4 xs[];                            // [R][turns][2][32]
+    __shared__ float2 stats[kFewThreads / 32][32];
+    ptx::grid_launch();
+    ptx::grid_wait();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, turns = (a.C + 255) / 256;
+    // where lane l's i-th column of a turn lies: kVec 256 t + 8 l + i, else 256 t + l + 32 i
+    const T *x = static_cast<const T *>(a.x), *w = static_cast<const T *>(a.w);
+    for (int i = threadIdx.x; i < R * turns * 256; i += kFewThreads) {
+        const int r = i / (turns * 256), c = i % (turns * 256), t = c >> 8, l = kVec ? c >> 3 & 31 : c & 31, e = kVec ? c & 7 : c >> 5 & 7;
+        reinterpret_cast<float *>(xs)[(((r * turns + t) * 2 + (e >> 2)) * 32 + l) * 4 + (e & 3)] = r < a.rows && c < a.C ? to_f32(x[r * a.ld_x + c]) : 0.f;
+    }
+    constexpr int kSums = kFewWords * R, kSkip = kSums == 32 ? 0 : kSums == 16 ? 1 : kSums == 8 ? 2 : 3;   // lanes that hold the same sum: 2^kSkip
+    const int mine = lane >> kSkip, row = mine / kFewWords, word = mine % kFewWords;
+    int64_t label = -1;
+    if (row < a.rows) label = label_at(a.labels, a.wide, row);
+    const float c2 = a.scale * 1.4426950408889634f;
+    float m = -INFINITY, l = 0.f;
+    __syncthreads();
+    const int groups = (a.V + kFewWords - 1) / kFewWords;
+    for (int g = blockIdx.x * (kFewThreads / 32) + warp; g < groups; g += gridDim.x * (kFewThreads / 32)) {
+        const T *p[kFewWords];
+#pragma unroll
+        for (int k = 0; k < kFewWords; ++k) p[k] = w + (long)min(g * kFewWords + k, a.V - 1) * a.ld_w;     // (beyond the last word: that again)
+        float s[kSums];
+#pragma unroll
+        for (int i = 0; i < kSums; ++i) s[i] = 0.f;
+#pragma unroll 2
+        for (int t = 0; t < turns; ++t) {
+            const int c = t * 256 + (kVec ? lane * 8 : lane);
+            LossEight<T> e[kFewWords];
+#pragma unroll
+            for (int k = 0; k < kFewWords; ++k) {
+                if (kVec) {
+                    if (c < a.C) eight_of(p[k] + c, true, 8, e[k]);
+                    else
+#pragma unroll
+                        for (int i = 0; i < (int)sizeof(T) / 2; ++i) e[k].q[i] = make_uint4(0, 0, 0, 0);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        if (c + 32 * i < a.C) reinterpret_cast<T *>(e[k].q)[i] = p[k][c + 32 * i];
+                        else from_f32(reinterpret_cast<T *>(e[k].q)[i], 0.f);
+                }
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    const float4 v = xs[((r * turns + t) * 2 + h) * 32 + lane];
+#pragma unroll
+                    for (int k = 0; k < kFewWords; ++k) {
+                        const T *u = reinterpret_cast<const T *>(e[k].q) + 4 * h;
+                        float &q = s[r * kFewWords + k];
+                        q = fmaf(to_f32(u[0]), v.x, q);
+                        q = fmaf(to_f32(u[1]), v.y, q);
+                        q = fmaf(to_f32(u[2]), v.z, q);
+                        q = fmaf(to_f32(u[3]), v.w, q);
+                    }
+                }
+        }
+#pragma unroll
+        for (int n = kSums / 2, o = 16; n > 0; n >>= 1, o >>= 1)
+#pragma unroll
+            for (int i = 0; i < kSums / 2; ++i)
+                if (i < n) {
+                    const bool up = lane & o;
+                    const float other = __shfl_xor_sync(0xffffffffu, up ? s[i] : s[i + n], o);
+                    s[i] = (up ? s[i + n] : s[i]) + other;
+                }
+#pragma unroll
+        for (int o = (1 << kSkip) >> 1; o > 0; o >>= 1) s[0] += __shfl_xor_sync(0xffffffffu, s[0], o);
+        const int v = g * kFewWords + word;
+        if (v < a.V) {
+            const float y = s[0] * c2, next = fmaxf(m, y), ref = next == -INFINITY ? 0.f : next;
+            l = l * ptx::ex2(m - ref) + ptx::ex2(y - ref);
+            m = next;
+            if (v == label && (lane & ((1 << kSkip) - 1)) == 0) a.chosen[row] = y;
+        }
+    }
+    stats[warp][lane] = make_float2(m, l);
+    __syncthreads();
+    if ((int)threadIdx.x < a.rows) {
+        m = -INFINITY, l = 0.f;
+        for (int u = 0; u < kFewThreads / 32; ++u)
+            for (int k = 0; k < kFewWords; ++k) {
+                const float2 y = stats[u][(threadIdx.x * kFewWords + k) << kSkip];
+                const float next = fmaxf(m, y.x), ref = next == -INFINITY ? 0.f : next;
+                l = l * ptx::ex2(m - ref) + y.y * ptx::ex2(y.x - ref);
+                m = next;
+            }
+        a.part[(long)blockIdx.x * a.cap + threadIdx.x] = make_float2(m, l);
     }
 }
 
 // Parts of a row's statistics, joined: 32 rows a block, its warps (as many as the parts keep busy) taking the parts in turn.
-constexpr int kMergeWarps = 16;
+constexpr int kMergeWarps = 32;
 struct LossMerge {
     const LossInfo *info;
     const float2 *part;
@@ -979,14 +1126,13 @@ __global__ void __launch_bounds__(32 * kMergeWarps) loss_merge_kernel(const Loss
         };
         if (row < rows) {
             int p = warp;
-            for (; p + 3 * warps < a.parts; p += 4 * warps) {
-                float2 x[4];
+            for (; p < a.parts; p += 8 * warps) {
+                float2 x[8];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) x[k] = a.part[(long)(p + k * warps) * a.cap + row];
+                for (int k = 0; k < 8; ++k) x[k] = p + k * warps < a.parts ? a.part[(long)(p + k * warps) * a.cap + row] : make_float2(-INFINITY, 0.f);
 #pragma unroll
-                for (int k = 0; k < 4; ++k) take(x[k]);
+                for (int k = 0; k < 8; ++k) take(x[k]);
             }
-            for (; p < a.parts; p += warps) take(a.part[(long)p * a.cap + row]);
         }
         if (warps > 1) {
             shared[warp][lane] = make_float2(m, l);

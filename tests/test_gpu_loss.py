@@ -97,6 +97,17 @@ def test_small(rows, vocab, width, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("rows", [1, 2, 3, 4, 5, 8, 9])
+@pytest.mark.parametrize("vocab,width,offset", [(1, 8, 0), (5, 1, 0), (4099, 520, 0), (4098, 261, 0), (1001, 264, 1), (40000, 72, 0), (70, 12296, 0)])
+def test_a_few_rows(rows, vocab, width, offset, dtype):
+    """Up to eight rows have a forward of their own, where X fits shared memory."""
+    x, w, labels, _ = problem(rows, vocab, width, dtype, ignored=0.0)
+    view = rows_at(w, width + offset, offset) if offset else w
+    check(x, w, labels, view_w=view, scale=0.7)
+    check(x, w, labels.int(), view_x=rows_at(x, width + 1, 1))
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
 def test_a_weight_for_every_row(dtype):
     x, w, labels, g = problem(700, 900, 136, dtype)
     dloss = torch.rand(700, device="cuda", generator=g) * 3e-3

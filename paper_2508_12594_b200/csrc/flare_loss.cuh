@@ -612,7 +612,7 @@ __device__ __forceinline__ bool loss_sums(LossPipe &q, int deep, int cols, float
         }
         ptx::tc_fence_before();
         __syncwarp();
-        if ((threadIdx.x & 31) == 0) ptx::mbar_arrive_cluster(ptx::in_block(q.acc_empty(q.c & 1), 0));
+        if ((threadIdx.x & 31) == 0) ptx::mbar_arrive_remote(ptx::in_block(q.acc_empty(q.c & 1), 0));
     }
     return true;
 }
@@ -696,7 +696,7 @@ __device__ __forceinline__ bool loss_stats(LossPipe &q, const LossArgs &a, const
             }
         ptx::tc_fence_before();
         __syncwarp();
-        if ((threadIdx.x & 31) == 0) ptx::mbar_arrive_cluster(ptx::in_block(q.acc_empty(q.c & 1), 0));
+        if ((threadIdx.x & 31) == 0) ptx::mbar_arrive_remote(ptx::in_block(q.acc_empty(q.c & 1), 0));
         ++q.c;
     } else {
         float v[128];

@@ -307,6 +307,11 @@ __device__ __forceinline__ uint32_t in_block(uint32_t addr, uint32_t rank) {
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
+// The same where nothing but tensor memory is handed over, whose accesses have their own fences: the release is the block's own, so that it does not wait until what this thread has stored to
+// global memory has arrived.
+__device__ __forceinline__ void mbar_arrive_remote(uint32_t bar) {
+    asm volatile("mbarrier.arrive.release.cta.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
 // kPair = 2: the two blocks of a cluster as one (256 rows, each block's 128 in its own tensor memory; each block holds half of B).
 template <int kPair> __device__ __forceinline__ void tmem_alloc_for(uint32_t slot, uint32_t cols) {
     if (kPair == 1) { tmem_alloc(slot, cols); return; }

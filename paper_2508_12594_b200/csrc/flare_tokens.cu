@@ -30,7 +30,11 @@ DropArgs drop_args(const flare_drop_t *d) {
     if (d == nullptr) return a;
     a.thr = (uint32_t)std::lrint((double)d->p * 65536.0);
     a.keep = a.thr < 65536 ? (float)(65536.0 / (65536 - a.thr)) : 0.f;
-    a.seed = d->seed; a.offset = d->offset; a.step = d->step;
+    for (uint32_t r = 0; r < 10; ++r) {
+        a.k0[r] = (uint32_t)d->seed + r * 0x9E3779B9u;
+        a.k1[r] = (uint32_t)(d->seed >> 32) + r * 0xBB67AE85u;
+    }
+    a.offset = d->offset; a.step = d->step;
     return a;
 }
 // Blocks of a kernel that walks over `items`: a thread an item, or sixteen blocks an SM (up to four of them at a time).
@@ -40,12 +44,20 @@ int check_dropout(const flare_dropout_desc_t *d) {
     if (d == nullptr || d->rows < 0 || d->width <= 0) return FLARE_ERR_INVALID_ARG;
     for (int64_t s : {d->stride_x, d->stride_residual, d->stride_y})
         if (s != 0 && s < d->width) return FLARE_ERR_INVALID_ARG;
+        else if (s > INT32_MAX) return FLARE_ERR_UNSUPPORTED;
     if (!a_type(d->dtype) || (d->residual_dtype != d->dtype && d->residual_dtype != FLARE_DTYPE_F32)) return FLARE_ERR_UNSUPPORTED;
     return d->rows > ((int64_t)1 << 31) - 1 ? FLARE_ERR_UNSUPPORTED : FLARE_OK;
 }
 
 template <typename X, typename R>
 int launch_dropout(const DropoutArgs &a, bool vec, cudaStream_t st) {
+    // one long row: some 4096 elements a block, of at least eight rows, whose bits fit shared memory
+    const bool flat = !vec && a.drop.thr && aligned16(a.x) && aligned16(a.residual) && aligned16(a.y) && a.ld_x == a.C && a.ld_y == a.C && (!a.residual || a.ld_r == a.C);
+    if (flat && a.C >= 8 && a.C <= 32768) {
+        DropoutFlat f{a, std::max(8u, 4096u / a.C / 8 * 8)};
+        FLARE_CUDA(launch_after(dropout_flat_kernel<X, R>, (a.rows + f.tile_rows - 1) / f.tile_rows, kTokenThreads, ((size_t)f.tile_rows * a.C + 31) / 32 * 4, st, f));
+        return FLARE_OK;
+    }
     if (vec) FLARE_CUDA(launch_after(dropout_kernel<X, R, true>, walk_blocks((uint64_t)a.rows * (a.C / 8), kTokenThreads), kTokenThreads, 0, st, a));
     else FLARE_CUDA(launch_after(dropout_kernel<X, R, false>, walk_blocks((uint64_t)a.rows * ((a.C + 255) / 256), kTokenThreads / 32), kTokenThreads, 0, st, a));
     return FLARE_OK;
@@ -62,6 +74,7 @@ int check_embed(const flare_embed_desc_t *d) {
     if (d->token_bits != 32 && d->token_bits != 64) return FLARE_ERR_INVALID_ARG;
     for (int64_t s : {d->stride_table, d->stride_out})
         if (s != 0 && s < d->width) return FLARE_ERR_INVALID_ARG;
+        else if (s > INT32_MAX) return FLARE_ERR_UNSUPPORTED;
     if (!a_type(d->dtype) || !a_type(d->out_dtype)) return FLARE_ERR_UNSUPPORTED;
     if (d->dtype != d->out_dtype && d->dtype != FLARE_DTYPE_F32 && d->out_dtype != FLARE_DTYPE_F32) return FLARE_ERR_UNSUPPORTED;
     return d->rows > ((int64_t)1 << 31) - 1 || d->width > (1 << 20) ? FLARE_ERR_UNSUPPORTED : FLARE_OK;
@@ -69,29 +82,46 @@ int check_embed(const flare_embed_desc_t *d) {
 
 template <typename T, typename O>
 int launch_embed(const EmbedArgs &a, bool vec, cudaStream_t st) {
-    if (vec) FLARE_CUDA(launch_after(embed_kernel<T, O, true>, walk_blocks((uint64_t)a.rows * (a.C / 8), kTokenThreads), kTokenThreads, 0, st, a));
-    else FLARE_CUDA(launch_after(embed_kernel<T, O, false>, walk_blocks((uint64_t)a.rows * ((a.C + 255) / 256), kTokenThreads / 32), kTokenThreads, 0, st, a));
+    // (two groups a thread where there are enough of them to keep every SM busy with half as many threads)
+    const uint64_t groups = (uint64_t)a.rows * (a.C / 8);
+    if (vec && a.C % 16 == 0 && groups >= 2048ull * device_info().sms)
+        FLARE_CUDA(launch_after(embed_kernel<T, O, 2>, walk_blocks(groups / 2, kTokenThreads), kTokenThreads, 0, st, a));
+    else if (vec) FLARE_CUDA(launch_after(embed_kernel<T, O, 1>, walk_blocks(groups, kTokenThreads), kTokenThreads, 0, st, a));
+    else FLARE_CUDA(launch_after(embed_kernel<T, O, 0>, walk_blocks((uint64_t)a.rows * ((a.C + 255) / 256), kTokenThreads / 32), kTokenThreads, 0, st, a));
     return FLARE_OK;
 }
 
-// Rows of a chunk of the backward's sums: such that there are some 1024 threads an SM, 8 to 64.
-int chunk_rows(const flare_embed_desc_t *d, int sms) {
-    const long groups = (d->width + 7) / 8, want = d->rows * groups / (1024L * sms);
-    return (int)std::min(64L, std::max(8L, want / 4 * 4));
+// Two groups a thread where that leaves some 256 threads an SM; 16-bit gradients (float32 ones would not fit the registers).
+bool sum_in_twos(const flare_embed_desc_t *d, int sms) {
+    return d->width % 16 == 0 && d->out_dtype != FLARE_DTYPE_F32 && d->rows * (d->width / 16) >= 8L * 256 * sms;
 }
-struct EmbedLayout { size_t key[2], index[2], part[2], total; long chunks; };
-EmbedLayout embed_layout(const flare_embed_desc_t *d, int sms) {
+// Rows of a chunk of the backward's sums: such that there are some six blocks an SM, 16 to 64.  Positions: whole runs (one row of every batch item) where they are not longer than that, so
+// that none reaches over a chunk's end.
+int chunk_rows(const flare_embed_desc_t *d, int sms) {
+    const long units = sum_in_twos(d, sms) ? d->width / 16 : (d->width + 7) / 8, want = d->rows * units / (6L * kTokenThreads * sms);
+    return (int)std::min(64L, std::max(16L, want / 4 * 4));
+}
+int chunk_rows_of_positions(const flare_embed_desc_t *d, int sms) {
+    const long T = chunk_rows(d, sms), batch = d->positions > 0 ? d->rows / d->positions : 1;
+    return (int)(batch > 64 || batch < 1 ? T : std::max(1L, T / batch) * batch);
+}
+// How the sums' blocks lie over the columns and along the order.
+struct SumShape { uint32_t lanes, tiles, chunks; };
+SumShape sum_shape(const flare_embed_desc_t *d, int sms, bool twos) {
+    const uint32_t units = twos ? (uint32_t)d->width / 16 : ((uint32_t)d->width + 7) / 8, lanes = std::min<uint32_t>(units, kTokenThreads);
+    return SumShape{lanes, (units + kTokenThreads - 1) / kTokenThreads, kTokenThreads / lanes};
+}
+struct EmbedLayout { size_t pairs[2], part[2], total; long spans[2]; };
+EmbedLayout embed_layout(const flare_embed_desc_t *d, int sms, bool twos) {
     EmbedLayout w{};
     size_t off = kHeaderBytes;
+    for (size_t &p : w.pairs) { p = off; off += align_up(sizeof(uint2) * (size_t)d->rows); }
+    const int T[2] = {chunk_rows(d, sms), chunk_rows_of_positions(d, sms)};
     for (int i = 0; i < 2; ++i) {
-        w.key[i] = off; off += align_up(sizeof(uint32_t) * (size_t)d->rows);
-        w.index[i] = off; off += align_up(sizeof(uint32_t) * (size_t)d->rows);
-    }
-    const int T = chunk_rows(d, sms);
-    w.chunks = (d->rows + T - 1) / T;
-    for (int i = 0; i < 2; ++i) {
+        const long rows = (long)T[i] * sum_shape(d, sms, twos).chunks;
+        w.spans[i] = (d->rows + rows - 1) / rows;
         w.part[i] = off;
-        if (i == 0 || d->positions > 0) off += align_up(sizeof(float) * 2 * (size_t)w.chunks * ((d->width + 7) / 8 * 8));
+        if (i == 0 || d->positions > 0) off += align_up(sizeof(float) * 2 * (size_t)w.spans[i] * ((d->width + 7) / 8 * 8));
     }
     w.total = off;
     return w;
@@ -121,42 +151,50 @@ int sort_cluster(size_t smem) {
     }
     return n;
 }
-constexpr size_t kSortSmem = sizeof(uint32_t) * ((33u << kSortBits) + 32);
+constexpr size_t kSortSmem = sizeof(uint32_t) * ((34u << kSortBits) + 64) + sizeof(uint2) * kSortStaged;
 
 int launch_sort(SortArgs s, cudaStream_t st) {
     static std::atomic<uint64_t> opt_in{0};
     if (int rc = ensure_big_smem(embed_sort_kernel, opt_in, (int)kSortSmem)) return rc;
-    int bits = 1;
-    while (bits < 32 && (uint64_t)s.vocab >> bits) ++bits;    // keys 0 .. vocab
-    s.passes = (bits + kSortBits - 1) / kSortBits;
-    s.bits = (bits + s.passes - 1) / s.passes;
     const int n = sort_cluster(kSortSmem);
-    // clusters beside the one that sorts, for what there is to set to zero: 64 KB a block and turn
-    const long others = s.zeros > 0 || s.heads || s.tails ? std::min<long>((long)(s.zeros / (4096L * n)) + 1, device_info().sms / n) : 0;
+    const uint64_t warps = 32ull * n, per_warp = ((s.rows + warps - 1) / warps + 31) / 32 * 32;   // (as the kernel has it)
+    s.staged = 32 * per_warp <= kSortStaged;
     cudaLaunchAttribute attr[2] = {};
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = n; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
     attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)(n * (1 + others)));
-    cfg.blockDim = kSortThreads; cfg.dynamicSmemBytes = sizeof(uint32_t) * ((33u << s.bits) + 32); cfg.stream = st;
+    cfg.gridDim = dim3((unsigned)n);
+    cfg.blockDim = kSortThreads; cfg.dynamicSmemBytes = sizeof(uint32_t) * ((34u << s.bits) + 64) + (s.staged ? sizeof(uint2) * kSortStaged : 0); cfg.stream = st;
     cfg.attrs = attr; cfg.numAttrs = 2;
     FLARE_CUDA(cudaLaunchKernelEx(&cfg, embed_sort_kernel, s));
     return FLARE_OK;
 }
 
+template <typename T>
+int launch_zero(ZeroArgs z, uint32_t first, uint32_t last, cudaStream_t st) {
+    z.first = first; z.last = last;
+    const unsigned blocks = std::max(1u, std::min((last - first + kZeroThreads / 32 - 1) / (kZeroThreads / 32), 8u * device_info().sms));
+    FLARE_CUDA(launch_after(sizeof(T) == 4 ? embed_zero_kernel<uint32_t> : embed_zero_kernel<uint16_t>, blocks, kZeroThreads, 0, st, z));
+    return FLARE_OK;
+}
 // dy's type first
 template <typename O, typename T>
-int launch_sums(const SumArgs &a, bool vec, cudaStream_t st) {
-    const unsigned blocks = a.task[0].blocks + a.task[1].blocks, chunks = a.task[0].chunks + a.task[1].chunks;
-    if (vec) {
-        FLARE_CUDA(launch_after(embed_sum_kernel<O, T, true>, blocks, kTokenThreads, 0, st, a));
-        FLARE_CUDA(launch_after(embed_join_kernel<T, true>, chunks, kTokenThreads, 0, st, a));
-    } else {
-        FLARE_CUDA(launch_after(embed_sum_kernel<O, T, false>, blocks, kTokenThreads, 0, st, a));
-        FLARE_CUDA(launch_after(embed_join_kernel<T, false>, chunks, kTokenThreads, 0, st, a));
-    }
+int launch_sums(const SumArgs &a, const ZeroArgs &z, int width, bool whole_positions, cudaStream_t st) {
+    const unsigned blocks = (a.task[0].spans + a.task[1].spans) * a.tiles;
+    auto joins = [](const SumTask &t) { return (t.spans + kJoinWarps - 1) / kJoinWarps; };
+    const unsigned joined = joins(a.task[0]) + (whole_positions ? 0 : joins(a.task[1]));
+    const uint32_t half = a.beside_zero == 2 ? z.last / 2 : z.last;
+    if (a.beside_zero)
+        if (int rc = launch_zero<T>(z, 0, half, st)) return rc;
+    if (width == 0) FLARE_CUDA(launch_after(embed_sum_kernel<O, T, 0>, blocks, kTokenThreads, 0, st, a));
+    else if (width == 1) FLARE_CUDA(launch_after(embed_sum_kernel<O, T, 1>, blocks, kTokenThreads, 0, st, a));
+    else if constexpr (sizeof(O) == 2) FLARE_CUDA(launch_after(embed_sum_kernel<O, T, 2>, blocks, kTokenThreads, 0, st, a));
+    if (a.beside_zero == 2)
+        if (int rc = launch_zero<T>(z, half, z.last, st)) return rc;
+    if (joined && width) FLARE_CUDA(launch_after(embed_join_kernel<T, true>, joined, kTokenThreads, 0, st, a));
+    else if (joined) FLARE_CUDA(launch_after(embed_join_kernel<T, false>, joined, kTokenThreads, 0, st, a));
     return FLARE_OK;
 }
 
@@ -176,7 +214,7 @@ int flare_dropout_forward(const flare_dropout_desc_t *desc, const flare_drop_t *
     if (int rc = need_device()) return rc;
     if (desc->rows == 0) return FLARE_OK;
     DropoutArgs a{};
-    auto ld = [&](int64_t s) { return (long)(s ? s : desc->width); };
+    auto ld = [&](int64_t s) { return (uint32_t)(s ? s : desc->width); };
     a.x = x; a.residual = residual; a.y = y;
     a.ld_x = ld(desc->stride_x); a.ld_r = ld(desc->stride_residual); a.ld_y = ld(desc->stride_y);
     a.rows = (uint32_t)desc->rows; a.C = (uint32_t)desc->width; a.drop = drop_args(drop);
@@ -194,7 +232,7 @@ int flare_dropout_backward(const flare_dropout_desc_t *desc, const flare_drop_t 
     if (desc->rows == 0) return FLARE_OK;
     DropoutArgs a{};
     a.x = dy; a.y = dx;
-    a.ld_x = desc->stride_y ? desc->stride_y : desc->width; a.ld_y = desc->stride_x ? desc->stride_x : desc->width;
+    a.ld_x = (uint32_t)(desc->stride_y ? desc->stride_y : desc->width); a.ld_y = (uint32_t)(desc->stride_x ? desc->stride_x : desc->width);
     a.rows = (uint32_t)desc->rows; a.C = (uint32_t)desc->width; a.drop = drop_args(drop);
     const bool vec = desc->width % 8 == 0 && rows16(dy, a.ld_x, r) && rows16(dx, a.ld_y, t);
     return FLARE_TWO_TYPES(desc->residual_dtype, desc->dtype, launch_dropout)(a, vec, reinterpret_cast<cudaStream_t>(stream));
@@ -211,15 +249,18 @@ int flare_embed_forward(const flare_embed_desc_t *desc, const flare_drop_t *drop
     if (desc->rows == 0) return FLARE_OK;
     EmbedArgs a{};
     a.tokens = tokens; a.table = table; a.positions = positions; a.y = y;
-    a.ld_t = desc->stride_table ? desc->stride_table : desc->width; a.ld_y = desc->stride_out ? desc->stride_out : desc->width;
+    a.ld_t = (uint32_t)(desc->stride_table ? desc->stride_table : desc->width); a.ld_y = (uint32_t)(desc->stride_out ? desc->stride_out : desc->width);
     a.rows = (uint32_t)desc->rows; a.C = (uint32_t)desc->width; a.L = (uint32_t)std::max<int64_t>(1, desc->positions);
-    a.vocab = desc->vocab; a.scale = desc->scale; a.drop = drop_args(drop); a.wide = desc->token_bits == 64;
+    a.vocab = (uint32_t)desc->vocab; a.scale = desc->scale; a.drop = drop_args(drop); a.wide = desc->token_bits == 64;
     const bool vec = desc->width % 8 == 0 && rows16(table, a.ld_t, t) && rows16(y, a.ld_y, o) && aligned16(positions);
     return FLARE_TWO_TYPES(desc->dtype, desc->out_dtype, launch_embed)(a, vec, reinterpret_cast<cudaStream_t>(stream));
 }
 
 size_t flare_embed_workspace_bytes(const flare_embed_desc_t *desc) {
-    return check_embed(desc) == FLARE_OK ? embed_layout(desc, device_info().sms).total : 0;
+    if (check_embed(desc) != FLARE_OK) return 0;
+    // (whether two groups can be taken at a time is known with the tensors' addresses)
+    const int sms = device_info().sms;
+    return std::max(embed_layout(desc, sms, false).total, embed_layout(desc, sms, sum_in_twos(desc, sms)).total);
 }
 
 int flare_embed_backward(const flare_embed_desc_t *desc, const flare_drop_t *drop, const void *tokens, const void *dy, void *dtable, void *dpositions, int32_t accumulate,
@@ -231,8 +272,10 @@ int flare_embed_backward(const flare_embed_desc_t *desc, const flare_drop_t *dro
     if (!natural(tokens, desc->token_bits / 8) || !natural(dy, o) || !natural(dtable, t) || !natural(dpositions, t)) return FLARE_ERR_INVALID_ARG;
     if (int rc = need_device()) return rc;
     const int sms = device_info().sms;
-    const EmbedLayout w = embed_layout(desc, sms);
-    if (workspace_bytes < w.total) return FLARE_ERR_WORKSPACE_TOO_SMALL;
+    if (workspace_bytes < flare_embed_workspace_bytes(desc)) return FLARE_ERR_WORKSPACE_TOO_SMALL;
+    const uint32_t ld_dy = (uint32_t)(desc->stride_out ? desc->stride_out : desc->width);
+    const bool vec = desc->width % 8 == 0 && rows16(dy, ld_dy, o) && aligned16(dtable) && aligned16(dpositions), twos = vec && sum_in_twos(desc, sms);
+    const EmbedLayout w = embed_layout(desc, sms, twos);
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     const size_t table_bytes = (size_t)desc->vocab * desc->width * t;
     if (desc->rows == 0) {
@@ -243,46 +286,44 @@ int flare_embed_backward(const flare_embed_desc_t *desc, const flare_drop_t *dro
     }
     char *ws = static_cast<char *>(workspace);
     SumArgs a{};
-    a.dy = dy; a.ld_dy = desc->stride_out ? desc->stride_out : desc->width;
-    a.C = (uint32_t)desc->width; a.columns = (a.C + 7) / 8 * 8; a.T = (uint32_t)chunk_rows(desc, sms); a.drop = drop_args(drop);
-    const uint64_t threads = (uint64_t)w.chunks * (a.columns / 8), blocks = (threads + kTokenThreads - 1) / kTokenThreads;
-    if (2 * blocks > ((1ull << 31) - 1)) return FLARE_ERR_UNSUPPORTED;
+    ZeroArgs z{};
+    const SumShape shape = sum_shape(desc, sms, twos);
+    a.dy = dy; a.ld_dy = ld_dy;
+    a.C = (uint32_t)desc->width; a.columns = (a.C + 7) / 8 * 8; a.drop = drop_args(drop);
+    a.lanes = shape.lanes; a.tiles = shape.tiles; a.chunks = shape.chunks;
+    if ((uint64_t)(w.spans[0] + w.spans[1]) * a.tiles > ((1ull << 31) - 1)) return FLARE_ERR_UNSUPPORTED;
+    const long batch = desc->positions > 0 ? desc->rows / desc->positions : 1;
+    const bool whole_positions = chunk_rows_of_positions(desc, sms) % batch == 0;      // no position's rows reach over a chunk's end
     if (dtable) {
         SortArgs s{};
-        s.tokens = tokens; s.wide = desc->token_bits == 64; s.rows = (uint32_t)desc->rows; s.vocab = desc->vocab;
-        for (int i = 0; i < 2; ++i) {
-            s.key[i] = reinterpret_cast<uint32_t *>(ws + w.key[i]);
-            s.index[i] = reinterpret_cast<uint32_t *>(ws + w.index[i]);
-        }
-        if (!accumulate) {
-            uint8_t *p = static_cast<uint8_t *>(dtable);
-            s.heads = (uint32_t)std::min<size_t>(table_bytes, -reinterpret_cast<uintptr_t>(p) & 15u);
-            s.head = p;
-            s.zero = reinterpret_cast<uint4 *>(p + s.heads);
-            s.zeros = (table_bytes - s.heads) / 16;
-            s.tail = p + s.heads + s.zeros * 16;
-            s.tails = (uint32_t)(table_bytes - s.heads - s.zeros * 16);
-        }
-        if (int rc = launch_sort(s, st)) return rc;
+        s.tokens = tokens; s.wide = desc->token_bits == 64; s.rows = (uint32_t)desc->rows; s.vocab = (uint32_t)desc->vocab;
+        for (int i = 0; i < 2; ++i) s.pairs[i] = reinterpret_cast<uint2 *>(ws + w.pairs[i]);
         int bits = 1;
-        while (bits < 32 && (uint64_t)desc->vocab >> bits) ++bits;
-        const int in = sorted_in((bits + kSortBits - 1) / kSortBits);
+        while (bits < 32 && (uint64_t)desc->vocab >> bits) ++bits;            // keys 0 .. vocab
+        s.passes = (bits + kSortBits - 1) / kSortBits;
+        s.bits = (bits + s.passes - 1) / s.passes;
+        if (int rc = launch_sort(s, st)) return rc;
+        if (!accumulate) {
+            const uint32_t groups = (s.vocab + 31) / 32;
+            z = ZeroArgs{s.pairs[sorted_in(s.passes)], s.rows, s.vocab, 0, groups, (uint64_t)desc->width * t, static_cast<uint8_t *>(dtable)};
+            // (16 MB and more: some 5 us of writing)
+            a.beside_zero = table_bytes >= (16u << 20) ? 2 : 1;
+        }
         SumTask &k = a.task[0];
-        k.key = s.key[in]; k.index = s.index[in];
-        k.items = s.rows; k.most = (uint32_t)desc->vocab; k.out = dtable; k.ld_out = desc->width; k.scale = desc->scale; k.add = accumulate != 0;
+        k.pairs = s.pairs[sorted_in(s.passes)];
+        k.items = s.rows; k.most = (uint32_t)desc->vocab; k.out = dtable; k.scale = desc->scale * a.drop.keep; k.add = accumulate != 0;
         k.part = reinterpret_cast<float *>(ws + w.part[0]);
-        k.chunks = (uint32_t)w.chunks; k.blocks = (uint32_t)blocks;
+        k.T = (uint32_t)chunk_rows(desc, sms); k.spans = (uint32_t)w.spans[0];
     }
     if (dpositions) {
         SumTask &k = a.task[1];
         k.items = (uint32_t)desc->rows; k.L = (uint32_t)desc->positions; k.batch = k.items / k.L; k.most = ~0u;
-        k.out = dpositions; k.ld_out = desc->width; k.scale = 1.f; k.add = accumulate != 0;
+        k.out = dpositions; k.scale = a.drop.keep; k.add = accumulate != 0;
         k.part = reinterpret_cast<float *>(ws + w.part[1]);
-        k.chunks = (uint32_t)w.chunks; k.blocks = (uint32_t)blocks;
+        k.T = (uint32_t)chunk_rows_of_positions(desc, sms); k.spans = (uint32_t)w.spans[1];
     }
     if (!dtable && !dpositions) return FLARE_OK;
-    const bool vec = desc->width % 8 == 0 && rows16(dy, a.ld_dy, o) && aligned16(dtable) && aligned16(dpositions);
-    return FLARE_TWO_TYPES(desc->out_dtype, desc->dtype, launch_sums)(a, vec, st);
+    return FLARE_TWO_TYPES(desc->out_dtype, desc->dtype, launch_sums)(a, z, vec ? (twos ? 2 : 1) : 0, whole_positions, st);
 }
 
 }  // extern "C"

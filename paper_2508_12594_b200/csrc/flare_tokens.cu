@@ -95,21 +95,23 @@ int launch_embed(const EmbedArgs &a, bool vec, cudaStream_t st) {
 bool sum_in_twos(const flare_embed_desc_t *d, int sms) {
     return d->width % 16 == 0 && d->out_dtype != FLARE_DTYPE_F32 && d->rows * (d->width / 16) >= 8L * 256 * sms;
 }
-// Rows of a chunk of the backward's sums: such that there are some six blocks an SM, 16 to 64.  Positions: whole runs (one row of every batch item) where they are not longer than that, so
+// How the sums' blocks lie over the columns and along the order.
+struct SumShape { uint32_t threads, lanes, tiles, chunks; };
+SumShape sum_shape(const flare_embed_desc_t *d, bool twos) {
+    const uint32_t units = twos ? (uint32_t)d->width / 16 : ((uint32_t)d->width + 7) / 8, threads = units <= 32 ? 64 : kSumThreads;
+    const uint32_t tiles = (units + threads - 1) / threads, lanes = (units + tiles - 1) / tiles;
+    return SumShape{threads, lanes, tiles, threads / lanes};
+}
+// Rows of a chunk of the backward's sums: such that there are some 1536 threads an SM, 16 to 64.  Positions: whole runs (one row of every batch item) where they are not longer than that, so
 // that none reaches over a chunk's end.
 int chunk_rows(const flare_embed_desc_t *d, int sms) {
-    const long units = sum_in_twos(d, sms) ? d->width / 16 : (d->width + 7) / 8, want = d->rows * units / (6L * kTokenThreads * sms);
+    const SumShape s = sum_shape(d, sum_in_twos(d, sms));
+    const long want = d->rows * s.lanes * s.tiles / (1536L * sms);
     return (int)std::min(64L, std::max(16L, want / 4 * 4));
 }
 int chunk_rows_of_positions(const flare_embed_desc_t *d, int sms) {
     const long T = chunk_rows(d, sms), batch = d->positions > 0 ? d->rows / d->positions : 1;
     return (int)(batch > 64 || batch < 1 ? T : std::max(1L, T / batch) * batch);
-}
-// How the sums' blocks lie over the columns and along the order.
-struct SumShape { uint32_t lanes, tiles, chunks; };
-SumShape sum_shape(const flare_embed_desc_t *d, int sms, bool twos) {
-    const uint32_t units = twos ? (uint32_t)d->width / 16 : ((uint32_t)d->width + 7) / 8, lanes = std::min<uint32_t>(units, kTokenThreads);
-    return SumShape{lanes, (units + kTokenThreads - 1) / kTokenThreads, kTokenThreads / lanes};
 }
 struct EmbedLayout { size_t pairs[2], part[2], total; long spans[2]; };
 EmbedLayout embed_layout(const flare_embed_desc_t *d, int sms, bool twos) {
@@ -118,7 +120,7 @@ EmbedLayout embed_layout(const flare_embed_desc_t *d, int sms, bool twos) {
     for (size_t &p : w.pairs) { p = off; off += align_up(sizeof(uint2) * (size_t)d->rows); }
     const int T[2] = {chunk_rows(d, sms), chunk_rows_of_positions(d, sms)};
     for (int i = 0; i < 2; ++i) {
-        const long rows = (long)T[i] * sum_shape(d, sms, twos).chunks;
+        const long rows = (long)T[i] * sum_shape(d, twos).chunks;
         w.spans[i] = (d->rows + rows - 1) / rows;
         w.part[i] = off;
         if (i == 0 || d->positions > 0) off += align_up(sizeof(float) * 2 * (size_t)w.spans[i] * ((d->width + 7) / 8 * 8));
@@ -188,9 +190,9 @@ int launch_sums(const SumArgs &a, const ZeroArgs &z, int width, bool whole_posit
     const uint32_t half = a.beside_zero == 2 ? z.last / 2 : z.last;
     if (a.beside_zero)
         if (int rc = launch_zero<T>(z, 0, half, st)) return rc;
-    if (width == 0) FLARE_CUDA(launch_after(embed_sum_kernel<O, T, 0>, blocks, kTokenThreads, 0, st, a));
-    else if (width == 1) FLARE_CUDA(launch_after(embed_sum_kernel<O, T, 1>, blocks, kTokenThreads, 0, st, a));
-    else if constexpr (sizeof(O) == 2) FLARE_CUDA(launch_after(embed_sum_kernel<O, T, 2>, blocks, kTokenThreads, 0, st, a));
+    if (width == 0) FLARE_CUDA(launch_after(embed_sum_kernel<O, T, 0>, blocks, a.threads, sum_smem(a.threads, 0 == 2 ? 2 : 1), st, a));
+    else if (width == 1) FLARE_CUDA(launch_after(embed_sum_kernel<O, T, 1>, blocks, a.threads, sum_smem(a.threads, 1 == 2 ? 2 : 1), st, a));
+    else if constexpr (sizeof(O) == 2) FLARE_CUDA(launch_after(embed_sum_kernel<O, T, 2>, blocks, a.threads, sum_smem(a.threads, 2 == 2 ? 2 : 1), st, a));
     if (a.beside_zero == 2)
         if (int rc = launch_zero<T>(z, half, z.last, st)) return rc;
     if (joined && width) FLARE_CUDA(launch_after(embed_join_kernel<T, true>, joined, kTokenThreads, 0, st, a));
@@ -287,10 +289,10 @@ int flare_embed_backward(const flare_embed_desc_t *desc, const flare_drop_t *dro
     char *ws = static_cast<char *>(workspace);
     SumArgs a{};
     ZeroArgs z{};
-    const SumShape shape = sum_shape(desc, sms, twos);
+    const SumShape shape = sum_shape(desc, twos);
     a.dy = dy; a.ld_dy = ld_dy;
     a.C = (uint32_t)desc->width; a.columns = (a.C + 7) / 8 * 8; a.drop = drop_args(drop);
-    a.lanes = shape.lanes; a.tiles = shape.tiles; a.chunks = shape.chunks;
+    a.threads = shape.threads; a.lanes = shape.lanes; a.tiles = shape.tiles; a.chunks = shape.chunks;
     if ((uint64_t)(w.spans[0] + w.spans[1]) * a.tiles > ((1ull << 31) - 1)) return FLARE_ERR_UNSUPPORTED;
     const long batch = desc->positions > 0 ? desc->rows / desc->positions : 1;
     const bool whole_positions = chunk_rows_of_positions(desc, sms) % batch == 0;      // no position's rows reach over a chunk's end

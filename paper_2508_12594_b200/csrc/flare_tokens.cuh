@@ -614,7 +614,7 @@ struct SumArgs {
     const void *dy;
     uint32_t ld_dy, C, columns;                               // columns: C up to whole groups of eight
     int beside_zero;                                          // launches with an embed_zero_kernel just before them: 1: the sums, 2: the joins too
-    uint32_t lanes, tiles, chunks;                            // threads side by side over a row's units of columns, blocks side by side, chunks of a block one after the other
+    uint32_t threads, lanes, tiles, chunks;                   // threads of a block; side by side over a row's units of columns, blocks side by side, chunks of a block one after the other
     DropArgs drop;
 };
 __device__ __forceinline__ uint32_t key_at(const SumTask &t, uint32_t i) { return t.pairs ? t.pairs[i].x : i / t.batch; }
@@ -675,14 +675,17 @@ __device__ __forceinline__ void add8(float (&v)[8], const float *from) {
     v[4] += y.x; v[5] += y.y; v[6] += y.z; v[7] += y.w;
 }
 enum { kRunOpen = 1, kRunGoesOn = 2, kRunThrough = 4 };       // a chunk's first run began before it; its last one goes on behind it; the two are the same and all of it
+// Blocks of 64 threads where a row takes few of them, of up to 256 where it takes more.  (32 x 4096 rows of 128, both gradients: 39 us with 256, too few of which were at work towards the end, 30 with 64.)
+constexpr int kSumThreads = 256;
+__host__ __device__ constexpr size_t sum_smem(uint32_t threads, int width) { return threads * (size_t)(2 * 32 * width + 8); }
 // kWidth: groups of eight columns next to each other that a thread adds up (two share what there is to know of a row: 167 instructions a group and row became 120), 0: one, off 16-byte boundaries.
 template <typename O, typename T, int kWidth>
-__global__ void __launch_bounds__(kTokenThreads, sizeof(O) == 4 || kWidth == 2 ? 2 : 3) embed_sum_kernel(const SumArgs a) {
+__global__ void __launch_bounds__(kSumThreads, sizeof(O) == 4 || kWidth == 2 ? 2 : 3) embed_sum_kernel(const SumArgs a) {
     constexpr int kW = kWidth == 2 ? 2 : 1;
     constexpr bool kVec = kWidth > 0;
-    __shared__ __align__(16) float first_sum[kTokenThreads][8 * kW], last_sum[kTokenThreads][8 * kW];
-    __shared__ uint32_t first_run[kTokenThreads];             // by chunk
-    __shared__ uint8_t flags[kTokenThreads];
+    extern __shared__ __align__(16) float first_sum[];        // [threads][8 kW], and the same of last runs; by chunk: key of the first run, flags
+    float *last_sum = first_sum + blockDim.x * 8 * kW;
+    uint32_t *first_run = reinterpret_cast<uint32_t *>(last_sum + blockDim.x * 8 * kW), *flags = first_run + blockDim.x;
     if (!a.beside_zero) {
         ptx::grid_launch();
         ptx::grid_wait();
@@ -690,7 +693,7 @@ __global__ void __launch_bounds__(kTokenThreads, sizeof(O) == 4 || kWidth == 2 ?
     const bool second = blockIdx.x < a.task[1].spans * a.tiles;           // (positions first: their chunks are the longer ones)
     const SumTask &t = a.task[second];
     const uint32_t at = blockIdx.x - (second ? 0 : a.task[1].spans * a.tiles), span = at / a.tiles, k = threadIdx.x / a.lanes;
-    const uint32_t group = ((at - span * a.tiles) * kTokenThreads + threadIdx.x - k * a.lanes) * kW, groups = a.columns / 8;
+    const uint32_t group = ((at - span * a.tiles) * a.lanes + threadIdx.x - k * a.lanes) * kW, groups = a.columns / 8;
     const uint64_t i0_64 = ((uint64_t)span * a.chunks + k) * t.T;
     const uint32_t i0 = (uint32_t)min(i0_64, (uint64_t)t.items), i1 = (uint32_t)min(i0_64 + t.T, (uint64_t)t.items);
     const bool active = k < a.chunks && group < groups;
@@ -717,7 +720,7 @@ __global__ void __launch_bounds__(kTokenThreads, sizeof(O) == 4 || kWidth == 2 ?
         float sum[kW][8] = {};
         bool one = true;                                      // still in the first run
         auto leave = [&]() {                                  // a run that ends in the chunk
-            if (one && open) put(first_sum[threadIdx.x], sum);
+            if (one && open) put(first_sum + threadIdx.x * 8 * kW, sum);
             else if (run < t.most) store(run, sum);
         };
         for (uint32_t i = i0; i < i1; i += kBatch) {
@@ -732,6 +735,25 @@ __global__ void __launch_bounds__(kTokenThreads, sizeof(O) == 4 || kWidth == 2 ?
             }
 #pragma unroll
             for (int j = 0; j < kBatch; ++j) next[j] = walk.next(i1);
+            auto add_row = [&](int j) {
+#pragma unroll
+                for (int w = 0; w < kW; ++w) {
+                    float v[8];
+                    floats8(e[j][w], v);
+                    if (a.drop.thr) add_kept8(a.drop, key, group + w, now[j].y, v, sum[w]);
+                    else
+#pragma unroll
+                        for (int c = 0; c < 8; ++c) sum[w][c] += v[c];
+                }
+            };
+            bool same = run < t.most;
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j) same = same && now[j].x == run;
+            if (same) {                                       // all of the run: no branches between the rows' generators
+#pragma unroll
+                for (int j = 0; j < kBatch; ++j) add_row(j);
+                continue;
+            }
 #pragma unroll
             for (int j = 0; j < kBatch; ++j) {
                 if (i + j >= i1) break;
@@ -744,22 +766,13 @@ __global__ void __launch_bounds__(kTokenThreads, sizeof(O) == 4 || kWidth == 2 ?
 #pragma unroll
                         for (int c = 0; c < 8; ++c) sum[w][c] = 0.f;
                 }
-                if (run >= t.most) continue;
-#pragma unroll
-                for (int w = 0; w < kW; ++w) {
-                    float v[8];
-                    floats8(e[j][w], v);
-                    if (a.drop.thr) add_kept8(a.drop, key, group + w, now[j].y, v, sum[w]);
-                    else
-#pragma unroll
-                        for (int c = 0; c < 8; ++c) sum[w][c] += v[c];
-                }
+                if (run < t.most) add_row(j);
             }
         }
         const bool goes_on = i1 < t.items && beyond == run;
         if (!goes_on) leave();
-        else if (one && open) put(first_sum[threadIdx.x], sum);
-        else put(last_sum[threadIdx.x], sum);
+        else if (one && open) put(first_sum + threadIdx.x * 8 * kW, sum);
+        else put(last_sum + threadIdx.x * 8 * kW, sum);
         if (threadIdx.x == k * a.lanes) {
             first_run[k] = head;
             flags[k] = (open ? kRunOpen : 0) | (goes_on ? kRunGoesOn : 0) | (open && goes_on && one ? kRunThrough : 0);
@@ -791,7 +804,7 @@ __global__ void __launch_bounds__(kTokenThreads, sizeof(O) == 4 || kWidth == 2 ?
                 clear();
                 has = before = true;
             }
-            add(first_sum[here]);
+            add(first_sum + here * 8 * kW);
             if (!(f & kRunThrough)) {
                 if (before) put(part, sum);
                 else if (first_run[c] < t.most) store(first_run[c], sum);
@@ -800,7 +813,7 @@ __global__ void __launch_bounds__(kTokenThreads, sizeof(O) == 4 || kWidth == 2 ?
         }
         if ((f & kRunGoesOn) && !(f & kRunThrough)) {
             clear();
-            add(last_sum[here]);
+            add(last_sum + here * 8 * kW);
             has = true;
             before = false;
         }

@@ -30,6 +30,7 @@ int check_loss(const flare_loss_desc_t *d) {
 // G of a piece of the vocabulary takes this much scratch (or 256 words of it where that is more).
 constexpr size_t kPieceBytes = 256u << 20;
 struct LossPlan {
+    int to;                      // what is multiplied: kAsIs, kToHalf, kToHalves
     int planes, Cp, chunks, x_blocks, w_blocks, pairs;
     long cap;
     int width;                   // of a tile of X W^T
@@ -42,9 +43,12 @@ int tile_width(long row_tiles, long words, int pairs) {
     const long wide = row_tiles * ((words + 255) / 256), narrow = row_tiles * ((words + 127) / 128);
     return 0.6 * (double)((narrow + pairs - 1) / pairs) < (double)((wide + pairs - 1) / pairs) ? 128 : 256;
 }
-LossPlan loss_plan(const flare_loss_desc_t *d, int sms) {
+LossPlan loss_plan(const flare_loss_desc_t *d, int sms, bool backward) {
     LossPlan p{};
     const bool f32 = d->dtype == FLARE_DTYPE_F32;
+    // bfloat16's G would be off by 2^-9 (its rms 1.7e-3, as much again as the rounding of the results): where W is small enough for another pass over it not to count, it, X and G are float16.
+    const bool bf16_small = d->dtype == FLARE_DTYPE_BF16 && backward && (long)d->vocab * d->width <= (4L << 20);
+    p.to = f32 ? kToHalves : bf16_small ? kToHalf : kAsIs;
     p.planes = f32 ? 2 : 1;
     // rows of packed X and W: whole 16 bytes, of wide ones whole lines (TMA takes 128-byte pieces of them)
     p.Cp = d->width > 256 ? (d->width + 63) / 64 * 64 : (d->width + 7) / 8 * 8;
@@ -52,7 +56,7 @@ LossPlan loss_plan(const flare_loss_desc_t *d, int sms) {
     p.pairs = std::max(1, sms / 2);
     p.cap = std::max(1L, (long)(d->rows + 255) / 256) * 256;
     p.width = tile_width(p.cap / 256, d->vocab, p.pairs);
-    if (f32) {
+    if (p.to != kAsIs) {
         auto blocks = [&](long rows) { return (int)std::max(1L, std::min(4L * sms, rows * d->width / 8192)); };
         p.x_blocks = blocks(d->rows);
         p.w_blocks = blocks(d->vocab);
@@ -92,11 +96,11 @@ LossLayout loss_layout(const flare_loss_desc_t *d, const LossPlan &p, bool backw
     take(w.label, sizeof(int) * (size_t)p.cap);
     if (!backward) {
         const long tiles = (d->vocab + p.width - 1) / p.width;
-        take(w.part, sizeof(float2) * std::max<size_t>(2 * (size_t)tiles, few_rows(d) ? few_blocks(d, 2 * p.pairs) : 0) * p.cap);
+        take(w.part, sizeof(float2) * std::max<size_t>((size_t)tiles, few_rows(d) ? few_blocks(d, 2 * p.pairs) : 0) * p.cap);
         take(w.chosen, sizeof(float) * (size_t)p.cap);
         take(w.gave_up, sizeof(uint32_t) * 2 * (size_t)p.pairs);
     } else {
-        take(w.pd, d->dtype == FLARE_DTYPE_BF16 ? 0 : row * p.cap);
+        take(w.pd, d->dtype == FLARE_DTYPE_BF16 && p.to == kAsIs ? 0 : row * p.cap);
         take(w.lse2, sizeof(float) * (size_t)p.cap);
         take(w.coef, sizeof(float) * (size_t)p.cap);
         take(w.g, sizeof(uint16_t) * (size_t)p.planes * p.cap * p.Vp);
@@ -151,8 +155,13 @@ int launch_merge(const LossMerge &m, long rows, cudaStream_t st) {
 }
 
 template <typename T>
+int launch_scan(const LossScan &s, cudaStream_t st) {
+    FLARE_CUDA(launch_after(loss_scan_kernel<T>, (unsigned)(s.chunks + s.x_blocks + s.w_blocks), kScanThreads, 0, st, s));
+    return FLARE_OK;
+}
+template <typename T, int kTo>
 int launch_pack(const LossPack &k, int blocks, cudaStream_t st) {
-    FLARE_CUDA(launch_after(loss_pack_kernel<T>, (unsigned)blocks, kPackThreads, 0, st, k));
+    FLARE_CUDA(launch_after(loss_pack_kernel<T, kTo>, (unsigned)blocks, kPackThreads, 0, st, k));
     return FLARE_OK;
 }
 
@@ -180,23 +189,24 @@ int check_loss_call(const flare_loss_desc_t *d, const void *x, const void *w, co
     if (!workspace || !aligned16(workspace) || !w || (d->rows > 0 && (!x || !labels))) return FLARE_ERR_INVALID_ARG;
     if (!natural(x, t) || !natural(w, t) || !natural(labels, d->label_bits / 8)) return FLARE_ERR_INVALID_ARG;
     if (int rc = need_device()) return rc;
-    return workspace_bytes < loss_layout(d, loss_plan(d, device_info().sms), backward).total ? FLARE_ERR_WORKSPACE_TOO_SMALL : FLARE_OK;
+    return workspace_bytes < loss_layout(d, loss_plan(d, device_info().sms, backward), backward).total ? FLARE_ERR_WORKSPACE_TOO_SMALL : FLARE_OK;
 }
 
 // Scan and packing, and the maps of X and W; what only the backward has is in k already.
 int prepare_loss(const flare_loss_desc_t *d, const LossPlan &p, const LossLayout &l, char *ws, const void *x, const void *w, const void *labels, LossPack k, LossMaps *maps,
                  LossArgs *a, cudaStream_t st) {
-    const bool f32 = d->dtype == FLARE_DTYPE_F32, bf16 = d->dtype == FLARE_DTYPE_BF16;
+    const bool f32 = d->dtype == FLARE_DTYPE_F32, bf16 = d->dtype == FLARE_DTYPE_BF16 && p.to == kAsIs;
     const long ld_x = d->stride_x ? d->stride_x : d->width, ld_w = d->stride_w ? d->stride_w : d->width;
-    const bool own_w = f32 || !aligned16(w) || ld_w % 8 != 0;
+    const bool own_w = p.to != kAsIs || !aligned16(w) || ld_w % 8 != 0;
     LossScan s{};
     s.labels = labels; s.wide = d->label_bits == 64; s.rows = d->rows; s.V = d->vocab; s.C = d->width;
-    s.chunks = p.chunks; s.x_blocks = p.x_blocks; s.w_blocks = p.w_blocks; s.dloss = bf16 ? nullptr : k.dloss;
+    s.chunks = p.chunks; s.x_blocks = p.x_blocks; s.w_blocks = p.w_blocks; s.dloss = k.dloss;
     s.rank = reinterpret_cast<int *>(ws + l.rank); s.chunk = reinterpret_cast<LossChunk *>(ws + l.chunk);
-    s.x = static_cast<const float *>(x); s.w = static_cast<const float *>(w); s.ld_x = ld_x; s.ld_w = ld_w;
+    s.x = x; s.w = w; s.ld_x = ld_x; s.ld_w = ld_w;
     s.largest = reinterpret_cast<float *>(ws + l.largest);
     s.status = reinterpret_cast<uint32_t *>(ws);
-    FLARE_CUDA(launch_after(loss_scan_kernel, (unsigned)(p.chunks + p.x_blocks + p.w_blocks), kScanThreads, 0, st, s));
+    int rc;
+    if ((rc = f32 ? launch_scan<float>(s, st) : d->dtype == FLARE_DTYPE_BF16 ? launch_scan<__nv_bfloat16>(s, st) : launch_scan<__half>(s, st)) != FLARE_OK) return rc;
     k.labels = labels; k.x = x; k.w = w; k.wide = s.wide; k.rows = d->rows; k.cap = p.cap; k.ld_x = ld_x; k.ld_w = ld_w;
     k.w_rows = own_w ? d->vocab : 0; k.C = d->width; k.Cp = p.Cp; k.V = d->vocab; k.chunks = p.chunks; k.x_blocks = p.x_blocks; k.w_blocks = p.w_blocks;
     k.pack_blocks = (int)((d->rows + kPackRows - 1) / kPackRows);
@@ -205,8 +215,11 @@ int prepare_loss(const flare_loss_desc_t *d, const LossPlan &p, const LossLayout
     k.px = reinterpret_cast<uint16_t *>(ws + l.px); k.pw = reinterpret_cast<uint16_t *>(ws + l.pw);
     k.index = reinterpret_cast<int *>(ws + l.index); k.label = reinterpret_cast<int *>(ws + l.label);
     const int blocks = k.pack_blocks + (int)std::min<long>((k.w_rows * (p.Cp / 8) + 4 * kPackThreads - 1) / (4 * kPackThreads), 16L * device_info().sms);
-    if (int rc = f32 ? launch_pack<float>(k, blocks, st) : bf16 ? launch_pack<__nv_bfloat16>(k, blocks, st) : launch_pack<__half>(k, blocks, st)) return rc;
-    int rc;
+    if ((rc = f32                             ? launch_pack<float, kToHalves>(k, blocks, st)
+              : d->dtype == FLARE_DTYPE_F16   ? launch_pack<__half, kAsIs>(k, blocks, st)
+              : p.to == kToHalf               ? launch_pack<__nv_bfloat16, kToHalf>(k, blocks, st)
+                                              : launch_pack<__nv_bfloat16, kAsIs>(k, blocks, st)) != FLARE_OK)
+        return rc;
     if ((rc = make_plane_map(&maps->x, k.px, bf16, p.Cp, p.cap, p.planes, p.Cp, 64)) != FLARE_OK) return rc;
     if ((rc = own_w ? make_plane_map(&maps->w, k.pw, bf16, p.Cp, d->vocab, p.planes, p.Cp, 64)
                     : make_plane_map(&maps->w, w, bf16, d->width, d->vocab, 1, ld_w, 64)) != FLARE_OK)
@@ -225,7 +238,7 @@ extern "C" {
 
 size_t flare_loss_workspace_bytes(const flare_loss_desc_t *desc, int32_t backward) {
     if (check_loss(desc) != FLARE_OK) return 0;
-    return loss_layout(desc, loss_plan(desc, device_info().sms), backward != 0).total;
+    return loss_layout(desc, loss_plan(desc, device_info().sms, backward != 0), backward != 0).total;
 }
 
 int flare_loss_forward(const flare_loss_desc_t *desc, const void *x, const void *w, const void *labels, float *loss, float *lse, void *workspace, size_t workspace_bytes,
@@ -238,7 +251,7 @@ int flare_loss_forward(const flare_loss_desc_t *desc, const void *x, const void 
         FLARE_CUDA(cudaMemsetAsync(workspace, 0, kHeaderBytes, st));
         return FLARE_OK;
     }
-    const LossPlan p = loss_plan(desc, device_info().sms);
+    const LossPlan p = loss_plan(desc, device_info().sms, false);
     const LossLayout l = loss_layout(desc, p, false);
     char *ws = static_cast<char *>(workspace);
     if (const int R = few_rows(desc)) {
@@ -277,7 +290,7 @@ int flare_loss_forward(const flare_loss_desc_t *desc, const void *x, const void 
     const int pairs = (int)std::min<long>(p.pairs, p.cap / 256 * a.tiles_v);
     if (int rc = p.planes == 2 ? launch_loss<kLossStats, 2, float>(maps, a, pairs, st) : launch_loss<kLossStats, 1, float>(maps, a, pairs, st)) return rc;
     LossMerge m{};
-    m.info = a.info; m.part = a.part; m.chosen = a.chosen; m.index = a.index; m.cap = p.cap; m.parts = 2 * a.tiles_v; m.loss = loss; m.lse = lse;
+    m.info = a.info; m.part = a.part; m.chosen = a.chosen; m.index = a.index; m.cap = p.cap; m.parts = a.tiles_v; m.loss = loss; m.lse = lse;
     m.labels = a.labels; m.wide = a.wide; m.V = a.V; m.direct = a.direct; m.gave_up = a.gave_up; m.status = a.status; m.blocks = 2 * pairs;
     return launch_merge(m, desc->rows, st);
 }
@@ -295,9 +308,9 @@ int flare_loss_backward(const flare_loss_desc_t *desc, const void *x, const void
         if (dw) FLARE_CUDA(cudaMemset2DAsync(dw, ld_dw * t, 0, desc->width * t, desc->vocab, st));
         return FLARE_OK;
     }
-    const LossPlan p = loss_plan(desc, device_info().sms);
+    const LossPlan p = loss_plan(desc, device_info().sms, true);
     const LossLayout l = loss_layout(desc, p, true);
-    const bool bf16 = desc->dtype == FLARE_DTYPE_BF16, f32 = desc->dtype == FLARE_DTYPE_F32;
+    const bool f32 = desc->dtype == FLARE_DTYPE_F32, bf16 = desc->dtype == FLARE_DTYPE_BF16 && p.to == kAsIs;   // (bf16: what is multiplied)
     char *ws = static_cast<char *>(workspace);
     LossPack k{};
     k.lse_in = lse; k.dloss = dloss; k.mult = desc->scale * desc->dloss_scale;
@@ -319,11 +332,13 @@ int flare_loss_backward(const flare_loss_desc_t *desc, const void *x, const void
     a.dw = dw; a.dx = dx; a.ld_dw = ld_dw; a.ld_dx = ld_dx;
     auto fours = [&](const void *q, long ld) { return desc->width % 4 == 0 && ld % 4 == 0 && reinterpret_cast<uintptr_t>(q) % (4 * t) == 0; };
     a.dw_fours = fours(dw, ld_dw); a.dx_fours = fours(dx, ld_dx);
-    a.dw_factor = k.mult / 32768.f;
+    // bfloat16's G: q where one dloss is that of all rows (a label's q is next to -1, which is no rounding), else times it; float16's: q times 2^15, dloss goes into X
+    a.g_factor = !bf16 ? 32768.f : dloss ? 0.f : 1.f;
+    a.dw_factor = a.g_factor != 0.f ? k.mult / a.g_factor : 0.f;
     a.acc = reinterpret_cast<float *>(ws + l.acc); a.slots = reinterpret_cast<float *>(ws + l.slots);
     auto weights = f32 ? launch_loss<kLossWeights, 2, float> : launch_loss<kLossWeights, 1, float>;
-    auto grads = f32 ? launch_loss<kLossGrads, 2, float> : bf16 ? launch_loss<kLossGrads, 1, __nv_bfloat16> : launch_loss<kLossGrads, 1, __half>;
-    auto *join = f32 ? loss_join_kernel<float> : bf16 ? loss_join_kernel<__nv_bfloat16> : loss_join_kernel<__half>;
+    auto grads = f32 ? launch_loss<kLossGrads, 2, float> : desc->dtype == FLARE_DTYPE_BF16 ? launch_loss<kLossGrads, 1, __nv_bfloat16> : launch_loss<kLossGrads, 1, __half>;
+    auto *join = f32 ? loss_join_kernel<float> : desc->dtype == FLARE_DTYPE_BF16 ? loss_join_kernel<__nv_bfloat16> : loss_join_kernel<__half>;
     // of tiles that several pairs can have shared: fewer than a round of either gradient
     const long warps = 2L * (p.pairs - 1) * 8 * (p.grad_width / 32);
     for (int i = 0; i < p.pieces; ++i) {

@@ -58,11 +58,11 @@ struct LossScan {
     const void *labels;
     int wide;
     long rows;
-    int V, C, chunks, x_blocks, w_blocks;     // blocks beyond the chunks' look for the largest |x| of labelled rows and |w| (float32)
+    int V, C, chunks, x_blocks, w_blocks;     // blocks beyond the chunks' look for the largest |x| of labelled rows and |w| (what is multiplied in float16 though it is not)
     const float *dloss;                       // or null
     int *rank;                                // [rows]: among the labelled rows of its chunk, or -1
     LossChunk *chunk;
-    const float *x, *w;
+    const void *x, *w;
     long ld_x, ld_w;
     float *largest;                           // [x_blocks + w_blocks]
     uint32_t *status;
@@ -78,6 +78,21 @@ __device__ __forceinline__ float block_max(float v, float *shared) {
     __syncthreads();
     return v;
 }
+// Eight columns as they lie in memory; `left` of them are, the others are zeros (vec: all or none).
+template <typename T> struct LossEight { uint4 q[sizeof(T) / 2]; };
+template <typename T> __device__ __forceinline__ void eight_of(const T *p, bool vec, int left, LossEight<T> &e) {
+    if (vec) {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) e.q[i] = left > 0 ? reinterpret_cast<const uint4 *>(p)[i] : make_uint4(0, 0, 0, 0);
+    } else {
+        T *t = reinterpret_cast<T *>(e.q);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < left) t[i] = p[i];
+            else from_f32(t[i], 0.f);
+    }
+}
+template <typename T>
 __global__ void __launch_bounds__(kScanThreads) loss_scan_kernel(const LossScan a) {
     __shared__ float shared[32];
     __shared__ uint32_t before[33];
@@ -88,37 +103,32 @@ __global__ void __launch_bounds__(kScanThreads) loss_scan_kernel(const LossScan 
     if ((int)blockIdx.x >= a.chunks) {
         const int b = blockIdx.x - a.chunks;
         const bool of_x = b < a.x_blocks;
-        const float *m = of_x ? a.x : a.w;
+        const T *m = static_cast<const T *>(of_x ? a.x : a.w);
         const long rows = of_x ? a.rows : a.V, ld = of_x ? a.ld_x : a.ld_w;
-        const bool fours = a.C % 4 == 0 && ld % 4 == 0 && (reinterpret_cast<uintptr_t>(m) & 15) == 0;
-        const uint32_t groups = (uint32_t)(a.C + 3) / 4;
+        const bool vec = a.C % 8 == 0 && ld * (long)sizeof(T) % 16 == 0 && (reinterpret_cast<uintptr_t>(m) & 15) == 0;
         const uint64_t blocks = of_x ? a.x_blocks : a.w_blocks, first = (uint64_t)(of_x ? b : b - a.x_blocks) * kScanThreads + threadIdx.x;
-        // (four groups of four columns are asked for before the first is looked at)
-        LossWalk walk(first, blocks * kScanThreads, groups);
+        // (a few groups of eight columns are asked for before the first is looked at)
+        constexpr int kBatch = sizeof(T) == 4 ? 2 : 4;
+        LossWalk walk(first, blocks * kScanThreads, (uint32_t)(a.C + 7) / 8);
         float most = 0.f;
         while (walk.row < rows) {
-            float4 v[4];
+            LossEight<T> e[kBatch];
+            bool use[kBatch];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-                const float *p = m + walk.row * ld + 4 * walk.group;
-                bool use = walk.row < rows;
-                if (use && of_x) {
+            for (int k = 0; k < kBatch; ++k) {
+                use[k] = walk.row < rows;
+                if (use[k] && of_x) {
                     const int64_t label = label_at(a.labels, a.wide, walk.row);
-                    use = label >= 0 && label < a.V;
+                    use[k] = label >= 0 && label < a.V;
                 }
-                if (use && fours) v[k] = *reinterpret_cast<const float4 *>(p);
-                else if (use) {
-                    const int n = a.C - (int)(4 * walk.group);
-                    v[k].x = p[0];
-                    if (n > 1) v[k].y = p[1];
-                    if (n > 2) v[k].z = p[2];
-                    if (n > 3) v[k].w = p[3];
-                }
+                if (use[k]) eight_of(m + walk.row * ld + 8 * walk.group, vec, a.C - (int)(8 * walk.group), e[k]);
                 walk.next();
             }
 #pragma unroll
-            for (int k = 0; k < 4; ++k) most = fmaxf(fmaxf(most, fmaxf(finite_abs(v[k].x), finite_abs(v[k].y))), fmaxf(finite_abs(v[k].z), finite_abs(v[k].w)));
+            for (int k = 0; k < kBatch; ++k)
+                if (use[k])
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) most = fmaxf(most, finite_abs(to_f32(reinterpret_cast<const T *>(e[k].q)[i])));
         }
         most = block_max(most, shared);
         if (threadIdx.x == 0) a.largest[b] = most;
@@ -190,49 +200,36 @@ __device__ __forceinline__ float half_scale(float most) {
     frexpf(most, &e);                         // most < 2^e
     return ldexpf(1.f, min(max(15 - e, -60), 60));
 }
-// Eight columns as they lie in memory; `left` of them are, the others are zeros (vec: all or none).
-template <typename T> struct LossEight { uint4 q[sizeof(T) / 2]; };
-template <typename T> __device__ __forceinline__ void eight_of(const T *p, bool vec, int left, LossEight<T> &e) {
-    if (vec) {
-#pragma unroll
-        for (int i = 0; i < (int)sizeof(T) / 2; ++i) e.q[i] = left > 0 ? reinterpret_cast<const uint4 *>(p)[i] : make_uint4(0, 0, 0, 0);
-    } else {
-        T *t = reinterpret_cast<T *>(e.q);
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (i < left) t[i] = p[i];
-            else from_f32(t[i], 0.f);
-    }
-}
-// Times f, into their planes.  T: float32 into two float16 halves, else the type itself; as they are where not `scaled`.
-template <typename T>
+// What the products multiply: the type as it is, or float16 times a power of two (one of bfloat16's values, two halves of float32's).
+enum { kAsIs = 0, kToHalf = 1, kToHalves = 2 };
+// Eight columns times f, into their planes; as they are where not `scaled`.
+template <typename T, int kTo>
 __device__ __forceinline__ void pack_eight(const LossEight<T> &e, float f, bool scaled, uint16_t *out, long plane) {
     const T *t = reinterpret_cast<const T *>(e.q);
     __align__(16) uint16_t h[8], l[8];
-    if constexpr (sizeof(T) == 2) {
+    if constexpr (kTo == kAsIs) {
         if (!scaled) {
             *reinterpret_cast<uint4 *>(out) = e.q[0];
             return;
         }
+    }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            T v;
-            from_f32(v, to_f32(t[i]) * f);
-            h[i] = *reinterpret_cast<const uint16_t *>(&v);
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float v = t[i] * f;
+    for (int i = 0; i < 8; ++i) {
+        const float v = to_f32(t[i]) * f;
+        if constexpr (kTo == kAsIs) {
+            T u;
+            from_f32(u, v);
+            h[i] = *reinterpret_cast<const uint16_t *>(&u);
+        } else {
             const __half hi = __float2half_rn(v);
             h[i] = __half_as_ushort(hi);
-            l[i] = __half_as_ushort(__float2half_rn(v - __half2float(hi)));
+            if constexpr (kTo == kToHalves) l[i] = __half_as_ushort(__float2half_rn(v - __half2float(hi)));
         }
-        *reinterpret_cast<uint4 *>(out + plane) = *reinterpret_cast<const uint4 *>(l);
     }
+    if constexpr (kTo == kToHalves) *reinterpret_cast<uint4 *>(out + plane) = *reinterpret_cast<const uint4 *>(l);
     *reinterpret_cast<uint4 *>(out) = *reinterpret_cast<const uint4 *>(h);
 }
-template <typename T>
+template <typename T, int kTo>
 __global__ void __launch_bounds__(kPackThreads) loss_pack_kernel(const LossPack a) {
     __shared__ float shared[32];
     __shared__ uint32_t sums[2][kPackThreads / 32];
@@ -241,11 +238,11 @@ __global__ void __launch_bounds__(kPackThreads) loss_pack_kernel(const LossPack 
     ptx::grid_launch();
     ptx::grid_wait();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    constexpr bool kHalves = sizeof(T) == 4;
+    constexpr bool kScaled = kTo != kAsIs;
     constexpr int kBatch = 4;                                 // groups of eight columns that are asked for before the first is stored
     const uint32_t groups = (uint32_t)a.Cp / 8;
     float sx = 1.f, sw = 1.f;
-    if constexpr (kHalves) {
+    if constexpr (kScaled) {
         float mx = 0.f, mw = 0.f;
         for (int i = threadIdx.x; i < a.x_blocks; i += kPackThreads) mx = fmaxf(mx, a.largest[i]);
         for (int i = threadIdx.x; i < a.w_blocks; i += kPackThreads) mw = fmaxf(mw, a.largest[a.x_blocks + i]);
@@ -267,7 +264,7 @@ __global__ void __launch_bounds__(kPackThreads) loss_pack_kernel(const LossPack 
             }
 #pragma unroll
             for (int k = 0; k < kBatch; ++k)
-                if (at[k] >= 0) pack_eight(e[k], sw, kHalves, a.pw + at[k], a.w_rows * a.Cp);
+                if (at[k] >= 0) pack_eight<T, kTo>(e[k], sw, kScaled, a.pw + at[k], a.w_rows * a.Cp);
         }
         return;
     }
@@ -334,8 +331,8 @@ __global__ void __launch_bounds__(kPackThreads) loss_pack_kernel(const LossPack 
             if (row[k] >= rows) break;
             const long to = to_row[row[k]];
             if (to >= 0) {
-                pack_eight(e[k], sx, kHalves, a.px + to * a.Cp + col[k], plane);
-                if (a.pd) pack_eight(e[k], sx * d_row[row[k]], true, a.pd + to * a.Cp + col[k], plane);
+                pack_eight<T, kTo>(e[k], sx, kScaled, a.px + to * a.Cp + col[k], plane);
+                if (a.pd) pack_eight<T, kTo>(e[k], sx * d_row[row[k]], true, a.pd + to * a.Cp + col[k], plane);
             } else if (dx) {
                 T *p = dx + (n0 + row[k]) * a.ld_dx + col[k];
                 if (col[k] >= a.C) continue;
@@ -355,7 +352,7 @@ __global__ void __launch_bounds__(kPackThreads) loss_pack_kernel(const LossPack 
     if (a.loss == nullptr) {
         const long end = min(a.cap, ((long)max(total, 1u) + 63) / 64 * 64);
         for (long r = total + (long)blockIdx.x * (kPackThreads / 32) + warp; r < end; r += (long)a.pack_blocks * (kPackThreads / 32))
-            for (int h = 0; h < (kHalves ? 2 : 1); ++h)
+            for (int h = 0; h < (kTo == kToHalves ? 2 : 1); ++h)
                 for (int c = lane * 8; c < a.Cp; c += 256) {
                     *reinterpret_cast<uint4 *>(a.px + h * plane + r * a.Cp + c) = make_uint4(0, 0, 0, 0);
                     if (a.pd) *reinterpret_cast<uint4 *>(a.pd + h * plane + r * a.Cp + c) = make_uint4(0, 0, 0, 0);
@@ -365,23 +362,23 @@ __global__ void __launch_bounds__(kPackThreads) loss_pack_kernel(const LossPack 
 
 // ---------------------------------------------------------------- the products
 enum { kLossStats = 0, kLossWeights = 1, kLossGrads = 2 };
-constexpr int kLossThreads = 384;                             // warp 0 loads, warp 1 issues, warps 4 to 11 take the sums out of tensor memory
+constexpr int kLossThreads = 640, kLossResults = 16;          // warp 0 loads, warp 1 issues, warps 4 to 19 take the sums out of tensor memory
 constexpr uint32_t kLossHalfTile = 128 * 128;                 // bytes: 128 rows (or 64 rows of two blocks of columns) of 64 elements
-constexpr uint32_t kLossPiece = 4096;                         // a warp's piece of a result on its way out
+constexpr uint32_t kLossPiece = 2048;                         // a warp's piece of a result on its way out: 32 rows of 64 bytes
 template <int kPlanes> struct LossShape {
     static constexpr int kStages = kPlanes == 1 ? 6 : 3;
     static constexpr uint32_t kStage = 2 * kPlanes * kLossHalfTile;        // A (high, low), B (high, low)
-    // 64-deep steps whose sums stay in tensor memory, where every addition truncates: of halves 4 (12 x 4 additions), of 16-bit factors, whose results
-    // are rounded to 2^-9 or 2^-12, 64
-    static constexpr int kChunk = kPlanes == 1 ? 64 : 4;
 };
-constexpr size_t kLossSmem = 1024 + 6 * 2 * kLossHalfTile + 8 * kLossPiece + 256;
+// 64-deep steps whose sums stay in tensor memory, where every addition truncates: of halves 4 (12 x 4 additions); of the forward's 16-bit factors 8 (a loss over 4096 columns is off by 2e-6 with all of
+// them there); of the backward's, whose results are rounded to 2^-9 or 2^-12, 64.
+template <int kKind, int kPlanes> constexpr int kLossDeep = kPlanes == 2 ? 4 : kKind == kLossStats ? 8 : 64;
+constexpr size_t kLossSmem = 1024 + 6 * 2 * kLossHalfTile + kLossResults * kLossPiece + 256;
 
 struct LossMaps { CUtensorMap x, d, w, g; };                  // in boxes of 64 x 64
 struct LossArgs {
     const LossInfo *info;
     uint32_t *status;
-    int C, V, bf16;
+    int C, V, bf16;              // bf16: the factors are bfloat16 (else float16)
     long cap;                    // rows up to whole tiles
     float scale;
     int v0, words;               // the piece of the vocabulary: from v0 on
@@ -396,11 +393,12 @@ struct LossArgs {
         return l >= 0 && l < V ? (int)l : -1;
     }
     uint32_t *gave_up;           // direct: a word for every pair's block, joined behind
-    // forward: maximum and sum of 2 tiles_v parts of a row (in units of ln 2), the label's logit
+    // forward: maximum and sum of tiles_v parts of a row (in units of ln 2), the label's logit
     float2 *part;
     float *chosen;
     // backward
     const float *lse2, *coef;
+    float g_factor;              // of q in G; 0: dloss scale, a row's own
     uint16_t *g;                 // planes [cap][ld_g]
     long ld_g;
     int grad_width, tiles_c;     // columns of a gradient's tile, tiles across
@@ -408,7 +406,7 @@ struct LossArgs {
     void *dw, *dx;
     long ld_dw, ld_dx;
     int dw_fours, dx_fours;      // rows can be written four columns at a time
-    float dw_factor;             // 16-bit scale of G, scale and dloss_scale (times dmax / x_scale)
+    float dw_factor;             // scale dloss_scale / g_factor (times dmax / x_scale)
     float *acc;                  // dX over the pieces before, by tile: [2 blocks][grad_width columns][128 rows]
     float *slots;                // sums of parts of tiles, likewise, two per pair
 };
@@ -563,7 +561,7 @@ __device__ __forceinline__ void loss_issue(LossPipe &q, const LossArgs &a, int r
             const uint32_t acc = q.tmem + (q.c & 1) * 256;
             if (q.c >= 2 && !ptx::mbar_wait(q.acc_empty(q.c & 1), (q.c / 2 - 1) & 1, q.abort_flag, 112)) return;
             ptx::tc_fence_after();
-            for (int k1 = min(kb + Shape::kChunk, u.kb1), first = 1; kb < k1; ++kb, ++q.n, first = 0) {
+            for (int k1 = min(kb + kLossDeep<kKind, kPlanes>, u.kb1), first = 1; kb < k1; ++kb, ++q.n, first = 0) {
                 const uint32_t s = q.n % Shape::kStages;
                 if (!ptx::mbar_wait(q.full(s), (q.n / Shape::kStages) & 1, q.abort_flag, 113)) return;
                 ptx::tc_fence_after();
@@ -585,29 +583,29 @@ __device__ __forceinline__ void loss_issue(LossPipe &q, const LossArgs &a, int r
     }
 }
 
-// The result warps' parts.  A unit's sums into registers, a row a thread and half of the tile's columns (`cols`): false if a wait gave up.
-template <int kPlanes>
-__device__ __forceinline__ bool loss_sums(LossPipe &q, int deep, int cols, float (&v)[128]) {
-    const int warp = ptx::warp_index(), quad = warp & 3, half = (warp - 4) >> 2;
-    const uint32_t acc = q.tmem + ((uint32_t)(quad * 32) << 16) + half * cols;
-    for (int kb = 0; kb < deep; kb += LossShape<kPlanes>::kChunk, ++q.c) {
+// The result warps' parts.  A unit's sums into registers, a row a thread and a quarter of the tile's columns (`cols`, 64 or 32): false if a wait gave up.
+template <int kKind, int kPlanes>
+__device__ __forceinline__ bool loss_sums(LossPipe &q, int deep, int cols, float (&v)[64]) {
+    const int warp = ptx::warp_index(), quad = warp & 3, part = (warp - 4) >> 2;
+    const uint32_t acc = q.tmem + ((uint32_t)(quad * 32) << 16) + part * cols;
+    for (int kb = 0; kb < deep; kb += kLossDeep<kKind, kPlanes>, ++q.c) {
         const bool ok = ptx::mbar_wait(q.acc_full(q.c & 1), (q.c / 2) & 1, q.abort_flag, 114);
         if (!__all_sync(0xffffffffu, ok)) return false;
         ptx::tc_fence_after();
         if (kb == 0) {
 #pragma unroll
-            for (int k = 0; k < 128; k += 32)
+            for (int k = 0; k < 64; k += 32)
                 if (k < cols) ptx::tmem_ld32(acc + (q.c & 1) * 256 + k, reinterpret_cast<uint32_t (&)[32]>(v[k]));
             ptx::tmem_wait_ld();
         } else {
 #pragma unroll
-            for (int k = 0; k < 128; k += 32) {
+            for (int k = 0; k < 64; k += 16) {
                 if (k >= cols) break;
-                uint32_t u[32];
-                ptx::tmem_ld32(acc + (q.c & 1) * 256 + k, u);
+                uint32_t u[16];
+                ptx::tmem_ld16(acc + (q.c & 1) * 256 + k, u);
                 ptx::tmem_wait_ld();
 #pragma unroll
-                for (int e = 0; e < 32; ++e) v[k + e] += __uint_as_float(u[e]);
+                for (int e = 0; e < 16; ++e) v[k + e] += __uint_as_float(u[e]);
             }
         }
         ptx::tc_fence_before();
@@ -615,6 +613,12 @@ __device__ __forceinline__ bool loss_sums(LossPipe &q, int deep, int cols, float
         if ((threadIdx.x & 31) == 0) ptx::mbar_arrive_remote(ptx::in_block(q.acc_empty(q.c & 1), 0));
     }
     return true;
+}
+// All result warps at one barrier: whether all of them have their sums, the same in all of their threads.  (A warp whose wait gave up comes here too.)
+__device__ __forceinline__ bool loss_agree(bool ok) {
+    uint32_t all;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbar.red.and.pred q, 1, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(all) : "r"((uint32_t)ok), "n"(32 * kLossResults) : "memory");
+    return all != 0;
 }
 
 // What a result warp needs of its lanes' rows, asked for before it waits for their sums.
@@ -631,10 +635,9 @@ __device__ __forceinline__ LossRow loss_row(const LossArgs &a, int rows, int row
     return r;
 }
 
-// Forward: maximum and sum of exponentials of 64 columns of a row more (`left` of them are words), in units of ln 2.
+// Forward: maximum and sum of exponentials of a row's `left` (up to 64) columns, in units of ln 2.
 struct LossStat { float m, l; };
-__device__ __forceinline__ void loss_stat(LossStat &s, float (&v)[64], int left, float c2) {
-    if (left <= 0) return;
+__device__ __forceinline__ LossStat loss_stat(float (&v)[64], int left, float c2) {
     if (left < 64) {
 #pragma unroll
         for (int e = 0; e < 64; ++e) v[e] = e < left ? v[e] : -INFINITY;
@@ -644,100 +647,92 @@ __device__ __forceinline__ void loss_stat(LossStat &s, float (&v)[64], int left,
     for (int e = 4; e < 64; e += 4)
 #pragma unroll
         for (int i = 0; i < 4; ++i) mx[i] = fmaxf(mx[i], v[e + i]);
-    const float next = fmaxf(s.m, fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * c2), ref = next == -INFINITY ? 0.f : next;
-    float l[4] = {s.l * ptx::ex2(s.m - ref), 0.f, 0.f, 0.f};
+    const float m = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * c2, ref = m == -INFINITY ? 0.f : m;
+    float l[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int e = 0; e < 64; ++e) l[e & 3] += ptx::ex2(fmaf(v[e], c2, -ref));
-    s.l = (l[0] + l[1]) + (l[2] + l[3]);
-    s.m = next;
+    return LossStat{m, (l[0] + l[1]) + (l[2] + l[3])};
 }
-// The value at place `at` (0 to 63), by halves.
+__device__ __forceinline__ LossStat loss_both(LossStat a, LossStat b) {
+    const float m = fmaxf(a.m, b.m), ref = m == -INFINITY ? 0.f : m;
+    return LossStat{m, a.l * ptx::ex2(a.m - ref) + b.l * ptx::ex2(b.m - ref)};
+}
+// The value at place `at` (0 to 63), by halves of sixteen at a time.
 __device__ __forceinline__ float loss_pick(const float (&v)[64], int at) {
-    float t[32];
+    float r = 0.f;
 #pragma unroll
-    for (int e = 0; e < 32; ++e) t[e] = at & 32 ? v[e + 32] : v[e];
+    for (int k = 0; k < 64; k += 16) {
+        float t[8];
 #pragma unroll
-    for (int n = 16; n > 0; n >>= 1)
+        for (int e = 0; e < 8; ++e) t[e] = at & 8 ? v[k + e + 8] : v[k + e];
 #pragma unroll
-        for (int e = 0; e < 16; ++e)
-            if (e < n) t[e] = at & n ? t[e + n] : t[e];
-    return t[0];
-}
-// A tile's part: the sums straight from tensor memory, 64 columns at a time, where one set of them is all there is; else (kPlanes = 2, widths beyond 4096) added up in
-// registers first.
-template <int kPlanes>
-__device__ __forceinline__ bool loss_stats(LossPipe &q, const LossArgs &a, const LossUnit &u, const LossRow &r, float c2, int rows, int row, int col0, int cols, int half) {
-    const bool any = row - (int)(threadIdx.x & 31) < rows;               // of the warp's rows
-    const int at = r.label - col0;                                       // the label's column here (no label: below zero)
-    LossStat s{-INFINITY, 0.f};
-    auto take = [&](float (&v)[64], int k) {
-        if (__any_sync(0xffffffffu, at >= k && at < k + 64)) {
-            const float c = loss_pick(v, at - k);
-            if (at >= k && at < k + 64) a.chosen[row] = c * c2;
-        }
-        loss_stat(s, v, a.V - col0 - k, c2);
-    };
-    if (kPlanes == 1 && u.kb1 <= LossShape<kPlanes>::kChunk) {
-        const int warp = ptx::warp_index(), quad = warp & 3;
-        const uint32_t acc = q.tmem + ((uint32_t)(quad * 32) << 16) + half * cols + (q.c & 1) * 256;
-        const bool ok = ptx::mbar_wait(q.acc_full(q.c & 1), (q.c / 2) & 1, q.abort_flag, 114);
-        if (!__all_sync(0xffffffffu, ok)) return false;
-        ptx::tc_fence_after();
-        if (any)
-            for (int k = 0; k < cols; k += 64) {
-                uint32_t t[2][32];
-                ptx::tmem_ld32(acc + k, t[0]);
-                ptx::tmem_ld32(acc + k + 32, t[1]);
-                ptx::tmem_wait_ld();
-                float v[64];
+        for (int n = 4; n > 0; n >>= 1)
 #pragma unroll
-                for (int e = 0; e < 64; ++e) v[e] = __uint_as_float(t[e >> 5][e & 31]);
-                take(v, k);
-            }
-        ptx::tc_fence_before();
-        __syncwarp();
-        if ((threadIdx.x & 31) == 0) ptx::mbar_arrive_remote(ptx::in_block(q.acc_empty(q.c & 1), 0));
-        ++q.c;
-    } else {
-        float v[128];
-        if (!loss_sums<kPlanes>(q, u.kb1, cols, v)) return false;
-        if (any) {
-            take(reinterpret_cast<float (&)[64]>(v[0]), 0);
-            if (cols > 64) take(reinterpret_cast<float (&)[64]>(v[64]), 64);
-        }
+            for (int e = 0; e < 4; ++e)
+                if (e < n) t[e] = at & n ? t[e + n] : t[e];
+        r = at >> 4 == k / 16 ? t[0] : r;
     }
-    if (row < rows) a.part[((long)u.j * 2 + half) * a.cap + row] = make_float2(s.m, s.l);
+    return r;
+}
+// A tile's part of a row: by four warps, a quarter of the columns each, joined in shared memory (two places in turn: a place is written again behind the next tile's barrier).
+template <int kPlanes>
+__device__ __forceinline__ bool loss_stats(LossPipe &q, const LossArgs &a, const LossUnit &u, const LossRow &r, float c2, int rows, int row, int cols, float2 *joint) {
+    const int warp = ptx::warp_index(), part = (warp - 4) >> 2, local = (warp & 3) * 32 + (threadIdx.x & 31), col0 = u.j * a.width + part * cols;
+    const int at = r.label - col0;                                       // the label's column here (no label: below zero)
+    float v[64];
+    const bool ok = loss_sums<kLossStats, kPlanes>(q, u.kb1, cols, v);
+    LossStat s{-INFINITY, 0.f};
+    if (ok && row - local % 32 < rows) {                                 // (some of the warp's rows are rows)
+        const bool mine = at >= 0 && at < cols;
+        if (__any_sync(0xffffffffu, mine)) {
+            const float c = loss_pick(v, at);
+            if (mine) a.chosen[row] = c * c2;
+        }
+        const int left = min(cols, a.V - col0);
+        if (left > 0) s = loss_stat(v, left, c2);
+    }
+    if (part > 0) joint[(part - 1) * 128 + local] = make_float2(s.m, s.l);
+    if (!loss_agree(ok)) return false;
+    if (part == 0 && row < rows) {
+#pragma unroll
+        for (int p = 0; p < 3; ++p) {
+            const float2 x = joint[p * 128 + local];
+            s = loss_both(s, LossStat{x.x, x.y});
+        }
+        a.part[(long)u.j * a.cap + row] = make_float2(s.m, s.l);
+    }
     return true;
 }
 
-// Backward: q of 32 rows and 64 columns at a time, in 16 bits (halves), to G by way of shared memory, so that eight lanes write 128 bytes of a row.
+// Where 16 bytes of a row of 64 lie in a piece: neither rows a lane nor four lanes a row meet a bank conflict.
+__device__ __forceinline__ uint32_t piece_at(int row, int chunk) { return row * 64 + ((chunk ^ (row >> 1 & 3)) << 4); }
+// Backward: q of 32 rows and 32 columns at a time, in 16 bits (halves), to G by way of shared memory, so that four lanes write 64 bytes of a row.
 template <int kPlanes>
-__device__ __forceinline__ void loss_weights(const LossPipe &q, const LossArgs &a, const LossRow &r, float c2, int rows, int row, int local0, int cols, float (&v)[128]) {
+__device__ __forceinline__ void loss_weights(uint32_t piece, const LossArgs &a, const LossRow &r, float c2, int rows, int row, int local0, int cols, float (&v)[64]) {
     const int lane = threadIdx.x & 31, col0 = a.v0 + local0;
-    const uint32_t piece = q.pieces0 + (ptx::warp_index() - 4) * kLossPiece;
     const bool in = row < rows;
     const int at = r.label - col0;                                       // (no label: below zero)
-    const float lse2 = r.lse2, f = !in ? 0.f : a.bf16 ? r.coef : 32768.f;
+    const float lse2 = r.lse2, f = a.g_factor != 0.f ? a.g_factor : r.coef;
     const int words = in ? a.V - col0 : 0;
 #pragma unroll
-    for (int k = 0; k < 128; k += 64) {
+    for (int k = 0; k < 64; k += 32) {
         if (k >= cols) break;
 #pragma unroll
-        for (int e = 0; e < 64; ++e) {
+        for (int e = 0; e < 32; ++e) {
             float p = ptx::ex2(fmaf(v[k + e], c2, -lse2));
             if (at == k + e) p -= 1.f;
             v[k + e] = p * f;
         }
-        if (words - k < 64) {                                            // beyond the vocabulary, or rows that are none: zeros whatever the sums hold
+        if (words - k < 32) {                                            // beyond the vocabulary, or rows that are none: zeros whatever the sums hold
 #pragma unroll
-            for (int e = 0; e < 64; ++e)
+            for (int e = 0; e < 32; ++e)
                 if (e >= words - k) v[k + e] = 0.f;
         }
 #pragma unroll
         for (int h = 0; h < kPlanes; ++h) {
             __syncwarp();
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
+            for (int e = 0; e < 4; ++e) {
                 uint32_t w[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
@@ -753,36 +748,33 @@ __device__ __forceinline__ void loss_weights(const LossPipe &q, const LossArgs &
                         }
                     }
                 }
-                ptx::sts128(piece + lane * 128 + ((e ^ (lane & 7)) << 4), w);
+                ptx::sts128(piece + piece_at(lane, e), w);
             }
             __syncwarp();
-            uint16_t *out = a.g + ((long)h * a.cap + (row - lane) + (lane >> 3)) * a.ld_g + local0 + k + (lane & 7) * 8;
+            uint16_t *out = a.g + ((long)h * a.cap + (row - lane) + (lane >> 2)) * a.ld_g + local0 + k + (lane & 3) * 8;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int t = 4 * e + (lane >> 3);
-                *reinterpret_cast<float4 *>(out + (long)4 * e * a.ld_g) = ptx::lds128(piece + t * 128 + (((lane & 7) ^ (t & 7)) << 4));
-            }
+            for (int e = 0; e < 4; ++e) *reinterpret_cast<float4 *>(out + (long)8 * e * a.ld_g) = ptx::lds128(piece + piece_at(8 * e + (lane >> 2), lane & 3));
         }
     }
 }
 
-// 32 rows (a row a lane, to go to row `to` of the output; -1: nowhere) of 32 columns from c0 on, times f, by way of shared memory, so that eight lanes write a row's 32 columns.
+// 32 rows (a row a lane, to go to row `to` of the output; -1: nowhere) of 16 columns from c0 on, times f, by way of shared memory, so that four lanes write a row's 16 columns.
 template <typename E>
 __device__ __forceinline__ void loss_out(uint32_t piece, E *out, long ld, int fours, int to, int c0, int C, float f, const float *v) {
     const int lane = threadIdx.x & 31;
     __syncwarp();
 #pragma unroll
-    for (int g = 0; g < 8; ++g) {
+    for (int g = 0; g < 4; ++g) {
         const uint32_t r[4] = {__float_as_uint(v[4 * g] * f), __float_as_uint(v[4 * g + 1] * f), __float_as_uint(v[4 * g + 2] * f), __float_as_uint(v[4 * g + 3] * f)};
-        ptx::sts128(piece + lane * 128 + ((g ^ (lane & 7)) << 4), r);
+        ptx::sts128(piece + piece_at(lane, g), r);
     }
     __syncwarp();
-    const int g = lane & 7, c = c0 + 4 * g;
+    const int c = c0 + 4 * (lane & 3);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-        const int r = 4 * k + (lane >> 3);
+    for (int k = 0; k < 4; ++k) {
+        const int r = 8 * k + (lane >> 2);
         const int t = __shfl_sync(0xffffffffu, to, r);
-        const float4 x = ptx::lds128(piece + r * 128 + ((g ^ (r & 7)) << 4));
+        const float4 x = ptx::lds128(piece + piece_at(r, lane & 3));
         if (t < 0 || c >= C) continue;
         E *p = out + (long)t * ld + c;
         __align__(16) E e[4];
@@ -796,7 +788,6 @@ __device__ __forceinline__ void loss_out(uint32_t piece, E *out, long ld, int fo
                 if (c + i < C) p[i] = e[i];
         }
     }
-    __syncwarp();
 }
 // 32 columns of a gradient's tile that are complete, tile-local from col on.
 template <typename E>
@@ -804,8 +795,9 @@ __device__ __forceinline__ void loss_gradient(uint32_t piece, const LossArgs &a,
     const int lane = threadIdx.x & 31, local = i * 256 + block * 128 + quad * 32 + lane, c0 = j * a.grad_width + col;
     if (c0 >= a.C) return;
     if (!dx) {
-        loss_out<E>(piece, static_cast<E *>(a.dw), a.ld_dw, a.dw_fours, local < a.words ? a.v0 + local : -1, c0, a.C,
-                    a.bf16 ? 1.f : a.dw_factor * info.dmax / info.x_scale, v);
+        const float f = a.g_factor != 0.f ? a.dw_factor * info.dmax / info.x_scale : 1.f;
+#pragma unroll
+        for (int k = 0; k < 32; k += 16) loss_out<E>(piece, static_cast<E *>(a.dw), a.ld_dw, a.dw_fours, local < a.words ? a.v0 + local : -1, c0 + k, a.C, f, v + k);
         return;
     }
     if (!a.first || !a.last) {
@@ -820,7 +812,9 @@ __device__ __forceinline__ void loss_gradient(uint32_t piece, const LossArgs &a,
             return;
         }
     }
-    loss_out<E>(piece, static_cast<E *>(a.dx), a.ld_dx, a.dx_fours, r.index, c0, a.C, a.bf16 ? 1.f : r.coef / (32768.f * info.w_scale), v);
+    const float f = a.g_factor != 0.f ? r.coef / (a.g_factor * info.w_scale) : 1.f;
+#pragma unroll
+    for (int k = 0; k < 32; k += 16) loss_out<E>(piece, static_cast<E *>(a.dx), a.ld_dx, a.dx_fours, r.index, c0 + k, a.C, f, v + k);
 }
 
 template <int kKind, int kPlanes, typename E>
@@ -832,14 +826,14 @@ __global__ void __launch_bounds__(kLossThreads, 1) loss_kernel(const __grid_cons
     LossPipe q;
     q.smem0 = ptx::smem_u32(ptx::align_1024(raw));
     q.pieces0 = q.smem0 + Shape::kStages * Shape::kStage;
-    q.bars = q.pieces0 + 8 * kLossPiece;
+    q.bars = q.pieces0 + kLossResults * kLossPiece;
     q.abort_flag = &abort_flag;
     q.n = q.c = 0;
     q.stages = Shape::kStages;
     if (threadIdx.x == 0) {
         abort_flag = 0;
         for (int s = 0; s < Shape::kStages; ++s) { ptx::mbar_init(q.full(s), 1); ptx::mbar_init(q.empty(s), 1); }
-        for (int b = 0; b < 2; ++b) { ptx::mbar_init(q.acc_full(b), 1); ptx::mbar_init(q.acc_empty(b), 16); }
+        for (int b = 0; b < 2; ++b) { ptx::mbar_init(q.acc_full(b), 1); ptx::mbar_init(q.acc_empty(b), 2 * kLossResults); }
         ptx::fence_mbar_init();
     }
     if (ptx::warp_index() == 1) ptx::tmem_alloc_for<2>(ptx::smem_u32(&tmem_slot), 512);
@@ -853,7 +847,8 @@ __global__ void __launch_bounds__(kLossThreads, 1) loss_kernel(const __grid_cons
     const int warp = ptx::warp_index(), pair = (int)(blockIdx.x >> 1), pairs = (int)(gridDim.x >> 1), in_pair = (int)(blockIdx.x & 1);
     const LossInfo info = kKind == kLossStats && a.direct ? LossInfo{(uint32_t)a.direct, 1.f, 1.f, 1.f} : *a.info;
     const int rows = (int)info.rows;
-    // Registers of the launch, 384 x 168, as 128 x 40 (the loading and the issuing warp, two that idle) and 256 x 232: the result warps' hold their 128 sums.
+    // Registers of the launch, 640 x 96, as 128 x 40 (the loading and the issuing warp, two that idle) and 512 x 104.  Sixteen result warps with a quarter of the columns each: with eight and half of them, which
+    // had 168, their own chain of waits took as long as four products (37137 rows of 128 over 25943 words: 469 us).
     if (warp == 0) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
         loss_load<kKind, kPlanes>(q, maps, a, rows, pair, pairs);
@@ -863,32 +858,37 @@ __global__ void __launch_bounds__(kLossThreads, 1) loss_kernel(const __grid_cons
     } else if (warp < 4) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
     } else {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
-        const int quad = warp & 3, half = (warp - 4) >> 2, lane = threadIdx.x & 31;
-        const int cols = (kKind == kLossGrads ? a.grad_width : a.width) / 2;
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
+        const int quad = warp & 3, part = (warp - 4) >> 2, lane = threadIdx.x & 31;
+        const int cols = (kKind == kLossGrads ? a.grad_width : a.width) / 4;
         const float c2 = a.scale * 1.4426950408889634f / (info.x_scale * info.w_scale);
         const uint32_t piece = q.pieces0 + (warp - 4) * kLossPiece;
+        auto row_of = [&](const LossUnit &u) { return u.i * 256 + in_pair * 128 + quad * 32 + lane; };
         LossUnits<kKind> units(a, rows, pair, pairs);
-        LossUnit u;
-        while (units.next(u)) {
-            const int row = u.i * 256 + in_pair * 128 + quad * 32 + lane;
+        LossUnit u, next;
+        bool more = units.next(u);
+        LossRow r = loss_row<kKind>(a, rows, row_of(u), more && (kKind != kLossGrads || u.dx)), r_next;
+        for (uint32_t turn = 0; more; u = next, r = r_next, ++turn) {
+            more = units.next(next);                          // (its rows are asked for a unit ahead)
+            r_next = loss_row<kKind>(a, rows, row_of(next), more && (kKind != kLossGrads || next.dx));
+            const int row = row_of(u);
             if constexpr (kKind == kLossStats) {
-                if (!loss_stats<kPlanes>(q, a, u, loss_row<kKind>(a, rows, row, true), c2, rows, row, u.j * a.width + half * cols, cols, half)) break;
-                continue;
-            }
-            const LossRow r = loss_row<kKind>(a, rows, row, kKind != kLossGrads || u.dx);
-            float v[128];
-            if (!loss_sums<kPlanes>(q, u.kb1 - u.kb0, cols, v)) break;
-            if constexpr (kKind == kLossWeights) loss_weights<kPlanes>(q, a, r, c2, rows, row, u.j * a.width + half * cols, cols, v);
-            else if (u.slot >= 0) {
-                float *slot = a.slots + (((long)u.slot * 2 + in_pair) * a.grad_width + half * cols) * 128 + quad * 32 + lane;
-#pragma unroll
-                for (int e = 0; e < 128; ++e)
-                    if (e < cols) slot[e * 128] = v[e];
+                float2 *joint = reinterpret_cast<float2 *>(ptx::align_1024(raw) + Shape::kStages * Shape::kStage) + (turn & 1) * 3 * 128;
+                if (!loss_stats<kPlanes>(q, a, u, r, c2, rows, row, cols, joint)) break;
             } else {
+                float v[64];
+                if (!loss_sums<kKind, kPlanes>(q, u.kb1 - u.kb0, cols, v)) break;
+                if constexpr (kKind == kLossWeights) loss_weights<kPlanes>(piece, a, r, c2, rows, row, u.j * a.width + part * cols, cols, v);
+                else if (u.slot >= 0) {
+                    float *slot = a.slots + (((long)u.slot * 2 + in_pair) * a.grad_width + part * cols) * 128 + quad * 32 + lane;
 #pragma unroll
-                for (int k = 0; k < 128; k += 32)
-                    if (k < cols) loss_gradient<E>(piece, a, info, r, u.dx, u.i, u.j, in_pair, quad, half * cols + k, v + k);
+                    for (int e = 0; e < 64; ++e)
+                        if (e < cols) slot[e * 128] = v[e];
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 64; k += 32)
+                        if (k < cols) loss_gradient<E>(piece, a, info, r, u.dx, u.i, u.j, in_pair, quad, part * cols + k, v + k);
+                }
             }
         }
     }
@@ -912,7 +912,7 @@ __global__ void __launch_bounds__(kLossThreads, 1) loss_kernel(const __grid_cons
 constexpr int kJoinWarps = 8;
 template <typename E>
 __global__ void __launch_bounds__(32 * kJoinWarps) loss_join_kernel(const LossArgs a, int pairs) {
-    __shared__ __align__(128) uint8_t pieces[kJoinWarps][kLossPiece];
+    __shared__ __align__(128) uint8_t pieces[kJoinWarps][4096];
     ptx::grid_launch();
     ptx::grid_wait();
     const LossInfo info = *a.info;

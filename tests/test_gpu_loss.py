@@ -47,7 +47,7 @@ class Reference:
             E = (3 + 48 + 16) * 2.0 ** -22 + (C / 256 + 2) * U32
             floor = 2.0 ** -38 * (x.abs().max() * w.abs().sum(1).max() + w.abs().max() * x.abs().sum(1).max()) * scale
         else:
-            E, floor = (C / 16 + 2) * 2.0 ** -22, 0.0
+            E, floor = (C / 16 + 2) * 2.0 ** -22, 0.0                           # (of the forward)
         size = scale * (x.abs() @ w.abs().T).max(1).values * E + floor          # of a row's logits
         sums = (128 + V / 2048 + 32 + 40 + 4) * U32
         self.lse_bound = torch.where(there, size + sums + 4 * U32 * self.lse.abs() + 2.0 ** -22, zero)
@@ -56,21 +56,26 @@ class Reference:
         q = p.scatter_add(1, at, -torch.ones_like(self.lse)[:, None])
         g = torch.where(there, dloss if isinstance(dloss, torch.Tensor) else torch.full_like(self.lse, dloss), 0.0).double() * scale
         self.dx, self.dw = g[:, None] * (q @ w), (g[:, None] * q).T @ x
+        # Small bfloat16 vocabularies (W up to 2^22 elements) are multiplied as float16 times powers of two that put the largest element of X and of W between 2^14 and 2^15 and of q at 2^15: a value
+        # that bfloat16 holds is held exactly down to 2^-14 of that scale (2^-28 of the largest), below to half of 2^-24, 2^-39 of the largest; q to 2^-11 and to 2^-40; and x dloss / max dloss to 2^-11.
+        half = T == BF16 and V * C <= 1 << 22
         # errors of q: of p, of its difference from the label's 1, and of its rounding (float32: 22 bits)
+        if half:
+            size = size + 2.0 ** -38 * (x.abs().max() * w.abs().sum(1).max() + w.abs().max() * x.abs().sum(1).max()) * scale
         eps = (size + self.lse_bound + 2.0 ** -21 + 42 * U32)[:, None] * p + 2 * U32 * (q.abs() + p)
         u = 2.0 ** -22 if T == F32 else UNIT[T]
-        dq = (eps + q.abs() * u + (2.0 ** -40 if T == F32 else 2.0 ** -39 if T == F16 else 0.0)) * there[:, None]
+        dq = (eps + q.abs() * u + (2.0 ** -40 if T == F32 else 2.0 ** -39 if T == F16 or half else 0.0)) * there[:, None]
         q = q.abs() * there[:, None]
         steps_x, steps_w = (V / 16 + 76) * 2.0 ** -22, (n / 16 + 76) * 2.0 ** -22
         if T == F32:
             steps_x, steps_w = (67 * 2.0 ** -22 + (V / 256 + 76) * U32), (67 * 2.0 ** -22 + (n / 256 + 76) * U32)
         ga = g.abs()[:, None]
         self.dx_bound = ga * (dq @ w.abs() + steps_x * (q @ w.abs())) + UNIT[T] * self.dx.abs()
-        self.dw_bound = (ga * dq).T @ x.abs() + (steps_w + (u if T != BF16 else 0.0)) * ((ga * q).T @ x.abs()) + UNIT[T] * self.dw.abs()
+        self.dw_bound = (ga * dq).T @ x.abs() + (steps_w + (u if T != BF16 else 2.0 ** -11 if half else 0.0)) * ((ga * q).T @ x.abs()) + UNIT[T] * self.dw.abs()
         if T == F16:                                         # results below the normal numbers; x times dloss / max dloss below them
             self.dx_bound += 2.0 ** -25
             self.dw_bound += 2.0 ** -25 + 2.0 ** -25 * g.abs().max() * q.sum(0)[:, None]
-        if T == F32:
+        if T == F32 or half:
             self.dw_bound += 2.0 ** -38 * x.abs().max() * g.abs().max() * q.sum(0)[:, None]
             self.dx_bound += 2.0 ** -38 * w.abs().max() * ga * q.sum(1)[:, None]
 

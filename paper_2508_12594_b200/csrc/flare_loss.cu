@@ -209,7 +209,10 @@ int prepare_loss(const flare_loss_desc_t *d, const LossPlan &p, const LossLayout
     if ((rc = f32 ? launch_scan<float>(s, st) : d->dtype == FLARE_DTYPE_BF16 ? launch_scan<__nv_bfloat16>(s, st) : launch_scan<__half>(s, st)) != FLARE_OK) return rc;
     k.labels = labels; k.x = x; k.w = w; k.wide = s.wide; k.rows = d->rows; k.cap = p.cap; k.ld_x = ld_x; k.ld_w = ld_w;
     k.w_rows = own_w ? d->vocab : 0; k.C = d->width; k.Cp = p.Cp; k.V = d->vocab; k.chunks = p.chunks; k.x_blocks = p.x_blocks; k.w_blocks = p.w_blocks;
-    k.pack_blocks = (int)((d->rows + kPackRows - 1) / kPackRows);
+    // rows of a block: what keeps four blocks an SM at work in one round, whole parts of a chunk
+    k.pack_rows = 64;
+    while (k.pack_rows < kLossChunk && (long)k.pack_rows * 4 * device_info().sms < d->rows) k.pack_rows *= 2;
+    k.pack_blocks = (int)((d->rows + k.pack_rows - 1) / k.pack_rows);
     k.rank = s.rank; k.chunk = s.chunk; k.largest = s.largest;
     k.info = reinterpret_cast<LossInfo *>(ws + l.info);
     k.px = reinterpret_cast<uint16_t *>(ws + l.px); k.pw = reinterpret_cast<uint16_t *>(ws + l.pw);
@@ -287,8 +290,10 @@ int flare_loss_forward(const flare_loss_desc_t *desc, const void *x, const void 
     }
     a.words = desc->vocab; a.width = p.width; a.tiles_v = (desc->vocab + p.width - 1) / p.width;
     a.part = reinterpret_cast<float2 *>(ws + l.part); a.chosen = reinterpret_cast<float *>(ws + l.chosen);
+    if (a.tiles_v == 1 && !direct) { a.loss = loss; a.lse = lse; }
     const int pairs = (int)std::min<long>(p.pairs, p.cap / 256 * a.tiles_v);
     if (int rc = p.planes == 2 ? launch_loss<kLossStats, 2, float>(maps, a, pairs, st) : launch_loss<kLossStats, 1, float>(maps, a, pairs, st)) return rc;
+    if (a.loss) return FLARE_OK;
     LossMerge m{};
     m.info = a.info; m.part = a.part; m.chosen = a.chosen; m.index = a.index; m.cap = p.cap; m.parts = a.tiles_v; m.loss = loss; m.lse = lse;
     m.labels = a.labels; m.wide = a.wide; m.V = a.V; m.direct = a.direct; m.gave_up = a.gave_up; m.status = a.status; m.blocks = 2 * pairs;

@@ -175,7 +175,7 @@ struct LossPack {
     const void *labels, *x, *w;
     int wide;
     long rows, cap, ld_x, ld_w, w_rows;       // cap: rows up to whole tiles; w_rows: of W to be packed too (0: it is taken as it stands)
-    int C, Cp, V, chunks, x_blocks, w_blocks, pack_blocks;   // Cp: C up to a multiple of eight
+    int C, Cp, V, chunks, x_blocks, w_blocks, pack_blocks, pack_rows;   // Cp: C up to a multiple of eight
     const int *rank;
     const LossChunk *chunk;
     const float *largest;
@@ -191,7 +191,7 @@ struct LossPack {
     void *dx;                                 // rows without a label: zeros
     long ld_dx;
 };
-constexpr int kPackRows = 64, kPackThreads = 256;
+constexpr int kPackThreads = 256;             // of a block, which takes 64 to 1024 rows (of one chunk)
 
 // The power of two that puts `most` between 2^14 and 2^15.
 __device__ __forceinline__ float half_scale(float most) {
@@ -233,8 +233,8 @@ template <typename T, int kTo>
 __global__ void __launch_bounds__(kPackThreads) loss_pack_kernel(const LossPack a) {
     __shared__ float shared[32];
     __shared__ uint32_t sums[2][kPackThreads / 32];
-    __shared__ long to_row[kPackRows];                        // of packed X; -1: no label
-    __shared__ float d_row[kPackRows];                        // dloss / dmax
+    __shared__ int to_row[kLossChunk];                        // of packed X; -1: no label
+    __shared__ float d_row[kLossChunk];                       // dloss / dmax
     ptx::grid_launch();
     ptx::grid_wait();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -269,7 +269,7 @@ __global__ void __launch_bounds__(kPackThreads) loss_pack_kernel(const LossPack 
         return;
     }
     // labelled rows before this block's chunk, and in all
-    const long n0 = (long)blockIdx.x * kPackRows;
+    const long n0 = (long)blockIdx.x * a.pack_rows;
     const int chunk = (int)(n0 / kLossChunk);
     uint32_t base = 0, total = 0;
     float dmax = 0.f;
@@ -290,18 +290,18 @@ __global__ void __launch_bounds__(kPackThreads) loss_pack_kernel(const LossPack 
     for (int w = 0; w < kPackThreads / 32; ++w) { base += sums[0][w]; total += sums[1][w]; }
     if (!a.dloss || !(dmax > 0.f)) dmax = 1.f;
     if (blockIdx.x == 0 && threadIdx.x == 0) *a.info = LossInfo{total, sx, sw, dmax};
-    const int rows = (int)min((long)kPackRows, a.rows - n0);
-    if ((int)threadIdx.x < rows) {
-        const long n = n0 + threadIdx.x;
+    const int rows = (int)min((long)a.pack_rows, a.rows - n0);
+    for (int i = threadIdx.x; i < rows; i += kPackThreads) {
+        const long n = n0 + i;
         const int rank = a.rank[n];
         const long to = rank < 0 ? -1 : (long)base + rank;
-        to_row[threadIdx.x] = to;
+        to_row[i] = (int)to;
         if (rank >= 0) {
             a.index[to] = (int)n;
             a.label[to] = (int)label_at(a.labels, a.wide, n);
             if (a.loss == nullptr) {
                 const float d = a.dloss ? a.dloss[n] : 1.f;
-                d_row[threadIdx.x] = d / dmax;
+                d_row[i] = d / dmax;
                 a.lse2[to] = a.lse_in[n] * 1.4426950408889634f;
                 a.coef[to] = d * a.mult;
             }
@@ -396,6 +396,7 @@ struct LossArgs {
     // forward: maximum and sum of tiles_v parts of a row (in units of ln 2), the label's logit
     float2 *part;
     float *chosen;
+    float *loss, *lse;           // not null: a tile is all of the vocabulary, which finishes its rows
     // backward
     const float *lse2, *coef;
     float g_factor;              // of q in G; 0: dloss scale, a row's own
@@ -629,7 +630,7 @@ __device__ __forceinline__ LossRow loss_row(const LossArgs &a, int rows, int row
     if (row < rows && wanted) {
         if (kKind != kLossGrads) r.label = a.label_of(row);
         if (kKind == kLossWeights) r.lse2 = a.lse2[row];
-        if (kKind == kLossGrads) r.index = a.index[row];
+        if (kKind == kLossGrads || (kKind == kLossStats && a.loss)) r.index = a.index[row];
         if (kKind != kLossStats) r.coef = a.coef[row];
     }
     return r;
@@ -644,14 +645,19 @@ __device__ __forceinline__ LossStat loss_stat(float (&v)[64], int left, float c2
     }
     float mx[4] = {v[0], v[1], v[2], v[3]};
 #pragma unroll
-    for (int e = 4; e < 64; e += 4)
+    for (int e = 4; e < 60; e += 8)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) mx[i] = fmaxf(mx[i], v[e + i]);
+        for (int i = 0; i < 4; ++i) mx[i] = ptx::max3(mx[i], v[e + i], v[e + 4 + i]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) mx[i] = fmaxf(mx[i], v[60 + i]);
     const float m = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * c2, ref = m == -INFINITY ? 0.f : m;
-    float l[4] = {0.f, 0.f, 0.f, 0.f};
+    float2 l[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
-    for (int e = 0; e < 64; ++e) l[e & 3] += ptx::ex2(fmaf(v[e], c2, -ref));
-    return LossStat{m, (l[0] + l[1]) + (l[2] + l[3])};
+    for (int e = 0; e < 64; e += 2) {
+        const float2 x = __ffma2_rn(make_float2(v[e], v[e + 1]), make_float2(c2, c2), make_float2(-ref, -ref));
+        l[e >> 1 & 1] = __fadd2_rn(l[e >> 1 & 1], make_float2(ptx::ex2(x.x), ptx::ex2(x.y)));
+    }
+    return LossStat{m, (l[0].x + l[0].y) + (l[1].x + l[1].y)};
 }
 __device__ __forceinline__ LossStat loss_both(LossStat a, LossStat b) {
     const float m = fmaxf(a.m, b.m), ref = m == -INFINITY ? 0.f : m;
@@ -686,7 +692,8 @@ __device__ __forceinline__ bool loss_stats(LossPipe &q, const LossArgs &a, const
         const bool mine = at >= 0 && at < cols;
         if (__any_sync(0xffffffffu, mine)) {
             const float c = loss_pick(v, at);
-            if (mine) a.chosen[row] = c * c2;
+            if (mine && a.loss) reinterpret_cast<float *>(joint + 3 * 128)[local] = c * c2;
+            else if (mine) a.chosen[row] = c * c2;
         }
         const int left = min(cols, a.V - col0);
         if (left > 0) s = loss_stat(v, left, c2);
@@ -699,7 +706,13 @@ __device__ __forceinline__ bool loss_stats(LossPipe &q, const LossArgs &a, const
             const float2 x = joint[p * 128 + local];
             s = loss_both(s, LossStat{x.x, x.y});
         }
-        a.part[(long)u.j * a.cap + row] = make_float2(s.m, s.l);
+        if (a.loss) {
+            const float log_l = logf(s.l);
+            a.loss[r.index] = (s.m - reinterpret_cast<const float *>(joint + 3 * 128)[local]) * 0.69314718056f + log_l;
+            a.lse[r.index] = s.m * 0.69314718056f + log_l;
+        } else {
+            a.part[(long)u.j * a.cap + row] = make_float2(s.m, s.l);
+        }
     }
     return true;
 }
@@ -714,14 +727,19 @@ __device__ __forceinline__ void loss_weights(uint32_t piece, const LossArgs &a, 
     const int at = r.label - col0;                                       // (no label: below zero)
     const float lse2 = r.lse2, f = a.g_factor != 0.f ? a.g_factor : r.coef;
     const int words = in ? a.V - col0 : 0;
+    // the label's, where it is among the columns: put into the piece on its own
+    const bool mine = at >= 0 && at < cols;
+    float own = 0.f;
+    if (__any_sync(0xffffffffu, mine)) own = (ptx::ex2(fmaf(loss_pick(v, at), c2, -lse2)) - 1.f) * f;
 #pragma unroll
     for (int k = 0; k < 64; k += 32) {
         if (k >= cols) break;
 #pragma unroll
-        for (int e = 0; e < 32; ++e) {
-            float p = ptx::ex2(fmaf(v[k + e], c2, -lse2));
-            if (at == k + e) p -= 1.f;
-            v[k + e] = p * f;
+        for (int e = 0; e < 32; e += 2) {
+            const float2 x = __ffma2_rn(make_float2(v[k + e], v[k + e + 1]), make_float2(c2, c2), make_float2(-lse2, -lse2));
+            const float2 y = __fmul2_rn(make_float2(ptx::ex2(x.x), ptx::ex2(x.y)), make_float2(f, f));
+            v[k + e] = y.x;
+            v[k + e + 1] = y.y;
         }
         if (words - k < 32) {                                            // beyond the vocabulary, or rows that are none: zeros whatever the sums hold
 #pragma unroll
@@ -749,6 +767,16 @@ __device__ __forceinline__ void loss_weights(uint32_t piece, const LossArgs &a, 
                     }
                 }
                 ptx::sts128(piece + piece_at(lane, e), w);
+            }
+            if (mine && (at & ~31) == k) {
+                uint16_t bits;
+                if (kPlanes == 1 && a.bf16) bits = __bfloat16_as_ushort(__float2bfloat16_rn(own));
+                else {
+                    const __half t = __float2half_rn(own);
+                    bits = __half_as_ushort(t);
+                    own -= __half2float(t);
+                }
+                asm volatile("st.shared.b16 [%0], %1;" ::"r"(piece + piece_at(lane, at >> 3 & 3) + (at & 7) * 2), "h"(bits) : "memory");
             }
             __syncwarp();
             uint16_t *out = a.g + ((long)h * a.cap + (row - lane) + (lane >> 2)) * a.ld_g + local0 + k + (lane & 3) * 8;
@@ -873,7 +901,7 @@ __global__ void __launch_bounds__(kLossThreads, 1) loss_kernel(const __grid_cons
             r_next = loss_row<kKind>(a, rows, row_of(next), more && (kKind != kLossGrads || next.dx));
             const int row = row_of(u);
             if constexpr (kKind == kLossStats) {
-                float2 *joint = reinterpret_cast<float2 *>(ptx::align_1024(raw) + Shape::kStages * Shape::kStage) + (turn & 1) * 3 * 128;
+                float2 *joint = reinterpret_cast<float2 *>(ptx::align_1024(raw) + Shape::kStages * Shape::kStage) + (turn & 1) * 4 * 128;
                 if (!loss_stats<kPlanes>(q, a, u, r, c2, rows, row, cols, joint)) break;
             } else {
                 float v[64];

@@ -837,6 +837,25 @@ struct DropArg {
         return x;
     }
 };
+// The call's device: that of its first tensor, which the others (tensors, None, or numbers) have to be on, and which is current for as long as the call lasts.
+struct OnDevice {
+    c10::cuda::OptionalCUDAGuard guard;
+    OnDevice(const at::Tensor &x, std::initializer_list<PyObject *> others) {
+        if (!x.is_cuda()) fail(PyExc_ValueError, "expected a CUDA tensor");
+        for (PyObject *o : others) {
+            if (o == Py_None) continue;
+            if (PyTuple_Check(o)) {
+                for (Py_ssize_t i = 0; i < PyTuple_GET_SIZE(o); ++i) same(x, PyTuple_GET_ITEM(o, i));
+            } else {
+                same(x, o);
+            }
+        }
+        guard.set_device(x.device());
+    }
+    static void same(const at::Tensor &x, PyObject *o) {
+        if (THPVariable_Check(o) && THPVariable_Unpack(o).device() != x.device()) fail(PyExc_ValueError, "expected all tensors on one device");
+    }
+};
 at::ScalarType dtype_or(PyObject *o, at::ScalarType other) {
     if (o == Py_None) return other;
     if (!THPDtype_Check(o)) fail(PyExc_TypeError, "dtype: expected a torch dtype");
@@ -865,6 +884,7 @@ PyObject *wrap_written(const at::Tensor &t, PyObject *out) {
 // x, drop, residual or None, out or None, stream -> y
 BINDING(dropout, 5)
     const at::Tensor &x = tensor(a[0]);
+    const OnDevice here(x, {a[1], a[2], a[3]});
     const DropArg drop(a[1]);
     flare_dropout_desc_t d{};
     if (x.dim() < 1) fail(PyExc_ValueError, "expected tensors [..., width], got shape " + shape_text(x.sizes()));
@@ -887,6 +907,7 @@ BINDING_END
 // dy, drop, dtype or None, out or None, stream -> dx
 BINDING(dropout_backward, 5)
     const at::Tensor &dy = tensor(a[0]);
+    const OnDevice here(dy, {a[1], a[3]});
     const DropArg drop(a[1]);
     flare_dropout_desc_t d{};
     if (dy.dim() < 1) fail(PyExc_ValueError, "expected tensors [..., width], got shape " + shape_text(dy.sizes()));
@@ -907,6 +928,7 @@ BINDING_END
 // tokens, table, positions or None, scale, drop or None, dtype or None, out or None, stream -> y
 BINDING(embed, 8)
     const at::Tensor &tokens = tensor(a[0]), &table = tensor(a[1]);
+    const OnDevice here(table, {a[0], a[2], a[4], a[6]});
     flare_embed_desc_t d{};
     const void *pt = numbers_of(tokens, d.token_bits, "tokens");
     if (table.dim() != 2 || table.size(0) < 1 || table.size(0) > INT32_MAX) fail(PyExc_ValueError, "table: expected shape (vocab, width), got " + shape_text(table.sizes()));
@@ -939,6 +961,7 @@ BINDING_END
 // tokens, dy, vocab, positions (0: none), scale, drop or None, dtype or None, accumulate, out (dtable, dpositions) or None, stream, class of the result
 BINDING(embed_backward, 11)
     const at::Tensor &tokens = tensor(a[0]), &dy = tensor(a[1]);
+    const OnDevice here(dy, {a[0], a[5], a[8]});
     flare_embed_desc_t d{};
     const void *pt = numbers_of(tokens, d.token_bits, "tokens");
     const int vocab = number_of(a[2]), positions = number_of(a[3]);
@@ -1003,6 +1026,7 @@ struct Vocabulary {
 // x, w, labels, scale, out (loss, lse) or None, stream -> (loss, lse, workspace)
 BINDING(token_loss, 6)
     const at::Tensor &x = tensor(a[0]);
+    const OnDevice here(x, {a[1], a[2], a[4]});
     const Vocabulary c(x, tensor(a[1]), tensor(a[2]), a[3]);
     flare_stream_t st = stream_of(a[5]);
     const Outputs output{a[4], a[5], st};
@@ -1021,6 +1045,7 @@ BINDING_END
 // x, w, labels, lse, dloss (a tensor or a number), scale, out (dx, dw) or None, stream, class of the result -> ((dx, dw), workspace)
 BINDING(token_loss_backward, 9)
     const at::Tensor &x = tensor(a[0]), &w = tensor(a[1]);
+    const OnDevice here(x, {a[1], a[2], a[3], a[4], a[6]});
     Vocabulary c(x, w, tensor(a[2]), a[5]);
     const at::Tensor &lse = tensor(a[3]);
     check(lse, at::kFloat, c.rows_shape);

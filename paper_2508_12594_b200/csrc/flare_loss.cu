@@ -292,7 +292,8 @@ int flare_loss_forward(const flare_loss_desc_t *desc, const void *x, const void 
     a.part = reinterpret_cast<float2 *>(ws + l.part); a.chosen = reinterpret_cast<float *>(ws + l.chosen);
     if (a.tiles_v == 1 && !direct) { a.loss = loss; a.lse = lse; }
     const int pairs = (int)std::min<long>(p.pairs, p.cap / 256 * a.tiles_v);
-    if (int rc = p.planes == 2 ? launch_loss<kLossStats, 2, float>(maps, a, pairs, st) : launch_loss<kLossStats, 1, float>(maps, a, pairs, st)) return rc;
+    auto stats = p.planes == 2 ? launch_loss<kLossStats, 2, float> : desc->width <= 64 * kLossDeep<kLossTurns, 1> ? launch_loss<kLossTurns, 1, float> : launch_loss<kLossStats, 1, float>;
+    if (int rc = stats(maps, a, pairs, st)) return rc;
     if (a.loss) return FLARE_OK;
     LossMerge m{};
     m.info = a.info; m.part = a.part; m.chosen = a.chosen; m.index = a.index; m.cap = p.cap; m.parts = a.tiles_v; m.loss = loss; m.lse = lse;

@@ -361,7 +361,8 @@ __global__ void __launch_bounds__(kPackThreads) loss_pack_kernel(const LossPack 
 }
 
 // ---------------------------------------------------------------- the products
-enum { kLossStats = 0, kLossWeights = 1, kLossGrads = 2 };
+enum { kLossStats = 0, kLossWeights = 1, kLossGrads = 2, kLossTurns = 3 };   // (kLossTurns: kLossStats with tiles by turns)
+__host__ __device__ constexpr bool loss_forward(int kind) { return kind == kLossStats || kind == kLossTurns; }
 constexpr int kLossThreads = 640, kLossResults = 16;          // warp 0 loads, warp 1 issues, warps 4 to 19 take the sums out of tensor memory
 constexpr uint32_t kLossHalfTile = 128 * 128;                 // bytes: 128 rows (or 64 rows of two blocks of columns) of 64 elements
 constexpr uint32_t kLossPiece = 2048;                         // a warp's piece of a result on its way out: 32 rows of 64 bytes
@@ -371,7 +372,7 @@ template <int kPlanes> struct LossShape {
 };
 // 64-deep steps whose sums stay in tensor memory, where every addition truncates: of halves 4 (12 x 4 additions); of the forward's 16-bit factors 8 (a loss over 4096 columns is off by 2e-6 with all of
 // them there); of the backward's, whose results are rounded to 2^-9 or 2^-12, 64.
-template <int kKind, int kPlanes> constexpr int kLossDeep = kPlanes == 2 ? 4 : kKind == kLossStats ? 8 : 64;
+template <int kKind, int kPlanes> constexpr int kLossDeep = kPlanes == 2 ? 4 : loss_forward(kKind) ? 8 : 64;
 constexpr size_t kLossSmem = 1024 + 6 * 2 * kLossHalfTile + kLossResults * kLossPiece + 256;
 
 struct LossMaps { CUtensorMap x, d, w, g; };                  // in boxes of 64 x 64
@@ -448,18 +449,21 @@ struct LossUnit { int dx, i, j, kb0, kb1, slot; };            // dx: of that pro
 // A pair's units of work, one after the other; every role walks through them for itself.
 template <int kKind> struct LossUnits;
 template <int kKind> struct LossTiles {                       // of X W^T: rows fastest, so that pairs side by side share words
-    int t, step, total, rb, deep;
-    __device__ __forceinline__ LossTiles(const LossArgs &a, int rows, int pair, int pairs) : t(pair), step(pairs), rb(max(1, (rows + 255) / 256)), deep((a.C + 63) / 64) {
-        total = rb * a.tiles_v;
+    int i, j, di, dj, rb, tiles_v, deep;
+    __device__ __forceinline__ LossTiles(const LossArgs &a, int rows, int pair, int pairs) : rb(max(1, (rows + 255) / 256)), tiles_v(a.tiles_v), deep((a.C + 63) / 64) {
+        i = pair % rb; j = pair / rb;
+        di = pairs % rb; dj = pairs / rb;
     }
     __device__ __forceinline__ bool next(LossUnit &u) {
-        if (t >= total) return false;
-        u = LossUnit{0, t % rb, t / rb, 0, deep, -1};
-        t += step;
+        if (j >= tiles_v) return false;
+        u = LossUnit{0, i, j, 0, deep, -1};
+        i += di; j += dj;
+        if (i >= rb) { i -= rb; ++j; }
         return true;
     }
 };
 template <> struct LossUnits<kLossStats> : LossTiles<kLossStats> { using LossTiles::LossTiles; };
+template <> struct LossUnits<kLossTurns> : LossTiles<kLossTurns> { using LossTiles::LossTiles; };
 template <> struct LossUnits<kLossWeights> : LossTiles<kLossWeights> { using LossTiles::LossTiles; };
 template <> struct LossUnits<kLossGrads> {
     LossSplit s;
@@ -615,10 +619,14 @@ __device__ __forceinline__ bool loss_sums(LossPipe &q, int deep, int cols, float
     }
     return true;
 }
-// All result warps at one barrier: whether all of them have their sums, the same in all of their threads.  (A warp whose wait gave up comes here too.)
+// So many result warps at one barrier: whether all of them have their sums, the same in all of their threads.  (A warp whose wait gave up comes here too.)
+template <int kBarrier, int kWarps>
 __device__ __forceinline__ bool loss_agree(bool ok) {
     uint32_t all;
-    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbar.red.and.pred q, 1, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(all) : "r"((uint32_t)ok), "n"(32 * kLossResults) : "memory");
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbar.red.and.pred q, %3, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                 : "=r"(all)
+                 : "r"((uint32_t)ok), "n"(32 * kWarps), "n"(kBarrier)
+                 : "memory");
     return all != 0;
 }
 
@@ -630,8 +638,8 @@ __device__ __forceinline__ LossRow loss_row(const LossArgs &a, int rows, int row
     if (row < rows && wanted) {
         if (kKind != kLossGrads) r.label = a.label_of(row);
         if (kKind == kLossWeights) r.lse2 = a.lse2[row];
-        if (kKind == kLossGrads || (kKind == kLossStats && a.loss)) r.index = a.index[row];
-        if (kKind != kLossStats) r.coef = a.coef[row];
+        if (kKind == kLossGrads || (loss_forward(kKind) && a.loss)) r.index = a.index[row];
+        if (!loss_forward(kKind)) r.coef = a.coef[row];
     }
     return r;
 }
@@ -659,9 +667,15 @@ __device__ __forceinline__ LossStat loss_stat(float (&v)[64], int left, float c2
     }
     return LossStat{m, (l[0].x + l[0].y) + (l[1].x + l[1].y)};
 }
-__device__ __forceinline__ LossStat loss_both(LossStat a, LossStat b) {
-    const float m = fmaxf(a.m, b.m), ref = m == -INFINITY ? 0.f : m;
-    return LossStat{m, a.l * ptx::ex2(a.m - ref) + b.l * ptx::ex2(b.m - ref)};
+template <int N> __device__ __forceinline__ LossStat loss_all(const LossStat (&s)[N]) {
+    float m = s[0].m;
+#pragma unroll
+    for (int i = 1; i < N; ++i) m = fmaxf(m, s[i].m);
+    const float ref = m == -INFINITY ? 0.f : m;
+    float l = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) l += s[i].l * ptx::ex2(s[i].m - ref);
+    return LossStat{m, l};
 }
 // The value at place `at` (0 to 63), by halves of sixteen at a time.
 __device__ __forceinline__ float loss_pick(const float (&v)[64], int at) {
@@ -680,39 +694,78 @@ __device__ __forceinline__ float loss_pick(const float (&v)[64], int at) {
     }
     return r;
 }
-// A tile's part of a row: by four warps, a quarter of the columns each, joined in shared memory (two places in turn: a place is written again behind the next tile's barrier).
+// What four (or two) warps' columns of a tile say of their rows, joined in shared memory; `joint`: [warps - 1][128 rows], then the labels' logits.
+__device__ __forceinline__ void loss_row_out(const LossArgs &a, const LossRow &r, int j, int row, int rows, LossStat s, const float *chosen) {
+    if (row >= rows) return;
+    if (a.loss) {
+        const float log_l = logf(s.l);
+        a.loss[r.index] = (s.m - *chosen) * 0.69314718056f + log_l;
+        a.lse[r.index] = s.m * 0.69314718056f + log_l;
+    } else {
+        a.part[(long)j * a.cap + row] = make_float2(s.m, s.l);
+    }
+}
+__device__ __forceinline__ LossStat loss_columns(const LossArgs &a, float (&v)[64], int at, int cols, int left, int row, float c2, float *chosen) {
+    const bool mine = at >= 0 && at < cols;
+    if (__any_sync(0xffffffffu, mine)) {
+        const float c = loss_pick(v, at);
+        if (mine) *(a.loss ? chosen : a.chosen + row) = c * c2;
+    }
+    return left > 0 ? loss_stat(v, min(cols, left), c2) : LossStat{-INFINITY, 0.f};
+}
+constexpr int kJoint = 4 * 128;                               // float2 of a place; places are written in turn: one again behind the next tile's barrier
+// A tile by all sixteen warps, a quarter of the columns each.
 template <int kPlanes>
 __device__ __forceinline__ bool loss_stats(LossPipe &q, const LossArgs &a, const LossUnit &u, const LossRow &r, float c2, int rows, int row, int cols, float2 *joint) {
     const int warp = ptx::warp_index(), part = (warp - 4) >> 2, local = (warp & 3) * 32 + (threadIdx.x & 31), col0 = u.j * a.width + part * cols;
-    const int at = r.label - col0;                                       // the label's column here (no label: below zero)
+    float *chosen = reinterpret_cast<float *>(joint + 3 * 128) + local;
     float v[64];
     const bool ok = loss_sums<kLossStats, kPlanes>(q, u.kb1, cols, v);
-    LossStat s{-INFINITY, 0.f};
-    if (ok && row - local % 32 < rows) {                                 // (some of the warp's rows are rows)
-        const bool mine = at >= 0 && at < cols;
-        if (__any_sync(0xffffffffu, mine)) {
-            const float c = loss_pick(v, at);
-            if (mine && a.loss) reinterpret_cast<float *>(joint + 3 * 128)[local] = c * c2;
-            else if (mine) a.chosen[row] = c * c2;
-        }
-        const int left = min(cols, a.V - col0);
-        if (left > 0) s = loss_stat(v, left, c2);
-    }
-    if (part > 0) joint[(part - 1) * 128 + local] = make_float2(s.m, s.l);
-    if (!loss_agree(ok)) return false;
-    if (part == 0 && row < rows) {
+    LossStat s[4] = {{-INFINITY, 0.f}, {-INFINITY, 0.f}, {-INFINITY, 0.f}, {-INFINITY, 0.f}};
+    if (ok && row - local % 32 < rows) s[0] = loss_columns(a, v, r.label - col0, cols, a.V - col0, row, c2, chosen);   // (some of the warp's rows are rows)
+    if (part > 0) joint[(part - 1) * 128 + local] = make_float2(s[0].m, s[0].l);
+    if (!loss_agree<1, kLossResults>(ok)) return false;
+    if (part == 0) {
 #pragma unroll
-        for (int p = 0; p < 3; ++p) {
-            const float2 x = joint[p * 128 + local];
-            s = loss_both(s, LossStat{x.x, x.y});
+        for (int p = 0; p < 3; ++p) s[p + 1] = LossStat{joint[p * 128 + local].x, joint[p * 128 + local].y};
+        loss_row_out(a, r, u.j, row, rows, loss_all(s), chosen);
+    }
+    return true;
+}
+// Tiles in turn by two sets of eight warps, half of the columns each in two steps, where one set of sums is all there is (up to 512 columns of 16 bits): then the sums come quicker than a tile's end, and with all warps
+// at the same tile, which wait for one another, the special-function units rest while the others' maxima, labels and joins are formed (131072 rows of 128 over 256 words: 25 us then, 20 in turns).
+__device__ __forceinline__ bool loss_stats_by_turns(LossPipe &q, const LossArgs &a, const LossUnit &u, const LossRow &r, float c2, int rows, int row, float2 *joint) {
+    const int warp = ptx::warp_index(), part = (warp - 4) >> 2, set = part >> 1, half = part & 1, local = (warp & 3) * 32 + (threadIdx.x & 31), cols = a.width / 2;
+    const uint32_t acc = q.tmem + ((uint32_t)((warp & 3) * 32) << 16) + half * cols + (q.c & 1) * 256;
+    float *chosen = reinterpret_cast<float *>(joint + 3 * 128) + local;
+    bool ok = ptx::mbar_wait(q.acc_full(q.c & 1), (q.c / 2) & 1, q.abort_flag, 114);
+    ok = __all_sync(0xffffffffu, ok);
+    LossStat s[2] = {{-INFINITY, 0.f}, {-INFINITY, 0.f}};
+    const int col0 = u.j * a.width + half * cols;
+    if (ok) {
+        ptx::tc_fence_after();
+#pragma unroll 1
+        for (int k = 0; 64 * k < cols; ++k) {
+            float v[64];
+            ptx::tmem_ld32(acc + 64 * k, reinterpret_cast<uint32_t (&)[32]>(v[0]));
+            ptx::tmem_ld32(acc + 64 * k + 32, reinterpret_cast<uint32_t (&)[32]>(v[32]));
+            ptx::tmem_wait_ld();
+            if (64 * (k + 1) >= cols) {
+                ptx::tc_fence_before();
+                __syncwarp();
+                if ((threadIdx.x & 31) == 0) ptx::mbar_arrive_remote(ptx::in_block(q.acc_empty(q.c & 1), 0));
+            }
+            if (row - local % 32 < rows) {
+                s[1] = loss_columns(a, v, r.label - col0 - 64 * k, 64, a.V - col0 - 64 * k, row, c2, chosen);
+                s[0] = loss_all(s);
+            }
         }
-        if (a.loss) {
-            const float log_l = logf(s.l);
-            a.loss[r.index] = (s.m - reinterpret_cast<const float *>(joint + 3 * 128)[local]) * 0.69314718056f + log_l;
-            a.lse[r.index] = s.m * 0.69314718056f + log_l;
-        } else {
-            a.part[(long)u.j * a.cap + row] = make_float2(s.m, s.l);
-        }
+    }
+    if (half > 0) joint[local] = make_float2(s[0].m, s[0].l);
+    if (!(set ? loss_agree<2, kLossResults / 2>(ok) : loss_agree<1, kLossResults / 2>(ok))) return false;
+    if (half == 0) {
+        s[1] = LossStat{joint[local].x, joint[local].y};
+        loss_row_out(a, r, u.j, row, rows, loss_all(s), chosen);
     }
     return true;
 }
@@ -858,10 +911,11 @@ __global__ void __launch_bounds__(kLossThreads, 1) loss_kernel(const __grid_cons
     q.abort_flag = &abort_flag;
     q.n = q.c = 0;
     q.stages = Shape::kStages;
+    constexpr bool by_turns = kKind == kLossTurns;
     if (threadIdx.x == 0) {
         abort_flag = 0;
         for (int s = 0; s < Shape::kStages; ++s) { ptx::mbar_init(q.full(s), 1); ptx::mbar_init(q.empty(s), 1); }
-        for (int b = 0; b < 2; ++b) { ptx::mbar_init(q.acc_full(b), 1); ptx::mbar_init(q.acc_empty(b), 2 * kLossResults); }
+        for (int b = 0; b < 2; ++b) { ptx::mbar_init(q.acc_full(b), 1); ptx::mbar_init(q.acc_empty(b), by_turns ? kLossResults : 2 * kLossResults); }
         ptx::fence_mbar_init();
     }
     if (ptx::warp_index() == 1) ptx::tmem_alloc_for<2>(ptx::smem_u32(&tmem_slot), 512);
@@ -873,7 +927,7 @@ __global__ void __launch_bounds__(kLossThreads, 1) loss_kernel(const __grid_cons
     ptx::grid_launch();
     ptx::grid_wait();
     const int warp = ptx::warp_index(), pair = (int)(blockIdx.x >> 1), pairs = (int)(gridDim.x >> 1), in_pair = (int)(blockIdx.x & 1);
-    const LossInfo info = kKind == kLossStats && a.direct ? LossInfo{(uint32_t)a.direct, 1.f, 1.f, 1.f} : *a.info;
+    const LossInfo info = loss_forward(kKind) && a.direct ? LossInfo{(uint32_t)a.direct, 1.f, 1.f, 1.f} : *a.info;
     const int rows = (int)info.rows;
     // Registers of the launch, 640 x 96, as 128 x 40 (the loading and the issuing warp, two that idle) and 512 x 104.  Sixteen result warps with a quarter of the columns each: with eight and half of them, which
     // had 168, their own chain of waits took as long as four products (37137 rows of 128 over 25943 words: 469 us).
@@ -894,15 +948,20 @@ __global__ void __launch_bounds__(kLossThreads, 1) loss_kernel(const __grid_cons
         auto row_of = [&](const LossUnit &u) { return u.i * 256 + in_pair * 128 + quad * 32 + lane; };
         LossUnits<kKind> units(a, rows, pair, pairs);
         LossUnit u, next;
+        float2 *joint = reinterpret_cast<float2 *>(ptx::align_1024(raw) + Shape::kStages * Shape::kStage);
         bool more = units.next(u);
+        if (by_turns && part >= 2) { more = units.next(u); q.c = 1; }     // (the second set begins with the second tile)
         LossRow r = loss_row<kKind>(a, rows, row_of(u), more && (kKind != kLossGrads || u.dx)), r_next;
         for (uint32_t turn = 0; more; u = next, r = r_next, ++turn) {
             more = units.next(next);                          // (its rows are asked for a unit ahead)
+            if (by_turns && more) more = units.next(next);
             r_next = loss_row<kKind>(a, rows, row_of(next), more && (kKind != kLossGrads || next.dx));
             const int row = row_of(u);
             if constexpr (kKind == kLossStats) {
-                float2 *joint = reinterpret_cast<float2 *>(ptx::align_1024(raw) + Shape::kStages * Shape::kStage) + (turn & 1) * 4 * 128;
-                if (!loss_stats<kPlanes>(q, a, u, r, c2, rows, row, cols, joint)) break;
+                if (!loss_stats<kPlanes>(q, a, u, r, c2, rows, row, cols, joint + (turn & 1) * kJoint)) break;
+            } else if constexpr (kKind == kLossTurns) {
+                if (!loss_stats_by_turns(q, a, u, r, c2, rows, row, joint + (2 * (part >> 1) + (turn & 1)) * kJoint)) break;
+                q.c += 2;
             } else {
                 float v[64];
                 if (!loss_sums<kKind, kPlanes>(q, u.kb1 - u.kb0, cols, v)) break;
@@ -926,7 +985,7 @@ __global__ void __launch_bounds__(kLossThreads, 1) loss_kernel(const __grid_cons
     let_arrive(q.abort_flag);
     ptx::cluster_meet();                                      // (nobody's shared or tensor memory is needed any more)
     if (threadIdx.x == 0) {
-        if (kKind == kLossStats && a.direct) a.gave_up[blockIdx.x] = abort_flag;
+        if (loss_forward(kKind) && a.direct) a.gave_up[blockIdx.x] = abort_flag;
         else if (abort_flag != 0) *a.status = abort_flag;
     }
     if (warp == 1) {

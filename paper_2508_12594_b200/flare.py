@@ -457,7 +457,7 @@ def dropout(x, drop: Drop, residual=None, out=None, stream=None):
 
 
 def dropout_backward(dy, drop: Drop, dtype=None, out=None, stream=None):
-    """The gradient of dropout's x, of `dtype` (dy's): the elements that the same Drop keeps.  The residual's is dy."""
+    """The gradient of dropout's x, of `dtype` (dy's; any where dy is float32): the elements that the same Drop keeps.  The residual's is dy."""
     return (_native or _bind()).dropout_backward(dy, drop, dtype, out, stream)
 
 

@@ -206,14 +206,15 @@ int prepare_loss(const flare_loss_desc_t *d, const LossPlan &p, const LossLayout
     s.largest = reinterpret_cast<float *>(ws + l.largest);
     s.status = reinterpret_cast<uint32_t *>(ws);
     int rc;
-    if ((rc = f32 ? launch_scan<float>(s, st) : d->dtype == FLARE_DTYPE_BF16 ? launch_scan<__nv_bfloat16>(s, st) : launch_scan<__half>(s, st)) != FLARE_OK) return rc;
-    k.labels = labels; k.x = x; k.w = w; k.wide = s.wide; k.rows = d->rows; k.cap = p.cap; k.ld_x = ld_x; k.ld_w = ld_w;
-    k.w_rows = own_w ? d->vocab : 0; k.C = d->width; k.Cp = p.Cp; k.V = d->vocab; k.chunks = p.chunks; k.x_blocks = p.x_blocks; k.w_blocks = p.w_blocks;
     // rows of a block: what keeps four blocks an SM at work in one round, whole parts of a chunk
     k.pack_rows = 64;
     while (k.pack_rows < kLossChunk && (long)k.pack_rows * 4 * device_info().sms < d->rows) k.pack_rows *= 2;
+    const bool alone = d->rows <= kPackAlone && p.to == kAsIs && k.pack_rows == 64;
+    if (!alone && (rc = f32 ? launch_scan<float>(s, st) : d->dtype == FLARE_DTYPE_BF16 ? launch_scan<__nv_bfloat16>(s, st) : launch_scan<__half>(s, st)) != FLARE_OK) return rc;
+    k.labels = labels; k.x = x; k.w = w; k.wide = s.wide; k.rows = d->rows; k.cap = p.cap; k.ld_x = ld_x; k.ld_w = ld_w;
+    k.w_rows = own_w ? d->vocab : 0; k.C = d->width; k.Cp = p.Cp; k.V = d->vocab; k.chunks = p.chunks; k.x_blocks = p.x_blocks; k.w_blocks = p.w_blocks;
     k.pack_blocks = (int)((d->rows + k.pack_rows - 1) / k.pack_rows);
-    k.rank = s.rank; k.chunk = s.chunk; k.largest = s.largest;
+    k.rank = alone ? nullptr : s.rank; k.status = s.status; k.chunk = s.chunk; k.largest = s.largest;
     k.info = reinterpret_cast<LossInfo *>(ws + l.info);
     k.px = reinterpret_cast<uint16_t *>(ws + l.px); k.pw = reinterpret_cast<uint16_t *>(ws + l.pw);
     k.index = reinterpret_cast<int *>(ws + l.index); k.label = reinterpret_cast<int *>(ws + l.label);

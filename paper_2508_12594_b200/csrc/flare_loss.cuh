@@ -176,9 +176,10 @@ struct LossPack {
     int wide;
     long rows, cap, ld_x, ld_w, w_rows;       // cap: rows up to whole tiles; w_rows: of W to be packed too (0: it is taken as it stands)
     int C, Cp, V, chunks, x_blocks, w_blocks, pack_blocks, pack_rows;   // Cp: C up to a multiple of eight
-    const int *rank;
+    const int *rank;                          // the scan's; null: there was none
     const LossChunk *chunk;
     const float *largest;
+    uint32_t *status;
     LossInfo *info;
     uint16_t *px, *pd, *pw;                   // packed X, packed dloss X (or null), packed W: planes of [cap][Cp], [V][Cp]
     int *index, *label;                       // of packed rows: row, label
@@ -192,6 +193,7 @@ struct LossPack {
     long ld_dx;
 };
 constexpr int kPackThreads = 256;             // of a block, which takes 64 to 1024 rows (of one chunk)
+constexpr int kPackAlone = 4096;              // rows up to which every block finds for itself, in all labels, what the scan would tell it, where no maxima are wanted: a launch less
 
 // The power of two that puts `most` between 2^14 and 2^15.
 __device__ __forceinline__ float half_scale(float most) {
@@ -268,12 +270,22 @@ __global__ void __launch_bounds__(kPackThreads) loss_pack_kernel(const LossPack 
         }
         return;
     }
-    // labelled rows before this block's chunk, and in all
+    // labelled rows before this block's chunk (alone: before its rows), and in all
+    const bool alone = a.rank == nullptr;
+    if (alone && blockIdx.x == 0 && threadIdx.x < kHeaderBytes / 4) a.status[threadIdx.x] = 0;
     const long n0 = (long)blockIdx.x * a.pack_rows;
     const int chunk = (int)(n0 / kLossChunk);
     uint32_t base = 0, total = 0;
     float dmax = 0.f;
-    for (int i = threadIdx.x; i < a.chunks; i += kPackThreads) {
+    if (alone)
+        for (long n = threadIdx.x; n < a.rows; n += kPackThreads) {
+            const int64_t label = label_at(a.labels, a.wide, n);
+            if (label < 0 || label >= a.V) continue;
+            ++total;
+            if (n < n0) ++base;
+            if (a.dloss) dmax = fmaxf(dmax, finite_abs(a.dloss[n]));
+        }
+    for (int i = alone ? a.chunks : threadIdx.x; i < a.chunks; i += kPackThreads) {
         const LossChunk c = a.chunk[i];
         total += c.rows;
         if (i < chunk) base += c.rows;
@@ -291,9 +303,20 @@ __global__ void __launch_bounds__(kPackThreads) loss_pack_kernel(const LossPack 
     if (!a.dloss || !(dmax > 0.f)) dmax = 1.f;
     if (blockIdx.x == 0 && threadIdx.x == 0) *a.info = LossInfo{total, sx, sw, dmax};
     const int rows = (int)min((long)a.pack_rows, a.rows - n0);
+    if (alone) {                                              // (64 rows: by the first two warps)
+        __syncthreads();                                      // (sums have been read)
+        int64_t label = -1;
+        if ((int)threadIdx.x < rows) label = label_at(a.labels, a.wide, n0 + threadIdx.x);
+        const bool there = label >= 0 && label < a.V;
+        const uint32_t m = __ballot_sync(0xffffffffu, there);
+        if (lane == 0) sums[0][warp] = __popc(m);
+        __syncthreads();
+        if (warp == 1) base += sums[0][0];
+        to_row[threadIdx.x] = there ? __popc(m & ((1u << lane) - 1)) : -1;
+    }
     for (int i = threadIdx.x; i < rows; i += kPackThreads) {
         const long n = n0 + i;
-        const int rank = a.rank[n];
+        const int rank = alone ? to_row[i] : a.rank[n];
         const long to = rank < 0 ? -1 : (long)base + rank;
         to_row[i] = (int)to;
         if (rank >= 0) {
@@ -413,12 +436,15 @@ struct LossArgs {
     float *slots;                // sums of parts of tiles, likewise, two per pair
 };
 
-// Who does what of the two gradients.  Tiles of dW (tall: a piece's words, sums over rows) come first, then tiles of dX (sums over words); whole rounds of
-// them are dealt out a tile a pair, so that pairs side by side read the same columns of G at the same time, and the tiles of the rounds that would not be full are cut along K into
-// equal shares: a pair takes the steps [p S / P, (p + 1) S / P) of theirs.  What is less than a tile goes to a slot of the pair's, to be joined.
+// Who does what of the two gradients.  Tiles of dW (a piece's words, sums over rows) come first, then tiles of dX (sums over words); whole rounds of
+// them are dealt out a tile a pair, so that pairs side by side read the same columns of G at the same time.  Of the rounds that would not be full, either's tiles go to a pair each or are cut along K: the pairs
+// that have none whole take equal shares of their steps, and what is less than a tile goes to a slot of the pair's, to be joined.  Which, by the longest pair's steps, where joining counts as 12 (of one gradient)
+// or 24 of them: 1999 rows of 200 over 10007 words, 40 tiles of 29 steps and 8 of 157, took 18 us to join with all 48 shared.
 struct LossSplit {
-    int tiles_w, tiles_x, deep_w, deep_x, full_w, full_x, pairs, sharing;
-    long steps;
+    int tiles_w, tiles_x, deep_w, deep_x, full_w, full_x, pairs;
+    int whole_w, whole_x;        // tiles of the last rounds that a pair each takes whole: the first pairs those of dW, the next those of dX
+    int sharing;                 // pairs behind them that share the others
+    long steps;                  // of the others
     __device__ __forceinline__ LossSplit(const LossArgs &a, int rows, int pairs_) : pairs(pairs_) {
         const int rb = max(1, (rows + 255) / 256);
         tiles_w = a.dw ? (a.words + 255) / 256 * a.tiles_c : 0;
@@ -429,13 +455,29 @@ struct LossSplit {
         auto full = [&](int tiles) { return tiles % pairs * 8 >= 7 * pairs ? tiles : tiles / pairs * pairs; };
         full_w = full(tiles_w);
         full_x = full(tiles_x);
-        steps = (long)(tiles_w - full_w) * deep_w + (long)(tiles_x - full_x) * deep_x;
-        sharing = (int)max(1L, min((long)pairs, steps / 4));   // at least four steps a share
+        const int rest_w = tiles_w - full_w, rest_x = tiles_x - full_x;
+        const long all_w = (long)rest_w * deep_w, all_x = (long)rest_x * deep_x;
+        whole_w = whole_x = 0;
+        long best = (all_w + all_x) / pairs + 24;
+        auto better = [&](int w, int x) {                     // these whole
+            const int left = pairs - w - x;
+            const long shared = (w ? 0 : all_w) + (x ? 0 : all_x);
+            if (left < 0 || (left == 0 && shared > 0)) return;
+            const long cost = max(max(w ? (long)deep_w : 0L, x ? (long)deep_x : 0L), shared > 0 ? shared / left + 12 : 0L);
+            if (cost < best) { best = cost; whole_w = w; whole_x = x; }
+        };
+        better(rest_w, 0);
+        better(0, rest_x);
+        better(rest_w, rest_x);
+        steps = (whole_w ? 0 : all_w) + (whole_x ? 0 : all_x);
+        sharing = (int)max(1L, min((long)(pairs - whole_w - whole_x), steps / 4));   // at least four steps a share
     }
+    __device__ __forceinline__ int shared_w() const { return whole_w ? 0 : tiles_w - full_w; }
+    __device__ __forceinline__ int shared_x() const { return whole_x ? 0 : tiles_x - full_x; }
     __device__ __forceinline__ long share(int p) const { return (long)p * steps / sharing; }
-    // The part of a tile that step s of the rest is of: its first step, depth and number (tiles of dX behind those of dW).
+    // The shared tile that step s is of: its first step, depth and number (tiles of dX behind those of dW).
     __device__ __forceinline__ void tile_of(long s, long &start, int &deep, int &tile) const {
-        const long w = (long)(tiles_w - full_w) * deep_w;
+        const long w = (long)shared_w() * deep_w;
         if (s < w) {
             const int t = (int)(s / deep_w);
             start = (long)t * deep_w; deep = deep_w; tile = full_w + t;
@@ -468,23 +510,26 @@ template <> struct LossUnits<kLossWeights> : LossTiles<kLossWeights> { using Los
 template <> struct LossUnits<kLossGrads> {
     LossSplit s;
     int pair, tiles_c, t;
+    bool rest;                   // the pair's whole tile of the last rounds is still to come
     long at, end;
     __device__ __forceinline__ LossUnits(const LossArgs &a, int rows, int pair_, int pairs) : s(a, rows, pairs), pair(pair_), tiles_c(a.tiles_c), t(pair_) {
+        const int me = pair - s.whole_w - s.whole_x;          // among those that share
+        rest = me < 0;
         at = end = 0;
-        if (pair < s.sharing) { at = s.share(pair); end = s.share(pair + 1); }
+        if (me >= 0 && me < s.sharing) { at = s.share(me); end = s.share(me + 1); }
     }
+    __device__ __forceinline__ LossUnit whole(int dx, int tile) const { return LossUnit{dx, tile / tiles_c, tile % tiles_c, 0, dx ? s.deep_x : s.deep_w, -1}; }
     __device__ __forceinline__ bool next(LossUnit &u) {
         const int rounds_w = (s.full_w + s.pairs - 1) / s.pairs * s.pairs;
         if (t < rounds_w && t >= s.full_w) t += s.pairs;                          // (no tile for this pair in the last round)
-        if (t < s.full_w) {
-            u = LossUnit{0, t / tiles_c, t % tiles_c, 0, s.deep_w, -1};
+        if (t < s.full_w || t - rounds_w < s.full_x) {
+            u = t < s.full_w ? whole(0, t) : whole(1, t - rounds_w);
             t += s.pairs;
             return true;
         }
-        const int x = t - rounds_w;
-        if (x < s.full_x) {
-            u = LossUnit{1, x / tiles_c, x % tiles_c, 0, s.deep_x, -1};
-            t += s.pairs;
+        if (rest) {
+            rest = false;
+            u = pair < s.whole_w ? whole(0, s.full_w + pair) : whole(1, s.full_x + pair - s.whole_w);
             return true;
         }
         if (at >= end) return false;
@@ -494,7 +539,7 @@ template <> struct LossUnits<kLossGrads> {
         const bool dx = tile >= s.tiles_w;
         if (dx) tile -= s.tiles_w;
         const int kb0 = (int)(at - start), kb1 = (int)min((long)deep, end - start);
-        u = LossUnit{dx, tile / tiles_c, tile % tiles_c, kb0, kb1, kb0 == 0 && kb1 == deep ? -1 : 2 * pair + (kb0 > 0 ? 0 : 1)};
+        u = LossUnit{dx, tile / tiles_c, tile % tiles_c, kb0, kb1, kb0 == 0 && kb1 == deep ? -1 : 2 * (pair - s.whole_w - s.whole_x) + (kb0 > 0 ? 0 : 1)};
         at = start + kb1;
         return true;
     }
@@ -1006,7 +1051,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) loss_join_kernel(const LossAr
     const LossSplit s(a, (int)info.rows, pairs);
     if (s.steps == 0) return;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, blocks_of_tile = 8 * (a.grad_width / 32);   // (2 blocks, 4 quarters of rows)
-    const int rest_w = s.tiles_w - s.full_w, rest_all = rest_w + s.tiles_x - s.full_x;
+    const int rest_w = s.shared_w(), rest_all = rest_w + s.shared_x();
     const long shares = (long)max(s.deep_w, s.deep_x) * s.sharing / s.steps;                                // of a tile, about
     const int team = shares < 4 ? 1 : shares < 8 ? 2 : shares < 16 ? 4 : 8, member = warp % team;
     const long items = (long)rest_all * blocks_of_tile, step = (long)gridDim.x * (kJoinWarps / team);

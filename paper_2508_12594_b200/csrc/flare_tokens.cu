@@ -183,16 +183,30 @@ int launch_zero(ZeroArgs z, uint32_t first, uint32_t last, cudaStream_t st) {
 }
 // dy's type first
 template <typename O, typename T>
-int launch_sums(const SumArgs &a, const ZeroArgs &z, int width, bool whole_positions, cudaStream_t st) {
+int launch_sum(const SumArgs &a, int width, cudaStream_t st) {
     const unsigned blocks = (a.task[0].spans + a.task[1].spans) * a.tiles;
+    if (width == 0) FLARE_CUDA(launch_after(embed_sum_kernel<O, T, 0>, blocks, a.threads, sum_smem(a.threads, 1), st, a));
+    else if (width == 1) FLARE_CUDA(launch_after(embed_sum_kernel<O, T, 1>, blocks, a.threads, sum_smem(a.threads, 1), st, a));
+    else if constexpr (sizeof(O) == 2) FLARE_CUDA(launch_after(embed_sum_kernel<O, T, 2>, blocks, a.threads, sum_smem(a.threads, 2), st, a));
+    return FLARE_OK;
+}
+template <typename O, typename T>
+int launch_sums(const SumArgs &a, const ZeroArgs &z, int width, bool whole_positions, cudaStream_t st) {
     auto joins = [](const SumTask &t) { return (t.spans + kJoinWarps - 1) / kJoinWarps; };
     const unsigned joined = joins(a.task[0]) + (whole_positions ? 0 : joins(a.task[1]));
+    // positions first, beside the sort, which they need not wait for (where there is one: of a few SMs); what comes behind them comes behind it
+    SumArgs positions = a;
+    positions.task[0].spans = 0;
+    positions.beside_zero = a.task[0].spans ? 1 : 0;
+    if (positions.task[1].spans)
+        if (int rc = launch_sum<O, T>(positions, width, st)) return rc;
     const uint32_t half = a.beside_zero == 2 ? z.last / 2 : z.last;
     if (a.beside_zero)
         if (int rc = launch_zero<T>(z, 0, half, st)) return rc;
-    if (width == 0) FLARE_CUDA(launch_after(embed_sum_kernel<O, T, 0>, blocks, a.threads, sum_smem(a.threads, 0 == 2 ? 2 : 1), st, a));
-    else if (width == 1) FLARE_CUDA(launch_after(embed_sum_kernel<O, T, 1>, blocks, a.threads, sum_smem(a.threads, 1 == 2 ? 2 : 1), st, a));
-    else if constexpr (sizeof(O) == 2) FLARE_CUDA(launch_after(embed_sum_kernel<O, T, 2>, blocks, a.threads, sum_smem(a.threads, 2 == 2 ? 2 : 1), st, a));
+    SumArgs tokens = a;
+    tokens.task[1].spans = 0;
+    if (tokens.task[0].spans)
+        if (int rc = launch_sum<O, T>(tokens, width, st)) return rc;
     if (a.beside_zero == 2)
         if (int rc = launch_zero<T>(z, half, z.last, st)) return rc;
     if (joined && width) FLARE_CUDA(launch_after(embed_join_kernel<T, true>, joined, kTokenThreads, 0, st, a));

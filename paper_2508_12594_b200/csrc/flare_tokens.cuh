@@ -458,8 +458,8 @@ __device__ __forceinline__ uint2 before_in_block(uint2 own, uint2 *scan) {
 }
 __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(const SortArgs a) {
     extern __shared__ __align__(16) uint32_t counts[];        // [32 warps][bins], [bins] of the block, [bins] from places here to places in memory, [32] pairs of a scan, pairs
+    ptx::grid_wait();                                         // (then the launch behind this one: positions, which wait for nothing of this one's, but for what came before it)
     ptx::grid_launch();
-    ptx::grid_wait();
     const uint32_t blocks = ptx::cluster_size(), rank = ptx::cluster_rank(), warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     // stretches: of a block, of a warp (whole groups of 32)
     const uint32_t per_warp = ((a.rows + blocks * 32 - 1) / (blocks * 32) + 31) / 32 * 32;
@@ -613,7 +613,7 @@ struct SumArgs {
     SumTask task[2];
     const void *dy;
     uint32_t ld_dy, C, columns;                               // columns: C up to whole groups of eight
-    int beside_zero;                                          // launches with an embed_zero_kernel just before them: 1: the sums, 2: the joins too
+    int beside_zero;                                          // launches that need not wait for the one before them (embed_zero_kernel; of positions: the sort): 1: the sums, 2: the joins too
     uint32_t threads, lanes, tiles, chunks;                   // threads of a block; side by side over a row's units of columns, blocks side by side, chunks of a block one after the other
     DropArgs drop;
 };

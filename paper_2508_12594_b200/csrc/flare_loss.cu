@@ -119,7 +119,7 @@ int make_plane_map(CUtensorMap *m, const void *base, bool bf16, long cols, long 
         return FLARE_ERR_CUDA;
     }
     cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)planes};
-    cuuint64_t strides[2] = {(cuuint64_t)ld * 2, (cuuint64_t)ld * 2 * (cuuint64_t)rows};
+    cuuint64_t strides[2] = {(cuuint64_t)ld * 2, (cuuint64_t)ld * 2 * (cuuint64_t)(planes > 1 ? rows : 1)};   // (of one plane the distance to the next is never used, but has a limit)
     cuuint32_t box[3] = {64, (cuuint32_t)box_rows, 1}, estr[3] = {1, 1, 1};
     const CUresult r = fn(m, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void *>(base), dims, strides, box, estr,
                           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
@@ -347,7 +347,7 @@ int flare_loss_backward(const flare_loss_desc_t *desc, const void *x, const void
     auto grads = f32 ? launch_loss<kLossGrads, 2, float> : desc->dtype == FLARE_DTYPE_BF16 ? launch_loss<kLossGrads, 1, __nv_bfloat16> : launch_loss<kLossGrads, 1, __half>;
     auto *join = f32 ? loss_join_kernel<float> : desc->dtype == FLARE_DTYPE_BF16 ? loss_join_kernel<__nv_bfloat16> : loss_join_kernel<__half>;
     // of tiles that several pairs can have shared: fewer than a round of either gradient
-    const long warps = 2L * (p.pairs - 1) * 8 * (p.grad_width / 32);
+    const long warps = 2L * (p.pairs - 1) * 8 * (p.grad_width / kJoinCols);
     for (int i = 0; i < p.pieces; ++i) {
         a.v0 = i * p.Vp;
         a.words = std::min(p.Vp, desc->vocab - a.v0);

@@ -444,7 +444,8 @@ struct LossSplit {
     int tiles_w, tiles_x, deep_w, deep_x, full_w, full_x, pairs;
     int whole_w, whole_x;        // tiles of the last rounds that a pair each takes whole: the first pairs those of dW, the next those of dX
     int sharing;                 // pairs behind them that share the others
-    long steps;                  // of the others
+    long steps, each;            // of the others; of a pair's, less what is `over`
+    int over;
     __device__ __forceinline__ LossSplit(const LossArgs &a, int rows, int pairs_) : pairs(pairs_) {
         const int rb = max(1, (rows + 255) / 256);
         tiles_w = a.dw ? (a.words + 255) / 256 * a.tiles_c : 0;
@@ -471,10 +472,12 @@ struct LossSplit {
         better(rest_w, rest_x);
         steps = (whole_w ? 0 : all_w) + (whole_x ? 0 : all_x);
         sharing = (int)max(1L, min((long)(pairs - whole_w - whole_x), steps / 4));   // at least four steps a share
+        each = steps / sharing;
+        over = (int)(steps - each * sharing);
     }
     __device__ __forceinline__ int shared_w() const { return whole_w ? 0 : tiles_w - full_w; }
     __device__ __forceinline__ int shared_x() const { return whole_x ? 0 : tiles_x - full_x; }
-    __device__ __forceinline__ long share(int p) const { return (long)p * steps / sharing; }
+    __device__ __forceinline__ long share(int p) const { return p * each + p * over / sharing; }   // (p steps / sharing, without a 64-bit division)
     // The shared tile that step s is of: its first step, depth and number (tiles of dX behind those of dW).
     __device__ __forceinline__ void tile_of(long s, long &start, int &deep, int &tile) const {
         const long w = (long)shared_w() * deep_w;
@@ -915,32 +918,32 @@ __device__ __forceinline__ void loss_out(uint32_t piece, E *out, long ld, int fo
         }
     }
 }
-// 32 columns of a gradient's tile that are complete, tile-local from col on.
-template <typename E>
+// kCols (16 or 32) columns of a gradient's tile that are complete, tile-local from col on.
+template <int kCols, typename E>
 __device__ __forceinline__ void loss_gradient(uint32_t piece, const LossArgs &a, const LossInfo &info, const LossRow &r, int dx, int i, int j, int block, int quad, int col, float *v) {
     const int lane = threadIdx.x & 31, local = i * 256 + block * 128 + quad * 32 + lane, c0 = j * a.grad_width + col;
     if (c0 >= a.C) return;
     if (!dx) {
         const float f = a.g_factor != 0.f ? a.dw_factor * info.dmax / info.x_scale : 1.f;
 #pragma unroll
-        for (int k = 0; k < 32; k += 16) loss_out<E>(piece, static_cast<E *>(a.dw), a.ld_dw, a.dw_fours, local < a.words ? a.v0 + local : -1, c0 + k, a.C, f, v + k);
+        for (int k = 0; k < kCols; k += 16) loss_out<E>(piece, static_cast<E *>(a.dw), a.ld_dw, a.dw_fours, local < a.words ? a.v0 + local : -1, c0 + k, a.C, f, v + k);
         return;
     }
     if (!a.first || !a.last) {
         float *acc = a.acc + ((((long)i * a.tiles_c + j) * 2 + block) * a.grad_width + col) * 128 + quad * 32 + lane;
         if (!a.first) {
 #pragma unroll
-            for (int e = 0; e < 32; ++e) v[e] += acc[e * 128];
+            for (int e = 0; e < kCols; ++e) v[e] += acc[e * 128];
         }
         if (!a.last) {
 #pragma unroll
-            for (int e = 0; e < 32; ++e) acc[e * 128] = v[e];
+            for (int e = 0; e < kCols; ++e) acc[e * 128] = v[e];
             return;
         }
     }
     const float f = a.g_factor != 0.f ? r.coef / (a.g_factor * info.w_scale) : 1.f;
 #pragma unroll
-    for (int k = 0; k < 32; k += 16) loss_out<E>(piece, static_cast<E *>(a.dx), a.ld_dx, a.dx_fours, r.index, c0 + k, a.C, f, v + k);
+    for (int k = 0; k < kCols; k += 16) loss_out<E>(piece, static_cast<E *>(a.dx), a.ld_dx, a.dx_fours, r.index, c0 + k, a.C, f, v + k);
 }
 
 template <int kKind, int kPlanes, typename E>
@@ -1019,7 +1022,7 @@ __global__ void __launch_bounds__(kLossThreads, 1) loss_kernel(const __grid_cons
                 } else {
 #pragma unroll
                     for (int k = 0; k < 64; k += 32)
-                        if (k < cols) loss_gradient<E>(piece, a, info, r, u.dx, u.i, u.j, in_pair, quad, part * cols + k, v + k);
+                        if (k < cols) loss_gradient<32, E>(piece, a, info, r, u.dx, u.i, u.j, in_pair, quad, part * cols + k, v + k);
                 }
             }
         }
@@ -1041,33 +1044,33 @@ __global__ void __launch_bounds__(kLossThreads, 1) loss_kernel(const __grid_cons
 
 // Tiles whose K several pairs have shared: 32 rows and 32 columns by one warp, or, where many pairs have (a few tiles summed over many rows), by 2, 4 or 8 that take their
 // shares in turn and are added up in order.
-constexpr int kJoinWarps = 8;
+constexpr int kJoinWarps = 8, kJoinCols = 32;
 template <typename E>
-__global__ void __launch_bounds__(32 * kJoinWarps) loss_join_kernel(const LossArgs a, int pairs) {
+__global__ void __launch_bounds__(32 * kJoinWarps, 2) loss_join_kernel(const LossArgs a, int pairs) {
     __shared__ __align__(128) uint8_t pieces[kJoinWarps][4096];
     ptx::grid_launch();
     ptx::grid_wait();
     const LossInfo info = *a.info;
     const LossSplit s(a, (int)info.rows, pairs);
     if (s.steps == 0) return;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, blocks_of_tile = 8 * (a.grad_width / 32);   // (2 blocks, 4 quarters of rows)
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, blocks_of_tile = 8 * (a.grad_width / kJoinCols);   // (2 blocks, 4 quarters of rows)
     const int rest_w = s.shared_w(), rest_all = rest_w + s.shared_x();
-    const long shares = (long)max(s.deep_w, s.deep_x) * s.sharing / s.steps;                                // of a tile, about
+    const long shares = max(s.deep_w, s.deep_x) / max(1L, s.each);                                // of a tile, about
     const int team = shares < 4 ? 1 : shares < 8 ? 2 : shares < 16 ? 4 : 8, member = warp % team;
     const long items = (long)rest_all * blocks_of_tile, step = (long)gridDim.x * (kJoinWarps / team);
     for (long first = (long)blockIdx.x * (kJoinWarps / team); first < items; first += step) {               // (the same for all warps of the block)
         const long at = first + warp / team;
-        const int rest = (int)(at / blocks_of_tile), part = (int)(at % blocks_of_tile), block = part & 1, quad = part >> 1 & 3, col = (part >> 3) * 32;
+        const int rest = (int)at / blocks_of_tile, part = (int)at - rest * blocks_of_tile, block = part & 1, quad = part >> 1 & 3, col = (part >> 3) * kJoinCols;
         const bool dx = rest >= rest_w;
         const long start = dx ? (long)rest_w * s.deep_w + (long)(rest - rest_w) * s.deep_x : (long)rest * s.deep_w, end = start + (dx ? s.deep_x : s.deep_w);
         const int tile = dx ? s.full_x + rest - rest_w : s.full_w + rest;
-        float v[32];
+        float v[kJoinCols];
 #pragma unroll
-        for (int e = 0; e < 32; ++e) v[e] = 0.f;
+        for (int e = 0; e < kJoinCols; ++e) v[e] = 0.f;
         bool shared = false;
         if (at < items) {
             // the first pair whose share reaches into the tile
-            int p = (int)(start * s.sharing / s.steps);
+            int p = min(s.sharing - 1, (int)((float)start * (float)s.sharing / (float)s.steps));
             while (p > 0 && s.share(p) > start) --p;
             while (s.share(p + 1) <= start) ++p;
             shared = s.share(p) > start || s.share(p + 1) < end;                                            // (else it is all one pair's, which has finished it)
@@ -1077,34 +1080,34 @@ __global__ void __launch_bounds__(32 * kJoinWarps) loss_join_kernel(const LossAr
                 const bool two = p1 < s.sharing && s.share(p1) < end;
                 const float *from = a.slots + (((long)(2 * p + (s.share(p) > start ? 0 : 1)) * 2 + block) * a.grad_width + col) * 128 + quad * 32 + lane;
                 const float *from1 = a.slots + (((long)(2 * p1 + (s.share(p1) > start ? 0 : 1)) * 2 + block) * a.grad_width + col) * 128 + quad * 32 + lane;
-                float t[32], t1[32];
+                float t[kJoinCols], t1[kJoinCols];
 #pragma unroll
-                for (int e = 0; e < 32; ++e) t[e] = from[e * 128];
+                for (int e = 0; e < kJoinCols; ++e) t[e] = from[e * 128];
                 if (two) {
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) t1[e] = from1[e * 128];
+                    for (int e = 0; e < kJoinCols; ++e) t1[e] = from1[e * 128];
                 }
 #pragma unroll
-                for (int e = 0; e < 32; ++e) v[e] += t[e];
+                for (int e = 0; e < kJoinCols; ++e) v[e] += t[e];
                 if (two) {
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) v[e] += t1[e];
+                    for (int e = 0; e < kJoinCols; ++e) v[e] += t1[e];
                 }
             }
         }
         if (team > 1) {
             float *own = reinterpret_cast<float *>(pieces[warp]);
 #pragma unroll
-            for (int e = 0; e < 32; ++e) own[e * 32 + lane] = v[e];
+            for (int e = 0; e < kJoinCols; ++e) own[e * 32 + lane] = v[e];
             __syncthreads();
             if (member == 0)
                 for (int m = 1; m < team; ++m)
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) v[e] += reinterpret_cast<const float *>(pieces[warp + m])[e * 32 + lane];
+                    for (int e = 0; e < kJoinCols; ++e) v[e] += reinterpret_cast<const float *>(pieces[warp + m])[e * 32 + lane];
             __syncthreads();
         }
         if (member == 0 && shared)
-            loss_gradient<E>(ptx::smem_u32(pieces[warp]), a, info, loss_row<kLossGrads>(a, (int)info.rows, tile / a.tiles_c * 256 + block * 128 + quad * 32 + lane, dx), dx, tile / a.tiles_c, tile % a.tiles_c, block, quad, col, v);
+            loss_gradient<kJoinCols, E>(ptx::smem_u32(pieces[warp]), a, info, loss_row<kLossGrads>(a, (int)info.rows, tile / a.tiles_c * 256 + block * 128 + quad * 32 + lane, dx), dx, tile / a.tiles_c, tile % a.tiles_c, block, quad, col, v);
     }
 }
 

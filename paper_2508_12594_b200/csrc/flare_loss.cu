@@ -206,10 +206,10 @@ int prepare_loss(const flare_loss_desc_t *d, const LossPlan &p, const LossLayout
     s.largest = reinterpret_cast<float *>(ws + l.largest);
     s.status = reinterpret_cast<uint32_t *>(ws);
     int rc;
-    // rows of a block: what keeps four blocks an SM at work in one round, whole parts of a chunk
-    k.pack_rows = 64;
-    while (k.pack_rows < kLossChunk && (long)k.pack_rows * 4 * device_info().sms < d->rows) k.pack_rows *= 2;
-    const bool alone = d->rows <= kPackAlone && p.to == kAsIs && k.pack_rows == 64;
+    // rows of a block: so many that a thread has four groups of columns, and that there are no more than four blocks an SM; whole parts of a chunk
+    k.pack_rows = 4;
+    while (k.pack_rows < kLossChunk && ((long)k.pack_rows * (p.Cp / 8) < 4 * kPackThreads || (long)k.pack_rows * 4 * device_info().sms < d->rows)) k.pack_rows *= 2;
+    const bool alone = d->rows <= kPackAlone && p.to == kAsIs && k.pack_rows <= kPackThreads;
     if (!alone && (rc = f32 ? launch_scan<float>(s, st) : d->dtype == FLARE_DTYPE_BF16 ? launch_scan<__nv_bfloat16>(s, st) : launch_scan<__half>(s, st)) != FLARE_OK) return rc;
     k.labels = labels; k.x = x; k.w = w; k.wide = s.wide; k.rows = d->rows; k.cap = p.cap; k.ld_x = ld_x; k.ld_w = ld_w;
     k.w_rows = own_w ? d->vocab : 0; k.C = d->width; k.Cp = p.Cp; k.V = d->vocab; k.chunks = p.chunks; k.x_blocks = p.x_blocks; k.w_blocks = p.w_blocks;
@@ -337,8 +337,8 @@ int flare_loss_backward(const flare_loss_desc_t *desc, const void *x, const void
     a.g = reinterpret_cast<uint16_t *>(ws + l.g); a.ld_g = p.Vp;
     a.lse2 = k.lse2; a.coef = k.coef; a.grad_width = p.grad_width; a.tiles_c = p.tiles_c;
     a.dw = dw; a.dx = dx; a.ld_dw = ld_dw; a.ld_dx = ld_dx;
-    auto fours = [&](const void *q, long ld) { return desc->width % 4 == 0 && ld % 4 == 0 && reinterpret_cast<uintptr_t>(q) % (4 * t) == 0; };
-    a.dw_fours = fours(dw, ld_dw); a.dx_fours = fours(dx, ld_dx);
+    auto vec = [&](const void *q, long ld) { return desc->width * t % 16 == 0 && ld * t % 16 == 0 && aligned16(q); };
+    a.dw_vec = vec(dw, ld_dw); a.dx_vec = vec(dx, ld_dx);
     // bfloat16's G: q where one dloss is that of all rows (a label's q is next to -1, which is no rounding), else times it; float16's: q times 2^15, dloss goes into X
     a.g_factor = !bf16 ? 32768.f : dloss ? 0.f : 1.f;
     a.dw_factor = a.g_factor != 0.f ? k.mult / a.g_factor : 0.f;

@@ -192,7 +192,7 @@ struct LossPack {
     void *dx;                                 // rows without a label: zeros
     long ld_dx;
 };
-constexpr int kPackThreads = 256;             // of a block, which takes 64 to 1024 rows (of one chunk)
+constexpr int kPackThreads = 256;             // of a block, which takes 4 to 1024 rows (of one chunk)
 constexpr int kPackAlone = 4096;              // rows up to which every block finds for itself, in all labels, what the scan would tell it, where no maxima are wanted: a launch less
 
 // The power of two that puts `most` between 2^14 and 2^15.
@@ -303,7 +303,7 @@ __global__ void __launch_bounds__(kPackThreads) loss_pack_kernel(const LossPack 
     if (!a.dloss || !(dmax > 0.f)) dmax = 1.f;
     if (blockIdx.x == 0 && threadIdx.x == 0) *a.info = LossInfo{total, sx, sw, dmax};
     const int rows = (int)min((long)a.pack_rows, a.rows - n0);
-    if (alone) {                                              // (64 rows: by the first two warps)
+    if (alone) {                                              // (up to a row a thread)
         __syncthreads();                                      // (sums have been read)
         int64_t label = -1;
         if ((int)threadIdx.x < rows) label = label_at(a.labels, a.wide, n0 + threadIdx.x);
@@ -311,8 +311,9 @@ __global__ void __launch_bounds__(kPackThreads) loss_pack_kernel(const LossPack 
         const uint32_t m = __ballot_sync(0xffffffffu, there);
         if (lane == 0) sums[0][warp] = __popc(m);
         __syncthreads();
-        if (warp == 1) base += sums[0][0];
-        to_row[threadIdx.x] = there ? __popc(m & ((1u << lane) - 1)) : -1;
+        int before = 0;
+        for (int w = 0; w < warp; ++w) before += (int)sums[0][w];
+        to_row[threadIdx.x] = there ? before + __popc(m & ((1u << lane) - 1)) : -1;
     }
     for (int i = threadIdx.x; i < rows; i += kPackThreads) {
         const long n = n0 + i;
@@ -430,7 +431,7 @@ struct LossArgs {
     int first, last;             // of the pieces
     void *dw, *dx;
     long ld_dw, ld_dx;
-    int dw_fours, dx_fours;      // rows can be written four columns at a time
+    int dw_vec, dx_vec;          // rows can be written 16 bytes at a time
     float dw_factor;             // scale dloss_scale / g_factor (times dmax / x_scale)
     float *acc;                  // dX over the pieces before, by tile: [2 blocks][grad_width columns][128 rows]
     float *slots;                // sums of parts of tiles, likewise, two per pair
@@ -887,63 +888,76 @@ __device__ __forceinline__ void loss_weights(uint32_t piece, const LossArgs &a, 
     }
 }
 
-// 32 rows (a row a lane, to go to row `to` of the output; -1: nowhere) of 16 columns from c0 on, times f, by way of shared memory, so that four lanes write a row's 16 columns.
+// 32 rows (a row a lane, to go to row `to` of the output; -1: nowhere) of 32 columns from c0 on, times f, by way of shared memory: rows on 16-byte boundaries by four lanes, 64 bytes a row and instruction (32 took
+// twice the time, which bounds gradients with few steps a tile: 18935 rows of 1536 over six words); others by lanes with neighbouring columns, a row at a time.
 template <typename E>
-__device__ __forceinline__ void loss_out(uint32_t piece, E *out, long ld, int fours, int to, int c0, int C, float f, const float *v) {
+__device__ __forceinline__ void loss_out(uint32_t piece, E *out, long ld, int vec, int to, int c0, int C, float f, const float *v) {
     const int lane = threadIdx.x & 31;
-    __syncwarp();
+    constexpr int kStep = 64 / (int)sizeof(E), kLane = 16 / (int)sizeof(E);      // columns of a piece, of 16 bytes
 #pragma unroll
-    for (int g = 0; g < 4; ++g) {
-        const uint32_t r[4] = {__float_as_uint(v[4 * g] * f), __float_as_uint(v[4 * g + 1] * f), __float_as_uint(v[4 * g + 2] * f), __float_as_uint(v[4 * g + 3] * f)};
-        ptx::sts128(piece + piece_at(lane, g), r);
-    }
-    __syncwarp();
-    const int c = c0 + 4 * (lane & 3);
+    for (int k = 0; k < 32; k += kStep) {
+        __syncwarp();
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        const int r = 8 * k + (lane >> 2);
-        const int t = __shfl_sync(0xffffffffu, to, r);
-        const float4 x = ptx::lds128(piece + piece_at(r, lane & 3));
-        if (t < 0 || c >= C) continue;
-        E *p = out + (long)t * ld + c;
-        __align__(16) E e[4];
-        from_f32(e[0], x.x); from_f32(e[1], x.y); from_f32(e[2], x.z); from_f32(e[3], x.w);
-        if (fours) {
-            if constexpr (sizeof(E) == 4) *reinterpret_cast<float4 *>(p) = *reinterpret_cast<const float4 *>(e);
-            else *reinterpret_cast<uint2 *>(p) = *reinterpret_cast<const uint2 *>(e);
+        for (int g = 0; g < 4; ++g) {
+            __align__(16) E e[kLane];
+#pragma unroll
+            for (int i = 0; i < kLane; ++i) from_f32(e[i], v[k + kLane * g + i] * f);
+            ptx::sts128(piece + piece_at(lane, g), reinterpret_cast<const uint32_t *>(e));
+        }
+        __syncwarp();
+        if (vec) {
+            const int c = c0 + k + kLane * (lane & 3);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int r = 8 * e + (lane >> 2), t = __shfl_sync(0xffffffffu, to, r);
+                const float4 x = ptx::lds128(piece + piece_at(r, lane & 3));
+                if (t >= 0 && c < C) *reinterpret_cast<float4 *>(out + (long)t * ld + c) = x;
+            }
         } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (c + i < C) p[i] = e[i];
+            const int col = lane % kStep, c = c0 + k + col;
+            const uint32_t from = (col % kLane) * (uint32_t)sizeof(E);
+#pragma unroll 8
+            for (int r0 = 0; r0 < 32; r0 += 32 / kStep) {
+                const int r = r0 + lane / kStep, t = __shfl_sync(0xffffffffu, to, r);
+                const uint32_t at = piece + piece_at(r, col / kLane) + from;
+                if (t < 0 || c >= C) continue;
+                if constexpr (sizeof(E) == 4) {
+                    uint32_t x;
+                    asm volatile("ld.shared.b32 %0, [%1];" : "=r"(x) : "r"(at) : "memory");
+                    reinterpret_cast<uint32_t *>(out)[(long)t * ld + c] = x;
+                } else {
+                    uint16_t x;
+                    asm volatile("ld.shared.b16 %0, [%1];" : "=h"(x) : "r"(at) : "memory");
+                    reinterpret_cast<uint16_t *>(out)[(long)t * ld + c] = x;
+                }
+            }
         }
     }
 }
-// kCols (16 or 32) columns of a gradient's tile that are complete, tile-local from col on.
-template <int kCols, typename E>
+// 32 columns of a gradient's tile that are complete, tile-local from col on.
+template <typename E>
 __device__ __forceinline__ void loss_gradient(uint32_t piece, const LossArgs &a, const LossInfo &info, const LossRow &r, int dx, int i, int j, int block, int quad, int col, float *v) {
     const int lane = threadIdx.x & 31, local = i * 256 + block * 128 + quad * 32 + lane, c0 = j * a.grad_width + col;
     if (c0 >= a.C) return;
     if (!dx) {
         const float f = a.g_factor != 0.f ? a.dw_factor * info.dmax / info.x_scale : 1.f;
-#pragma unroll
-        for (int k = 0; k < kCols; k += 16) loss_out<E>(piece, static_cast<E *>(a.dw), a.ld_dw, a.dw_fours, local < a.words ? a.v0 + local : -1, c0 + k, a.C, f, v + k);
+        loss_out<E>(piece, static_cast<E *>(a.dw), a.ld_dw, a.dw_vec, local < a.words ? a.v0 + local : -1, c0, a.C, f, v);
         return;
     }
     if (!a.first || !a.last) {
         float *acc = a.acc + ((((long)i * a.tiles_c + j) * 2 + block) * a.grad_width + col) * 128 + quad * 32 + lane;
         if (!a.first) {
 #pragma unroll
-            for (int e = 0; e < kCols; ++e) v[e] += acc[e * 128];
+            for (int e = 0; e < 32; ++e) v[e] += acc[e * 128];
         }
         if (!a.last) {
 #pragma unroll
-            for (int e = 0; e < kCols; ++e) acc[e * 128] = v[e];
+            for (int e = 0; e < 32; ++e) acc[e * 128] = v[e];
             return;
         }
     }
     const float f = a.g_factor != 0.f ? r.coef / (a.g_factor * info.w_scale) : 1.f;
-#pragma unroll
-    for (int k = 0; k < kCols; k += 16) loss_out<E>(piece, static_cast<E *>(a.dx), a.ld_dx, a.dx_fours, r.index, c0 + k, a.C, f, v + k);
+    loss_out<E>(piece, static_cast<E *>(a.dx), a.ld_dx, a.dx_vec, r.index, c0, a.C, f, v);
 }
 
 template <int kKind, int kPlanes, typename E>
@@ -1022,7 +1036,7 @@ __global__ void __launch_bounds__(kLossThreads, 1) loss_kernel(const __grid_cons
                 } else {
 #pragma unroll
                     for (int k = 0; k < 64; k += 32)
-                        if (k < cols) loss_gradient<32, E>(piece, a, info, r, u.dx, u.i, u.j, in_pair, quad, part * cols + k, v + k);
+                        if (k < cols) loss_gradient<E>(piece, a, info, r, u.dx, u.i, u.j, in_pair, quad, part * cols + k, v + k);
                 }
             }
         }
@@ -1107,7 +1121,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps, 2) loss_join_kernel(const Los
             __syncthreads();
         }
         if (member == 0 && shared)
-            loss_gradient<kJoinCols, E>(ptx::smem_u32(pieces[warp]), a, info, loss_row<kLossGrads>(a, (int)info.rows, tile / a.tiles_c * 256 + block * 128 + quad * 32 + lane, dx), dx, tile / a.tiles_c, tile % a.tiles_c, block, quad, col, v);
+            loss_gradient<E>(ptx::smem_u32(pieces[warp]), a, info, loss_row<kLossGrads>(a, (int)info.rows, tile / a.tiles_c * 256 + block * 128 + quad * 32 + lane, dx), dx, tile / a.tiles_c, tile % a.tiles_c, block, quad, col, v);
     }
 }
 

@@ -513,10 +513,13 @@ template <> struct LossUnits<kLossTurns> : LossTiles<kLossTurns> { using LossTil
 template <> struct LossUnits<kLossWeights> : LossTiles<kLossWeights> { using LossTiles::LossTiles; };
 template <> struct LossUnits<kLossGrads> {
     LossSplit s;
-    int pair, tiles_c, t;
+    int pair, tiles_c, t, dx;    // next tile of the full rounds, of which gradient (2: none)
+    int i, j, i0, j0, di, dj;    // where it is, where the pair's first one is, from one round's to the next's
     bool rest;                   // the pair's whole tile of the last rounds is still to come
     long at, end;
-    __device__ __forceinline__ LossUnits(const LossArgs &a, int rows, int pair_, int pairs) : s(a, rows, pairs), pair(pair_), tiles_c(a.tiles_c), t(pair_) {
+    __device__ __forceinline__ LossUnits(const LossArgs &a, int rows, int pair_, int pairs) : s(a, rows, pairs), pair(pair_), tiles_c(a.tiles_c), t(pair_), dx(0) {
+        i = i0 = pair / tiles_c; j = j0 = pair % tiles_c;
+        di = pairs / tiles_c; dj = pairs % tiles_c;
         const int me = pair - s.whole_w - s.whole_x;          // among those that share
         rest = me < 0;
         at = end = 0;
@@ -524,11 +527,13 @@ template <> struct LossUnits<kLossGrads> {
     }
     __device__ __forceinline__ LossUnit whole(int dx, int tile) const { return LossUnit{dx, tile / tiles_c, tile % tiles_c, 0, dx ? s.deep_x : s.deep_w, -1}; }
     __device__ __forceinline__ bool next(LossUnit &u) {
-        const int rounds_w = (s.full_w + s.pairs - 1) / s.pairs * s.pairs;
-        if (t < rounds_w && t >= s.full_w) t += s.pairs;                          // (no tile for this pair in the last round)
-        if (t < s.full_w || t - rounds_w < s.full_x) {
-            u = t < s.full_w ? whole(0, t) : whole(1, t - rounds_w);
+        if (dx == 0 && t >= s.full_w) { dx = 1; t = pair; i = i0; j = j0; }
+        if (dx == 1 && t >= s.full_x) dx = 2;
+        if (dx < 2) {
+            u = LossUnit{dx, i, j, 0, dx ? s.deep_x : s.deep_w, -1};
             t += s.pairs;
+            i += di; j += dj;
+            if (j >= tiles_c) { j -= tiles_c; ++i; }
             return true;
         }
         if (rest) {
@@ -540,10 +545,10 @@ template <> struct LossUnits<kLossGrads> {
         long start;
         int deep, tile;
         s.tile_of(at, start, deep, tile);
-        const bool dx = tile >= s.tiles_w;
-        if (dx) tile -= s.tiles_w;
+        const bool of_x = tile >= s.tiles_w;
+        if (of_x) tile -= s.tiles_w;
         const int kb0 = (int)(at - start), kb1 = (int)min((long)deep, end - start);
-        u = LossUnit{dx, tile / tiles_c, tile % tiles_c, kb0, kb1, kb0 == 0 && kb1 == deep ? -1 : 2 * (pair - s.whole_w - s.whole_x) + (kb0 > 0 ? 0 : 1)};
+        u = LossUnit{of_x, tile / tiles_c, tile % tiles_c, kb0, kb1, kb0 == 0 && kb1 == deep ? -1 : 2 * (pair - s.whole_w - s.whole_x) + (kb0 > 0 ? 0 : 1)};
         at = start + kb1;
         return true;
     }

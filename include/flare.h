@@ -420,8 +420,8 @@ int flare_embed_backward(const flare_embed_desc_t *desc, const flare_drop_t *dro
  * Softmax cross entropy over a vocabulary, l[n, v] = scale x[n] . w[v]:
  *     lse[n] = log sum_v exp l[n, v];   loss[n] = lse[n] - l[n, labels[n]]
  *     dx[n] = g_n scale sum_v (p[n, v] - [v = labels[n]]) w[v];   dw[v] = scale sum_n g_n (p[n, v] - [v = labels[n]]) x[n];   p = exp(l - lse), g_n = dloss_scale dloss[n]
- * The logits are never kept: forward they stay on the chip, backward they are formed again, a piece of the vocabulary at a time (scratch of 256 MB, or 512 bytes a row where that is
- * more).  A row whose label is outside [0, vocab) takes no part: loss, lse and dx are 0, and what x holds there is not looked at.
+ * The logits are never kept: forward they stay on the chip, backward they are formed again, a piece of the vocabulary at a time (scratch of 512 MB at most, or of 512 bytes a row,
+ * 1024 for float32, where that is more).  A row whose label is outside [0, vocab) takes no part: loss, lse and dx are 0, and what x holds there is not looked at.
  * x, dx [rows, width], w, dw [vocab, width] of dtype, rows stride_* apart; labels [rows] of label_bits (32 or 64); loss, lse, dloss [rows] float32 (dloss NULL: ones); dx or dw may
  * be NULL if not wanted.  Products run on the tensor cores with float32 sums: 16-bit types as they are, p in the same type (rounded once); float32 in two float16 halves (22 bits; x and w are held
  * down to 2^-39 of their largest element).  A wait inside the kernels that gave up is reported by flare_check(workspace).

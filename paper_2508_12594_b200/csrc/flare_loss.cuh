@@ -441,6 +441,8 @@ struct LossArgs {
 // them are dealt out a tile a pair, so that pairs side by side read the same columns of G at the same time.  Of the rounds that would not be full, either's tiles go to a pair each or are cut along K: the pairs
 // that have none whole take equal shares of their steps, and what is less than a tile goes to a slot of the pair's, to be joined.  Which, by the longest pair's steps, where joining counts as 12 (of one gradient)
 // or 24 of them: 1999 rows of 200 over 10007 words, 40 tiles of 29 steps and 8 of 157, took 18 us to join with all 48 shared.
+// Equal shares begin anywhere along K, so that no two pairs read the same lines of G and W at a time: of a G of half a gigabyte a step then takes half as long again (4096 rows over 64000 words of 1024, the tiles
+// of dX shared: 885 us and 4.4 GB read; a pair each, on 64 of 74 pairs: 740 us).
 struct LossSplit {
     int tiles_w, tiles_x, deep_w, deep_x, full_w, full_x, pairs;
     int whole_w, whole_x;        // tiles of the last rounds that a pair each takes whole: the first pairs those of dW, the next those of dX
@@ -460,12 +462,14 @@ struct LossSplit {
         const int rest_w = tiles_w - full_w, rest_x = tiles_x - full_x;
         const long all_w = (long)rest_w * deep_w, all_x = (long)rest_x * deep_x;
         whole_w = whole_x = 0;
-        long best = (all_w + all_x) / pairs + 24;
+        const float far = 1.f + fminf(0.5f, (float)rows * (float)a.words * 0x1p-29f);
+        auto equal = [&](long steps, int left) { return (long)((float)(steps / left) * far); };      // how long a share takes
+        long best = equal(all_w + all_x, pairs) + 24;
         auto better = [&](int w, int x) {                     // these whole
             const int left = pairs - w - x;
             const long shared = (w ? 0 : all_w) + (x ? 0 : all_x);
             if (left < 0 || (left == 0 && shared > 0)) return;
-            const long cost = max(max(w ? (long)deep_w : 0L, x ? (long)deep_x : 0L), shared > 0 ? shared / left + 12 : 0L);
+            const long cost = max(max(w ? (long)deep_w : 0L, x ? (long)deep_x : 0L), shared > 0 ? equal(shared, left) + 12 : 0L);
             if (cost < best) { best = cost; whole_w = w; whole_x = x; }
         };
         better(rest_w, 0);

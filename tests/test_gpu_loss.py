@@ -199,7 +199,8 @@ def test_tiny_and_huge_float32():
     (600, 50021, 256, F16),                                   # the same of dX
     (2500, 12000, 1000, F16),
     (1500, 6000, 384, F32),
-    (70000, 5000, 64, BF16),                                  # three pieces of the vocabulary
+    (70000, 5000, 64, BF16),                                  # two pieces of the vocabulary
+    (70000, 8000, 32, F16),                                   # three
     (40000, 3400, 72, F32),
     (130, 70, 4104, BF16), (130, 300, 2056, F32)])
 def test_larger(rows, vocab, width, dtype):

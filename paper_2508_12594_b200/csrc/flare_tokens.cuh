@@ -213,7 +213,7 @@ __global__ void __launch_bounds__(kTokenThreads) dropout_kernel(const DropoutArg
 
 // Contiguous rows whose width eight does not divide: moved 16 bytes at a time all the same, as one long row.  A block has rows that begin on an eighth element (a multiple of eight of them),
 // forms their bits, a call of the generator a group of a row's columns, and lays them in shared memory bit by bit, where eight elements find theirs as one byte.  40028 x 333 in float16
-// (53 MB): 28 us with neighbouring lanes on neighbouring columns, above.
+// (53 MB): 28 us with neighbouring lanes on neighbouring columns, above; 18.1 (2.9 TB/s) this way, bound by instructions.
 struct DropoutFlat {
     DropoutArgs a;
     uint32_t tile_rows;
@@ -300,7 +300,7 @@ __device__ __forceinline__ uint32_t token_at(const void *tokens, int wide, uint3
     const uint2 t = static_cast<const uint2 *>(tokens)[n];
     return t.y == 0 && t.x < vocab ? t.x : ~0u;
 }
-// T: type of the tables, O: of the rows.  kWidth: groups of eight columns next to each other that a thread takes (two share a row's token and addresses: 260 instructions a group became 150), 0: rows
+// T: type of the tables, O: of the rows.  kWidth: groups of eight columns next to each other that a thread takes (two share a row's token and addresses: 260 instructions a group became 189 with positions and dropout, which is what bounds it: 131072 rows of 128 over 256 words take 17.3 us, 3.1 TB/s of rows read and written), 0: rows
 // off 16-byte boundaries.
 template <typename T, typename O, int kWidth>
 __global__ void __launch_bounds__(kTokenThreads, kWidth == 2 && sizeof(T) + sizeof(O) > 4 ? 3 : 4) embed_kernel(const EmbedArgs a) {
@@ -557,7 +557,7 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(const SortArgs
 
 // Rows of the gradient that no token has met: zeros.  A lane looks one row up among the sorted tokens, a warp writes what 32 of them want.  The launch behind it (the sums; of a large table half is left to be
 // done beside the joins) need not wait for this, only for the one before it, which has ended when every block here has got past its wait, and runs beside it; its last block then waits, so that what comes
-// behind both comes behind this too.  16396 tokens over 50021 rows of 1000, whose 200 MB take 29 us on their own: 87 us one after the other, 83 with all of it beside the sums.
+// behind both comes behind this too.  16396 tokens over 50021 rows of 1000, whose 200 MB take 29 us on their own: 87 us one after the other, 83 with all of it beside the sums, 73 to 78 so.
 constexpr int kZeroThreads = 128;
 struct ZeroArgs {
     const uint2 *pairs;
@@ -675,10 +675,12 @@ __device__ __forceinline__ void add8(float (&v)[8], const float *from) {
     v[4] += y.x; v[5] += y.y; v[6] += y.z; v[7] += y.w;
 }
 enum { kRunOpen = 1, kRunGoesOn = 2, kRunThrough = 4 };       // a chunk's first run began before it; its last one goes on behind it; the two are the same and all of it
-// Blocks of 64 threads where a row takes few of them, of up to 256 where it takes more.  (32 x 4096 rows of 128, both gradients: 39 us with 256, too few of which were at work towards the end, 30 with 64.)
+// Blocks of 128 threads where a row takes up to 16 of them, so that no SM waits for the last of few large ones, else of 256, where a block joins more chunks by itself (65536 rows of 256 over 32000 words: 84 us with
+// blocks of 64, 80 with 128 or 256; of 512: 92, 78, 74).  Chunks are 16 rows, longer where there is more to do: 16384 rows of 4096 take 186 us in chunks of 16, 144 of 64; 65536 of 512 over 256 words take 61 of 16
+// (and 64 threads), 47 of 32; 131072 of 128 over 32000 take 65.6 of 16, 79.5 of 32.  It is bound by instructions: 32 x 4096 rows of 128 over 256 words with positions take 41 us in all, 17 of them the sort.
 constexpr int kSumThreads = 256;
 __host__ __device__ constexpr size_t sum_smem(uint32_t threads, int width) { return threads * (size_t)(2 * 32 * width + 8); }
-// kWidth: groups of eight columns next to each other that a thread adds up (two share what there is to know of a row: 167 instructions a group and row became 120), 0: one, off 16-byte boundaries.
+// kWidth: groups of eight columns next to each other that a thread adds up (two share what there is to know of a row: 167 instructions a group and row became 108; of 1024 columns 50.5 us against 54.7 for 16384 rows, but of 128 columns 72 against 64 for 131072: rows need 32 such threads), 0: one, off 16-byte boundaries.
 template <typename O, typename T, int kWidth>
 __global__ void __launch_bounds__(kSumThreads, sizeof(O) == 4 || kWidth == 2 ? 2 : 3) embed_sum_kernel(const SumArgs a) {
     constexpr int kW = kWidth == 2 ? 2 : 1;

@@ -380,7 +380,7 @@ typedef struct {
     uint64_t seed, offset;
     const int64_t *step;
 } flare_drop_t;
-/* y = drop(x) + residual (NULL: none); tensors of rows as around a block.  y may be x (with residual_dtype = dtype) or residual, with the same strides. */
+/* y = drop(x) + residual (NULL: none); tensors of rows as around a block, strides up to 2^31 - 1.  y may be x (with residual_dtype = dtype) or residual, with the same strides. */
 typedef struct {
     int64_t rows;           /* 0 is allowed */
     int32_t width;
@@ -396,7 +396,7 @@ int flare_dropout_backward(const flare_dropout_desc_t *desc, const flare_drop_t 
  * Embedding: y[n] = drop(scale table[tokens[n]] + position_table[n mod positions]).  A token outside [0, vocab) has no row: zeros in its place, and no gradient.
  * tokens [rows] of token_bits (32 or 64); table [vocab, width] of dtype, rows stride_table apart; position_table [positions, width] of dtype, contiguous
  * (positions = 0: none; else a divisor of rows); y, dy of out_dtype, rows stride_out apart.  dtype and out_dtype are the same, or one of them is float32.
- * drop may be NULL.
+ * drop may be NULL.  Up to 2^31 - 1 rows and elements between rows, widths up to 2^20.
  */
 typedef struct {
     int64_t rows;           /* 0 is allowed */
@@ -423,8 +423,9 @@ int flare_embed_backward(const flare_embed_desc_t *desc, const flare_drop_t *dro
  * The logits are never kept: forward they stay on the chip, backward they are formed again, a piece of the vocabulary at a time (scratch of 512 MB at most, or of 512 bytes a row,
  * 1024 for float32, where that is more).  A row whose label is outside [0, vocab) takes no part: loss, lse and dx are 0, and what x holds there is not looked at.
  * x, dx [rows, width], w, dw [vocab, width] of dtype, rows stride_* apart; labels [rows] of label_bits (32 or 64); loss, lse, dloss [rows] float32 (dloss NULL: ones); dx or dw may
- * be NULL if not wanted.  Products run on the tensor cores with float32 sums: 16-bit types as they are, p in the same type (rounded once); float32 in two float16 halves (22 bits; x and w are held
- * down to 2^-39 of their largest element).  A wait inside the kernels that gave up is reported by flare_check(workspace).
+ * be NULL if not wanted.  Products run on the tensor cores with float32 sums.  float16: x and w as they are, p - [v = labels[n]] rounded to float16 times 2^15, and so is x dloss for dw.
+ * bfloat16: x and w as they are, p - [v = labels[n]] (times dloss[n], if given) rounded to bfloat16; in the backward of a vocabulary with vocab x width up to 2^22 instead in float16 like the above, x and w held
+ * down to 2^-39 of their largest element.  float32: two float16 halves each (22 bits), held likewise.  A wait inside the kernels that gave up is reported by flare_check(workspace).
  */
 typedef struct {
     int64_t rows;           /* 0 is allowed */

@@ -261,8 +261,9 @@ int flare_loss_forward(const flare_loss_desc_t *desc, const void *x, const void 
     const LossLayout l = loss_layout(desc, p, false);
     char *ws = static_cast<char *>(workspace);
     const long ld_x = desc->stride_x ? desc->stride_x : desc->width, ld_w = desc->stride_w ? desc->stride_w : desc->width;
-    // X and W as they stand, without packing, where all rows are one tile's: 64 rows over 32000 words of 1024 take 20.3 us, packed 24.4
-    const bool direct = desc->rows <= 256 && p.planes == 1 && aligned16(x) && aligned16(w) && ld_x % 8 == 0 && ld_w % 8 == 0;
+    // X and W as they stand, without packing, where all rows are one tile's (64 rows over 32000 words of 1024 take 20.3 us, packed 24.4) or the vocabulary is so small that rows without a label cost less than
+    // another pass over X: with 0.3 of them, 20000 rows over 1000 words of 512 24.0 us, packed 31.5; 40000 over 2025 of 64 46.4 and 43.3 (all labelled: 40.0 and 46.4)
+    const bool direct = (desc->rows <= 256 || desc->vocab <= 2048) && p.planes == 1 && aligned16(x) && aligned16(w) && ld_x % 8 == 0 && ld_w % 8 == 0;
     // (five to eight rows that need no packing are done sooner by the tensor cores: 8 rows over 32000 words of 1024 in bfloat16 in 26 us instead of 32.6, where four take 23.2 and 22.0, one 26.4 and 16.6; of 1001,
     // which are packed, eight take 54 and 36.5; in float32, of 2048, 220 and 72)
     const int R = direct && desc->rows > 4 ? 0 : few_rows(desc);

@@ -11,15 +11,19 @@
 // Rows without a label are left out, not multiplied by zero: the rows that have one are packed, in their order, before anything else (loss_scan_kernel,
 // loss_pack_kernel), their number stays on the device, and all products run over packed rows.  So a padded batch takes the time of its labelled rows, and
 // nothing that stands in the others can reach a gradient.  The pass costs two bytes in and out per element of X, and leaves rows that TMA can take whatever stride and alignment X has.
+// (Up to 256 rows that lie well are scored as they stand.)
 //
 // Every product is the same kernel (loss_kernel): pairs of blocks, tiles of 256 x 256 (or 256 x 128), operands by TMA, sums in tensor memory twice over so
 // that a tile's end runs under the next tile's products.  It is bound by the tensor pipe.
 //
-// bfloat16 and float16 are multiplied as they are, G in the same type: bfloat16's holds dloss scale q (rounded once, 2^-9, as the gradients themselves will be); float16's
-// q times 2^15, so that probabilities down to 2^-29 are normal numbers, and dloss goes into X (scaled so that the largest is one) and into dX's rows.
+// bfloat16 and float16 are multiplied as they are, G in the same type, rounded once.  bfloat16's G is q where one dloss is that of all rows (next to a label q is next to -1, which is no rounding), else dloss scale q
+// (2^-9, as the gradients themselves will be; dloss in a second X instead put the same rounding there, and as many more elements were moved).  float16's G is q times 2^15, so that probabilities down to 2^-29 are
+// normal numbers, and dloss goes into X (scaled so that the largest is one) and into dX's rows.  Small vocabularies in bfloat16 take float16's way backward, X and W times powers of two.
 // float32: X, W, G as two float16 halves each (22 bits; X and W times a power of two that puts their largest near 2^15, held down to 2^-39 of it), a
 // product as three, and sums leave tensor memory, which truncates, every 256 of K to be added up in registers.
 #pragma once
+
+#include <type_traits>
 
 #include "flare_common.cuh"
 #include "flare_ptx.cuh"
@@ -442,7 +446,8 @@ struct LossArgs {
 // that have none whole take equal shares of their steps, and what is less than a tile goes to a slot of the pair's, to be joined.  Which, by the longest pair's steps, where joining counts as 12 (of one gradient)
 // or 24 of them: 1999 rows of 200 over 10007 words, 40 tiles of 29 steps and 8 of 157, took 18 us to join with all 48 shared.
 // Equal shares begin anywhere along K, so that no two pairs read the same lines of G and W at a time: of a G of half a gigabyte a step then takes half as long again (4096 rows over 64000 words of 1024, the tiles
-// of dX shared: 885 us and 4.4 GB read; a pair each, on 64 of 74 pairs: 740 us).
+// of dX shared: 885 us and 4.4 GB read; a pair each, on 64 of 74 pairs: 740 us).  Shares of tiles of few steps
+// have many ends (17 rows over 67126 words of 83, forward and backward: 14 tiles of dW for each of three pairs, 156 us; a pair each 84).
 struct LossSplit {
     int tiles_w, tiles_x, deep_w, deep_x, full_w, full_x, pairs;
     int whole_w, whole_x;        // tiles of the last rounds that a pair each takes whole: the first pairs those of dW, the next those of dX
@@ -463,13 +468,14 @@ struct LossSplit {
         const long all_w = (long)rest_w * deep_w, all_x = (long)rest_x * deep_x;
         whole_w = whole_x = 0;
         const float far = 1.f + fminf(0.5f, (float)rows * (float)a.words * 0x1p-29f);
-        auto equal = [&](long steps, int left) { return (long)((float)(steps / left) * far); };      // how long a share takes
-        long best = equal(all_w + all_x, pairs) + 24;
+        // how long a share takes: its steps, but four for a tile of fewer (its end runs under the next one's steps).  (Every kernel has to come to the same: nothing here may be fused in one and not in another.)
+        auto equal = [&](long steps, int left, int deep) { return __fmul_rn(__fdividef((float)steps, (float)left), far + (deep == 1 ? 3.f : deep == 2 ? 1.f : deep == 3 ? 0.333f : 0.f)); };
+        float best = __fadd_rn(equal(all_w + all_x, pairs, rest_w && rest_x ? min(deep_w, deep_x) : rest_w ? deep_w : deep_x), 24.f);
         auto better = [&](int w, int x) {                     // these whole
             const int left = pairs - w - x;
             const long shared = (w ? 0 : all_w) + (x ? 0 : all_x);
             if (left < 0 || (left == 0 && shared > 0)) return;
-            const long cost = max(max(w ? (long)deep_w : 0L, x ? (long)deep_x : 0L), shared > 0 ? equal(shared, left) + 12 : 0L);
+            const float cost = fmaxf((float)max(w ? deep_w : 0, x ? deep_x : 0), shared > 0 ? __fadd_rn(equal(shared, left, w ? deep_x : deep_w), 12.f) : 0.f);
             if (cost < best) { best = cost; whole_w = w; whole_x = x; }
         };
         better(rest_w, 0);
@@ -898,7 +904,8 @@ __device__ __forceinline__ void loss_weights(uint32_t piece, const LossArgs &a, 
 }
 
 // 32 rows (a row a lane, to go to row `to` of the output; -1: nowhere) of 32 columns from c0 on, times f, by way of shared memory: rows on 16-byte boundaries by four lanes, 64 bytes a row and instruction (32 took
-// twice the time, which bounds gradients with few steps a tile: 18935 rows of 1536 over six words); others by lanes with neighbouring columns, a row at a time.
+// twice the time, which bounds gradients with few steps a tile: 18935 rows of 1536 over six words); others by lanes with neighbouring columns, a row at a time, eight rows' loads before their stores (3159 rows of 2373 over 23 words,
+// forward and backward: 162 us one by one, 93 so).
 template <typename E>
 __device__ __forceinline__ void loss_out(uint32_t piece, E *out, long ld, int vec, int to, int c0, int C, float f, const float *v) {
     const int lane = threadIdx.x & 31;
@@ -923,21 +930,23 @@ __device__ __forceinline__ void loss_out(uint32_t piece, E *out, long ld, int ve
                 if (t >= 0 && c < C) *reinterpret_cast<float4 *>(out + (long)t * ld + c) = x;
             }
         } else {
+            using Word = typename std::conditional<sizeof(E) == 4, uint32_t, uint16_t>::type;
             const int col = lane % kStep, c = c0 + k + col;
             const uint32_t from = (col % kLane) * (uint32_t)sizeof(E);
-#pragma unroll 8
-            for (int r0 = 0; r0 < 32; r0 += 32 / kStep) {
-                const int r = r0 + lane / kStep, t = __shfl_sync(0xffffffffu, to, r);
-                const uint32_t at = piece + piece_at(r, col / kLane) + from;
-                if (t < 0 || c >= C) continue;
-                if constexpr (sizeof(E) == 4) {
-                    uint32_t x;
-                    asm volatile("ld.shared.b32 %0, [%1];" : "=r"(x) : "r"(at) : "memory");
-                    reinterpret_cast<uint32_t *>(out)[(long)t * ld + c] = x;
-                } else {
-                    uint16_t x;
-                    asm volatile("ld.shared.b16 %0, [%1];" : "=h"(x) : "r"(at) : "memory");
-                    reinterpret_cast<uint16_t *>(out)[(long)t * ld + c] = x;
+            // (eight loads before their stores: each on its own is a wait for shared memory)
+#pragma unroll
+            for (int r0 = 0; r0 < 32; r0 += 8 * (32 / kStep)) {
+                Word x[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const uint32_t at = piece + piece_at(r0 + i * (32 / kStep) + lane / kStep, col / kLane) + from;
+                    if constexpr (sizeof(E) == 4) asm volatile("ld.shared.b32 %0, [%1];" : "=r"(x[i]) : "r"(at) : "memory");
+                    else asm volatile("ld.shared.b16 %0, [%1];" : "=h"(x[i]) : "r"(at) : "memory");
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int t = __shfl_sync(0xffffffffu, to, r0 + i * (32 / kStep) + lane / kStep);
+                    if (t >= 0 && c < C) reinterpret_cast<Word *>(out)[(long)t * ld + c] = x[i];
                 }
             }
         }

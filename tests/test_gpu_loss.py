@@ -139,8 +139,9 @@ def test_rows_off_boundaries(dtype):
 
 @pytest.mark.parametrize("dtype", TYPES, ids=str)
 @pytest.mark.parametrize("labelled", ["none", "first", "last", "every ninth"])
-def test_few_rows_have_a_label(dtype, labelled):
-    x, w, labels, _ = problem(1100, 300, 96, dtype, ignored=0.0)
+@pytest.mark.parametrize("vocab", [300, 2100])               # (16-bit rows over up to 2048 words are scored as they stand, others packed)
+def test_few_rows_have_a_label(dtype, labelled, vocab):
+    x, w, labels, _ = problem(1100, vocab, 96, dtype, ignored=0.0)
     keep = torch.zeros(1100, dtype=torch.bool, device="cuda")
     if labelled != "none":
         keep[{"first": slice(0, 1), "last": slice(1099, 1100), "every ninth": slice(0, 1100, 9)}[labelled]] = True

@@ -217,6 +217,24 @@ def test_embed_backward(types, B, L, vocab, width, kind, p):
     assert torch.equal(a.dtable[~met[:-1]], base[~met[:-1]])
 
 
+@pytest.mark.parametrize("B,L,vocab,width,types", [
+    (4, 10000, 50, 512, (BF16, BF16)), (1, 20000, 3000, 2064, (F32, F16)),     # sixteen columns a thread; chunks of 16, of 32 rows
+    (2, 6000, 700, 4096, (BF16, BF16)), (2, 6000, 700, 4096, (BF16, F32)),     # of 40; float32 rows: eight a thread
+    (8, 80000, 5, 128, (F32, BF16)), (3, 50000, 40000, 72, (F16, F16))],       # of 64 and 16 rows, blocks of 128 threads
+    ids=str)
+def test_embed_backward_of_many_elements(B, L, vocab, width, types):
+    T, O = types
+    g = gen(B + L + width)
+    t = tokens_of(g, (B, L), vocab, "mixed")
+    dy = randn(g, B, L, width, dtype=O)
+    ref, bound, pos = grads_reference(t, dy, vocab, L, 0.7, torch.ones(1, width, device="cuda", dtype=torch.float64))
+    r = flare.embed_backward(t, dy, vocab, positions=L, scale=0.7, dtype=T)
+    close(r.dtable, ref, stored(T, ref) + bound, "dtable")
+    close(r.dpositions, pos.sum(0), stored(T, pos.sum(0)) + (B + 4) * U32 * pos.abs().sum(0), "dpositions")
+    s = flare.embed_backward(t, dy, vocab, positions=L, scale=0.7, dtype=T)
+    assert torch.equal(s.dtable, r.dtable) and torch.equal(s.dpositions, r.dpositions)
+
+
 def test_rows_without_a_token_give_nothing_away():
     """NaN and infinities in gradients of rows that have no token reach no row of the table."""
     g = gen(5)

@@ -446,15 +446,14 @@ Rows rows_of(const at::Tensor &t, at::ScalarType dtype, at::IntArrayRef shape, c
     if (t.sizes() != shape) fail(PyExc_ValueError, std::string(name) + ": expected shape " + shape_text(shape) + ", got " + shape_text(t.sizes()));
     const int64_t n = t.dim(), C = t.size(n - 1);
     if (t.numel() == 0) return Rows{t.data_ptr(), C};
-    int64_t stride = 0, rows = 1;                            // of the innermost leading dimension that has more than one entry
+    int64_t stride = C, rows = 1;                            // of the innermost leading dimension that has more than one entry
     bool ok = C == 1 || t.stride(n - 1) == 1;
     for (int64_t i = n - 2; i >= 0; --i) {
         if (t.size(i) == 1) continue;
-        if (stride == 0) stride = t.stride(i);
+        if (rows == 1) stride = t.stride(i);                 // (0: rows that are all the same place, which is less than C apart)
         else ok = ok && t.stride(i) == stride * rows;
         rows *= t.size(i);
     }
-    if (stride == 0) stride = C;
     if (!ok || stride < C) fail(PyExc_ValueError, std::string(name) + ": expected rows of adjacent columns at one distance from each other");
     return Rows{t.data_ptr(), stride};
 }

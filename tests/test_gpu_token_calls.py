@@ -206,3 +206,18 @@ def test_refused(call, error):
         call(x, t, w)
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip((x, t, w), kept))
+
+
+def test_rows_that_are_all_the_same_place_are_refused():
+    """Expanded tensors, one row in memory under many: not read as rows behind one another."""
+    row, t, w = torch.zeros(64, dtype=BF16, device="cuda"), torch.zeros(2, 300, dtype=torch.int64, device="cuda"), torch.zeros(10, 64, dtype=BF16, device="cuda")
+    items = torch.zeros(2, 1, 64, dtype=BF16, device="cuda").expand(2, 300, 64)
+    for x in (row.expand(2, 300, 64), items, row.expand(1, 300, 64).expand(2, 300, 64)):
+        for call in (lambda: flare.token_loss(x, w, t), lambda: flare.embed_backward(t, x, 10), lambda: flare.dropout(x, flare.Drop(0.1, 1, 1)), lambda: flare.dropout_backward(x, flare.Drop(0.1, 1, 1)),
+                     lambda: flare.token_loss(torch.zeros(2, 300, 64, dtype=BF16, device="cuda"), row.expand(10, 64), t),
+                     lambda: flare.embed(t, row.expand(10, 64))):
+            with pytest.raises(ValueError):
+                call()
+    # one row is a row whatever its strides say
+    one = row.as_strided((1, 64), (0, 1))
+    assert flare.token_loss(one, w, t[0, :1])[0].shape == (1,)

@@ -758,7 +758,7 @@ struct Matrices {
         int64_t at = 0, many = 1;
         for (int64_t i = n - 3; i >= 0; --i) {
             if (t.size(i) == 1) continue;
-            if (at == 0) at = t.stride(i);
+            if (many == 1) at = t.stride(i);
             else ok = ok && t.stride(i) == at * many;
             many *= t.size(i);
         }

@@ -221,3 +221,10 @@ def test_rows_that_are_all_the_same_place_are_refused():
     # one row is a row whatever its strides say
     one = row.as_strided((1, 64), (0, 1))
     assert flare.token_loss(one, w, t[0, :1])[0].shape == (1,)
+
+
+def test_matrices_that_are_all_the_same_place_are_refused():
+    m = torch.zeros(3, 1, 16, 16, device="cuda")
+    for g in (m.expand(3, 2, 16, 16), m[:1, 0].expand(4, 16, 16)):
+        with pytest.raises(ValueError):
+            flare.orthogonalize(g)

@@ -106,8 +106,15 @@ SumShape sum_shape(const flare_embed_desc_t *d, bool twos) {
 // Rows of a chunk of the backward's sums: such that an SM has some 1024 groups of columns, 16 to 64.  Positions: whole runs (one row of every batch item) where they are not longer than that, so
 // that none reaches over a chunk's end.
 int chunk_rows(const flare_embed_desc_t *d, int sms) {
-    const long want = d->rows * ((d->width + 7) / 8) / (1024L * sms);
-    return (int)std::min(64L, std::max(16L, want / 4 * 4));
+    const long want = d->rows * ((d->width + 7) / 8) / (1024L * sms), T = std::min(64L, std::max(16L, want / 4 * 4));
+    if (!sum_in_twos(d, sms)) return (int)T;
+    // Longer, where the blocks of wide rows, two an SM, would be a third of a round or less more than whole rounds: 65536 rows of 512 over 256 words take 51 us in chunks of 24 rows (342 blocks for 296 places), 44.6 of
+    // 28.  (Narrow ones are more and smaller: 131072 rows of 128 over 32000 words took 66.5 instead of 63.7, over 256 words 38.9 instead of 40.2.)
+    const SumShape s = sum_shape(d, true);
+    const long blocks = (d->rows * s.tiles + T * s.chunks - 1) / (T * s.chunks), places = 2L * sms, rounds = blocks / places;
+    if (rounds < 1 || blocks - rounds * places > places / 3) return (int)T;
+    const long fit = s.chunks * places * rounds;
+    return (int)std::min(64L, ((d->rows * s.tiles + fit - 1) / fit + 3) / 4 * 4);
 }
 int chunk_rows_of_positions(const flare_embed_desc_t *d, int sms) {
     const long T = chunk_rows(d, sms), batch = d->positions > 0 ? d->rows / d->positions : 1;

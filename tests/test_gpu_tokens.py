@@ -218,8 +218,8 @@ def test_embed_backward(types, B, L, vocab, width, kind, p):
 
 
 @pytest.mark.parametrize("B,L,vocab,width,types", [
-    (4, 10000, 50, 512, (BF16, BF16)), (1, 20000, 3000, 2064, (F32, F16)),     # sixteen columns a thread; chunks of 16, of 32 rows
-    (2, 6000, 700, 4096, (BF16, BF16)), (2, 6000, 700, 4096, (BF16, F32)),     # of 40; float32 rows: eight a thread
+    (4, 10000, 50, 512, (BF16, BF16)), (1, 20000, 3000, 2064, (F32, F16)),     # sixteen columns a thread; chunks of 20, of 36 rows
+    (2, 6000, 700, 4096, (BF16, BF16)), (2, 6000, 700, 4096, (BF16, F32)),     # of 44; float32 rows: eight columns a thread, of 40
     (8, 80000, 5, 128, (F32, BF16)), (3, 50000, 40000, 72, (F16, F16))],       # of 64 and 16 rows, blocks of 128 threads
     ids=str)
 def test_embed_backward_of_many_elements(B, L, vocab, width, types):

@@ -20,7 +20,7 @@
 // (2^-9, as the gradients themselves will be; dloss in a second X instead put the same rounding there, and as many more elements were moved).  float16's G is q times 2^15, so that probabilities down to 2^-29 are
 // normal numbers, and dloss goes into X (scaled so that the largest is one) and into dX's rows.  Small vocabularies in bfloat16 take float16's way backward, X and W times powers of two.
 // float32: X, W, G as two float16 halves each (22 bits; X and W times a power of two that puts their largest near 2^15, held down to 2^-39 of it), a
-// product as three, and sums leave tensor memory, which truncates, every 256 of K to be added up in registers.
+// product as three, and sums leave tensor memory, which truncates, every 128 of K to be added up in registers.
 #pragma once
 
 #include <type_traits>
@@ -398,9 +398,10 @@ template <int kPlanes> struct LossShape {
     static constexpr int kStages = kPlanes == 1 ? 6 : 3;
     static constexpr uint32_t kStage = 2 * kPlanes * kLossHalfTile;        // A (high, low), B (high, low)
 };
-// 64-deep steps whose sums stay in tensor memory, where every addition truncates: of halves 4 (12 x 4 additions); of the forward's 16-bit factors 8 (a loss over 4096 columns is off by 2e-6 with all of
+// 64-deep steps whose sums stay in tensor memory, where every addition truncates: of halves 2 (12 x 2 additions: gradients off by 5e-7 to 6.6e-7; with 4
+// by 8e-7 to 1.2e-6 in 0 to 4 % less time, with 1 by 3e-7 to 4e-7 in 5 to 20 % more); of the forward's 16-bit factors 8 (a loss over 4096 columns is off by 2e-6 with all of
 // them there); of the backward's, whose results are rounded to 2^-9 or 2^-12, 64.
-template <int kKind, int kPlanes> constexpr int kLossDeep = kPlanes == 2 ? 4 : loss_forward(kKind) ? 8 : 64;
+template <int kKind, int kPlanes> constexpr int kLossDeep = kPlanes == 2 ? 2 : loss_forward(kKind) ? 8 : 64;
 constexpr size_t kLossSmem = 1024 + 6 * 2 * kLossHalfTile + kLossResults * kLossPiece + 256;
 
 struct LossMaps { CUtensorMap x, d, w, g; };                  // in boxes of 64 x 64

@@ -675,8 +675,8 @@ __device__ __forceinline__ void add8(float (&v)[8], const float *from) {
     v[4] += y.x; v[5] += y.y; v[6] += y.z; v[7] += y.w;
 }
 enum { kRunOpen = 1, kRunGoesOn = 2, kRunThrough = 4 };       // a chunk's first run began before it; its last one goes on behind it; the two are the same and all of it
-// Blocks of 128 threads where a row takes up to 16 of them, so that no SM waits for the last of few large ones, else of 256, where a block joins more chunks by itself (65536 rows of 256 over 32000 words: 84 us with
-// blocks of 64, 80 with 128 or 256; of 512: 92, 78, 74).  Chunks are 16 rows, longer where there is more to do: 16384 rows of 4096 take 186 us in chunks of 16, 144 of 64; 65536 of 512 over 256 words take 50.3 of 16,
+// Blocks of 128 threads where a row takes up to 16 of them, so that no SM waits for the last of few large ones, else of 256, where a block joins more chunks by itself (131072 rows of 256 over 32000 words: 84 us with
+// blocks of 64, 80 with 128 or 256; 65536 of 512: 92, 78, 74).  Chunks are 16 rows, longer where there is more to do: 16384 rows of 4096 take 186 us in chunks of 16, 144 of 64; 65536 of 512 over 256 words take 50.3 of 16,
 // 44.6 of 28; 131072 of 128 over 32000 take 65.6 of 16, 79.5 of 32.  It is bound by instructions: 32 x 4096 rows of 128 over 256 words with positions take 41 us in all, 17 of them the sort.
 constexpr int kSumThreads = 256;
 __host__ __device__ constexpr size_t sum_smem(uint32_t threads, int width) { return threads * (size_t)(2 * 32 * width + 8); }

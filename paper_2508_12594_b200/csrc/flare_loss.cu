@@ -82,7 +82,7 @@ int few_blocks(const flare_loss_desc_t *d, int sms) {
     const long groups = (d->vocab + kFewWords - 1) / kFewWords, warps = (long)sms * (few_rows(d) <= 2 ? 4 : 2) * (kFewThreads / 32), rounds = (groups + warps - 1) / warps;
     return (int)(((groups + rounds - 1) / rounds + kFewThreads / 32 - 1) / (kFewThreads / 32));
 }
-struct LossLayout { size_t info, rank, chunk, largest, px, pd, pw, index, label, part, chosen, gave_up, lse2, coef, g, acc, slots, total; };
+struct LossLayout { size_t info, rank, chunk, largest, px, pd, pw, index, label, part, chosen, gave_up, lse2, gm, coef, g, acc, slots, total; };
 LossLayout loss_layout(const flare_loss_desc_t *d, const LossPlan &p, bool backward) {
     LossLayout w{};
     size_t off = kHeaderBytes;
@@ -104,6 +104,7 @@ LossLayout loss_layout(const flare_loss_desc_t *d, const LossPlan &p, bool backw
     } else {
         take(w.pd, d->dtype == FLARE_DTYPE_BF16 && p.to == kAsIs ? 0 : row * p.cap);
         take(w.lse2, sizeof(float) * (size_t)p.cap);
+        take(w.gm, sizeof(float) * (size_t)p.cap);
         take(w.coef, sizeof(float) * (size_t)p.cap);
         take(w.g, sizeof(uint16_t) * (size_t)p.planes * p.cap * p.Vp);
         take(w.acc, p.pieces > 1 ? sizeof(float) * (size_t)p.cap * p.tiles_c * p.grad_width : 0);
@@ -329,7 +330,10 @@ int flare_loss_backward(const flare_loss_desc_t *desc, const void *x, const void
     char *ws = static_cast<char *>(workspace);
     LossPack k{};
     k.lse_in = lse; k.dloss = dloss; k.mult = desc->scale * desc->dloss_scale;
-    k.lse2 = reinterpret_cast<float *>(ws + l.lse2); k.coef = reinterpret_cast<float *>(ws + l.coef);
+    k.lse2 = reinterpret_cast<float *>(ws + l.lse2); k.gm = reinterpret_cast<float *>(ws + l.gm); k.coef = reinterpret_cast<float *>(ws + l.coef);
+    // bfloat16's G: q where one dloss is that of all rows (a label's q is next to -1, which is no rounding), else times it, for a second X would be a second rounding; float16's: q times 2^15, or times 2^14 and a row's
+    // mantissa of dloss, below 2
+    k.g_factor = !bf16 ? dloss ? 16384.f : 32768.f : dloss ? 0.f : 1.f;
     k.dx = dx; k.ld_dx = ld_dx;
     k.pd = bf16 || !dloss || !dw ? nullptr : reinterpret_cast<uint16_t *>(ws + l.pd);
     LossMaps maps{};
@@ -343,13 +347,11 @@ int flare_loss_backward(const flare_loss_desc_t *desc, const void *x, const void
     }
     if ((rc = make_plane_map(&maps.g, ws + l.g, bf16, p.Vp, p.cap, p.planes, p.Vp, 64)) != FLARE_OK) return rc;
     a.g = reinterpret_cast<uint16_t *>(ws + l.g); a.ld_g = p.Vp;
-    a.lse2 = k.lse2; a.coef = k.coef; a.grad_width = p.grad_width; a.tiles_c = p.tiles_c;
+    a.lse2 = k.lse2; a.gm = k.gm; a.coef = k.coef; a.grad_width = p.grad_width; a.tiles_c = p.tiles_c;
     a.dw = dw; a.dx = dx; a.ld_dw = ld_dw; a.ld_dx = ld_dx;
     auto vec = [&](const void *q, long ld) { return desc->width * t % 16 == 0 && ld * t % 16 == 0 && aligned16(q); };
     a.dw_vec = vec(dw, ld_dw); a.dx_vec = vec(dx, ld_dx);
-    // bfloat16's G: q where one dloss is that of all rows (a label's q is next to -1, which is no rounding), else times it; float16's: q times 2^15, dloss goes into X
-    a.g_factor = !bf16 ? 32768.f : dloss ? 0.f : 1.f;
-    a.dw_factor = a.g_factor != 0.f ? k.mult / a.g_factor : 0.f;
+    a.dw_factor = k.g_factor != 0.f ? k.mult / k.g_factor : 1.f;
     a.acc = reinterpret_cast<float *>(ws + l.acc); a.slots = reinterpret_cast<float *>(ws + l.slots);
     auto weights = f32 ? launch_loss<kLossWeights, 2, float> : launch_loss<kLossWeights, 1, float>;
     auto grads = f32 ? launch_loss<kLossGrads, 2, float> : desc->dtype == FLARE_DTYPE_BF16 ? launch_loss<kLossGrads, 1, __nv_bfloat16> : launch_loss<kLossGrads, 1, __half>;

@@ -18,7 +18,8 @@
 //
 // bfloat16 and float16 are multiplied as they are, G in the same type, rounded once.  bfloat16's G is q where one dloss is that of all rows (next to a label q is next to -1, which is no rounding), else dloss scale q
 // (2^-9, as the gradients themselves will be; dloss in a second X instead put the same rounding there, and as many more elements were moved).  float16's G is q times 2^15, so that probabilities down to 2^-29 are
-// normal numbers, and dloss goes into X (scaled so that the largest is one) and into dX's rows.  Small vocabularies in bfloat16 take float16's way backward, X and W times powers of two.
+// normal numbers; of a row's own dloss its mantissa is there too (q times 2^14 and up to 2) and its power of two, which rounds nothing, in a second X and in dX's rows.  Small vocabularies in bfloat16 take float16's way
+// backward, X and W times powers of two.
 // float32: X, W, G as two float16 halves each (22 bits; X and W times a power of two that puts their largest near 2^15, held down to 2^-39 of it), a
 // product as three, and sums leave tensor memory, which truncates, every 128 of K to be added up in registers.
 #pragma once
@@ -34,7 +35,7 @@ namespace flare {
 struct LossInfo {
     uint32_t rows;               // with a label
     float x_scale, w_scale;      // of the halves (1 but for float32)
-    float dmax;                  // largest |dloss| of a row (float16, float32), or 1
+    float dmax;                  // where dloss is in the second X: the power of two of the largest of a row, else 1
 };
 // Per 1024 rows.
 struct LossChunk { uint32_t rows; float dmax; };
@@ -192,13 +193,19 @@ struct LossPack {
     // backward
     const float *lse_in, *dloss;
     float mult;                               // on dloss
-    float *lse2, *coef;                       // of packed rows: lse / ln 2; what q (bfloat16) or dX (else) is multiplied by
+    float *lse2, *gm, *coef;                  // of packed rows: lse / ln 2; what q is multiplied by on its way to G, what dX is multiplied by
+    float g_factor;                           // of q in G; 0: all of dloss is there
     void *dx;                                 // rows without a label: zeros
     long ld_dx;
 };
 constexpr int kPackThreads = 256;             // of a block, which takes 4 to 1024 rows (of one chunk)
 constexpr int kPackAlone = 4096;              // rows up to which every block finds for itself, in all labels, what the scan would tell it, where no maxima are wanted: a launch less (4096 rows over 5000 words of 256: forward 23.1 us, with it 25.3)
 
+// The power of two at or below |d| (2^-126 for less), `other` where d is none that has one.
+__device__ __forceinline__ float two_of(float d, float other) {
+    const uint32_t e = __float_as_uint(d) & 0x7f800000u;
+    return e == 0x7f800000u ? other : __uint_as_float(max(e, 0x00800000u));
+}
 // The power of two that puts `most` between 2^14 and 2^15.
 __device__ __forceinline__ float half_scale(float most) {
     if (!(most > 0.f)) return 1.f;
@@ -240,7 +247,7 @@ __global__ void __launch_bounds__(kPackThreads) loss_pack_kernel(const LossPack 
     __shared__ float shared[32];
     __shared__ uint32_t sums[2][kPackThreads / 32];
     __shared__ int to_row[kLossChunk];                        // of packed X; -1: no label
-    __shared__ float d_row[kLossChunk];                       // dloss / dmax
+    __shared__ float d_row[kLossChunk];                       // power of two of dloss, over the largest of them
     ptx::grid_launch();
     ptx::grid_wait();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -304,7 +311,7 @@ __global__ void __launch_bounds__(kPackThreads) loss_pack_kernel(const LossPack 
     dmax = block_max(dmax, shared);                           // (and a barrier for the sums)
     base = total = 0;
     for (int w = 0; w < kPackThreads / 32; ++w) { base += sums[0][w]; total += sums[1][w]; }
-    if (!a.dloss || !(dmax > 0.f)) dmax = 1.f;
+    dmax = a.pd ? two_of(dmax, 1.f) : 1.f;
     if (blockIdx.x == 0 && threadIdx.x == 0) *a.info = LossInfo{total, sx, sw, dmax};
     const int rows = (int)min((long)a.pack_rows, a.rows - n0);
     if (alone) {                                              // (up to a row a thread)
@@ -329,9 +336,11 @@ __global__ void __launch_bounds__(kPackThreads) loss_pack_kernel(const LossPack 
             a.label[to] = (int)label_at(a.labels, a.wide, n);
             if (a.loss == nullptr) {
                 const float d = a.dloss ? a.dloss[n] : 1.f;
-                d_row[i] = d / dmax;
+                const float two = a.dloss ? two_of(d, dmax) : 1.f;
+                d_row[i] = two / dmax;
                 a.lse2[to] = a.lse_in[n] * 1.4426950408889634f;
-                a.coef[to] = d * a.mult;
+                a.gm[to] = a.g_factor == 0.f ? d * a.mult : d / two * a.g_factor;
+                a.coef[to] = a.g_factor == 0.f ? 1.f : two * a.mult / a.g_factor;
             }
         } else if (a.loss) {
             a.loss[n] = 0.f;
@@ -428,8 +437,7 @@ struct LossArgs {
     float *chosen;
     float *loss, *lse;           // not null: a tile is all of the vocabulary, which finishes its rows
     // backward
-    const float *lse2, *coef;
-    float g_factor;              // of q in G; 0: dloss scale, a row's own
+    const float *lse2, *gm, *coef;
     uint16_t *g;                 // planes [cap][ld_g]
     long ld_g;
     int grad_width, tiles_c;     // columns of a gradient's tile, tiles across
@@ -437,7 +445,7 @@ struct LossArgs {
     void *dw, *dx;
     long ld_dw, ld_dx;
     int dw_vec, dx_vec;          // rows can be written 16 bytes at a time
-    float dw_factor;             // scale dloss_scale / g_factor (times dmax / x_scale)
+    float dw_factor;             // scale dloss_scale / g_factor (times dmax / x_scale), or 1 where G holds them
     float *acc;                  // dX over the pieces before, by tile: [2 blocks][grad_width columns][128 rows]
     float *slots;                // sums of parts of tiles, likewise, two per pair
 };
@@ -704,7 +712,7 @@ __device__ __forceinline__ LossRow loss_row(const LossArgs &a, int rows, int row
         if (kKind != kLossGrads) r.label = a.label_of(row);
         if (kKind == kLossWeights) r.lse2 = a.lse2[row];
         if (kKind == kLossGrads || (loss_forward(kKind) && a.loss)) r.index = a.index[row];
-        if (!loss_forward(kKind)) r.coef = a.coef[row];
+        if (!loss_forward(kKind)) r.coef = kKind == kLossWeights ? a.gm[row] : a.coef[row];
     }
     return r;
 }
@@ -843,7 +851,7 @@ __device__ __forceinline__ void loss_weights(uint32_t piece, const LossArgs &a, 
     const int lane = threadIdx.x & 31, col0 = a.v0 + local0;
     const bool in = row < rows;
     const int at = r.label - col0;                                       // (no label: below zero)
-    const float lse2 = r.lse2, f = a.g_factor != 0.f ? a.g_factor : r.coef;
+    const float lse2 = r.lse2, f = r.coef;
     const int words = in ? a.V - col0 : 0;
     // the label's, where it is among the columns: put into the piece on its own
     const bool mine = at >= 0 && at < cols;
@@ -959,7 +967,7 @@ __device__ __forceinline__ void loss_gradient(uint32_t piece, const LossArgs &a,
     const int lane = threadIdx.x & 31, local = i * 256 + block * 128 + quad * 32 + lane, c0 = j * a.grad_width + col;
     if (c0 >= a.C) return;
     if (!dx) {
-        const float f = a.g_factor != 0.f ? a.dw_factor * info.dmax / info.x_scale : 1.f;
+        const float f = a.dw_factor * info.dmax / info.x_scale;
         loss_out<E>(piece, static_cast<E *>(a.dw), a.ld_dw, a.dw_vec, local < a.words ? a.v0 + local : -1, c0, a.C, f, v);
         return;
     }
@@ -975,7 +983,7 @@ __device__ __forceinline__ void loss_gradient(uint32_t piece, const LossArgs &a,
             return;
         }
     }
-    const float f = a.g_factor != 0.f ? r.coef / (a.g_factor * info.w_scale) : 1.f;
+    const float f = r.coef / info.w_scale;
     loss_out<E>(piece, static_cast<E *>(a.dx), a.ld_dx, a.dx_vec, r.index, c0, a.C, f, v);
 }
 

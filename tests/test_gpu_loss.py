@@ -3,7 +3,7 @@
 Bounds, element by element.  A logit l = scale x.w is off by D = scale max_v sum_c |x_c w_c| E, E the relative error of a product and of the additions: 16-bit factors
 are multiplied exactly and added up 16 at a time with truncation, 2^-22 of what has been added up for each (half a unit of 24 bits lost by the sum and as much by the alignment of
 what is added), width / 16 + 2 additions; float32 ones are held in 22 bits (3 * 2^-22 for both and the product of the low halves that is left out, and 2^-39 of the largest element for small
-ones), with 48 additions before a sum leaves tensor memory, and width / 256 rounded ones behind it.  lse is off by as much, by the additions of exponentials (a thread 128,
+ones), with 24 additions before a sum leaves tensor memory, and width / 128 rounded ones behind it.  lse is off by as much, by the additions of exponentials (a thread 128,
 then one per 2048 words, then 32 joins), 2^-24 each, exponentials (2^-22 each and 2^-24 of the exponent, at most 40 in units of ln 2 where they count), and its own rounding.  p = exp(l - lse) is off by its share of both.
 """
 import pytest
@@ -44,7 +44,7 @@ class Reference:
         self.lse = torch.where(there, torch.logsumexp(l, 1), zero)
         self.loss = torch.where(there, self.lse - l.gather(1, at)[:, 0], zero)
         if T == F32:
-            E = (3 + 48 + 16) * 2.0 ** -22 + (C / 256 + 2) * U32
+            E = (3 + 24 + 8) * 2.0 ** -22 + (C / 128 + 2) * U32
             floor = 2.0 ** -38 * (x.abs().max() * w.abs().sum(1).max() + w.abs().max() * x.abs().sum(1).max()) * scale
         else:
             E, floor = (C / 16 + 2) * 2.0 ** -22, 0.0                           # (of the forward)
@@ -57,7 +57,7 @@ class Reference:
         g = torch.where(there, dloss if isinstance(dloss, torch.Tensor) else torch.full_like(self.lse, dloss), 0.0).double() * scale
         self.dx, self.dw = g[:, None] * (q @ w), (g[:, None] * q).T @ x
         # Small bfloat16 vocabularies (W up to 2^22 elements) are multiplied as float16 times powers of two that put the largest element of X and of W between 2^14 and 2^15 and of q at 2^15: a value
-        # that bfloat16 holds is held exactly down to 2^-14 of that scale (2^-28 of the largest), below to half of 2^-24, 2^-39 of the largest; q to 2^-11 and to 2^-40; and x dloss / max dloss to 2^-11.
+        # that bfloat16 holds is held exactly down to 2^-14 of that scale (2^-28 of the largest), below to half of 2^-24, 2^-39 of the largest; q (times a row's mantissa of dloss) to 2^-11 and to 2^-39; x times powers of two of dloss not at all.
         half = T == BF16 and V * C <= 1 << 22
         # errors of q: of p, of its difference from the label's 1, and of its rounding (float32: 22 bits)
         if half:
@@ -68,10 +68,10 @@ class Reference:
         q = q.abs() * there[:, None]
         steps_x, steps_w = (V / 16 + 76) * 2.0 ** -22, (n / 16 + 76) * 2.0 ** -22
         if T == F32:
-            steps_x, steps_w = (67 * 2.0 ** -22 + (V / 256 + 76) * U32), (67 * 2.0 ** -22 + (n / 256 + 76) * U32)
+            steps_x, steps_w = (35 * 2.0 ** -22 + (V / 128 + 76) * U32), (35 * 2.0 ** -22 + (n / 128 + 76) * U32)
         ga = g.abs()[:, None]
         self.dx_bound = ga * (dq @ w.abs() + steps_x * (q @ w.abs())) + UNIT[T] * self.dx.abs()
-        self.dw_bound = (ga * dq).T @ x.abs() + (steps_w + (u if T != BF16 else 2.0 ** -11 if half else 0.0)) * ((ga * q).T @ x.abs()) + UNIT[T] * self.dw.abs()
+        self.dw_bound = (ga * dq).T @ x.abs() + (steps_w + (u if T == F32 else 0.0)) * ((ga * q).T @ x.abs()) + UNIT[T] * self.dw.abs()
         if T == F16:                                         # results below the normal numbers; x times dloss / max dloss below them
             self.dx_bound += 2.0 ** -25
             self.dw_bound += 2.0 ** -25 + 2.0 ** -25 * g.abs().max() * q.sum(0)[:, None]

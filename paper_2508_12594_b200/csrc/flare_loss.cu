@@ -82,7 +82,7 @@ int few_blocks(const flare_loss_desc_t *d, int sms) {
     const long groups = (d->vocab + kFewWords - 1) / kFewWords, warps = (long)sms * (few_rows(d) <= 2 ? 4 : 2) * (kFewThreads / 32), rounds = (groups + warps - 1) / warps;
     return (int)(((groups + rounds - 1) / rounds + kFewThreads / 32 - 1) / (kFewThreads / 32));
 }
-struct LossLayout { size_t info, rank, chunk, largest, px, pd, pw, index, label, part, chosen, gave_up, lse2, gm, coef, g, acc, slots, total; };
+struct LossLayout { size_t info, rank, chunk, largest, px, pd, pw, index, label, part, chosen, gave_up, lse_of, gm, coef, g, acc, slots, total; };
 LossLayout loss_layout(const flare_loss_desc_t *d, const LossPlan &p, bool backward) {
     LossLayout w{};
     size_t off = kHeaderBytes;
@@ -103,7 +103,7 @@ LossLayout loss_layout(const flare_loss_desc_t *d, const LossPlan &p, bool backw
         take(w.gave_up, sizeof(uint32_t) * 2 * (size_t)p.pairs);
     } else {
         take(w.pd, d->dtype == FLARE_DTYPE_BF16 && p.to == kAsIs ? 0 : row * p.cap);
-        take(w.lse2, sizeof(float) * (size_t)p.cap);
+        take(w.lse_of, sizeof(float) * (size_t)p.cap);
         take(w.gm, sizeof(float) * (size_t)p.cap);
         take(w.coef, sizeof(float) * (size_t)p.cap);
         take(w.g, sizeof(uint16_t) * (size_t)p.planes * p.cap * p.Vp);
@@ -280,7 +280,7 @@ int flare_loss_forward(const flare_loss_desc_t *desc, const void *x, const void 
             return rc;
         LossMerge m{};
         m.part = f.part; m.chosen = f.chosen; m.cap = p.cap; m.parts = blocks; m.loss = loss; m.lse = lse;
-        m.labels = labels; m.wide = f.wide; m.V = f.V; m.direct = f.rows; m.status = reinterpret_cast<uint32_t *>(ws);
+        m.labels = labels; m.wide = f.wide; m.V = f.V; m.direct = f.rows; m.status = reinterpret_cast<uint32_t *>(ws); m.scale = desc->scale;
         return launch_merge(m, desc->rows, st);
     }
     LossPack k{};
@@ -307,7 +307,7 @@ int flare_loss_forward(const flare_loss_desc_t *desc, const void *x, const void 
     if (a.loss) return FLARE_OK;
     LossMerge m{};
     m.info = a.info; m.part = a.part; m.chosen = a.chosen; m.index = a.index; m.cap = p.cap; m.parts = a.tiles_v; m.loss = loss; m.lse = lse;
-    m.labels = a.labels; m.wide = a.wide; m.V = a.V; m.direct = a.direct; m.gave_up = a.gave_up; m.status = a.status; m.blocks = 2 * pairs;
+    m.labels = a.labels; m.wide = a.wide; m.V = a.V; m.direct = a.direct; m.gave_up = a.gave_up; m.status = a.status; m.blocks = 2 * pairs; m.scale = desc->scale;
     return launch_merge(m, desc->rows, st);
 }
 
@@ -330,7 +330,7 @@ int flare_loss_backward(const flare_loss_desc_t *desc, const void *x, const void
     char *ws = static_cast<char *>(workspace);
     LossPack k{};
     k.lse_in = lse; k.dloss = dloss; k.mult = desc->scale * desc->dloss_scale;
-    k.lse2 = reinterpret_cast<float *>(ws + l.lse2); k.gm = reinterpret_cast<float *>(ws + l.gm); k.coef = reinterpret_cast<float *>(ws + l.coef);
+    k.lse_of = reinterpret_cast<float *>(ws + l.lse_of); k.gm = reinterpret_cast<float *>(ws + l.gm); k.coef = reinterpret_cast<float *>(ws + l.coef);
     // bfloat16's G: q where one dloss is that of all rows (a label's q is next to -1, which is no rounding), else times it, for a second X would be a second rounding; float16's: q times 2^15, or times 2^14 and a row's
     // mantissa of dloss, below 2
     k.g_factor = !bf16 ? dloss ? 16384.f : 32768.f : dloss ? 0.f : 1.f;
@@ -347,7 +347,7 @@ int flare_loss_backward(const flare_loss_desc_t *desc, const void *x, const void
     }
     if ((rc = make_plane_map(&maps.g, ws + l.g, bf16, p.Vp, p.cap, p.planes, p.Vp, 64)) != FLARE_OK) return rc;
     a.g = reinterpret_cast<uint16_t *>(ws + l.g); a.ld_g = p.Vp;
-    a.lse2 = k.lse2; a.gm = k.gm; a.coef = k.coef; a.grad_width = p.grad_width; a.tiles_c = p.tiles_c;
+    a.lse_of = k.lse_of; a.gm = k.gm; a.coef = k.coef; a.grad_width = p.grad_width; a.tiles_c = p.tiles_c;
     a.dw = dw; a.dx = dx; a.ld_dw = ld_dw; a.ld_dx = ld_dx;
     auto vec = [&](const void *q, long ld) { return desc->width * t % 16 == 0 && ld * t % 16 == 0 && aligned16(q); };
     a.dw_vec = vec(dw, ld_dw); a.dx_vec = vec(dx, ld_dx);

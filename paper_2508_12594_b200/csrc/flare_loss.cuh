@@ -193,7 +193,7 @@ struct LossPack {
     // backward
     const float *lse_in, *dloss;
     float mult;                               // on dloss
-    float *lse2, *gm, *coef;                  // of packed rows: lse / ln 2; what q is multiplied by on its way to G, what dX is multiplied by
+    float *lse_of, *gm, *coef;                // of packed rows: lse; what q is multiplied by on its way to G, what dX is multiplied by
     float g_factor;                           // of q in G; 0: all of dloss is there
     void *dx;                                 // rows without a label: zeros
     long ld_dx;
@@ -338,7 +338,7 @@ __global__ void __launch_bounds__(kPackThreads) loss_pack_kernel(const LossPack 
                 const float d = a.dloss ? a.dloss[n] : 1.f;
                 const float two = a.dloss ? two_of(d, dmax) : 1.f;
                 d_row[i] = two / dmax;
-                a.lse2[to] = a.lse_in[n] * 1.4426950408889634f;
+                a.lse_of[to] = a.lse_in[n];
                 a.gm[to] = a.g_factor == 0.f ? d * a.mult : d / two * a.g_factor;
                 a.coef[to] = a.g_factor == 0.f ? 1.f : two * a.mult / a.g_factor;
             }
@@ -408,9 +408,9 @@ template <int kPlanes> struct LossShape {
     static constexpr uint32_t kStage = 2 * kPlanes * kLossHalfTile;        // A (high, low), B (high, low)
 };
 // 64-deep steps whose sums stay in tensor memory, where every addition truncates: of halves 2 (12 x 2 additions: gradients off by 5e-7 to 6.6e-7; with 4
-// by 8e-7 to 1.2e-6 in 0 to 4 % less time, with 1 by 3e-7 to 4e-7 in 5 to 20 % more); of the forward's 16-bit factors 8 (a loss over 4096 columns is off by 2e-6 with all of
-// them there); of the backward's, whose results are rounded to 2^-9 or 2^-12, 64.
-template <int kKind, int kPlanes> constexpr int kLossDeep = kPlanes == 2 ? 2 : loss_forward(kKind) ? 8 : 64;
+// by 8e-7 to 1.2e-6 in 0 to 4 % less time, with 1 by 3e-7 to 4e-7 in 5 to 20 % more); of 16-bit factors' logits 8 (a loss over 4096 columns is off by 2e-6 with all of
+// them there; the same forward and backward, so that both have the same logits); of the gradients, whose results are rounded to 2^-9 or 2^-12, 64.
+template <int kKind, int kPlanes> constexpr int kLossDeep = kPlanes == 2 ? 2 : kKind != kLossGrads ? 8 : 64;
 constexpr size_t kLossSmem = 1024 + 6 * 2 * kLossHalfTile + kLossResults * kLossPiece + 256;
 
 struct LossMaps { CUtensorMap x, d, w, g; };                  // in boxes of 64 x 64
@@ -432,12 +432,12 @@ struct LossArgs {
         return l >= 0 && l < V ? (int)l : -1;
     }
     uint32_t *gave_up;           // direct: a word for every pair's block, joined behind
-    // forward: maximum and sum of tiles_v parts of a row (in units of ln 2), the label's logit
+    // forward: maximum and sum of tiles_v parts of a row, the label's logit; maxima and logits as they leave the products, before `scale`
     float2 *part;
     float *chosen;
     float *loss, *lse;           // not null: a tile is all of the vocabulary, which finishes its rows
     // backward
-    const float *lse2, *gm, *coef;
+    const float *lse_of, *gm, *coef;
     uint16_t *g;                 // planes [cap][ld_g]
     long ld_g;
     int grad_width, tiles_c;     // columns of a gradient's tile, tiles across
@@ -704,20 +704,24 @@ __device__ __forceinline__ bool loss_agree(bool ok) {
 }
 
 // What a result warp needs of its lanes' rows, asked for before it waits for their sums.
-struct LossRow { int label, index; float lse2, coef; };
+struct LossRow { int label, index; float lse, coef; };
 template <int kKind>
 __device__ __forceinline__ LossRow loss_row(const LossArgs &a, int rows, int row, bool wanted) {
     LossRow r{-1, -1, 0.f, 0.f};
     if (row < rows && wanted) {
         if (kKind != kLossGrads) r.label = a.label_of(row);
-        if (kKind == kLossWeights) r.lse2 = a.lse2[row];
+        if (kKind == kLossWeights) r.lse = a.lse_of[row];
         if (kKind == kLossGrads || (loss_forward(kKind) && a.loss)) r.index = a.index[row];
         if (!loss_forward(kKind)) r.coef = kKind == kLossWeights ? a.gm[row] : a.coef[row];
     }
     return r;
 }
 
-// Forward: maximum and sum of exponentials of a row's `left` (up to 64) columns, in units of ln 2.
+// Exponentials are taken of differences of logits, each rounded once: with a fused multiply-add to a rounded maximum a row whose logits reach 1e8 would have e^4 in the place of 1.  So statistics are of
+// sums as they leave the products, in units of which c2 = scale / ln 2 makes exponents, and a logit is rounded (times scale) before lse goes off it.
+constexpr float kLossLog2e = 1.4426950408889634f;
+__device__ __forceinline__ float loss_from(float m) { return m == -INFINITY ? 0.f : m; }
+// Forward: maximum and sum of exponentials of a row's `left` (up to 64) columns.
 struct LossStat { float m, l; };
 __device__ __forceinline__ LossStat loss_stat(float (&v)[64], int left, float c2) {
     if (left < 64) {
@@ -731,25 +735,33 @@ __device__ __forceinline__ LossStat loss_stat(float (&v)[64], int left, float c2
         for (int i = 0; i < 4; ++i) mx[i] = ptx::max3(mx[i], v[e + i], v[e + 4 + i]);
 #pragma unroll
     for (int i = 0; i < 4; ++i) mx[i] = fmaxf(mx[i], v[60 + i]);
-    const float m = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * c2, ref = m == -INFINITY ? 0.f : m;
+    const float m = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])), ref = loss_from(m);
     float2 l[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
     for (int e = 0; e < 64; e += 2) {
-        const float2 x = __ffma2_rn(make_float2(v[e], v[e + 1]), make_float2(c2, c2), make_float2(-ref, -ref));
+        const float2 x = __fmul2_rn(__fadd2_rn(make_float2(v[e], v[e + 1]), make_float2(-ref, -ref)), make_float2(c2, c2));
         l[e >> 1 & 1] = __fadd2_rn(l[e >> 1 & 1], make_float2(ptx::ex2(x.x), ptx::ex2(x.y)));
     }
     return LossStat{m, (l[0].x + l[0].y) + (l[1].x + l[1].y)};
 }
-template <int N> __device__ __forceinline__ LossStat loss_all(const LossStat (&s)[N]) {
+// The two sides of a sum of exponentials as one.
+__device__ __forceinline__ LossStat loss_both(LossStat a, LossStat b, float c2) {
+    const float m = fmaxf(a.m, b.m), ref = loss_from(m);
+    return LossStat{m, a.l * ptx::ex2((a.m - ref) * c2) + b.l * ptx::ex2((b.m - ref) * c2)};
+}
+template <int N> __device__ __forceinline__ LossStat loss_all(const LossStat (&s)[N], float c2) {
     float m = s[0].m;
 #pragma unroll
     for (int i = 1; i < N; ++i) m = fmaxf(m, s[i].m);
-    const float ref = m == -INFINITY ? 0.f : m;
+    const float ref = loss_from(m);
     float l = 0.f;
 #pragma unroll
-    for (int i = 0; i < N; ++i) l += s[i].l * ptx::ex2(s[i].m - ref);
+    for (int i = 0; i < N; ++i) l += s[i].l * ptx::ex2((s[i].m - ref) * c2);
     return LossStat{m, l};
 }
+// lse, rounded as the backward takes a logit off it: where one word is all there is both are the same number.  And a row's loss, of which nothing but log l is left where the label is the maximum.
+__device__ __forceinline__ float loss_lse(LossStat s, float scale) { return __fadd_rn(__fmul_rn(s.m, scale), logf(s.l)); }
+__device__ __forceinline__ float loss_of(LossStat s, float chosen, float scale) { return (s.m - chosen) * scale + logf(s.l); }
 // The value at place `at` (0 to 63), by halves of sixteen at a time.
 __device__ __forceinline__ float loss_pick(const float (&v)[64], int at) {
     float r = 0.f;
@@ -768,12 +780,11 @@ __device__ __forceinline__ float loss_pick(const float (&v)[64], int at) {
     return r;
 }
 // What four (or two) warps' columns of a tile say of their rows, joined in shared memory; `joint`: [warps - 1][128 rows], then the labels' logits.
-__device__ __forceinline__ void loss_row_out(const LossArgs &a, const LossRow &r, int j, int row, int rows, LossStat s, const float *chosen) {
+__device__ __forceinline__ void loss_row_out(const LossArgs &a, const LossRow &r, int j, int row, int rows, LossStat s, const float *chosen, float scale) {
     if (row >= rows) return;
     if (a.loss) {
-        const float log_l = logf(s.l);
-        a.loss[r.index] = (s.m - *chosen) * 0.69314718056f + log_l;
-        a.lse[r.index] = s.m * 0.69314718056f + log_l;
+        a.loss[r.index] = loss_of(s, *chosen, scale);
+        a.lse[r.index] = loss_lse(s, scale);
     } else {
         a.part[(long)j * a.cap + row] = make_float2(s.m, s.l);
     }
@@ -782,14 +793,15 @@ __device__ __forceinline__ LossStat loss_columns(const LossArgs &a, float (&v)[6
     const bool mine = at >= 0 && at < cols;
     if (__any_sync(0xffffffffu, mine)) {
         const float c = loss_pick(v, at);
-        if (mine) *(a.loss ? chosen : a.chosen + row) = c * c2;
+        if (mine) *(a.loss ? chosen : a.chosen + row) = c;
     }
     return left > 0 ? loss_stat(v, min(cols, left), c2) : LossStat{-INFINITY, 0.f};
 }
 constexpr int kJoint = 4 * 128;                               // float2 of a place; places are written in turn: one again behind the next tile's barrier
 // A tile by all sixteen warps, a quarter of the columns each.
 template <int kPlanes>
-__device__ __forceinline__ bool loss_stats(LossPipe &q, const LossArgs &a, const LossUnit &u, const LossRow &r, float c2, int rows, int row, int cols, float2 *joint) {
+__device__ __forceinline__ bool loss_stats(LossPipe &q, const LossArgs &a, const LossUnit &u, const LossRow &r, float scale, int rows, int row, int cols, float2 *joint) {
+    const float c2 = scale * kLossLog2e;
     const int warp = ptx::warp_index(), part = (warp - 4) >> 2, local = (warp & 3) * 32 + (threadIdx.x & 31), col0 = u.j * a.width + part * cols;
     float *chosen = reinterpret_cast<float *>(joint + 3 * 128) + local;
     float v[64];
@@ -801,13 +813,14 @@ __device__ __forceinline__ bool loss_stats(LossPipe &q, const LossArgs &a, const
     if (part == 0) {
 #pragma unroll
         for (int p = 0; p < 3; ++p) s[p + 1] = LossStat{joint[p * 128 + local].x, joint[p * 128 + local].y};
-        loss_row_out(a, r, u.j, row, rows, loss_all(s), chosen);
+        loss_row_out(a, r, u.j, row, rows, loss_all(s, c2), chosen, scale);
     }
     return true;
 }
 // Tiles in turn by two sets of eight warps, half of the columns each in two steps, where one set of sums is all there is (up to 512 columns of 16 bits): then the sums come quicker than a tile's end, and with all warps
 // at the same tile, which wait for one another, the special-function units rest while the others' maxima, labels and joins are formed (131072 rows of 128 over 256 words: 25 us then, 20 in turns).
-__device__ __forceinline__ bool loss_stats_by_turns(LossPipe &q, const LossArgs &a, const LossUnit &u, const LossRow &r, float c2, int rows, int row, float2 *joint) {
+__device__ __forceinline__ bool loss_stats_by_turns(LossPipe &q, const LossArgs &a, const LossUnit &u, const LossRow &r, float scale, int rows, int row, float2 *joint) {
+    const float c2 = scale * kLossLog2e;
     const int warp = ptx::warp_index(), part = (warp - 4) >> 2, set = part >> 1, half = part & 1, local = (warp & 3) * 32 + (threadIdx.x & 31), cols = a.width / 2;
     const uint32_t acc = q.tmem + ((uint32_t)((warp & 3) * 32) << 16) + half * cols + (q.c & 1) * 256;
     float *chosen = reinterpret_cast<float *>(joint + 3 * 128) + local;
@@ -830,7 +843,7 @@ __device__ __forceinline__ bool loss_stats_by_turns(LossPipe &q, const LossArgs 
             }
             if (row - local % 32 < rows) {
                 s[1] = loss_columns(a, v, r.label - col0 - 64 * k, 64, a.V - col0 - 64 * k, row, c2, chosen);
-                s[0] = loss_all(s);
+                s[0] = loss_all(s, c2);
             }
         }
     }
@@ -838,32 +851,37 @@ __device__ __forceinline__ bool loss_stats_by_turns(LossPipe &q, const LossArgs 
     if (!(set ? loss_agree<2, kLossResults / 2>(ok) : loss_agree<1, kLossResults / 2>(ok))) return false;
     if (half == 0) {
         s[1] = LossStat{joint[local].x, joint[local].y};
-        loss_row_out(a, r, u.j, row, rows, loss_all(s), chosen);
+        loss_row_out(a, r, u.j, row, rows, loss_all(s, c2), chosen, scale);
     }
     return true;
 }
 
 // Where 16 bytes of a row of 64 lie in a piece: neither rows a lane nor four lanes a row meet a bank conflict.
 __device__ __forceinline__ uint32_t piece_at(int row, int chunk) { return row * 64 + ((chunk ^ (row >> 1 & 3)) << 4); }
+// (Up to eight rows have lse from other sums, loss_few_kernel's: p is held to 1 there, for a logit of 1e8 may come out ten above its lse.)
+__device__ __forceinline__ float loss_most_one(float p) { return p > 1.f ? 1.f : p; }   // (NaN stays)
 // Backward: q of 32 rows and 32 columns at a time, in 16 bits (halves), to G by way of shared memory, so that four lanes write 64 bytes of a row.
 template <int kPlanes>
-__device__ __forceinline__ void loss_weights(uint32_t piece, const LossArgs &a, const LossRow &r, float c2, int rows, int row, int local0, int cols, float (&v)[64]) {
+__device__ __forceinline__ void loss_weights(uint32_t piece, const LossArgs &a, const LossRow &r, float scale, int rows, int row, int local0, int cols, float (&v)[64]) {
     const int lane = threadIdx.x & 31, col0 = a.v0 + local0;
     const bool in = row < rows;
     const int at = r.label - col0;                                       // (no label: below zero)
-    const float lse2 = r.lse2, f = r.coef;
+    const float lse = r.lse, f = r.coef;
     const int words = in ? a.V - col0 : 0;
     // the label's, where it is among the columns: put into the piece on its own
     const bool mine = at >= 0 && at < cols;
     float own = 0.f;
-    if (__any_sync(0xffffffffu, mine)) own = (ptx::ex2(fmaf(loss_pick(v, at), c2, -lse2)) - 1.f) * f;
+    if (__any_sync(0xffffffffu, mine)) own = (loss_most_one(ptx::ex2(__fsub_rn(__fmul_rn(loss_pick(v, at), scale), lse) * kLossLog2e)) - 1.f) * f;
 #pragma unroll
     for (int k = 0; k < 64; k += 32) {
         if (k >= cols) break;
 #pragma unroll
         for (int e = 0; e < 32; e += 2) {
-            const float2 x = __ffma2_rn(make_float2(v[k + e], v[k + e + 1]), make_float2(c2, c2), make_float2(-lse2, -lse2));
-            const float2 y = __fmul2_rn(make_float2(ptx::ex2(x.x), ptx::ex2(x.y)), make_float2(f, f));
+            // (products one by one: two at a time came out fused with the addition, whatever their rounding said)
+            const float2 d = __fadd2_rn(make_float2(__fmul_rn(v[k + e], scale), __fmul_rn(v[k + e + 1], scale)), make_float2(-lse, -lse)), x = __fmul2_rn(d, make_float2(kLossLog2e, kLossLog2e));
+            float2 p = make_float2(ptx::ex2(x.x), ptx::ex2(x.y));
+            if (rows <= 8) p = make_float2(loss_most_one(p.x), loss_most_one(p.y));
+            const float2 y = __fmul2_rn(p, make_float2(f, f));
             v[k + e] = y.x;
             v[k + e + 1] = y.y;
         }
@@ -1032,7 +1050,7 @@ __global__ void __launch_bounds__(kLossThreads, 1) loss_kernel(const __grid_cons
         asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
         const int quad = warp & 3, part = (warp - 4) >> 2, lane = threadIdx.x & 31;
         const int cols = (kKind == kLossGrads ? a.grad_width : a.width) / 4;
-        const float c2 = a.scale * 1.4426950408889634f / (info.x_scale * info.w_scale);
+        const float scale = a.scale / (info.x_scale * info.w_scale);
         const uint32_t piece = q.pieces0 + (warp - 4) * kLossPiece;
         auto row_of = [&](const LossUnit &u) { return u.i * 256 + in_pair * 128 + quad * 32 + lane; };
         LossUnits<kKind> units(a, rows, pair, pairs);
@@ -1047,14 +1065,14 @@ __global__ void __launch_bounds__(kLossThreads, 1) loss_kernel(const __grid_cons
             r_next = loss_row<kKind>(a, rows, row_of(next), more && (kKind != kLossGrads || next.dx));
             const int row = row_of(u);
             if constexpr (kKind == kLossStats) {
-                if (!loss_stats<kPlanes>(q, a, u, r, c2, rows, row, cols, joint + (turn & 1) * kJoint)) break;
+                if (!loss_stats<kPlanes>(q, a, u, r, scale, rows, row, cols, joint + (turn & 1) * kJoint)) break;
             } else if constexpr (kKind == kLossTurns) {
-                if (!loss_stats_by_turns(q, a, u, r, c2, rows, row, joint + (2 * (part >> 1) + (turn & 1)) * kJoint)) break;
+                if (!loss_stats_by_turns(q, a, u, r, scale, rows, row, joint + (2 * (part >> 1) + (turn & 1)) * kJoint)) break;
                 q.c += 2;
             } else {
                 float v[64];
                 if (!loss_sums<kKind, kPlanes>(q, u.kb1 - u.kb0, cols, v)) break;
-                if constexpr (kKind == kLossWeights) loss_weights<kPlanes>(piece, a, r, c2, rows, row, u.j * a.width + part * cols, cols, v);
+                if constexpr (kKind == kLossWeights) loss_weights<kPlanes>(piece, a, r, scale, rows, row, u.j * a.width + part * cols, cols, v);
                 else if (u.slot >= 0) {
                     float *slot = a.slots + (((long)u.slot * 2 + in_pair) * a.grad_width + part * cols) * 128 + quad * 32 + lane;
 #pragma unroll
@@ -1185,8 +1203,8 @@ __global__ void __launch_bounds__(kFewThreads, R <= 2 ? 4 : 2) loss_few_kernel(c
     const int mine = lane >> kSkip, row = mine / kFewWords, word = mine % kFewWords;
     int64_t label = -1;
     if (row < a.rows) label = label_at(a.labels, a.wide, row);
-    const float c2 = a.scale * 1.4426950408889634f;
-    float m = -INFINITY, l = 0.f;
+    const float c2 = a.scale * kLossLog2e;
+    LossStat stat{-INFINITY, 0.f};
     __syncthreads();
     const int groups = (a.V + kFewWords - 1) / kFewWords;
     for (int g = blockIdx.x * (kFewThreads / 32) + warp; g < groups; g += gridDim.x * (kFewThreads / 32)) {
@@ -1243,24 +1261,20 @@ __global__ void __launch_bounds__(kFewThreads, R <= 2 ? 4 : 2) loss_few_kernel(c
         for (int o = (1 << kSkip) >> 1; o > 0; o >>= 1) s[0] += __shfl_xor_sync(0xffffffffu, s[0], o);
         const int v = g * kFewWords + word;
         if (v < a.V) {
-            const float y = s[0] * c2, next = fmaxf(m, y), ref = next == -INFINITY ? 0.f : next;
-            l = l * ptx::ex2(m - ref) + ptx::ex2(y - ref);
-            m = next;
-            if (v == label && (lane & ((1 << kSkip) - 1)) == 0) a.chosen[row] = y;
+            stat = loss_both(stat, LossStat{s[0], 1.f}, c2);
+            if (v == label && (lane & ((1 << kSkip) - 1)) == 0) a.chosen[row] = s[0];
         }
     }
-    stats[warp][lane] = make_float2(m, l);
+    stats[warp][lane] = make_float2(stat.m, stat.l);
     __syncthreads();
     if ((int)threadIdx.x < a.rows) {
-        m = -INFINITY, l = 0.f;
+        stat = LossStat{-INFINITY, 0.f};
         for (int u = 0; u < kFewThreads / 32; ++u)
             for (int k = 0; k < kFewWords; ++k) {
                 const float2 y = stats[u][(threadIdx.x * kFewWords + k) << kSkip];
-                const float next = fmaxf(m, y.x), ref = next == -INFINITY ? 0.f : next;
-                l = l * ptx::ex2(m - ref) + y.y * ptx::ex2(y.x - ref);
-                m = next;
+                stat = loss_both(stat, LossStat{y.x, y.y}, c2);
             }
-        a.part[(long)blockIdx.x * a.cap + threadIdx.x] = make_float2(m, l);
+        a.part[(long)blockIdx.x * a.cap + threadIdx.x] = make_float2(stat.m, stat.l);
     }
 }
 
@@ -1280,6 +1294,7 @@ struct LossMerge {
     const uint32_t *gave_up;
     uint32_t *status;
     int blocks;
+    float scale;
 };
 __global__ void __launch_bounds__(32 * kMergeWarps) loss_merge_kernel(const LossMerge a) {
     __shared__ float2 shared[kMergeWarps][32];
@@ -1292,40 +1307,37 @@ __global__ void __launch_bounds__(32 * kMergeWarps) loss_merge_kernel(const Loss
         code = __reduce_max_sync(0xffffffffu, code);
         for (int i = lane; i < (int)(kHeaderBytes / 4); i += 32) a.status[i] = i == 0 ? code : 0;
     }
+    const float scale = a.direct ? a.scale : a.scale / (a.info->x_scale * a.info->w_scale), c2 = scale * kLossLog2e;
     for (long r0 = (long)blockIdx.x * 32; r0 < rows; r0 += (long)gridDim.x * 32) {
         const long row = r0 + lane;
-        float m = -INFINITY, l = 0.f;
-        auto take = [&](float2 x) {
-            const float next = fmaxf(m, x.x), ref = next == -INFINITY ? 0.f : next;
-            l = l * ptx::ex2(m - ref) + x.y * ptx::ex2(x.x - ref);
-            m = next;
-        };
+        LossStat stat{-INFINITY, 0.f};
         if (row < rows) {
             int p = warp;
             for (; p < a.parts; p += 8 * warps) {
-                float2 x[8];
+                LossStat s[9];
 #pragma unroll
-                for (int k = 0; k < 8; ++k) x[k] = p + k * warps < a.parts ? a.part[(long)(p + k * warps) * a.cap + row] : make_float2(-INFINITY, 0.f);
-#pragma unroll
-                for (int k = 0; k < 8; ++k) take(x[k]);
+                for (int k = 0; k < 8; ++k) {
+                    const float2 x = p + k * warps < a.parts ? a.part[(long)(p + k * warps) * a.cap + row] : make_float2(-INFINITY, 0.f);
+                    s[k] = LossStat{x.x, x.y};
+                }
+                s[8] = stat;
+                stat = loss_all(s, c2);
             }
         }
         if (warps > 1) {
-            shared[warp][lane] = make_float2(m, l);
+            shared[warp][lane] = make_float2(stat.m, stat.l);
             __syncthreads();
         }
         if (warp == 0 && row < rows) {
-            for (int w = 1; w < warps; ++w) take(shared[w][lane]);
+            for (int w = 1; w < warps; ++w) stat = loss_both(stat, LossStat{shared[w][lane].x, shared[w][lane].y}, c2);
             bool there = true;
             if (a.direct) {
                 const int64_t label = label_at(a.labels, a.wide, row);
                 there = label >= 0 && label < a.V;
             }
-            // (m and the label's logit were rounded alike: where the label is the maximum nothing is left of their difference)
-            const float log_l = logf(l);
             const long n = a.direct ? row : a.index[row];
-            a.loss[n] = there ? (m - a.chosen[row]) * 0.69314718056f + log_l : 0.f;
-            a.lse[n] = there ? m * 0.69314718056f + log_l : 0.f;
+            a.loss[n] = there ? loss_of(stat, a.chosen[row], scale) : 0.f;
+            a.lse[n] = there ? loss_lse(stat, scale) : 0.f;
         }
         if (warps > 1) __syncthreads();
     }

@@ -1,0 +1,123 @@
+"""The loss over a vocabulary where sizes differ by many powers of two: logits far beyond what their differences need (needs a B200).
+
+Bounds, element by element, relative to a row's own magnitudes.  A logit is off by scale max_v sum_c |x_c w_c| E.  16-bit factors are multiplied exactly and added up 16 at a time with truncation,
+2^-22 of what has been added up for each addition (half a unit of 24 bits lost by the sum and as much by the alignment of what is added): width / 16 + 2 of them.  float32 factors are three bfloat16
+values each, which hold all 24 bits; of their nine products six are formed, the others are up to 2^-24 of it; 24 additions before a sum leaves tensor memory, and width / 64 rounded ones behind it.  lse is off by as
+much, by the additions of exponentials (a thread 128, then one per 2048 words, then 32 joins), 2^-24 each, by the exponentials (2^-22 each, and 2^-24 of an exponent of at most 40 that counts), and by
+its own rounding; p = exp(l - lse) by its share of both.
+"""
+import pytest
+import torch
+
+from paper_2508_12594_b200 import flare
+from tests._tokens import U32, UNIT, close
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+
+
+def problem(rows, vocab, width, dtype, size=1.0):
+    g = torch.Generator(device="cuda").manual_seed(rows + 7 * vocab + 13 * width)
+    x = (torch.randn(rows, width, device="cuda", generator=g) * size).to(dtype)
+    w = (torch.randn(vocab, width, device="cuda", generator=g) * 2.0 / (width ** 0.5 * size)).to(dtype)
+    labels = torch.randint(0, vocab, (rows,), device="cuda", generator=g)
+    labels[torch.rand(rows, device="cuda", generator=g) < 0.1] = -100
+    labels[0], labels[1] = 1, 2
+    return x, w, labels, g
+
+
+class Reference:
+    """Values and bounds of the rows that have a label, float64."""
+
+    def __init__(self, x, w, labels, dloss=1.0, scale=1.0):
+        T, (n, C), V = x.dtype, x.shape, w.shape[0]
+        there = (labels >= 0) & (labels < V)
+        x, w = torch.where(there[:, None], x.double(), 0.0), w.double()
+        l = scale * x @ w.T
+        at = labels.clamp(0, V - 1)[:, None]
+        zero = torch.zeros((), dtype=torch.float64, device="cuda")
+        self.lse = torch.where(there, torch.logsumexp(l, 1), zero)
+        self.loss = torch.where(there, self.lse - l.gather(1, at)[:, 0], zero)
+        E = 2.0 ** -24 + (24 + 2) * 2.0 ** -22 + (C / 64 + 2) * U32 if T == F32 else (C / 16 + 2) * 2.0 ** -22
+        size = scale * (x.abs() @ w.abs().T).max(1).values * E
+        sums = (128 + V / 2048 + 32 + 40 + 4) * U32
+        self.lse_bound = torch.where(there, size + sums + 4 * U32 * self.lse.abs() + 2.0 ** -22, zero)
+        self.loss_bound = torch.where(there, 2 * size + sums + 4 * U32 * (self.loss.abs() + 1) + 2.0 ** -22, zero)
+        p = torch.exp(l - self.lse[:, None])
+        q = p.scatter_add(1, at, -torch.ones_like(self.lse)[:, None])
+        g = torch.where(there, dloss if isinstance(dloss, torch.Tensor) else torch.full_like(self.lse, dloss), 0.0).double() * scale
+        self.dx, self.dw = g[:, None] * (q @ w), (g[:, None] * q).T @ x
+        # q: of p, of its difference from the label's 1, of its rounding: 24 bits (float32), two bfloat16 values' (bfloat16 where w has up to 2^22 elements), one's, or float16's and 2^-39
+        two = T == BF16 and V * C <= 1 << 22
+        u = U32 if T == F32 else 2.0 ** -17 if two else UNIT[T]
+        eps = (size + self.lse_bound + 2.0 ** -21 + 42 * U32)[:, None] * p + 2 * U32 * (q.abs() + p)
+        dq = (eps + q.abs() * u + (2.0 ** -39 if T == F16 else 0.0)) * there[:, None]
+        q, products = q.abs() * there[:, None], 2 if two else 1
+        steps_x, steps_w = (products * V / 16 + 76) * 2.0 ** -22, (products * n / 16 + 76) * 2.0 ** -22
+        if T == F32:
+            steps_x, steps_w = 2.0 ** -24 + 26 * 2.0 ** -22 + (V / 64 + 76) * U32, 2.0 ** -24 + 26 * 2.0 ** -22 + (n / 64 + 76) * U32
+        ga = g.abs()[:, None]
+        self.dx_bound = ga * (dq @ w.abs() + steps_x * (q @ w.abs())) + UNIT[T] * self.dx.abs()
+        self.dw_bound = (ga * dq).T @ x.abs() + steps_w * ((ga * q).T @ x.abs()) + UNIT[T] * self.dw.abs()
+        if T == F16:                                         # below the normal numbers: results; and x times a row's power of two, whose largest is between 2^14 and 2^15
+            self.dx_bound += 2.0 ** -25
+            self.dw_bound += 2.0 ** -25 + 2.0 ** -38 * (x.abs().max(1).values * g.abs()).max() * q.sum(0)[:, None]
+
+
+def run(x, w, labels, dloss=1.0, scale=1.0):
+    loss, lse = flare.token_loss(x, w, labels, scale=scale, check=True)
+    return (loss, lse, *flare.token_loss_backward(x, w, labels, lse, dloss, scale=scale, check=True))
+
+
+def held(got, r, rows=slice(None), words=slice(None)):
+    loss, lse, dx, dw = got
+    close(lse[rows], r.lse[rows], r.lse_bound[rows], "lse")
+    close(loss[rows], r.loss[rows], r.loss_bound[rows], "loss")
+    close(dx[rows], r.dx[rows], r.dx_bound[rows], "dx")
+    close(dw[words], r.dw[words], r.dw_bound[words], "dw")
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16], ids=str)
+@pytest.mark.parametrize("width", [64, 520, 1096])
+@pytest.mark.parametrize("vocab", [300, 2100])
+def test_logits_far_beyond_what_their_difference_needs(dtype, width, vocab):
+    """Certain rows with logits up to 1e8: their loss is 0 or the distance to the label, their p 1 or 0."""
+    x, w, labels, _ = problem(300, vocab, width, dtype)
+    scale = 1e7 if dtype == F16 else 0.7
+    if dtype != F16:
+        x = (x.float() * 1e8).to(dtype)
+    l = scale * (x.double() @ w.double().T)
+    top, two = l.argmax(1), l.topk(2, 1).values
+    labels = torch.where(torch.arange(300, device="cuda") % 2 == 0, top, labels)
+    certain = (two[:, 0] - two[:, 1] > 1e-3 * two[:, 0]) & (labels >= 0)
+    assert int(certain.sum()) > 150
+    loss, lse, dx, _ = run(x, w, labels, 1.0 / scale, scale)
+    r = Reference(x, w, labels, scale=scale)
+    close(lse[certain], r.lse[certain], r.lse_bound[certain], "lse")
+    close(loss[certain], r.loss[certain], r.loss_bound[certain], "loss")
+    learned = certain & (labels == top)
+    assert int(learned.sum()) > 100 and (loss[learned] == 0).all() and (dx[learned] == 0).all()
+    others = certain & ~learned
+    a, b = w.double()[top][others], w.double()[labels.clamp(min=0)][others]
+    close(dx[others], a - b, 4 * UNIT[dtype] * (a.abs() + b.abs()) + 2.0 ** -24, "dx")
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16], ids=str)
+@pytest.mark.parametrize("rows,width", [(1, 64), (3, 520), (4, 100), (8, 1001)])
+def test_logits_far_beyond_of_a_few_rows(dtype, rows, width):
+    """The same, scored by the kernels of few rows; there p is formed from other sums than lse and is not further than 1 from what it is."""
+    x, w, labels, _ = problem(300, 500, width, dtype)
+    scale = 1e7 if dtype == F16 else 0.7
+    x = x[:rows] if dtype == F16 else (x[:rows].float() * 1e8).to(dtype)
+    l = scale * (x.double() @ w.double().T)
+    labels = l.argmax(1)
+    two = l.topk(2, 1).values
+    certain = two[:, 0] - two[:, 1] > 1e-3 * two[:, 0]
+    loss, lse, dx, dw = run(x, w, labels, 1.0 / scale, scale)
+    r = Reference(x, w, labels, scale=scale)
+    close(lse, r.lse, r.lse_bound, "lse")
+    assert (loss[certain] == 0).all()
+    # (1 - p) w times dloss scale = 1: both and their product rounded to 2^-24, w held in at least 22 bits, dx rounded
+    most = w[labels].double().abs() * (1 + 2.0 ** -20 + UNIT[dtype]) + 2.0 ** -24
+    assert dw.isfinite().all() and (dx.double().abs()[certain] <= most[certain]).all()

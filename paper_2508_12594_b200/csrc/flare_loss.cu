@@ -31,8 +31,10 @@ int check_loss(const flare_loss_desc_t *d) {
 // 512 take 3.2 ms in pieces of 256 MB, 2.83 of 512, 2.97 of 1024; 18944 over 50021 of 256 take 2.34, 2.06, 1.97; 8192 over 128256 of 1024 take 6.6 in each.
 constexpr size_t kPieceBytes = 512u << 20;
 struct LossPlan {
-    int to;                      // what is multiplied: kAsIs, kToHalf, kToHalves
-    int planes, Cp, chunks, x_blocks, w_blocks, pairs;
+    int to;                      // what is multiplied: kAsIs, kToHalf, kToThree
+    bool bf16;                   // in bfloat16 (else float16)
+    int planes, g_planes;        // values of 16 bits to an element of X and W, of G
+    int Cp, chunks, x_blocks, w_blocks, pairs;
     long cap;
     int width;                   // of a tile of X W^T
     int Vp, pieces;              // words of a piece
@@ -50,20 +52,21 @@ LossPlan loss_plan(const flare_loss_desc_t *d, int sms, bool backward) {
     // bfloat16's G would be off by 2^-9 (its rms 1.7e-3, as much again as the rounding of the results): where W is small enough for another pass over it not to count, it, X and G are float16.  (That costs a tenth: a step
     // over 2000 rows, 4096 words, C = 1024 takes 102.5 us instead of 93, one over 131072 rows, 256 words, C = 128 takes 148 instead of 130; its error against 64 bits is 1.05 times that of rounding alone instead of 1.4.)
     const bool bf16_small = d->dtype == FLARE_DTYPE_BF16 && backward && (long)d->vocab * d->width <= (4L << 20);
-    p.to = f32 ? kToHalves : bf16_small ? kToHalf : kAsIs;
-    p.planes = f32 ? 2 : 1;
+    p.to = f32 ? kToThree : bf16_small ? kToHalf : kAsIs;
+    p.bf16 = f32 || (d->dtype == FLARE_DTYPE_BF16 && !bf16_small);
+    p.planes = p.g_planes = f32 ? 3 : 1;
     // rows of packed X and W: whole 16 bytes, of wide ones whole lines (TMA takes 128-byte pieces of them)
     p.Cp = d->width > 256 ? (d->width + 63) / 64 * 64 : (d->width + 7) / 8 * 8;
     p.chunks = (int)((d->rows + kLossChunk - 1) / kLossChunk);
     p.pairs = std::max(1, sms / 2);
     p.cap = std::max(1L, (long)(d->rows + 255) / 256) * 256;
     p.width = tile_width(p.cap / 256, d->vocab, p.pairs);
-    if (p.to != kAsIs) {
+    if (p.to == kToHalf) {
         auto blocks = [&](long rows) { return (int)std::max(1L, std::min(4L * sms, rows * d->width / 8192)); };
         p.x_blocks = blocks(d->rows);
         p.w_blocks = blocks(d->vocab);
     }
-    const long words = ((long)d->vocab + 255) / 256 * 256, most = std::max(256L, (long)(kPieceBytes / (2 * p.planes * p.cap)) / 256 * 256);
+    const long words = ((long)d->vocab + 255) / 256 * 256, most = std::max(256L, (long)(kPieceBytes / (2 * p.g_planes * p.cap)) / 256 * 256);
     p.pieces = (int)((words + most - 1) / most);
     p.Vp = (int)((words / 256 + p.pieces - 1) / p.pieces * 256);
     p.pieces = (int)((words + p.Vp - 1) / p.Vp);
@@ -102,11 +105,11 @@ LossLayout loss_layout(const flare_loss_desc_t *d, const LossPlan &p, bool backw
         take(w.chosen, sizeof(float) * (size_t)p.cap);
         take(w.gave_up, sizeof(uint32_t) * 2 * (size_t)p.pairs);
     } else {
-        take(w.pd, d->dtype == FLARE_DTYPE_BF16 && p.to == kAsIs ? 0 : row * p.cap);
+        take(w.pd, p.bf16 ? 0 : row * p.cap);
         take(w.lse_of, sizeof(float) * (size_t)p.cap);
         take(w.gm, sizeof(float) * (size_t)p.cap);
         take(w.coef, sizeof(float) * (size_t)p.cap);
-        take(w.g, sizeof(uint16_t) * (size_t)p.planes * p.cap * p.Vp);
+        take(w.g, sizeof(uint16_t) * (size_t)p.g_planes * p.cap * p.Vp);
         take(w.acc, p.pieces > 1 ? sizeof(float) * (size_t)p.cap * p.tiles_c * p.grad_width : 0);
         take(w.slots, sizeof(float) * 4 * (size_t)p.pairs * p.grad_width * 128);
     }
@@ -133,10 +136,10 @@ int make_plane_map(CUtensorMap *m, const void *base, bool bf16, long cols, long 
     return FLARE_OK;
 }
 
-template <int kKind, int kPlanes, typename E>
+template <int kKind, int kF, int kG, typename E>
 int launch_loss(const LossMaps &maps, const LossArgs &a, int pairs, cudaStream_t st) {
     static std::atomic<uint64_t> opt_in{0};
-    auto *kernel = loss_kernel<kKind, kPlanes, E>;
+    auto *kernel = loss_kernel<kKind, kF, kG, E>;
     if (int rc = ensure_big_smem(kernel, opt_in, (int)kLossSmem)) return rc;
     cudaLaunchAttribute attr[2] = {};
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -198,7 +201,7 @@ int check_loss_call(const flare_loss_desc_t *d, const void *x, const void *w, co
 // Scan and packing, and the maps of X and W; what only the backward has is in k already.
 int prepare_loss(const flare_loss_desc_t *d, const LossPlan &p, const LossLayout &l, char *ws, const void *x, const void *w, const void *labels, LossPack k, LossMaps *maps,
                  LossArgs *a, cudaStream_t st) {
-    const bool f32 = d->dtype == FLARE_DTYPE_F32, bf16 = d->dtype == FLARE_DTYPE_BF16 && p.to == kAsIs;
+    const bool f32 = d->dtype == FLARE_DTYPE_F32, bf16 = p.bf16;
     const long ld_x = d->stride_x ? d->stride_x : d->width, ld_w = d->stride_w ? d->stride_w : d->width;
     const bool own_w = p.to != kAsIs || !aligned16(w) || ld_w % 8 != 0;
     LossScan s{};
@@ -212,7 +215,7 @@ int prepare_loss(const flare_loss_desc_t *d, const LossPlan &p, const LossLayout
     // rows of a block: so many that a thread has four groups of columns, and that there are no more than four blocks an SM; whole parts of a chunk
     k.pack_rows = 4;
     while (k.pack_rows < kLossChunk && ((long)k.pack_rows * (p.Cp / 8) < 4 * kPackThreads || (long)k.pack_rows * 4 * device_info().sms < d->rows)) k.pack_rows *= 2;
-    const bool alone = d->rows <= kPackAlone && p.to == kAsIs && k.pack_rows <= kPackThreads;
+    const bool alone = d->rows <= kPackAlone && p.to != kToHalf && k.pack_rows <= kPackThreads;
     if (!alone && (rc = f32 ? launch_scan<float>(s, st) : d->dtype == FLARE_DTYPE_BF16 ? launch_scan<__nv_bfloat16>(s, st) : launch_scan<__half>(s, st)) != FLARE_OK) return rc;
     k.labels = labels; k.x = x; k.w = w; k.wide = s.wide; k.rows = d->rows; k.cap = p.cap; k.ld_x = ld_x; k.ld_w = ld_w;
     k.w_rows = own_w ? d->vocab : 0; k.C = d->width; k.Cp = p.Cp; k.V = d->vocab; k.chunks = p.chunks; k.x_blocks = p.x_blocks; k.w_blocks = p.w_blocks;
@@ -222,7 +225,7 @@ int prepare_loss(const flare_loss_desc_t *d, const LossPlan &p, const LossLayout
     k.px = reinterpret_cast<uint16_t *>(ws + l.px); k.pw = reinterpret_cast<uint16_t *>(ws + l.pw);
     k.index = reinterpret_cast<int *>(ws + l.index); k.label = reinterpret_cast<int *>(ws + l.label);
     const int blocks = k.pack_blocks + (int)std::min<long>((k.w_rows * (p.Cp / 8) + 4 * kPackThreads - 1) / (4 * kPackThreads), 16L * device_info().sms);
-    if ((rc = f32                             ? launch_pack<float, kToHalves>(k, blocks, st)
+    if ((rc = f32                             ? launch_pack<float, kToThree>(k, blocks, st)
               : d->dtype == FLARE_DTYPE_F16   ? launch_pack<__half, kAsIs>(k, blocks, st)
               : p.to == kToHalf               ? launch_pack<__nv_bfloat16, kToHalf>(k, blocks, st)
                                               : launch_pack<__nv_bfloat16, kAsIs>(k, blocks, st)) != FLARE_OK)
@@ -302,7 +305,7 @@ int flare_loss_forward(const flare_loss_desc_t *desc, const void *x, const void 
     if (a.tiles_v == 1 && !direct) { a.loss = loss; a.lse = lse; }
     const int pairs = (int)std::min<long>(p.pairs, p.cap / 256 * a.tiles_v);
     // (products of few steps, whose ends bound the tile, in turns: 37137 rows over 25943 words of 128 take 356 us instead of 444, 5003 over 10007 of 512 45.7 and 46.2)
-    auto stats = p.planes == 2 ? launch_loss<kLossStats, 2, float> : desc->width <= 64 * kLossDeep<kLossTurns, 1> ? launch_loss<kLossTurns, 1, float> : launch_loss<kLossStats, 1, float>;
+    auto stats = p.planes == 3 ? launch_loss<kLossStats, 3, 1, float> : desc->width <= 64 * kLossDeep<kLossTurns, 1> ? launch_loss<kLossTurns, 1, 1, float> : launch_loss<kLossStats, 1, 1, float>;
     if (int rc = stats(maps, a, pairs, st)) return rc;
     if (a.loss) return FLARE_OK;
     LossMerge m{};
@@ -326,12 +329,12 @@ int flare_loss_backward(const flare_loss_desc_t *desc, const void *x, const void
     }
     const LossPlan p = loss_plan(desc, device_info().sms, true);
     const LossLayout l = loss_layout(desc, p, true);
-    const bool f32 = desc->dtype == FLARE_DTYPE_F32, bf16 = desc->dtype == FLARE_DTYPE_BF16 && p.to == kAsIs;   // (bf16: what is multiplied)
+    const bool f32 = desc->dtype == FLARE_DTYPE_F32, bf16 = p.bf16;
     char *ws = static_cast<char *>(workspace);
     LossPack k{};
     k.lse_in = lse; k.dloss = dloss; k.mult = desc->scale * desc->dloss_scale;
     k.lse_of = reinterpret_cast<float *>(ws + l.lse_of); k.gm = reinterpret_cast<float *>(ws + l.gm); k.coef = reinterpret_cast<float *>(ws + l.coef);
-    // bfloat16's G: q where one dloss is that of all rows (a label's q is next to -1, which is no rounding), else times it, for a second X would be a second rounding; float16's: q times 2^15, or times 2^14 and a row's
+    // G in bfloat16: q where one dloss is that of all rows (a label's q is next to -1, which is no rounding), else times it, for a second X would be a second rounding; in float16: q times 2^15, or times 2^14 and a row's
     // mantissa of dloss, below 2
     k.g_factor = !bf16 ? dloss ? 16384.f : 32768.f : dloss ? 0.f : 1.f;
     k.dx = dx; k.ld_dx = ld_dx;
@@ -345,7 +348,7 @@ int flare_loss_backward(const flare_loss_desc_t *desc, const void *x, const void
     } else {
         maps.d = maps.x;
     }
-    if ((rc = make_plane_map(&maps.g, ws + l.g, bf16, p.Vp, p.cap, p.planes, p.Vp, 64)) != FLARE_OK) return rc;
+    if ((rc = make_plane_map(&maps.g, ws + l.g, bf16, p.Vp, p.cap, p.g_planes, p.Vp, 64)) != FLARE_OK) return rc;
     a.g = reinterpret_cast<uint16_t *>(ws + l.g); a.ld_g = p.Vp;
     a.lse_of = k.lse_of; a.gm = k.gm; a.coef = k.coef; a.grad_width = p.grad_width; a.tiles_c = p.tiles_c;
     a.dw = dw; a.dx = dx; a.ld_dw = ld_dw; a.ld_dx = ld_dx;
@@ -353,8 +356,8 @@ int flare_loss_backward(const flare_loss_desc_t *desc, const void *x, const void
     a.dw_vec = vec(dw, ld_dw); a.dx_vec = vec(dx, ld_dx);
     a.dw_factor = k.g_factor != 0.f ? k.mult / k.g_factor : 1.f;
     a.acc = reinterpret_cast<float *>(ws + l.acc); a.slots = reinterpret_cast<float *>(ws + l.slots);
-    auto weights = f32 ? launch_loss<kLossWeights, 2, float> : launch_loss<kLossWeights, 1, float>;
-    auto grads = f32 ? launch_loss<kLossGrads, 2, float> : desc->dtype == FLARE_DTYPE_BF16 ? launch_loss<kLossGrads, 1, __nv_bfloat16> : launch_loss<kLossGrads, 1, __half>;
+    auto weights = f32 ? launch_loss<kLossWeights, 3, 3, float> : launch_loss<kLossWeights, 1, 1, float>;
+    auto grads = f32 ? launch_loss<kLossGrads, 3, 3, float> : desc->dtype == FLARE_DTYPE_BF16 ? launch_loss<kLossGrads, 1, 1, __nv_bfloat16> : launch_loss<kLossGrads, 1, 1, __half>;
     auto *join = f32 ? loss_join_kernel<float> : desc->dtype == FLARE_DTYPE_BF16 ? loss_join_kernel<__nv_bfloat16> : loss_join_kernel<__half>;
     // of tiles that several pairs can have shared: fewer than a round of either gradient
     const long warps = 2L * (p.pairs - 1) * 8 * (p.grad_width / kJoinCols);

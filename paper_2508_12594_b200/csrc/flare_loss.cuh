@@ -20,8 +20,9 @@
 // (2^-9, as the gradients themselves will be; dloss in a second X instead put the same rounding there, and as many more elements were moved).  float16's G is q times 2^15, so that probabilities down to 2^-29 are
 // normal numbers; of a row's own dloss its mantissa is there too (q times 2^14 and up to 2) and its power of two, which rounds nothing, in a second X and in dX's rows.  Small vocabularies in bfloat16 take float16's way
 // backward, X and W times powers of two.
-// float32: X, W, G as two float16 halves each (22 bits; X and W times a power of two that puts their largest near 2^15, held down to 2^-39 of it), a
-// product as three, and sums leave tensor memory, which truncates, every 128 of K to be added up in registers.
+// float32: X, W, G as three bfloat16 values each, which hold all 24 bits over all of float32's range, a product as the six of them that are above 2^-24 of it; sums leave tensor memory, which
+// truncates, every 64 of K to be added up in registers.  (Two float16 halves, 22 bits, take three products, but want one power of two for all of X, of W and of a row's dloss: an element
+// of 1e9 in one row put the others' losses off by 3e-3, one of 1e13 by 4.)
 #pragma once
 
 #include <type_traits>
@@ -34,7 +35,7 @@ namespace flare {
 // What the packing leaves for the kernels behind it, on the device.
 struct LossInfo {
     uint32_t rows;               // with a label
-    float x_scale, w_scale;      // of the halves (1 but for float32)
+    float x_scale, w_scale;      // of what is multiplied in float16 though it is not (else 1)
     float dmax;                  // where dloss is in the second X: the power of two of the largest of a row, else 1
 };
 // Per 1024 rows.
@@ -213,13 +214,35 @@ __device__ __forceinline__ float half_scale(float most) {
     frexpf(most, &e);                         // most < 2^e
     return ldexpf(1.f, min(max(15 - e, -60), 60));
 }
-// What the products multiply: the type as it is, or float16 times a power of two (one of bfloat16's values, two halves of float32's).
-enum { kAsIs = 0, kToHalf = 1, kToHalves = 2 };
+// What the products multiply: the type as it is; bfloat16 as float16 times a power of two; float32 as three bfloat16 values, each what rounding to those before it has left.
+enum { kAsIs = 0, kToHalf = 1, kToThree = 2 };
+template <int kTo> constexpr int kPacked = kTo == kToThree ? 3 : 1;
+__device__ __forceinline__ void three_of(float v, uint16_t (&t)[3]) {
+    __nv_bfloat16 h = fabsf(v) > 3.3895314e38f ? __float2bfloat16_rz(v) : __float2bfloat16_rn(v);         // (beyond bfloat16's largest: not to infinity)
+    t[0] = __bfloat16_as_ushort(h);
+    float left = fabsf(v) <= 3.4028234e38f ? v - __bfloat162float(h) : 0.f;
+    h = __float2bfloat16_rn(left);
+    t[1] = __bfloat16_as_ushort(h);
+    t[2] = __bfloat16_as_ushort(__float2bfloat16_rn(left - __bfloat162float(h)));
+}
 // Eight columns times f, into their planes; as they are where not `scaled`.
 template <typename T, int kTo>
 __device__ __forceinline__ void pack_eight(const LossEight<T> &e, float f, bool scaled, uint16_t *out, long plane) {
     const T *t = reinterpret_cast<const T *>(e.q);
-    __align__(16) uint16_t h[8], l[8];
+    __align__(16) uint16_t h[8];
+    if constexpr (kTo == kToThree) {
+        __align__(16) uint16_t m[8], l[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            uint16_t three[3];
+            three_of(to_f32(t[i]), three);
+            h[i] = three[0]; m[i] = three[1]; l[i] = three[2];
+        }
+        *reinterpret_cast<uint4 *>(out) = *reinterpret_cast<const uint4 *>(h);
+        *reinterpret_cast<uint4 *>(out + plane) = *reinterpret_cast<const uint4 *>(m);
+        *reinterpret_cast<uint4 *>(out + 2 * plane) = *reinterpret_cast<const uint4 *>(l);
+        return;
+    }
     if constexpr (kTo == kAsIs) {
         if (!scaled) {
             *reinterpret_cast<uint4 *>(out) = e.q[0];
@@ -234,12 +257,9 @@ __device__ __forceinline__ void pack_eight(const LossEight<T> &e, float f, bool 
             from_f32(u, v);
             h[i] = *reinterpret_cast<const uint16_t *>(&u);
         } else {
-            const __half hi = __float2half_rn(v);
-            h[i] = __half_as_ushort(hi);
-            if constexpr (kTo == kToHalves) l[i] = __half_as_ushort(__float2half_rn(v - __half2float(hi)));
+            h[i] = __half_as_ushort(__float2half_rn(v));
         }
     }
-    if constexpr (kTo == kToHalves) *reinterpret_cast<uint4 *>(out + plane) = *reinterpret_cast<const uint4 *>(l);
     *reinterpret_cast<uint4 *>(out) = *reinterpret_cast<const uint4 *>(h);
 }
 template <typename T, int kTo>
@@ -251,7 +271,7 @@ __global__ void __launch_bounds__(kPackThreads) loss_pack_kernel(const LossPack 
     ptx::grid_launch();
     ptx::grid_wait();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    constexpr bool kScaled = kTo != kAsIs;
+    constexpr bool kScaled = kTo == kToHalf;
     constexpr int kBatch = 4;                                 // groups of eight columns that are asked for before the first is stored
     const uint32_t groups = (uint32_t)a.Cp / 8;
     float sx = 1.f, sw = 1.f;
@@ -389,7 +409,7 @@ __global__ void __launch_bounds__(kPackThreads) loss_pack_kernel(const LossPack 
     if (a.loss == nullptr) {
         const long end = min(a.cap, ((long)max(total, 1u) + 63) / 64 * 64);
         for (long r = total + (long)blockIdx.x * (kPackThreads / 32) + warp; r < end; r += (long)a.pack_blocks * (kPackThreads / 32))
-            for (int h = 0; h < (kTo == kToHalves ? 2 : 1); ++h)
+            for (int h = 0; h < kPacked<kTo>; ++h)
                 for (int c = lane * 8; c < a.Cp; c += 256) {
                     *reinterpret_cast<uint4 *>(a.px + h * plane + r * a.Cp + c) = make_uint4(0, 0, 0, 0);
                     if (a.pd) *reinterpret_cast<uint4 *>(a.pd + h * plane + r * a.Cp + c) = make_uint4(0, 0, 0, 0);
@@ -403,14 +423,14 @@ __host__ __device__ constexpr bool loss_forward(int kind) { return kind == kLoss
 constexpr int kLossThreads = 640, kLossResults = 16;          // warp 0 loads, warp 1 issues, warps 4 to 19 take the sums out of tensor memory
 constexpr uint32_t kLossHalfTile = 128 * 128;                 // bytes: 128 rows (or 64 rows of two blocks of columns) of 64 elements
 constexpr uint32_t kLossPiece = 2048;                         // a warp's piece of a result on its way out: 32 rows of 64 bytes
-template <int kPlanes> struct LossShape {
-    static constexpr int kStages = kPlanes == 1 ? 6 : 3;
-    static constexpr uint32_t kStage = 2 * kPlanes * kLossHalfTile;        // A (high, low), B (high, low)
+// kA, kB: values of 16 bits that an element of a product's two factors is held in; what they come to are the products of the i-th and the j-th of them with i + j below the larger number.
+template <int kA, int kB> struct LossShape {
+    static constexpr int kStages = 12 / (kA + kB), kProducts = kA > kB ? kA : kB;
+    static constexpr uint32_t kStage = (kA + kB) * kLossHalfTile;
 };
-// 64-deep steps whose sums stay in tensor memory, where every addition truncates: of halves 2 (12 x 2 additions: gradients off by 5e-7 to 6.6e-7; with 4
-// by 8e-7 to 1.2e-6 in 0 to 4 % less time, with 1 by 3e-7 to 4e-7 in 5 to 20 % more); of 16-bit factors' logits 8 (a loss over 4096 columns is off by 2e-6 with all of
+// 64-deep steps whose sums stay in tensor memory, where every addition truncates: of float32 1 (6 x 4 additions: gradients off by 3.8e-7 to 4.0e-7); of 16-bit factors' logits 8 (a loss over 4096 columns is off by 2e-6 with all of
 // them there; the same forward and backward, so that both have the same logits); of the gradients, whose results are rounded to 2^-9 or 2^-12, 64.
-template <int kKind, int kPlanes> constexpr int kLossDeep = kPlanes == 2 ? 2 : kKind != kLossGrads ? 8 : 64;
+template <int kKind, int kF> constexpr int kLossDeep = kF == 3 ? 1 : kKind != kLossGrads ? 8 : 64;
 constexpr size_t kLossSmem = 1024 + 6 * 2 * kLossHalfTile + kLossResults * kLossPiece + 256;
 
 struct LossMaps { CUtensorMap x, d, w, g; };                  // in boxes of 64 x 64
@@ -585,9 +605,9 @@ struct LossPipe {
 };
 
 // The loading warp's part.
-template <int kKind, int kPlanes>
+template <int kKind, int kA, int kB>
 __device__ __forceinline__ void loss_load(LossPipe &q, const LossMaps &m, const LossArgs &a, int rows, int pair, int pairs) {
-    using Shape = LossShape<kPlanes>;
+    using Shape = LossShape<kA, kB>;
     if (!ptx::elect_one()) return;
     const int in_pair = (int)(blockIdx.x & 1);
     asm volatile("fence.proxy.async.global;" ::: "memory");              // (what was stored by the kernels before this, for the loads by TMA)
@@ -599,33 +619,36 @@ __device__ __forceinline__ void loss_load(LossPipe &q, const LossMaps &m, const 
         for (int kb = u.kb0; kb < u.kb1; ++kb, ++q.n) {
             const uint32_t s = q.n % Shape::kStages;
             if (q.n >= Shape::kStages && !ptx::mbar_wait(q.empty(s), (q.n / Shape::kStages - 1) & 1, q.abort_flag, 111)) return;
-            const uint32_t at = q.smem0 + s * Shape::kStage, bar = ptx::in_block(q.full(s), 0), bt = at + kPlanes * kLossHalfTile;
-            if (in_pair == 0) ptx::mbar_arrive_expect_tx(q.full(s), 2 * kPlanes * (kLossHalfTile + right * 128));
+            const uint32_t at = q.smem0 + s * Shape::kStage, bar = ptx::in_block(q.full(s), 0), bt = at + kA * kLossHalfTile;
+            if (in_pair == 0) ptx::mbar_arrive_expect_tx(q.full(s), 2 * (kA * kLossHalfTile + kB * right * 128));
 #pragma unroll
-            for (int h = 0; h < kPlanes; ++h)
+            for (int h = 0; h < kA; ++h)
 #pragma unroll
                 for (int r = 0; r < 2; ++r) {
-                    const uint32_t pa = at + h * kLossHalfTile + r * 8192, pb = bt + h * kLossHalfTile + r * 8192;
-                    if (kKind != kLossGrads) {
-                        ptx::tma_load_3d_for<2>(pa, &m.x, bar, kb * 64, ra + r * 64, h);
-                        if (r * 64 < right) ptx::tma_load_3d_for<2>(pb, &m.w, bar, kb * 64, a.v0 + rb + r * 64, h);
-                    } else if (u.dx) {
-                        ptx::tma_load_3d_for<2>(pa, &m.g, bar, kb * 64, ra + r * 64, h);
-                        if (r * 64 < right) ptx::tma_load_3d_for<2>(pb, &m.w, bar, rb + r * 64, a.v0 + kb * 64, h);
-                    } else {
-                        ptx::tma_load_3d_for<2>(pa, &m.g, bar, ra + r * 64, kb * 64, h);
-                        if (r * 64 < right) ptx::tma_load_3d_for<2>(pb, &m.d, bar, rb + r * 64, kb * 64, h);
-                    }
+                    const uint32_t pa = at + h * kLossHalfTile + r * 8192;
+                    if (kKind != kLossGrads) ptx::tma_load_3d_for<2>(pa, &m.x, bar, kb * 64, ra + r * 64, h);
+                    else if (u.dx) ptx::tma_load_3d_for<2>(pa, &m.g, bar, kb * 64, ra + r * 64, h);
+                    else ptx::tma_load_3d_for<2>(pa, &m.g, bar, ra + r * 64, kb * 64, h);
+                }
+#pragma unroll
+            for (int h = 0; h < kB; ++h)
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    const uint32_t pb = bt + h * kLossHalfTile + r * 8192;
+                    if (r * 64 >= right) continue;
+                    if (kKind != kLossGrads) ptx::tma_load_3d_for<2>(pb, &m.w, bar, kb * 64, a.v0 + rb + r * 64, h);
+                    else if (u.dx) ptx::tma_load_3d_for<2>(pb, &m.w, bar, rb + r * 64, a.v0 + kb * 64, h);
+                    else ptx::tma_load_3d_for<2>(pb, &m.d, bar, rb + r * 64, kb * 64, h);
                 }
         }
     }
 }
 // The issuing warp's part (its pair's first block's).
-template <int kKind, int kPlanes>
+template <int kKind, int kA, int kB>
 __device__ __forceinline__ void loss_issue(LossPipe &q, const LossArgs &a, int rows, int pair, int pairs) {
-    using Shape = LossShape<kPlanes>;
+    using Shape = LossShape<kA, kB>;
     if (!ptx::elect_one()) return;
-    constexpr uint32_t hi = ptx::desc_hi(1024, 2), low = kLossHalfTile >> 4;
+    constexpr uint32_t hi = ptx::desc_hi(1024, 2), value = kLossHalfTile >> 4;
     LossUnits<kKind> units(a, rows, pair, pairs);
     LossUnit u;
     while (units.next(u)) {
@@ -639,20 +662,23 @@ __device__ __forceinline__ void loss_issue(LossPipe &q, const LossArgs &a, int r
             const uint32_t acc = q.tmem + (q.c & 1) * 256;
             if (q.c >= 2 && !ptx::mbar_wait(q.acc_empty(q.c & 1), (q.c / 2 - 1) & 1, q.abort_flag, 112)) return;
             ptx::tc_fence_after();
-            for (int k1 = min(kb + kLossDeep<kKind, kPlanes>, u.kb1), first = 1; kb < k1; ++kb, ++q.n, first = 0) {
+            for (int k1 = min(kb + kLossDeep<kKind, kB>, u.kb1), first = 1; kb < k1; ++kb, ++q.n, first = 0) {
                 const uint32_t s = q.n % Shape::kStages;
                 if (!ptx::mbar_wait(q.full(s), (q.n / Shape::kStages) & 1, q.abort_flag, 113)) return;
                 ptx::tc_fence_after();
                 const uint32_t at = q.smem0 + s * Shape::kStage;
-                const uint32_t a0 = ptx::desc_lo(at, a_lbo), b0 = ptx::desc_lo(at + kPlanes * kLossHalfTile, b_lbo);
+                const uint32_t a0 = ptx::desc_lo(at, a_lbo), b0 = ptx::desc_lo(at + kA * kLossHalfTile, b_lbo);
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {                             // (what lies beyond K is zeros)
-                    const uint32_t x = a0 + k * a_step, y = b0 + k * b_step;
-                    if (kPlanes == 2) {
-                        ptx::mma_ss_for<2>(acc, ptx::desc(x + low, hi), ptx::desc(y, hi), idesc, !first || k > 0);
-                        ptx::mma_ss_for<2>(acc, ptx::desc(x, hi), ptx::desc(y + low, hi), idesc, 1);
-                    }
-                    ptx::mma_ss_for<2>(acc, ptx::desc(x, hi), ptx::desc(y, hi), idesc, kPlanes == 2 || !first || k > 0);
+                    uint32_t more = !first || k > 0;
+#pragma unroll
+                    for (int t = Shape::kProducts - 1; t >= 0; --t)       // (small ones first)
+#pragma unroll
+                        for (int i = 0; i < kA; ++i) {
+                            if (t - i < 0 || t - i >= kB) continue;
+                            ptx::mma_ss_for<2>(acc, ptx::desc(a0 + k * a_step + i * value, hi), ptx::desc(b0 + k * b_step + (t - i) * value, hi), idesc, more);
+                            more = 1;
+                        }
                 }
                 ptx::mma_commit_for<2>(q.empty(s));
             }
@@ -662,11 +688,11 @@ __device__ __forceinline__ void loss_issue(LossPipe &q, const LossArgs &a, int r
 }
 
 // The result warps' parts.  A unit's sums into registers, a row a thread and a quarter of the tile's columns (`cols`, 64 or 32): false if a wait gave up.
-template <int kKind, int kPlanes>
+template <int kDeep>
 __device__ __forceinline__ bool loss_sums(LossPipe &q, int deep, int cols, float (&v)[64]) {
     const int warp = ptx::warp_index(), quad = warp & 3, part = (warp - 4) >> 2;
     const uint32_t acc = q.tmem + ((uint32_t)(quad * 32) << 16) + part * cols;
-    for (int kb = 0; kb < deep; kb += kLossDeep<kKind, kPlanes>, ++q.c) {
+    for (int kb = 0; kb < deep; kb += kDeep, ++q.c) {
         const bool ok = ptx::mbar_wait(q.acc_full(q.c & 1), (q.c / 2) & 1, q.abort_flag, 114);
         if (!__all_sync(0xffffffffu, ok)) return false;
         ptx::tc_fence_after();
@@ -799,13 +825,13 @@ __device__ __forceinline__ LossStat loss_columns(const LossArgs &a, float (&v)[6
 }
 constexpr int kJoint = 4 * 128;                               // float2 of a place; places are written in turn: one again behind the next tile's barrier
 // A tile by all sixteen warps, a quarter of the columns each.
-template <int kPlanes>
+template <int kF>
 __device__ __forceinline__ bool loss_stats(LossPipe &q, const LossArgs &a, const LossUnit &u, const LossRow &r, float scale, int rows, int row, int cols, float2 *joint) {
     const float c2 = scale * kLossLog2e;
     const int warp = ptx::warp_index(), part = (warp - 4) >> 2, local = (warp & 3) * 32 + (threadIdx.x & 31), col0 = u.j * a.width + part * cols;
     float *chosen = reinterpret_cast<float *>(joint + 3 * 128) + local;
     float v[64];
-    const bool ok = loss_sums<kLossStats, kPlanes>(q, u.kb1, cols, v);
+    const bool ok = loss_sums<kLossDeep<kLossStats, kF>>(q, u.kb1, cols, v);
     LossStat s[4] = {{-INFINITY, 0.f}, {-INFINITY, 0.f}, {-INFINITY, 0.f}, {-INFINITY, 0.f}};
     if (ok && row - local % 32 < rows) s[0] = loss_columns(a, v, r.label - col0, cols, a.V - col0, row, c2, chosen);   // (some of the warp's rows are rows)
     if (part > 0) joint[(part - 1) * 128 + local] = make_float2(s[0].m, s[0].l);
@@ -860,8 +886,8 @@ __device__ __forceinline__ bool loss_stats_by_turns(LossPipe &q, const LossArgs 
 __device__ __forceinline__ uint32_t piece_at(int row, int chunk) { return row * 64 + ((chunk ^ (row >> 1 & 3)) << 4); }
 // (Up to eight rows have lse from other sums, loss_few_kernel's: p is held to 1 there, for a logit of 1e8 may come out ten above its lse.)
 __device__ __forceinline__ float loss_most_one(float p) { return p > 1.f ? 1.f : p; }   // (NaN stays)
-// Backward: q of 32 rows and 32 columns at a time, in 16 bits (halves), to G by way of shared memory, so that four lanes write 64 bytes of a row.
-template <int kPlanes>
+// Backward: q of 32 rows and 32 columns at a time, as kG values of 16 bits, to G by way of shared memory, so that four lanes write 64 bytes of a row.
+template <int kG>
 __device__ __forceinline__ void loss_weights(uint32_t piece, const LossArgs &a, const LossRow &r, float scale, int rows, int row, int local0, int cols, float (&v)[64]) {
     const int lane = threadIdx.x & 31, col0 = a.v0 + local0;
     const bool in = row < rows;
@@ -891,7 +917,7 @@ __device__ __forceinline__ void loss_weights(uint32_t piece, const LossArgs &a, 
                 if (e >= words - k) v[k + e] = 0.f;
         }
 #pragma unroll
-        for (int h = 0; h < kPlanes; ++h) {
+        for (int h = 0; h < kG; ++h) {
             __syncwarp();
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -899,26 +925,27 @@ __device__ __forceinline__ void loss_weights(uint32_t piece, const LossArgs &a, 
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     float &x = v[k + 8 * e + 2 * i], &y = v[k + 8 * e + 2 * i + 1];
-                    if (kPlanes == 1 && a.bf16) w[i] = ptx::pack_bf16(x, y);
-                    else {
+                    if (kG > 1 || a.bf16) {
+                        w[i] = ptx::pack_bf16(x, y);
+                        if (h + 1 < kG) {                                 // (what is left is the next one's)
+                            x -= __uint_as_float(w[i] << 16);
+                            y -= __uint_as_float(w[i] & 0xffff0000u);
+                        }
+                    } else {
                         const __half2 t = __floats2half2_rn(x, y);
                         w[i] = *reinterpret_cast<const uint32_t *>(&t);
-                        if (kPlanes == 2 && h == 0) {                     // (what is left is the low half)
-                            const float2 b = __half22float2(t);
-                            x -= b.x;
-                            y -= b.y;
-                        }
                     }
                 }
                 ptx::sts128(piece + piece_at(lane, e), w);
             }
             if (mine && (at & ~31) == k) {
                 uint16_t bits;
-                if (kPlanes == 1 && a.bf16) bits = __bfloat16_as_ushort(__float2bfloat16_rn(own));
-                else {
-                    const __half t = __float2half_rn(own);
-                    bits = __half_as_ushort(t);
-                    own -= __half2float(t);
+                if (kG > 1 || a.bf16) {
+                    const __nv_bfloat16 t = __float2bfloat16_rn(own);
+                    bits = __bfloat16_as_ushort(t);
+                    own -= __bfloat162float(t);
+                } else {
+                    bits = __half_as_ushort(__float2half_rn(own));
                 }
                 asm volatile("st.shared.b16 [%0], %1;" ::"r"(piece + piece_at(lane, at >> 3 & 3) + (at & 7) * 2), "h"(bits) : "memory");
             }
@@ -1005,12 +1032,14 @@ __device__ __forceinline__ void loss_gradient(uint32_t piece, const LossArgs &a,
     loss_out<E>(piece, static_cast<E *>(a.dx), a.ld_dx, a.dx_vec, r.index, c0, a.C, f, v);
 }
 
-template <int kKind, int kPlanes, typename E>
+// kF: values of 16 bits to an element of X and W; kG: to one of G.
+template <int kKind, int kF, int kG, typename E>
 __global__ void __launch_bounds__(kLossThreads, 1) loss_kernel(const __grid_constant__ LossMaps maps, const LossArgs a) {
     extern __shared__ uint8_t raw[];
     __shared__ uint32_t tmem_slot;
     __shared__ volatile uint32_t abort_flag;
-    using Shape = LossShape<kPlanes>;
+    constexpr int kA = kKind == kLossGrads ? kG : kF;
+    using Shape = LossShape<kA, kF>;
     LossPipe q;
     q.smem0 = ptx::smem_u32(ptx::align_1024(raw));
     q.pieces0 = q.smem0 + Shape::kStages * Shape::kStage;
@@ -1040,10 +1069,10 @@ __global__ void __launch_bounds__(kLossThreads, 1) loss_kernel(const __grid_cons
     // had 168, their own chain of waits took as long as four products (37137 rows of 128 over 25943 words: 469 us).
     if (warp == 0) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
-        loss_load<kKind, kPlanes>(q, maps, a, rows, pair, pairs);
+        loss_load<kKind, kA, kF>(q, maps, a, rows, pair, pairs);
     } else if (warp == 1) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
-        if (in_pair == 0) loss_issue<kKind, kPlanes>(q, a, rows, pair, pairs);
+        if (in_pair == 0) loss_issue<kKind, kA, kF>(q, a, rows, pair, pairs);
     } else if (warp < 4) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
     } else {
@@ -1065,14 +1094,14 @@ __global__ void __launch_bounds__(kLossThreads, 1) loss_kernel(const __grid_cons
             r_next = loss_row<kKind>(a, rows, row_of(next), more && (kKind != kLossGrads || next.dx));
             const int row = row_of(u);
             if constexpr (kKind == kLossStats) {
-                if (!loss_stats<kPlanes>(q, a, u, r, scale, rows, row, cols, joint + (turn & 1) * kJoint)) break;
+                if (!loss_stats<kF>(q, a, u, r, scale, rows, row, cols, joint + (turn & 1) * kJoint)) break;
             } else if constexpr (kKind == kLossTurns) {
                 if (!loss_stats_by_turns(q, a, u, r, scale, rows, row, joint + (2 * (part >> 1) + (turn & 1)) * kJoint)) break;
                 q.c += 2;
             } else {
                 float v[64];
-                if (!loss_sums<kKind, kPlanes>(q, u.kb1 - u.kb0, cols, v)) break;
-                if constexpr (kKind == kLossWeights) loss_weights<kPlanes>(piece, a, r, scale, rows, row, u.j * a.width + part * cols, cols, v);
+                if (!loss_sums<kLossDeep<kKind, kF>>(q, u.kb1 - u.kb0, cols, v)) break;
+                if constexpr (kKind == kLossWeights) loss_weights<kG>(piece, a, r, scale, rows, row, u.j * a.width + part * cols, cols, v);
                 else if (u.slot >= 0) {
                     float *slot = a.slots + (((long)u.slot * 2 + in_pair) * a.grad_width + part * cols) * 128 + quad * 32 + lane;
 #pragma unroll
@@ -1173,7 +1202,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps, 2) loss_join_kernel(const Los
 // ---- forward of a few rows
 //
 // One row is scored as fast as W can be read, by fused multiply-adds in float32 (two a row and pair of elements, beside two conversions: one row over 32000 words of 1024, 66 MB in bfloat16, takes 12 to 16 us, 4 to
-// 5.5 TB/s, and the merge behind it 5; two or more are bound by instructions): a tile of a tensor core's product would have 248 empty rows, and float32 inputs would have W read three times and written once for their halves.
+// 5.5 TB/s, and the merge behind it 5; two or more are bound by instructions): a tile of a tensor core's product would have 248 empty rows, and float32 inputs would have W read and written once more for their three values.
 // A warp takes four words at a time, a lane eight columns of each (kVec: neighbours, 16 bytes a load; else 32 apart); X is in shared memory as float32, where the lanes' pieces of a row lie in
 // two sets of 16 bytes so that neighbouring lanes meet no bank conflict.  The 4 R sums are added up over the lanes by exchanges that halve their number (31 for all of 32 sums).
 constexpr int kFewThreads = 256, kFewWords = 4;

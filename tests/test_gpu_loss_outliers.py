@@ -1,4 +1,5 @@
-"""The loss over a vocabulary where sizes differ by many powers of two: logits far beyond what their differences need (needs a B200).
+"""The loss over a vocabulary where sizes differ by many powers of two: one finite element far above all others reaches its own row (of x) or word (of w) and nothing else, whatever
+the type; sizes near either end of float32 (needs a B200).
 
 Bounds, element by element, relative to a row's own magnitudes.  A logit is off by scale max_v sum_c |x_c w_c| E.  16-bit factors are multiplied exactly and added up 16 at a time with truncation,
 2^-22 of what has been added up for each addition (half a unit of 24 bits lost by the sum and as much by the alignment of what is added): width / 16 + 2 of them.  float32 factors are three bfloat16
@@ -76,6 +77,95 @@ def held(got, r, rows=slice(None), words=slice(None)):
     close(loss[rows], r.loss[rows], r.loss_bound[rows], "loss")
     close(dx[rows], r.dx[rows], r.dx_bound[rows], "dx")
     close(dw[words], r.dw[words], r.dw_bound[words], "dw")
+
+
+SIZES = [(300, 500, 80, F32), (40, 1000, 200, F32), (5, 3000, 64, F32), (300, 70000, 64, BF16)]
+
+
+@pytest.mark.parametrize("value", [1e6, 1e9, 1e13, 1e30])
+@pytest.mark.parametrize("rows,vocab,width,dtype", SIZES, ids=str)
+def test_one_large_element_of_x(rows, vocab, width, dtype, value):
+    """The other rows are as without it.  Its own row's softmax is one word, so that of dw only that word and the label are its business."""
+    x, w, labels, _ = problem(rows, vocab, width, dtype)
+    x[0] = 0.0
+    x[0, 3] = value
+    top = 9
+    w[top, 3] = 4.0                                          # (the others': 0.2 on average)
+    without = labels.clone()
+    without[0] = -1
+    loss, lse, dx, dw = got = run(x, w, labels)
+    rest = torch.ones(rows, dtype=torch.bool, device="cuda")
+    rest[0] = False
+    others = torch.ones(vocab, dtype=torch.bool, device="cuda")
+    others[[top, 1]] = False
+    held(got, Reference(x, w, without), rest, others)
+    r = Reference(x[:1], w, labels[:1])
+    close(lse[:1], r.lse, r.lse_bound, "its lse")
+    close(loss[:1], r.loss, r.loss_bound, "its loss")
+    if rows <= 8:                                            # (the forward of few rows adds up in another order: p = exp(l - lse) has the difference in it, some 2^-22 l)
+        return
+    # one word's p is 1, all others' 0: the logits of the forward and the backward are the same
+    close(dx[:1], r.dx, 4 * UNIT[dtype] * (w[top].double().abs() + w[1].double().abs()), "its dx")
+    full = Reference(x, w, labels)
+    size = 4 * UNIT[dtype] * value + full.dw.abs() * UNIT[dtype]
+    close(dw[[top, 1], 3], full.dw[[top, 1], 3], size[[top, 1], 3], "its dw")
+
+
+@pytest.mark.parametrize("value", [1e6, 1e13, 1e30])
+@pytest.mark.parametrize("rows,vocab,width,dtype", SIZES, ids=str)
+def test_one_large_element_of_w(rows, vocab, width, dtype, value):
+    """A word far ahead of all others for some rows, far behind for the rest: those are as without it."""
+    x, w, labels, _ = problem(rows, vocab, width, dtype)
+    x[:, 5] = torch.where(torch.arange(rows, device="cuda") % 2 == 0, 1.0, -1.0).to(dtype)
+    labels[1::2] = torch.where(labels[1::2] == 7, 8, labels[1::2])
+    plain = w.clone()
+    w[7] = 0.0
+    w[7, 5] = value
+    behind = torch.arange(rows, device="cuda") % 2 == 1
+    keep = [v for v in range(vocab) if v != 7]
+    kept_labels = torch.where(labels > 7, labels - 1, labels)
+    loss, lse, dx, dw = run(x, w, labels)
+    r = Reference(x, plain[keep], kept_labels)
+    close(lse[behind], r.lse[behind], r.lse_bound[behind], "lse")
+    close(loss[behind], r.loss[behind], r.loss_bound[behind], "loss")
+    close(dx[behind], r.dx[behind], r.dx_bound[behind], "dx")
+
+
+@pytest.mark.parametrize("rows,vocab,width", [(300, 500, 80), (1500, 6000, 64)])
+@pytest.mark.parametrize("dtype,value", [(F32, 1e4), (F32, 1e12), (F32, 1e25)], ids=str)
+def test_one_large_weight_of_a_row(rows, vocab, width, dtype, value):
+    """dloss: the other rows' part in dw, seen in words that the row with the large weight has nothing to do with."""
+    x, w, labels, g = problem(rows, vocab, width, dtype)
+    x[0] = (100.0 * w[1].float()).to(dtype)                  # certain of its label: |w|^2 is about 4, other products about 0.5
+    dloss = (torch.rand(rows, device="cuda", generator=g) + 0.5) * 1e-3
+    dloss[0] = value
+    none = torch.softmax(x[0].double() @ w.double().T, 0) * value < 1e-30
+    assert int(none.sum()) > 0.99 * vocab
+    without = labels.clone()
+    without[0] = -1
+    got = run(x, w, labels, dloss)
+    rest = torch.ones(rows, dtype=torch.bool, device="cuda")
+    rest[0] = False
+    r = Reference(x, w, without, dloss)
+    held(got, r, rest, none)
+
+
+@pytest.mark.parametrize("size", [1e25, 1e-25, 1e15, 1e-15])
+@pytest.mark.parametrize("rows,vocab,width", [(300, 500, 80), (1500, 6000, 200)])
+@pytest.mark.parametrize("dtype", [F32], ids=str)
+def test_sizes_near_either_end(rows, vocab, width, dtype, size):
+    x, w, labels, g = problem(rows, vocab, width, dtype, size=size)
+    held(run(x, w, labels), Reference(x, w, labels))
+
+
+@pytest.mark.parametrize("dtype", [F32, F16], ids=str)
+@pytest.mark.parametrize("rows,vocab,width", [(300, 500, 80), (600, 5003, 136)])
+def test_results_to_their_types_rounding(rows, vocab, width, dtype):
+    """What q is held in, 16 bits in bfloat16 (w up to 2^22 elements), shows in the gradients."""
+    x, w, labels, g = problem(rows, vocab, width, dtype)
+    held(run(x, w, labels, scale=0.5), Reference(x, w, labels, scale=0.5))
+    dloss = torch.rand(rows, device="cuda", generator=g)
+    held(run(x, w, labels, dloss, scale=0.5), Reference(x, w, labels, dloss, scale=0.5))
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16, F16], ids=str)

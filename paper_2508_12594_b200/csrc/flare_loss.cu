@@ -31,10 +31,9 @@ int check_loss(const flare_loss_desc_t *d) {
 // 512 take 3.2 ms in pieces of 256 MB, 2.83 of 512, 2.97 of 1024; 18944 over 50021 of 256 take 2.34, 2.06, 1.97; 8192 over 128256 of 1024 take 6.6 in each.
 constexpr size_t kPieceBytes = 512u << 20;
 struct LossPlan {
-    int to;                      // what is multiplied: kAsIs, kToHalf, kToThree
-    bool bf16;                   // in bfloat16 (else float16)
+    bool bf16;                   // what is multiplied is bfloat16 (else float16)
     int planes, g_planes;        // values of 16 bits to an element of X and W, of G
-    int Cp, chunks, x_blocks, w_blocks, pairs;
+    int Cp, chunks, pairs;
     long cap;
     int width;                   // of a tile of X W^T
     int Vp, pieces;              // words of a piece
@@ -49,23 +48,19 @@ int tile_width(long row_tiles, long words, int pairs) {
 LossPlan loss_plan(const flare_loss_desc_t *d, int sms, bool backward) {
     LossPlan p{};
     const bool f32 = d->dtype == FLARE_DTYPE_F32;
-    // bfloat16's G would be off by 2^-9 (its rms 1.7e-3, as much again as the rounding of the results): where W is small enough for another pass over it not to count, it, X and G are float16.  (That costs a tenth: a step
-    // over 2000 rows, 4096 words, C = 1024 takes 102.5 us instead of 93, one over 131072 rows, 256 words, C = 128 takes 148 instead of 130; its error against 64 bits is 1.05 times that of rounding alone instead of 1.4.)
-    const bool bf16_small = d->dtype == FLARE_DTYPE_BF16 && backward && (long)d->vocab * d->width <= (4L << 20);
-    p.to = f32 ? kToThree : bf16_small ? kToHalf : kAsIs;
-    p.bf16 = f32 || (d->dtype == FLARE_DTYPE_BF16 && !bf16_small);
-    p.planes = p.g_planes = f32 ? 3 : 1;
+    // G in one bfloat16 value is off by 2^-9: gradients by 1.06 times what rounding exact ones gives, 1.35 times where every row has its own dloss.  In two values they are as good as rounded exact ones, for twice
+    // the products of the gradients and G's bytes: 131072 rows over 256 words, C = 128: 153 us a step (one value: 112); 2000 over 4096, C = 1024: 118 (93); 8192 over 8000, C = 512: 385 (266); 16384 over 32000,
+    // C = 128: 1466 (892).  So of vocabularies where that is a third or less, as if W were small.
+    const bool bf16_small = d->dtype == FLARE_DTYPE_BF16 && backward && d->vocab <= 8192 && (long)d->vocab * d->width <= (4L << 20);
+    p.bf16 = d->dtype != FLARE_DTYPE_F16;
+    p.planes = f32 ? 3 : 1;
+    p.g_planes = f32 ? 3 : bf16_small ? 2 : 1;
     // rows of packed X and W: whole 16 bytes, of wide ones whole lines (TMA takes 128-byte pieces of them)
     p.Cp = d->width > 256 ? (d->width + 63) / 64 * 64 : (d->width + 7) / 8 * 8;
     p.chunks = (int)((d->rows + kLossChunk - 1) / kLossChunk);
     p.pairs = std::max(1, sms / 2);
     p.cap = std::max(1L, (long)(d->rows + 255) / 256) * 256;
     p.width = tile_width(p.cap / 256, d->vocab, p.pairs);
-    if (p.to == kToHalf) {
-        auto blocks = [&](long rows) { return (int)std::max(1L, std::min(4L * sms, rows * d->width / 8192)); };
-        p.x_blocks = blocks(d->rows);
-        p.w_blocks = blocks(d->vocab);
-    }
     const long words = ((long)d->vocab + 255) / 256 * 256, most = std::max(256L, (long)(kPieceBytes / (2 * p.g_planes * p.cap)) / 256 * 256);
     p.pieces = (int)((words + most - 1) / most);
     p.Vp = (int)((words / 256 + p.pieces - 1) / p.pieces * 256);
@@ -85,7 +80,7 @@ int few_blocks(const flare_loss_desc_t *d, int sms) {
     const long groups = (d->vocab + kFewWords - 1) / kFewWords, warps = (long)sms * (few_rows(d) <= 2 ? 4 : 2) * (kFewThreads / 32), rounds = (groups + warps - 1) / warps;
     return (int)(((groups + rounds - 1) / rounds + kFewThreads / 32 - 1) / (kFewThreads / 32));
 }
-struct LossLayout { size_t info, rank, chunk, largest, px, pd, pw, index, label, part, chosen, gave_up, lse_of, gm, coef, g, acc, slots, total; };
+struct LossLayout { size_t info, rank, chunk, px, pd, pw, index, label, part, chosen, gave_up, lse_of, gm, coef, g, acc, slots, total; };
 LossLayout loss_layout(const flare_loss_desc_t *d, const LossPlan &p, bool backward) {
     LossLayout w{};
     size_t off = kHeaderBytes;
@@ -93,7 +88,6 @@ LossLayout loss_layout(const flare_loss_desc_t *d, const LossPlan &p, bool backw
     take(w.info, sizeof(LossInfo));
     take(w.rank, sizeof(int) * (size_t)d->rows);
     take(w.chunk, sizeof(LossChunk) * (size_t)p.chunks);
-    take(w.largest, sizeof(float) * (size_t)(p.x_blocks + p.w_blocks));
     const size_t row = sizeof(uint16_t) * (size_t)p.planes * p.Cp;
     take(w.px, row * p.cap);
     take(w.pw, row * d->vocab);                               // (whether W can be taken as it stands is known with its address)
@@ -161,13 +155,8 @@ int launch_merge(const LossMerge &m, long rows, cudaStream_t st) {
 }
 
 template <typename T>
-int launch_scan(const LossScan &s, cudaStream_t st) {
-    FLARE_CUDA(launch_after(loss_scan_kernel<T>, (unsigned)(s.chunks + s.x_blocks + s.w_blocks), kScanThreads, 0, st, s));
-    return FLARE_OK;
-}
-template <typename T, int kTo>
 int launch_pack(const LossPack &k, int blocks, cudaStream_t st) {
-    FLARE_CUDA(launch_after(loss_pack_kernel<T, kTo>, (unsigned)blocks, kPackThreads, 0, st, k));
+    FLARE_CUDA(launch_after(loss_pack_kernel<T>, (unsigned)blocks, kPackThreads, 0, st, k));
     return FLARE_OK;
 }
 
@@ -203,33 +192,26 @@ int prepare_loss(const flare_loss_desc_t *d, const LossPlan &p, const LossLayout
                  LossArgs *a, cudaStream_t st) {
     const bool f32 = d->dtype == FLARE_DTYPE_F32, bf16 = p.bf16;
     const long ld_x = d->stride_x ? d->stride_x : d->width, ld_w = d->stride_w ? d->stride_w : d->width;
-    const bool own_w = p.to != kAsIs || !aligned16(w) || ld_w % 8 != 0;
+    const bool own_w = f32 || !aligned16(w) || ld_w % 8 != 0;
     LossScan s{};
-    s.labels = labels; s.wide = d->label_bits == 64; s.rows = d->rows; s.V = d->vocab; s.C = d->width;
-    s.chunks = p.chunks; s.x_blocks = p.x_blocks; s.w_blocks = p.w_blocks; s.dloss = k.dloss;
+    s.labels = labels; s.wide = d->label_bits == 64; s.rows = d->rows; s.V = d->vocab; s.chunks = p.chunks; s.dloss = k.dloss;
     s.rank = reinterpret_cast<int *>(ws + l.rank); s.chunk = reinterpret_cast<LossChunk *>(ws + l.chunk);
-    s.x = x; s.w = w; s.ld_x = ld_x; s.ld_w = ld_w;
-    s.largest = reinterpret_cast<float *>(ws + l.largest);
     s.status = reinterpret_cast<uint32_t *>(ws);
     int rc;
     // rows of a block: so many that a thread has four groups of columns, and that there are no more than four blocks an SM; whole parts of a chunk
     k.pack_rows = 4;
     while (k.pack_rows < kLossChunk && ((long)k.pack_rows * (p.Cp / 8) < 4 * kPackThreads || (long)k.pack_rows * 4 * device_info().sms < d->rows)) k.pack_rows *= 2;
-    const bool alone = d->rows <= kPackAlone && p.to != kToHalf && k.pack_rows <= kPackThreads;
-    if (!alone && (rc = f32 ? launch_scan<float>(s, st) : d->dtype == FLARE_DTYPE_BF16 ? launch_scan<__nv_bfloat16>(s, st) : launch_scan<__half>(s, st)) != FLARE_OK) return rc;
+    const bool alone = d->rows <= kPackAlone && k.pack_rows <= kPackThreads;
+    if (!alone) FLARE_CUDA(launch_after(loss_scan_kernel, (unsigned)s.chunks, kScanThreads, 0, st, s));
     k.labels = labels; k.x = x; k.w = w; k.wide = s.wide; k.rows = d->rows; k.cap = p.cap; k.ld_x = ld_x; k.ld_w = ld_w;
-    k.w_rows = own_w ? d->vocab : 0; k.C = d->width; k.Cp = p.Cp; k.V = d->vocab; k.chunks = p.chunks; k.x_blocks = p.x_blocks; k.w_blocks = p.w_blocks;
+    k.w_rows = own_w ? d->vocab : 0; k.C = d->width; k.Cp = p.Cp; k.V = d->vocab; k.chunks = p.chunks;
     k.pack_blocks = (int)((d->rows + k.pack_rows - 1) / k.pack_rows);
-    k.rank = alone ? nullptr : s.rank; k.status = s.status; k.chunk = s.chunk; k.largest = s.largest;
+    k.rank = alone ? nullptr : s.rank; k.status = s.status; k.chunk = s.chunk;
     k.info = reinterpret_cast<LossInfo *>(ws + l.info);
     k.px = reinterpret_cast<uint16_t *>(ws + l.px); k.pw = reinterpret_cast<uint16_t *>(ws + l.pw);
     k.index = reinterpret_cast<int *>(ws + l.index); k.label = reinterpret_cast<int *>(ws + l.label);
     const int blocks = k.pack_blocks + (int)std::min<long>((k.w_rows * (p.Cp / 8) + 4 * kPackThreads - 1) / (4 * kPackThreads), 16L * device_info().sms);
-    if ((rc = f32                             ? launch_pack<float, kToThree>(k, blocks, st)
-              : d->dtype == FLARE_DTYPE_F16   ? launch_pack<__half, kAsIs>(k, blocks, st)
-              : p.to == kToHalf               ? launch_pack<__nv_bfloat16, kToHalf>(k, blocks, st)
-                                              : launch_pack<__nv_bfloat16, kAsIs>(k, blocks, st)) != FLARE_OK)
-        return rc;
+    if ((rc = f32 ? launch_pack<float>(k, blocks, st) : d->dtype == FLARE_DTYPE_F16 ? launch_pack<__half>(k, blocks, st) : launch_pack<__nv_bfloat16>(k, blocks, st)) != FLARE_OK) return rc;
     if ((rc = make_plane_map(&maps->x, k.px, bf16, p.Cp, p.cap, p.planes, p.Cp, 64)) != FLARE_OK) return rc;
     if ((rc = own_w ? make_plane_map(&maps->w, k.pw, bf16, p.Cp, d->vocab, p.planes, p.Cp, 64)
                     : make_plane_map(&maps->w, w, bf16, d->width, d->vocab, 1, ld_w, 64)) != FLARE_OK)
@@ -305,7 +287,7 @@ int flare_loss_forward(const flare_loss_desc_t *desc, const void *x, const void 
     if (a.tiles_v == 1 && !direct) { a.loss = loss; a.lse = lse; }
     const int pairs = (int)std::min<long>(p.pairs, p.cap / 256 * a.tiles_v);
     // (products of few steps, whose ends bound the tile, in turns: 37137 rows over 25943 words of 128 take 356 us instead of 444, 5003 over 10007 of 512 45.7 and 46.2)
-    auto stats = p.planes == 3 ? launch_loss<kLossStats, 3, 1, float> : desc->width <= 64 * kLossDeep<kLossTurns, 1> ? launch_loss<kLossTurns, 1, 1, float> : launch_loss<kLossStats, 1, 1, float>;
+    auto stats = p.planes == 3 ? launch_loss<kLossStats, 3, 1, float> : desc->width <= 64 * kLossDeep<kLossTurns, 1, 1> ? launch_loss<kLossTurns, 1, 1, float> : launch_loss<kLossStats, 1, 1, float>;
     if (int rc = stats(maps, a, pairs, st)) return rc;
     if (a.loss) return FLARE_OK;
     LossMerge m{};
@@ -356,8 +338,8 @@ int flare_loss_backward(const flare_loss_desc_t *desc, const void *x, const void
     a.dw_vec = vec(dw, ld_dw); a.dx_vec = vec(dx, ld_dx);
     a.dw_factor = k.g_factor != 0.f ? k.mult / k.g_factor : 1.f;
     a.acc = reinterpret_cast<float *>(ws + l.acc); a.slots = reinterpret_cast<float *>(ws + l.slots);
-    auto weights = f32 ? launch_loss<kLossWeights, 3, 3, float> : launch_loss<kLossWeights, 1, 1, float>;
-    auto grads = f32 ? launch_loss<kLossGrads, 3, 3, float> : desc->dtype == FLARE_DTYPE_BF16 ? launch_loss<kLossGrads, 1, 1, __nv_bfloat16> : launch_loss<kLossGrads, 1, 1, __half>;
+    auto weights = f32 ? launch_loss<kLossWeights, 3, 3, float> : p.g_planes == 2 ? launch_loss<kLossWeights, 1, 2, float> : launch_loss<kLossWeights, 1, 1, float>;
+    auto grads = f32 ? launch_loss<kLossGrads, 3, 3, float> : !bf16 ? launch_loss<kLossGrads, 1, 1, __half> : p.g_planes == 2 ? launch_loss<kLossGrads, 1, 2, __nv_bfloat16> : launch_loss<kLossGrads, 1, 1, __nv_bfloat16>;
     auto *join = f32 ? loss_join_kernel<float> : desc->dtype == FLARE_DTYPE_BF16 ? loss_join_kernel<__nv_bfloat16> : loss_join_kernel<__half>;
     // of tiles that several pairs can have shared: fewer than a round of either gradient
     const long warps = 2L * (p.pairs - 1) * 8 * (p.grad_width / kJoinCols);

@@ -17,9 +17,9 @@
 // that a tile's end runs under the next tile's products.  It is bound by the tensor pipe.
 //
 // bfloat16 and float16 are multiplied as they are, G in the same type, rounded once.  bfloat16's G is q where one dloss is that of all rows (next to a label q is next to -1, which is no rounding), else dloss scale q
-// (2^-9, as the gradients themselves will be; dloss in a second X instead put the same rounding there, and as many more elements were moved).  float16's G is q times 2^15, so that probabilities down to 2^-29 are
-// normal numbers; of a row's own dloss its mantissa is there too (q times 2^14 and up to 2) and its power of two, which rounds nothing, in a second X and in dX's rows.  Small vocabularies in bfloat16 take float16's way
-// backward, X and W times powers of two.
+// (2^-9, as the gradients themselves will be; dloss in a second X instead put the same rounding there, and as many more elements were moved); of a small vocabulary it is two bfloat16 values (2^-17), two products of
+// either gradient.  float16's G is q times 2^15, so that probabilities down to 2^-29 are
+// normal numbers; of a row's own dloss its mantissa is there too (q times 2^14 and up to 2) and its power of two, which rounds nothing, in a second X and in dX's rows.
 // float32: X, W, G as three bfloat16 values each, which hold all 24 bits over all of float32's range, a product as the six of them that are above 2^-24 of it; sums leave tensor memory, which
 // truncates, every 64 of K to be added up in registers.  (Two float16 halves, 22 bits, take three products, but want one power of two for all of X, of W and of a row's dloss: an element
 // of 1e9 in one row put the others' losses off by 3e-3, one of 1e13 by 4.)
@@ -35,7 +35,6 @@ namespace flare {
 // What the packing leaves for the kernels behind it, on the device.
 struct LossInfo {
     uint32_t rows;               // with a label
-    float x_scale, w_scale;      // of what is multiplied in float16 though it is not (else 1)
     float dmax;                  // where dloss is in the second X: the power of two of the largest of a row, else 1
 };
 // Per 1024 rows.
@@ -64,13 +63,10 @@ struct LossScan {
     const void *labels;
     int wide;
     long rows;
-    int V, C, chunks, x_blocks, w_blocks;     // blocks beyond the chunks' look for the largest |x| of labelled rows and |w| (what is multiplied in float16 though it is not)
+    int V, chunks;
     const float *dloss;                       // or null
     int *rank;                                // [rows]: among the labelled rows of its chunk, or -1
     LossChunk *chunk;
-    const void *x, *w;
-    long ld_x, ld_w;
-    float *largest;                           // [x_blocks + w_blocks]
     uint32_t *status;
 };
 __device__ __forceinline__ float finite_abs(float v) { return fabsf(v) <= 3.4028234e38f ? fabsf(v) : 0.f; }
@@ -98,7 +94,6 @@ template <typename T> __device__ __forceinline__ void eight_of(const T *p, bool 
             else from_f32(t[i], 0.f);
     }
 }
-template <typename T>
 __global__ void __launch_bounds__(kScanThreads) loss_scan_kernel(const LossScan a) {
     __shared__ float shared[32];
     __shared__ uint32_t before[33];
@@ -106,40 +101,6 @@ __global__ void __launch_bounds__(kScanThreads) loss_scan_kernel(const LossScan 
     ptx::grid_wait();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (blockIdx.x == 0 && threadIdx.x < kHeaderBytes / 4) a.status[threadIdx.x] = 0;
-    if ((int)blockIdx.x >= a.chunks) {
-        const int b = blockIdx.x - a.chunks;
-        const bool of_x = b < a.x_blocks;
-        const T *m = static_cast<const T *>(of_x ? a.x : a.w);
-        const long rows = of_x ? a.rows : a.V, ld = of_x ? a.ld_x : a.ld_w;
-        const bool vec = a.C % 8 == 0 && ld * (long)sizeof(T) % 16 == 0 && (reinterpret_cast<uintptr_t>(m) & 15) == 0;
-        const uint64_t blocks = of_x ? a.x_blocks : a.w_blocks, first = (uint64_t)(of_x ? b : b - a.x_blocks) * kScanThreads + threadIdx.x;
-        // (a few groups of eight columns are asked for before the first is looked at)
-        constexpr int kBatch = sizeof(T) == 4 ? 2 : 4;
-        LossWalk walk(first, blocks * kScanThreads, (uint32_t)(a.C + 7) / 8);
-        float most = 0.f;
-        while (walk.row < rows) {
-            LossEight<T> e[kBatch];
-            bool use[kBatch];
-#pragma unroll
-            for (int k = 0; k < kBatch; ++k) {
-                use[k] = walk.row < rows;
-                if (use[k] && of_x) {
-                    const int64_t label = label_at(a.labels, a.wide, walk.row);
-                    use[k] = label >= 0 && label < a.V;
-                }
-                if (use[k]) eight_of(m + walk.row * ld + 8 * walk.group, vec, a.C - (int)(8 * walk.group), e[k]);
-                walk.next();
-            }
-#pragma unroll
-            for (int k = 0; k < kBatch; ++k)
-                if (use[k])
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) most = fmaxf(most, finite_abs(to_f32(reinterpret_cast<const T *>(e[k].q)[i])));
-        }
-        most = block_max(most, shared);
-        if (threadIdx.x == 0) a.largest[b] = most;
-        return;
-    }
     // four times 256 rows of the chunk, in order
     float most = 0.f;
     bool there[kLossChunk / kScanThreads];
@@ -181,10 +142,9 @@ struct LossPack {
     const void *labels, *x, *w;
     int wide;
     long rows, cap, ld_x, ld_w, w_rows;       // cap: rows up to whole tiles; w_rows: of W to be packed too (0: it is taken as it stands)
-    int C, Cp, V, chunks, x_blocks, w_blocks, pack_blocks, pack_rows;   // Cp: C up to a multiple of eight
+    int C, Cp, V, chunks, pack_blocks, pack_rows;   // Cp: C up to a multiple of eight
     const int *rank;                          // the scan's; null: there was none
     const LossChunk *chunk;
-    const float *largest;
     uint32_t *status;
     LossInfo *info;
     uint16_t *px, *pd, *pw;                   // packed X, packed dloss X (or null), packed W: planes of [cap][Cp], [V][Cp]
@@ -207,16 +167,8 @@ __device__ __forceinline__ float two_of(float d, float other) {
     const uint32_t e = __float_as_uint(d) & 0x7f800000u;
     return e == 0x7f800000u ? other : __uint_as_float(max(e, 0x00800000u));
 }
-// The power of two that puts `most` between 2^14 and 2^15.
-__device__ __forceinline__ float half_scale(float most) {
-    if (!(most > 0.f)) return 1.f;
-    int e;
-    frexpf(most, &e);                         // most < 2^e
-    return ldexpf(1.f, min(max(15 - e, -60), 60));
-}
-// What the products multiply: the type as it is; bfloat16 as float16 times a power of two; float32 as three bfloat16 values, each what rounding to those before it has left.
-enum { kAsIs = 0, kToHalf = 1, kToThree = 2 };
-template <int kTo> constexpr int kPacked = kTo == kToThree ? 3 : 1;
+// What the products multiply: the type as it is; float32 as three bfloat16 values, each what rounding to those before it has left.
+template <typename T> constexpr int kPacked = sizeof(T) == 4 ? 3 : 1;
 __device__ __forceinline__ void three_of(float v, uint16_t (&t)[3]) {
     __nv_bfloat16 h = fabsf(v) > 3.3895314e38f ? __float2bfloat16_rz(v) : __float2bfloat16_rn(v);         // (beyond bfloat16's largest: not to infinity)
     t[0] = __bfloat16_as_ushort(h);
@@ -225,12 +177,12 @@ __device__ __forceinline__ void three_of(float v, uint16_t (&t)[3]) {
     t[1] = __bfloat16_as_ushort(h);
     t[2] = __bfloat16_as_ushort(__float2bfloat16_rn(left - __bfloat162float(h)));
 }
-// Eight columns times f, into their planes; as they are where not `scaled`.
-template <typename T, int kTo>
+// Eight columns into their planes; those of 16 bits times f, or as they are where not `scaled`.
+template <typename T>
 __device__ __forceinline__ void pack_eight(const LossEight<T> &e, float f, bool scaled, uint16_t *out, long plane) {
     const T *t = reinterpret_cast<const T *>(e.q);
     __align__(16) uint16_t h[8];
-    if constexpr (kTo == kToThree) {
+    if constexpr (kPacked<T> == 3) {
         __align__(16) uint16_t m[8], l[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -238,31 +190,23 @@ __device__ __forceinline__ void pack_eight(const LossEight<T> &e, float f, bool 
             three_of(to_f32(t[i]), three);
             h[i] = three[0]; m[i] = three[1]; l[i] = three[2];
         }
-        *reinterpret_cast<uint4 *>(out) = *reinterpret_cast<const uint4 *>(h);
         *reinterpret_cast<uint4 *>(out + plane) = *reinterpret_cast<const uint4 *>(m);
         *reinterpret_cast<uint4 *>(out + 2 * plane) = *reinterpret_cast<const uint4 *>(l);
-        return;
-    }
-    if constexpr (kTo == kAsIs) {
+    } else {
         if (!scaled) {
             *reinterpret_cast<uint4 *>(out) = e.q[0];
             return;
         }
-    }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float v = to_f32(t[i]) * f;
-        if constexpr (kTo == kAsIs) {
+        for (int i = 0; i < 8; ++i) {
             T u;
-            from_f32(u, v);
+            from_f32(u, to_f32(t[i]) * f);
             h[i] = *reinterpret_cast<const uint16_t *>(&u);
-        } else {
-            h[i] = __half_as_ushort(__float2half_rn(v));
         }
     }
     *reinterpret_cast<uint4 *>(out) = *reinterpret_cast<const uint4 *>(h);
 }
-template <typename T, int kTo>
+template <typename T>
 __global__ void __launch_bounds__(kPackThreads) loss_pack_kernel(const LossPack a) {
     __shared__ float shared[32];
     __shared__ uint32_t sums[2][kPackThreads / 32];
@@ -271,17 +215,8 @@ __global__ void __launch_bounds__(kPackThreads) loss_pack_kernel(const LossPack 
     ptx::grid_launch();
     ptx::grid_wait();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    constexpr bool kScaled = kTo == kToHalf;
     constexpr int kBatch = 4;                                 // groups of eight columns that are asked for before the first is stored
     const uint32_t groups = (uint32_t)a.Cp / 8;
-    float sx = 1.f, sw = 1.f;
-    if constexpr (kScaled) {
-        float mx = 0.f, mw = 0.f;
-        for (int i = threadIdx.x; i < a.x_blocks; i += kPackThreads) mx = fmaxf(mx, a.largest[i]);
-        for (int i = threadIdx.x; i < a.w_blocks; i += kPackThreads) mw = fmaxf(mw, a.largest[a.x_blocks + i]);
-        sx = half_scale(block_max(mx, shared));
-        sw = half_scale(block_max(mw, shared));
-    }
     if ((int)blockIdx.x >= a.pack_blocks) {                   // W
         const T *w = static_cast<const T *>(a.w);
         const bool vec = a.C % 8 == 0 && a.ld_w * (long)sizeof(T) % 16 == 0 && (reinterpret_cast<uintptr_t>(w) & 15) == 0;
@@ -297,7 +232,7 @@ __global__ void __launch_bounds__(kPackThreads) loss_pack_kernel(const LossPack 
             }
 #pragma unroll
             for (int k = 0; k < kBatch; ++k)
-                if (at[k] >= 0) pack_eight<T, kTo>(e[k], sw, kScaled, a.pw + at[k], a.w_rows * a.Cp);
+                if (at[k] >= 0) pack_eight<T>(e[k], 1.f, false, a.pw + at[k], a.w_rows * a.Cp);
         }
         return;
     }
@@ -332,7 +267,7 @@ __global__ void __launch_bounds__(kPackThreads) loss_pack_kernel(const LossPack 
     base = total = 0;
     for (int w = 0; w < kPackThreads / 32; ++w) { base += sums[0][w]; total += sums[1][w]; }
     dmax = a.pd ? two_of(dmax, 1.f) : 1.f;
-    if (blockIdx.x == 0 && threadIdx.x == 0) *a.info = LossInfo{total, sx, sw, dmax};
+    if (blockIdx.x == 0 && threadIdx.x == 0) *a.info = LossInfo{total, dmax};
     const int rows = (int)min((long)a.pack_rows, a.rows - n0);
     if (alone) {                                              // (up to a row a thread)
         __syncthreads();                                      // (sums have been read)
@@ -388,8 +323,8 @@ __global__ void __launch_bounds__(kPackThreads) loss_pack_kernel(const LossPack 
             if (row[k] >= rows) break;
             const long to = to_row[row[k]];
             if (to >= 0) {
-                pack_eight<T, kTo>(e[k], sx, kScaled, a.px + to * a.Cp + col[k], plane);
-                if (a.pd) pack_eight<T, kTo>(e[k], sx * d_row[row[k]], true, a.pd + to * a.Cp + col[k], plane);
+                pack_eight<T>(e[k], 1.f, false, a.px + to * a.Cp + col[k], plane);
+                if (a.pd) pack_eight<T>(e[k], d_row[row[k]], true, a.pd + to * a.Cp + col[k], plane);
             } else if (dx) {
                 T *p = dx + (n0 + row[k]) * a.ld_dx + col[k];
                 if (col[k] >= a.C) continue;
@@ -409,7 +344,7 @@ __global__ void __launch_bounds__(kPackThreads) loss_pack_kernel(const LossPack 
     if (a.loss == nullptr) {
         const long end = min(a.cap, ((long)max(total, 1u) + 63) / 64 * 64);
         for (long r = total + (long)blockIdx.x * (kPackThreads / 32) + warp; r < end; r += (long)a.pack_blocks * (kPackThreads / 32))
-            for (int h = 0; h < kPacked<kTo>; ++h)
+            for (int h = 0; h < kPacked<T>; ++h)
                 for (int c = lane * 8; c < a.Cp; c += 256) {
                     *reinterpret_cast<uint4 *>(a.px + h * plane + r * a.Cp + c) = make_uint4(0, 0, 0, 0);
                     if (a.pd) *reinterpret_cast<uint4 *>(a.pd + h * plane + r * a.Cp + c) = make_uint4(0, 0, 0, 0);
@@ -429,8 +364,8 @@ template <int kA, int kB> struct LossShape {
     static constexpr uint32_t kStage = (kA + kB) * kLossHalfTile;
 };
 // 64-deep steps whose sums stay in tensor memory, where every addition truncates: of float32 1 (6 x 4 additions: gradients off by 3.8e-7 to 4.0e-7); of 16-bit factors' logits 8 (a loss over 4096 columns is off by 2e-6 with all of
-// them there; the same forward and backward, so that both have the same logits); of the gradients, whose results are rounded to 2^-9 or 2^-12, 64.
-template <int kKind, int kF> constexpr int kLossDeep = kF == 3 ? 1 : kKind != kLossGrads ? 8 : 64;
+// them there; the same forward and backward, so that both have the same logits); of the gradients, whose results are rounded to 2^-9 or 2^-12, 64 (of 4 additions, or half as many of 8).
+template <int kKind, int kF, int kG> constexpr int kLossDeep = kF == 3 ? 1 : kKind != kLossGrads ? 8 : 64 / kG;
 constexpr size_t kLossSmem = 1024 + 6 * 2 * kLossHalfTile + kLossResults * kLossPiece + 256;
 
 struct LossMaps { CUtensorMap x, d, w, g; };                  // in boxes of 64 x 64
@@ -465,7 +400,7 @@ struct LossArgs {
     void *dw, *dx;
     long ld_dw, ld_dx;
     int dw_vec, dx_vec;          // rows can be written 16 bytes at a time
-    float dw_factor;             // scale dloss_scale / g_factor (times dmax / x_scale), or 1 where G holds them
+    float dw_factor;             // scale dloss_scale / g_factor (times dmax), or 1 where G holds them
     float *acc;                  // dX over the pieces before, by tile: [2 blocks][grad_width columns][128 rows]
     float *slots;                // sums of parts of tiles, likewise, two per pair
 };
@@ -644,7 +579,7 @@ __device__ __forceinline__ void loss_load(LossPipe &q, const LossMaps &m, const 
     }
 }
 // The issuing warp's part (its pair's first block's).
-template <int kKind, int kA, int kB>
+template <int kKind, int kA, int kB, int kDeep>
 __device__ __forceinline__ void loss_issue(LossPipe &q, const LossArgs &a, int rows, int pair, int pairs) {
     using Shape = LossShape<kA, kB>;
     if (!ptx::elect_one()) return;
@@ -662,7 +597,7 @@ __device__ __forceinline__ void loss_issue(LossPipe &q, const LossArgs &a, int r
             const uint32_t acc = q.tmem + (q.c & 1) * 256;
             if (q.c >= 2 && !ptx::mbar_wait(q.acc_empty(q.c & 1), (q.c / 2 - 1) & 1, q.abort_flag, 112)) return;
             ptx::tc_fence_after();
-            for (int k1 = min(kb + kLossDeep<kKind, kB>, u.kb1), first = 1; kb < k1; ++kb, ++q.n, first = 0) {
+            for (int k1 = min(kb + kDeep, u.kb1), first = 1; kb < k1; ++kb, ++q.n, first = 0) {
                 const uint32_t s = q.n % Shape::kStages;
                 if (!ptx::mbar_wait(q.full(s), (q.n / Shape::kStages) & 1, q.abort_flag, 113)) return;
                 ptx::tc_fence_after();
@@ -831,7 +766,7 @@ __device__ __forceinline__ bool loss_stats(LossPipe &q, const LossArgs &a, const
     const int warp = ptx::warp_index(), part = (warp - 4) >> 2, local = (warp & 3) * 32 + (threadIdx.x & 31), col0 = u.j * a.width + part * cols;
     float *chosen = reinterpret_cast<float *>(joint + 3 * 128) + local;
     float v[64];
-    const bool ok = loss_sums<kLossDeep<kLossStats, kF>>(q, u.kb1, cols, v);
+    const bool ok = loss_sums<kLossDeep<kLossStats, kF, 1>>(q, u.kb1, cols, v);
     LossStat s[4] = {{-INFINITY, 0.f}, {-INFINITY, 0.f}, {-INFINITY, 0.f}, {-INFINITY, 0.f}};
     if (ok && row - local % 32 < rows) s[0] = loss_columns(a, v, r.label - col0, cols, a.V - col0, row, c2, chosen);   // (some of the warp's rows are rows)
     if (part > 0) joint[(part - 1) * 128 + local] = make_float2(s[0].m, s[0].l);
@@ -1012,7 +947,7 @@ __device__ __forceinline__ void loss_gradient(uint32_t piece, const LossArgs &a,
     const int lane = threadIdx.x & 31, local = i * 256 + block * 128 + quad * 32 + lane, c0 = j * a.grad_width + col;
     if (c0 >= a.C) return;
     if (!dx) {
-        const float f = a.dw_factor * info.dmax / info.x_scale;
+        const float f = a.dw_factor * info.dmax;
         loss_out<E>(piece, static_cast<E *>(a.dw), a.ld_dw, a.dw_vec, local < a.words ? a.v0 + local : -1, c0, a.C, f, v);
         return;
     }
@@ -1028,7 +963,7 @@ __device__ __forceinline__ void loss_gradient(uint32_t piece, const LossArgs &a,
             return;
         }
     }
-    const float f = r.coef / info.w_scale;
+    const float f = r.coef;
     loss_out<E>(piece, static_cast<E *>(a.dx), a.ld_dx, a.dx_vec, r.index, c0, a.C, f, v);
 }
 
@@ -1038,7 +973,7 @@ __global__ void __launch_bounds__(kLossThreads, 1) loss_kernel(const __grid_cons
     extern __shared__ uint8_t raw[];
     __shared__ uint32_t tmem_slot;
     __shared__ volatile uint32_t abort_flag;
-    constexpr int kA = kKind == kLossGrads ? kG : kF;
+    constexpr int kA = kKind == kLossGrads ? kG : kF, kDeep = kLossDeep<kKind, kF, kG>;
     using Shape = LossShape<kA, kF>;
     LossPipe q;
     q.smem0 = ptx::smem_u32(ptx::align_1024(raw));
@@ -1063,7 +998,7 @@ __global__ void __launch_bounds__(kLossThreads, 1) loss_kernel(const __grid_cons
     ptx::grid_launch();
     ptx::grid_wait();
     const int warp = ptx::warp_index(), pair = (int)(blockIdx.x >> 1), pairs = (int)(gridDim.x >> 1), in_pair = (int)(blockIdx.x & 1);
-    const LossInfo info = loss_forward(kKind) && a.direct ? LossInfo{(uint32_t)a.direct, 1.f, 1.f, 1.f} : *a.info;
+    const LossInfo info = loss_forward(kKind) && a.direct ? LossInfo{(uint32_t)a.direct, 1.f} : *a.info;
     const int rows = (int)info.rows;
     // Registers of the launch, 640 x 96, as 128 x 40 (the loading and the issuing warp, two that idle) and 512 x 104.  Sixteen result warps with a quarter of the columns each: with eight and half of them, which
     // had 168, their own chain of waits took as long as four products (37137 rows of 128 over 25943 words: 469 us).
@@ -1072,14 +1007,13 @@ __global__ void __launch_bounds__(kLossThreads, 1) loss_kernel(const __grid_cons
         loss_load<kKind, kA, kF>(q, maps, a, rows, pair, pairs);
     } else if (warp == 1) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
-        if (in_pair == 0) loss_issue<kKind, kA, kF>(q, a, rows, pair, pairs);
+        if (in_pair == 0) loss_issue<kKind, kA, kF, kDeep>(q, a, rows, pair, pairs);
     } else if (warp < 4) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
         const int quad = warp & 3, part = (warp - 4) >> 2, lane = threadIdx.x & 31;
         const int cols = (kKind == kLossGrads ? a.grad_width : a.width) / 4;
-        const float scale = a.scale / (info.x_scale * info.w_scale);
         const uint32_t piece = q.pieces0 + (warp - 4) * kLossPiece;
         auto row_of = [&](const LossUnit &u) { return u.i * 256 + in_pair * 128 + quad * 32 + lane; };
         LossUnits<kKind> units(a, rows, pair, pairs);
@@ -1094,14 +1028,14 @@ __global__ void __launch_bounds__(kLossThreads, 1) loss_kernel(const __grid_cons
             r_next = loss_row<kKind>(a, rows, row_of(next), more && (kKind != kLossGrads || next.dx));
             const int row = row_of(u);
             if constexpr (kKind == kLossStats) {
-                if (!loss_stats<kF>(q, a, u, r, scale, rows, row, cols, joint + (turn & 1) * kJoint)) break;
+                if (!loss_stats<kF>(q, a, u, r, a.scale, rows, row, cols, joint + (turn & 1) * kJoint)) break;
             } else if constexpr (kKind == kLossTurns) {
-                if (!loss_stats_by_turns(q, a, u, r, scale, rows, row, joint + (2 * (part >> 1) + (turn & 1)) * kJoint)) break;
+                if (!loss_stats_by_turns(q, a, u, r, a.scale, rows, row, joint + (2 * (part >> 1) + (turn & 1)) * kJoint)) break;
                 q.c += 2;
             } else {
                 float v[64];
-                if (!loss_sums<kLossDeep<kKind, kF>>(q, u.kb1 - u.kb0, cols, v)) break;
-                if constexpr (kKind == kLossWeights) loss_weights<kG>(piece, a, r, scale, rows, row, u.j * a.width + part * cols, cols, v);
+                if (!loss_sums<kDeep>(q, u.kb1 - u.kb0, cols, v)) break;
+                if constexpr (kKind == kLossWeights) loss_weights<kG>(piece, a, r, a.scale, rows, row, u.j * a.width + part * cols, cols, v);
                 else if (u.slot >= 0) {
                     float *slot = a.slots + (((long)u.slot * 2 + in_pair) * a.grad_width + part * cols) * 128 + quad * 32 + lane;
 #pragma unroll
@@ -1336,7 +1270,7 @@ __global__ void __launch_bounds__(32 * kMergeWarps) loss_merge_kernel(const Loss
         code = __reduce_max_sync(0xffffffffu, code);
         for (int i = lane; i < (int)(kHeaderBytes / 4); i += 32) a.status[i] = i == 0 ? code : 0;
     }
-    const float scale = a.direct ? a.scale : a.scale / (a.info->x_scale * a.info->w_scale), c2 = scale * kLossLog2e;
+    const float c2 = a.scale * kLossLog2e;
     for (long r0 = (long)blockIdx.x * 32; r0 < rows; r0 += (long)gridDim.x * 32) {
         const long row = r0 + lane;
         LossStat stat{-INFINITY, 0.f};
@@ -1365,8 +1299,8 @@ __global__ void __launch_bounds__(32 * kMergeWarps) loss_merge_kernel(const Loss
                 there = label >= 0 && label < a.V;
             }
             const long n = a.direct ? row : a.index[row];
-            a.loss[n] = there ? loss_of(stat, a.chosen[row], scale) : 0.f;
-            a.lse[n] = there ? loss_lse(stat, scale) : 0.f;
+            a.loss[n] = there ? loss_of(stat, a.chosen[row], a.scale) : 0.f;
+            a.lse[n] = there ? loss_lse(stat, a.scale) : 0.f;
         }
         if (warps > 1) __syncthreads();
     }

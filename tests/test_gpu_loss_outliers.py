@@ -49,8 +49,8 @@ class Reference:
         q = p.scatter_add(1, at, -torch.ones_like(self.lse)[:, None])
         g = torch.where(there, dloss if isinstance(dloss, torch.Tensor) else torch.full_like(self.lse, dloss), 0.0).double() * scale
         self.dx, self.dw = g[:, None] * (q @ w), (g[:, None] * q).T @ x
-        # q: of p, of its difference from the label's 1, of its rounding: 24 bits (float32), two bfloat16 values' (bfloat16 where w has up to 2^22 elements), one's, or float16's and 2^-39
-        two = T == BF16 and V * C <= 1 << 22
+        # q: of p, of its difference from the label's 1, of its rounding: 24 bits (float32), two bfloat16 values' (bfloat16 over up to 8192 words, w of up to 2^22 elements), one's, or float16's and 2^-39
+        two = T == BF16 and V <= 8192 and V * C <= 1 << 22
         u = U32 if T == F32 else 2.0 ** -17 if two else UNIT[T]
         eps = (size + self.lse_bound + 2.0 ** -21 + 42 * U32)[:, None] * p + 2 * U32 * (q.abs() + p)
         dq = (eps + q.abs() * u + (2.0 ** -39 if T == F16 else 0.0)) * there[:, None]
@@ -79,7 +79,7 @@ def held(got, r, rows=slice(None), words=slice(None)):
     close(dw[words], r.dw[words], r.dw_bound[words], "dw")
 
 
-SIZES = [(300, 500, 80, F32), (40, 1000, 200, F32), (5, 3000, 64, F32), (300, 70000, 64, BF16)]
+SIZES = [(300, 500, 80, F32), (40, 1000, 200, F32), (5, 3000, 64, F32), (300, 500, 80, BF16), (2100, 256, 128, BF16), (300, 70000, 64, BF16)]
 
 
 @pytest.mark.parametrize("value", [1e6, 1e9, 1e13, 1e30])
@@ -132,7 +132,7 @@ def test_one_large_element_of_w(rows, vocab, width, dtype, value):
 
 
 @pytest.mark.parametrize("rows,vocab,width", [(300, 500, 80), (1500, 6000, 64)])
-@pytest.mark.parametrize("dtype,value", [(F32, 1e4), (F32, 1e12), (F32, 1e25)], ids=str)
+@pytest.mark.parametrize("dtype,value", [(F32, 1e4), (F32, 1e12), (F32, 1e25), (BF16, 1e4), (BF16, 1e12), (BF16, 1e25)], ids=str)
 def test_one_large_weight_of_a_row(rows, vocab, width, dtype, value):
     """dloss: the other rows' part in dw, seen in words that the row with the large weight has nothing to do with."""
     x, w, labels, g = problem(rows, vocab, width, dtype)
@@ -152,13 +152,13 @@ def test_one_large_weight_of_a_row(rows, vocab, width, dtype, value):
 
 @pytest.mark.parametrize("size", [1e25, 1e-25, 1e15, 1e-15])
 @pytest.mark.parametrize("rows,vocab,width", [(300, 500, 80), (1500, 6000, 200)])
-@pytest.mark.parametrize("dtype", [F32], ids=str)
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=str)
 def test_sizes_near_either_end(rows, vocab, width, dtype, size):
     x, w, labels, g = problem(rows, vocab, width, dtype, size=size)
     held(run(x, w, labels), Reference(x, w, labels))
 
 
-@pytest.mark.parametrize("dtype", [F32, F16], ids=str)
+@pytest.mark.parametrize("dtype", [F32, BF16, F16], ids=str)
 @pytest.mark.parametrize("rows,vocab,width", [(300, 500, 80), (600, 5003, 136)])
 def test_results_to_their_types_rounding(rows, vocab, width, dtype):
     """What q is held in, 16 bits in bfloat16 (w up to 2^22 elements), shows in the gradients."""

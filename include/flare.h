@@ -424,7 +424,7 @@ int flare_embed_backward(const flare_embed_desc_t *desc, const flare_drop_t *dro
  * 1024 or 1536 where p is held in two or three values, where that is more).  A row whose label is outside [0, vocab) takes no part: loss, lse and dx are 0, and what x holds there is not looked at.
  * x, dx [rows, width], w, dw [vocab, width] of dtype, rows stride_* apart; labels [rows] of label_bits (32 or 64); loss, lse, dloss [rows] float32 (dloss NULL: ones); dx or dw may
  * be NULL if not wanted.  Products run on the tensor cores with float32 sums.  float16: x and w as they are, p - [v = labels[n]] (times what dloss[n] is beyond a power of two, if given) rounded to float16 times 2^15
- * (2^14), x times that power of two, over the largest of them, for dw held down to 2^-25.
+ * (2^14), x times that power of two, for dw, held down to 2^-39 of the largest of those.
  * bfloat16: x and w as they are, p - [v = labels[n]] (times dloss[n], if given) rounded to bfloat16, with up to 8192 words and vocab x width up to 2^22 to two bfloat16 values (2^-17).  float32: three bfloat16 values each, which hold all 24 bits whatever the sizes, products to 2^-24.  A wait inside the kernels that gave up is reported by flare_check(workspace).
  */
 typedef struct {

@@ -33,7 +33,7 @@ constexpr size_t kPieceBytes = 512u << 20;
 struct LossPlan {
     bool bf16;                   // what is multiplied is bfloat16 (else float16)
     int planes, g_planes;        // values of 16 bits to an element of X and W, of G
-    int Cp, chunks, pairs;
+    int Cp, chunks, x_blocks, pairs;
     long cap;
     int width;                   // of a tile of X W^T
     int Vp, pieces;              // words of a piece
@@ -58,6 +58,7 @@ LossPlan loss_plan(const flare_loss_desc_t *d, int sms, bool backward) {
     // rows of packed X and W: whole 16 bytes, of wide ones whole lines (TMA takes 128-byte pieces of them)
     p.Cp = d->width > 256 ? (d->width + 63) / 64 * 64 : (d->width + 7) / 8 * 8;
     p.chunks = (int)((d->rows + kLossChunk - 1) / kLossChunk);
+    p.x_blocks = d->dtype == FLARE_DTYPE_F16 && backward ? (int)std::max(1L, std::min(4L * sms, (long)d->rows * d->width / 8192)) : 0;
     p.pairs = std::max(1, sms / 2);
     p.cap = std::max(1L, (long)(d->rows + 255) / 256) * 256;
     p.width = tile_width(p.cap / 256, d->vocab, p.pairs);
@@ -80,7 +81,7 @@ int few_blocks(const flare_loss_desc_t *d, int sms) {
     const long groups = (d->vocab + kFewWords - 1) / kFewWords, warps = (long)sms * (few_rows(d) <= 2 ? 4 : 2) * (kFewThreads / 32), rounds = (groups + warps - 1) / warps;
     return (int)(((groups + rounds - 1) / rounds + kFewThreads / 32 - 1) / (kFewThreads / 32));
 }
-struct LossLayout { size_t info, rank, chunk, px, pd, pw, index, label, part, chosen, gave_up, lse_of, gm, coef, g, acc, slots, total; };
+struct LossLayout { size_t info, rank, chunk, largest, px, pd, pw, index, label, part, chosen, gave_up, lse_of, gm, coef, g, acc, slots, total; };
 LossLayout loss_layout(const flare_loss_desc_t *d, const LossPlan &p, bool backward) {
     LossLayout w{};
     size_t off = kHeaderBytes;
@@ -88,6 +89,7 @@ LossLayout loss_layout(const flare_loss_desc_t *d, const LossPlan &p, bool backw
     take(w.info, sizeof(LossInfo));
     take(w.rank, sizeof(int) * (size_t)d->rows);
     take(w.chunk, sizeof(LossChunk) * (size_t)p.chunks);
+    take(w.largest, sizeof(int) * (size_t)p.x_blocks);
     const size_t row = sizeof(uint16_t) * (size_t)p.planes * p.Cp;
     take(w.px, row * p.cap);
     take(w.pw, row * d->vocab);                               // (whether W can be taken as it stands is known with its address)
@@ -194,19 +196,23 @@ int prepare_loss(const flare_loss_desc_t *d, const LossPlan &p, const LossLayout
     const long ld_x = d->stride_x ? d->stride_x : d->width, ld_w = d->stride_w ? d->stride_w : d->width;
     const bool own_w = f32 || !aligned16(w) || ld_w % 8 != 0;
     LossScan s{};
-    s.labels = labels; s.wide = d->label_bits == 64; s.rows = d->rows; s.V = d->vocab; s.chunks = p.chunks; s.dloss = k.dloss;
+    s.labels = labels; s.wide = d->label_bits == 64; s.rows = d->rows; s.V = d->vocab; s.chunks = p.chunks;
+    if (k.pd) {
+        s.C = d->width; s.x_blocks = p.x_blocks; s.x = x; s.ld_x = ld_x; s.dloss = k.dloss;
+        s.largest = reinterpret_cast<int *>(ws + l.largest);
+    }
     s.rank = reinterpret_cast<int *>(ws + l.rank); s.chunk = reinterpret_cast<LossChunk *>(ws + l.chunk);
     s.status = reinterpret_cast<uint32_t *>(ws);
     int rc;
     // rows of a block: so many that a thread has four groups of columns, and that there are no more than four blocks an SM; whole parts of a chunk
     k.pack_rows = 4;
     while (k.pack_rows < kLossChunk && ((long)k.pack_rows * (p.Cp / 8) < 4 * kPackThreads || (long)k.pack_rows * 4 * device_info().sms < d->rows)) k.pack_rows *= 2;
-    const bool alone = d->rows <= kPackAlone && k.pack_rows <= kPackThreads;
-    if (!alone) FLARE_CUDA(launch_after(loss_scan_kernel, (unsigned)s.chunks, kScanThreads, 0, st, s));
+    const bool alone = d->rows <= kPackAlone && !k.pd && k.pack_rows <= kPackThreads;
+    if (!alone) FLARE_CUDA(launch_after(loss_scan_kernel, (unsigned)(s.chunks + s.x_blocks), kScanThreads, 0, st, s));
     k.labels = labels; k.x = x; k.w = w; k.wide = s.wide; k.rows = d->rows; k.cap = p.cap; k.ld_x = ld_x; k.ld_w = ld_w;
     k.w_rows = own_w ? d->vocab : 0; k.C = d->width; k.Cp = p.Cp; k.V = d->vocab; k.chunks = p.chunks;
     k.pack_blocks = (int)((d->rows + k.pack_rows - 1) / k.pack_rows);
-    k.rank = alone ? nullptr : s.rank; k.status = s.status; k.chunk = s.chunk;
+    k.rank = alone ? nullptr : s.rank; k.status = s.status; k.chunk = s.chunk; k.largest = s.largest; k.x_blocks = s.x_blocks;
     k.info = reinterpret_cast<LossInfo *>(ws + l.info);
     k.px = reinterpret_cast<uint16_t *>(ws + l.px); k.pw = reinterpret_cast<uint16_t *>(ws + l.pw);
     k.index = reinterpret_cast<int *>(ws + l.index); k.label = reinterpret_cast<int *>(ws + l.label);

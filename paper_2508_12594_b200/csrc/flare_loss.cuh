@@ -19,7 +19,8 @@
 // bfloat16 and float16 are multiplied as they are, G in the same type, rounded once.  bfloat16's G is q where one dloss is that of all rows (next to a label q is next to -1, which is no rounding), else dloss scale q
 // (2^-9, as the gradients themselves will be; dloss in a second X instead put the same rounding there, and as many more elements were moved); of a small vocabulary it is two bfloat16 values (2^-17), two products of
 // either gradient.  float16's G is q times 2^15, so that probabilities down to 2^-29 are
-// normal numbers; of a row's own dloss its mantissa is there too (q times 2^14 and up to 2) and its power of two, which rounds nothing, in a second X and in dX's rows.
+// normal numbers; of a row's own dloss its mantissa is there too (q times 2^14 and up to 2) and its power of two in dX's rows and in a second X, times one more that puts the largest element of that just
+// below 2^15: elements of x times dloss are held down to 2^-39 of the largest of them.
 // float32: X, W, G as three bfloat16 values each, which hold all 24 bits over all of float32's range, a product as the six of them that are above 2^-24 of it; sums leave tensor memory, which
 // truncates, every 64 of K to be added up in registers.  (Two float16 halves, 22 bits, take three products, but want one power of two for all of X, of W and of a row's dloss: an element
 // of 1e9 in one row put the others' losses off by 3e-3, one of 1e13 by 4.)
@@ -35,10 +36,10 @@ namespace flare {
 // What the packing leaves for the kernels behind it, on the device.
 struct LossInfo {
     uint32_t rows;               // with a label
-    float dmax;                  // where dloss is in the second X: the power of two of the largest of a row, else 1
+    float d_scale;               // where dloss is in the second X: that is 1 / d_scale times what it stands for, else 1
 };
 // Per 1024 rows.
-struct LossChunk { uint32_t rows; float dmax; };
+struct LossChunk { uint32_t rows; };
 
 __device__ __forceinline__ int64_t label_at(const void *labels, int wide, long n) {
     return wide ? static_cast<const int64_t *>(labels)[n] : (int64_t) static_cast<const int32_t *>(labels)[n];
@@ -64,19 +65,28 @@ struct LossScan {
     int wide;
     long rows;
     int V, chunks;
-    const float *dloss;                       // or null
+    // blocks beyond the chunks', where there is to be a second X: the largest sum of the binary exponents of an element of x and of its row's dloss (float16)
+    int C, x_blocks;
+    const void *x;
+    long ld_x;
+    const float *dloss;
+    int *largest;                             // [x_blocks]
     int *rank;                                // [rows]: among the labelled rows of its chunk, or -1
     LossChunk *chunk;
     uint32_t *status;
 };
-__device__ __forceinline__ float finite_abs(float v) { return fabsf(v) <= 3.4028234e38f ? fabsf(v) : 0.f; }
-__device__ __forceinline__ float block_max(float v, float *shared) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+// The binary exponent of v (2^e <= |v| < 2^(e + 1)): -126 for less than a normal number, 0 for what is none.
+__device__ __forceinline__ int exponent_of(float v) {
+    const int e = (int)(__float_as_uint(v) >> 23 & 255);
+    return e == 255 ? 0 : max(e, 1) - 127;
+}
+constexpr int kNoExponent = -1000;
+__device__ __forceinline__ int block_max(int v, int *shared) {
+    v = __reduce_max_sync(0xffffffffu, v);
     if ((threadIdx.x & 31) == 0) shared[threadIdx.x >> 5] = v;
     __syncthreads();
-    v = 0.f;
-    for (int w = 0; w < (int)blockDim.x / 32; ++w) v = fmaxf(v, shared[w]);
+    v = shared[0];
+    for (int w = 1; w < (int)blockDim.x / 32; ++w) v = max(v, shared[w]);
     __syncthreads();
     return v;
 }
@@ -95,14 +105,48 @@ template <typename T> __device__ __forceinline__ void eight_of(const T *p, bool 
     }
 }
 __global__ void __launch_bounds__(kScanThreads) loss_scan_kernel(const LossScan a) {
-    __shared__ float shared[32];
+    __shared__ int shared[32];
     __shared__ uint32_t before[33];
     ptx::grid_launch();
     ptx::grid_wait();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (blockIdx.x == 0 && threadIdx.x < kHeaderBytes / 4) a.status[threadIdx.x] = 0;
+    if ((int)blockIdx.x >= a.chunks) {
+        const __half *x = static_cast<const __half *>(a.x);
+        const bool vec = a.C % 8 == 0 && a.ld_x % 8 == 0 && (reinterpret_cast<uintptr_t>(x) & 15) == 0;
+        constexpr int kBatch = 4;                             // groups of eight columns that are asked for before the first is looked at
+        LossWalk walk((uint64_t)(blockIdx.x - a.chunks) * kScanThreads + threadIdx.x, (uint64_t)a.x_blocks * kScanThreads, (uint32_t)(a.C + 7) / 8);
+        int most = kNoExponent;
+        while (walk.row < a.rows) {
+            LossEight<__half> e[kBatch];
+            float d[kBatch];                                  // 0: not looked at
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) {
+                d[k] = 0.f;
+                if (walk.row < a.rows) {
+                    const int64_t label = label_at(a.labels, a.wide, walk.row);
+                    if (label >= 0 && label < a.V) d[k] = a.dloss[walk.row];
+                    if (d[k] != 0.f) eight_of(x + walk.row * a.ld_x + 8 * walk.group, vec, a.C - (int)(8 * walk.group), e[k]);
+                }
+                walk.next();
+            }
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) {
+                if (d[k] == 0.f) continue;
+                float v = 0.f;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float u = fabsf(__half2float(reinterpret_cast<const __half *>(e[k].q)[i]));
+                    if (u <= 65504.f) v = fmaxf(v, u);
+                }
+                if (v > 0.f) most = max(most, exponent_of(v) + exponent_of(d[k]));
+            }
+        }
+        most = block_max(most, shared);
+        if (threadIdx.x == 0) a.largest[blockIdx.x - a.chunks] = most;
+        return;
+    }
     // four times 256 rows of the chunk, in order
-    float most = 0.f;
     bool there[kLossChunk / kScanThreads];
 #pragma unroll
     for (int k = 0; k < kLossChunk / kScanThreads; ++k) {
@@ -111,7 +155,6 @@ __global__ void __launch_bounds__(kScanThreads) loss_scan_kernel(const LossScan 
         if (n < a.rows) {
             const int64_t label = label_at(a.labels, a.wide, n);
             there[k] = label >= 0 && label < a.V;
-            if (there[k] && a.dloss) most = fmaxf(most, finite_abs(a.dloss[n]));
         }
         const uint32_t m = __ballot_sync(0xffffffffu, there[k]);
         if (lane == 0) before[k * (kScanThreads / 32) + warp] = __popc(m);
@@ -128,8 +171,8 @@ __global__ void __launch_bounds__(kScanThreads) loss_scan_kernel(const LossScan 
         before[lane] = sum - own;
         if (lane == 31) before[32] = sum;
     }
-    most = block_max(most, shared);
-    if (threadIdx.x == 0) a.chunk[blockIdx.x] = LossChunk{before[32], most};
+    __syncthreads();
+    if (threadIdx.x == 0) a.chunk[blockIdx.x] = LossChunk{before[32]};
 #pragma unroll
     for (int k = 0; k < kLossChunk / kScanThreads; ++k) {
         const long n = (long)blockIdx.x * kLossChunk + k * kScanThreads + threadIdx.x;
@@ -145,6 +188,8 @@ struct LossPack {
     int C, Cp, V, chunks, pack_blocks, pack_rows;   // Cp: C up to a multiple of eight
     const int *rank;                          // the scan's; null: there was none
     const LossChunk *chunk;
+    const int *largest;                       // with pd: the scan's
+    int x_blocks;
     uint32_t *status;
     LossInfo *info;
     uint16_t *px, *pd, *pw;                   // packed X, packed dloss X (or null), packed W: planes of [cap][Cp], [V][Cp]
@@ -160,13 +205,8 @@ struct LossPack {
     long ld_dx;
 };
 constexpr int kPackThreads = 256;             // of a block, which takes 4 to 1024 rows (of one chunk)
-constexpr int kPackAlone = 4096;              // rows up to which every block finds for itself, in all labels, what the scan would tell it, where no maxima are wanted: a launch less (4096 rows over 5000 words of 256: forward 23.1 us, with it 25.3)
+constexpr int kPackAlone = 4096;              // rows up to which every block finds for itself, in all labels, what the scan would tell it, where there is no second X: a launch less (4096 rows over 5000 words of 256: forward 23.1 us, with it 25.3)
 
-// The power of two at or below |d| (2^-126 for less), `other` where d is none that has one.
-__device__ __forceinline__ float two_of(float d, float other) {
-    const uint32_t e = __float_as_uint(d) & 0x7f800000u;
-    return e == 0x7f800000u ? other : __uint_as_float(max(e, 0x00800000u));
-}
 // What the products multiply: the type as it is; float32 as three bfloat16 values, each what rounding to those before it has left.
 template <typename T> constexpr int kPacked = sizeof(T) == 4 ? 3 : 1;
 __device__ __forceinline__ void three_of(float v, uint16_t (&t)[3]) {
@@ -208,10 +248,10 @@ __device__ __forceinline__ void pack_eight(const LossEight<T> &e, float f, bool 
 }
 template <typename T>
 __global__ void __launch_bounds__(kPackThreads) loss_pack_kernel(const LossPack a) {
-    __shared__ float shared[32];
+    __shared__ int shared[32];
     __shared__ uint32_t sums[2][kPackThreads / 32];
     __shared__ int to_row[kLossChunk];                        // of packed X; -1: no label
-    __shared__ float d_row[kLossChunk];                       // power of two of dloss, over the largest of them
+    __shared__ float d_row[kLossChunk];                       // what x is multiplied by in the second X
     ptx::grid_launch();
     ptx::grid_wait();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -242,20 +282,17 @@ __global__ void __launch_bounds__(kPackThreads) loss_pack_kernel(const LossPack 
     const long n0 = (long)blockIdx.x * a.pack_rows;
     const int chunk = (int)(n0 / kLossChunk);
     uint32_t base = 0, total = 0;
-    float dmax = 0.f;
     if (alone)
         for (long n = threadIdx.x; n < a.rows; n += kPackThreads) {
             const int64_t label = label_at(a.labels, a.wide, n);
             if (label < 0 || label >= a.V) continue;
             ++total;
             if (n < n0) ++base;
-            if (a.dloss) dmax = fmaxf(dmax, finite_abs(a.dloss[n]));
         }
     for (int i = alone ? a.chunks : threadIdx.x; i < a.chunks; i += kPackThreads) {
         const LossChunk c = a.chunk[i];
         total += c.rows;
         if (i < chunk) base += c.rows;
-        dmax = fmaxf(dmax, c.dmax);
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
@@ -263,11 +300,17 @@ __global__ void __launch_bounds__(kPackThreads) loss_pack_kernel(const LossPack 
         total += __shfl_xor_sync(0xffffffffu, total, o);
     }
     if (lane == 0) { sums[0][warp] = base; sums[1][warp] = total; }
-    dmax = block_max(dmax, shared);                           // (and a barrier for the sums)
+    int d_shift = 0;                                          // binary exponent of d_scale
+    if (a.pd) {
+        int most = kNoExponent;
+        for (int i = threadIdx.x; i < a.x_blocks; i += kPackThreads) most = max(most, a.largest[i]);
+        most = block_max(most, shared);
+        if (most != kNoExponent) d_shift = min(max(most - 14, -126), 127);
+    }
+    __syncthreads();
     base = total = 0;
     for (int w = 0; w < kPackThreads / 32; ++w) { base += sums[0][w]; total += sums[1][w]; }
-    dmax = a.pd ? two_of(dmax, 1.f) : 1.f;
-    if (blockIdx.x == 0 && threadIdx.x == 0) *a.info = LossInfo{total, dmax};
+    if (blockIdx.x == 0 && threadIdx.x == 0) *a.info = LossInfo{total, ldexpf(1.f, d_shift)};
     const int rows = (int)min((long)a.pack_rows, a.rows - n0);
     if (alone) {                                              // (up to a row a thread)
         __syncthreads();                                      // (sums have been read)
@@ -291,8 +334,9 @@ __global__ void __launch_bounds__(kPackThreads) loss_pack_kernel(const LossPack 
             a.label[to] = (int)label_at(a.labels, a.wide, n);
             if (a.loss == nullptr) {
                 const float d = a.dloss ? a.dloss[n] : 1.f;
-                const float two = a.dloss ? two_of(d, dmax) : 1.f;
-                d_row[i] = two / dmax;
+                const int e = a.dloss ? exponent_of(d) : 0;
+                const float two = __uint_as_float((uint32_t)(e + 127) << 23);
+                d_row[i] = ldexpf(1.f, min(e - d_shift, 120));            // (beyond 2^38 x is zeros)
                 a.lse_of[to] = a.lse_in[n];
                 a.gm[to] = a.g_factor == 0.f ? d * a.mult : d / two * a.g_factor;
                 a.coef[to] = a.g_factor == 0.f ? 1.f : two * a.mult / a.g_factor;
@@ -400,7 +444,7 @@ struct LossArgs {
     void *dw, *dx;
     long ld_dw, ld_dx;
     int dw_vec, dx_vec;          // rows can be written 16 bytes at a time
-    float dw_factor;             // scale dloss_scale / g_factor (times dmax), or 1 where G holds them
+    float dw_factor;             // scale dloss_scale / g_factor (times d_scale), or 1 where G holds them
     float *acc;                  // dX over the pieces before, by tile: [2 blocks][grad_width columns][128 rows]
     float *slots;                // sums of parts of tiles, likewise, two per pair
 };
@@ -947,7 +991,7 @@ __device__ __forceinline__ void loss_gradient(uint32_t piece, const LossArgs &a,
     const int lane = threadIdx.x & 31, local = i * 256 + block * 128 + quad * 32 + lane, c0 = j * a.grad_width + col;
     if (c0 >= a.C) return;
     if (!dx) {
-        const float f = a.dw_factor * info.dmax;
+        const float f = a.dw_factor * info.d_scale;
         loss_out<E>(piece, static_cast<E *>(a.dw), a.ld_dw, a.dw_vec, local < a.words ? a.v0 + local : -1, c0, a.C, f, v);
         return;
     }

@@ -132,7 +132,7 @@ def test_one_large_element_of_w(rows, vocab, width, dtype, value):
 
 
 @pytest.mark.parametrize("rows,vocab,width", [(300, 500, 80), (1500, 6000, 64)])
-@pytest.mark.parametrize("dtype,value", [(F32, 1e4), (F32, 1e12), (F32, 1e25), (BF16, 1e4), (BF16, 1e12), (BF16, 1e25)], ids=str)
+@pytest.mark.parametrize("dtype,value", [(F32, 1e4), (F32, 1e12), (F32, 1e25), (BF16, 1e4), (BF16, 1e12), (BF16, 1e25), (F16, 1e4)], ids=str)
 def test_one_large_weight_of_a_row(rows, vocab, width, dtype, value):
     """dloss: the other rows' part in dw, seen in words that the row with the large weight has nothing to do with."""
     x, w, labels, g = problem(rows, vocab, width, dtype)
@@ -147,7 +147,26 @@ def test_one_large_weight_of_a_row(rows, vocab, width, dtype, value):
     rest = torch.ones(rows, dtype=torch.bool, device="cuda")
     rest[0] = False
     r = Reference(x, w, without, dloss)
+    if dtype == F16:                                         # (what x times a power of two is held down to is by the largest, which is that row's)
+        q = (torch.softmax(x.double() @ w.double().T, 1) - torch.nn.functional.one_hot(labels.clamp(0), vocab)).abs()
+        r.dw_bound += 2.0 ** -38 * value * float(x[0].abs().max()) * (q * ((without >= 0) & (without < vocab))[:, None]).sum(0)[:, None]
     held(got, r, rest, none)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16], ids=str)
+def test_weights_of_nothing(dtype):
+    """dloss of zeros, of one row only, of the smallest numbers beside one."""
+    x, w, labels, _ = problem(300, 500, 80, dtype)
+    dloss = torch.zeros(300, device="cuda")
+    for tiny in (0.0, 1e-38, 1e-42):
+        dloss[:] = tiny
+        loss, lse, dx, dw = run(x, w, labels, dloss)
+        assert (dx.abs() <= 1e-34).all() and (dw.abs() <= 1e-34).all()
+        dloss[1] = 1.0
+        r = Reference(x, w, labels, dloss)
+        r.dx_bound += 1e-34                                  # (what is below float32's normal numbers: 300 rows of 1e-38 times up to 5)
+        r.dw_bound += 1e-34
+        held(run(x, w, labels, dloss), r)
 
 
 @pytest.mark.parametrize("size", [1e25, 1e-25, 1e15, 1e-15])

@@ -459,6 +459,7 @@ __device__ __forceinline__ uint2 before_in_block(uint2 own, uint2 *scan) {
 __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(const SortArgs a) {
     extern __shared__ __align__(16) uint32_t counts[];        // [32 warps][bins], [bins] of the block, [bins] from places here to places in memory, [32] pairs of a scan, pairs
     ptx::grid_wait();                                         // (then the launch behind this one: positions, which wait for nothing of this one's, but for what came before it)
+    __threadfence();                                          // (SumArgs::beside_zero)
     ptx::grid_launch();
     const uint32_t blocks = ptx::cluster_size(), rank = ptx::cluster_rank(), warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     // stretches: of a block, of a warp (whole groups of 32)
@@ -578,6 +579,7 @@ __device__ __forceinline__ void zero_bytes(uint8_t *p, uint64_t n) {
 template <typename T>
 __global__ void __launch_bounds__(kZeroThreads) embed_zero_kernel(const ZeroArgs a) {
     ptx::grid_wait();
+    __threadfence();                                          // (SumArgs::beside_zero)
     ptx::grid_launch();
     const uint32_t warps = gridDim.x * (kZeroThreads / 32), lane = threadIdx.x & 31;
     for (uint32_t g = a.first + blockIdx.x * (kZeroThreads / 32) + (threadIdx.x >> 5); g < a.last; g += warps) {
@@ -613,7 +615,9 @@ struct SumArgs {
     SumTask task[2];
     const void *dy;
     uint32_t ld_dy, C, columns;                               // columns: C up to whole groups of eight
-    int beside_zero;                                          // launches that need not wait for the one before them (embed_zero_kernel; of positions: the sort): 1: the sums, 2: the joins too
+    // Launches that need not wait for the one before them (embed_zero_kernel; of positions: the sort): 1: the sums, 2: the joins too.  They begin when all blocks of that one have got past their wait for what these
+    // need too.  A wait makes what came before visible to the grid that waits; to these it is made so by fences on both sides: of the grid between before it lets them begin, and of theirs before they read.
+    int beside_zero;
     uint32_t threads, lanes, tiles, chunks;                   // threads of a block; side by side over a row's units of columns, blocks side by side, chunks of a block one after the other
     DropArgs drop;
 };
@@ -688,7 +692,9 @@ __global__ void __launch_bounds__(kSumThreads, sizeof(O) == 4 || kWidth == 2 ? 2
     extern __shared__ __align__(16) float first_sum[];        // [threads][8 kW], and the same of last runs; by chunk: key of the first run, flags
     float *last_sum = first_sum + blockDim.x * 8 * kW;
     uint32_t *first_run = reinterpret_cast<uint32_t *>(last_sum + blockDim.x * 8 * kW), *flags = first_run + blockDim.x;
-    if (!a.beside_zero) {
+    if (a.beside_zero) {
+        __threadfence();
+    } else {
         ptx::grid_launch();
         ptx::grid_wait();
     }
@@ -829,7 +835,9 @@ template <typename T, bool kVec>
 __global__ void __launch_bounds__(kTokenThreads) embed_join_kernel(const SumArgs a) {
     __shared__ __align__(16) float sums[kTokenThreads][8];
     __shared__ uint32_t run_of[kJoinWarps], last_of[kJoinWarps];                // of a long run that begins in a warp's span: its key, its last span (0: none)
-    if (a.beside_zero < 2) {
+    if (a.beside_zero == 2) {
+        __threadfence();
+    } else {
         ptx::grid_launch();
         ptx::grid_wait();
     }

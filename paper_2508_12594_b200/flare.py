@@ -431,6 +431,13 @@ def muon_update(w, m, g, lr, momentum=0.95, weight_decay=0.0, nesterov=True, upd
 # ---- tokens: embedding, dropout, the loss over a vocabulary
 
 
+def _check_waits(ws, stream):
+    """Waits for the call that has used ws (on its tensors' device, which need not be the current one) and raises if a wait of it gave up."""
+    (stream or torch.cuda.current_stream(ws.device)).synchronize()
+    with torch.cuda.device(ws.device):
+        flare_check(ws, stream)
+
+
 class Drop(NamedTuple):
     """Dropout: the share p of elements (to 2^-17) that become 0, by a counter-based generator from seed and offset, 64 bits each.  step: an int64 tensor of one
     number on the GPU that the kernels add to offset when they run, so that a captured graph that counts it up drops other elements every time."""
@@ -480,8 +487,7 @@ def token_loss(x, w, labels, scale=1.0, out=None, stream=None, check=False):
     part: 0 and 0.  out: (loss, lse) to write to, either None.  With check=True the stream is synchronised and a device-side wait that gave up raises."""
     r, ws = (_native or _bind()).token_loss(x, w, labels, scale, out, stream)
     if check:
-        (stream or torch.cuda.current_stream()).synchronize()
-        flare_check(ws, stream)
+        _check_waits(ws, stream)
     return r
 
 
@@ -490,6 +496,5 @@ def token_loss_backward(x, w, labels, lse, dloss=1.0, scale=1.0, out=None, strea
     out: (dx, dw) to write to, either None."""
     r, ws = (_native or _bind()).token_loss_backward(x, w, labels, lse, dloss, scale, out, stream, LossGrads)
     if check:
-        (stream or torch.cuda.current_stream()).synchronize()
-        flare_check(ws, stream)
+        _check_waits(ws, stream)
     return r

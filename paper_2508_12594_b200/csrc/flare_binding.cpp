@@ -557,6 +557,13 @@ struct Outputs {
         if (given(i).defined()) fail(PyExc_ValueError, "stats: a tensor to write to, but want_stats is false");
         return at::Tensor();
     }
+    // a result that may not be wanted
+    bool wanted(PyObject *want, Py_ssize_t i, const char *name) const {
+        const int yes = PyObject_IsTrue(want);
+        if (yes < 0) throw PythonError{};
+        if (!yes && given(i).defined()) fail(PyExc_ValueError, std::string(name) + ": a tensor to write to, but want_" + name + " is false");
+        return yes != 0;
+    }
 };
 
 // What a call says about its rows: shape, types and norms.
@@ -957,8 +964,8 @@ BINDING(embed, 8)
     return wrap_written(y, a[6]);
 BINDING_END
 
-// tokens, dy, vocab, positions (0: none), scale, drop or None, dtype or None, accumulate, out (dtable, dpositions) or None, stream, class of the result
-BINDING(embed_backward, 11)
+// tokens, dy, vocab, positions (0: none), scale, drop or None, dtype or None, accumulate, out (dtable, dpositions) or None, stream, want_dtable, class of the result
+BINDING(embed_backward, 12)
     const at::Tensor &tokens = tensor(a[0]), &dy = tensor(a[1]);
     const OnDevice here(dy, {a[0], a[5], a[8]});
     flare_embed_desc_t d{};
@@ -972,7 +979,8 @@ BINDING(embed_backward, 11)
     const DropArg drop(a[5]);
     flare_stream_t st = stream_of(a[9]);
     const Outputs output{a[8], a[9], st};
-    const at::Tensor given = output.given(0);
+    const bool want_table = output.wanted(a[10], 0, "dtable");
+    const at::Tensor given = output.given(want_table ? 0 : 1);
     const at::ScalarType ot = dy.scalar_type(), dt = dtype_or(a[6], given.defined() ? given.scalar_type() : ot);
     d.dtype = dtype_code(dt); d.out_dtype = dtype_code(ot);
     std::vector<int64_t> shape = tokens.sizes().vec();
@@ -982,16 +990,17 @@ BINDING(embed_backward, 11)
     const int accumulate = PyObject_IsTrue(a[7]);
     if (accumulate < 0) throw PythonError{};
     if (accumulate && (!given.defined() || (positions > 0 && !output.given(1).defined()))) fail(PyExc_ValueError, "accumulate: expected tensors to add to as out");
+    if (!want_table && positions == 0) fail(PyExc_ValueError, "embed_backward: neither gradient is wanted");
     const auto options = dy.options().dtype(dt);
-    const at::Tensor table = output(0, {d.vocab, d.width}, options), pos = positions > 0 ? output(1, {d.positions, d.width}, options) : at::Tensor();
-    check(table, dt, {d.vocab, d.width});
+    const at::Tensor table = want_table ? output(0, {d.vocab, d.width}, options) : at::Tensor(), pos = positions > 0 ? output(1, {d.positions, d.width}, options) : at::Tensor();
+    if (table.defined()) check(table, dt, {d.vocab, d.width});
     if (pos.defined()) check(pos, dt, {d.positions, d.width});
     const size_t need = lib.embed_workspace_bytes(&d);
     if (need == 0) check_status(std::isfinite(d.scale) ? FLARE_ERR_UNSUPPORTED : FLARE_ERR_INVALID_ARG, "flare_embed_backward");
     const at::Tensor ws = scratch(need, dy, a[9], st);
-    check_status(unlocked([&] { return lib.embed_backward(&d, drop.get(), pt, ry.p, table.data_ptr(), pos.defined() ? pos.data_ptr() : nullptr, accumulate, ws.data_ptr(), need, st); }),
+    check_status(unlocked([&] { return lib.embed_backward(&d, drop.get(), pt, ry.p, table.defined() ? table.data_ptr() : nullptr, pos.defined() ? pos.data_ptr() : nullptr, accumulate, ws.data_ptr(), need, st); }),
                  "flare_embed_backward");
-    return named(a[10], output.wrapped({table, pos}));
+    return named(a[11], output.wrapped({table, pos}));
 BINDING_END
 
 // What forward and backward of the loss share.
@@ -1041,8 +1050,8 @@ BINDING(token_loss, 6)
     return Py_BuildValue("(NN)", r, wrap(ws));
 BINDING_END
 
-// x, w, labels, lse, dloss (a tensor or a number), scale, out (dx, dw) or None, stream, class of the result -> ((dx, dw), workspace)
-BINDING(token_loss_backward, 9)
+// x, w, labels, lse, dloss (a tensor or a number), scale, out (dx, dw) or None, stream, want_dx, want_dw, class of the result -> ((dx, dw), workspace)
+BINDING(token_loss_backward, 11)
     const at::Tensor &x = tensor(a[0]), &w = tensor(a[1]);
     const OnDevice here(x, {a[1], a[2], a[3], a[4], a[6]});
     Vocabulary c(x, w, tensor(a[2]), a[5]);
@@ -1059,14 +1068,25 @@ BINDING(token_loss_backward, 9)
     }
     flare_stream_t st = stream_of(a[7]);
     const Outputs output{a[6], a[7], st};
-    const at::Tensor dx = output(0, x.sizes(), x.options()), dw = output(1, w.sizes(), w.options());
-    const Rows rdx = rows_of(dx, c.dt, x.sizes(), "dx"), rdw = rows_of(dw, c.dt, w.sizes(), "dw");
-    c.d.stride_dx = rdx.stride; c.d.stride_dw = rdw.stride;
+    const bool want_dx = output.wanted(a[8], 0, "dx"), want_dw = output.wanted(a[9], 1, "dw");
+    if (!want_dx && !want_dw) fail(PyExc_ValueError, "token_loss_backward: neither gradient is wanted");
+    at::Tensor dx, dw;
+    Rows rdx, rdw;
+    if (want_dx) {
+        dx = output(0, x.sizes(), x.options());
+        rdx = rows_of(dx, c.dt, x.sizes(), "dx");
+        c.d.stride_dx = rdx.stride;
+    }
+    if (want_dw) {
+        dw = output(1, w.sizes(), w.options());
+        rdw = rows_of(dw, c.dt, w.sizes(), "dw");
+        c.d.stride_dw = rdw.stride;
+    }
     const size_t need = c.need(true, "flare_loss_backward");
     const at::Tensor ws = scratch(need, x, a[7], st);
     check_status(unlocked([&] { return lib.loss_backward(&c.d, c.rx.p, c.rw.p, c.labels, (const float *)lse.data_ptr(), dloss, rdx.p, rdw.p, ws.data_ptr(), need, st); }),
                  "flare_loss_backward");
-    PyObject *r = named(a[8], output.wrapped({dx, dw}));
+    PyObject *r = named(a[10], output.wrapped({dx, dw}));
     return Py_BuildValue("(NN)", r, wrap(ws));
 BINDING_END
 

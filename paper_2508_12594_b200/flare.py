@@ -448,13 +448,13 @@ class Drop(NamedTuple):
 
 
 class EmbedGrads(NamedTuple):
-    dtable: torch.Tensor
+    dtable: Optional[torch.Tensor]
     dpositions: Optional[torch.Tensor]
 
 
 class LossGrads(NamedTuple):
-    dx: torch.Tensor
-    dw: torch.Tensor
+    dx: Optional[torch.Tensor]
+    dw: Optional[torch.Tensor]
 
 
 def dropout(x, drop: Drop, residual=None, out=None, stream=None):
@@ -475,10 +475,10 @@ def embed(tokens, table, positions=None, scale=1.0, drop: Optional[Drop] = None,
 
 
 def embed_backward(tokens, dy, vocab: int, positions: int = 0, scale=1.0, drop: Optional[Drop] = None, dtype=None, accumulate=False, out=None,
-                   stream=None) -> EmbedGrads:
-    """Gradients of embed's tables, of `dtype` (dy's): dtable [vocab, width] and, with positions = L, dpositions [L, width].  out: (dtable, dpositions) to
-    write to, either None; accumulate: they are added to instead."""
-    return (_native or _bind()).embed_backward(tokens, dy, vocab, positions, scale, drop, dtype, accumulate, out, stream, EmbedGrads)
+                   stream=None, want_dtable=True) -> EmbedGrads:
+    """Gradients of embed's tables, of `dtype` (dy's): dtable [vocab, width] (None without want_dtable) and, with positions = L, dpositions [L, width].
+    out: (dtable, dpositions) to write to, either None; accumulate: they are added to instead."""
+    return (_native or _bind()).embed_backward(tokens, dy, vocab, positions, scale, drop, dtype, accumulate, out, stream, want_dtable, EmbedGrads)
 
 
 def token_loss(x, w, labels, scale=1.0, out=None, stream=None, check=False):
@@ -491,10 +491,10 @@ def token_loss(x, w, labels, scale=1.0, out=None, stream=None, check=False):
     return r
 
 
-def token_loss_backward(x, w, labels, lse, dloss=1.0, scale=1.0, out=None, stream=None, check=False) -> LossGrads:
+def token_loss_backward(x, w, labels, lse, dloss=1.0, scale=1.0, out=None, stream=None, check=False, want_dx=True, want_dw=True) -> LossGrads:
     """Gradients of token_loss from its inputs and its lse.  dloss: what reaches every row's loss, a float32 tensor like lse or one number for all.
-    out: (dx, dw) to write to, either None."""
-    r, ws = (_native or _bind()).token_loss_backward(x, w, labels, lse, dloss, scale, out, stream, LossGrads)
+    out: (dx, dw) to write to, either None.  want_dx, want_dw: one that is not wanted is not computed, and None."""
+    r, ws = (_native or _bind()).token_loss_backward(x, w, labels, lse, dloss, scale, out, stream, want_dx, want_dw, LossGrads)
     if check:
         _check_waits(ws, stream)
     return r

@@ -420,12 +420,17 @@ int flare_embed_backward(const flare_embed_desc_t *desc, const flare_drop_t *dro
  * Softmax cross entropy over a vocabulary, l[n, v] = scale x[n] . w[v]:
  *     lse[n] = log sum_v exp l[n, v];   loss[n] = lse[n] - l[n, labels[n]]
  *     dx[n] = g_n scale sum_v (p[n, v] - [v = labels[n]]) w[v];   dw[v] = scale sum_n g_n (p[n, v] - [v = labels[n]]) x[n];   p = exp(l - lse), g_n = dloss_scale dloss[n]
- * The logits are never kept: forward they stay on the chip, backward they are formed again, a piece of the vocabulary at a time (scratch of 512 MB at most, or of 512 bytes a row,
- * 1024 or 1536 where p is held in two or three values, where that is more).  A row whose label is outside [0, vocab) takes no part: loss, lse and dx are 0, and what x holds there is not looked at.
+ * The logits are never kept: forward they stay on the chip, backward they are formed again, a piece of the vocabulary at a time.  Scratch: backward, p of a piece (512 MB at most, or 512 bytes a row, 1024 or 1536
+ * where p is held in two or three values, where that is more), x packed (float16 with dloss: twice), w packed where it has to be (float32; rows off 16-byte boundaries), 4 bytes an element of dx where there
+ * are several pieces, up to 38 MB of shared tiles; forward, those two packed where they have to be, and 8 bytes a row and 256 (or 128) words.
+ * A row whose label is outside [0, vocab) takes no part: loss, lse and dx are 0, and what x holds there is not looked at.
  * x, dx [rows, width], w, dw [vocab, width] of dtype, rows stride_* apart; labels [rows] of label_bits (32 or 64); loss, lse, dloss [rows] float32 (dloss NULL: ones); dx or dw may
- * be NULL if not wanted.  Products run on the tensor cores with float32 sums.  float16: x and w as they are, p - [v = labels[n]] (times what dloss[n] is beyond a power of two, if given) rounded to float16 times 2^15
- * (2^14), x times that power of two, for dw, held down to 2^-39 of the largest of those.
- * bfloat16: x and w as they are, p - [v = labels[n]] (times dloss[n], if given) rounded to bfloat16, with up to 8192 words and vocab x width up to 2^22 to two bfloat16 values (2^-17).  float32: three bfloat16 values each, which hold all 24 bits whatever the sizes, products to 2^-24.  A wait inside the kernels that gave up is reported by flare_check(workspace).
+ * be NULL if not wanted.  Products run on the tensor cores with float32 sums, and p is formed from the same logits forward and backward (but for up to eight rows).  No row or word is held in fewer bits for what
+ * another holds, but for dw in float16 with dloss:
+ * float16: x and w as they are, p - [v = labels[n]] (times what dloss[n] is beyond a power of two, if given) rounded to float16 times 2^15 (2^14); x times that power of two, for dw, held down to 2^-39 of the largest.
+ * bfloat16: x and w as they are, p - [v = labels[n]] (times dloss[n], if given) rounded to bfloat16, over up to 8192 words with vocab x width up to 2^22 to two bfloat16 values (2^-17).
+ * float32: three bfloat16 values each, which hold all 24 bits; products to 2^-24.
+ * A wait inside the kernels that gave up is reported by flare_check(workspace).
  */
 typedef struct {
     int64_t rows;           /* 0 is allowed */
@@ -435,6 +440,8 @@ typedef struct {
     float dloss_scale;      /* backward */
     int64_t stride_x, stride_w, stride_dx, stride_dw;
 } flare_loss_desc_t;
+/* backward: 0 or 1; plus FLARE_LOSS_ALIGNED if x and w will begin on 16-byte boundaries (without it the size is enough wherever they begin). */
+#define FLARE_LOSS_ALIGNED 2
 size_t flare_loss_workspace_bytes(const flare_loss_desc_t *desc, int32_t backward);
 int flare_loss_forward(const flare_loss_desc_t *desc, const void *x, const void *w, const void *labels, float *loss, float *lse, void *workspace, size_t workspace_bytes,
                        flare_stream_t stream);

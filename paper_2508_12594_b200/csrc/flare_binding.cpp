@@ -1025,7 +1025,8 @@ struct Vocabulary {
         labels = numbers_of(l, d.label_bits, "labels");
     }
     size_t need(bool backward, const char *where) const {
-        const size_t n = lib.loss_workspace_bytes(&d, backward);
+        const bool aligned = reinterpret_cast<uintptr_t>(rx.p) % 16 == 0 && reinterpret_cast<uintptr_t>(rw.p) % 16 == 0;
+        const size_t n = lib.loss_workspace_bytes(&d, (backward ? 1 : 0) | (aligned ? FLARE_LOSS_ALIGNED : 0));
         if (n == 0) check_status(d.scale > 0.f && std::isfinite(d.scale) && std::isfinite(d.dloss_scale) ? FLARE_ERR_UNSUPPORTED : FLARE_ERR_INVALID_ARG, where);
         return n;
     }

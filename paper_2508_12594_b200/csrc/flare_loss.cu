@@ -82,7 +82,21 @@ int few_blocks(const flare_loss_desc_t *d, int sms) {
     return (int)(((groups + rounds - 1) / rounds + kFewThreads / 32 - 1) / (kFewThreads / 32));
 }
 struct LossLayout { size_t info, rank, chunk, largest, px, pd, pw, index, label, part, chosen, gave_up, lse_of, gm, coef, g, acc, slots, total; };
-LossLayout loss_layout(const flare_loss_desc_t *d, const LossPlan &p, bool backward) {
+// What is taken as it stands and needs no place for a packed copy: W of 16 bits, and X of few rows or of a small vocabulary in the forward, on 16-byte boundaries.
+struct LossLies { bool w, x; };
+long row_stride(int64_t stride, int width) { return stride ? stride : width; }
+LossLies loss_lies(const flare_loss_desc_t *d, bool backward, bool x_aligned, bool w_aligned) {
+    if (d->dtype == FLARE_DTYPE_F32) return LossLies{false, false};
+    const bool w = w_aligned && row_stride(d->stride_w, d->width) % 8 == 0, x = x_aligned && row_stride(d->stride_x, d->width) % 8 == 0;
+    // X too without packing, where all rows are one tile's (64 rows over 32000 words of 1024 take 20.3 us, packed 24.4) or the vocabulary is so small that rows without a label cost less than
+    // another pass over X: with 0.3 of them, 20000 rows over 1000 words of 512 24.0 us, packed 31.5; 40000 over 2025 of 64 46.4 and 43.3 (all labelled: 40.0 and 46.4)
+    return LossLies{w, !backward && w && x && (d->rows <= 256 || d->vocab <= 2048)};
+}
+// Rows that loss_few_kernel is run for, 0: it is not.  (Five to eight rows that need no packing are done sooner by the tensor cores: 8 rows over 32000 words of 1024 in bfloat16 in 26 us instead of 32.6, where four take
+// 23.2 and 22.0, one 26.4 and 16.6; of 1001, which are packed, eight take 54 and 36.5; in float32, of 2048, 220 and 72.)
+int few_rows_of(const flare_loss_desc_t *d, LossLies lies) { return lies.x && d->rows > 4 ? 0 : few_rows(d); }
+LossLayout loss_layout(const flare_loss_desc_t *d, const LossPlan &p, bool backward, LossLies lies) {
+    const bool few = !backward && few_rows_of(d, lies) > 0;   // (nothing is packed)
     LossLayout w{};
     size_t off = kHeaderBytes;
     auto take = [&](size_t &at, size_t bytes) { at = off; off += align_up(bytes); };
@@ -91,13 +105,13 @@ LossLayout loss_layout(const flare_loss_desc_t *d, const LossPlan &p, bool backw
     take(w.chunk, sizeof(LossChunk) * (size_t)p.chunks);
     take(w.largest, sizeof(int) * (size_t)p.x_blocks);
     const size_t row = sizeof(uint16_t) * (size_t)p.planes * p.Cp;
-    take(w.px, row * p.cap);
-    take(w.pw, row * d->vocab);                               // (whether W can be taken as it stands is known with its address)
+    take(w.px, lies.x || few ? 0 : row * p.cap);
+    take(w.pw, lies.w || few ? 0 : row * d->vocab);
     take(w.index, sizeof(int) * (size_t)p.cap);
     take(w.label, sizeof(int) * (size_t)p.cap);
     if (!backward) {
         const long tiles = (d->vocab + p.width - 1) / p.width;
-        take(w.part, sizeof(float2) * std::max<size_t>((size_t)tiles, few_rows(d) ? few_blocks(d, 2 * p.pairs) : 0) * p.cap);
+        take(w.part, sizeof(float2) * (few ? (size_t)few_blocks(d, 2 * p.pairs) : (size_t)tiles) * p.cap);
         take(w.chosen, sizeof(float) * (size_t)p.cap);
         take(w.gave_up, sizeof(uint32_t) * 2 * (size_t)p.pairs);
     } else {
@@ -186,15 +200,15 @@ int check_loss_call(const flare_loss_desc_t *d, const void *x, const void *w, co
     if (!workspace || !aligned16(workspace) || !w || (d->rows > 0 && (!x || !labels))) return FLARE_ERR_INVALID_ARG;
     if (!natural(x, t) || !natural(w, t) || !natural(labels, d->label_bits / 8)) return FLARE_ERR_INVALID_ARG;
     if (int rc = need_device()) return rc;
-    return workspace_bytes < loss_layout(d, loss_plan(d, device_info().sms, backward), backward).total ? FLARE_ERR_WORKSPACE_TOO_SMALL : FLARE_OK;
+    return workspace_bytes < loss_layout(d, loss_plan(d, device_info().sms, backward), backward, loss_lies(d, backward, aligned16(x), aligned16(w))).total ? FLARE_ERR_WORKSPACE_TOO_SMALL : FLARE_OK;
 }
 
 // Scan and packing, and the maps of X and W; what only the backward has is in k already.
-int prepare_loss(const flare_loss_desc_t *d, const LossPlan &p, const LossLayout &l, char *ws, const void *x, const void *w, const void *labels, LossPack k, LossMaps *maps,
+int prepare_loss(const flare_loss_desc_t *d, const LossPlan &p, const LossLayout &l, LossLies lies, char *ws, const void *x, const void *w, const void *labels, LossPack k, LossMaps *maps,
                  LossArgs *a, cudaStream_t st) {
     const bool f32 = d->dtype == FLARE_DTYPE_F32, bf16 = p.bf16;
-    const long ld_x = d->stride_x ? d->stride_x : d->width, ld_w = d->stride_w ? d->stride_w : d->width;
-    const bool own_w = f32 || !aligned16(w) || ld_w % 8 != 0;
+    const long ld_x = row_stride(d->stride_x, d->width), ld_w = row_stride(d->stride_w, d->width);
+    const bool own_w = !lies.w;
     LossScan s{};
     s.labels = labels; s.wide = d->label_bits == 64; s.rows = d->rows; s.V = d->vocab; s.chunks = p.chunks;
     if (k.pd) {
@@ -236,7 +250,11 @@ extern "C" {
 
 size_t flare_loss_workspace_bytes(const flare_loss_desc_t *desc, int32_t backward) {
     if (check_loss(desc) != FLARE_OK) return 0;
-    return loss_layout(desc, loss_plan(desc, device_info().sms, backward != 0), backward != 0).total;
+    const bool back = (backward & ~FLARE_LOSS_ALIGNED) != 0;
+    const LossPlan p = loss_plan(desc, device_info().sms, back);
+    auto bytes = [&](bool x, bool w) { return loss_layout(desc, p, back, loss_lies(desc, back, x, w)).total; };
+    if (backward & FLARE_LOSS_ALIGNED) return bytes(true, true);
+    return std::max(bytes(true, true), std::max(bytes(false, true), std::max(bytes(true, false), bytes(false, false))));
 }
 
 int flare_loss_forward(const flare_loss_desc_t *desc, const void *x, const void *w, const void *labels, float *loss, float *lse, void *workspace, size_t workspace_bytes,
@@ -250,15 +268,12 @@ int flare_loss_forward(const flare_loss_desc_t *desc, const void *x, const void 
         return FLARE_OK;
     }
     const LossPlan p = loss_plan(desc, device_info().sms, false);
-    const LossLayout l = loss_layout(desc, p, false);
+    const LossLies lies = loss_lies(desc, false, aligned16(x), aligned16(w));
+    const LossLayout l = loss_layout(desc, p, false, lies);
     char *ws = static_cast<char *>(workspace);
-    const long ld_x = desc->stride_x ? desc->stride_x : desc->width, ld_w = desc->stride_w ? desc->stride_w : desc->width;
-    // X and W as they stand, without packing, where all rows are one tile's (64 rows over 32000 words of 1024 take 20.3 us, packed 24.4) or the vocabulary is so small that rows without a label cost less than
-    // another pass over X: with 0.3 of them, 20000 rows over 1000 words of 512 24.0 us, packed 31.5; 40000 over 2025 of 64 46.4 and 43.3 (all labelled: 40.0 and 46.4)
-    const bool direct = (desc->rows <= 256 || desc->vocab <= 2048) && p.planes == 1 && aligned16(x) && aligned16(w) && ld_x % 8 == 0 && ld_w % 8 == 0;
-    // (five to eight rows that need no packing are done sooner by the tensor cores: 8 rows over 32000 words of 1024 in bfloat16 in 26 us instead of 32.6, where four take 23.2 and 22.0, one 26.4 and 16.6; of 1001,
-    // which are packed, eight take 54 and 36.5; in float32, of 2048, 220 and 72)
-    const int R = direct && desc->rows > 4 ? 0 : few_rows(desc);
+    const long ld_x = row_stride(desc->stride_x, desc->width), ld_w = row_stride(desc->stride_w, desc->width);
+    const bool direct = lies.x;
+    const int R = few_rows_of(desc, lies);
     if (R) {
         LossFew f{};
         f.x = x; f.w = w; f.labels = labels; f.wide = desc->label_bits == 64; f.rows = (int)desc->rows; f.C = desc->width; f.V = desc->vocab;
@@ -285,7 +300,7 @@ int flare_loss_forward(const flare_loss_desc_t *desc, const void *x, const void 
         if ((rc = make_plane_map(&maps.w, w, bf16, desc->width, desc->vocab, 1, ld_w, 64)) != FLARE_OK) return rc;
         a.C = desc->width; a.V = desc->vocab; a.bf16 = bf16; a.cap = p.cap; a.scale = desc->scale; a.status = reinterpret_cast<uint32_t *>(ws);
         a.labels = labels; a.wide = desc->label_bits == 64; a.direct = (int)desc->rows; a.gave_up = reinterpret_cast<uint32_t *>(ws + l.gave_up);
-    } else if (int rc = prepare_loss(desc, p, l, ws, x, w, labels, k, &maps, &a, st)) {
+    } else if (int rc = prepare_loss(desc, p, l, lies, ws, x, w, labels, k, &maps, &a, st)) {
         return rc;
     }
     a.words = desc->vocab; a.width = p.width; a.tiles_v = (desc->vocab + p.width - 1) / p.width;
@@ -316,7 +331,8 @@ int flare_loss_backward(const flare_loss_desc_t *desc, const void *x, const void
         return FLARE_OK;
     }
     const LossPlan p = loss_plan(desc, device_info().sms, true);
-    const LossLayout l = loss_layout(desc, p, true);
+    const LossLies lies = loss_lies(desc, true, aligned16(x), aligned16(w));
+    const LossLayout l = loss_layout(desc, p, true, lies);
     const bool f32 = desc->dtype == FLARE_DTYPE_F32, bf16 = p.bf16;
     char *ws = static_cast<char *>(workspace);
     LossPack k{};
@@ -329,7 +345,7 @@ int flare_loss_backward(const flare_loss_desc_t *desc, const void *x, const void
     k.pd = bf16 || !dloss || !dw ? nullptr : reinterpret_cast<uint16_t *>(ws + l.pd);
     LossMaps maps{};
     LossArgs a{};
-    if (int rc = prepare_loss(desc, p, l, ws, x, w, labels, k, &maps, &a, st)) return rc;
+    if (int rc = prepare_loss(desc, p, l, lies, ws, x, w, labels, k, &maps, &a, st)) return rc;
     int rc;
     if (k.pd) {
         if ((rc = make_plane_map(&maps.d, k.pd, bf16, p.Cp, p.cap, p.planes, p.Cp, 64)) != FLARE_OK) return rc;

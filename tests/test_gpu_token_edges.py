@@ -108,3 +108,35 @@ def test_one_gradient_of_the_embedding_is_refused():
     for kw in (dict(want_dtable=False), dict(positions=8, want_dtable=False, out=(torch.zeros(5, 16, device="cuda"), None)), dict(positions=8, want_dtable=False, accumulate=True)):
         with pytest.raises(ValueError):
             flare.embed_backward(t, dy, 5, **kw)
+
+
+@pytest.mark.parametrize("rows,vocab,width,dtype", [(8, 300000, 8, BF16), (3, 1000, 64, F32), (6, 5000, 64, F16), (300, 1000, 64, BF16), (300, 5000, 64, F16), (300, 500, 64, F32)], ids=str)
+@pytest.mark.parametrize("off", [(0, 0), (1, 0), (0, 1), (1, 1)], ids=str)
+def test_the_scratch_that_is_asked_for_is_enough(rows, vocab, width, dtype, off):
+    """Through the C-ABI, x and w on 16-byte boundaries or not, with a workspace of just the size that is given without and, where they are, with FLARE_LOSS_ALIGNED; what lies behind it stays as it is."""
+    x, w, labels, _ = problem(rows, vocab, width, dtype)
+    x, w = (torch.cat([torch.zeros(o, device="cuda", dtype=dtype), t.reshape(-1)])[o:].view(t.shape) for t, o in zip((x, w), off))
+    want = flare.token_loss(x, w, labels)
+    d = flare.token_loss_backward(x, w, labels, want[1])
+    lib, code = flare.load(), {F32: flare.DTYPE_F32, BF16: flare.DTYPE_BF16, F16: flare.DTYPE_F16}
+    desc = flare.FlareLossDesc(rows=rows, width=width, vocab=vocab, dtype=code[dtype], label_bits=64, scale=1.0, dloss_scale=1.0)
+    for aligned in (0, 2):
+        loss, lse, dx, dw = torch.empty_like(want[0]), torch.empty_like(want[1]), torch.empty_like(x), torch.empty_like(w)
+        for backward in (0, 1):
+            need = lib.flare_loss_workspace_bytes(ctypes.byref(desc), backward | aligned)
+            ws = torch.full((need + 4096,), 0x5A, dtype=torch.uint8, device="cuda")
+            torch.cuda.synchronize()
+            p = [t.data_ptr() for t in (x, w, labels, lse, loss, dx, dw, ws)]
+            if backward:
+                status = lib.flare_loss_backward(ctypes.byref(desc), p[0], p[1], p[2], p[3], None, p[5], p[6], p[7], need, None)
+            else:
+                status = lib.flare_loss_forward(ctypes.byref(desc), p[0], p[1], p[2], p[4], p[3], p[7], need, None)
+            torch.cuda.synchronize()
+            assert (ws[need:] == 0x5A).all()
+            if aligned and any(off):
+                assert status in (flare.OK, flare.ERR_WORKSPACE_TOO_SMALL)
+                if status != flare.OK:
+                    break
+            assert status == flare.OK
+        else:
+            assert torch.equal(loss, want[0]) and torch.equal(lse, want[1]) and torch.equal(dx, d.dx) and torch.equal(dw, d.dw)

@@ -425,7 +425,7 @@ int flare_embed_backward(const flare_embed_desc_t *desc, const flare_drop_t *dro
  * are several pieces, up to 38 MB of shared tiles; forward, those two packed where they have to be, and 8 bytes a row and 256 (or 128) words.
  * A row whose label is outside [0, vocab) takes no part: loss, lse and dx are 0, and what x holds there is not looked at.
  * x, dx [rows, width], w, dw [vocab, width] of dtype, rows stride_* apart; labels [rows] of label_bits (32 or 64); loss, lse, dloss [rows] float32 (dloss NULL: ones); dx or dw may
- * be NULL if not wanted.  Products run on the tensor cores with float32 sums, and p is formed from the same logits forward and backward (but for up to eight rows).  No row or word is held in fewer bits for what
+ * be NULL if not wanted.  Products run on the tensor cores with float32 sums, and p is formed from the same logits forward and backward.  No row or word is held in fewer bits for what
  * another holds, but for dw in float16 with dloss:
  * float16: x and w as they are, p - [v = labels[n]] (times what dloss[n] is beyond a power of two, if given) rounded to float16 times 2^15 (2^14); x times that power of two, for dw, held down to 2^-39 of the largest.
  * bfloat16: x and w as they are, p - [v = labels[n]] (times dloss[n], if given) rounded to bfloat16, over up to 8192 words with vocab x width up to 2^22 to two bfloat16 values (2^-17).

@@ -76,9 +76,9 @@ int few_rows(const flare_loss_desc_t *d) {
     const int R = d->rows <= 1 ? 1 : d->rows <= 2 ? 2 : d->rows <= 4 ? 4 : 8;
     return d->rows <= 8 && few_smem(R, d->width) <= 96 * 1024 ? R : 0;
 }
-int few_blocks(const flare_loss_desc_t *d, int sms) {
+int few_blocks(const flare_loss_desc_t *d, long words, int sms) {
     // rounds of equal size over the warps that are at work at a time
-    const long groups = (d->vocab + kFewWords - 1) / kFewWords, warps = (long)sms * (few_rows(d) <= 2 ? 4 : 2) * (kFewThreads / 32), rounds = (groups + warps - 1) / warps;
+    const long groups = (words + kFewWords - 1) / kFewWords, warps = (long)sms * (few_rows(d) <= 2 ? 4 : 2) * (kFewThreads / 32), rounds = (groups + warps - 1) / warps;
     return (int)(((groups + rounds - 1) / rounds + kFewThreads / 32 - 1) / (kFewThreads / 32));
 }
 struct LossLayout { size_t info, rank, chunk, largest, px, pd, pw, index, label, part, chosen, gave_up, lse_of, gm, coef, g, acc, slots, total; };
@@ -111,7 +111,7 @@ LossLayout loss_layout(const flare_loss_desc_t *d, const LossPlan &p, bool backw
     take(w.label, sizeof(int) * (size_t)p.cap);
     if (!backward) {
         const long tiles = (d->vocab + p.width - 1) / p.width;
-        take(w.part, sizeof(float2) * (few ? (size_t)few_blocks(d, 2 * p.pairs) : (size_t)tiles) * p.cap);
+        take(w.part, sizeof(float2) * (few ? (size_t)few_blocks(d, d->vocab, 2 * p.pairs) : (size_t)tiles) * p.cap);
         take(w.chosen, sizeof(float) * (size_t)p.cap);
         take(w.gave_up, sizeof(uint32_t) * 2 * (size_t)p.pairs);
     } else {
@@ -176,22 +176,35 @@ int launch_pack(const LossPack &k, int blocks, cudaStream_t st) {
     return FLARE_OK;
 }
 
-template <typename T, int R, bool kVec>
+template <typename T, int R, bool kVec, int kG>
 int launch_few_as(const LossFew &f, int blocks, cudaStream_t st) {
     static std::atomic<uint64_t> opt_in{0};
-    auto *kernel = loss_few_kernel<T, R, kVec>;
+    auto *kernel = loss_few_kernel<T, R, kVec, kG>;
     if (int rc = ensure_big_smem(kernel, opt_in, 96 * 1024)) return rc;
     FLARE_CUDA(launch_after(kernel, (unsigned)blocks, kFewThreads, few_smem(R, f.C), st, f));
     return FLARE_OK;
 }
-template <typename T>
-int launch_few(const LossFew &f, int R, int blocks, cudaStream_t st) {
+template <typename T, int kG>
+int launch_few_of(const LossFew &f, int R, int blocks, cudaStream_t st) {
     const bool vec = f.C % 8 == 0 && aligned16(f.w) && f.ld_w * (long)sizeof(T) % 16 == 0;
-    auto launch = R == 1   ? (vec ? launch_few_as<T, 1, true> : launch_few_as<T, 1, false>)
-                  : R == 2 ? (vec ? launch_few_as<T, 2, true> : launch_few_as<T, 2, false>)
-                  : R == 4 ? (vec ? launch_few_as<T, 4, true> : launch_few_as<T, 4, false>)
-                           : (vec ? launch_few_as<T, 8, true> : launch_few_as<T, 8, false>);
+    auto launch = R == 1   ? (vec ? launch_few_as<T, 1, true, kG> : launch_few_as<T, 1, false, kG>)
+                  : R == 2 ? (vec ? launch_few_as<T, 2, true, kG> : launch_few_as<T, 2, false, kG>)
+                  : R == 4 ? (vec ? launch_few_as<T, 4, true, kG> : launch_few_as<T, 4, false, kG>)
+                           : (vec ? launch_few_as<T, 8, true, kG> : launch_few_as<T, 8, false, kG>);
     return launch(f, blocks, st);
+}
+// g_planes: of G, 0: forward
+int launch_few(const LossFew &f, int dtype, int g_planes, int R, int blocks, cudaStream_t st) {
+    auto launch = dtype == FLARE_DTYPE_F32    ? (g_planes ? launch_few_of<float, 3> : launch_few_of<float, 0>)
+                  : dtype == FLARE_DTYPE_BF16 ? (g_planes == 2 ? launch_few_of<__nv_bfloat16, 2> : g_planes ? launch_few_of<__nv_bfloat16, 1> : launch_few_of<__nv_bfloat16, 0>)
+                                              : (g_planes ? launch_few_of<__half, 1> : launch_few_of<__half, 0>);
+    return launch(f, R, blocks, st);
+}
+LossFew few_args(const flare_loss_desc_t *d, const LossPlan &p, const void *x, const void *w, const void *labels) {
+    LossFew f{};
+    f.x = x; f.w = w; f.labels = labels; f.wide = d->label_bits == 64; f.rows = (int)d->rows; f.C = d->width; f.V = d->vocab; f.words = d->vocab;
+    f.ld_x = row_stride(d->stride_x, d->width); f.ld_w = row_stride(d->stride_w, d->width); f.cap = p.cap; f.scale = d->scale;
+    return f;
 }
 
 // Checks that forward and backward share.
@@ -275,15 +288,10 @@ int flare_loss_forward(const flare_loss_desc_t *desc, const void *x, const void 
     const bool direct = lies.x;
     const int R = few_rows_of(desc, lies);
     if (R) {
-        LossFew f{};
-        f.x = x; f.w = w; f.labels = labels; f.wide = desc->label_bits == 64; f.rows = (int)desc->rows; f.C = desc->width; f.V = desc->vocab;
-        f.ld_x = ld_x; f.ld_w = ld_w; f.cap = p.cap; f.scale = desc->scale;
+        LossFew f = few_args(desc, p, x, w, labels);
         f.part = reinterpret_cast<float2 *>(ws + l.part); f.chosen = reinterpret_cast<float *>(ws + l.chosen);
-        const int blocks = few_blocks(desc, 2 * p.pairs);
-        if (int rc = desc->dtype == FLARE_DTYPE_F32    ? launch_few<float>(f, R, blocks, st)
-                     : desc->dtype == FLARE_DTYPE_BF16 ? launch_few<__nv_bfloat16>(f, R, blocks, st)
-                                                       : launch_few<__half>(f, R, blocks, st))
-            return rc;
+        const int blocks = few_blocks(desc, desc->vocab, 2 * p.pairs);
+        if (int rc = launch_few(f, desc->dtype, 0, R, blocks, st)) return rc;
         LossMerge m{};
         m.part = f.part; m.chosen = f.chosen; m.cap = p.cap; m.parts = blocks; m.loss = loss; m.lse = lse;
         m.labels = labels; m.wide = f.wide; m.V = f.V; m.direct = f.rows; m.status = reinterpret_cast<uint32_t *>(ws); m.scale = desc->scale;
@@ -363,6 +371,10 @@ int flare_loss_backward(const flare_loss_desc_t *desc, const void *x, const void
     auto weights = f32 ? launch_loss<kLossWeights, 3, 3, float> : p.g_planes == 2 ? launch_loss<kLossWeights, 1, 2, float> : launch_loss<kLossWeights, 1, 1, float>;
     auto grads = f32 ? launch_loss<kLossGrads, 3, 3, float> : !bf16 ? launch_loss<kLossGrads, 1, 1, __half> : p.g_planes == 2 ? launch_loss<kLossGrads, 1, 2, __nv_bfloat16> : launch_loss<kLossGrads, 1, 1, __nv_bfloat16>;
     auto *join = f32 ? loss_join_kernel<float> : desc->dtype == FLARE_DTYPE_BF16 ? loss_join_kernel<__nv_bfloat16> : loss_join_kernel<__half>;
+    // few rows: G by the kernel that the forward's statistics are of
+    const int R = few_rows_of(desc, loss_lies(desc, false, aligned16(x), aligned16(w)));
+    LossFew few = few_args(desc, p, x, w, labels);
+    few.lse_in = lse; few.gm = k.gm; few.g = a.g; few.ld_g = a.ld_g;
     // of tiles that several pairs can have shared: fewer than a round of either gradient
     const long warps = 2L * (p.pairs - 1) * 8 * (p.grad_width / kJoinCols);
     for (int i = 0; i < p.pieces; ++i) {
@@ -371,7 +383,12 @@ int flare_loss_backward(const flare_loss_desc_t *desc, const void *x, const void
         a.first = i == 0; a.last = i + 1 == p.pieces;
         a.width = tile_width(p.cap / 256, a.words, p.pairs);
         a.tiles_v = (a.words + a.width - 1) / a.width;
-        if ((rc = weights(maps, a, (int)std::min<long>(p.pairs, p.cap / 256 * a.tiles_v), st)) != FLARE_OK) return rc;
+        if (R) {
+            few.v0 = a.v0; few.words = a.words;
+            if ((rc = launch_few(few, desc->dtype, p.g_planes, R, few_blocks(desc, a.words, 2 * p.pairs), st)) != FLARE_OK) return rc;
+        } else if ((rc = weights(maps, a, (int)std::min<long>(p.pairs, p.cap / 256 * a.tiles_v), st)) != FLARE_OK) {
+            return rc;
+        }
         if ((rc = grads(maps, a, p.pairs, st)) != FLARE_OK) return rc;
         FLARE_CUDA(launch_after(join, (unsigned)((warps + kJoinWarps - 1) / kJoinWarps), 32 * kJoinWarps, 0, st, a, p.pairs));
     }

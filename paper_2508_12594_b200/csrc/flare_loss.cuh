@@ -863,8 +863,6 @@ __device__ __forceinline__ bool loss_stats_by_turns(LossPipe &q, const LossArgs 
 
 // Where 16 bytes of a row of 64 lie in a piece: neither rows a lane nor four lanes a row meet a bank conflict.
 __device__ __forceinline__ uint32_t piece_at(int row, int chunk) { return row * 64 + ((chunk ^ (row >> 1 & 3)) << 4); }
-// (Up to eight rows have lse from other sums, loss_few_kernel's: p is held to 1 there, for a logit of 1e8 may come out ten above its lse.)
-__device__ __forceinline__ float loss_most_one(float p) { return p > 1.f ? 1.f : p; }   // (NaN stays)
 // Backward: q of 32 rows and 32 columns at a time, as kG values of 16 bits, to G by way of shared memory, so that four lanes write 64 bytes of a row.
 template <int kG>
 __device__ __forceinline__ void loss_weights(uint32_t piece, const LossArgs &a, const LossRow &r, float scale, int rows, int row, int local0, int cols, float (&v)[64]) {
@@ -876,7 +874,7 @@ __device__ __forceinline__ void loss_weights(uint32_t piece, const LossArgs &a, 
     // the label's, where it is among the columns: put into the piece on its own
     const bool mine = at >= 0 && at < cols;
     float own = 0.f;
-    if (__any_sync(0xffffffffu, mine)) own = (loss_most_one(ptx::ex2(__fsub_rn(__fmul_rn(loss_pick(v, at), scale), lse) * kLossLog2e)) - 1.f) * f;
+    if (__any_sync(0xffffffffu, mine)) own = (ptx::ex2(__fsub_rn(__fmul_rn(loss_pick(v, at), scale), lse) * kLossLog2e) - 1.f) * f;
 #pragma unroll
     for (int k = 0; k < 64; k += 32) {
         if (k >= cols) break;
@@ -884,9 +882,7 @@ __device__ __forceinline__ void loss_weights(uint32_t piece, const LossArgs &a, 
         for (int e = 0; e < 32; e += 2) {
             // (products one by one: two at a time came out fused with the addition, whatever their rounding said)
             const float2 d = __fadd2_rn(make_float2(__fmul_rn(v[k + e], scale), __fmul_rn(v[k + e + 1], scale)), make_float2(-lse, -lse)), x = __fmul2_rn(d, make_float2(kLossLog2e, kLossLog2e));
-            float2 p = make_float2(ptx::ex2(x.x), ptx::ex2(x.y));
-            if (rows <= 8) p = make_float2(loss_most_one(p.x), loss_most_one(p.y));
-            const float2 y = __fmul2_rn(p, make_float2(f, f));
+            const float2 y = __fmul2_rn(make_float2(ptx::ex2(x.x), ptx::ex2(x.y)), make_float2(f, f));
             v[k + e] = y.x;
             v[k + e + 1] = y.y;
         }
@@ -1177,23 +1173,30 @@ __global__ void __launch_bounds__(32 * kJoinWarps, 2) loss_join_kernel(const Los
     }
 }
 
-// ---- forward of a few rows
+// ---- a few rows
 //
 // One row is scored as fast as W can be read, by fused multiply-adds in float32 (two a row and pair of elements, beside two conversions: one row over 32000 words of 1024, 66 MB in bfloat16, takes 12 to 16 us, 4 to
 // 5.5 TB/s, and the merge behind it 5; two or more are bound by instructions): a tile of a tensor core's product would have 248 empty rows, and float32 inputs would have W read and written once more for their three values.
 // A warp takes four words at a time, a lane eight columns of each (kVec: neighbours, 16 bytes a load; else 32 apart); X is in shared memory as float32, where the lanes' pieces of a row lie in
 // two sets of 16 bytes so that neighbouring lanes meet no bank conflict.  The 4 R sums are added up over the lanes by exchanges that halve their number (31 for all of 32 sums).
+//
+// Backward (kG > 0) the same sums give G, so that p = exp(l - lse) has the very logits that lse was formed of: of a row that has learned its label 1 - p is what counts, and another order of addition, the tensor cores',
+// put 35 times the error of a plain float32 gradient into it (2 rows over three words of 4032).  Both gradients are then taken from G as of many rows.
 constexpr int kFewThreads = 256, kFewWords = 4;
 struct LossFew {
     const void *x, *w, *labels;
-    int wide, rows, C, V;
+    int wide, rows, C, V, v0, words;          // words: of V, from v0 on
     long ld_x, ld_w, cap;
     float scale;
     float2 *part;                // [blocks][cap]
     float *chosen;
+    // backward
+    const float *lse_in, *gm;    // of rows; of packed rows
+    uint16_t *g;                 // planes [cap][ld_g]
+    long ld_g;
 };
 __host__ __device__ constexpr size_t few_smem(int R, int C) { return (size_t)R * ((C + 255) / 256 * 256) * sizeof(float); }
-template <typename T, int R, bool kVec>
+template <typename T, int R, bool kVec, int kG>
 __global__ void __launch_bounds__(kFewThreads, R <= 2 ? 4 : 2) loss_few_kernel(const LossFew a) {
     extern __shared__ float4 xs[];                            // [R][turns][2][32]
     __shared__ float2 stats[kFewThreads / 32][32];
@@ -1212,12 +1215,32 @@ __global__ void __launch_bounds__(kFewThreads, R <= 2 ? 4 : 2) loss_few_kernel(c
     if (row < a.rows) label = label_at(a.labels, a.wide, row);
     const float c2 = a.scale * kLossLog2e;
     LossStat stat{-INFINITY, 0.f};
+    int labelled = 0, to = -1;                                // backward: rows with a label; this one's place among them, -1: none
+    float lse = 0.f, gm = 0.f;
+    if constexpr (kG > 0) {
+        for (int r = 0; r < a.rows; ++r) {
+            const int64_t l = label_at(a.labels, a.wide, r);
+            if (l < 0 || l >= a.V) continue;
+            if (r == row) to = labelled;
+            ++labelled;
+        }
+        if (to >= 0) { lse = a.lse_in[row]; gm = a.gm[to]; }
+        // zeros in the rows up to 64 that the products over rows read, and in the columns up to whole 64 that those over words do
+        const int cols = (a.words + 63) / 64 * 8;
+        for (int i = blockIdx.x * kFewThreads + threadIdx.x; i < (64 - labelled) * cols; i += gridDim.x * kFewThreads)
+#pragma unroll
+            for (int h = 0; h < kG; ++h) *reinterpret_cast<uint4 *>(a.g + (h * a.cap + labelled + i / cols) * a.ld_g + i % cols * 8) = make_uint4(0, 0, 0, 0);
+        if (blockIdx.x == 0)
+            for (int i = threadIdx.x; i < labelled * 64; i += kFewThreads)
+                if (a.words + i % 64 < 8 * cols)
+                    for (int h = 0; h < kG; ++h) a.g[(h * a.cap + i / 64) * a.ld_g + a.words + i % 64] = 0;
+    }
     __syncthreads();
-    const int groups = (a.V + kFewWords - 1) / kFewWords;
+    const int groups = (a.words + kFewWords - 1) / kFewWords;
     for (int g = blockIdx.x * (kFewThreads / 32) + warp; g < groups; g += gridDim.x * (kFewThreads / 32)) {
         const T *p[kFewWords];
 #pragma unroll
-        for (int k = 0; k < kFewWords; ++k) p[k] = w + (long)min(g * kFewWords + k, a.V - 1) * a.ld_w;     // (beyond the last word: that again)
+        for (int k = 0; k < kFewWords; ++k) p[k] = w + (long)(a.v0 + min(g * kFewWords + k, a.words - 1)) * a.ld_w;     // (beyond the last word: that again)
         float s[kSums];
 #pragma unroll
         for (int i = 0; i < kSums; ++i) s[i] = 0.f;
@@ -1267,11 +1290,24 @@ __global__ void __launch_bounds__(kFewThreads, R <= 2 ? 4 : 2) loss_few_kernel(c
 #pragma unroll
         for (int o = (1 << kSkip) >> 1; o > 0; o >>= 1) s[0] += __shfl_xor_sync(0xffffffffu, s[0], o);
         const int v = g * kFewWords + word;
-        if (v < a.V) {
+        if constexpr (kG > 0) {
+            if (v < a.words && to >= 0 && (lane & ((1 << kSkip) - 1)) == 0) {
+                const float e = ptx::ex2(__fsub_rn(__fmul_rn(s[0], a.scale), lse) * kLossLog2e);
+                float q = (a.v0 + v == label ? e - 1.f : e) * gm;
+#pragma unroll
+                for (int h = 0; h < kG; ++h) {
+                    typename std::conditional<std::is_same<T, __half>::value, __half, __nv_bfloat16>::type t;
+                    from_f32(t, q);
+                    q -= to_f32(t);
+                    a.g[(h * a.cap + to) * a.ld_g + v] = *reinterpret_cast<const uint16_t *>(&t);
+                }
+            }
+        } else if (v < a.words) {
             stat = loss_both(stat, LossStat{s[0], 1.f}, c2);
             if (v == label && (lane & ((1 << kSkip) - 1)) == 0) a.chosen[row] = s[0];
         }
     }
+    if constexpr (kG > 0) return;
     stats[warp][lane] = make_float2(stat.m, stat.l);
     __syncthreads();
     if ((int)threadIdx.x < a.rows) {

@@ -428,7 +428,8 @@ int flare_embed_backward(const flare_embed_desc_t *desc, const flare_drop_t *dro
  * be NULL if not wanted.  Products run on the tensor cores with float32 sums, and p is formed from the same logits forward and backward.  No row or word is held in fewer bits for what
  * another holds, but for dw in float16 with dloss:
  * float16: x and w as they are, p - [v = labels[n]] (times what dloss[n] is beyond a power of two, if given) rounded to float16 times 2^15 (2^14); x times that power of two, for dw, held down to 2^-39 of the largest.
- * bfloat16: x and w as they are, p - [v = labels[n]] (times dloss[n], if given) rounded to bfloat16, over up to 8192 words with vocab x width up to 2^22 to two bfloat16 values (2^-17).
+ * bfloat16: x and w as they are, p - [v = labels[n]] (times dloss[n], if given) rounded to bfloat16.
+ * Either, up to 256 rows, or up to 8192 words with vocab x width up to 2^22: p - [v = labels[n]] to two such values.
  * float32: three bfloat16 values each, which hold all 24 bits; products to 2^-24.
  * A wait inside the kernels that gave up is reported by flare_check(workspace).
  */

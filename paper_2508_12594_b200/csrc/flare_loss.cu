@@ -48,13 +48,14 @@ int tile_width(long row_tiles, long words, int pairs) {
 LossPlan loss_plan(const flare_loss_desc_t *d, int sms, bool backward) {
     LossPlan p{};
     const bool f32 = d->dtype == FLARE_DTYPE_F32;
-    // G in one bfloat16 value is off by 2^-9: gradients by 1.06 times what rounding exact ones gives, 1.35 times where every row has its own dloss.  In two values they are as good as rounded exact ones, for twice
-    // the products of the gradients and G's bytes: 131072 rows over 256 words, C = 128: 153 us a step (one value: 112); 2000 over 4096, C = 1024: 118 (93); 8192 over 8000, C = 512: 385 (266); 16384 over 32000,
-    // C = 128: 1466 (892).  So of vocabularies where that is a third or less, as if W were small.
-    const bool bf16_small = d->dtype == FLARE_DTYPE_BF16 && backward && d->vocab <= 8192 && (long)d->vocab * d->width <= (4L << 20);
+    // G in one 16-bit value is off by 2^-9 (2^-12): gradients by 1.06 times what rounding exact ones gives, 1.3 to 1.45 times where every row has its own dloss, or of few words, where a label's p is not next to 0; of few
+    // rows, whose rounding does not average out, up to 1.76 times.  In two values they are as good as rounded exact ones, for twice the products of the gradients and G's bytes: bfloat16, 131072 rows over 256 words,
+    // C = 128: 153 us a step (one value: 112); 2000 over 4096, C = 1024: 118 (93); 8192 over 8000, C = 512: 385 (266); 16384 over 32000, C = 128: 1466 (892); 64 over 32000, C = 1024: 146 (111).  So of one tile of
+    // rows, and of vocabularies where it is a third or less, as if W were small.
+    const bool two = !f32 && backward && (d->rows <= 256 || (d->vocab <= 8192 && (long)d->vocab * d->width <= (4L << 20)));
     p.bf16 = d->dtype != FLARE_DTYPE_F16;
     p.planes = f32 ? 3 : 1;
-    p.g_planes = f32 ? 3 : bf16_small ? 2 : 1;
+    p.g_planes = f32 ? 3 : two ? 2 : 1;
     // rows of packed X and W: whole 16 bytes, of wide ones whole lines (TMA takes 128-byte pieces of them)
     p.Cp = d->width > 256 ? (d->width + 63) / 64 * 64 : (d->width + 7) / 8 * 8;
     p.chunks = (int)((d->rows + kLossChunk - 1) / kLossChunk);
@@ -197,7 +198,7 @@ int launch_few_of(const LossFew &f, int R, int blocks, cudaStream_t st) {
 int launch_few(const LossFew &f, int dtype, int g_planes, int R, int blocks, cudaStream_t st) {
     auto launch = dtype == FLARE_DTYPE_F32    ? (g_planes ? launch_few_of<float, 3> : launch_few_of<float, 0>)
                   : dtype == FLARE_DTYPE_BF16 ? (g_planes == 2 ? launch_few_of<__nv_bfloat16, 2> : g_planes ? launch_few_of<__nv_bfloat16, 1> : launch_few_of<__nv_bfloat16, 0>)
-                                              : (g_planes ? launch_few_of<__half, 1> : launch_few_of<__half, 0>);
+                                              : (g_planes == 2 ? launch_few_of<__half, 2> : g_planes ? launch_few_of<__half, 1> : launch_few_of<__half, 0>);
     return launch(f, R, blocks, st);
 }
 LossFew few_args(const flare_loss_desc_t *d, const LossPlan &p, const void *x, const void *w, const void *labels) {
@@ -369,7 +370,9 @@ int flare_loss_backward(const flare_loss_desc_t *desc, const void *x, const void
     a.dw_factor = k.g_factor != 0.f ? k.mult / k.g_factor : 1.f;
     a.acc = reinterpret_cast<float *>(ws + l.acc); a.slots = reinterpret_cast<float *>(ws + l.slots);
     auto weights = f32 ? launch_loss<kLossWeights, 3, 3, float> : p.g_planes == 2 ? launch_loss<kLossWeights, 1, 2, float> : launch_loss<kLossWeights, 1, 1, float>;
-    auto grads = f32 ? launch_loss<kLossGrads, 3, 3, float> : !bf16 ? launch_loss<kLossGrads, 1, 1, __half> : p.g_planes == 2 ? launch_loss<kLossGrads, 1, 2, __nv_bfloat16> : launch_loss<kLossGrads, 1, 1, __nv_bfloat16>;
+    auto grads = f32 ? launch_loss<kLossGrads, 3, 3, float>
+                 : bf16 ? (p.g_planes == 2 ? launch_loss<kLossGrads, 1, 2, __nv_bfloat16> : launch_loss<kLossGrads, 1, 1, __nv_bfloat16>)
+                        : (p.g_planes == 2 ? launch_loss<kLossGrads, 1, 2, __half> : launch_loss<kLossGrads, 1, 1, __half>);
     auto *join = f32 ? loss_join_kernel<float> : desc->dtype == FLARE_DTYPE_BF16 ? loss_join_kernel<__nv_bfloat16> : loss_join_kernel<__half>;
     // few rows: G by the kernel that the forward's statistics are of
     const int R = few_rows_of(desc, loss_lies(desc, false, aligned16(x), aligned16(w)));

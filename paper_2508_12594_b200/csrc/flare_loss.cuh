@@ -17,10 +17,10 @@
 // that a tile's end runs under the next tile's products.  It is bound by the tensor pipe.
 //
 // bfloat16 and float16 are multiplied as they are, G in the same type, rounded once.  bfloat16's G is q where one dloss is that of all rows (next to a label q is next to -1, which is no rounding), else dloss scale q
-// (2^-9, as the gradients themselves will be; dloss in a second X instead put the same rounding there, and as many more elements were moved); of a small vocabulary it is two bfloat16 values (2^-17), two products of
-// either gradient.  float16's G is q times 2^15, so that probabilities down to 2^-29 are
+// (2^-9, as the gradients themselves will be; dloss in a second X instead put the same rounding there, and as many more elements were moved).  float16's G is q times 2^15, so that probabilities down to 2^-29 are
 // normal numbers; of a row's own dloss its mantissa is there too (q times 2^14 and up to 2) and its power of two in dX's rows and in a second X, times one more that puts the largest element of that just
 // below 2^15: elements of x times dloss are held down to 2^-39 of the largest of them.
+// Of a small vocabulary or of few rows G is two values of the type (2^-17, 2^-23), two products of either gradient.
 // float32: X, W, G as three bfloat16 values each, which hold all 24 bits over all of float32's range, a product as the six of them that are above 2^-24 of it; sums leave tensor memory, which
 // truncates, every 64 of K to be added up in registers.  (Two float16 halves, 22 bits, take three products, but want one power of two for all of X, of W and of a row's dloss: an element
 // of 1e9 in one row put the others' losses off by 3e-3, one of 1e13 by 4.)
@@ -900,7 +900,7 @@ __device__ __forceinline__ void loss_weights(uint32_t piece, const LossArgs &a, 
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     float &x = v[k + 8 * e + 2 * i], &y = v[k + 8 * e + 2 * i + 1];
-                    if (kG > 1 || a.bf16) {
+                    if (kG == 3 || a.bf16) {
                         w[i] = ptx::pack_bf16(x, y);
                         if (h + 1 < kG) {                                 // (what is left is the next one's)
                             x -= __uint_as_float(w[i] << 16);
@@ -909,18 +909,25 @@ __device__ __forceinline__ void loss_weights(uint32_t piece, const LossArgs &a, 
                     } else {
                         const __half2 t = __floats2half2_rn(x, y);
                         w[i] = *reinterpret_cast<const uint32_t *>(&t);
+                        if (h + 1 < kG) {
+                            const float2 b = __half22float2(t);
+                            x -= b.x;
+                            y -= b.y;
+                        }
                     }
                 }
                 ptx::sts128(piece + piece_at(lane, e), w);
             }
             if (mine && (at & ~31) == k) {
                 uint16_t bits;
-                if (kG > 1 || a.bf16) {
+                if (kG == 3 || a.bf16) {
                     const __nv_bfloat16 t = __float2bfloat16_rn(own);
                     bits = __bfloat16_as_ushort(t);
                     own -= __bfloat162float(t);
                 } else {
-                    bits = __half_as_ushort(__float2half_rn(own));
+                    const __half t = __float2half_rn(own);
+                    bits = __half_as_ushort(t);
+                    own -= __half2float(t);
                 }
                 asm volatile("st.shared.b16 [%0], %1;" ::"r"(piece + piece_at(lane, at >> 3 & 3) + (at & 7) * 2), "h"(bits) : "memory");
             }

@@ -49,9 +49,9 @@ class Reference:
         q = p.scatter_add(1, at, -torch.ones_like(self.lse)[:, None])
         g = torch.where(there, dloss if isinstance(dloss, torch.Tensor) else torch.full_like(self.lse, dloss), 0.0).double() * scale
         self.dx, self.dw = g[:, None] * (q @ w), (g[:, None] * q).T @ x
-        # q: of p, of its difference from the label's 1, of its rounding: 24 bits (float32), two bfloat16 values' (bfloat16 over up to 8192 words, w of up to 2^22 elements), one's, or float16's and 2^-39
-        two = T == BF16 and V <= 8192 and V * C <= 1 << 22
-        u = U32 if T == F32 else 2.0 ** -17 if two else UNIT[T]
+        # q: of p, of its difference from the label's 1, of its rounding: 24 bits (float32), two 16-bit values' (up to 256 rows, or up to 8192 words and w of up to 2^22 elements), or one's, float16's down to 2^-39
+        two = T != F32 and (n <= 256 or (V <= 8192 and V * C <= 1 << 22))
+        u = U32 if T == F32 else 2 * (UNIT[T] / 2) ** 2 if two else UNIT[T]
         eps = (size + self.lse_bound + 2.0 ** -21 + 42 * U32)[:, None] * p + 2 * U32 * (q.abs() + p)
         dq = (eps + q.abs() * u + (2.0 ** -39 if T == F16 else 0.0)) * there[:, None]
         q, products = q.abs() * there[:, None], 2 if two else 1
@@ -176,7 +176,7 @@ def test_sizes_near_either_end(rows, vocab, width, dtype, size):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16, F16], ids=str)
-@pytest.mark.parametrize("rows,vocab,width", [(300, 500, 80), (600, 5003, 136)])
+@pytest.mark.parametrize("rows,vocab,width", [(300, 500, 80), (600, 5003, 136), (200, 20000, 264), (2, 9000, 520), (7, 9000, 261)])
 def test_results_to_their_types_rounding(rows, vocab, width, dtype):
     """What q is held in, 16 bits in bfloat16 (w up to 2^22 elements), shows in the gradients."""
     x, w, labels, g = problem(rows, vocab, width, dtype)
@@ -250,8 +250,8 @@ def test_rows_that_have_learned_their_label(dtype, rows, vocab, width):
     size = (xd.abs() @ wd.abs().T).max(1, keepdim=True).values * E
     share = 2 * size + (128 + vocab / 2048 + 80) * U32 + 2.0 ** -20
     whole = 4 * U32 * (r.lse[:, None].abs() + l.abs() + 1)
-    two = dtype == BF16 and vocab <= 8192 and vocab * width <= 1 << 22
-    u = U32 if dtype == F32 else 2.0 ** -17 if two else UNIT[dtype]
+    two = dtype != F32                                       # (vocab x width up to 2^22)
+    u = U32 if dtype == F32 else 2 * (UNIT[dtype] / 2) ** 2 if two else UNIT[dtype]
     dq = others * (share + whole)
     dq.scatter_(1, at, one * share + whole.gather(1, at) + 2.0 ** -21)
     dq += q.abs() * u + (2.0 ** -39 if dtype == F16 else 0.0)

@@ -871,10 +871,10 @@ __device__ __forceinline__ void loss_weights(uint32_t piece, const LossArgs &a, 
     const int at = r.label - col0;                                       // (no label: below zero)
     const float lse = r.lse, f = r.coef;
     const int words = in ? a.V - col0 : 0;
-    // the label's, where it is among the columns: put into the piece on its own
+    // the label's, where it is among the columns: put into the piece on its own (p - 1 in one function: of a row that has learned its label ex2's error would be most of it)
     const bool mine = at >= 0 && at < cols;
     float own = 0.f;
-    if (__any_sync(0xffffffffu, mine)) own = (ptx::ex2(__fsub_rn(__fmul_rn(loss_pick(v, at), scale), lse) * kLossLog2e) - 1.f) * f;
+    if (__any_sync(0xffffffffu, mine)) own = expm1f(__fsub_rn(__fmul_rn(loss_pick(v, at), scale), lse)) * f;
 #pragma unroll
     for (int k = 0; k < 64; k += 32) {
         if (k >= cols) break;
@@ -1299,8 +1299,8 @@ __global__ void __launch_bounds__(kFewThreads, R <= 2 ? 4 : 2) loss_few_kernel(c
         const int v = g * kFewWords + word;
         if constexpr (kG > 0) {
             if (v < a.words && to >= 0 && (lane & ((1 << kSkip) - 1)) == 0) {
-                const float e = ptx::ex2(__fsub_rn(__fmul_rn(s[0], a.scale), lse) * kLossLog2e);
-                float q = (a.v0 + v == label ? e - 1.f : e) * gm;
+                const float d = __fsub_rn(__fmul_rn(s[0], a.scale), lse);
+                float q = (a.v0 + v == label ? expm1f(d) : ptx::ex2(d * kLossLog2e)) * gm;
 #pragma unroll
                 for (int h = 0; h < kG; ++h) {
                     typename std::conditional<std::is_same<T, __half>::value, __half, __nv_bfloat16>::type t;

@@ -40,7 +40,7 @@ struct LossPlan {
     int grad_width, tiles_c;
 };
 // Columns of a tile of X W^T.  Tiles of 128 take some 0.6 of the time of one of 256 (they read as many rows), which pays where they fill the last
-// round of pairs better: 1000 rows over 5000 words of 256, forward and backward, 60.9 us, with 256 columns 62.4; 256 rows over 32000 words of 1024 28.0 us, with 256 columns 23.9.
+// round of pairs better: 1000 rows over 5000 words of 256, forward and backward, 60.7 us, with 256 columns 62.3; forward of 256 rows over 32000 words of 1024 28.0 us, with 256 columns 19.2.
 int tile_width(long row_tiles, long words, int pairs) {
     const long wide = row_tiles * ((words + 255) / 256), narrow = row_tiles * ((words + 127) / 128);
     return 0.6 * (double)((narrow + pairs - 1) / pairs) < (double)((wide + pairs - 1) / pairs) ? 128 : 256;
@@ -67,7 +67,7 @@ LossPlan loss_plan(const flare_loss_desc_t *d, int sms, bool backward) {
     p.pieces = (int)((words + most - 1) / most);
     p.Vp = (int)((words / 256 + p.pieces - 1) / p.pieces * 256);
     p.pieces = (int)((words + p.Vp - 1) / p.Vp);
-    // (a width that 256 does not divide well is worked off in 128s, which take 0.6 each: 8192 rows over 32000 words, C = 128: 497 us, with 256 columns 517; C = 256: 726, with 256 columns 604)
+    // (a width that 256 does not divide well is worked off in 128s, which take 0.6 each: 8192 rows over 32000 words, C = 128: 502 us, with 256 columns 517; C = 256: 726, with 256 columns 622)
     p.grad_width = 1.2 * ((d->width + 127) / 128) < 2.0 * ((d->width + 255) / 256) ? 128 : 256;
     p.tiles_c = (d->width + p.grad_width - 1) / p.grad_width;
     return p;
@@ -89,12 +89,13 @@ long row_stride(int64_t stride, int width) { return stride ? stride : width; }
 LossLies loss_lies(const flare_loss_desc_t *d, bool backward, bool x_aligned, bool w_aligned) {
     if (d->dtype == FLARE_DTYPE_F32) return LossLies{false, false};
     const bool w = w_aligned && row_stride(d->stride_w, d->width) % 8 == 0, x = x_aligned && row_stride(d->stride_x, d->width) % 8 == 0;
-    // X too without packing, where all rows are one tile's (64 rows over 32000 words of 1024 take 20.3 us, packed 24.4) or the vocabulary is so small that rows without a label cost less than
-    // another pass over X: with 0.3 of them, 20000 rows over 1000 words of 512 24.0 us, packed 31.5; 40000 over 2025 of 64 46.4 and 43.3 (all labelled: 40.0 and 46.4)
+    // X too without packing, where all rows are one tile's (64 rows over 32000 words of 1024 take 20.3 us, packed 24.4) or the vocabulary is so small that another pass over X costs more than most rows without a label
+    // do, whose share is known to the device alone: 131072 rows over 256 words of 128 take 22.9 us whatever it is, packed 30.1 with 0.1 of them, 25.4 with 0.3, 21.9 with 0.5, 17.4 with 0.85; 20000 over 1000 of 512
+    // 21.1 and 30.4, 27.1, 26.0, 19.9
     return LossLies{w, !backward && w && x && (d->rows <= 256 || d->vocab <= 2048)};
 }
-// Rows that loss_few_kernel is run for, 0: it is not.  (Five to eight rows that need no packing are done sooner by the tensor cores: 8 rows over 32000 words of 1024 in bfloat16 in 26 us instead of 32.6, where four take
-// 23.2 and 22.0, one 26.4 and 16.6; of 1001, which are packed, eight take 54 and 36.5; in float32, of 2048, 220 and 72.)
+// Rows that loss_few_kernel is run for, 0: it is not.  (Five to eight rows that need no packing are done sooner by the tensor cores: 8 rows over 32000 words of 1024 in bfloat16 in 23 us instead of 32.6, where four take
+// 25.7 and 22.0, two 23.7 and 20.2, one 26.2 and 16.5; of 1001, which are packed, eight take 54 and 36.6; in float32, of 2048, 240 and 73.)
 int few_rows_of(const flare_loss_desc_t *d, LossLies lies) { return lies.x && d->rows > 4 ? 0 : few_rows(d); }
 LossLayout loss_layout(const flare_loss_desc_t *d, const LossPlan &p, bool backward, LossLies lies) {
     const bool few = !backward && few_rows_of(d, lies) > 0;   // (nothing is packed)

@@ -5,13 +5,13 @@
 //
 // Four matrix products of rows x width x vocabulary (X W^T forward, X W^T again, G^T X and G W backward), of which the logits would be the largest
 // matrix by far: 2.1 GB in bfloat16 for 8192 rows and 128256 words, where X and W are 17 and 263 MB.  Forward they stay in tensor memory: a tile's end takes
-// them from there to a maximum and a sum of exponentials per row.  Backward they are formed again, a piece of the vocabulary at a time: G, the piece of q in 16
-// bits, is written to scratch (bounded), and one launch takes both products from it.  The fourth product is what keeping no logits costs.
+// them from there to a maximum and a sum of exponentials per row.  Backward they are formed again, a piece of the vocabulary at a time: G, the piece of q in one to
+// three values of 16 bits, is written to scratch (bounded), and one launch takes both products from it.  The fourth product is what keeping no logits costs.
 //
 // Rows without a label are left out, not multiplied by zero: the rows that have one are packed, in their order, before anything else (loss_scan_kernel,
 // loss_pack_kernel), their number stays on the device, and all products run over packed rows.  So a padded batch takes the time of its labelled rows, and
 // nothing that stands in the others can reach a gradient.  The pass costs two bytes in and out per element of X, and leaves rows that TMA can take whatever stride and alignment X has.
-// (Up to 256 rows that lie well are scored as they stand.)
+// (Rows of 16 bits that lie well are scored as they stand where they are up to 256, or of any number over up to 2048 words.)
 //
 // Every product is the same kernel (loss_kernel): pairs of blocks, tiles of 256 x 256 (or 256 x 128), operands by TMA, sums in tensor memory twice over so
 // that a tile's end runs under the next tile's products.  It is bound by the tensor pipe.
@@ -185,7 +185,7 @@ struct LossPack {
     const void *labels, *x, *w;
     int wide;
     long rows, cap, ld_x, ld_w, w_rows;       // cap: rows up to whole tiles; w_rows: of W to be packed too (0: it is taken as it stands)
-    int C, Cp, V, chunks, pack_blocks, pack_rows;   // Cp: C up to a multiple of eight
+    int C, Cp, V, chunks, pack_blocks, pack_rows;   // Cp: C up to a multiple of eight, above 256 of 64
     const int *rank;                          // the scan's; null: there was none
     const LossChunk *chunk;
     const int *largest;                       // with pd: the scan's
@@ -205,7 +205,9 @@ struct LossPack {
     long ld_dx;
 };
 constexpr int kPackThreads = 256;             // of a block, which takes 4 to 1024 rows (of one chunk)
-constexpr int kPackAlone = 4096;              // rows up to which every block finds for itself, in all labels, what the scan would tell it, where there is no second X: a launch less (4096 rows over 5000 words of 256: forward 23.1 us, with it 25.3)
+// Rows up to which every block finds for itself, in all labels, what the scan would tell it, where there is no second X: a launch less, for a pass over all labels a block.  Forward over 5000 words of 256: 1000 rows
+// 14.3 us (with the scan 15.3), 4096 20.7 (21.9), 8192 28.5 (28.7), 16384 47.4 (43.9).
+constexpr int kPackAlone = 4096;
 
 // What the products multiply: the type as it is; float32 as three bfloat16 values, each what rounding to those before it has left.
 template <typename T> constexpr int kPacked = sizeof(T) == 4 ? 3 : 1;
@@ -422,7 +424,7 @@ struct LossArgs {
     int v0, words;               // the piece of the vocabulary: from v0 on
     int width, tiles_v;          // X W^T: columns of a tile, tiles across
     const int *label, *index;
-    // X as it stands, all of its rows (a single tile of them, where packing would save none): labels as they stand, and how many rows
+    // X as it stands, all of its rows (up to 256, or over a small vocabulary): labels as they stand, and how many rows
     const void *labels;
     int wide, direct;
     __device__ __forceinline__ int label_of(int row) const {
@@ -455,7 +457,7 @@ struct LossArgs {
 // or 24 of them: 1999 rows of 200 over 10007 words, 40 tiles of 29 steps and 8 of 157, took 18 us to join with all 48 shared.
 // Equal shares begin anywhere along K, so that no two pairs read the same lines of G and W at a time: of a G of half a gigabyte a step then takes half as long again (4096 rows over 64000 words of 1024, the tiles
 // of dX shared: 885 us and 4.4 GB read; a pair each, on 64 of 74 pairs: 740 us).  Shares of tiles of few steps
-// have many ends (17 rows over 67126 words of 83, forward and backward: 14 tiles of dW for each of three pairs, 156 us; a pair each 84).
+// have many ends (17 rows over 67126 words of 83, forward and backward: 14 tiles of dW for each of three pairs, 156 us; a pair each 84; both with G in one value).
 struct LossSplit {
     int tiles_w, tiles_x, deep_w, deep_x, full_w, full_x, pairs;
     int whole_w, whole_x;        // tiles of the last rounds that a pair each takes whole: the first pairs those of dW, the next those of dX
@@ -823,7 +825,7 @@ __device__ __forceinline__ bool loss_stats(LossPipe &q, const LossArgs &a, const
     return true;
 }
 // Tiles in turn by two sets of eight warps, half of the columns each in two steps, where one set of sums is all there is (up to 512 columns of 16 bits): then the sums come quicker than a tile's end, and with all warps
-// at the same tile, which wait for one another, the special-function units rest while the others' maxima, labels and joins are formed (131072 rows of 128 over 256 words: 25 us then, 20 in turns).
+// at the same tile, which wait for one another, the special-function units rest while the others' maxima, labels and joins are formed (forward of 131072 rows of 128 over 256 words: 27.4 us then, 22.9 in turns; of 37137 over 25943: 409 and 334).
 __device__ __forceinline__ bool loss_stats_by_turns(LossPipe &q, const LossArgs &a, const LossUnit &u, const LossRow &r, float scale, int rows, int row, float2 *joint) {
     const float c2 = scale * kLossLog2e;
     const int warp = ptx::warp_index(), part = (warp - 4) >> 2, set = part >> 1, half = part & 1, local = (warp & 3) * 32 + (threadIdx.x & 31), cols = a.width / 2;
@@ -940,8 +942,8 @@ __device__ __forceinline__ void loss_weights(uint32_t piece, const LossArgs &a, 
 }
 
 // 32 rows (a row a lane, to go to row `to` of the output; -1: nowhere) of 32 columns from c0 on, times f, by way of shared memory: rows on 16-byte boundaries by four lanes, 64 bytes a row and instruction (32 took
-// twice the time, which bounds gradients with few steps a tile: 18935 rows of 1536 over six words); others by lanes with neighbouring columns, a row at a time, eight rows' loads before their stores (3159 rows of 2373 over 23 words,
-// forward and backward: 162 us one by one, 93 so).
+// twice the time, which bounds gradients with few steps a tile: 18935 rows of 1536 over six words, G in one value); others by lanes with neighbouring columns, a row at a time, eight rows' loads before their stores (3159 rows of 2373 over 23 words,
+// G in one value, forward and backward: 162 us one by one, 93 so).
 template <typename E>
 __device__ __forceinline__ void loss_out(uint32_t piece, E *out, long ld, int vec, int to, int c0, int C, float f, const float *v) {
     const int lane = threadIdx.x & 31;
@@ -1047,7 +1049,7 @@ __global__ void __launch_bounds__(kLossThreads, 1) loss_kernel(const __grid_cons
     const int warp = ptx::warp_index(), pair = (int)(blockIdx.x >> 1), pairs = (int)(gridDim.x >> 1), in_pair = (int)(blockIdx.x & 1);
     const LossInfo info = loss_forward(kKind) && a.direct ? LossInfo{(uint32_t)a.direct, 1.f} : *a.info;
     const int rows = (int)info.rows;
-    // Registers of the launch, 640 x 96, as 128 x 40 (the loading and the issuing warp, two that idle) and 512 x 104.  Sixteen result warps with a quarter of the columns each: with eight and half of them, which
+    // Registers of the launch, 640 x 96 (every form's: the split counts on it), as 128 x 40 (the loading and the issuing warp, two that idle) and 512 x 104.  Sixteen result warps with a quarter of the columns each: with eight and half of them, which
     // had 168, their own chain of waits took as long as four products (37137 rows of 128 over 25943 words: 469 us).
     if (warp == 0) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");

@@ -396,7 +396,7 @@ __global__ void __launch_bounds__(kTokenThreads, kWidth == 2 && sizeof(T) + size
 // The sort: one cluster of blocks (up to 16 of 1024 threads), each a stretch of the tokens, each of its warps a stretch of that.  A pass over a digit of up to
 // ten bits: every warp counts its stretch, the counts before it are added up over the warps in shared memory and over the blocks through distributed shared memory, and
 // every warp puts its tokens where those say (lanes with the same digit find one another by a ballot a bit): in shared memory first, so that what goes to memory are stretches of
-// neighbours (up to kSortStaged tokens a block; beyond that as they come).  One launch, two barriers of the cluster a pass, where kernels of a count, a scan and a scatter each would be three launches a
+// neighbours (up to kSortStaged tokens a block, 64 KB beside the counts of ten bits; beyond that as they come: gradients of 131072 tokens of 16 columns over 256 words take 33.4 us, of 132000 33.9, over 32000 words 60.0 and 60.8).  One launch, two barriers of the cluster a pass, where kernels of a count, a scan and a scatter each would be three launches a
 // pass: 17 us for 131072 tokens in one pass and for 16396 in two, by latency.
 constexpr int kSortThreads = 1024, kSortBits = 10, kSortBatch = 4, kSortBlocks = 16;
 constexpr uint32_t kSortStaged = 8192;
@@ -681,7 +681,7 @@ __device__ __forceinline__ void add8(float (&v)[8], const float *from) {
 enum { kRunOpen = 1, kRunGoesOn = 2, kRunThrough = 4 };       // a chunk's first run began before it; its last one goes on behind it; the two are the same and all of it
 // Blocks of 128 threads where a row takes up to 16 of them, so that no SM waits for the last of few large ones, else of 256, where a block joins more chunks by itself (131072 rows of 256 over 32000 words: 84 us with
 // blocks of 64, 80 with 128 or 256; 65536 of 512: 92, 78, 74).  Chunks are 16 rows, longer where there is more to do: 16384 rows of 4096 take 186 us in chunks of 16, 144 of 64; 65536 of 512 over 256 words take 50.3 of 16,
-// 44.6 of 28; 131072 of 128 over 32000 take 65.6 of 16, 79.5 of 32.  It is bound by instructions: 32 x 4096 rows of 128 over 256 words with positions take 41 us in all, 17 of them the sort.
+// 44.6 of 28; 131072 of 128 over 32000 take 65.6 of 16, 79.5 of 32.  It is bound by instructions: 32 x 4096 rows of 128 over 256 words with positions take 42 to 45 us in all, 17 to 20 of them the sort.
 constexpr int kSumThreads = 256;
 __host__ __device__ constexpr size_t sum_smem(uint32_t threads, int width) { return threads * (size_t)(2 * 32 * width + 8); }
 // kWidth: groups of eight columns next to each other that a thread adds up (two share what there is to know of a row: 167 instructions a group and row became 108; of 1024 columns 50.5 us against 54.7 for 16384 rows, but of 128 columns 72 against 64 for 131072: rows need 32 such threads), 0: one, off 16-byte boundaries.

@@ -195,11 +195,11 @@ int launch_few_of(const LossFew &f, int R, int blocks, cudaStream_t st) {
                            : (vec ? launch_few_as<T, 8, true, kG> : launch_few_as<T, 8, false, kG>);
     return launch(f, blocks, st);
 }
-// g_planes: of G, 0: forward
-int launch_few(const LossFew &f, int dtype, int g_planes, int R, int blocks, cudaStream_t st) {
-    auto launch = dtype == FLARE_DTYPE_F32    ? (g_planes ? launch_few_of<float, 3> : launch_few_of<float, 0>)
-                  : dtype == FLARE_DTYPE_BF16 ? (g_planes == 2 ? launch_few_of<__nv_bfloat16, 2> : g_planes ? launch_few_of<__nv_bfloat16, 1> : launch_few_of<__nv_bfloat16, 0>)
-                                              : (g_planes == 2 ? launch_few_of<__half, 2> : g_planes ? launch_few_of<__half, 1> : launch_few_of<__half, 0>);
+// (G of few rows is three or two values: loss_plan)
+int launch_few(const LossFew &f, int dtype, bool backward, int R, int blocks, cudaStream_t st) {
+    auto launch = dtype == FLARE_DTYPE_F32    ? (backward ? launch_few_of<float, 3> : launch_few_of<float, 0>)
+                  : dtype == FLARE_DTYPE_BF16 ? (backward ? launch_few_of<__nv_bfloat16, 2> : launch_few_of<__nv_bfloat16, 0>)
+                                              : (backward ? launch_few_of<__half, 2> : launch_few_of<__half, 0>);
     return launch(f, R, blocks, st);
 }
 LossFew few_args(const flare_loss_desc_t *d, const LossPlan &p, const void *x, const void *w, const void *labels) {
@@ -293,7 +293,7 @@ int flare_loss_forward(const flare_loss_desc_t *desc, const void *x, const void 
         LossFew f = few_args(desc, p, x, w, labels);
         f.part = reinterpret_cast<float2 *>(ws + l.part); f.chosen = reinterpret_cast<float *>(ws + l.chosen);
         const int blocks = few_blocks(desc, desc->vocab, 2 * p.pairs);
-        if (int rc = launch_few(f, desc->dtype, 0, R, blocks, st)) return rc;
+        if (int rc = launch_few(f, desc->dtype, false, R, blocks, st)) return rc;
         LossMerge m{};
         m.part = f.part; m.chosen = f.chosen; m.cap = p.cap; m.parts = blocks; m.loss = loss; m.lse = lse;
         m.labels = labels; m.wide = f.wide; m.V = f.V; m.direct = f.rows; m.status = reinterpret_cast<uint32_t *>(ws); m.scale = desc->scale;
@@ -389,7 +389,7 @@ int flare_loss_backward(const flare_loss_desc_t *desc, const void *x, const void
         a.tiles_v = (a.words + a.width - 1) / a.width;
         if (R) {
             few.v0 = a.v0; few.words = a.words;
-            if ((rc = launch_few(few, desc->dtype, p.g_planes, R, few_blocks(desc, a.words, 2 * p.pairs), st)) != FLARE_OK) return rc;
+            if ((rc = launch_few(few, desc->dtype, true, R, few_blocks(desc, a.words, 2 * p.pairs), st)) != FLARE_OK) return rc;
         } else if ((rc = weights(maps, a, (int)std::min<long>(p.pairs, p.cap / 256 * a.tiles_v), st)) != FLARE_OK) {
             return rc;
         }
